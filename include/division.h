@@ -353,6 +353,71 @@ float division_block_mean_rule(double block_sum, uint32_t count, int *divided);
 float division_block_mean_rule_rcp(double block_sum, uint32_t count, double reciprocal, int *divided);
 double division_count_reciprocal(uint32_t count, double estimate);
 
+/*
+ * Operators of a token model's training step beside its matrix products.  T rows of D elements of type dt (DIVISION_F32 or
+ * DIVISION_BF16), each row's elements next to one another, rows `stride` elements apart (any stride from 0 up, also 0: every row the same);
+ * outputs are dense.  All statistics, sums and scales are fp32 or more.  T == 0 is a call without rows.  Pointers are device pointers aligned to
+ * their elements; T and D up to 2^31-1, T*D and T*stride up to 2^40 (DIVISION_ERANGE).  Results do not depend on the launch geometry of another
+ * call or on timing: the same call gives the same bits.
+ *
+ * Codes of 8 bits: a group of a row's columns (32, 64 or 128 of them, the last group of a row what is left; or the row: group = 0) has one fp32
+ * scale.  With a = the group's largest magnitude and Q = 127 (INT8, two's complement) or 448 (E4M3: 4 bits of exponent, 3 of mantissa, no
+ * infinities): scale = a / Q, code = y * Q / a rounded to nearest even, value = code * scale.  A group with a < 2^-90 has scale 0 and codes 0, one
+ * that holds a NaN or an infinity has scale NaN and codes 0 (its values read back as NaN).  scales is [T][groups], groups = ceil(D / group) or 1.
+ */
+typedef enum { DIVISION_CODE_NONE = 0, DIVISION_CODE_INT8 = 1, DIVISION_CODE_E4M3 = 2 } division_code;
+
+/*
+ * Root-mean-square norm, with the residual stream's addition before it and an output in 8 bits behind it:
+ *   s = x + residual (x where residual is null),  rstd = 1 / sqrt(mean of s^2 over the row + eps),  y = s * rstd * weight,
+ * s and y in fp32; `sum` receives s rounded to dt, `y` y rounded to dt, the codes are y's own (not of the rounded y).
+ *   sum     required with a residual (may be x or residual itself where that is dense), unused without one
+ *   y       may be null (only codes are wanted)
+ *   rstd    [T], may be null
+ *   codes   [T][D] bytes and scales, where code is not DIVISION_CODE_NONE
+ */
+typedef struct division_norm {
+    const void *x, *residual, *weight;
+    int64_t x_stride, residual_stride;
+    int64_t T, D;
+    division_dtype dt, weight_dt;
+    float eps;
+    void *sum, *y;
+    float *rstd;
+    division_code code;
+    int group;
+    void *codes;
+    float *scales;
+} division_norm;
+
+int division_rms_norm(const division_norm *norm, void *hip_stream);
+
+/* The values of codes that division_rms_norm wrote: out [T][D] of type dt. */
+int division_read_codes(const void *codes, const float *scales, int64_t T, int64_t D, division_code code, int group,
+                        division_dtype dt, void *out, void *hip_stream);
+
+/*
+ * Its backward pass.  grad_y: the gradient of y (or of the codes' values), sum: s as stored (x where there was no residual), rstd as
+ * written by the forward call, grad_sum: the gradient that reaches `sum` by other ways (null: none).
+ *   grad_x       [T][D] of type dt: the gradient of x, and of the residual; may be grad_y, sum or grad_sum itself where that is dense
+ *   grad_weight  [D] of type weight_dt: the sum over all rows, in an order that T and D alone decide (zeros for T == 0)
+ *   workspace    division_rms_norm_backward_workspace(T, D) bytes
+ */
+typedef struct division_norm_back {
+    const void *grad_y, *sum, *grad_sum, *weight;
+    const float *rstd;
+    int64_t grad_y_stride, sum_stride, grad_sum_stride;
+    int64_t T, D;
+    division_dtype dt, weight_dt;
+    void *grad_x, *grad_weight;
+    void *workspace;
+    size_t workspace_bytes;
+} division_norm_back;
+
+size_t division_rms_norm_backward_workspace(int64_t T, int64_t D);
+
+int division_rms_norm_backward(const division_norm_back *norm, void *hip_stream);
+
 /* Version of this ABI (host-only): DIVISION_ABI_VERSION of the header that the library was built with. */
 #define DIVISION_ABI_VERSION 1
 int division_abi_version(void);

@@ -1,8 +1,8 @@
 """Builds libdivision.so (HIP kernels + C ABI) for gfx950 with hipcc, in-tree.
 
 division.hip (with the kernel families and the host side in the .h fragments it includes) instantiates
-its kernels once per element / cache type; it is compiled as three translation units (-DDIVISION_PART=0, 1, 2: float, bfloat16, bfloat16-cached float) beside masks.hip,
-all four in parallel, and the objects are linked into the one library.
+its kernels once per element / cache type; it is compiled as three translation units (-DDIVISION_PART=0, 1, 2: float, bfloat16, bfloat16-cached float) beside masks.hip and the operators
+of a token model's step (norm.hip), all in parallel, and the objects are linked into the one library.
 """
 from __future__ import annotations
 
@@ -16,7 +16,8 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 DIVISION = PKG / "csrc" / "division.hip"
 MASKS = PKG / "csrc" / "masks.hip"
-SRCS = [DIVISION, MASKS]
+NORM = PKG / "csrc" / "norm.hip"
+SRCS = [DIVISION, MASKS, NORM]
 LIB = PKG / "libdivision.so"
 CHECKS = PKG.parent / "tests" / "device_checks.hip"          # device helpers on their own, for the tests
 FASTCALL = PKG / "_fastcall.so"                              # imported by binding.py
@@ -31,6 +32,7 @@ UNITS = [
     ("division_bf16.o", DIVISION, ["-DDIVISION_PART=1"]),
     ("division_c16.o", DIVISION, ["-DDIVISION_PART=2"]),
     ("masks.o", MASKS, []),
+    ("norm.o", NORM, []),
 ]
 
 HIPCC_FLAGS = [

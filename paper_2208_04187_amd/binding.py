@@ -25,6 +25,10 @@ _LIB_PATH = Path(__file__).resolve().parent / "libdivision.so"
 _lib = None
 
 
+# Entries of the operators in operators.py: (name, argument types, result)
+OPERATOR_ENTRIES = []
+
+
 class DivisionError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what} failed: {ERRORS.get(code, code)}")
@@ -87,6 +91,9 @@ def lib() -> ctypes.CDLL:
         L.division_decompress_3d.argtypes = [vp, sz, i64, i64, i64, i64, i64, ci, ci, ci, vp, vp]
         L.division_kernel_name_3d.restype = ci
         L.division_kernel_name_3d.argtypes = [ci, vp, i64, i64, i64, i64, i64, ci, ci, ci, ctypes.c_char_p, sz]
+        for name, arguments, result in OPERATOR_ENTRIES:
+            entry = getattr(L, name)
+            entry.argtypes, entry.restype = arguments, result
         _lib = L
     return _lib
 

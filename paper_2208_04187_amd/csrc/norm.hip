@@ -1,0 +1,527 @@
+// Root-mean-square norm of token vectors for AMD MI355X (gfx950): forward with the residual's addition and an output in
+// 8 bits, the codes' values, backward.
+//
+//   s = x + residual;  rstd = (mean(s^2) + eps)^(-1/2);  y = s * rstd * w
+//   group of y:  a = max|y|;  scale = a / Q;  code = nearest(y * Q / a)          (Q = 127: int8, 448: e4m3)
+//   u = dy * w;  n = s * rstd;  dx = rstd * (u - n * mean(u * n)) + dsum;  dw = sum over rows of dy * n
+//
+// A row is held in the registers of the threads that share it, so it is read once; sums, statistics and scales are fp32.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <stddef.h>
+#include "../../include/division.h"
+
+namespace {
+#include "rows.h"
+
+constexpr float kTiny = 0x1p-90f;                          // a group whose largest value is smaller is held as zeros
+
+struct NormArgs {
+    const void *x, *residual;
+    const void* weight;
+    void *sum, *y;
+    float* rstd;
+    uint8_t* codes;
+    float* scales;
+    int64_t x_stride, residual_stride, T, D;
+    int64_t groups;                                         // scales of a row
+    float eps;
+    int code, group, shift;                                 // division_code; columns a scale (1 << shift), 0 = the row's
+    int weight_bf16;
+};
+
+template <typename C> __device__ __forceinline__ void load_weight(const void* weight, int is_bf16, C c, C D, float* w) {
+    if (is_bf16) {
+        const Piece<uint16_t> q = load_piece(static_cast<const uint16_t*>(weight), c, D);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = q[i];
+    } else {
+        const Piece<float> q = load_piece(static_cast<const float*>(weight), c, D);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = q[i];
+    }
+}
+
+// The codes of eight values of a group whose largest has these bits (without its sign).  A group that is not finite has scale NaN and
+// codes 0, one of next to nothing scale 0 and codes 0.
+struct Coded { uint32_t lo, hi; float scale; };
+__device__ __forceinline__ Coded code_piece(const float* v, uint32_t most_bits, int code) {
+    const float most = __uint_as_float(most_bits);
+    const bool finite = most_bits < 0x7f800000u, held = finite && most >= kTiny;
+    const float top = code == DIVISION_CODE_INT8 ? 127.0f : 448.0f;
+    const float inverse = top / most;
+    Coded r;
+    if (code == DIVISION_CODE_INT8) {
+        // rounded to nearest even by the addition of 1.5 * 2^23, whose last byte then holds the code
+        uint32_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = __float_as_uint(__builtin_fmaf(v[i], inverse, 12582912.0f)) & 0xffu;
+        r.lo = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+        r.hi = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
+    } else {
+        int lo = 0, hi = 0;
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inverse, v[1] * inverse, lo, false);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inverse, v[3] * inverse, lo, true);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * inverse, v[5] * inverse, hi, false);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * inverse, v[7] * inverse, hi, true);
+        r.lo = (uint32_t)lo;
+        r.hi = (uint32_t)hi;
+    }
+    if (!held) r.lo = r.hi = 0;
+    r.scale = !finite ? __uint_as_float(0x7fc00000u) : held ? most / top : 0.0f;
+    return r;
+}
+template <typename C> __device__ __forceinline__ void store_codes(uint8_t* row, C c, C D, const Coded& k) {
+    if (c + kPiece <= D) {
+        const u32x2 q = {k.lo, k.hi};
+        __builtin_memcpy(row + c, &q, 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (c + i < D) row[c + i] = (uint8_t)((i < 4 ? k.lo : k.hi) >> (i % 4 * 8));
+    }
+}
+__device__ __forceinline__ uint32_t most_of(const float* v) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = MaxU::of(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+}
+// the largest of a group of columns: 4, 8 or 16 neighbouring lanes of a piece each
+__device__ __forceinline__ uint32_t most_of_group(uint32_t m, int group) {
+    m = over_lanes<MaxU, 4>(m);
+    if (group >= 64) m = MaxU::of(m, dpp<kHalfMirror>(m));
+    if (group >= 128) m = MaxU::of(m, dpp<kMirror>(m));
+    return m;
+}
+
+// the scale of the group that starts with the piece at column c
+template <typename C> __device__ __forceinline__ void store_scale(const NormArgs& a, int64_t row, C c, C D, float scale) {
+    if (a.group == 0 ? c == 0 : c < D && (c & (a.group - 1)) == 0) a.scales[row * a.groups + (a.group ? c >> a.shift : 0)] = scale;
+}
+
+// s of the piece at column c
+template <typename T, bool RES, typename C> __device__ __forceinline__ void load_sum(const NormArgs& a, int64_t row, C c, C D, float* v) {
+    const Piece<T> q = load_piece(static_cast<const T*>(a.x) + row * a.x_stride, c, D);
+    if constexpr (RES) {
+        const Piece<T> p = load_piece(static_cast<const T*>(a.residual) + row * a.residual_stride, c, D);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = q[i] + p[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = q[i];
+    }
+}
+
+// A row per NT threads, R pieces each, NT * R * 8 >= D.
+template <typename T, int NT, int R, bool RES>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_rows(NormArgs a) {
+    constexpr int ROWS = NT < 256 ? 256 / NT : 1;
+    __shared__ uint32_t slots[NT > 64 ? 3 * (NT / 64) : 1];
+    const int lane = threadIdx.x % NT, D = (int)a.D;
+    float w[R][8];
+    int turn = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) load_weight(a.weight, a.weight_bf16, (r * NT + lane) * kPiece, D, w[r]);
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / NT; row < a.T; row += (int64_t)gridDim.x * ROWS) {
+        float v[R][8], sq = 0.0f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) load_sum<T, RES>(a, row, (r * NT + lane) * kPiece, D, v[r]);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sq = __builtin_fmaf(v[r][i], v[r][i], sq);
+        sq = row_sum<NT>(sq, slots + turn);
+        if constexpr (NT > 64) turn ^= NT / 64;
+        const float rstd = 1.0f / sqrtf(sq / (float)a.D + a.eps);
+        if (lane == 0 && a.rstd) a.rstd[row] = rstd;
+        uint32_t most = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int c = (r * NT + lane) * kPiece;
+            if constexpr (RES) store_piece(static_cast<T*>(a.sum) + row * a.D, c, D, v[r]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[r][i] = v[r][i] * rstd * w[r][i];
+            if (a.y) store_piece(static_cast<T*>(a.y) + row * a.D, c, D, v[r]);
+            most = MaxU::of(most, most_of(v[r]));
+        }
+        if (a.code == DIVISION_CODE_NONE) continue;
+        if (a.group == 0) most = over_row<MaxU, NT>(most, slots + (NT > 64 ? 2 * (NT / 64) : 0));
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int c = (r * NT + lane) * kPiece;
+            const uint32_t m = a.group == 0 ? most : most_of_group(most_of(v[r]), a.group);
+            const Coded k = code_piece(v[r], m, a.code);
+            store_codes(a.codes + row * a.D, c, D, k);
+            store_scale(a, row, c, D, k.scale);
+        }
+    }
+}
+
+// Rows too long for the registers: read twice (the second time from the caches where they hold it).  The largest |y| of the row is
+// that of |s * w| times rstd, which the first pass finds beside the sum.
+template <typename T, bool RES>
+__global__ __launch_bounds__(1024) void norm_wide(NormArgs a) {
+    __shared__ uint32_t slots[2 * 16];
+    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+        float sq = 0.0f;
+        uint32_t most = 0;
+        for (int64_t c = (int64_t)threadIdx.x * kPiece; c < a.D; c += 1024 * kPiece) {
+            float v[8], w[8];
+            load_sum<T, RES>(a, row, c, a.D, v);
+            load_weight(a.weight, a.weight_bf16, c, a.D, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sq = __builtin_fmaf(v[i], v[i], sq);
+                most = MaxU::of(most, __float_as_uint(v[i] * w[i]) & 0x7fffffffu);
+            }
+        }
+        sq = row_sum<1024>(sq, slots);
+        most = over_row<MaxU, 1024>(most, slots + 16);
+        const float rstd = 1.0f / sqrtf(sq / (float)a.D + a.eps);
+        most = __float_as_uint(__uint_as_float(most) * rstd);
+        if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+        for (int64_t c0 = 0; c0 < a.D; c0 += 1024 * kPiece) {          // every lane takes part in its group's maximum
+            const int64_t c = c0 + (int64_t)threadIdx.x * kPiece;
+            float v[8], w[8];
+            load_sum<T, RES>(a, row, c, a.D, v);
+            load_weight(a.weight, a.weight_bf16, c, a.D, w);
+            if constexpr (RES) store_piece(static_cast<T*>(a.sum) + row * a.D, c, a.D, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * w[i];
+            if (a.y) store_piece(static_cast<T*>(a.y) + row * a.D, c, a.D, v);
+            if (a.code == DIVISION_CODE_NONE) continue;
+            const Coded k = code_piece(v, a.group == 0 ? most : most_of_group(most_of(v), a.group), a.code);
+            store_codes(a.codes + row * a.D, c, a.D, k);
+            store_scale(a, row, c, a.D, k.scale);
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ the codes' values
+
+struct ReadArgs {
+    const uint8_t* codes;
+    const float* scales;
+    void* out;
+    int64_t T, D, groups;
+    int code, group, shift, lanes;                                 // lanes a row: a power of two up to 256
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void read_codes(ReadArgs a) {
+    const int rows = 256 / a.lanes, lane = threadIdx.x & (a.lanes - 1);
+    for (int64_t row = (int64_t)blockIdx.x * rows + threadIdx.x / a.lanes; row < a.T; row += (int64_t)gridDim.x * rows) {
+        const uint8_t* in = a.codes + row * a.D;
+        for (int64_t c = (int64_t)lane * kPiece; c < a.D; c += (int64_t)a.lanes * kPiece) {
+            uint32_t q[2] = {0, 0};
+            if (c + kPiece <= a.D) __builtin_memcpy(q, in + c, 8);
+            else for (int i = 0; c + i < a.D; ++i) q[i / 4] |= (uint32_t)in[c + i] << (i % 4 * 8);
+            const float scale = a.scales[row * a.groups + (a.group ? c >> a.shift : 0)];
+            float v[8];
+            if (a.code == DIVISION_CODE_INT8) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(q[i / 4] >> (i % 4 * 8)) * scale;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[i], true);
+                    v[4 * i] = lo.x * scale;
+                    v[4 * i + 1] = lo.y * scale;
+                    v[4 * i + 2] = hi.x * scale;
+                    v[4 * i + 3] = hi.y * scale;
+                }
+            }
+            store_piece(static_cast<T*>(a.out) + row * a.D, c, a.D, v);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ backward
+
+struct BackArgs {
+    const void *grad, *s, *grad_sum;
+    const void* weight;
+    const float* rstd;
+    void* dx;
+    float* parts;                                           // [gridDim.x][D]: each workgroup's share of dw
+    int64_t grad_stride, s_stride, grad_sum_stride, T, D;
+    int weight_bf16;
+};
+
+// dx of a piece from u = dy * w and n = s * rstd, whose mean product over the row is `along`
+template <typename T, typename C>
+__device__ __forceinline__ void store_dx(const BackArgs& a, int64_t row, C c, C D, float rstd, float along, const float* u, const float* n) {
+    float d[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] = rstd * __builtin_fmaf(-n[i], along, u[i]);
+    if (a.grad_sum) {
+        const Piece<T> q = load_piece(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, c, D);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] += q[i];
+    }
+    store_piece(static_cast<T*>(a.dx) + row * a.D, c, D, d);
+}
+
+// A row per NT threads as in norm_rows; dw grows in the registers of the thread that owns its columns, over all rows of the workgroup.
+template <typename T, int NT, int R>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_back_rows(BackArgs a) {
+    constexpr int ROWS = NT < 256 ? 256 / NT : 1;
+    __shared__ uint32_t slots[NT > 64 ? 2 * (NT / 64) : 1];
+    __shared__ float shares[ROWS > 1 ? ROWS * NT * R * 8 : 1];
+    const int lane = threadIdx.x % NT, D = (int)a.D;
+    float w[R][8], dw[R][8];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        load_weight(a.weight, a.weight_bf16, (r * NT + lane) * kPiece, D, w[r]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[r][i] = 0.0f;
+    }
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / NT; row < a.T; row += (int64_t)gridDim.x * ROWS) {
+        const float rstd = a.rstd[row];
+        float u[R][8], n[R][8], dot = 0.0f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int c = (r * NT + lane) * kPiece;
+            const Piece<T> g = load_piece(static_cast<const T*>(a.grad) + row * a.grad_stride, c, D);
+            const Piece<T> s = load_piece(static_cast<const T*>(a.s) + row * a.s_stride, c, D);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[r][i] = s[i] * rstd;
+                u[r][i] = g[i] * w[r][i];
+                dot = __builtin_fmaf(u[r][i], n[r][i], dot);
+                dw[r][i] = __builtin_fmaf(g[i], n[r][i], dw[r][i]);
+            }
+        }
+        const float along = row_sum<NT>(dot, slots + turn) / (float)a.D;
+        if constexpr (NT > 64) turn ^= NT / 64;
+#pragma unroll
+        for (int r = 0; r < R; ++r) store_dx<T>(a, row, (r * NT + lane) * kPiece, D, rstd, along, u[r], n[r]);
+    }
+    float* part = a.parts + (int64_t)blockIdx.x * a.D;
+    if constexpr (ROWS > 1) {                               // the workgroup's rows: added up in their order
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) shares[((threadIdx.x / NT) * R + r) * (NT * 8) + i * NT + lane] = dw[r][i];
+        __syncthreads();
+        for (int j = threadIdx.x; j < NT * R * 8; j += 256) {
+            const int r = j / (NT * 8), i = j % (NT * 8) / NT, l = j % NT;
+            const int c = (r * NT + l) * kPiece + i;
+            float t = 0.0f;
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) t += shares[k * (R * NT * 8) + j];
+            if (c < D) part[c] = t;
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) store_piece(part, (r * NT + lane) * kPiece, D, dw[r]);
+    }
+}
+
+// Rows too long for the registers: read twice; a workgroup's share of dw lies in memory, each column a thread's own.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_back_wide(BackArgs a) {
+    __shared__ uint32_t slots[2 * 16];
+    float* part = a.parts + (int64_t)blockIdx.x * a.D;
+    int turn = 0;
+    bool first = true;
+    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+        const float rstd = a.rstd[row];
+        const T* grad = static_cast<const T*>(a.grad) + row * a.grad_stride;
+        const T* s = static_cast<const T*>(a.s) + row * a.s_stride;
+        float dot = 0.0f;
+        for (int64_t c = (int64_t)threadIdx.x * kPiece; c < a.D; c += 1024 * kPiece) {
+            const Piece<T> p = load_piece(grad, c, a.D), q = load_piece(s, c, a.D);
+            float w[8];
+            load_weight(a.weight, a.weight_bf16, c, a.D, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dot = __builtin_fmaf(p[i] * w[i], q[i] * rstd, dot);
+        }
+        const float along = row_sum<1024>(dot, slots + turn) / (float)a.D;
+        turn ^= 16;
+        for (int64_t c = (int64_t)threadIdx.x * kPiece; c < a.D; c += 1024 * kPiece) {
+            const Piece<T> p = load_piece(grad, c, a.D), q = load_piece(s, c, a.D);
+            float w[8], u[8], n[8], dw[8];
+            load_weight(a.weight, a.weight_bf16, c, a.D, w);
+            const Piece<float> had = first ? Piece<float>{} : load_piece(static_cast<const float*>(part), c, a.D);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[i] = q[i] * rstd;
+                u[i] = p[i] * w[i];
+                dw[i] = __builtin_fmaf(p[i], n[i], first ? 0.0f : had[i]);
+            }
+            store_dx<T>(a, row, c, a.D, rstd, along, u, n);
+            store_piece(part, c, a.D, dw);
+        }
+        first = false;
+    }
+}
+
+// dw: the workgroups' shares added up, 64 columns and 16 runs of shares a workgroup, always in the same order
+__global__ __launch_bounds__(1024) void add_shares(const float* parts, int64_t count, int64_t D, void* dw, int is_bf16) {
+    __shared__ float runs[16][64];
+    const int col = threadIdx.x & 63, run = threadIdx.x >> 6;
+    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < D; c0 += (int64_t)gridDim.x * 64) {
+        const int64_t c = c0 + col;
+        float t = 0.0f;
+        if (c < D) {
+#pragma unroll 8
+            for (int64_t g = run; g < count; g += 16) t += parts[g * D + c];
+        }
+        runs[run][col] = t;
+        __syncthreads();
+        if (run == 0 && c < D) {
+#pragma unroll
+            for (int i = 1; i < 16; ++i) t += runs[i][col];
+            if (is_bf16) static_cast<uint16_t*>(dw)[c] = (uint16_t)bf16_pack2(t, 0.0f);
+            else static_cast<float*>(dw)[c] = t;
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+bool type_ok(division_dtype dt) { return dt == DIVISION_F32 || dt == DIVISION_BF16; }
+size_t size_of(division_dtype dt) { return dt == DIVISION_BF16 ? 2 : 4; }
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP; }
+// sizes that a call takes: rows and columns in 31 bits, elements (strides counted) in 40
+int rows_ok(int64_t T, int64_t D) {
+    if (T < 0 || D < 1) return DIVISION_EINVAL;
+    return T > INT32_MAX || D > INT32_MAX || (T > 0 && D > (int64_t(1) << 40) / T) ? DIVISION_ERANGE : DIVISION_OK;
+}
+int stride_ok(int64_t stride, int64_t T) {
+    if (stride < 0) return DIVISION_EINVAL;
+    return T > 0 && stride > (int64_t(1) << 40) / T ? DIVISION_ERANGE : DIVISION_OK;
+}
+#define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
+
+int shift_of(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
+
+constexpr int64_t kMostInRegisters = 16384;                // elements of a row (more of them spill at 1024 threads)
+constexpr int64_t kMostWorkgroups = 2048;
+
+// threads a row and pieces a thread for rows of D
+#define WITH_ROWS(D, CALL)                  \
+    if ((D) <= 128) CALL(16, 1);            \
+    else if ((D) <= 512) CALL(64, 1);       \
+    else if ((D) <= 1024) CALL(64, 2);      \
+    else if ((D) <= 2048) CALL(256, 1);     \
+    else if ((D) <= 4096) CALL(256, 2);     \
+    else if ((D) <= 8192) CALL(256, 4);     \
+    else CALL(1024, 2)
+
+template <typename T, bool RES> void launch_norm(const NormArgs& a, hipStream_t st) {
+    if (a.D > kMostInRegisters) {
+        hipLaunchKernelGGL((norm_wide<T, RES>), dim3((uint32_t)(a.T < kMostWorkgroups ? a.T : kMostWorkgroups)), dim3(1024), 0, st, a);
+        return;
+    }
+#define CALL(NT, R) do { \
+        const int64_t rows = NT < 256 ? 256 / NT : 1, grid = (a.T + rows - 1) / rows; \
+        hipLaunchKernelGGL((norm_rows<T, NT, R, RES>), dim3((uint32_t)(grid < kMostWorkgroups ? grid : kMostWorkgroups)), dim3(NT < 256 ? 256 : NT), 0, st, a); \
+    } while (0)
+    WITH_ROWS(a.D, CALL);
+#undef CALL
+}
+
+int64_t back_workgroups(int64_t T, int64_t D) {
+    const int64_t rows = D <= 128 ? 16 : D <= 1024 ? 4 : 1, grid = (T + rows - 1) / rows, most = D <= 8192 ? 512 : 256;
+    return grid < most ? grid : most;
+}
+
+template <typename T> void launch_back(const BackArgs& a, hipStream_t st) {
+    const uint32_t grid = (uint32_t)back_workgroups(a.T, a.D);
+    if (a.D > kMostInRegisters) {
+        hipLaunchKernelGGL((norm_back_wide<T>), dim3(grid), dim3(1024), 0, st, a);
+        return;
+    }
+#define CALL(NT, R) hipLaunchKernelGGL((norm_back_rows<T, NT, R>), dim3(grid), dim3(NT < 256 ? 256 : NT), 0, st, a)
+    WITH_ROWS(a.D, CALL);
+#undef CALL
+}
+
+}  // namespace
+
+extern "C" {
+
+int division_rms_norm(const division_norm* n, void* hip_stream) {
+    if (!n || !type_ok(n->dt) || !type_ok(n->weight_dt) || !(n->eps >= 0.0f)) return DIVISION_EINVAL;
+    CHECKED(rows_ok(n->T, n->D));
+    const bool coded = n->code != DIVISION_CODE_NONE;
+    if (coded && n->code != DIVISION_CODE_INT8 && n->code != DIVISION_CODE_E4M3) return DIVISION_EINVAL;
+    if (coded && n->group != 0 && n->group != 32 && n->group != 64 && n->group != 128) return DIVISION_EINVAL;
+    if (n->T == 0) return DIVISION_OK;
+    if (!n->x || !n->weight || (n->residual && !n->sum) || (coded && (!n->codes || !n->scales))) return DIVISION_EINVAL;
+    CHECKED(stride_ok(n->x_stride, n->T));
+    if (n->residual) CHECKED(stride_ok(n->residual_stride, n->T));
+    const size_t e = size_of(n->dt);
+    if (!aligned(n->x, e) || !aligned(n->residual, e) || !aligned(n->sum, e) || !aligned(n->y, e) || !aligned(n->weight, size_of(n->weight_dt)) ||
+        !aligned(n->rstd, 4) || !aligned(n->scales, 4))
+        return DIVISION_EALIGN;
+    NormArgs a{};
+    a.x = n->x; a.residual = n->residual; a.weight = n->weight; a.sum = n->sum; a.y = n->y; a.rstd = n->rstd;
+    a.codes = static_cast<uint8_t*>(n->codes); a.scales = n->scales;
+    a.x_stride = n->x_stride; a.residual_stride = n->residual_stride; a.T = n->T; a.D = n->D;
+    a.groups = n->group ? (n->D + n->group - 1) / n->group : 1;
+    a.eps = n->eps; a.code = n->code; a.group = n->group; a.shift = shift_of(n->group); a.weight_bf16 = n->weight_dt == DIVISION_BF16;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (n->dt == DIVISION_F32) n->residual ? launch_norm<float, true>(a, st) : launch_norm<float, false>(a, st);
+    else n->residual ? launch_norm<uint16_t, true>(a, st) : launch_norm<uint16_t, false>(a, st);
+    return launched();
+}
+
+int division_read_codes(const void* codes, const float* scales, int64_t T, int64_t D, division_code code, int group, division_dtype dt, void* out,
+                        void* hip_stream) {
+    if (!type_ok(dt) || (code != DIVISION_CODE_INT8 && code != DIVISION_CODE_E4M3) || (group != 0 && group != 32 && group != 64 && group != 128)) return DIVISION_EINVAL;
+    CHECKED(rows_ok(T, D));
+    if (T == 0) return DIVISION_OK;
+    if (!codes || !scales || !out) return DIVISION_EINVAL;
+    if (!aligned(scales, 4) || !aligned(out, size_of(dt))) return DIVISION_EALIGN;
+    ReadArgs a{};
+    a.codes = static_cast<const uint8_t*>(codes); a.scales = scales; a.out = out; a.T = T; a.D = D;
+    a.code = code; a.group = group; a.shift = shift_of(group); a.groups = group ? (D + group - 1) / group : 1;
+    a.lanes = 1;
+    while (a.lanes < 256 && (int64_t)a.lanes * kPiece < D) a.lanes *= 2;
+    const int64_t rows = 256 / a.lanes, grid = (T + rows - 1) / rows;
+    hipLaunchKernelGGL(dt == DIVISION_F32 ? read_codes<float> : read_codes<uint16_t>, dim3((uint32_t)(grid < 16384 ? grid : 16384)), dim3(256), 0,
+                       static_cast<hipStream_t>(hip_stream), a);
+    return launched();
+}
+
+size_t division_rms_norm_backward_workspace(int64_t T, int64_t D) {
+    return rows_ok(T, D) != DIVISION_OK ? 0 : (size_t)back_workgroups(T, D) * (size_t)D * 4u;
+}
+
+int division_rms_norm_backward(const division_norm_back* n, void* hip_stream) {
+    if (!n || !type_ok(n->dt) || !type_ok(n->weight_dt)) return DIVISION_EINVAL;
+    CHECKED(rows_ok(n->T, n->D));
+    if (!n->grad_weight || (n->T > 0 && (!n->grad_y || !n->sum || !n->weight || !n->rstd || !n->grad_x || !n->workspace))) return DIVISION_EINVAL;
+    CHECKED(stride_ok(n->grad_y_stride, n->T));
+    CHECKED(stride_ok(n->sum_stride, n->T));
+    if (n->grad_sum) CHECKED(stride_ok(n->grad_sum_stride, n->T));
+    const size_t e = size_of(n->dt), we = size_of(n->weight_dt);
+    if (!aligned(n->grad_y, e) || !aligned(n->sum, e) || !aligned(n->grad_sum, e) || !aligned(n->grad_x, e) || !aligned(n->weight, we) ||
+        !aligned(n->grad_weight, we) || !aligned(n->rstd, 4) || !aligned(n->workspace, 4))
+        return DIVISION_EALIGN;
+    if (n->workspace_bytes < division_rms_norm_backward_workspace(n->T, n->D)) return DIVISION_ESIZE;
+    BackArgs a{};
+    a.grad = n->grad_y; a.s = n->sum; a.grad_sum = n->grad_sum; a.weight = n->weight; a.rstd = n->rstd; a.dx = n->grad_x;
+    a.parts = static_cast<float*>(n->workspace);
+    a.grad_stride = n->grad_y_stride; a.s_stride = n->sum_stride; a.grad_sum_stride = n->grad_sum_stride; a.T = n->T; a.D = n->D;
+    a.weight_bf16 = n->weight_dt == DIVISION_BF16;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (n->T > 0) {
+        if (n->dt == DIVISION_F32) launch_back<float>(a, st);
+        else launch_back<uint16_t>(a, st);
+        CHECKED(launched());
+    }
+    const int64_t grid = (n->D + 63) / 64;
+    hipLaunchKernelGGL(add_shares, dim3((uint32_t)(grid < 65536 ? grid : 65536)), dim3(1024), 0, st, a.parts, n->T > 0 ? back_workgroups(n->T, n->D) : 0, n->D,
+                       n->grad_weight, a.weight_bf16);
+    return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,107 @@
+// Included inside the unnamed namespaces of norm.hip, logprobs.hip and gradnorm.hip: rows of fp32 or bfloat16 elements in
+// pieces of eight, reductions over lanes, launches.
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kPiece = 8;                                   // elements a lane takes at a time: 16 bytes of bfloat16, 32 of fp32
+
+__device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
+// two fp32 -> bfloat16 in one word, to nearest even, a NaN kept
+__device__ __forceinline__ uint32_t bf16_pack2(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2_t));
+}
+
+// Element types: fp32 as float, bfloat16 as uint16_t.  A row may start at any element: rows of an odd width do, and then no
+// 16-byte access is aligned.  The machine takes such accesses of global memory (the ABI sets the unaligned mode); memcpy says so to the compiler, which
+// keeps them whole.
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+    u32x4 w[2];
+    __device__ __forceinline__ void load(const float* p) { __builtin_memcpy(w, p, 32); }
+    __device__ __forceinline__ void load(const float* p, int n) {
+        uint32_t* e = reinterpret_cast<uint32_t*>(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < n ? __float_as_uint(p[i]) : 0u;
+    }
+    __device__ __forceinline__ void zero() { w[0] = u32x4{0, 0, 0, 0}; w[1] = w[0]; }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i / 4][i % 4]); }
+    static __device__ __forceinline__ void store(float* p, const float* v) { __builtin_memcpy(p, v, 32); }
+    static __device__ __forceinline__ void store(float* p, const float* v, int n) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < n) p[i] = v[i];
+    }
+};
+template <> struct Piece<uint16_t> {
+    u32x4 w;
+    __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(&w, p, 16); }
+    __device__ __forceinline__ void load(const uint16_t* p, int n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = 2 * i < n ? p[2 * i] : 0u, hi = 2 * i + 1 < n ? p[2 * i + 1] : 0u;
+            w[i] = lo | hi << 16;
+        }
+    }
+    __device__ __forceinline__ void zero() { w = u32x4{0, 0, 0, 0}; }
+    __device__ __forceinline__ float operator[](int i) const { return i & 1 ? __uint_as_float(w[i / 2] & 0xffff0000u) : bf16_value(w[i / 2]); }
+    static __device__ __forceinline__ u32x4 packed(const float* v) {
+        return u32x4{bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]), bf16_pack2(v[4], v[5]), bf16_pack2(v[6], v[7])};
+    }
+    static __device__ __forceinline__ void store(uint16_t* p, const float* v) { const u32x4 q = packed(v); __builtin_memcpy(p, &q, 16); }
+    static __device__ __forceinline__ void store(uint16_t* p, const float* v, int n) {
+        const u32x4 q = packed(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < n) p[i] = (uint16_t)(q[i / 2] >> (i & 1 ? 16 : 0));
+    }
+};
+// The piece of a row that starts at column c of D: whole, the row's last, or behind its end (zeros, nothing stored).  C: int where c + 8 fits it, else int64_t
+template <typename T, typename C> __device__ __forceinline__ Piece<T> load_piece(const T* row, C c, C D) {
+    Piece<T> q;
+    if (c + kPiece <= D) q.load(row + c);
+    else if (c < D) q.load(row + c, (int)(D - c));
+    else q.zero();
+    return q;
+}
+template <typename T, typename C> __device__ __forceinline__ void store_piece(T* row, C c, C D, const float* v) {
+    if (c + kPiece <= D) Piece<T>::store(row + c, v);
+    else if (c < D) Piece<T>::store(row + c, v, (int)(D - c));
+}
+
+// Reductions over aligned groups of lanes by DPP (no LDS, no waits): every lane gets the result.  Within 16 lanes the four steps pair each lane with
+// its neighbour, the other pair of its quad, the mirrored half-row and the mirrored row; across rows through the permutes of 16 and 32 lanes.
+template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false); }
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+struct AddF { static __device__ __forceinline__ uint32_t of(uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); } };
+struct MaxU { static __device__ __forceinline__ uint32_t of(uint32_t a, uint32_t b) { return a > b ? a : b; } };
+struct MaxF { static __device__ __forceinline__ uint32_t of(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); } };
+// LANES: 4, 8, 16, 32 or 64; all lanes active
+template <typename Op, int LANES> __device__ __forceinline__ uint32_t over_lanes(uint32_t v) {
+    v = Op::of(v, dpp<kXor1>(v));
+    v = Op::of(v, dpp<kXor2>(v));
+    if constexpr (LANES >= 8) v = Op::of(v, dpp<kHalfMirror>(v));
+    if constexpr (LANES >= 16) v = Op::of(v, dpp<kMirror>(v));
+    if constexpr (LANES >= 32) v = Op::of(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+    if constexpr (LANES >= 64) v = Op::of(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+    return v;
+}
+template <int LANES> __device__ __forceinline__ float sum_lanes(float v) { return __uint_as_float(over_lanes<AddF, LANES>(__float_as_uint(v))); }
+
+// A value of a row over the NT threads that share it: NT up to 64 lanes of a wavefront, or whole wavefronts through `slots` (one per wavefront, two
+// sets that calls take in turn, so that a call needs one barrier; the caller's first call on a row follows the last row's by two)
+template <typename Op, int NT> __device__ __forceinline__ uint32_t over_row(uint32_t v, uint32_t* slots) {
+    if constexpr (NT <= 64) {
+        return over_lanes<Op, NT>(v);
+    } else {
+        constexpr int W = NT / 64;
+        v = over_lanes<Op, 64>(v);
+        if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
+        __syncthreads();
+        uint32_t r = slots[0];
+#pragma unroll
+        for (int i = 1; i < W; ++i) r = Op::of(r, slots[i]);
+        return r;
+    }
+}
+template <int NT> __device__ __forceinline__ float row_sum(float v, uint32_t* slots) { return __uint_as_float(over_row<AddF, NT>(__float_as_uint(v), slots)); }

@@ -1,0 +1,200 @@
+"""Python binding of the operators of a token model's training step that include/division.h declares beside the codec: the
+root-mean-square norm with an output in 8 bits.
+
+Argument marshalling only, as in binding.py: device tensors in, device tensors out, all arithmetic in the HIP library, on torch's
+current stream or the one given.  Token vectors are the last dimension of a tensor, next to one another; the dimensions before it may
+have any stride that lets them count as rows (slices of a wider tensor do).
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple
+
+import torch
+
+from .binding import OPERATOR_ENTRIES, DivisionError, _dt, _stream, lib
+
+_vp, _i64, _ci, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
+_CODES = {None: 0, "int8": 1, "e4m3": 2}
+_CODE_TYPES = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
+
+class _NormDesc(ctypes.Structure):
+    """division_norm of include/division.h"""
+    _fields_ = [("x", _vp), ("residual", _vp), ("weight", _vp), ("x_stride", _i64), ("residual_stride", _i64), ("T", _i64), ("D", _i64),
+                ("dt", _ci), ("weight_dt", _ci), ("eps", ctypes.c_float), ("sum", _vp), ("y", _vp), ("rstd", _vp), ("code", _ci),
+                ("group", _ci), ("codes", _vp), ("scales", _vp)]
+
+
+class _NormBackDesc(ctypes.Structure):
+    """division_norm_back of include/division.h"""
+    _fields_ = [("grad_y", _vp), ("sum", _vp), ("grad_sum", _vp), ("weight", _vp), ("rstd", _vp), ("grad_y_stride", _i64), ("sum_stride", _i64),
+                ("grad_sum_stride", _i64), ("T", _i64), ("D", _i64), ("dt", _ci), ("weight_dt", _ci), ("grad_x", _vp), ("grad_weight", _vp),
+                ("workspace", _vp), ("workspace_bytes", _sz)]
+
+
+OPERATOR_ENTRIES += [
+    ("division_rms_norm", [_vp, _vp], _ci),
+    ("division_read_codes", [_vp, _vp, _i64, _i64, _ci, _ci, _ci, _vp, _vp], _ci),
+    ("division_rms_norm_backward_workspace", [_i64, _i64], _sz),
+    ("division_rms_norm_backward", [_vp, _vp], _ci),
+]
+
+
+def _checked(rc: int, what: str):
+    if rc:
+        raise DivisionError(rc, what)
+
+
+def _rows(t: torch.Tensor, what: str):
+    """(rows, their stride, columns) of a device tensor whose last dimension is one row."""
+    if not t.is_cuda or t.dim() == 0 or (t.stride(-1) != 1 and t.shape[-1] != 1):
+        raise ValueError(f"{what} must be a device tensor whose last dimension is contiguous")
+    D = t.shape[-1]
+    n = t.numel() // D if D else 0
+    if t.dim() == 1 or n <= 1:
+        return n if t.dim() > 1 else 1, D, D
+    stride, inner = 0, 1                  # of the rows, from the innermost dimension that has more than one
+    for size, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if inner == 1:
+            stride = st
+        elif st != stride * inner:
+            raise ValueError(f"{what}: its leading dimensions do not count as rows of one stride")
+        inner *= size
+    return n, stride, D
+
+
+def _dense(t: torch.Tensor, what: str, dtype=None, shape=None, device=None):
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous device tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must have shape {tuple(shape)}")
+    _beside(t, device, what)
+
+
+def _beside(t: torch.Tensor, device, what: str):
+    if device is not None and t.device != device:
+        raise ValueError(f"{what} lies on another device")
+
+
+def _at(t) -> int | None:
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(nbytes: int, device, stream):
+    """Memory for one call.  torch hands it out again when the call's tensors are gone: to the current stream's next call, behind this
+    one, or, where the call runs on another stream, not before that stream has passed it."""
+    ws = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
+    if stream is not None:
+        ws.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device))
+    return ws
+
+
+def _group_count(D: int, group: int) -> int:
+    return -(-D // group) if group else 1
+
+
+class Normed(NamedTuple):
+    """What division_rms_norm returns; None for what was not asked for."""
+    y: torch.Tensor | None
+    sum: torch.Tensor                   # the residual stream behind the addition (x itself where there was none)
+    rstd: torch.Tensor
+    codes: torch.Tensor | None          # int8, or float8_e4m3fn
+    scales: torch.Tensor | None
+
+
+def _check_code(code, group):
+    if code not in _CODES:
+        raise ValueError("code is None, 'int8' or 'e4m3'")
+    if group not in (0, 32, 64, 128):
+        raise ValueError("a scale is for 32, 64 or 128 columns, or the row (0)")
+
+
+def division_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None, code: str | None = None,
+                      group: int = 0, want_y: bool = True, stream=None) -> Normed:
+    """Root-mean-square norm over the last dimension, of x + residual where a residual is given.
+
+    code 'int8' or 'e4m3' gives the output in 8 bits too, with a scale for each row (group 0) or for 32, 64 or 128 of its columns;
+    want_y=False then leaves y out.  x and residual: float32 or bfloat16; weight: either."""
+    _check_code(code, group)
+    T, xs, D = _rows(x, "x")
+    _dense(weight, "weight", shape=(D,), device=x.device)
+    dt, wdt = _dt(x.dtype), _dt(weight.dtype)
+    rs = 0
+    if residual is not None:
+        if residual.shape != x.shape or residual.dtype != x.dtype:
+            raise ValueError("residual must have x's shape and type")
+        _beside(residual, x.device, "residual")
+        _, rs, _ = _rows(residual, "residual")
+    if not want_y and code is None:
+        raise ValueError("want_y=False leaves nothing to compute without a code")
+    lead = x.shape[:-1]
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_y else None
+    total = torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual is not None else x
+    rstd = torch.empty(lead, dtype=torch.float32, device=x.device)
+    codes = scales = None
+    if code is not None:
+        codes = torch.empty(x.shape, dtype=_CODE_TYPES[code], device=x.device)
+        scales = torch.empty((*lead, _group_count(D, group)), dtype=torch.float32, device=x.device)
+    d = _NormDesc(x.data_ptr(), _at(residual), weight.data_ptr(), xs, rs, T, D, dt, wdt, eps, total.data_ptr() if residual is not None else None,
+                  _at(y), rstd.data_ptr(), _CODES[code], group, _at(codes), _at(scales))
+    _checked(lib().division_rms_norm(ctypes.byref(d), _stream(stream)), "division_rms_norm")
+    return Normed(y, total, rstd, codes, scales)
+
+
+def division_read_codes(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
+                        stream=None) -> torch.Tensor:
+    """The values of division_rms_norm's codes; the last dimension of scales says how many columns have one: the row, or 128, 64 or 32."""
+    code = {torch.int8: "int8", torch.float8_e4m3fn: "e4m3"}.get(codes.dtype)
+    if code is None or codes.dim() == 0:
+        raise TypeError("codes are int8 or float8_e4m3fn")
+    _dense(codes, "codes")
+    _dense(scales, "scales", dtype=torch.float32, device=codes.device)
+    D, lead = codes.shape[-1], tuple(codes.shape[:-1])
+    fits = [g for g in (0, 32, 64, 128) if tuple(scales.shape) == (*lead, _group_count(D, g))]
+    if not fits:
+        raise ValueError("scales do not fit the codes")
+    group = fits[0]                     # more than one scale a row: of one group size alone
+    if out is None:
+        out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+    else:
+        _dense(out, "out", shape=codes.shape, device=codes.device)
+    if D == 0:
+        raise DivisionError(1, "division_read_codes")
+    _checked(lib().division_read_codes(codes.data_ptr(), scales.data_ptr(), codes.numel() // D, D, _CODES[code], group, _dt(out.dtype),
+                                       out.data_ptr(), _stream(stream)), "division_read_codes")
+    return out
+
+
+def division_rms_norm_backward(grad_y: torch.Tensor, sum: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor,
+                               grad_sum: torch.Tensor | None = None, out: torch.Tensor | None = None, stream=None):
+    """(the gradient of x, which is the residual's too, the gradient of weight) from the gradient of y and what the forward call gave.
+
+    grad_sum: the gradient that the residual stream brings from further on.  out: where the gradient of x goes (grad_y, sum or grad_sum
+    themselves, for instance)."""
+    T, ss, D = _rows(sum, "sum")
+    _dense(weight, "weight", shape=(D,), device=sum.device)
+    _dense(rstd, "rstd", dtype=torch.float32, shape=sum.shape[:-1], device=sum.device)
+    dt, wdt = _dt(sum.dtype), _dt(weight.dtype)
+    strides = []
+    for name, g in (("grad_y", grad_y), ("grad_sum", grad_sum)):
+        if g is not None and (g.shape != sum.shape or g.dtype != sum.dtype):
+            raise ValueError(f"{name} must have sum's shape and type")
+        if g is not None:
+            _beside(g, sum.device, name)
+        strides.append(_rows(g, name)[1] if g is not None else 0)
+    if out is None:
+        out = torch.empty(sum.shape, dtype=sum.dtype, device=sum.device)
+    else:
+        _dense(out, "out", dtype=sum.dtype, shape=sum.shape, device=sum.device)
+    grad_weight = torch.empty_like(weight)
+    nbytes = int(lib().division_rms_norm_backward_workspace(T, D))
+    ws = _workspace(nbytes, sum.device, stream)
+    d = _NormBackDesc(grad_y.data_ptr(), sum.data_ptr(), _at(grad_sum), weight.data_ptr(), rstd.data_ptr(), strides[0], ss, strides[1], T, D, dt, wdt,
+                      out.data_ptr(), grad_weight.data_ptr(), ws.data_ptr(), nbytes)
+    _checked(lib().division_rms_norm_backward(ctypes.byref(d), _stream(stream)), "division_rms_norm_backward")
+    return out, grad_weight

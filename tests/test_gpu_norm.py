@@ -1,0 +1,252 @@
+"""The root-mean-square norm, its 8-bit output and its backward pass against the definition in 64 bits.
+
+Bounds.  EPS is half a unit in the last place of binary32.  The sum of a row is at most 32 products a thread one after the other and a tree of ten
+steps over the threads (rows beyond 16384: D / 8192 pieces of eight more), each step off by EPS of a sum of positive terms; the root halves that; eight more operations follow.
+Results in bfloat16 are what some number within the bound rounds to."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2208_04187_amd as pkg
+from paper_2208_04187_amd import operators as ops
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+SIZES = [(1, 1), (3, 7), (2, 8), (5, 64), (33, 100), (17, 128), (6, 129), (70, 512), (9, 513), (130, 768), (5, 1024), (11, 1155), (4, 2048),
+         (7, 2561), (3, 4096), (2, 5121), (5, 8192), (2, 8200), (3, 16384), (2, 16385), (2, 40003), (4099, 96), (9000, 16), (2, 70000)]
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def _steps(D):
+    return 32 + 10 + 8 + 8 * (D // 8192 if D > 16384 else 0)
+
+
+def _inputs(T, D, dtype, seed=0):
+    gen = torch.Generator().manual_seed(1000 * T + D + seed)
+    gain = torch.rand(D, generator=gen) * 1.9 + 0.1
+    x, r = (torch.randn(T, D, generator=gen) * gain).to(dtype), torch.randn(T, D, generator=gen).to(dtype)
+    return x, r, torch.rand(D, generator=gen) + 0.5
+
+
+def _within(got, want, bound):
+    lo, hi = want - bound, want + bound
+    if got.dtype == torch.bfloat16:                 # rounding keeps the order
+        lo, hi = lo.float().bfloat16().double(), hi.float().bfloat16().double()
+    got = got.double().cpu()
+    bad = ~((lo <= got) & (got <= hi))
+    assert not bad.any(), (int(bad.sum()), ((got - want).abs() - bound).max().item())
+
+
+def _norm64(x, r, w, eps):
+    s = x.double() + (r.double() if r is not None else 0.0)
+    rstd = 1.0 / torch.sqrt((s * s).mean(-1) + eps)
+    return s, rstd, s * rstd[..., None] * w.double()
+
+
+def _check_codes(n, y, code, group, slack):
+    """Every value is as near to y as its code's step allows, scales are the largest / Q"""
+    T, D = y.shape
+    g = group or D
+    top = 127.0 if code == "int8" else 448.0
+    most = torch.stack([p.abs().amax(1) for p in y.split(g, 1)], 1)
+    scales = n.scales.double().cpu().view(T, -1)
+    _within(scales, most / top, most / top * slack)
+    per = scales.repeat_interleave(g, 1)[:, :D]
+    off = most.repeat_interleave(g, 1)[:, :D] * slack
+    raw = n.codes.view(torch.int8).cpu()
+    q = raw.double() if code == "int8" else n.codes.cpu().float().double()
+    # the nearest code: half a step away (int8: 1/2; e4m3: 2^-4 of the value, or half of 2^-9)
+    half = 0.5 * per if code == "int8" else torch.maximum(y.abs() * 2.0 ** -4, per * 2.0 ** -10)
+    assert not ((q * per - y).abs() > half + off).any()
+    if code == "int8":
+        assert int(raw.min()) >= -127
+    values = pkg.division_read_codes(n.codes, n.scales, torch.float32)
+    assert torch.equal(values.cpu(), (q.float().view(T, D) * n.scales.cpu().view(T, -1).repeat_interleave(g, 1)[:, :D]))
+    half_values = pkg.division_read_codes(n.codes, n.scales, torch.bfloat16)
+    assert torch.equal(half_values, values.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,D", SIZES)
+def test_forward_matches_the_definition(T, D, dtype):
+    x, r, w = _inputs(T, D, dtype)
+    slack = _steps(D) * EPS
+    for k, (res, wt, code, group, want_y) in enumerate([(None, torch.float32, None, 0, True), (r, torch.bfloat16, "int8", 0, True), (r, torch.float32, "e4m3", 128, False),
+                                                        (None, torch.float32, "int8", 32, True), (r, torch.float32, "e4m3", 0, True), (r, torch.float32, "int8", 64, False)]):
+        wk = w.to(wt)
+        s, rstd, y = _norm64(x, res, wk, 1e-6)
+        n = pkg.division_rms_norm(x.cuda(), wk.cuda(), 1e-6, residual=None if res is None else res.cuda(), code=code, group=group, want_y=want_y)
+        torch.cuda.synchronize()
+        assert (n.y is not None) == want_y and (n.codes is not None) == (code is not None), k
+        _within(n.rstd, rstd, rstd * slack)
+        if want_y:
+            assert n.y.dtype == dtype
+            _within(n.y, y, y.abs() * slack)
+        if res is not None:
+            _within(n.sum, s, s.abs() * EPS + 1e-45)
+        if code:
+            # the addition of x and the residual loses EPS of s before the norm
+            _check_codes(n, y, code, group, slack)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_of_other_strides_and_shapes(dtype):
+    gen = torch.Generator().manual_seed(5)
+    wide = torch.randn(3, 12, 1000, generator=gen).to(dtype).cuda()
+    w = torch.rand(333, generator=gen).cuda()
+    for x in (wide[..., 1:334], wide[:, ::2, 5:338], wide[0, 3, 7:340], wide[:1, :1, 3:336], wide[2][:, 666:999], wide[0, :1, 1:334].expand(7, 333)):
+        dense = x.contiguous()
+        r = torch.randn(x.shape, generator=gen).to(dtype).cuda()
+        for res in (None, r):
+            a = pkg.division_rms_norm(x, w, residual=res, code="int8", group=64)
+            b = pkg.division_rms_norm(dense, w, residual=res, code="int8", group=64)
+            for p, q in zip(a, b):
+                assert p.shape == q.shape and torch.equal(p, q)
+        ga, gw = pkg.division_rms_norm_backward(r, x, w, a.rstd, grad_sum=x)
+        gb, hw = pkg.division_rms_norm_backward(r, dense, w, a.rstd, grad_sum=dense)
+        assert torch.equal(ga, gb) and torch.equal(gw, hw)
+    with pytest.raises(ValueError):
+        pkg.division_rms_norm(wide[..., ::3], w)
+    with pytest.raises(ValueError):
+        pkg.division_rms_norm(wide[:2, :, 1:334].transpose(0, 1), w)
+    empty = pkg.division_rms_norm(wide[:0, 0, :333], w, code="e4m3")
+    assert empty.y.shape == (0, 333) and empty.scales.shape == (0, 1) and pkg.division_read_codes(empty.codes, empty.scales).shape == (0, 333)
+    dx, dw = pkg.division_rms_norm_backward(wide[:0, 0, :333], wide[:0, 0, :333], w, empty.rstd)
+    assert dx.shape == (0, 333) and not dw.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [40, 700, 3000, 20000])
+def test_groups_of_zeros_tiny_values_and_values_that_are_not_finite(D, dtype):
+    x = torch.randn(9, D, generator=torch.Generator().manual_seed(D)).to(dtype)
+    x[0] = 0.0
+    x[1, :35] = 0.0
+    x[2, 3] = float("nan")
+    x[3, 36] = float("inf")
+    x[4] = 2.0 ** -100
+    x[5] = torch.finfo(dtype).tiny / 4              # subnormal
+    x[6, 0] = 1e18
+    for code in ("int8", "e4m3"):
+        for group in (0, 32):
+            n = pkg.division_rms_norm(x.cuda(), torch.ones(D).cuda(), 1e-6, code=code, group=group)
+            v = pkg.division_read_codes(n.codes, n.scales, torch.float32).cpu()
+            y, sc = n.y.float().cpu(), n.scales.cpu().view(9, -1)
+            assert not v[0].any() and not sc[0].any() and not v[1, :32].any()
+            assert torch.isnan(v[2]).all() and torch.isnan(y[2]).all()      # the row's norm is NaN
+            # an infinity: its norm is infinite, the finite values become zero, the infinite one NaN
+            assert torch.isnan(y[3, 36]) and not y[3, :36].any() and torch.isnan(v[3]).any()
+            if group:
+                assert not v[3, :32].any() and (D <= 64 or not v[3, 64:].any())
+            # values of 2^-100 under eps: y = 2^-100 * 10^3, below what a scale holds
+            assert not v[4].any() and not v[5].any()
+            assert torch.isfinite(v[6:]).all()
+            for t in (0, 1, 7, 8):
+                assert torch.isfinite(v[t]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,D", SIZES)
+def test_backward_matches_the_definition(T, D, dtype):
+    s, extra, w = _inputs(T, D, dtype, 1)
+    dy, _, _ = _inputs(T, D, dtype, 2)
+    for wt, gs in ((torch.float32, None), (torch.bfloat16, extra)):
+        wk = w.to(wt)
+        _, rstd, _ = _norm64(s, None, wk, 1e-6)
+        rstd = rstd.float()
+        n, u, r1 = s.double() * rstd.double()[:, None], dy.double() * wk.double(), rstd.double()[:, None]
+        along = (u * n).mean(1, keepdim=True)
+        dx = r1 * (u - n * along) + (gs.double() if gs is not None else 0.0)
+        # every step of the sum is off by EPS of the sum of magnitudes so far
+        bound = _steps(D) * EPS * r1 * (u.abs() + n.abs() * (u * n).abs().mean(1, keepdim=True)) + (dx.abs() if gs is None else dx.abs() + gs.double().abs()) * 2 * EPS
+        got, dw = pkg.division_rms_norm_backward(dy.cuda(), s.cuda(), wk.cuda(), rstd.cuda(), grad_sum=None if gs is None else gs.cuda())
+        _within(got, dx, bound)
+        # a column's products: one after the other over the rows of a workgroup, then over the workgroups
+        want = (dy.double() * n).sum(0)
+        _within(dw, want, (T + 64) * EPS * (dy.double() * n).abs().sum(0))
+
+
+def test_gradient_matches_differences():
+    T, D, h = 5, 203, 1e-4
+    x, _, w = _inputs(T, D, torch.float32, 3)
+    dy = torch.randn(T, D, generator=torch.Generator().manual_seed(9))
+    n = pkg.division_rms_norm(x.cuda(), w.cuda(), 1e-3)
+    dx, dw = pkg.division_rms_norm_backward(dy.cuda(), x.cuda(), w.cuda(), n.rstd)
+
+    def loss(x, w):
+        return (_norm64(x, None, w, 1e-3)[2] * dy.double()).sum()
+    gen = torch.Generator().manual_seed(4)
+    for _ in range(6):
+        v, u = torch.randn(T, D, generator=gen).double(), torch.randn(D, generator=gen).double()
+        slope = (loss(x.double() + h * v, w) - loss(x.double() - h * v, w)) / (2 * h)
+        # central differences: h^2 times a third derivative of order one per element; the gradient: some EPS of its terms
+        assert abs((dx.cpu().double() * v).sum() - slope) < 1e-5 * (dx.cpu().double() * v).abs().sum()
+        slope = (loss(x, w.double() + h * u) - loss(x, w.double() - h * u)) / (2 * h)
+        assert abs((dw.cpu().double() * u).sum() - slope) < 1e-5 * (dw.cpu().double() * u).abs().sum()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,D", [(9, 333), (3, 4096), (5, 17001)])
+def test_nothing_is_written_beside_the_outputs_and_outputs_may_be_inputs(T, D, dtype):
+    x, r, w = (t.cuda() for t in _inputs(T, D, dtype))
+    ref = pkg.division_rms_norm(x, w, residual=r, code="e4m3", group=32)
+    back = pkg.division_rms_norm_backward(r, x, w, ref.rstd, grad_sum=r)
+    e = x.element_size()
+    for shift in (0, 1, 3):
+        def guarded(n, size):
+            t = torch.full((n * size + 64 * size,), 0x5A, dtype=torch.uint8, device="cuda")
+            return t, t.data_ptr() + (16 + shift) * size
+        groups = -(-D // 32)
+        (bs, ps), (by, py), (br, pr), (bc, pc), (bk, pk) = (guarded(*v) for v in ((T * D, e), (T * D, e), (T, 4), (T * D, 1), (T * groups, 4)))
+        wt = torch.empty(D + 8, device="cuda")[shift:shift + D].copy_(w)
+        d = ops._NormDesc(x.data_ptr(), r.data_ptr(), wt.data_ptr(), D, D, T, D, int(dtype == torch.bfloat16), 0, 1e-6, ps, py, pr, 2, 32, pc, pk)
+        assert pkg.lib().division_rms_norm(ctypes.byref(d), torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        for t, n, size, want in ((bs, T * D, e, ref.sum), (by, T * D, e, ref.y), (br, T, 4, ref.rstd), (bc, T * D, 1, ref.codes), (bk, T * groups, 4, ref.scales)):
+            lo, hi = (16 + shift) * size, (16 + shift + n) * size
+            assert torch.equal(t[lo:hi], want.contiguous().view(torch.uint8).view(-1)) and (t[:lo] == 0x5A).all() and (t[hi:] == 0x5A).all()
+    # in place: the stream's sum over x and over the residual, the gradient over each of its inputs
+    for k in range(2):
+        ins = [x.clone(), r.clone()]
+        y, rstd = torch.empty_like(x), torch.empty(T, device="cuda")
+        d = ops._NormDesc(ins[0].data_ptr(), ins[1].data_ptr(), w.data_ptr(), D, D, T, D, int(dtype == torch.bfloat16), 0, 1e-6, ins[k].data_ptr(), y.data_ptr(),
+                          rstd.data_ptr(), 0, 0, None, None)
+        assert pkg.lib().division_rms_norm(ctypes.byref(d), torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        assert torch.equal(ins[k], ref.sum) and torch.equal(y, ref.y) and torch.equal(rstd, ref.rstd)
+    for k in range(3):
+        ins = [r.clone(), x.clone(), r.clone()]
+        dx, dw = pkg.division_rms_norm_backward(ins[0], ins[1], w, ref.rstd, grad_sum=ins[2], out=ins[k])
+        assert dx is ins[k] and torch.equal(dx, back[0]) and torch.equal(dw, back[1])
+
+
+def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_a_graph():
+    x, r, w = (t.cuda() for t in _inputs(3000, 768, torch.bfloat16))
+
+    def calls(stream=None):
+        n = pkg.division_rms_norm(x, w, residual=r, code="e4m3", group=64, stream=stream)
+        v = pkg.division_read_codes(n.codes, n.scales, stream=stream)
+        return [n.y, n.sum, n.rstd, n.scales, v, *pkg.division_rms_norm_backward(r, n.sum, w, n.rstd, grad_sum=x, stream=stream)]
+    want = calls()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        side.wait_stream(torch.cuda.current_stream())
+        got = calls(side)
+        torch.empty(3000 * 768 * 4, dtype=torch.uint8, device="cuda").fill_(255)        # takes memory that a call has let go of
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        raw = calls(side.cuda_stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(raw, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls()
+    keep = x.clone()
+    for k in range(3):
+        x.copy_(keep * (k + 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = calls()
+        assert all(torch.equal(a, b) for a, b in zip(out, eager)), k

@@ -1,0 +1,70 @@
+"""The operators of a token model's step refuse what they cannot take, before anything is launched (no GPU needed)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2208_04187_amd as pkg
+from paper_2208_04187_amd import operators as ops
+
+EINVAL, ESIZE, EALIGN, ERANGE = 1, 2, 3, 4
+
+
+def _norm(**kw):
+    d = dict(x=4096, residual=None, weight=8192, x_stride=64, residual_stride=64, T=4, D=64, dt=0, weight_dt=0, eps=1e-6, sum=None, y=16384, rstd=None, code=0, group=0,
+             codes=None, scales=None)
+    return pkg.lib().division_rms_norm(ctypes.byref(ops._NormDesc(*{**d, **kw}.values())), None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(x=None), EINVAL), (dict(weight=None), EINVAL), (dict(dt=2), EINVAL), (dict(dt=7), EINVAL), (dict(weight_dt=2), EINVAL), (dict(eps=-1.0), EINVAL),
+    (dict(eps=float("nan")), EINVAL), (dict(D=0), EINVAL), (dict(T=-1), EINVAL), (dict(x_stride=-1), EINVAL), (dict(residual=64), EINVAL), (dict(code=3), EINVAL),
+    (dict(code=1, codes=64), EINVAL), (dict(code=1, scales=64), EINVAL), (dict(code=1, codes=64, scales=64, group=16), EINVAL), (dict(x=4098), EALIGN), (dict(y=4097, dt=1), EALIGN),
+    (dict(weight=4098), EALIGN), (dict(weight=4097, weight_dt=1), EALIGN), (dict(rstd=4098), EALIGN), (dict(code=1, codes=1, scales=2), EALIGN),
+    (dict(T=1 << 31), ERANGE), (dict(D=1 << 31), ERANGE), (dict(T=1 << 20, D=(1 << 20) + 1), ERANGE), (dict(x_stride=1 << 40), ERANGE), (dict(T=0, x=None), 0)])
+def test_norm_refuses(change, code):
+    assert _norm(**change) == code
+
+
+def _back(**kw):
+    d = dict(grad_y=4096, sum=8192, grad_sum=None, weight=4096, rstd=4096, grad_y_stride=64, sum_stride=64, grad_sum_stride=64, T=4, D=64, dt=0, weight_dt=0, grad_x=4096,
+             grad_weight=4096, workspace=4096, workspace_bytes=1 << 30)
+    return pkg.lib().division_rms_norm_backward(ctypes.byref(ops._NormBackDesc(*{**d, **kw}.values())), None)
+
+
+@pytest.mark.parametrize("change,code", [
+    *[({k: None}, EINVAL) for k in ("grad_y", "sum", "weight", "rstd", "grad_x", "grad_weight", "workspace")], (dict(dt=2), EINVAL), (dict(weight_dt=5), EINVAL),
+    (dict(D=0), EINVAL), (dict(T=-2), EINVAL), (dict(grad_y_stride=-1), EINVAL), (dict(sum_stride=-1), EINVAL), (dict(grad_sum=64, grad_sum_stride=-1), EINVAL),
+    (dict(grad_y=2), EALIGN), (dict(sum=2), EALIGN), (dict(grad_sum=2), EALIGN), (dict(grad_x=2), EALIGN), (dict(weight=2), EALIGN), (dict(grad_weight=2), EALIGN),
+    (dict(rstd=2), EALIGN), (dict(workspace=2), EALIGN), (dict(workspace_bytes=255), ESIZE), (dict(T=1 << 31), ERANGE), (dict(sum_stride=1 << 40), ERANGE)])
+def test_norm_backward_refuses(change, code):
+    assert _back(**change) == code
+
+
+def test_null_descriptors_and_workspaces():
+    L = pkg.lib()
+    assert L.division_rms_norm(None, None) == EINVAL and L.division_rms_norm_backward(None, None) == EINVAL
+    assert L.division_rms_norm_backward_workspace(0, 64) == 0 and L.division_rms_norm_backward_workspace(4, 0) == 0
+    assert L.division_rms_norm_backward_workspace(4, 64) >= 64 * 4
+
+
+def _read(codes=64, scales=64, T=4, D=64, code=1, group=0, dt=0, out=64):
+    return pkg.lib().division_read_codes(codes, scales, T, D, code, group, dt, out, None)
+
+
+@pytest.mark.parametrize("change,code", [(dict(codes=None), EINVAL), (dict(scales=None), EINVAL), (dict(out=None), EINVAL), (dict(code=0), EINVAL), (dict(code=3), EINVAL),
+                                         (dict(group=48), EINVAL), (dict(dt=2), EINVAL), (dict(D=0), EINVAL), (dict(T=-1), EINVAL), (dict(scales=2), EALIGN),
+                                         (dict(out=2), EALIGN), (dict(out=1, dt=1), EALIGN), (dict(T=1 << 31), ERANGE), (dict(T=0, codes=None), 0)])
+def test_read_codes_refuses(change, code):
+    assert _read(**change) == code
+
+
+def test_tensors_of_the_host_and_wrong_arguments_are_refused():
+    x, w = torch.zeros(2, 64), torch.ones(64)
+    for call in (lambda: pkg.division_rms_norm(x, w), lambda: pkg.division_rms_norm(x, w, code="int4"), lambda: pkg.division_rms_norm(x, w, code="int8", group=48),
+                 lambda: pkg.division_read_codes(torch.zeros(2, 64, dtype=torch.int8), torch.zeros(2)),
+                 lambda: pkg.division_rms_norm_backward(x, x, w, torch.zeros(2)), lambda: pkg.division_rms_norm(torch.zeros(()), w)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        pkg.division_read_codes(torch.zeros(2, 64), torch.zeros(2))
