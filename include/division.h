@@ -418,6 +418,49 @@ size_t division_rms_norm_backward_workspace(int64_t T, int64_t D);
 
 int division_rms_norm_backward(const division_norm_back *norm, void *hip_stream);
 
+/*
+ * Log probabilities of given tokens (logits: T rows of V, type dt), with the entropy of each row and its most probable tokens:
+ *   lse = ln(sum of e^z over the row),  logp = z[id] - lse,  entropy = -(sum of p ln p),  p = e^(z - lse).
+ *   ids        [T] token numbers.  ignore_index: logp 0, and no gradient from it.  Any other number outside [0, V): logp NaN.
+ *   logp, lse  [T];  entropy  [T], may be null
+ *   top        how many alternatives, 0 to 64 and at most V: top_logp, top_ids [T][top], by falling logit, equal ones (and +0, -0) by the lower number;
+ *              NaN counts as -inf there
+ *   workspace  division_log_probs_workspace(T, V, top) bytes (may be 0), 8-byte aligned
+ * A logit of -inf is a token that cannot be: its p is 0, also where the row's largest logit is the type's lowest number.  A row with nothing but -inf has
+ * lse -inf, logp -inf, entropy 0, alternatives 0, 1, ... of log probability -inf, and a gradient of zeros.  A NaN or +inf in a row makes all of the row's
+ * results NaN (the alternatives' numbers are still those of the order above).
+ */
+typedef struct division_logits {
+    const void *logits;
+    const int64_t *ids;
+    int64_t stride, T, V, ignore_index;
+    division_dtype dt;
+    int top;
+    float *logp, *entropy, *lse, *top_logp;
+    int64_t *top_ids;
+    void *workspace;
+    size_t workspace_bytes;
+} division_logits;
+
+size_t division_log_probs_workspace(int64_t T, int64_t V, int top);
+
+int division_log_probs(const division_logits *logits, void *hip_stream);
+
+/*
+ * Its gradient: grad_logits = grad_logp (1 at id - p) - grad_entropy p (ln p + entropy), of type dt.  lse and entropy as the forward call wrote them;
+ * grad_entropy (and then entropy) may be null.  grad_logits has rows grad_stride elements apart and may be logits itself (the same stride).
+ */
+typedef struct division_logits_back {
+    const void *logits;
+    const int64_t *ids;
+    const float *lse, *entropy, *grad_logp, *grad_entropy;
+    int64_t stride, grad_stride, T, V, ignore_index;
+    division_dtype dt;
+    void *grad_logits;
+} division_logits_back;
+
+int division_log_probs_backward(const division_logits_back *logits, void *hip_stream);
+
 /* Version of this ABI (host-only): DIVISION_ABI_VERSION of the header that the library was built with. */
 #define DIVISION_ABI_VERSION 1
 int division_abi_version(void);

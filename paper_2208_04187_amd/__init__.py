@@ -14,3 +14,4 @@ from .binding import (division_compress_3d, division_decompress_3d, division_ker
 from .binding import division_compress_maps, division_decompress_maps  # noqa: F401,E402
 from .binding import division_relu_compress, division_relu_compress_fused  # noqa: F401,E402
 from .operators import Normed, division_read_codes, division_rms_norm, division_rms_norm_backward  # noqa: F401,E402
+from .operators import LogProbs, division_log_probs, division_log_probs_backward  # noqa: F401,E402

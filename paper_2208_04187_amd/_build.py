@@ -2,7 +2,7 @@
 
 division.hip (with the kernel families and the host side in the .h fragments it includes) instantiates
 its kernels once per element / cache type; it is compiled as three translation units (-DDIVISION_PART=0, 1, 2: float, bfloat16, bfloat16-cached float) beside masks.hip and the operators
-of a token model's step (norm.hip), all in parallel, and the objects are linked into the one library.
+of a token model's step (norm.hip, logprobs.hip), all in parallel, and the objects are linked into the one library.
 """
 from __future__ import annotations
 
@@ -17,7 +17,8 @@ PKG = Path(__file__).resolve().parent
 DIVISION = PKG / "csrc" / "division.hip"
 MASKS = PKG / "csrc" / "masks.hip"
 NORM = PKG / "csrc" / "norm.hip"
-SRCS = [DIVISION, MASKS, NORM]
+LOGPROBS = PKG / "csrc" / "logprobs.hip"
+SRCS = [DIVISION, MASKS, NORM, LOGPROBS]
 LIB = PKG / "libdivision.so"
 CHECKS = PKG.parent / "tests" / "device_checks.hip"          # device helpers on their own, for the tests
 FASTCALL = PKG / "_fastcall.so"                              # imported by binding.py
@@ -33,6 +34,7 @@ UNITS = [
     ("division_c16.o", DIVISION, ["-DDIVISION_PART=2"]),
     ("masks.o", MASKS, []),
     ("norm.o", NORM, []),
+    ("logprobs.o", LOGPROBS, []),
 ]
 
 HIPCC_FLAGS = [

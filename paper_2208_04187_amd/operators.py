@@ -1,5 +1,5 @@
 """Python binding of the operators of a token model's training step that include/division.h declares beside the codec: the
-root-mean-square norm with an output in 8 bits.
+root-mean-square norm with an output in 8 bits, the log probabilities of given tokens.
 
 Argument marshalling only, as in binding.py: device tensors in, device tensors out, all arithmetic in the HIP library, on torch's
 current stream or the one given.  Token vectors are the last dimension of a tensor, next to one another; the dimensions before it may
@@ -33,11 +33,26 @@ class _NormBackDesc(ctypes.Structure):
                 ("workspace", _vp), ("workspace_bytes", _sz)]
 
 
+class _LogitsDesc(ctypes.Structure):
+    """division_logits of include/division.h"""
+    _fields_ = [("logits", _vp), ("ids", _vp), ("stride", _i64), ("T", _i64), ("V", _i64), ("ignore_index", _i64), ("dt", _ci), ("top", _ci), ("logp", _vp),
+                ("entropy", _vp), ("lse", _vp), ("top_logp", _vp), ("top_ids", _vp), ("workspace", _vp), ("workspace_bytes", _sz)]
+
+
+class _LogitsBackDesc(ctypes.Structure):
+    """division_logits_back of include/division.h"""
+    _fields_ = [("logits", _vp), ("ids", _vp), ("lse", _vp), ("entropy", _vp), ("grad_logp", _vp), ("grad_entropy", _vp), ("stride", _i64), ("grad_stride", _i64),
+                ("T", _i64), ("V", _i64), ("ignore_index", _i64), ("dt", _ci), ("grad_logits", _vp)]
+
+
 OPERATOR_ENTRIES += [
     ("division_rms_norm", [_vp, _vp], _ci),
     ("division_read_codes", [_vp, _vp, _i64, _i64, _ci, _ci, _ci, _vp, _vp], _ci),
     ("division_rms_norm_backward_workspace", [_i64, _i64], _sz),
     ("division_rms_norm_backward", [_vp, _vp], _ci),
+    ("division_log_probs_workspace", [_i64, _i64, _ci], _sz),
+    ("division_log_probs", [_vp, _vp], _ci),
+    ("division_log_probs_backward", [_vp, _vp], _ci),
 ]
 
 
@@ -198,3 +213,64 @@ def division_rms_norm_backward(grad_y: torch.Tensor, sum: torch.Tensor, weight: 
                       out.data_ptr(), grad_weight.data_ptr(), ws.data_ptr(), nbytes)
     _checked(lib().division_rms_norm_backward(ctypes.byref(d), _stream(stream)), "division_rms_norm_backward")
     return out, grad_weight
+
+
+class LogProbs(NamedTuple):
+    """What division_log_probs returns; None for what was not asked for."""
+    logp: torch.Tensor
+    entropy: torch.Tensor | None
+    lse: torch.Tensor
+    top_logp: torch.Tensor | None
+    top_ids: torch.Tensor | None
+
+
+def division_log_probs(logits: torch.Tensor, ids: torch.Tensor, top: int = 0, want_entropy: bool = True, ignore_index: int = -100, stream=None) -> LogProbs:
+    """Log probability of ids[...] among logits[..., V] (float32 or bfloat16), the entropy and, for top > 0, the `top` most probable tokens (at most 64).
+
+    ids: int64.  Where it is ignore_index the log probability is 0; any other number outside the vocabulary gives NaN.  Logits of -inf are tokens
+    that cannot be; a row of nothing else has log probability -inf and entropy 0."""
+    T, stride, V = _rows(logits, "logits")
+    lead = logits.shape[:-1]
+    _dense(ids, "ids", dtype=torch.int64, shape=lead, device=logits.device)
+    dt = _dt(logits.dtype)
+    if not 0 <= top <= min(64, V):
+        raise ValueError("top is 0 to 64, and at most the vocabulary")
+    f32 = dict(dtype=torch.float32, device=logits.device)
+    logp, lse = torch.empty(lead, **f32), torch.empty(lead, **f32)
+    entropy = torch.empty(lead, **f32) if want_entropy else None
+    top_logp = torch.empty((*lead, top), **f32) if top else None
+    top_ids = torch.empty((*lead, top), dtype=torch.int64, device=logits.device) if top else None
+    nbytes = int(lib().division_log_probs_workspace(T, V, top))
+    ws = _workspace(nbytes, logits.device, stream) if nbytes else None
+    d = _LogitsDesc(logits.data_ptr(), ids.data_ptr(), stride, T, V, ignore_index, dt, top, logp.data_ptr(), _at(entropy), lse.data_ptr(), _at(top_logp),
+                    _at(top_ids), _at(ws), nbytes)
+    _checked(lib().division_log_probs(ctypes.byref(d), _stream(stream)), "division_log_probs")
+    return LogProbs(logp, entropy, lse, top_logp, top_ids)
+
+
+def division_log_probs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: torch.Tensor, grad_logp: torch.Tensor, entropy: torch.Tensor | None = None,
+                                grad_entropy: torch.Tensor | None = None, ignore_index: int = -100, out: torch.Tensor | None = None,
+                                stream=None) -> torch.Tensor:
+    """The gradient of logits from those of logp and of the entropy (None: no gradient comes that way).
+
+    lse and entropy are what division_log_probs gave.  out: where the gradient goes; out=logits overwrites them, which saves a step its second-largest
+    tensor."""
+    T, stride, V = _rows(logits, "logits")
+    lead = logits.shape[:-1]
+    _dense(ids, "ids", dtype=torch.int64, shape=lead, device=logits.device)
+    dt = _dt(logits.dtype)
+    if grad_entropy is not None and entropy is None:
+        raise ValueError("the entropy's gradient needs the entropy")
+    for name, t in (("lse", lse), ("grad_logp", grad_logp), ("entropy", entropy), ("grad_entropy", grad_entropy)):
+        if t is not None:
+            _dense(t, name, dtype=torch.float32, shape=lead, device=logits.device)
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    elif out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out must have the logits' shape and type")
+    _beside(out, logits.device, "out")
+    _, out_stride, _ = _rows(out, "out")
+    d = _LogitsBackDesc(logits.data_ptr(), ids.data_ptr(), lse.data_ptr(), _at(entropy), grad_logp.data_ptr(), _at(grad_entropy), stride, out_stride, T, V,
+                        ignore_index, dt, out.data_ptr())
+    _checked(lib().division_log_probs_backward(ctypes.byref(d), _stream(stream)), "division_log_probs_backward")
+    return out

@@ -1,0 +1,274 @@
+"""Log probabilities of given tokens, entropy, alternatives and the gradient against the definition in 64 bits.
+
+Bounds.  EPS is half a unit in the last place of binary32.  e^d of d = z - max <= 0 is off by (2 |d| + 3) EPS of itself (the difference, its product
+with log2 e, the machine's 2^x); a thread adds up to V / 256 of them and joins in twenty steps more, so S is off by (V / 256 + 30 + 2 mean |d|) EPS of itself.
+Results in bfloat16 are what some number within the bound rounds to."""
+import math
+
+import pytest
+import torch
+
+import paper_2208_04187_amd as pkg
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+INF = math.inf
+TYPES = [torch.float32, torch.bfloat16]
+SIZES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 65), (7, 250), (1, 1000), (33, 2047), (2, 2048), (3, 2049), (6, 8191), (1, 8193), (2, 20001), (1, 50021), (3, 131072),
+         (1, 262147), (1500, 300), (1030, 9001), (300, 6007)]
+
+
+def _logits(T, V, dtype, seed=0, scale=2.5):
+    gen = torch.Generator().manual_seed(T * 7919 + V + seed)
+    z = torch.randn(T, V, generator=gen) * scale
+    ids = torch.randint(0, V, (T,), generator=gen)
+    z.scatter_add_(1, ids[:, None], torch.rand(T, 1, generator=gen) * 10)
+    return z.to(dtype), ids
+
+
+def _definition(z, ids, ignore=-100):
+    """lse, logp, entropy and mean |d| in 64 bits"""
+    z = z.double()
+    most = z.amax(1, keepdim=True)
+    empty = most[:, 0] == -INF
+    d = torch.where(z == -INF, -INF, z - torch.where(most == -INF, 0.0, most))
+    e = d.exp()
+    S, U = e.sum(1), -(e * d.clamp(min=-1e30)).sum(1)
+    lse = torch.where(empty, -INF, most[:, 0] + S.log())
+    H = torch.where(empty, 0.0, S.log() + U / S)
+    logp = torch.where(empty, -INF, z.gather(1, ids.clamp(0, z.shape[1] - 1)[:, None])[:, 0] - lse)
+    return lse, torch.where(ids == ignore, 0.0, logp), H, torch.where(empty, 0.0, U / S)
+
+
+def _order(z, top):
+    z = torch.where(z.isnan(), -INF, z.float())
+    return z.sort(dim=1, descending=True, stable=True).indices[:, :top]
+
+
+def _near(got, want, bound, what):
+    got = got.double().cpu()
+    same = got == want.float().double()             # infinities, also of numbers beyond binary32's range
+    bad = ~(same | ((got - want).abs() <= bound))
+    assert not bad.any(), (what, int(bad.sum()), got[bad][:4], want[bad][:4])
+
+
+def _check(z, ids, got, top=0, ignore=-100):
+    lse, logp, H, mean = _definition(z.cpu(), ids.cpu(), ignore)
+    V = z.shape[1]
+    off = (V / 256 + 30 + 2 * mean) * EPS
+    _near(got.lse, lse, off + 2 * EPS * lse.abs(), "lse")
+    _near(got.logp, logp, off + 2 * EPS * (lse.abs() + logp.abs()), "logp")
+    if got.entropy is not None:
+        # ln S and U / S: U's terms are off as S's are, and by EPS (2 |d| + 3) more
+        _near(got.entropy, H, (off + 10 * EPS) * (1 + H + 3 * mean) + 2 * EPS * H, "entropy")
+    if top:
+        want = _order(z.cpu(), top)
+        assert torch.equal(got.top_ids.cpu(), want)
+        values = z.cpu().double().gather(1, want)
+        _near(got.top_logp, torch.where(lse[:, None] == -INF, -INF, values - lse[:, None]), (off + 2 * EPS * lse.abs())[:, None] + 2 * EPS * (values - lse[:, None]).abs(), "top")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", SIZES)
+def test_forward_matches_the_definition(T, V, dtype):
+    z, ids = _logits(T, V, dtype)
+    for top, entropy in ((0, True), (0, False), (min(V, 1), True), (min(V, 20), False), (min(V, 64), True)):
+        got = pkg.division_log_probs(z.cuda(), ids.cuda(), top=top, want_entropy=entropy)
+        torch.cuda.synchronize()
+        assert (got.entropy is not None) == entropy and (got.top_ids is not None) == (top > 0)
+        _check(z, ids, got, top)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [40, 3000, 70001])
+def test_masks_ties_and_ends_of_the_range(V, dtype):
+    z, ids = _logits(16, V, dtype, 5)
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    z[0] = -INF                                     # nothing left
+    z[1] = -INF
+    z[1, V // 2] = 1.0                              # one token left
+    z[2] = low                                      # the type's lowest number everywhere: all tokens alike
+    z[3, ::2] = low                                 # as a mask
+    z[4] = 0.0                                      # all equal
+    z[5] = (z[5] * 2).round()                       # many ties
+    z[6, : V - 1] = -INF                            # the last token alone
+    z[7, 5:] = -INF                                 # fewer tokens than alternatives
+    z[8] = low
+    z[8, V - 2] = high                              # both ends
+    z[9] = torch.where(torch.arange(V) % 2 == 0, 0.0, -0.0)
+    z[10] = high
+    z[11] *= 1e4
+    z[12, ids[12]] = -INF                           # the token itself cannot be
+    z[13] = torch.linspace(-20, 20, V).to(dtype)
+    z[14] = torch.linspace(20, -20, V).to(dtype)
+    ids[15] = -100
+    for rows in (slice(None), slice(0, 1), slice(2, 3)):
+        got = pkg.division_log_probs(z[rows].cuda(), ids[rows].cuda(), top=20)
+        _check(z[rows], ids[rows], got, 20)
+    got = pkg.division_log_probs(z.cuda(), ids.cuda(), top=20)
+    assert got.lse[0] == -INF and got.logp[0] == -INF and got.entropy[0] == 0 and got.top_ids[0].tolist() == list(range(20)) and (got.top_logp[0] == -INF).all()
+    assert got.entropy[1] == 0 and got.logp[12] == -INF and got.logp[15] == 0
+    assert abs(got.entropy[2].item() - math.log(V)) < 1e-5 and abs(got.entropy[10].item() - math.log(V)) < 1e-5
+    # the gradient of every row is finite, and zero where nothing is left
+    back = pkg.division_log_probs_backward(z.cuda(), ids.cuda(), got.lse, torch.ones(16).cuda(), entropy=got.entropy, grad_entropy=torch.ones(16).cuda())
+    assert torch.isfinite(back).all() and not back[0].any()
+    back[8, ids[8]] -= 1.0                          # one token has all probability
+    assert not back[8, : V - 2].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_values_that_are_not_finite_and_numbers_that_are_no_tokens(dtype):
+    z, ids = _logits(8, 5000, dtype, 6)
+    z[1, 4321] = float("nan")
+    z[2, 17] = INF
+    z[3] = float("nan")
+    z[4, 100] = -float("nan")
+    ids[5], ids[6] = 5000, -1
+    for rows in (z, z.repeat(300, 1)):
+        got = pkg.division_log_probs(rows.cuda(), ids.repeat(len(rows) // 8).cuda(), top=7)
+        for t in (1, 2, 3, 4):
+            assert got.lse[t].isnan() and got.logp[t].isnan() and got.entropy[t].isnan() and got.top_logp[t].isnan().any()
+        assert got.logp[5].isnan() and got.logp[6].isnan() and torch.isfinite(got.lse[5:8]).all() and torch.isfinite(got.entropy[5:8]).all()
+        assert torch.equal(got.top_ids.cpu(), _order(rows, 7))
+    back = pkg.division_log_probs_backward(z.cuda(), ids.cuda(), got.lse[:8], torch.ones(8).cuda())
+    assert back[1:7].isnan().all() and torch.isfinite(back[0]).all() and torch.isfinite(back[7]).all()
+
+
+def test_alternatives_that_a_few_threads_hold():
+    """More large logits with the threads that hold the largest than fit beside one another"""
+    V = 131072 + 24
+    c = torch.arange(V)
+    gen = torch.Generator().manual_seed(3)
+    # every 2048th run of 160 columns large, all different, or all equal
+    high = torch.where(c % 2048 < 160, 50 + torch.rand(V, generator=gen), torch.randn(V, generator=gen))
+    equal = torch.where(c % 2048 < 160, 50.0, 0.0)
+    for z, dtype in ((high, torch.float32), (equal, torch.bfloat16), (high, torch.bfloat16)):
+        z = z.to(dtype)[None]
+        ids = torch.tensor([5])
+        for T, top in ((1, 64), (1100, 20), (1100, 64)):
+            got = pkg.division_log_probs(z.cuda().expand(T, V), ids.expand(T).contiguous().cuda(), top=top)
+            assert torch.equal(got.top_ids[0].cpu(), _order(z, top)[0]) and (got.top_ids == got.top_ids[:1]).all()
+            for a in (got.lse, got.logp, got.entropy, got.top_logp):
+                assert (a == a[:1]).all()
+            _check(z, ids, type(got)(*(a[:1] for a in got)), top)
+
+
+def _gradient(z, ids, lse, g, H=None, gh=None, ignore=-100):
+    z, lse, g = z.double(), lse.double()[:, None], torch.where(ids == ignore, 0.0, g.double())[:, None]
+    d = torch.where(z == -INF, -1e4, z - torch.where(lse == -INF, 0.0, lse))
+    p = torch.where((z == -INF) | (lse == -INF), 0.0, d.exp())
+    per = g + (0.0 if gh is None else gh.double()[:, None] * (d + H.double()[:, None]))
+    size = g.abs() + (0.0 if gh is None else gh.double().abs()[:, None] * (d.abs() + H.double().abs()[:, None]))
+    one = torch.zeros_like(z).scatter_(1, ids.clamp(min=0)[:, None], 1.0) * (lse != -INF)
+    return g * one - p * per, p * size * (2 * d.abs() + 8) * EPS + 1e-37
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", SIZES)
+def test_gradient_matches_the_definition(T, V, dtype):
+    z, ids = _logits(T, V, dtype, 1)
+    z[0, V // 3 + 1:] = -INF
+    ids[0] = 0
+    ids[T // 2] = -100
+    gen = torch.Generator().manual_seed(2)
+    g, gh = torch.randn(T, generator=gen), torch.randn(T, generator=gen)
+    lse, _, H, _ = (v.float() for v in _definition(z, ids))
+    zc, ic = z.cuda(), ids.cuda()
+    for entropy in (False, True):
+        want, bound = _gradient(z, ids, lse, g, *((H, gh) if entropy else ()))
+        kw = dict(entropy=H.cuda(), grad_entropy=gh.cuda()) if entropy else {}
+        got = pkg.division_log_probs_backward(zc, ic, lse.cuda(), g.cuda(), **kw)
+        lo, hi = want - bound - 2 * EPS * want.abs(), want + bound + 2 * EPS * want.abs()
+        if dtype == torch.bfloat16:
+            lo, hi = lo.float().bfloat16().double(), hi.float().bfloat16().double()
+        r = got.double().cpu()
+        bad = ~((lo <= r) & (r <= hi))
+        assert not bad.any(), (entropy, int(bad.sum()), r[bad][:4], want[bad][:4])
+        over = zc.clone()                           # in place of the logits
+        assert pkg.division_log_probs_backward(over, ic, lse.cuda(), g.cuda(), out=over, **kw) is over and torch.equal(over, got)
+
+
+def test_gradient_matches_differences():
+    z, ids = _logits(4, 67, torch.float32, 3, scale=1.0)
+    gen = torch.Generator().manual_seed(8)
+    g, gh = torch.randn(4, generator=gen), torch.randn(4, generator=gen)
+    f = pkg.division_log_probs(z.cuda(), ids.cuda())
+    dz = pkg.division_log_probs_backward(z.cuda(), ids.cuda(), f.lse, g.cuda(), entropy=f.entropy, grad_entropy=gh.cuda()).cpu().double()
+
+    def loss(z):
+        _, logp, H, _ = _definition(z, ids)
+        return (logp * g.double() + H * gh.double()).sum()
+    h = 1e-4
+    for _ in range(6):
+        v = torch.randn(4, 67, generator=gen).double()
+        slope = (loss(z.double() + h * v) - loss(z.double() - h * v)) / (2 * h)
+        # central differences: h^2 times a third derivative; the gradient: some EPS of its terms
+        assert abs((dz * v).sum() - slope) < 1e-5 * (dz * v).abs().sum()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides_shapes_and_guards(dtype):
+    gen = torch.Generator().manual_seed(5)
+    wide = torch.randn(3, 4, 2500, generator=gen).to(dtype).cuda()
+    for z in (wide[..., 1:2346], wide[:, ::2, 100:2447], wide[0, 3, 7:2300], wide[1, :1, 3:1000].expand(5, 997), wide[:2, 0, :2500]):
+        dense = z.contiguous()
+        ids = torch.randint(0, z.shape[-1], z.shape[:-1], generator=gen).cuda()
+        a, b = pkg.division_log_probs(z, ids, top=9), pkg.division_log_probs(dense, ids, top=9)
+        for p, q in zip(a, b):
+            assert p.shape == q.shape and torch.equal(p, q)
+        g = torch.rand(z.shape[:-1], generator=gen).cuda()
+        ga = pkg.division_log_probs_backward(z, ids, a.lse, g, entropy=a.entropy, grad_entropy=g)
+        assert torch.equal(ga, pkg.division_log_probs_backward(dense, ids, a.lse, g, entropy=a.entropy, grad_entropy=g))
+    # a slice of a wider tensor in place: its neighbours stay
+    for lo, hi in ((1, 2346), (8, 2400)):
+        buf = wide.clone()
+        z = buf[..., lo:hi]
+        ids = torch.randint(0, hi - lo, (3, 4), generator=gen).cuda()
+        f = pkg.division_log_probs(z, ids)
+        want = pkg.division_log_probs_backward(z, ids, f.lse, f.lse)
+        pkg.division_log_probs_backward(z, ids, f.lse, f.lse, out=z)
+        assert torch.equal(z, want) and torch.equal(buf[..., :lo], wide[..., :lo]) and torch.equal(buf[..., hi:], wide[..., hi:])
+    empty = pkg.division_log_probs(wide[:0, 0], torch.empty(0, dtype=torch.int64, device="cuda"), top=3)
+    assert empty.logp.shape == (0,) and empty.top_ids.shape == (0, 3)
+    assert pkg.division_log_probs_backward(wide[:0, 0], torch.empty(0, dtype=torch.int64, device="cuda"), empty.lse, empty.logp).shape == (0, 2500)
+
+
+def test_refusals():
+    z, ids = torch.randn(4, 100, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    f = pkg.division_log_probs(z, ids)
+    for call, err in ((lambda: pkg.division_log_probs(z, ids.int()), TypeError), (lambda: pkg.division_log_probs(z, ids[:3]), ValueError), (lambda: pkg.division_log_probs(z.half(), ids), TypeError),
+                      (lambda: pkg.division_log_probs(z, ids, top=101), ValueError), (lambda: pkg.division_log_probs(z, ids, top=65), ValueError), (lambda: pkg.division_log_probs(z, ids, top=-1), ValueError),
+                      (lambda: pkg.division_log_probs(z[:, ::2], ids), ValueError), (lambda: pkg.division_log_probs(z, ids.cpu()), ValueError),
+                      (lambda: pkg.division_log_probs_backward(z, ids, f.lse, f.logp.double()), TypeError), (lambda: pkg.division_log_probs_backward(z, ids, f.lse, f.logp, grad_entropy=f.logp), ValueError),
+                      (lambda: pkg.division_log_probs_backward(z, ids, f.lse, f.logp, out=z[:, :99]), ValueError), (lambda: pkg.division_log_probs_backward(z, ids, f.lse, f.logp, out=z.bfloat16()), ValueError),
+                      (lambda: pkg.division_log_probs_backward(z, ids, f.lse, f.logp, out=z[:1].expand(4, 100)), pkg.DivisionError)):
+        with pytest.raises(err):
+            call()
+
+
+def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_a_graph():
+    z, ids = _logits(3, 60001, torch.bfloat16, 9)
+    z, ids = z.cuda(), ids.cuda()
+    g = torch.rand(3, device="cuda")
+
+    def calls(stream=None):
+        f = pkg.division_log_probs(z, ids, top=20, stream=stream)
+        return [*f, pkg.division_log_probs_backward(z, ids, f.lse, g, entropy=f.entropy, grad_entropy=g, stream=stream)]
+    want = calls()
+    side = torch.cuda.Stream()
+    for handle in (side, side.cuda_stream, side):
+        side.wait_stream(torch.cuda.current_stream())
+        got = calls(handle)
+        torch.empty(1 << 20, dtype=torch.uint8, device="cuda").fill_(255)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls()
+    keep = z.clone()
+    for k in range(3):
+        z.copy_(keep * (k + 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, calls())), k

@@ -68,3 +68,41 @@ def test_tensors_of_the_host_and_wrong_arguments_are_refused():
             call()
     with pytest.raises(TypeError):
         pkg.division_read_codes(torch.zeros(2, 64), torch.zeros(2))
+
+
+def _logits(**kw):
+    d = dict(logits=4096, ids=4096, stride=64, T=4096, V=64, ignore_index=-100, dt=0, top=0, logp=4096, entropy=None, lse=4096, top_logp=None, top_ids=None, workspace=None,
+             workspace_bytes=0)
+    return pkg.lib().division_log_probs(ctypes.byref(ops._LogitsDesc(*{**d, **kw}.values())), None)
+
+
+@pytest.mark.parametrize("change,code", [
+    *[({k: None}, EINVAL) for k in ("logits", "ids", "logp", "lse")], (dict(dt=2), EINVAL), (dict(V=0), EINVAL), (dict(T=-1), EINVAL), (dict(stride=-1), EINVAL), (dict(top=-1), EINVAL),
+    (dict(top=65, V=100), EINVAL), (dict(top=64, V=63), EINVAL), (dict(top=2, top_logp=4096), EINVAL), (dict(top=2, top_ids=4096), EINVAL), (dict(T=1, V=1 << 20), EINVAL),
+    (dict(T=1, V=1 << 20, workspace=4096, workspace_bytes=11), ESIZE), (dict(T=1, V=1 << 20, workspace=4100, workspace_bytes=1 << 20), EALIGN), (dict(logits=2), EALIGN),
+    (dict(logits=1, dt=1), EALIGN), (dict(ids=4), EALIGN), (dict(logp=2), EALIGN), (dict(lse=2), EALIGN), (dict(entropy=2), EALIGN), (dict(top=2, top_logp=2, top_ids=8), EALIGN),
+    (dict(top=2, top_logp=4, top_ids=4), EALIGN), (dict(T=1 << 31), ERANGE), (dict(V=1 << 31), ERANGE), (dict(stride=1 << 39), ERANGE), (dict(T=0, logits=None), 0)])
+def test_log_probs_refuses(change, code):
+    assert _logits(**change) == code
+
+
+def _logits_back(**kw):
+    d = dict(logits=4096, ids=4096, lse=4096, entropy=None, grad_logp=4096, grad_entropy=None, stride=64, grad_stride=64, T=4, V=64, ignore_index=-100, dt=0, grad_logits=4096)
+    return pkg.lib().division_log_probs_backward(ctypes.byref(ops._LogitsBackDesc(*{**d, **kw}.values())), None)
+
+
+@pytest.mark.parametrize("change,code", [
+    *[({k: None}, EINVAL) for k in ("logits", "ids", "lse", "grad_logp", "grad_logits")], (dict(grad_entropy=64), EINVAL), (dict(dt=2), EINVAL), (dict(V=0), EINVAL),
+    (dict(T=-1), EINVAL), (dict(stride=-1), EINVAL), (dict(grad_stride=63), EINVAL), (dict(grad_stride=-1), EINVAL), *[({k: 2}, EALIGN) for k in ("logits", "lse", "grad_logp", "grad_logits")],
+    (dict(ids=4), EALIGN), (dict(grad_entropy=2, entropy=4), EALIGN), (dict(grad_entropy=4, entropy=2), EALIGN), (dict(grad_stride=1 << 39), ERANGE), (dict(T=0, logits=None), 0)])
+def test_log_probs_backward_refuses(change, code):
+    assert _logits_back(**change) == code
+
+
+def test_log_probs_workspace():
+    L = pkg.lib()
+    assert L.division_log_probs_workspace(1 << 20, 64, 0) == 0 and L.division_log_probs_workspace(1, 64, 65) == 0 and L.division_log_probs_workspace(1, 0, 0) == 0
+    assert 0 < L.division_log_probs_workspace(1, 1 << 17, 0) < L.division_log_probs_workspace(1, 1 << 17, 20)
+    with pytest.raises(ValueError):
+        pkg.division_log_probs(torch.zeros(2, 64), torch.zeros(2, dtype=torch.int64))
+    assert L.division_log_probs(None, None) == EINVAL and L.division_log_probs_backward(None, None) == EINVAL
