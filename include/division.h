@@ -461,6 +461,31 @@ typedef struct division_logits_back {
 
 int division_log_probs_backward(const division_logits_back *logits, void *hip_stream);
 
+/*
+ * The global norm of many gradients, and their clipping: norm = sqrt(sum of the squares of all elements), added up in binary64;
+ * with c = min(1, limit / (norm + 1e-6)), out = c * grad for every tensor, rounded once to its type.  Where the norm is infinite c is 0 (an infinite
+ * element becomes NaN), where it is NaN everything becomes NaN: look at *norm to skip such a step.
+ *
+ *   grads      HOST array of `count` descriptors, read during the call only: n elements of type dt next to one another (n == 0: none; the
+ *              pointers may then be null), and for the clipping where they go: `out`, n elements of type out_dt, which may be grad itself under
+ *              the same type (other overlaps are not allowed, neither of two tensors).  A tensor that stays where it is under c == 1 is not touched.
+ *   clip       0: only the norm (out, out_dt and limit are not looked at)
+ *   norm       device, one float, written in any case (count == 0: zero)
+ *   workspace  division_grad_norm_workspace(count, grads) bytes, 16-byte aligned
+ * The sums are taken in an order that the list alone decides.
+ */
+typedef struct division_gradient {
+    const void *grad;
+    void *out;
+    int64_t n;
+    division_dtype dt, out_dt;
+} division_gradient;
+
+size_t division_grad_norm_workspace(int64_t count, const division_gradient *grads);
+
+int division_clip_grads(int64_t count, const division_gradient *grads, float limit, int clip, float *norm,
+                        void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Version of this ABI (host-only): DIVISION_ABI_VERSION of the header that the library was built with. */
 #define DIVISION_ABI_VERSION 1
 int division_abi_version(void);

@@ -2,7 +2,7 @@
 
 division.hip (with the kernel families and the host side in the .h fragments it includes) instantiates
 its kernels once per element / cache type; it is compiled as three translation units (-DDIVISION_PART=0, 1, 2: float, bfloat16, bfloat16-cached float) beside masks.hip and the operators
-of a token model's step (norm.hip, logprobs.hip), all in parallel, and the objects are linked into the one library.
+of a token model's step (norm.hip, logprobs.hip, gradnorm.hip), all in parallel, and the objects are linked into the one library.
 """
 from __future__ import annotations
 
@@ -18,7 +18,8 @@ DIVISION = PKG / "csrc" / "division.hip"
 MASKS = PKG / "csrc" / "masks.hip"
 NORM = PKG / "csrc" / "norm.hip"
 LOGPROBS = PKG / "csrc" / "logprobs.hip"
-SRCS = [DIVISION, MASKS, NORM, LOGPROBS]
+GRADNORM = PKG / "csrc" / "gradnorm.hip"
+SRCS = [DIVISION, MASKS, NORM, LOGPROBS, GRADNORM]
 LIB = PKG / "libdivision.so"
 CHECKS = PKG.parent / "tests" / "device_checks.hip"          # device helpers on their own, for the tests
 FASTCALL = PKG / "_fastcall.so"                              # imported by binding.py
@@ -35,6 +36,7 @@ UNITS = [
     ("masks.o", MASKS, []),
     ("norm.o", NORM, []),
     ("logprobs.o", LOGPROBS, []),
+    ("gradnorm.o", GRADNORM, []),
 ]
 
 HIPCC_FLAGS = [

@@ -1,5 +1,5 @@
 """Python binding of the operators of a token model's training step that include/division.h declares beside the codec: the
-root-mean-square norm with an output in 8 bits, the log probabilities of given tokens.
+root-mean-square norm with an output in 8 bits, the log probabilities of given tokens, the norm and clipping of all gradients.
 
 Argument marshalling only, as in binding.py: device tensors in, device tensors out, all arithmetic in the HIP library, on torch's
 current stream or the one given.  Token vectors are the last dimension of a tensor, next to one another; the dimensions before it may
@@ -45,6 +45,11 @@ class _LogitsBackDesc(ctypes.Structure):
                 ("T", _i64), ("V", _i64), ("ignore_index", _i64), ("dt", _ci), ("grad_logits", _vp)]
 
 
+class _GradientDesc(ctypes.Structure):
+    """division_gradient of include/division.h"""
+    _fields_ = [("grad", _vp), ("out", _vp), ("n", _i64), ("dt", _ci), ("out_dt", _ci)]
+
+
 OPERATOR_ENTRIES += [
     ("division_rms_norm", [_vp, _vp], _ci),
     ("division_read_codes", [_vp, _vp, _i64, _i64, _ci, _ci, _ci, _vp, _vp], _ci),
@@ -53,6 +58,8 @@ OPERATOR_ENTRIES += [
     ("division_log_probs_workspace", [_i64, _i64, _ci], _sz),
     ("division_log_probs", [_vp, _vp], _ci),
     ("division_log_probs_backward", [_vp, _vp], _ci),
+    ("division_grad_norm_workspace", [_i64, _vp], _sz),
+    ("division_clip_grads", [_i64, _vp, ctypes.c_float, _ci, _vp, _vp, _sz, _vp], _ci),
 ]
 
 
@@ -274,3 +281,57 @@ def division_log_probs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: to
                         ignore_index, dt, out.data_ptr())
     _checked(lib().division_log_probs_backward(ctypes.byref(d), _stream(stream)), "division_log_probs_backward")
     return out
+
+
+def _fills_its_memory(t: torch.Tensor) -> bool:
+    """Whether the elements lie next to one another in some order of the dimensions (channels-last weights do, for instance)."""
+    if t.is_contiguous():
+        return True
+    expected = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != expected:
+            return False
+        expected *= size
+    return True
+
+
+def _grads(grads, out, limit, stream, what):
+    grads = list(grads)
+    outs = grads if out is None else list(out)
+    if len(outs) != len(grads):
+        raise ValueError("one output per gradient")
+    if not grads:
+        raise ValueError("no gradients")
+    device = grads[0].device
+    descs = (_GradientDesc * len(grads))()
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        if not g.is_cuda or not _fills_its_memory(g):
+            raise ValueError("every gradient must be a device tensor whose elements lie next to one another")
+        _beside(g, device, "a gradient")
+        if o is not g:
+            # element by element in memory: the same order on both sides
+            if o.shape != g.shape or not (o.is_contiguous() and g.is_contiguous() or o.stride() == g.stride()):
+                raise ValueError("an output must have its gradient's shape and strides")
+            _beside(o, device, "an output")
+        n = g.numel()
+        descs[i] = _GradientDesc(g.data_ptr() if n else None, o.data_ptr() if n else None, n, _dt(g.dtype), _dt(o.dtype))
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    nbytes = int(lib().division_grad_norm_workspace(len(grads), descs))
+    ws = _workspace(nbytes, device, stream)
+    _checked(lib().division_clip_grads(len(grads), descs, limit if limit is not None else 0.0, limit is not None, norm.data_ptr(), ws.data_ptr(), nbytes,
+                                       _stream(stream)), what)
+    return norm
+
+
+def division_grad_norm(grads, stream=None) -> torch.Tensor:
+    """The 2-norm of all elements of a list of gradients (float32 or bfloat16, mixed as they come): one float32 on the device."""
+    return _grads(grads, None, None, stream, "division_grad_norm")
+
+
+def division_clip_grads(grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
+    """Scales the gradients by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out` (of the same shapes; float32
+    outputs for bfloat16 gradients, for instance), and returns their norm before that.  Nothing waits for the device: where the
+    norm is not finite the gradients are not either, and the caller that wants to skip the step looks at it."""
+    if not max_norm >= 0:
+        raise ValueError("max_norm is a number from 0 up")
+    return _grads(grads, out, float(max_norm), stream, "division_clip_grads")

@@ -106,3 +106,27 @@ def test_log_probs_workspace():
     with pytest.raises(ValueError):
         pkg.division_log_probs(torch.zeros(2, 64), torch.zeros(2, dtype=torch.int64))
     assert L.division_log_probs(None, None) == EINVAL and L.division_log_probs_backward(None, None) == EINVAL
+
+
+def _clip(grads=((4096, 4096, 10, 0, 0),), count=None, limit=1.0, clip=1, norm=4096, workspace=4096, workspace_bytes=1 << 30, entry=True):
+    d = (ops._GradientDesc * max(1, len(grads)))(*[ops._GradientDesc(*g) for g in grads])
+    n = len(grads) if count is None else count
+    return pkg.lib().division_clip_grads(n, d if entry else None, limit, clip, norm, workspace, workspace_bytes, None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(count=-1), EINVAL), (dict(entry=False), EINVAL), (dict(norm=None), EINVAL), (dict(workspace=None), EINVAL), (dict(limit=-1.0), EINVAL), (dict(limit=float("nan")), EINVAL),
+    (dict(grads=((None, 64, 10, 0, 0),)), EINVAL), (dict(grads=((64, None, 10, 0, 0),)), EINVAL), (dict(grads=((64, 64, -1, 0, 0),)), EINVAL), (dict(grads=((64, 64, 1, 2, 0),)), EINVAL),
+    (dict(grads=((64, 64, 1, 0, 2),)), EINVAL), (dict(grads=((64, 64, 1, 0, 0), (66, 64, 1, 0, 0))), EALIGN), (dict(grads=((64, 66, 1, 0, 0),)), EALIGN), (dict(grads=((65, 64, 1, 1, 0),)), EALIGN),
+    (dict(grads=((64, 64, (1 << 40) + 1, 0, 0),)), ERANGE), (dict(norm=2), EALIGN), (dict(workspace=8), EALIGN), (dict(workspace_bytes=23), ESIZE)])
+def test_clipping_refuses(change, code):
+    assert _clip(**change) == code
+
+
+def test_gradient_workspace():
+    L = pkg.lib()
+    d = (ops._GradientDesc * 2)(ops._GradientDesc(64, None, 10, 0, 0), ops._GradientDesc(None, None, 0, 0, 0))
+    assert L.division_grad_norm_workspace(2, d) == 24 and L.division_grad_norm_workspace(0, None) == 16 and L.division_grad_norm_workspace(-1, None) == 0
+    for call in (lambda: pkg.division_grad_norm([torch.zeros(3)]), lambda: pkg.division_clip_grads([torch.zeros(3)], 1.0), lambda: pkg.division_clip_grads([torch.zeros(3)], -1.0)):
+        with pytest.raises(ValueError):
+            call()
