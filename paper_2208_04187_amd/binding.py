@@ -25,8 +25,9 @@ _LIB_PATH = Path(__file__).resolve().parent / "libdivision.so"
 _lib = None
 
 
-# Entries of the operators in operators.py: (name, argument types, result)
+# Entries of the operators in operators.py: (name, argument types, result), and their descriptors
 OPERATOR_ENTRIES = []
+OPERATOR_DESCS = []
 
 
 class DivisionError(RuntimeError):
@@ -129,6 +130,7 @@ def _load_fast():
                 importlib.invalidate_caches()
             module = importlib.import_module("._fastcall", __package__)
             module.bind([ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _FAST_ENTRIES], L.division_abi_version(), ctypes.sizeof(_MapDesc))
+            module.bind_operators([ctypes.cast(getattr(L, entry[0]), ctypes.c_void_p).value for entry in OPERATOR_ENTRIES], [ctypes.sizeof(d) for d in OPERATOR_DESCS])
         except (ImportError, ValueError, TypeError, RuntimeError, OSError) as err:
             warnings.warn(f"the native side of the binding is not used, small calls take twice as long on the host: {err}", RuntimeWarning, stacklevel=3)
             module = _NothingFast()

@@ -28,6 +28,16 @@ decltype(&division_mask_backward) mask_backward;
 decltype(&division_maxpool_forward) maxpool_forward;
 decltype(&division_maxpool_backward) maxpool_backward;
 decltype(&division_mask_bytes) mask_bytes;
+// ... of the operators of a token model's step; null until bind_operators()
+decltype(&division_rms_norm) rms_norm;
+decltype(&division_read_codes) read_codes;
+decltype(&division_rms_norm_backward_workspace) rms_norm_backward_workspace;
+decltype(&division_rms_norm_backward) rms_norm_backward;
+decltype(&division_log_probs_workspace) log_probs_workspace;
+decltype(&division_log_probs) log_probs;
+decltype(&division_log_probs_backward) log_probs_backward;
+decltype(&division_grad_norm_workspace) grad_norm_workspace;
+decltype(&division_clip_grads) clip_grads;
 
 // A mode of torch that replaces or watches calls sees those of binding.py
 bool plain_state() { return !c10::impl::TorchDispatchModeTLS::any_modes_set() && !at::impl::torch_function_mode_enabled(); }
@@ -400,6 +410,267 @@ PyObject* py_maxpool_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the operators of a token model's step: contiguous tensors on one device; rows = everything before the last dimension
+
+// as device_tensor, or a parameter
+const at::Tensor* weight_tensor(PyObject* o) {
+    if (!THPVariable_CheckExact(o) && Py_TYPE(o) != reinterpret_cast<PyTypeObject*>(ParameterClass)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.is_cuda() && t.layout() == at::kStrided && t.has_storage() ? &t : nullptr;
+}
+struct RowsOf { int64_t T, D; int dt; };
+bool rows_of(const at::Tensor* x, RowsOf* r) {
+    if (!x || x->dim() < 1 || x->numel() == 0 || !x->is_contiguous()) return false;
+    r->D = x->size(-1);
+    r->T = x->numel() / r->D;
+    r->dt = type_of(x->scalar_type(), false);
+    return r->dt >= 0;
+}
+// like x, of its type and device
+bool is_like(const at::Tensor* t, const at::Tensor& x) {
+    return t && t->scalar_type() == x.scalar_type() && t->device() == x.device() && t->sizes() == x.sizes() && t->is_contiguous();
+}
+// one value a row of x
+bool per_row(const at::Tensor* t, at::ScalarType type, const at::Tensor& x) {
+    return t && t->scalar_type() == type && t->device() == x.device() && t->sizes() == x.sizes().slice(0, (size_t)x.dim() - 1) && t->is_contiguous();
+}
+// None, or what `get` makes of it; false: something else
+bool maybe(PyObject* o, const at::Tensor** t) {
+    *t = nullptr;
+    return o == Py_None || (*t = device_tensor(o)) != nullptr;
+}
+std::vector<int64_t> rows_and(const at::Tensor& x, int64_t last) {
+    std::vector<int64_t> v = x.sizes().vec();
+    v.back() = last;
+    return v;
+}
+at::IntArrayRef rows_alone(const at::Tensor& x) { return x.sizes().slice(0, (size_t)x.dim() - 1); }
+void* at_or_null(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+const void* at_or_null(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+PyObject* tuple_or_none(std::initializer_list<at::Tensor> ts) {
+    PyObject* r = PyTuple_New((Py_ssize_t)ts.size());
+    if (!r) return nullptr;
+    Py_ssize_t i = 0;
+    for (const at::Tensor& t : ts) {
+        PyObject* o = t.defined() ? wrap(t) : Py_None;
+        if (!o) { Py_DECREF(r); return nullptr; }
+        if (o == Py_None) Py_INCREF(o);
+        PyTuple_SET_ITEM(r, i++, o);
+    }
+    return r;
+}
+at::Tensor workspace(size_t n, const at::Tensor& x) { return make({(int64_t)(n ? n : 1)}, at::kByte, x.device()); }
+
+// rms_norm(x, weight, eps, residual, code, group, want_y): code as a number
+PyObject* py_rms_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(7);
+    const at::Tensor *x = device_tensor(a[0]), *w = weight_tensor(a[1]), *res;
+    RowsOf r;
+    int code, group;
+    if (!rms_norm || !rows_of(x, &r) || !w || w->dim() != 1 || w->size(0) != r.D || !w->is_contiguous() || w->device() != x->device() || !PyFloat_CheckExact(a[2]) ||
+        !maybe(a[3], &res) || !whole32(a[4], &code) || !whole32(a[5], &group) || !PyBool_Check(a[6]))
+        return none();
+    const int wdt = type_of(w->scalar_type(), false);
+    if (wdt < 0 || (res && !is_like(res, *x)) || (a[6] != Py_True && code == DIVISION_CODE_NONE)) return none();
+    division_norm n{};
+    n.x = x->data_ptr(); n.residual = at_or_null(res); n.weight = w->data_ptr();
+    n.x_stride = n.residual_stride = n.D = r.D;
+    n.T = r.T; n.dt = (division_dtype)r.dt; n.weight_dt = (division_dtype)wdt; n.eps = (float)PyFloat_AS_DOUBLE(a[2]);
+    n.code = (division_code)code; n.group = group;
+    const bool want_y = a[6] == Py_True;
+    void* st = current_stream();
+    const at::Tensor in = *x;                              // held: the caller's reference may go while the lock is open
+    at::Tensor y, sum, rstd, codes, scales;
+    const int rc = without_lock([&] {
+        if (want_y) y = at::empty_like(in);
+        if (n.residual) sum = at::empty_like(in);
+        rstd = make(rows_alone(in), at::kFloat, in.device());
+        if (code) {
+            codes = make(in.sizes(), code == DIVISION_CODE_INT8 ? at::kChar : at::kFloat8_e4m3fn, in.device());
+            scales = make(rows_and(in, group > 0 ? (r.D + group - 1) / group : 1), at::kFloat, in.device());
+        }
+        n.y = at_or_null(y); n.sum = at_or_null(sum); n.rstd = rstd.data_ptr<float>(); n.codes = at_or_null(codes);
+        n.scales = static_cast<float*>(at_or_null(scales));
+        return rms_norm(&n, st);
+    });
+    return rc ? PyLong_FromLong(rc) : tuple_or_none({y, n.residual ? sum : in, rstd, codes, scales});
+    END_HANDLE_TH_ERRORS
+}
+
+// read_codes(codes, scales, dtype)
+PyObject* py_read_codes(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(3);
+    const at::Tensor *codes = device_tensor(a[0]), *scales = device_tensor(a[1]);
+    if (!read_codes || !codes || !scales || codes->dim() < 1 || codes->numel() == 0 || !codes->is_contiguous() || !scales->is_contiguous() || !THPDtype_Check(a[2]) ||
+        scales->scalar_type() != at::kFloat || scales->device() != codes->device() || scales->dim() != codes->dim())
+        return none();
+    const int code = codes->scalar_type() == at::kChar ? DIVISION_CODE_INT8 : codes->scalar_type() == at::kFloat8_e4m3fn ? DIVISION_CODE_E4M3 : 0;
+    const at::ScalarType t = reinterpret_cast<THPDtype*>(a[2])->scalar_type;
+    const int dt = type_of(t, false);
+    const int64_t D = codes->size(-1), T = codes->numel() / D, groups = scales->size(-1);
+    int group = 0;
+    if (groups != 1) for (int g : {32, 64, 128}) if (groups == (D + g - 1) / g) { group = g; break; }
+    if (!code || dt < 0 || (groups != 1 && !group) || rows_alone(*scales) != rows_alone(*codes)) return none();
+    const at::Tensor in = *codes, by = *scales;
+    const void* cp = in.data_ptr();
+    const float* sp = by.data_ptr<float>();
+    void* st = current_stream();
+    at::Tensor out;
+    const int rc = without_lock([&] {
+        out = make(in.sizes(), t, in.device());
+        return read_codes(cp, sp, T, D, (division_code)code, group, (division_dtype)dt, out.data_ptr(), st);
+    });
+    return rc ? PyLong_FromLong(rc) : wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// rms_norm_backward(grad_y, sum, weight, rstd, grad_sum)
+PyObject* py_rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(5);
+    const at::Tensor *g = device_tensor(a[0]), *s = device_tensor(a[1]), *w = weight_tensor(a[2]), *rstd = device_tensor(a[3]), *gs;
+    RowsOf r;
+    if (!rms_norm_backward || !rows_of(s, &r) || !is_like(g, *s) || !maybe(a[4], &gs) || (gs && !is_like(gs, *s)) || !per_row(rstd, at::kFloat, *s) || !w || w->dim() != 1 ||
+        w->size(0) != r.D || !w->is_contiguous() || w->device() != s->device())
+        return none();
+    const int wdt = type_of(w->scalar_type(), false);
+    if (wdt < 0) return none();
+    division_norm_back n{};
+    n.grad_y = g->data_ptr(); n.sum = s->data_ptr(); n.grad_sum = at_or_null(gs); n.weight = w->data_ptr(); n.rstd = rstd->data_ptr<float>();
+    n.grad_y_stride = n.sum_stride = n.grad_sum_stride = n.D = r.D;
+    n.T = r.T; n.dt = (division_dtype)r.dt; n.weight_dt = (division_dtype)wdt;
+    void* st = current_stream();
+    const at::Tensor in = *s, weight = w->detach();
+    at::Tensor dx, dw, ws;
+    const int rc = without_lock([&] {
+        dx = at::empty_like(in);
+        dw = at::empty_like(weight);
+        n.workspace_bytes = rms_norm_backward_workspace(r.T, r.D);
+        ws = workspace(n.workspace_bytes, in);
+        n.grad_x = dx.data_ptr(); n.grad_weight = dw.data_ptr(); n.workspace = ws.data_ptr();
+        return rms_norm_backward(&n, st);
+    });
+    return rc ? PyLong_FromLong(rc) : tuple_of({dx, dw});
+    END_HANDLE_TH_ERRORS
+}
+
+// log_probs(logits, ids, top, want_entropy, ignore_index)
+PyObject* py_log_probs(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(5);
+    const at::Tensor *z = device_tensor(a[0]), *ids = device_tensor(a[1]);
+    RowsOf r;
+    int top;
+    int64_t ignore;
+    if (!log_probs || !rows_of(z, &r) || !per_row(ids, at::kLong, *z) || !whole32(a[2], &top) || top < 0 || top > 64 || top > r.D || !PyBool_Check(a[3]) || !whole(a[4], &ignore)) return none();
+    division_logits n{};
+    n.logits = z->data_ptr(); n.ids = ids->data_ptr<int64_t>(); n.stride = n.V = r.D; n.T = r.T; n.ignore_index = ignore; n.dt = (division_dtype)r.dt; n.top = top;
+    const bool want_entropy = a[3] == Py_True;
+    void* st = current_stream();
+    const at::Tensor in = *z;
+    at::Tensor logp, entropy, lse, top_logp, top_ids, ws;
+    const int rc = without_lock([&] {
+        logp = make(rows_alone(in), at::kFloat, in.device());
+        lse = make(rows_alone(in), at::kFloat, in.device());
+        if (want_entropy) entropy = make(rows_alone(in), at::kFloat, in.device());
+        if (top) {
+            top_logp = make(rows_and(in, top), at::kFloat, in.device());
+            top_ids = make(rows_and(in, top), at::kLong, in.device());
+        }
+        n.workspace_bytes = log_probs_workspace(r.T, r.D, top);
+        if (n.workspace_bytes) ws = workspace(n.workspace_bytes, in);
+        n.logp = logp.data_ptr<float>(); n.lse = lse.data_ptr<float>(); n.entropy = static_cast<float*>(at_or_null(entropy));
+        n.top_logp = static_cast<float*>(at_or_null(top_logp)); n.top_ids = static_cast<int64_t*>(at_or_null(top_ids)); n.workspace = at_or_null(ws);
+        return log_probs(&n, st);
+    });
+    return rc ? PyLong_FromLong(rc) : tuple_or_none({logp, entropy, lse, top_logp, top_ids});
+    END_HANDLE_TH_ERRORS
+}
+
+// log_probs_backward(logits, ids, lse, grad_logp, entropy, grad_entropy, ignore_index)
+PyObject* py_log_probs_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(7);
+    const at::Tensor *z = device_tensor(a[0]), *ids = device_tensor(a[1]), *lse = device_tensor(a[2]), *g = device_tensor(a[3]), *h, *gh;
+    RowsOf r;
+    int64_t ignore;
+    if (!log_probs_backward || !rows_of(z, &r) || !per_row(ids, at::kLong, *z) || !per_row(lse, at::kFloat, *z) || !per_row(g, at::kFloat, *z) || !maybe(a[4], &h) ||
+        !maybe(a[5], &gh) || (h && !per_row(h, at::kFloat, *z)) || (gh && (!h || !per_row(gh, at::kFloat, *z))) || !whole(a[6], &ignore))
+        return none();
+    division_logits_back n{};
+    n.logits = z->data_ptr(); n.ids = ids->data_ptr<int64_t>(); n.lse = lse->data_ptr<float>(); n.grad_logp = g->data_ptr<float>();
+    n.entropy = static_cast<const float*>(at_or_null(h)); n.grad_entropy = static_cast<const float*>(at_or_null(gh));
+    n.stride = n.grad_stride = n.V = r.D; n.T = r.T; n.ignore_index = ignore; n.dt = (division_dtype)r.dt;
+    void* st = current_stream();
+    const at::Tensor in = *z;
+    at::Tensor out;
+    const int rc = without_lock([&] {
+        out = at::empty_like(in);
+        n.grad_logits = out.data_ptr();
+        return log_probs_backward(&n, st);
+    });
+    return rc ? PyLong_FromLong(rc) : wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// clip_grads(grads, out, limit): out None for in place, limit None for the norm alone; contiguous tensors in a list or tuple
+PyObject* py_clip_grads(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(3);
+    if (!clip_grads || !is_sequence(a[0]) || (a[1] != Py_None && !is_sequence(a[1])) || (a[2] != Py_None && !PyFloat_CheckExact(a[2]))) return none();
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(a[0]);
+    if (count == 0 || (a[1] != Py_None && PySequence_Fast_GET_SIZE(a[1]) != count)) return none();
+    std::vector<division_gradient> grads((size_t)count);
+    at::Tensor one;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        const at::Tensor* g = device_tensor(PySequence_Fast_GET_ITEM(a[0], i));
+        const at::Tensor* o = a[1] == Py_None ? g : device_tensor(PySequence_Fast_GET_ITEM(a[1], i));
+        if (!g || !o || !g->is_contiguous() || (o != g && (!o->is_contiguous() || o->sizes() != g->sizes()))) return none();
+        if (i == 0) one = *g;
+        const int dt = type_of(g->scalar_type(), false), odt = type_of(o->scalar_type(), false);
+        if (dt < 0 || odt < 0 || g->device() != one.device() || o->device() != one.device()) return none();
+        const int64_t n = g->numel();
+        grads[(size_t)i] = {n ? g->data_ptr() : nullptr, n ? o->data_ptr() : nullptr, n, (division_dtype)dt, (division_dtype)odt};
+    }
+    const bool clip = a[2] != Py_None;
+    const float limit = clip ? (float)PyFloat_AS_DOUBLE(a[2]) : 0.0f;
+    void* st = current_stream();
+    at::Tensor norm, ws;
+    // the lock is kept: the list and its tensors stay what they are
+    norm = make({}, at::kFloat, one.device());
+    const size_t need = grad_norm_workspace(count, grads.data());
+    ws = workspace(need, one);
+    const int rc = clip_grads(count, grads.data(), limit, clip, norm.data_ptr<float>(), ws.data_ptr(), need, st);
+    return rc ? PyLong_FromLong(rc) : wrap(std::move(norm));
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_operators(addresses, sizes): their entries in the order of the table, and the sizes of their descriptors
+PyObject* py_bind_operators(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    void** at[] = {(void**)&rms_norm, (void**)&read_codes, (void**)&rms_norm_backward_workspace, (void**)&rms_norm_backward, (void**)&log_probs_workspace,
+                   (void**)&log_probs, (void**)&log_probs_backward, (void**)&grad_norm_workspace, (void**)&clip_grads};
+    const size_t sizes[] = {sizeof(division_norm), sizeof(division_norm_back), sizeof(division_logits), sizeof(division_logits_back), sizeof(division_gradient)};
+    constexpr Py_ssize_t n = sizeof at / sizeof at[0], m = sizeof sizes / sizeof sizes[0];
+    bool ok = nargs == 2 && PyList_CheckExact(a[0]) && PyList_GET_SIZE(a[0]) == n && PyList_CheckExact(a[1]) && PyList_GET_SIZE(a[1]) == m;
+    void* found[n];
+    for (Py_ssize_t i = 0; ok && i < m; ++i) {
+        int64_t v = 0;
+        ok = whole(PyList_GET_ITEM(a[1], i), &v) && v == (int64_t)sizes[i];
+    }
+    for (Py_ssize_t i = 0; ok && i < n; ++i) {
+        found[i] = PyLong_AsVoidPtr(PyList_GET_ITEM(a[0], i));
+        if (!found[i]) { PyErr_Clear(); ok = false; }
+    }
+    if (!ok) {
+        PyErr_SetString(PyExc_ValueError, "built for another set of operators");
+        return nullptr;
+    }
+    for (Py_ssize_t i = 0; i < n; ++i) *at[i] = found[i];
+    Py_RETURN_NONE;
+}
+
 // bind(addresses, version, map_bytes): the entries above in the order of the table, of a library of this ABI version whose descriptors
 // are so large.  A ValueError where this module was built for another library.
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
@@ -425,7 +696,8 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
 #define FAST(name) {#name, (PyCFunction)(void*)py_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(compress), FAST(decompress), FAST(compress_maps), FAST(decompress_maps), FAST(relu_forward), FAST(relu_compress),
                          FAST(dropout_forward), FAST(mask_backward), FAST(maxpool_forward), FAST(maxpool_backward),
-                         FAST(bind), {nullptr, nullptr, 0, nullptr}};
+                         FAST(rms_norm), FAST(read_codes), FAST(rms_norm_backward), FAST(log_probs), FAST(log_probs_backward), FAST(clip_grads),
+                         FAST(bind_operators), FAST(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
