@@ -1,11 +1,11 @@
 // Log probabilities of given tokens for AMD MI355X (gfx950), with the entropy and the most probable alternatives of each row of
 // logits, and their gradient.  The softmax itself is never stored: a row keeps its logarithm of the sum and its entropy.
 //
-//   d_j = z_j - max z;  S = sum e^d;  U = sum d e^d;   lse = max + ln S;  logp_t = z_t - lse;  H = ln S - U / S
+//   t_j = (z_j - m) log2 e;  S = sum 2^t;  U = sum t 2^t;   lse = m + ln S;  logp_i = z_i - lse;  H = ln S - U / S ln 2
 //   p = e^(z - lse);    dz = g (delta_t - p) - gh p (ln p + H)
 //
-// One pass over the logits each.  A thread keeps the running (max, S, U) of its share of a row; shares are joined by
-// rescaling both sums to the larger maximum.  S and U are sums of terms of one sign (U <= 0), so nothing cancels.
+// One pass over the logits each.  A thread keeps a running (m, S, U) of its share of a row; shares are joined by
+// moving both to the larger m.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stddef.h>
@@ -16,21 +16,34 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.4028234663852886e38f;         // a maximum to start from that z - max is never -inf - -inf with
-constexpr float kGone = -150.0f;                           // e^d is zero from here on, and d * e^d may be taken as zero
+constexpr float kGone = -150.0f;                           // 2^t is zero from here on, and t 2^t may be taken as zero
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;                                 // pieces a thread has in flight
+constexpr int kBatch = kUnroll * kThreads * kPiece;    // columns of a workgroup's batch
 
-// e^d, d <= 0: one multiplication and the machine's 2^x
-__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+// e^z is taken as 2^(z * kLog2e - r) with r = most * kLog2e rounded: one fused multiplication and the machine's 2^x.  What the rounding of r leaves out is
+// put back where the row's sum is known (finish), and kLog2e's own error counts z - most times 1e-8.  Beyond kHuge the products would leave
+// binary32, but there two different numbers are more than 10^29 apart: a term is 1 at the maximum and 0 elsewhere.
+constexpr float kHuge = 1e37f;
+__device__ __forceinline__ bool huge(float most) { return !(fabsf(most) < kHuge); }
+__device__ __forceinline__ float point_of(float most) { return huge(most) ? (most < 0.0f ? -2.0f * kHuge : 2.0f * kHuge) : most * kLog2e; }
+__device__ __forceinline__ float exp2_of(float t) { return __builtin_amdgcn_exp2f(t); }
 
-struct Share { float most, sum, moment; };                 // of (d, e^d): max z, S, U
-__device__ __forceinline__ Share joined(const Share& a, const Share& b) {
-    Share r;
-    r.most = fmaxf(a.most, b.most);
-    const float da = fmaxf(a.most - r.most, kGone), db = fmaxf(b.most - r.most, kGone), ca = exp_of(a.most - r.most), cb = exp_of(b.most - r.most);
-    r.sum = a.sum * ca + b.sum * cb;
-    r.moment = ca * __builtin_fmaf(da, a.sum, a.moment) + cb * __builtin_fmaf(db, b.sum, b.moment);
-    return r;
+// Part of a row: r belongs to `most`, which is at least the largest logit so far less the margin; S = sum of 2^t, U = sum of t 2^t, t = z * kLog2e - r
+struct Share { float most, sum, moment; };
+// the share seen from a larger maximum
+__device__ __forceinline__ void move(Share& s, float most) {
+    float t = s.most == most ? 0.0f : huge(most) ? kGone : fmaxf(point_of(s.most) - point_of(most), kGone);
+    const float c = exp2_of(t);
+    s.moment = c * __builtin_fmaf(t, s.sum, s.moment);
+    s.sum *= c;
+    s.most = most;
+}
+__device__ __forceinline__ Share joined(Share a, Share b) {
+    const float most = fmaxf(a.most, b.most);
+    move(a, most);
+    move(b, most);
+    return Share{most, a.sum + b.sum, a.moment + b.moment};
 }
 
 // The order of logits: by value, NaN as -inf, equal ones by the lower column.  Both in one whole number, larger = before; 0 = none.
@@ -54,6 +67,7 @@ struct LogpArgs {
     uint64_t* keys;                                         // [T][splits][top]
     int64_t stride, T, V, ignore;
     int64_t split;                                          // columns of a share (a multiple of 8)
+    int64_t first;                                          // share that the launch's first workgroup works on
     int splits, top;
 };
 
@@ -65,9 +79,10 @@ template <> __device__ __forceinline__ float element(const uint16_t* p) { return
 template <typename T> __device__ __forceinline__ float finish(const LogpArgs& a, int64_t row, const Share& s) {
     const bool empty = s.sum == 0.0f;                       // every logit -inf
     const float ln = logf(s.sum);
-    const float lse = empty ? -__builtin_inff() : s.most + ln;
+    const float left = huge(s.most) ? 0.0f : kLn2 * __builtin_fmaf(-s.most, kLog2e, point_of(s.most));     // r less its exact value
+    const float lse = empty ? -__builtin_inff() : s.most + (ln + left);
     a.lse[row] = lse;
-    if (a.entropy) a.entropy[row] = empty ? 0.0f : ln - s.moment / s.sum;
+    if (a.entropy) a.entropy[row] = empty ? 0.0f : ln - s.moment / s.sum * kLn2;
     const int64_t id = a.ids[row];
     float logp = 0.0f;
     if (id != a.ignore) {
@@ -80,7 +95,7 @@ template <typename T> __device__ __forceinline__ float finish(const LogpArgs& a,
 __device__ __forceinline__ float logp_of_top(float z, float lse) { return lse == -__builtin_inff() ? lse : z - lse; }
 
 // The piece at column c of a row that ends at column `end`, -inf behind it
-template <typename T> __device__ __forceinline__ void load_logits(const T* row, int64_t c, int64_t end, float* v) {
+template <typename T> __device__ __forceinline__ void load_logits(const T* row, int c, int end, float* v) {
     if (c + kPiece <= end) {
         Piece<T> q;
         q.load(row + c);
@@ -95,73 +110,130 @@ template <typename T> __device__ __forceinline__ void load_logits(const T* row, 
 constexpr int kMostTop = 64;
 constexpr int kCandidates = 1024;
 struct TopLds {
-    uint64_t keys[kThreads];
+    uint64_t keys[kThreads / 2];
     uint64_t found[kCandidates];
-    uint32_t winners[kMostTop];
-    uint32_t count;
+    uint64_t bound;
+    uint32_t winners[kThreads];
+    uint32_t count, threads;
 };
 
-// The `top` first keys of columns [c0, c1) of a row, in order, at out[0..top) (0 where there are fewer).  best: the first key of the calling
-// thread's columns, which are the pieces c0 + (s * kThreads + thread) * 8, s = 0, 1, ...: the top-th of those bounds the top-th of all
-// from below, so that only the columns of the `top` threads with the first keys are looked at again, and of those only what reaches the bound.
-template <typename T>
-__device__ void find_top(const T* row, int64_t c0, int64_t c1, int top, uint64_t best, TopLds& lds, uint64_t* out) {
-    const int t = threadIdx.x;
-    lds.keys[t] = best;
-    if (t == 0) lds.count = 0;
-    if (t < kMostTop) lds.winners[t] = 0xffffffffu;
+template <int CTRL> __device__ __forceinline__ uint64_t max_with(uint64_t k) {
+    const uint64_t o = (uint64_t)dpp<CTRL>((uint32_t)(k >> 32)) << 32 | dpp<CTRL>((uint32_t)k);
+    return o > k ? o : k;
+}
+
+// Collects the keys from lds.bound up among the columns of the threads whose first key may reach it (upper).  In any order; lds.count may be more than fit.
+template <typename T> __device__ __forceinline__ void collect(const T* row, int c0, int end, uint64_t upper, TopLds& lds) {
+    const uint64_t bound = lds.bound;
+    const float least = bound == 1 ? -__builtin_inff() : value_of(bound);
+    if (upper >= bound) lds.winners[atomicAdd(&lds.threads, 1u)] = threadIdx.x;
     __syncthreads();
-    int before = 0;
-    for (int i = 0; i < kThreads; ++i) before += lds.keys[i] > best;
-    if (best && before < top) lds.winners[before] = (uint32_t)t;
-    __syncthreads();
-    const uint32_t last = lds.winners[top - 1];
-    const uint64_t bound = last == 0xffffffffu ? 1 : lds.keys[last];          // fewer threads than `top` have columns: all of them
-    for (int w = t >> 6; w < top; w += kThreads / 64) {
-        const uint32_t who = lds.winners[w];
-        if (who == 0xffffffffu) break;
-        for (int64_t c = c0 + ((int64_t)(t & 63) * kThreads + who) * kPiece; c < c1; c += 64 * kThreads * kPiece) {
-            float v[8];
-            load_logits(row, c, c1, v);
+    const uint32_t steps = (uint32_t)(end - c0 + kThreads * kPiece - 1) / (kThreads * kPiece), all = lds.threads * steps;
+    for (uint32_t i = threadIdx.x; i < all; i += kThreads) {
+        const uint32_t w = i / steps;
+        const int c = c0 + (int)((i - w * steps) * kThreads + lds.winners[w]) * kPiece;
+        if (c >= end) continue;
+        float v[8];
+        load_logits(row, c, end, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint64_t k = key_of(v[i], (uint32_t)(c + i));
-                if (k >= bound && c + i < c1) {
-                    const uint32_t at = atomicAdd(&lds.count, 1u);             // any order: keys differ, and are put in order below
-                    if (at < kCandidates) lds.found[at] = k;
-                }
-            }
+        for (int j = 0; j < 8; ++j) {
+            if (fmaxf(v[j], -__builtin_inff()) < least || c + j >= end) continue;     // (NaN as -inf)
+            const uint64_t k = key_of(v[j], (uint32_t)(c + j));
+            if (k < bound) continue;
+            const uint32_t at = atomicAdd(&lds.count, 1u);
+            if (at < kCandidates) lds.found[at] = k;
         }
     }
     __syncthreads();
+}
+
+// The `top` first keys of a row's columns from c0 to end, in order, at out[0..top) (0 where there are fewer).  The calling thread's columns are the pieces
+// c0 + (s * kThreads + thread) * 8, s = 0, 1, ...; `seen` is the largest of them, in the batch at column `where` for the first time.  That bounds its first key from both
+// sides, without another look.  The top-th of the lower bounds of all groups of threads bounds the top-th key of all from below: only the
+// threads that may reach it are looked at again.  64 groups of four threads let through G ln(G / (G - top)) = 24 keys for twenty, but all for 64: from 24 on
+// 128 groups of two (89 for 64; putting them in order takes four times as long).  A key for each of the 256 threads instead: 2048 rows of 50048 with
+// twenty keys 77 us, 64 here.
+template <typename T>
+__device__ __forceinline__ void find_top(const T* row, int c0, int end, int top, float seen, int where, TopLds& lds, uint64_t* out) {
+    const int t = threadIdx.x;
+    const bool has = c0 + t * kPiece < end;
+    const int last = where + (kUnroll - 1) * kThreads * kPiece + kPiece - 1;
+    const int to = last < end ? last : end - 1;
+    uint64_t lower = max_with<kXor1>(has ? key_of(seen, (uint32_t)to) : 0);
+    const int size = top < 24 ? 4 : 2, groups = kThreads / size;
+    if (size == 4) lower = max_with<kXor2>(lower);
+    if (t % size == 0) lds.keys[t / size] = lower;
+    if (t == 0) lds.count = lds.threads = 0;
+    __syncthreads();
+    if (t < groups) {
+        const uint64_t mine = lds.keys[t];
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < groups; ++j) {
+            const uint64_t k = lds.keys[j];
+            rank += k > mine || (k == mine && j < t);
+        }
+        if (rank == top - 1) lds.bound = mine ? mine : 1;   // fewer groups than `top` have columns: all of them
+    }
+    __syncthreads();
+    collect(row, c0, end, has ? key_of(seen, (uint32_t)where) : 0, lds);
+    if (lds.count > kCandidates) {
+        // many equal logits at the bound: the threads' first keys themselves give a closer one
+        __syncthreads();
+        uint64_t best = 0;
+        if (has) {
+            int first_at = where;                           // where every one is -inf or NaN: the first of all
+#pragma unroll 1
+            for (int u = kUnroll - 1; u >= 0; --u) {
+                const int c = where + u * (kThreads * kPiece);
+                if (c >= end) continue;
+                float v[8];
+                load_logits(row, c, end, v);
+#pragma unroll
+                for (int i = 7; i >= 0; --i) if (v[i] == seen && c + i < end) first_at = c + i;
+            }
+            best = key_of(seen, (uint32_t)first_at);
+        }
+        lds.found[t] = best;
+        if (t == 0) { lds.count = lds.threads = 0; lds.bound = 1; }
+        __syncthreads();
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < kThreads; ++j) rank += lds.found[j] > best;
+        if (best && rank == top - 1) lds.bound = best;
+        __syncthreads();
+        collect(row, c0, end, best, lds);
+    }
     const int n = (int)lds.count;
     if (n <= kCandidates) {
         if (t < top && t >= n) out[t] = 0;
         for (int i = t; i < n; i += kThreads) {
             const uint64_t k = lds.found[i];
             int rank = 0;
+#pragma unroll 8
             for (int j = 0; j < n; ++j) rank += lds.found[j] > k;
             if (rank < top) out[rank] = k;
         }
     } else {
-        // more than fit (a few threads hold nearly all large logits): one after the other, each the first behind the last one
+        // still more than fit (a few threads hold nearly all large logits): one after the other, each the first behind the last one
         uint64_t prior = ~0ull;
         for (int r = 0; r < top; ++r) {
             uint64_t mine = 0;
-            for (int64_t c = c0 + (int64_t)t * kPiece; c < c1; c += kThreads * kPiece) {
+            for (int c = c0 + t * kPiece; c < end; c += kThreads * kPiece) {
                 float v[8];
-                load_logits(row, c, c1, v);
+                load_logits(row, c, end, v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint64_t k = key_of(v[i], (uint32_t)(c + i));
-                    if (k < prior && k > mine && c + i < c1) mine = k;
+                    if (k < prior && k > mine && c + i < end) mine = k;
                 }
             }
             __syncthreads();                                // behind the last round's reads
-            lds.keys[t] = mine;
+            lds.found[t] = mine;
             __syncthreads();
             uint64_t first = 0;
-            for (int i = 0; i < kThreads; ++i) first = lds.keys[i] > first ? lds.keys[i] : first;
+#pragma unroll 8
+            for (int i = 0; i < kThreads; ++i) first = lds.found[i] > first ? lds.found[i] : first;
             if (t == 0) out[r] = first;
             prior = first;
         }
@@ -171,11 +243,10 @@ __device__ void find_top(const T* row, int64_t c0, int64_t c1, int top, uint64_t
 // The workgroup's shares joined; every thread gets the result.  slots: 3 * (kThreads / 64)
 __device__ __forceinline__ Share over_workgroup(const Share& s, float* slots) {
     constexpr int W = kThreads / 64;
-    Share r;
-    r.most = __uint_as_float(over_lanes<MaxF, 64>(__float_as_uint(s.most)));
-    const float c = exp_of(s.most - r.most), d = fmaxf(s.most - r.most, kGone);
-    r.sum = sum_lanes<64>(s.sum * c);
-    r.moment = sum_lanes<64>(c * __builtin_fmaf(d, s.sum, s.moment));
+    Share r = s;
+    move(r, __uint_as_float(over_lanes<MaxF, 64>(__float_as_uint(s.most))));
+    r.sum = sum_lanes<64>(r.sum);
+    r.moment = sum_lanes<64>(r.moment);
     if ((threadIdx.x & 63) == 0) {
         const int w = threadIdx.x >> 6;
         slots[w] = r.most; slots[W + w] = r.sum; slots[2 * W + w] = r.moment;
@@ -187,81 +258,91 @@ __device__ __forceinline__ Share over_workgroup(const Share& s, float* slots) {
     return r;
 }
 
-// A row, or a share of one, per workgroup and turn.
+// A thread's next logits.  most: the largest so far; s is only moved to it where it lies kMargin above: seldom after the first batch,
+// while moving every time would be ten instructions for a batch's 330.
+constexpr float kMargin = 8.0f;
+template <bool ENTROPY, bool TOP>
+__device__ __forceinline__ void add_batch(const float (&v)[kUnroll][8], int c, Share& s, float& most, float& seen, int& where) {
+    float m = v[0][0];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+        for (int i = u ? 0 : 1; i < 8; ++i) m = fmaxf(m, v[u][i]);
+    if constexpr (TOP) {
+        if (m > seen) { seen = m; where = c; }
+    }
+    most = fmaxf(most, m);
+    if (most - s.most > kMargin || huge(most)) move(s, most);
+    const float r = point_of(s.most);
+    if (!huge(most)) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float t = __builtin_fmaf(v[u][i], kLog2e, -r), e = exp2_of(t);
+                s.sum += e;
+                if constexpr (ENTROPY) s.moment = __builtin_fmaf(fmaxf(t, kGone), e, s.moment);
+            }
+    } else {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = v[u][i] - most;             // NaN: a NaN, or +inf
+                s.sum += d < 0.0f ? 0.0f : d == 0.0f ? 1.0f : d;
+            }
+    }
+}
+
+// A row, or a share of one, per workgroup.
 template <typename T, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(kThreads) void log_probs(LogpArgs a) {
     __shared__ float slots[3 * (kThreads / 64)];
     __shared__ TopLds lds;
     __shared__ float result;
     __shared__ uint64_t first[TOP ? kMostTop : 1];
-    for (int64_t item = blockIdx.x; item < a.T * a.splits; item += gridDim.x) {
-        const int64_t at = item / a.splits;
-        const int part = (int)(item - at * a.splits);
-        const T* row = static_cast<const T*>(a.z) + at * a.stride;
-        const int64_t c0 = part * a.split, c1 = c0 + a.split < a.V ? c0 + a.split : a.V;
-        Share s{kLowest, 0.0f, 0.0f};
-        float seen = -__builtin_inff();
-        int64_t where = c0 + (int64_t)threadIdx.x * kPiece;                    // the batch of the thread's largest logit
-        for (int64_t c = c0 + (int64_t)threadIdx.x * kPiece; c < c1; c += kUnroll * kThreads * kPiece) {
-            float v[kUnroll][8];
+    const int64_t item = a.first + blockIdx.x, at = a.splits == 1 ? item : item / a.splits;
+    const int part = (int)(item - at * a.splits);
+    const T* row = static_cast<const T*>(a.z) + at * a.stride;
+    const int c0 = (int)(part * a.split), end = (int)(c0 + a.split < a.V ? c0 + a.split : a.V);
+    Share s{kLowest, 0.0f, 0.0f};
+    float seen = -__builtin_inff(), most = kLowest;
+    int where = c0 + (int)threadIdx.x * kPiece;             // the batch of the thread's largest logit
+    for (int b = c0; b < end; b += kBatch) {
+        const int c = b + (int)threadIdx.x * kPiece;
+        float v[kUnroll][8];
+        if (b + kBatch <= end) {
+            Piece<T> q[kUnroll];
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) load_logits(row, c + u * (kThreads * kPiece), c1, v[u]);
-            float most = s.most;
-            if constexpr (TOP) most = -__builtin_inff();
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) most = fmaxf(most, v[u][i]);
-            if constexpr (TOP) {
-                if (most > seen) { seen = most; where = c; }
-                most = fmaxf(most, s.most);
-            }
-            const float scale = exp_of(s.most - most);
-            if constexpr (ENTROPY) s.moment = scale * __builtin_fmaf(fmaxf(s.most - most, kGone), s.sum, s.moment);
-            s.sum *= scale;
-            s.most = most;
+            for (int u = 0; u < kUnroll; ++u) q[u].load(row + c + u * (kThreads * kPiece));
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float d = v[u][i] - most, e = exp_of(d);
-                    s.sum += e;
-                    if constexpr (ENTROPY) s.moment = __builtin_fmaf(fmaxf(d, kGone), e, s.moment);
-                }
+                for (int i = 0; i < 8; ++i) v[u][i] = q[u][i];
+        } else {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) load_logits(row, c + u * (kThreads * kPiece), end, v[u]);
         }
-        const Share all = over_workgroup(s, slots);
+        add_batch<ENTROPY, TOP>(v, c, s, most, seen, where);
+    }
+    move(s, most);                                      // to the thread's largest itself
+    const Share all = over_workgroup(s, slots);
+    if (a.splits == 1) {
+        if (threadIdx.x == 0) result = finish<T>(a, at, all);
+    } else if (threadIdx.x == 0) {
+        a.shares[item] = all;
+    }
+    if constexpr (TOP) {
+        find_top(row, c0, end, a.top, seen, where, lds, a.splits == 1 ? first : a.keys + item * a.top);
         if (a.splits == 1) {
-            if (threadIdx.x == 0) result = finish<T>(a, at, all);
-        } else if (threadIdx.x == 0) {
-            a.shares[item] = all;
-        }
-        if constexpr (TOP) {
-            uint64_t best = 0;
-            if (c0 + (int64_t)threadIdx.x * kPiece < c1) {
-                for (int u = 0; u < kUnroll; ++u) {
-                    const int64_t c = where + u * (kThreads * kPiece);
-                    if (c >= c1) break;
-                    float v[8];
-                    load_logits(row, c, c1, v);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint64_t k = key_of(v[i], (uint32_t)(c + i));
-                        if (k > best && c + i < c1) best = k;
-                    }
-                }
-            }
-            find_top(row, c0, c1, a.top, best, lds, a.splits == 1 ? first : a.keys + item * a.top);
-            if (a.splits == 1) {
-                __syncthreads();
-                const float lse = result;
-                if ((int)threadIdx.x < a.top) {
-                    const uint64_t k = first[threadIdx.x];
-                    a.top_ids[at * a.top + threadIdx.x] = column_of(k);
-                    a.top_logp[at * a.top + threadIdx.x] = logp_of_top(value_of(k), lse);
-                }
+            __syncthreads();
+            const float lse = result;
+            if ((int)threadIdx.x < a.top) {
+                const uint64_t k = first[threadIdx.x];
+                a.top_ids[at * a.top + threadIdx.x] = column_of(k);
+                a.top_logp[at * a.top + threadIdx.x] = logp_of_top(value_of(k), lse);
             }
         }
-        __syncthreads();                                    // before the next turn's slots
     }
 }
 
@@ -271,22 +352,40 @@ constexpr int kMostKeys = 1024;                             // splits * top
 template <typename T, bool TOP>
 __global__ __launch_bounds__(kThreads) void join_shares(LogpArgs a) {
     __shared__ float slots[3 * (kThreads / 64)];
-    __shared__ uint64_t keys[TOP ? kMostKeys : 1];
+    __shared__ uint64_t keys[TOP ? kMostKeys : 1], found[TOP ? kMostKeys : 1], bound;
+    __shared__ uint32_t count;
     __shared__ float result;
     for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
         const int t = threadIdx.x;
         const Share all = over_workgroup(t < a.splits ? a.shares[row * a.splits + t] : Share{kLowest, 0.0f, 0.0f}, slots);
         if (t == 0) result = finish<T>(a, row, all);
         if constexpr (TOP) {
-            const int n = a.splits * a.top;
+            // each share's keys are in order: of the first few of every share, `top` or more in all, the top-th bounds the row's top-th from
+            // below, and only what reaches the bound is put in order
+            const int n = a.splits * a.top, per = (a.top + a.splits - 1) / a.splits;
             for (int i = t; i < n; i += kThreads) keys[i] = a.keys[row * n + i];
+            if (t == 0) { count = 0; bound = 1; }
             __syncthreads();
             const float lse = result;
-            for (int i = t; i < n; i += kThreads) {
-                const uint64_t k = keys[i];
+            if (t < a.splits * per) {
+                const uint64_t k = keys[t / per * a.top + t % per];
                 int rank = 0;
-                for (int j = 0; j < n; ++j) rank += keys[j] > k;
-                if (k && rank < a.top) {
+                for (int l = 0; l < a.splits; ++l)
+                    for (int j = 0; j < per; ++j) rank += keys[l * a.top + j] > k;
+                if (k && rank == a.top - 1) bound = k;
+            }
+            __syncthreads();
+            const uint64_t least = bound;
+            for (int i = t; i < n; i += kThreads)
+                if (keys[i] >= least) found[atomicAdd(&count, 1u)] = keys[i];  // any order, put in order below
+            __syncthreads();
+            const int m = (int)count;
+            for (int i = t; i < m; i += kThreads) {
+                const uint64_t k = found[i];
+                int rank = 0;
+#pragma unroll 8
+                for (int j = 0; j < m; ++j) rank += found[j] > k;
+                if (rank < a.top) {
                     a.top_ids[row * a.top + rank] = column_of(k);
                     a.top_logp[row * a.top + rank] = logp_of_top(value_of(k), lse);
                 }
@@ -306,12 +405,24 @@ struct LogpBackArgs {
     int64_t stride, out_stride, T, V, ignore, parts;        // parts: of a row, kUnroll * kThreads pieces each
 };
 
+// Columns are counted from the 16-byte boundary at or before a row's first element, so that pieces are aligned in rows of any width too; the row's
+// are those from lo to end.  (Not in the forward pass, where it would make a row's last bits depend on where the row lies.)
+struct Span {
+    int lo, end;
+    __device__ __forceinline__ bool holds_piece(int c) const { return c >= lo && c + kPiece <= end; }
+};
+
 template <typename T, bool ENTROPY>
 __global__ __launch_bounds__(kThreads) void log_probs_back(LogpBackArgs a) {
     for (int64_t item = blockIdx.x; item < a.T * a.parts; item += gridDim.x) {
-        const int64_t at = item / a.parts, c0 = (item - at * a.parts) * (kUnroll * kThreads * kPiece) + (int64_t)threadIdx.x * kPiece;
+        const int64_t at = item / a.parts;
         const T* row = static_cast<const T*>(a.z) + at * a.stride;
         T* out = static_cast<T*>(a.out) + at * a.out_stride;
+        const int before = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)), b = (int)(item - at * a.parts) * kBatch, c0 = b + (int)threadIdx.x * kPiece;
+        const Span in{before, (int)a.V + before};
+        row -= before;
+        out -= before;
+        const bool whole = b >= before && b + kBatch <= in.end;
         const float lse = a.lse[at], h = ENTROPY ? a.entropy[at] : 0.0f, gh = ENTROPY ? a.gh[at] : 0.0f;
         const int64_t id = a.ids[at];
         const bool empty = lse == -__builtin_inff();
@@ -319,27 +430,38 @@ __global__ __launch_bounds__(kThreads) void log_probs_back(LogpBackArgs a) {
         if (id == a.ignore) g = 0.0f;
         else if (id < 0 || id >= a.V) g = __uint_as_float(0x7fc00000u);
         Piece<T> q[kUnroll];
+        if (whole) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) q[u] = load_piece(row, c0 + u * (kThreads * kPiece), a.V);
+            for (int u = 0; u < kUnroll; ++u) q[u].load(row + c0 + u * (kThreads * kPiece));
+        } else {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int c = c0 + u * (kThreads * kPiece);
+                if (in.holds_piece(c)) q[u].load(row + c);
+                else q[u].load(row + c, in.lo - c, in.end - c);
+            }
+        }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            const int64_t c = c0 + u * (kThreads * kPiece);
-            if (c >= a.V) break;
+            const int c = c0 + u * (kThreads * kPiece);
+            if (c >= in.end) break;
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = q[u][i] - lse, p = exp_of(d);
+                const float d = q[u][i] - lse, p = exp2_of(d * kLog2e);
                 v[i] = -p * (ENTROPY ? __builtin_fmaf(gh, fmaxf(d, kGone) + h, g) : g);
             }
-            if (id >= c && id < c + kPiece && id != a.ignore) {
+            const int64_t own = id + before - c;
+            if (own >= 0 && own < kPiece && id != a.ignore) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (id == c + i) v[i] += g;
+                for (int i = 0; i < 8; ++i) if (own == i) v[i] += g;
             }
             if (empty) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = 0.0f;
             }
-            store_piece(out, c, a.V, v);
+            if (whole || in.holds_piece(c)) Piece<T>::store(out + c, v);
+            else Piece<T>::store(out + c, v, in.lo - c, in.end - c);
         }
     }
 }
@@ -350,13 +472,14 @@ bool type_ok(division_dtype dt) { return dt == DIVISION_F32 || dt == DIVISION_BF
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP; }
 #define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
-constexpr int64_t kMostWorkgroups = 1 << 16;
+constexpr int64_t kMostItems = 1 << 23;                    // workgroups of a launch (which may have 2^32 threads)
+constexpr int64_t kMostWorkgroups = 1 << 16;               // of a launch whose workgroups take turns
 uint32_t grid_of(int64_t items) { return (uint32_t)(items < kMostWorkgroups ? items : kMostWorkgroups); }
 
 int sizes_ok(int64_t T, int64_t V, int64_t stride) {
     if (T < 0 || V < 1 || stride < 0) return DIVISION_EINVAL;
     const int64_t most = int64_t(1) << 40;
-    return T > INT32_MAX || V > INT32_MAX - 8 * 8192 || (T > 0 && (V > most / T || stride > most / T)) ? DIVISION_ERANGE : DIVISION_OK;
+    return T > INT32_MAX || V > INT32_MAX - 64 * kThreads * kPiece || (T > 0 && (V > most / T || stride > most / T)) ? DIVISION_ERANGE : DIVISION_OK;
 }
 
 // Shares of a row: few rows leave CUs idle
@@ -371,13 +494,18 @@ Split split_of(int64_t T, int64_t V, int top) {
     return {(int)((V + columns - 1) / columns), columns};
 }
 
-template <typename T> void launch_log_probs(const LogpArgs& a, hipStream_t st) {
+template <typename T> int launch_log_probs(LogpArgs a, hipStream_t st) {
     void (*kern)(LogpArgs) = a.top ? (a.entropy ? log_probs<T, true, true> : log_probs<T, false, true>)
                                    : (a.entropy ? log_probs<T, true, false> : log_probs<T, false, false>);
-    hipLaunchKernelGGL(kern, dim3(grid_of(a.T * a.splits)), dim3(kThreads), 0, st, a);
-    if (a.splits == 1) return;
+    for (a.first = 0; a.first < a.T * a.splits; a.first += kMostItems) {
+        const int64_t items = a.T * a.splits - a.first;
+        hipLaunchKernelGGL(kern, dim3((uint32_t)(items < kMostItems ? items : kMostItems)), dim3(kThreads), 0, st, a);
+        CHECKED(launched());
+    }
+    if (a.splits == 1) return DIVISION_OK;
     kern = a.top ? join_shares<T, true> : join_shares<T, false>;
     hipLaunchKernelGGL(kern, dim3(grid_of(a.T)), dim3(kThreads), 0, st, a);
+    return launched();
 }
 
 }  // namespace
@@ -407,9 +535,8 @@ int division_log_probs(const division_logits* n, void* hip_stream) {
     a.keys = static_cast<uint64_t*>(n->workspace);
     a.shares = reinterpret_cast<Share*>(static_cast<char*>(n->workspace) + (size_t)n->T * s.splits * n->top * 8u);
     a.stride = n->stride; a.T = n->T; a.V = n->V; a.ignore = n->ignore_index; a.split = s.columns; a.splits = s.splits; a.top = n->top;
-    if (n->dt == DIVISION_F32) launch_log_probs<float>(a, static_cast<hipStream_t>(hip_stream));
-    else launch_log_probs<uint16_t>(a, static_cast<hipStream_t>(hip_stream));
-    return launched();
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    return n->dt == DIVISION_F32 ? launch_log_probs<float>(a, st) : launch_log_probs<uint16_t>(a, st);
 }
 
 int division_log_probs_backward(const division_logits_back* n, void* hip_stream) {
@@ -426,7 +553,7 @@ int division_log_probs_backward(const division_logits_back* n, void* hip_stream)
     LogpBackArgs a{};
     a.z = n->logits; a.ids = n->ids; a.lse = n->lse; a.entropy = n->entropy; a.g = n->grad_logp; a.gh = n->grad_entropy; a.out = n->grad_logits;
     a.stride = n->stride; a.out_stride = n->grad_stride; a.T = n->T; a.V = n->V; a.ignore = n->ignore_index;
-    a.parts = (n->V + kUnroll * kThreads * kPiece - 1) / (kUnroll * kThreads * kPiece);
+    a.parts = (n->V + kPiece - 1 + kBatch - 1) / kBatch;                    // with the columns before a row's first
     void (*kern)(LogpBackArgs) = n->dt == DIVISION_F32 ? (a.gh ? log_probs_back<float, true> : log_probs_back<float, false>)
                                                       : (a.gh ? log_probs_back<uint16_t, true> : log_probs_back<uint16_t, false>);
     hipLaunchKernelGGL(kern, dim3(grid_of(a.T * a.parts)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), a);

@@ -21,27 +21,28 @@ template <typename T> struct Piece;
 template <> struct Piece<float> {
     u32x4 w[2];
     __device__ __forceinline__ void load(const float* p) { __builtin_memcpy(w, p, 32); }
-    __device__ __forceinline__ void load(const float* p, int n) {
+    // its elements lo .. hi - 1 alone, zeros beside them
+    __device__ __forceinline__ void load(const float* p, int lo, int hi) {
         uint32_t* e = reinterpret_cast<uint32_t*>(w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i < n ? __float_as_uint(p[i]) : 0u;
+        for (int i = 0; i < 8; ++i) e[i] = i >= lo && i < hi ? __float_as_uint(p[i]) : 0u;
     }
     __device__ __forceinline__ void zero() { w[0] = u32x4{0, 0, 0, 0}; w[1] = w[0]; }
     __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i / 4][i % 4]); }
     static __device__ __forceinline__ void store(float* p, const float* v) { __builtin_memcpy(p, v, 32); }
-    static __device__ __forceinline__ void store(float* p, const float* v, int n) {
+    static __device__ __forceinline__ void store(float* p, const float* v, int lo, int hi) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) p[i] = v[i];
+        for (int i = 0; i < 8; ++i) if (i >= lo && i < hi) p[i] = v[i];
     }
 };
 template <> struct Piece<uint16_t> {
     u32x4 w;
     __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(&w, p, 16); }
-    __device__ __forceinline__ void load(const uint16_t* p, int n) {
+    __device__ __forceinline__ void load(const uint16_t* p, int lo, int hi) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = 2 * i < n ? p[2 * i] : 0u, hi = 2 * i + 1 < n ? p[2 * i + 1] : 0u;
-            w[i] = lo | hi << 16;
+            const uint32_t even = 2 * i >= lo && 2 * i < hi ? p[2 * i] : 0u, odd = 2 * i + 1 >= lo && 2 * i + 1 < hi ? p[2 * i + 1] : 0u;
+            w[i] = even | odd << 16;
         }
     }
     __device__ __forceinline__ void zero() { w = u32x4{0, 0, 0, 0}; }
@@ -50,23 +51,23 @@ template <> struct Piece<uint16_t> {
         return u32x4{bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]), bf16_pack2(v[4], v[5]), bf16_pack2(v[6], v[7])};
     }
     static __device__ __forceinline__ void store(uint16_t* p, const float* v) { const u32x4 q = packed(v); __builtin_memcpy(p, &q, 16); }
-    static __device__ __forceinline__ void store(uint16_t* p, const float* v, int n) {
+    static __device__ __forceinline__ void store(uint16_t* p, const float* v, int lo, int hi) {
         const u32x4 q = packed(v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) p[i] = (uint16_t)(q[i / 2] >> (i & 1 ? 16 : 0));
+        for (int i = 0; i < 8; ++i) if (i >= lo && i < hi) p[i] = (uint16_t)(q[i / 2] >> (i & 1 ? 16 : 0));
     }
 };
 // The piece of a row that starts at column c of D: whole, the row's last, or behind its end (zeros, nothing stored).  C: int where c + 8 fits it, else int64_t
 template <typename T, typename C> __device__ __forceinline__ Piece<T> load_piece(const T* row, C c, C D) {
     Piece<T> q;
     if (c + kPiece <= D) q.load(row + c);
-    else if (c < D) q.load(row + c, (int)(D - c));
+    else if (c < D) q.load(row + c, 0, (int)(D - c));
     else q.zero();
     return q;
 }
 template <typename T, typename C> __device__ __forceinline__ void store_piece(T* row, C c, C D, const float* v) {
     if (c + kPiece <= D) Piece<T>::store(row + c, v);
-    else if (c < D) Piece<T>::store(row + c, v, (int)(D - c));
+    else if (c < D) Piece<T>::store(row + c, v, 0, (int)(D - c));
 }
 
 // Reductions over aligned groups of lanes by DPP (no LDS, no waits): every lane gets the result.  Within 16 lanes the four steps pair each lane with
