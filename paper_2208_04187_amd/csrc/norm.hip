@@ -122,7 +122,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_rows(NormArgs a) {
     int turn = 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) load_weight(a.weight, a.weight_bf16, (r * NT + lane) * kPiece, D, w[r]);
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / NT; row < a.T; row += (int64_t)gridDim.x * ROWS) {
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + row_of_thread<NT>(); row < a.T; row += (int64_t)gridDim.x * ROWS) {
         float v[R][8], sq = 0.0f;
 #pragma unroll
         for (int r = 0; r < R; ++r) load_sum<T, RES>(a, row, (r * NT + lane) * kPiece, D, v[r]);
@@ -249,26 +249,39 @@ struct BackArgs {
     int weight_bf16;
 };
 
-// dx of a piece from u = dy * w and n = s * rstd, whose mean product over the row is `along`
-template <typename T, typename C>
-__device__ __forceinline__ void store_dx(const BackArgs& a, int64_t row, C c, C D, float rstd, float along, const float* u, const float* n) {
-    float d[8];
+// What a thread reads of a row
+template <typename T, int R> struct BackRow {
+    Piece<T> grad[R], s[R], extra[R];
+    float rstd;
+    template <int NT> __device__ __forceinline__ void load(const BackArgs& a, int64_t row, int lane, int D) {
+        if (row >= a.T) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) d[i] = rstd * __builtin_fmaf(-n[i], along, u[i]);
-    if (a.grad_sum) {
-        const Piece<T> q = load_piece(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, c, D);
+            for (int r = 0; r < R; ++r) { grad[r].zero(); s[r].zero(); }
+            rstd = 0.0f;
+            return;
+        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] += q[i];
+        for (int r = 0; r < R; ++r) {
+            const int c = (r * NT + lane) * kPiece;
+            grad[r] = load_piece(static_cast<const T*>(a.grad) + row * a.grad_stride, c, D);
+            s[r] = load_piece(static_cast<const T*>(a.s) + row * a.s_stride, c, D);
+        }
+        if (a.grad_sum) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) extra[r] = load_piece(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, (r * NT + lane) * kPiece, D);
+        }
+        rstd = a.rstd[row];
     }
-    store_piece(static_cast<T*>(a.dx) + row * a.D, c, D, d);
-}
+};
 
-// A row per NT threads as in norm_rows; dw grows in the registers of the thread that owns its columns, over all rows of the workgroup.
-template <typename T, int NT, int R>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_back_rows(BackArgs a) {
-    constexpr int ROWS = NT < 256 ? 256 / NT : 1;
-    __shared__ uint32_t slots[NT > 64 ? 2 * (NT / 64) : 1];
-    __shared__ float shares[ROWS > 1 ? ROWS * NT * R * 8 : 1];
+// A row per NT threads as in norm_rows, THREADS / NT rows a workgroup side by side; dw grows in the registers of the thread that owns its columns over all
+// rows of the workgroup, whose sums meet in LDS at the end: large workgroups leave few shares to add up.  Where the registers hold it (AHEAD), a
+// row is loaded while the one before it is worked on.
+template <typename T, int NT, int R, int THREADS, bool AHEAD>
+__global__ __launch_bounds__(THREADS) void norm_back_rows(BackArgs a) {
+    constexpr int ROWS = THREADS / NT;
+    __shared__ uint32_t slots[NT > 64 ? 2 * (THREADS / 64) : 1];
+    __shared__ float shares[ROWS > 1 ? THREADS * kPiece : 1];
     const int lane = threadIdx.x % NT, D = (int)a.D;
     float w[R][8], dw[R][8];
 #pragma unroll
@@ -278,45 +291,58 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_back_rows(BackArgs a
         for (int i = 0; i < 8; ++i) dw[r][i] = 0.0f;
     }
     int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / NT; row < a.T; row += (int64_t)gridDim.x * ROWS) {
-        const float rstd = a.rstd[row];
-        float u[R][8], n[R][8], dot = 0.0f;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int c = (r * NT + lane) * kPiece;
-            const Piece<T> g = load_piece(static_cast<const T*>(a.grad) + row * a.grad_stride, c, D);
-            const Piece<T> s = load_piece(static_cast<const T*>(a.s) + row * a.s_stride, c, D);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                n[r][i] = s[i] * rstd;
-                u[r][i] = g[i] * w[r][i];
-                dot = __builtin_fmaf(u[r][i], n[r][i], dot);
-                dw[r][i] = __builtin_fmaf(g[i], n[r][i], dw[r][i]);
-            }
-        }
-        const float along = row_sum<NT>(dot, slots + turn) / (float)a.D;
-        if constexpr (NT > 64) turn ^= NT / 64;
-#pragma unroll
-        for (int r = 0; r < R; ++r) store_dx<T>(a, row, (r * NT + lane) * kPiece, D, rstd, along, u[r], n[r]);
-    }
-    float* part = a.parts + (int64_t)blockIdx.x * a.D;
-    if constexpr (ROWS > 1) {                               // the workgroup's rows: added up in their order
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    BackRow<T, R> q;
+    q.template load<NT>(a, (int64_t)blockIdx.x * ROWS + row_of_thread<NT>(), lane, D);
+    for (int64_t base = (int64_t)blockIdx.x * ROWS; base < a.T; base += step) {
+        const int64_t row = base + row_of_thread<NT>();
+        BackRow<T, R> next;
+        if constexpr (AHEAD) next.template load<NT>(a, row + step, lane, D);
+        float dot = 0.0f;
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) shares[((threadIdx.x / NT) * R + r) * (NT * 8) + i * NT + lane] = dw[r][i];
-        __syncthreads();
-        for (int j = threadIdx.x; j < NT * R * 8; j += 256) {
-            const int r = j / (NT * 8), i = j % (NT * 8) / NT, l = j % NT;
-            const int c = (r * NT + l) * kPiece + i;
-            float t = 0.0f;
+            for (int i = 0; i < 8; ++i) {
+                const float n = q.s[r][i] * q.rstd, g = q.grad[r][i];
+                dot = __builtin_fmaf(g * w[r][i], n, dot);
+                dw[r][i] = __builtin_fmaf(g, n, dw[r][i]);
+            }
+        const float along = row_sum<NT>(dot, slots + turn) / (float)a.D;
+        if constexpr (NT > 64) turn ^= THREADS / 64;
+        if (row < a.T) {
 #pragma unroll
-            for (int k = 0; k < ROWS; ++k) t += shares[k * (R * NT * 8) + j];
-            if (c < D) part[c] = t;
+            for (int r = 0; r < R; ++r) {
+                float d[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] = q.rstd * __builtin_fmaf(-(q.s[r][i] * q.rstd), along, q.grad[r][i] * w[r][i]);
+                if (a.grad_sum) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] += q.extra[r][i];
+                }
+                store_piece(static_cast<T*>(a.dx) + row * a.D, (r * NT + lane) * kPiece, D, d);
+            }
         }
-    } else {
+        if constexpr (AHEAD) q = next;
+        else q.template load<NT>(a, row + step, lane, D);
+    }
+    float* part = a.parts + (int64_t)blockIdx.x * a.D;
 #pragma unroll
-        for (int r = 0; r < R; ++r) store_piece(part, (r * NT + lane) * kPiece, D, dw[r]);
+    for (int r = 0; r < R; ++r) {
+        if constexpr (ROWS > 1) {                           // the workgroup's rows: added up in their order
+            if (r) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) shares[threadIdx.x / NT * (NT * 8) + i * NT + lane] = dw[r][i];
+            __syncthreads();
+            for (int j = threadIdx.x; j < NT * 8; j += THREADS) {
+                const int c = (r * NT + j % NT) * kPiece + j / NT;
+                float t = 0.0f;
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) t += shares[k * (NT * 8) + j];
+                if (c < D) part[c] = t;
+            }
+        } else {
+            store_piece(part, (r * NT + lane) * kPiece, D, dw[r]);
+        }
     }
 }
 
@@ -352,7 +378,15 @@ __global__ __launch_bounds__(1024) void norm_back_wide(BackArgs a) {
                 u[i] = p[i] * w[i];
                 dw[i] = __builtin_fmaf(p[i], n[i], first ? 0.0f : had[i]);
             }
-            store_dx<T>(a, row, c, a.D, rstd, along, u, n);
+            float d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = rstd * __builtin_fmaf(-n[i], along, u[i]);
+            if (a.grad_sum) {
+                const Piece<T> extra = load_piece(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, c, a.D);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] += extra[i];
+            }
+            store_piece(static_cast<T*>(a.dx) + row * a.D, c, a.D, d);
             store_piece(part, c, a.D, dw);
         }
         first = false;
@@ -401,46 +435,37 @@ int stride_ok(int64_t stride, int64_t T) {
 
 int shift_of(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
 
-constexpr int64_t kMostInRegisters = 16384;                // elements of a row (more of them spill at 1024 threads)
 constexpr int64_t kMostWorkgroups = 2048;
 
-// threads a row and pieces a thread for rows of D
-#define WITH_ROWS(D, CALL)                  \
-    if ((D) <= 128) CALL(16, 1);            \
-    else if ((D) <= 512) CALL(64, 1);       \
-    else if ((D) <= 1024) CALL(64, 2);      \
-    else if ((D) <= 2048) CALL(256, 1);     \
-    else if ((D) <= 4096) CALL(256, 2);     \
-    else if ((D) <= 8192) CALL(256, 4);     \
-    else CALL(1024, 2)
-
+// The forward pass: threads a row and pieces a thread.  Up to 1024 columns a row is one wavefront's, which needs no barrier.
 template <typename T, bool RES> void launch_norm(const NormArgs& a, hipStream_t st) {
-    if (a.D > kMostInRegisters) {
-        hipLaunchKernelGGL((norm_wide<T, RES>), dim3((uint32_t)(a.T < kMostWorkgroups ? a.T : kMostWorkgroups)), dim3(1024), 0, st, a);
-        return;
+    const int64_t D = a.D;
+    void (*kern)(NormArgs) = D <= 128 ? norm_rows<T, 16, 1, RES> : D <= 512 ? norm_rows<T, 64, 1, RES> : D <= 1024 ? norm_rows<T, 64, 2, RES>
+                           : D <= 2048 ? norm_rows<T, 256, 1, RES> : D <= 4096 ? norm_rows<T, 256, 2, RES> : D <= 8192 ? norm_rows<T, 256, 4, RES>
+                           : D <= 16384 ? norm_rows<T, 1024, 2, RES> : norm_wide<T, RES>;
+    if constexpr (sizeof(T) == 2 || !RES) {                 // (fp32 with a residual would spill)
+        if (D > 16384 && D <= 32768) kern = norm_rows<T, 1024, 4, RES>;
     }
-#define CALL(NT, R) do { \
-        const int64_t rows = NT < 256 ? 256 / NT : 1, grid = (a.T + rows - 1) / rows; \
-        hipLaunchKernelGGL((norm_rows<T, NT, R, RES>), dim3((uint32_t)(grid < kMostWorkgroups ? grid : kMostWorkgroups)), dim3(NT < 256 ? 256 : NT), 0, st, a); \
-    } while (0)
-    WITH_ROWS(a.D, CALL);
-#undef CALL
+    const int64_t rows = D <= 128 ? 16 : D <= 1024 ? 4 : 1, grid = (a.T + rows - 1) / rows;
+    hipLaunchKernelGGL(kern, dim3((uint32_t)(grid < kMostWorkgroups ? grid : kMostWorkgroups)), dim3(D <= 8192 ? 256 : 1024), 0, st, a);
 }
 
+// The backward pass: workgroups of 1024 threads, one a CU, so that few shares of dw are left to add up (16384 x 512 bfloat16: 14.6 us, 17.6 with four
+// times as many of 256 threads; 8191 x 2561 fp32 68 either way).  A piece a thread and the next row's loads ahead of the work, except from 513 to 1024 columns, where
+// two pieces on one wavefront need no barriers and leave fewer lanes idle (16384 x 768 bfloat16 26.4 -> 20.8 us), and beyond 8192.
+constexpr int kBackThreads = 1024;
 int64_t back_workgroups(int64_t T, int64_t D) {
-    const int64_t rows = D <= 128 ? 16 : D <= 1024 ? 4 : 1, grid = (T + rows - 1) / rows, most = D <= 8192 ? 512 : 256;
+    const int rows = kBackThreads / (D <= 128 ? 16 : D <= 1024 ? 64 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024);
+    const int64_t grid = (T + rows - 1) / rows, most = 256;
     return grid < most ? grid : most;
 }
 
 template <typename T> void launch_back(const BackArgs& a, hipStream_t st) {
-    const uint32_t grid = (uint32_t)back_workgroups(a.T, a.D);
-    if (a.D > kMostInRegisters) {
-        hipLaunchKernelGGL((norm_back_wide<T>), dim3(grid), dim3(1024), 0, st, a);
-        return;
-    }
-#define CALL(NT, R) hipLaunchKernelGGL((norm_back_rows<T, NT, R>), dim3(grid), dim3(NT < 256 ? 256 : NT), 0, st, a)
-    WITH_ROWS(a.D, CALL);
-#undef CALL
+    void (*kern)(BackArgs) = a.D <= 128 ? norm_back_rows<T, 16, 1, kBackThreads, true> : a.D <= 512 ? norm_back_rows<T, 64, 1, kBackThreads, true>
+                           : a.D <= 1024 ? norm_back_rows<T, 64, 2, kBackThreads, false> : a.D <= 2048 ? norm_back_rows<T, 256, 1, kBackThreads, true>
+                           : a.D <= 4096 ? norm_back_rows<T, 512, 1, kBackThreads, true> : a.D <= 8192 ? norm_back_rows<T, 1024, 1, kBackThreads, true>
+                           : a.D <= 16384 ? norm_back_rows<T, 1024, 2, kBackThreads, false> : norm_back_wide<T>;
+    hipLaunchKernelGGL(kern, dim3((uint32_t)back_workgroups(a.T, a.D)), dim3(kBackThreads), 0, st, a);
 }
 
 }  // namespace

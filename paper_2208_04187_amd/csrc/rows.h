@@ -89,8 +89,15 @@ template <typename Op, int LANES> __device__ __forceinline__ uint32_t over_lanes
 }
 template <int LANES> __device__ __forceinline__ float sum_lanes(float v) { return __uint_as_float(over_lanes<AddF, LANES>(__float_as_uint(v))); }
 
-// A value of a row over the NT threads that share it: NT up to 64 lanes of a wavefront, or whole wavefronts through `slots` (one per wavefront, two
-// sets that calls take in turn, so that a call needs one barrier; the caller's first call on a row follows the last row's by two)
+// Which of a workgroup's rows, NT threads each, the thread works on; the same for all of a wavefront where it has one, and then in a scalar register: the
+// row's addresses take no vector registers
+template <int NT> __device__ __forceinline__ int row_of_thread() {
+    if constexpr (NT >= 64) return __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
+    else return (int)threadIdx.x / NT;
+}
+
+// A value of a row over the NT threads that share it: NT up to 64 lanes of a wavefront, or whole wavefronts through `slots`, one per wavefront of the
+// workgroup (which may hold several rows; all of it takes part).  One barrier: the next call but one may take the same slots again.
 template <typename Op, int NT> __device__ __forceinline__ uint32_t over_row(uint32_t v, uint32_t* slots) {
     if constexpr (NT <= 64) {
         return over_lanes<Op, NT>(v);
@@ -99,9 +106,10 @@ template <typename Op, int NT> __device__ __forceinline__ uint32_t over_row(uint
         v = over_lanes<Op, 64>(v);
         if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
         __syncthreads();
-        uint32_t r = slots[0];
+        const uint32_t* own = slots + threadIdx.x / NT * W;
+        uint32_t r = own[0];
 #pragma unroll
-        for (int i = 1; i < W; ++i) r = Op::of(r, slots[i]);
+        for (int i = 1; i < W; ++i) r = Op::of(r, own[i]);
         return r;
     }
 }
