@@ -15,39 +15,44 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;
-constexpr int64_t kRun = kThreads * kUnroll * kPiece;      // elements of a run: 8192
+constexpr int kRun = kThreads * kUnroll * kPiece;          // elements of a run: 8192
 
-// The tensors of a launch: their first element, where they go (clipping), their number of elements, and the first of their runs counted
-// through the launch
-template <int N> struct Table {
+// The tensors of a launch: their first element and, for the clipping, where they go; the first of their runs, counted through the launch; how many elements
+// their last run has, and their types in the bits above.  The argument block of a launch may have 4 KB.
+constexpr uint32_t kElements = 0x3fff, kInBf16 = 0x4000, kOutBf16 = 0x8000;
+template <int N> struct Sources {
+    static constexpr int kMost = N;
     const void* in[N];
-    void* out[N];
-    int64_t n[N];
     uint32_t first[N];
-    uint32_t type[N];                                       // bit 0: in is bfloat16, bit 1: out is
+    uint16_t last[N];
     uint32_t runs;                                          // of all
     int count;
 };
-constexpr int kTensors = 120;                               // 32 bytes each: within 4 KB of arguments
-struct NormArgs { Table<kTensors> t; double* parts; };
-struct ClipArgs { Table<kTensors> t; const float* factor; };
+template <int N> struct Targets { void* out[N]; };
+struct NormArgs { Sources<288> t; double* parts; };
+struct ClipArgs { Sources<184> t; Targets<184> to; const double* parts; const float* factor; float* norm; float limit; int count; };
 static_assert(sizeof(NormArgs) <= 4096 && sizeof(ClipArgs) <= 4096, "kernel arguments");
 
-template <int N> __device__ __forceinline__ int tensor_of(const Table<N>& t, uint32_t run) {
-    int lo = 0, hi = t.count;                               // the last tensor whose first run is not behind `run`
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (t.first[mid] <= run) lo = mid;
+// the tensor of a run: the last one whose first run is not behind it, from tensor k on
+template <typename S> __device__ __forceinline__ int tensor_of(const S& t, uint32_t run, int k) {
+    int hi = t.count;
+    while (hi - k > 1) {
+        const int mid = (k + hi) / 2;
+        if (t.first[mid] <= run) k = mid;
         else hi = mid;
     }
-    return lo;
+    return k;
+}
+template <typename S> __device__ __forceinline__ int elements_of(const S& t, uint32_t run, int k) {
+    const uint32_t end = k + 1 < t.count ? t.first[k + 1] : t.runs;
+    return run + 1 < end ? kRun : (int)(t.last[k] & kElements);
 }
 
-template <typename T> __device__ __forceinline__ double squares(const T* p, int64_t c, int64_t n) {
+template <typename T> __device__ __forceinline__ double squares(const T* p, int n) {
     double s = 0.0;
     Piece<T> q[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) q[u] = load_piece(p, c + u * (kThreads * kPiece), n);
+    for (int u = 0; u < kUnroll; ++u) q[u] = load_piece(p, (u * kThreads + (int)threadIdx.x) * kPiece, n);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
@@ -58,13 +63,14 @@ template <typename T> __device__ __forceinline__ double squares(const T* p, int6
     return s;
 }
 
-__device__ __forceinline__ double over_workgroup(double v, double* slots, int waves) {
+template <int THREADS> __device__ __forceinline__ double over_workgroup(double v, double* slots) {
 #pragma unroll
     for (int m = 32; m > 0; m /= 2) v += __shfl_xor(v, m, 64);
     if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
     __syncthreads();
     v = slots[0];
-    for (int i = 1; i < waves; ++i) v += slots[i];
+#pragma unroll
+    for (int i = 1; i < THREADS / 64; ++i) v += slots[i];
     return v;
 }
 
@@ -72,63 +78,113 @@ __device__ __forceinline__ double over_workgroup(double v, double* slots, int wa
 __global__ __launch_bounds__(kThreads) void add_squares(NormArgs a) {
     __shared__ double slots[kThreads / 64];
     double s = 0.0;
+    int k = 0;
     for (uint32_t run = blockIdx.x; run < a.t.runs; run += gridDim.x) {
-        const int k = tensor_of(a.t, run);
-        const int64_t c = (int64_t)(run - a.t.first[k]) * kRun + (int64_t)threadIdx.x * kPiece;
-        s += a.t.type[k] & 1 ? squares(static_cast<const uint16_t*>(a.t.in[k]), c, a.t.n[k]) : squares(static_cast<const float*>(a.t.in[k]), c, a.t.n[k]);
+        k = tensor_of(a.t, run, k);
+        const int64_t c = (int64_t)(run - a.t.first[k]) * kRun;
+        const int n = elements_of(a.t, run, k);
+        s += a.t.last[k] & kInBf16 ? squares(static_cast<const uint16_t*>(a.t.in[k]) + c, n) : squares(static_cast<const float*>(a.t.in[k]) + c, n);
     }
-    s = over_workgroup(s, slots, kThreads / 64);
+    s = over_workgroup<kThreads>(s, slots);
     if (threadIdx.x == 0) a.parts[blockIdx.x] = s;
 }
 
-// The norm from the parts, and the factor of the clipping (null: only the norm)
+// The factor of the clipping, in two: the second is 1, or a power of two where the first alone would leave binary32's normal range
+struct Factor { float f, power; };
+__device__ __forceinline__ Factor factor_of(double norm, float limit) {
+    double c = limit / (norm + 1e-6);
+    c = c > 1.0 ? 1.0 : c;                                  // NaN stays
+    const bool small = c < 0x1p-100;
+    return {(float)(small ? c * 0x1p126 : c), small ? 0x1p-126f : 1.0f};
+}
+
+// The norm from the parts, and the factor (null: only the norm)
 __global__ __launch_bounds__(1024) void join_squares(const double* parts, int64_t count, float limit, float* norm, float* factor) {
     __shared__ double slots[16];
     double s = 0.0;
     for (int64_t i = threadIdx.x; i < count; i += 1024) s += parts[i];
-    s = over_workgroup(s, slots, 16);
+    s = over_workgroup<1024>(s, slots);
     if (threadIdx.x == 0) {
         const double n = sqrt(s);
         *norm = (float)n;
         if (factor) {
-            // in two factors: the second is 1, or a power of two where the first alone would leave binary32's normal range
-            double c = limit / (n + 1e-6);
-            c = c > 1.0 ? 1.0 : c;                          // NaN stays
-            const bool small = c < 0x1p-100;
-            factor[0] = (float)(small ? c * 0x1p126 : c);
-            factor[1] = small ? 0x1p-126f : 1.0f;
+            const Factor c = factor_of(n, limit);
+            factor[0] = c.f;
+            factor[1] = c.power;
         }
     }
 }
 
-template <typename I, typename O> __device__ __forceinline__ void scale(const I* p, O* o, int64_t c, int64_t n, float f, float power) {
-    Piece<I> q[kUnroll];
+// Four elements a lane and access, so that the lanes' stores lie next to one another whatever the two types are (eight of fp32 are two stores with gaps: 336 M
+// gradients 641 us, 491 with four).  Stores go past the caches, which keep what the first pass has read of the gradients instead: 459 us, and of 25.6 M gradients 38 us
+// instead of 46.
+template <typename T> struct Four;
+template <> struct Four<float> {
+    u32x4 w;
+    __device__ __forceinline__ void load(const float* p) { __builtin_memcpy(&w, p, 16); }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i]); }
+    static __device__ __forceinline__ void store(float* p, const float* v) { store_past(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}); }
+};
+template <> struct Four<uint16_t> {
+    u32x2 w;
+    __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(&w, p, 8); }
+    __device__ __forceinline__ float operator[](int i) const { return i & 1 ? __uint_as_float(w[i / 2] & 0xffff0000u) : bf16_value(w[i / 2]); }
+    static __device__ __forceinline__ void store(uint16_t* p, const float* v) {
+        store_past(p, u32x2{bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3])});
+    }
+};
+__device__ __forceinline__ float value(const float* p) { return *p; }
+__device__ __forceinline__ float value(const uint16_t* p) { return bf16_value(*p); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(uint16_t* p, float v) { *p = (uint16_t)bf16_pack2(v, 0.0f); }
+
+// A run of n elements
+template <typename I, typename O> __device__ __forceinline__ void scale(const I* p, O* o, int n, float f, float power) {
+    constexpr int U = (int)(kRun / (kThreads * 4));
+    if (n == kRun) {
+        Four<I> q[U];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) q[u] = load_piece(p, c + u * (kThreads * kPiece), n);
+        for (int u = 0; u < U; ++u) q[u].load(p + (u * kThreads + threadIdx.x) * 4);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        float v[8];
+        for (int u = 0; u < U; ++u) {
+            float v[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = q[u][i] * f * power;
-        store_piece(o, c + u * (kThreads * kPiece), n, v);
+            for (int i = 0; i < 4; ++i) v[i] = q[u][i] * f * power;
+            Four<O>::store(o + (u * kThreads + threadIdx.x) * 4, v);
+        }
+    } else {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n; i += kThreads) put(o + i, value(p + i) * f * power);
     }
 }
 
-// Every tensor times the factor; one that stays where it is under a factor of 1 is not touched
+// Every tensor times the factor, a run a workgroup; one that stays where it is under a factor of 1 is not touched.  JOIN: every workgroup adds up the
+// parts itself, in the same order, instead of a launch between the two passes.
+template <bool JOIN>
 __global__ __launch_bounds__(kThreads) void scale_all(ClipArgs a) {
-    const float f = a.factor[0], power = a.factor[1];
-    for (uint32_t run = blockIdx.x; run < a.t.runs; run += gridDim.x) {
-        const int k = tensor_of(a.t, run);
-        if (f == 1.0f && power == 1.0f && a.t.in[k] == a.t.out[k]) continue;
-        const int64_t c = (int64_t)(run - a.t.first[k]) * kRun + (int64_t)threadIdx.x * kPiece, n = a.t.n[k];
-        const void* in = a.t.in[k];
-        void* out = a.t.out[k];
-        switch (a.t.type[k]) {
-            case 0: scale(static_cast<const float*>(in), static_cast<float*>(out), c, n, f, power); break;
-            case 1: scale(static_cast<const uint16_t*>(in), static_cast<float*>(out), c, n, f, power); break;
-            case 2: scale(static_cast<const float*>(in), static_cast<uint16_t*>(out), c, n, f, power); break;
-            default: scale(static_cast<const uint16_t*>(in), static_cast<uint16_t*>(out), c, n, f, power);
-        }
+    Factor f;
+    if constexpr (JOIN) {
+        __shared__ double slots[kThreads / 64];
+        double s = 0.0;
+        for (int i = threadIdx.x; i < a.count; i += kThreads) s += a.parts[i];
+        const double norm = sqrt(over_workgroup<kThreads>(s, slots));
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
+        f = factor_of(norm, a.limit);
+    } else {
+        f = {a.factor[0], a.factor[1]};
+    }
+    const uint32_t run = blockIdx.x;
+    const int k = tensor_of(a.t, run, 0);
+    const void* in = a.t.in[k];
+    void* out = a.to.out[k];
+    if (f.f == 1.0f && f.power == 1.0f && in == out) return;
+    const int64_t c = (int64_t)(run - a.t.first[k]) * kRun;
+    const int n = elements_of(a.t, run, k);
+    switch (a.t.last[k] & (kInBf16 | kOutBf16)) {
+        case 0: scale(static_cast<const float*>(in) + c, static_cast<float*>(out) + c, n, f.f, f.power); break;
+        case kInBf16: scale(static_cast<const uint16_t*>(in) + c, static_cast<float*>(out) + c, n, f.f, f.power); break;
+        case kOutBf16: scale(static_cast<const float*>(in) + c, static_cast<uint16_t*>(out) + c, n, f.f, f.power); break;
+        default: scale(static_cast<const uint16_t*>(in) + c, static_cast<uint16_t*>(out) + c, n, f.f, f.power);
     }
 }
 
@@ -139,8 +195,11 @@ bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % 
 int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP; }
 #define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
 
-constexpr uint32_t kMostWorkgroups = 2048;                  // of a launch
-constexpr uint32_t kMostRuns = 1u << 27;                    // of a launch: 2^40 elements
+constexpr uint32_t kMostParts = 2048;                       // workgroups of a launch of add_squares
+constexpr uint32_t kMostRuns = 1u << 23;                    // of a launch: 2^31 threads
+// Up to so many runs every workgroup of the second pass adds up the parts of the first, which saves a launch (1 M gradients 10.4 -> 8.2 us); of 3200 runs it
+// costs as much as it saves, of many more 10 us.
+constexpr int64_t kFewRuns = 2048;
 
 int check(int64_t count, const division_gradient* g, bool clip) {
     if (count < 0 || (count > 0 && !g)) return DIVISION_EINVAL;
@@ -154,31 +213,33 @@ int check(int64_t count, const division_gradient* g, bool clip) {
     return DIVISION_OK;
 }
 
-// The launches of a list: calls f(table) for each; tensors without elements are left out
-template <typename F> int launches(int64_t count, const division_gradient* g, F&& f) {
-    Table<kTensors> t;
+// The launches of a list: calls f(sources) for each, put(place, gradient, element) for each tensor of it.  Tensors without elements are left out, ones of more runs than a launch
+// has take several places.
+template <int N, typename P, typename F> int launches(int64_t count, const division_gradient* g, Sources<N>& t, P&& put, F&& f) {
     t.count = 0;
     t.runs = 0;
-    for (int64_t i = 0; i <= count; ++i) {
-        if (i < count && g[i].n == 0) continue;
-        const uint32_t runs = i < count ? (uint32_t)((g[i].n + kRun - 1) / kRun) : 0;
-        if (t.count > 0 && (i == count || t.count == kTensors || t.runs + runs > kMostRuns)) {
-            CHECKED(f(t));
-            t.count = 0;
-            t.runs = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        const uint32_t types = (g[i].dt == DIVISION_BF16 ? kInBf16 : 0u) | (g[i].out_dt == DIVISION_BF16 ? kOutBf16 : 0u);
+        for (int64_t from = 0; from < g[i].n;) {
+            if (t.count == N || t.runs == kMostRuns) {
+                CHECKED(f(t));
+                t.count = 0;
+                t.runs = 0;
+            }
+            const int64_t left = g[i].n - from, room = (int64_t)(kMostRuns - t.runs) * kRun, n = left < room ? left : room;
+            const int k = t.count++;
+            t.in[k] = static_cast<const char*>(g[i].grad) + from * (g[i].dt == DIVISION_BF16 ? 2 : 4);
+            t.first[k] = t.runs;
+            t.last[k] = (uint16_t)(types | (uint32_t)((n - 1) % kRun + 1));
+            put(k, g[i], from);
+            t.runs += (uint32_t)((n + kRun - 1) / kRun);
+            from += n;
         }
-        if (i == count) break;
-        t.in[t.count] = g[i].grad;
-        t.out[t.count] = g[i].out;
-        t.n[t.count] = g[i].n;
-        t.first[t.count] = t.runs;
-        t.type[t.count] = (g[i].dt == DIVISION_BF16 ? 1u : 0u) | (g[i].out_dt == DIVISION_BF16 ? 2u : 0u);
-        t.runs += runs;
-        ++t.count;
     }
-    return DIVISION_OK;
+    return t.count ? f(t) : DIVISION_OK;
 }
-uint32_t workgroups(uint32_t runs) { return runs < kMostWorkgroups ? runs : kMostWorkgroups; }
+uint32_t parts_of(uint32_t runs) { return runs < kMostParts ? runs : kMostParts; }
+const auto nothing = [](int, const division_gradient&, int64_t) {};
 
 }  // namespace
 
@@ -187,7 +248,8 @@ extern "C" {
 size_t division_grad_norm_workspace(int64_t count, const division_gradient* grads) {
     if (check(count, grads, false) != DIVISION_OK) return 0;
     size_t parts = 0;
-    launches(count, grads, [&](const Table<kTensors>& t) { parts += workgroups(t.runs); return DIVISION_OK; });
+    NormArgs a;
+    launches(count, grads, a.t, nothing, [&](const auto& t) { parts += parts_of(t.runs); return DIVISION_OK; });
     return 16 + parts * 8;
 }
 
@@ -200,18 +262,28 @@ int division_clip_grads(int64_t count, const division_gradient* grads, float lim
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     float* factor = static_cast<float*>(workspace);
     double* parts = reinterpret_cast<double*>(static_cast<char*>(workspace) + 16);
-    int64_t done = 0;
-    CHECKED(launches(count, grads, [&](const Table<kTensors>& t) {
-        const uint32_t grid = workgroups(t.runs);
-        hipLaunchKernelGGL(add_squares, dim3(grid), dim3(kThreads), 0, st, NormArgs{t, parts + done});
+    int64_t done = 0, runs = 0, made = 0;
+    NormArgs a;
+    CHECKED(launches(count, grads, a.t, nothing, [&](const auto& t) {
+        a.parts = parts + done;
+        const uint32_t grid = parts_of(t.runs);
+        hipLaunchKernelGGL(add_squares, dim3(grid), dim3(kThreads), 0, st, a);
         done += grid;
+        runs += t.runs;
+        ++made;
         return launched();
     }));
-    hipLaunchKernelGGL(join_squares, dim3(1), dim3(1024), 0, st, parts, done, limit, norm, clip ? factor : nullptr);
-    CHECKED(launched());
+    const bool join = clip && made == 1 && runs <= kFewRuns;
+    if (!join) {
+        hipLaunchKernelGGL(join_squares, dim3(1), dim3(1024), 0, st, parts, done, limit, norm, clip ? factor : nullptr);
+        CHECKED(launched());
+    }
     if (!clip) return DIVISION_OK;
-    return launches(count, grads, [&](const Table<kTensors>& t) {
-        hipLaunchKernelGGL(scale_all, dim3(workgroups(t.runs)), dim3(kThreads), 0, st, ClipArgs{t, factor});
+    ClipArgs b;
+    b.parts = parts; b.factor = factor; b.norm = norm; b.limit = limit; b.count = (int)done;
+    const auto put = [&](int k, const division_gradient& g, int64_t from) { b.to.out[k] = static_cast<char*>(g.out) + from * (g.out_dt == DIVISION_BF16 ? 2 : 4); };
+    return launches(count, grads, b.t, put, [&](const auto& t) {
+        hipLaunchKernelGGL(join ? scale_all<true> : scale_all<false>, dim3(t.runs), dim3(kThreads), 0, st, b);
         return launched();
     });
 }

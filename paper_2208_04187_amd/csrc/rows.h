@@ -14,6 +14,12 @@ __device__ __forceinline__ uint32_t bf16_pack2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2_t));
 }
 
+// a store that the caches do not keep
+template <typename T, typename V> __device__ __forceinline__ void store_past(T* p, V q) {
+    typedef V at_any_element __attribute__((aligned(alignof(T))));
+    __builtin_nontemporal_store(q, reinterpret_cast<at_any_element*>(p));
+}
+
 // Element types: fp32 as float, bfloat16 as uint16_t.  A row may start at any element: rows of an odd width do, and then no
 // 16-byte access is aligned.  The machine takes such accesses of global memory (the ABI sets the unaligned mode); memcpy says so to the compiler, which
 // keeps them whole.
