@@ -16,3 +16,4 @@ from .binding import division_relu_compress, division_relu_compress_fused  # noq
 from .operators import Normed, division_read_codes, division_rms_norm, division_rms_norm_backward  # noqa: F401,E402
 from .operators import LogProbs, division_log_probs, division_log_probs_backward  # noqa: F401,E402
 from .operators import division_clip_grads, division_grad_norm  # noqa: F401,E402
+from .token_modules import DivisionNormLinear, DivisionRMSNorm, division_token_log_probs  # noqa: F401,E402

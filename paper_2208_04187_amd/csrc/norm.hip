@@ -100,10 +100,10 @@ template <typename C> __device__ __forceinline__ void store_scale(const NormArgs
 }
 
 // s of the piece at column c
-template <typename T, bool RES, typename C> __device__ __forceinline__ void load_sum(const NormArgs& a, int64_t row, C c, C D, float* v) {
-    const Piece<T> q = load_piece(static_cast<const T*>(a.x) + row * a.x_stride, c, D);
+template <typename T, bool RES, bool PAST, typename C> __device__ __forceinline__ void load_sum(const NormArgs& a, int64_t row, C c, C D, float* v) {
+    const Piece<T> q = load_piece<PAST>(static_cast<const T*>(a.x) + row * a.x_stride, c, D);
     if constexpr (RES) {
-        const Piece<T> p = load_piece(static_cast<const T*>(a.residual) + row * a.residual_stride, c, D);
+        const Piece<T> p = load_piece<PAST>(static_cast<const T*>(a.residual) + row * a.residual_stride, c, D);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = q[i] + p[i];
     } else {
@@ -113,7 +113,7 @@ template <typename T, bool RES, typename C> __device__ __forceinline__ void load
 }
 
 // A row per NT threads, R pieces each, NT * R * 8 >= D.
-template <typename T, int NT, int R, bool RES>
+template <typename T, int NT, int R, bool RES, bool PAST>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_rows(NormArgs a) {
     constexpr int ROWS = NT < 256 ? 256 / NT : 1;
     __shared__ uint32_t slots[NT > 64 ? 3 * (NT / 64) : 1];
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_rows(NormArgs a) {
     for (int64_t row = (int64_t)blockIdx.x * ROWS + row_of_thread<NT>(); row < a.T; row += (int64_t)gridDim.x * ROWS) {
         float v[R][8], sq = 0.0f;
 #pragma unroll
-        for (int r = 0; r < R; ++r) load_sum<T, RES>(a, row, (r * NT + lane) * kPiece, D, v[r]);
+        for (int r = 0; r < R; ++r) load_sum<T, RES, PAST>(a, row, (r * NT + lane) * kPiece, D, v[r]);
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -138,10 +138,10 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_rows(NormArgs a) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int c = (r * NT + lane) * kPiece;
-            if constexpr (RES) store_piece(static_cast<T*>(a.sum) + row * a.D, c, D, v[r]);
+            if constexpr (RES) store_piece<PAST>(static_cast<T*>(a.sum) + row * a.D, c, D, v[r]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[r][i] = v[r][i] * rstd * w[r][i];
-            if (a.y) store_piece(static_cast<T*>(a.y) + row * a.D, c, D, v[r]);
+            if (a.y) store_piece<PAST>(static_cast<T*>(a.y) + row * a.D, c, D, v[r]);
             most = MaxU::of(most, most_of(v[r]));
         }
         if (a.code == DIVISION_CODE_NONE) continue;
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(1024) void norm_wide(NormArgs a) {
         uint32_t most = 0;
         for (int64_t c = (int64_t)threadIdx.x * kPiece; c < a.D; c += 1024 * kPiece) {
             float v[8], w[8];
-            load_sum<T, RES>(a, row, c, a.D, v);
+            load_sum<T, RES, false>(a, row, c, a.D, v);
             load_weight(a.weight, a.weight_bf16, c, a.D, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(1024) void norm_wide(NormArgs a) {
         for (int64_t c0 = 0; c0 < a.D; c0 += 1024 * kPiece) {          // every lane takes part in its group's maximum
             const int64_t c = c0 + (int64_t)threadIdx.x * kPiece;
             float v[8], w[8];
-            load_sum<T, RES>(a, row, c, a.D, v);
+            load_sum<T, RES, false>(a, row, c, a.D, v);
             load_weight(a.weight, a.weight_bf16, c, a.D, w);
             if constexpr (RES) store_piece(static_cast<T*>(a.sum) + row * a.D, c, a.D, v);
 #pragma unroll
@@ -250,7 +250,7 @@ struct BackArgs {
 };
 
 // What a thread reads of a row
-template <typename T, int R> struct BackRow {
+template <typename T, int R, bool PAST> struct BackRow {
     Piece<T> grad[R], s[R], extra[R];
     float rstd;
     template <int NT> __device__ __forceinline__ void load(const BackArgs& a, int64_t row, int lane, int D) {
@@ -263,12 +263,12 @@ template <typename T, int R> struct BackRow {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int c = (r * NT + lane) * kPiece;
-            grad[r] = load_piece(static_cast<const T*>(a.grad) + row * a.grad_stride, c, D);
-            s[r] = load_piece(static_cast<const T*>(a.s) + row * a.s_stride, c, D);
+            grad[r] = load_piece<PAST>(static_cast<const T*>(a.grad) + row * a.grad_stride, c, D);
+            s[r] = load_piece<PAST>(static_cast<const T*>(a.s) + row * a.s_stride, c, D);
         }
         if (a.grad_sum) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) extra[r] = load_piece(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, (r * NT + lane) * kPiece, D);
+            for (int r = 0; r < R; ++r) extra[r] = load_piece<PAST>(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, (r * NT + lane) * kPiece, D);
         }
         rstd = a.rstd[row];
     }
@@ -277,7 +277,7 @@ template <typename T, int R> struct BackRow {
 // A row per NT threads as in norm_rows, THREADS / NT rows a workgroup side by side; dw grows in the registers of the thread that owns its columns over all
 // rows of the workgroup, whose sums meet in LDS at the end: large workgroups leave few shares to add up.  Where the registers hold it (AHEAD), a
 // row is loaded while the one before it is worked on.
-template <typename T, int NT, int R, int THREADS, bool AHEAD>
+template <typename T, int NT, int R, int THREADS, bool AHEAD, bool PAST>
 __global__ __launch_bounds__(THREADS) void norm_back_rows(BackArgs a) {
     constexpr int ROWS = THREADS / NT;
     __shared__ uint32_t slots[NT > 64 ? 2 * (THREADS / 64) : 1];
@@ -292,11 +292,11 @@ __global__ __launch_bounds__(THREADS) void norm_back_rows(BackArgs a) {
     }
     int turn = 0;
     const int64_t step = (int64_t)gridDim.x * ROWS;
-    BackRow<T, R> q;
+    BackRow<T, R, PAST> q;
     q.template load<NT>(a, (int64_t)blockIdx.x * ROWS + row_of_thread<NT>(), lane, D);
     for (int64_t base = (int64_t)blockIdx.x * ROWS; base < a.T; base += step) {
         const int64_t row = base + row_of_thread<NT>();
-        BackRow<T, R> next;
+        BackRow<T, R, PAST> next;
         if constexpr (AHEAD) next.template load<NT>(a, row + step, lane, D);
         float dot = 0.0f;
 #pragma unroll
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(THREADS) void norm_back_rows(BackArgs a) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) d[i] += q.extra[r][i];
                 }
-                store_piece(static_cast<T*>(a.dx) + row * a.D, (r * NT + lane) * kPiece, D, d);
+                store_piece<PAST>(static_cast<T*>(a.dx) + row * a.D, (r * NT + lane) * kPiece, D, d);
             }
         }
         if constexpr (AHEAD) q = next;
@@ -438,16 +438,24 @@ int shift_of(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
 constexpr int64_t kMostWorkgroups = 2048;
 
 // The forward pass: threads a row and pieces a thread.  Up to 1024 columns a row is one wavefront's, which needs no barrier.
-template <typename T, bool RES> void launch_norm(const NormArgs& a, hipStream_t st) {
+template <typename T, bool RES, bool PAST> void launch_norm(const NormArgs& a, hipStream_t st) {
     const int64_t D = a.D;
-    void (*kern)(NormArgs) = D <= 128 ? norm_rows<T, 16, 1, RES> : D <= 512 ? norm_rows<T, 64, 1, RES> : D <= 1024 ? norm_rows<T, 64, 2, RES>
-                           : D <= 2048 ? norm_rows<T, 256, 1, RES> : D <= 4096 ? norm_rows<T, 256, 2, RES> : D <= 8192 ? norm_rows<T, 256, 4, RES>
-                           : D <= 16384 ? norm_rows<T, 1024, 2, RES> : norm_wide<T, RES>;
+    void (*kern)(NormArgs) = D <= 128 ? norm_rows<T, 16, 1, RES, PAST> : D <= 512 ? norm_rows<T, 64, 1, RES, PAST> : D <= 1024 ? norm_rows<T, 64, 2, RES, PAST>
+                           : D <= 2048 ? norm_rows<T, 256, 1, RES, PAST> : D <= 4096 ? norm_rows<T, 256, 2, RES, PAST> : D <= 8192 ? norm_rows<T, 256, 4, RES, PAST>
+                           : D <= 16384 ? norm_rows<T, 1024, 2, RES, PAST> : norm_wide<T, RES>;
     if constexpr (sizeof(T) == 2 || !RES) {                 // (fp32 with a residual would spill)
-        if (D > 16384 && D <= 32768) kern = norm_rows<T, 1024, 4, RES>;
+        if (D > 16384 && D <= 32768) kern = norm_rows<T, 1024, 4, RES, PAST>;
     }
     const int64_t rows = D <= 128 ? 16 : D <= 1024 ? 4 : 1, grid = (a.T + rows - 1) / rows;
     hipLaunchKernelGGL(kern, dim3((uint32_t)(grid < kMostWorkgroups ? grid : kMostWorkgroups)), dim3(D <= 8192 ? 256 : 1024), 0, st, a);
+}
+// bfloat16 alone: 16384 x 4096 with the residual and int8 codes 118 us through the caches, 102 past them (backward 99.6 and 92.5); of 16384 x 1024, which they
+// hold, 27.7 and 27.8 (backward 24.9 and 26.6).  fp32, whose stores are two to a piece: 8191 x 2561 with the residual 69 and 74.
+template <typename T, bool RES> void launch_norm(const NormArgs& a, hipStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if ((1 + 2 * RES + (a.y != nullptr)) * a.T * a.D * (int64_t)sizeof(T) > kCached) return launch_norm<T, RES, true>(a, st);
+    }
+    launch_norm<T, RES, false>(a, st);
 }
 
 // The backward pass: workgroups of 1024 threads, one a CU, so that few shares of dw are left to add up (16384 x 512 bfloat16: 14.6 us, 17.6 with four
@@ -460,12 +468,18 @@ int64_t back_workgroups(int64_t T, int64_t D) {
     return grid < most ? grid : most;
 }
 
-template <typename T> void launch_back(const BackArgs& a, hipStream_t st) {
-    void (*kern)(BackArgs) = a.D <= 128 ? norm_back_rows<T, 16, 1, kBackThreads, true> : a.D <= 512 ? norm_back_rows<T, 64, 1, kBackThreads, true>
-                           : a.D <= 1024 ? norm_back_rows<T, 64, 2, kBackThreads, false> : a.D <= 2048 ? norm_back_rows<T, 256, 1, kBackThreads, true>
-                           : a.D <= 4096 ? norm_back_rows<T, 512, 1, kBackThreads, true> : a.D <= 8192 ? norm_back_rows<T, 1024, 1, kBackThreads, true>
-                           : a.D <= 16384 ? norm_back_rows<T, 1024, 2, kBackThreads, false> : norm_back_wide<T>;
+template <typename T, bool PAST> void launch_back(const BackArgs& a, hipStream_t st) {
+    void (*kern)(BackArgs) = a.D <= 128 ? norm_back_rows<T, 16, 1, kBackThreads, true, PAST> : a.D <= 512 ? norm_back_rows<T, 64, 1, kBackThreads, true, PAST>
+                           : a.D <= 1024 ? norm_back_rows<T, 64, 2, kBackThreads, false, PAST> : a.D <= 2048 ? norm_back_rows<T, 256, 1, kBackThreads, true, PAST>
+                           : a.D <= 4096 ? norm_back_rows<T, 512, 1, kBackThreads, true, PAST> : a.D <= 8192 ? norm_back_rows<T, 1024, 1, kBackThreads, true, PAST>
+                           : a.D <= 16384 ? norm_back_rows<T, 1024, 2, kBackThreads, false, PAST> : norm_back_wide<T>;
     hipLaunchKernelGGL(kern, dim3((uint32_t)back_workgroups(a.T, a.D)), dim3(kBackThreads), 0, st, a);
+}
+template <typename T> void launch_back(const BackArgs& a, hipStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if ((3 + (a.grad_sum != nullptr)) * a.T * a.D * (int64_t)sizeof(T) > kCached) return launch_back<T, true>(a, st);
+    }
+    launch_back<T, false>(a, st);
 }
 
 }  // namespace

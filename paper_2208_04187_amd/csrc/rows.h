@@ -14,7 +14,13 @@ __device__ __forceinline__ uint32_t bf16_pack2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2_t));
 }
 
-// a store that the caches do not keep
+// Accesses that the caches do not keep.  Calls whose tensors are more than kCached together take them: what is read would not stay till the next
+// one, and the last-level cache (256 MB) loses nothing that it would give.
+constexpr int64_t kCached = int64_t(1) << 28;
+template <typename V, typename T> __device__ __forceinline__ V load_past(const T* p) {
+    typedef V at_any_element __attribute__((aligned(alignof(T))));
+    return __builtin_nontemporal_load(reinterpret_cast<const at_any_element*>(p));
+}
 template <typename T, typename V> __device__ __forceinline__ void store_past(T* p, V q) {
     typedef V at_any_element __attribute__((aligned(alignof(T))));
     __builtin_nontemporal_store(q, reinterpret_cast<at_any_element*>(p));
@@ -26,7 +32,10 @@ template <typename T, typename V> __device__ __forceinline__ void store_past(T* 
 template <typename T> struct Piece;
 template <> struct Piece<float> {
     u32x4 w[2];
-    __device__ __forceinline__ void load(const float* p) { __builtin_memcpy(w, p, 32); }
+    template <bool PAST = false> __device__ __forceinline__ void load(const float* p) {
+        if constexpr (PAST) { w[0] = load_past<u32x4>(p); w[1] = load_past<u32x4>(p + 4); }
+        else __builtin_memcpy(w, p, 32);
+    }
     // its elements lo .. hi - 1 alone, zeros beside them
     __device__ __forceinline__ void load(const float* p, int lo, int hi) {
         uint32_t* e = reinterpret_cast<uint32_t*>(w);
@@ -35,7 +44,12 @@ template <> struct Piece<float> {
     }
     __device__ __forceinline__ void zero() { w[0] = u32x4{0, 0, 0, 0}; w[1] = w[0]; }
     __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i / 4][i % 4]); }
-    static __device__ __forceinline__ void store(float* p, const float* v) { __builtin_memcpy(p, v, 32); }
+    template <bool PAST = false> static __device__ __forceinline__ void store(float* p, const float* v) {
+        u32x4 q[2];
+        __builtin_memcpy(q, v, 32);
+        if constexpr (PAST) { store_past(p, q[0]); store_past(p + 4, q[1]); }
+        else __builtin_memcpy(p, q, 32);
+    }
     static __device__ __forceinline__ void store(float* p, const float* v, int lo, int hi) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) if (i >= lo && i < hi) p[i] = v[i];
@@ -43,7 +57,10 @@ template <> struct Piece<float> {
 };
 template <> struct Piece<uint16_t> {
     u32x4 w;
-    __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(&w, p, 16); }
+    template <bool PAST = false> __device__ __forceinline__ void load(const uint16_t* p) {
+        if constexpr (PAST) w = load_past<u32x4>(p);
+        else __builtin_memcpy(&w, p, 16);
+    }
     __device__ __forceinline__ void load(const uint16_t* p, int lo, int hi) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -56,7 +73,11 @@ template <> struct Piece<uint16_t> {
     static __device__ __forceinline__ u32x4 packed(const float* v) {
         return u32x4{bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]), bf16_pack2(v[4], v[5]), bf16_pack2(v[6], v[7])};
     }
-    static __device__ __forceinline__ void store(uint16_t* p, const float* v) { const u32x4 q = packed(v); __builtin_memcpy(p, &q, 16); }
+    template <bool PAST = false> static __device__ __forceinline__ void store(uint16_t* p, const float* v) {
+        const u32x4 q = packed(v);
+        if constexpr (PAST) store_past(p, q);
+        else __builtin_memcpy(p, &q, 16);
+    }
     static __device__ __forceinline__ void store(uint16_t* p, const float* v, int lo, int hi) {
         const u32x4 q = packed(v);
 #pragma unroll
@@ -64,15 +85,15 @@ template <> struct Piece<uint16_t> {
     }
 };
 // The piece of a row that starts at column c of D: whole, the row's last, or behind its end (zeros, nothing stored).  C: int where c + 8 fits it, else int64_t
-template <typename T, typename C> __device__ __forceinline__ Piece<T> load_piece(const T* row, C c, C D) {
+template <bool PAST = false, typename T, typename C> __device__ __forceinline__ Piece<T> load_piece(const T* row, C c, C D) {
     Piece<T> q;
-    if (c + kPiece <= D) q.load(row + c);
+    if (c + kPiece <= D) q.template load<PAST>(row + c);
     else if (c < D) q.load(row + c, 0, (int)(D - c));
     else q.zero();
     return q;
 }
-template <typename T, typename C> __device__ __forceinline__ void store_piece(T* row, C c, C D, const float* v) {
-    if (c + kPiece <= D) Piece<T>::store(row + c, v);
+template <bool PAST = false, typename T, typename C> __device__ __forceinline__ void store_piece(T* row, C c, C D, const float* v) {
+    if (c + kPiece <= D) Piece<T>::template store<PAST>(row + c, v);
     else if (c < D) Piece<T>::store(row + c, v, 0, (int)(D - c));
 }
 

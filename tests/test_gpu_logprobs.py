@@ -272,3 +272,23 @@ def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, calls())), k
+
+
+@pytest.mark.parametrize("dtype,T,V", [(torch.bfloat16, 1400, 50021), (torch.bfloat16, 1030, 65544), (torch.float32, 700, 50021)])
+def test_gradients_beyond_the_caches_are_what_their_slices_are(dtype, T, V):
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    z = (torch.randn(T, V, device="cuda", generator=gen) * 3).to(dtype)
+    ids = torch.randint(0, V, (T,), device="cuda", generator=gen)
+    g = torch.randn(T, device="cuda", generator=gen)
+    f = pkg.division_log_probs(z, ids, top=3)
+    for kw in ({}, dict(entropy=f.entropy, grad_entropy=g)):
+        big = pkg.division_log_probs_backward(z, ids, f.lse, g, **kw)
+        for lo in range(0, T, T // 4):
+            s = slice(lo, lo + T // 4)
+            part = pkg.division_log_probs_backward(z[s], ids[s], f.lse[s], g[s], **{k: v[s] for k, v in kw.items()})
+            assert torch.equal(big[s], part)
+    # the forward pass of a slice may split its rows among workgroups, where that of all does not
+    part = pkg.division_log_probs(z[5:9], ids[5:9], top=3)
+    assert torch.equal(part.top_ids, f.top_ids[5:9])
+    _check(z[5:9], ids[5:9], part, 3)
+    _check(z[5:9], ids[5:9], type(f)(*(v[5:9] for v in f)), 3)

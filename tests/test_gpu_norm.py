@@ -250,3 +250,27 @@ def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_a_graph():
         torch.cuda.synchronize()
         eager = calls()
         assert all(torch.equal(a, b) for a, b in zip(out, eager)), k
+
+
+@pytest.mark.parametrize("T,D", [(9001, 4104), (140003, 255), (3001, 16001), (2101, 20007), (35001, 1001)])
+def test_tensors_beyond_the_caches_give_what_their_slices_give(T, D):
+    """Calls of more than 256 MB go past the caches; rows do not depend on one another"""
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    x, r, g = ((torch.randn(T, D, device="cuda", generator=gen) * (k + 1)).bfloat16() for k in range(3))
+    w = torch.rand(D, device="cuda", generator=gen) + 0.5
+    big = pkg.division_rms_norm(x, w, residual=r, code="e4m3", group=64)
+    dx, dw = pkg.division_rms_norm_backward(g, big.sum, w, big.rstd, grad_sum=r)
+    plain, _ = pkg.division_rms_norm_backward(g, big.sum, w, big.rstd)
+    want, size = torch.zeros(D, dtype=torch.float64, device="cuda"), torch.zeros(D, dtype=torch.float64, device="cuda")
+    for lo in range(0, T, T // 8 + 1):
+        s = slice(lo, lo + T // 8 + 1)
+        part = pkg.division_rms_norm(x[s], w, residual=r[s], code="e4m3", group=64)
+        for a, b in zip(part, big):
+            assert torch.equal(a.view(torch.int8), b[s].view(torch.int8))
+        assert torch.equal(pkg.division_rms_norm_backward(g[s], big.sum[s], w, big.rstd[s], grad_sum=r[s])[0], dx[s])
+        assert torch.equal(pkg.division_rms_norm_backward(g[s], big.sum[s], w, big.rstd[s])[0], plain[s])
+        term = g[s].double() * big.sum[s].double() * big.rstd[s].double()[:, None]
+        want += term.sum(0)
+        size += term.abs().sum(0)
+    # a column's products: one after the other over the rows of a workgroup (256 of them), then over the workgroups
+    assert ((dw.double() - want).abs() <= (T / 256 + 64) * EPS * size).all()
