@@ -402,67 +402,86 @@ struct LogpBackArgs {
     const int64_t* ids;
     const float *lse, *entropy, *g, *gh;
     void* out;
-    int64_t stride, out_stride, T, V, ignore, parts;        // parts: of a row, kUnroll * kThreads pieces each
+    int64_t stride, out_stride, T, V, ignore;
+    int64_t parts, first;                                   // batches of a row; the batch that the launch's first workgroup works on
 };
 
-// Columns are counted from the 16-byte boundary at or before a row's first element, so that pieces are aligned in rows of any width too; the row's
-// are those from lo to end.  (Not in the forward pass, where it would make a row's last bits depend on where the row lies.)
-struct Span {
-    int lo, end;
-    __device__ __forceinline__ bool holds_piece(int c) const { return c >= lo && c + kPiece <= end; }
+// Sixteen bytes of a row: eight of bfloat16, or four of fp32 (eight would be two stores with gaps: 513 x 32003 fp32 31 us, 24 with four)
+template <typename T> struct Unit : Piece<T> { static constexpr int kSize = kPiece; };
+template <> struct Unit<float> {
+    static constexpr int kSize = 4;
+    u32x4 w;
+    template <bool PAST> __device__ __forceinline__ void load(const float* p) {
+        if constexpr (PAST) w = load_past<u32x4>(p);
+        else __builtin_memcpy(&w, p, 16);
+    }
+    __device__ __forceinline__ void load(const float* p, int lo, int hi) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = i >= lo && i < hi ? __float_as_uint(p[i]) : 0u;
+    }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i]); }
+    template <bool PAST> static __device__ __forceinline__ void store(float* p, const float* v) {
+        u32x4 q;
+        __builtin_memcpy(&q, v, 16);
+        if constexpr (PAST) store_past(p, q);
+        else __builtin_memcpy(p, &q, 16);
+    }
+    static __device__ __forceinline__ void store(float* p, const float* v, int lo, int hi) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (i >= lo && i < hi) p[i] = v[i];
+    }
 };
 
+// A batch of a row per workgroup.  Columns are counted from the 16-byte boundary at or before a row's first element, so that units are aligned in rows of any width too; the row's
+// are those from `before` to `end`.  (Not in the forward pass, where it would make a row's last bits depend on where the row lies.)
 template <typename T, bool ENTROPY, bool PAST>
 __global__ __launch_bounds__(kThreads) void log_probs_back(LogpBackArgs a) {
-    for (int64_t item = blockIdx.x; item < a.T * a.parts; item += gridDim.x) {
-        const int64_t at = item / a.parts;
-        const T* row = static_cast<const T*>(a.z) + at * a.stride;
-        T* out = static_cast<T*>(a.out) + at * a.out_stride;
-        const int before = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)), b = (int)(item - at * a.parts) * kBatch, c0 = b + (int)threadIdx.x * kPiece;
-        const Span in{before, (int)a.V + before};
-        row -= before;
-        out -= before;
-        const bool whole = b >= before && b + kBatch <= in.end;
-        const float lse = a.lse[at], h = ENTROPY ? a.entropy[at] : 0.0f, gh = ENTROPY ? a.gh[at] : 0.0f;
-        const int64_t id = a.ids[at];
-        const bool empty = lse == -__builtin_inff();
-        float g = a.g[at];
-        if (id == a.ignore) g = 0.0f;
-        else if (id < 0 || id >= a.V) g = __uint_as_float(0x7fc00000u);
-        Piece<T> q[kUnroll];
-        if (whole) {
+    constexpr int N = Unit<T>::kSize, U = kBatch / (kThreads * N);
+    const int64_t item = a.first + blockIdx.x, at = item / a.parts;
+    const T* row = static_cast<const T*>(a.z) + at * a.stride;
+    T* out = static_cast<T*>(a.out) + at * a.out_stride;
+    const int before = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)), end = (int)a.V + before;
+    const int b = (int)(item - at * a.parts) * kBatch, c0 = b + (int)threadIdx.x * N;
+    row -= before;
+    out -= before;
+    const bool whole = b >= before && b + kBatch <= end;
+    const float lse = a.lse[at], h = ENTROPY ? a.entropy[at] : 0.0f, gh = ENTROPY ? a.gh[at] : 0.0f;
+    const int64_t id = a.ids[at];
+    const bool empty = lse == -__builtin_inff(), token = id >= 0 && id < a.V && id != a.ignore;
+    const int own = token ? (int)id + before : -N;
+    const float g = id == a.ignore ? 0.0f : token ? a.g[at] : __uint_as_float(0x7fc00000u);
+    Unit<T> q[U];
+    if (whole) {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) q[u].template load<PAST>(row + c0 + u * (kThreads * kPiece));
-        } else {
+        for (int u = 0; u < U; ++u) q[u].template load<PAST>(row + c0 + u * (kThreads * N));
+    } else {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const int c = c0 + u * (kThreads * kPiece);
-                if (in.holds_piece(c)) q[u].load(row + c);
-                else q[u].load(row + c, in.lo - c, in.end - c);
-            }
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + u * (kThreads * N);
+            if (c >= before && c + N <= end) q[u].template load<PAST>(row + c);
+            else q[u].load(row + c, before - c, end - c);
         }
+    }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int c = c0 + u * (kThreads * kPiece);
-            if (c >= in.end) break;
-            float v[8];
+    for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * (kThreads * N);
+        if (c >= end) break;
+        float v[N];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = q[u][i] - lse, p = exp2_of(d * kLog2e);
-                v[i] = -p * (ENTROPY ? __builtin_fmaf(gh, fmaxf(d, kGone) + h, g) : g);
-            }
-            const int64_t own = id + before - c;
-            if (own >= 0 && own < kPiece && id != a.ignore) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) if (own == i) v[i] += g;
-            }
-            if (empty) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-            }
-            if (whole || in.holds_piece(c)) Piece<T>::template store<PAST>(out + c, v);
-            else Piece<T>::store(out + c, v, in.lo - c, in.end - c);
+        for (int i = 0; i < N; ++i) {
+            const float d = q[u][i] - lse, p = exp2_of(d * kLog2e);
+            v[i] = -p * (ENTROPY ? __builtin_fmaf(gh, fmaxf(d, kGone) + h, g) : g);
         }
+        if (own >= c && own < c + N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) if (own == c + i) v[i] += g;
+        }
+        if (empty) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = 0.0f;
+        }
+        if (whole || (c >= before && c + N <= end)) Unit<T>::template store<PAST>(out + c, v);
+        else Unit<T>::store(out + c, v, before - c, end - c);
     }
 }
 
@@ -560,8 +579,12 @@ int division_log_probs_backward(const division_logits_back* n, void* hip_stream)
         ? (past ? (a.gh ? log_probs_back<float, true, true> : log_probs_back<float, false, true>) : (a.gh ? log_probs_back<float, true, false> : log_probs_back<float, false, false>))
         : (past ? (a.gh ? log_probs_back<uint16_t, true, true> : log_probs_back<uint16_t, false, true>)
                 : (a.gh ? log_probs_back<uint16_t, true, false> : log_probs_back<uint16_t, false, false>));
-    hipLaunchKernelGGL(kern, dim3(grid_of(a.T * a.parts)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), a);
-    return launched();
+    for (a.first = 0; a.first < a.T * a.parts; a.first += kMostItems) {
+        const int64_t items = a.T * a.parts - a.first;
+        hipLaunchKernelGGL(kern, dim3((uint32_t)(items < kMostItems ? items : kMostItems)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), a);
+        CHECKED(launched());
+    }
+    return DIVISION_OK;
 }
 
 }  // extern "C"
