@@ -52,7 +52,7 @@ template <typename T> __device__ __forceinline__ double squares(const T* p, int 
     double s = 0.0;
     Piece<T> q[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) q[u] = load_piece(p, (u * kThreads + (int)threadIdx.x) * kPiece, n);
+    for (int u = 0; u < kUnroll; ++u) q[u] = load_some<Piece<T>>(p, (u * kThreads + (int)threadIdx.x) * kPiece, n);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
@@ -115,34 +115,18 @@ __global__ __launch_bounds__(1024) void join_squares(const double* parts, int64_
     }
 }
 
-// Four elements a lane and access, so that the lanes' stores lie next to one another whatever the two types are (eight of fp32 are two stores with gaps: 336 M
-// gradients 641 us, 491 with four).  Stores go past the caches, which keep what the first pass has read of the gradients instead: 459 us, and of 25.6 M gradients 38 us
-// instead of 46.
-template <typename T> struct Four;
-template <> struct Four<float> {
-    u32x4 w;
-    __device__ __forceinline__ void load(const float* p) { __builtin_memcpy(&w, p, 16); }
-    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i]); }
-    static __device__ __forceinline__ void store(float* p, const float* v) { store_past(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}); }
-};
-template <> struct Four<uint16_t> {
-    u32x2 w;
-    __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(&w, p, 8); }
-    __device__ __forceinline__ float operator[](int i) const { return i & 1 ? __uint_as_float(w[i / 2] & 0xffff0000u) : bf16_value(w[i / 2]); }
-    static __device__ __forceinline__ void store(uint16_t* p, const float* v) {
-        store_past(p, u32x2{bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3])});
-    }
-};
 __device__ __forceinline__ float value(const float* p) { return *p; }
 __device__ __forceinline__ float value(const uint16_t* p) { return bf16_value(*p); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put(uint16_t* p, float v) { *p = (uint16_t)bf16_pack2(v, 0.0f); }
+__device__ __forceinline__ void put(uint16_t* p, float v) { *p = bf16_of(v); }
 
-// A run of n elements
+// A run of n elements.  Four a lane and access, so that the lanes' stores lie next to one another whatever the two types are (eight of fp32 are two stores
+// with gaps: 336 M gradients 641 us, 491 with four).  Stores go past the caches, which keep what the first pass has read of the gradients instead: 460 us, and of 25.6 M
+// gradients 38 us instead of 46.
 template <typename I, typename O> __device__ __forceinline__ void scale(const I* p, O* o, int n, float f, float power) {
     constexpr int U = (int)(kRun / (kThreads * 4));
     if (n == kRun) {
-        Four<I> q[U];
+        Some<I, 4> q[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) q[u].load(p + (u * kThreads + threadIdx.x) * 4);
 #pragma unroll
@@ -150,7 +134,7 @@ template <typename I, typename O> __device__ __forceinline__ void scale(const I*
             float v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = q[u][i] * f * power;
-            Four<O>::store(o + (u * kThreads + threadIdx.x) * 4, v);
+            Some<O, 4>::template store<true>(o + (u * kThreads + threadIdx.x) * 4, v);
         }
     } else {
 #pragma unroll 4

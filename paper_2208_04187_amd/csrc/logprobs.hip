@@ -406,33 +406,7 @@ struct LogpBackArgs {
     int64_t parts, first;                                   // batches of a row; the batch that the launch's first workgroup works on
 };
 
-// Sixteen bytes of a row: eight of bfloat16, or four of fp32 (eight would be two stores with gaps: 513 x 32003 fp32 31 us, 24 with four)
-template <typename T> struct Unit : Piece<T> { static constexpr int kSize = kPiece; };
-template <> struct Unit<float> {
-    static constexpr int kSize = 4;
-    u32x4 w;
-    template <bool PAST> __device__ __forceinline__ void load(const float* p) {
-        if constexpr (PAST) w = load_past<u32x4>(p);
-        else __builtin_memcpy(&w, p, 16);
-    }
-    __device__ __forceinline__ void load(const float* p, int lo, int hi) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = i >= lo && i < hi ? __float_as_uint(p[i]) : 0u;
-    }
-    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i]); }
-    template <bool PAST> static __device__ __forceinline__ void store(float* p, const float* v) {
-        u32x4 q;
-        __builtin_memcpy(&q, v, 16);
-        if constexpr (PAST) store_past(p, q);
-        else __builtin_memcpy(p, &q, 16);
-    }
-    static __device__ __forceinline__ void store(float* p, const float* v, int lo, int hi) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) if (i >= lo && i < hi) p[i] = v[i];
-    }
-};
-
-// A batch of a row per workgroup.  Columns are counted from the 16-byte boundary at or before a row's first element, so that units are aligned in rows of any width too; the row's
+// A batch of a row per workgroup, in units of sixteen bytes (513 x 32003 fp32 31 us in pieces of eight elements, 24 so).  Columns are counted from the 16-byte boundary at or before a row's first element, so that units are aligned in rows of any width too; the row's
 // are those from `before` to `end`.  (Not in the forward pass, where it would make a row's last bits depend on where the row lies.)
 template <typename T, bool ENTROPY, bool PAST>
 __global__ __launch_bounds__(kThreads) void log_probs_back(LogpBackArgs a) {

@@ -30,106 +30,109 @@ struct NormArgs {
     int weight_bf16;
 };
 
-template <typename C> __device__ __forceinline__ void load_weight(const void* weight, int is_bf16, C c, C D, float* w) {
+// N columns of the weight, whichever type it has
+template <int N, typename C> __device__ __forceinline__ void load_weight(const void* weight, int is_bf16, C c, C D, float* w) {
     if (is_bf16) {
-        const Piece<uint16_t> q = load_piece(static_cast<const uint16_t*>(weight), c, D);
+        const auto q = load_some<Some<uint16_t, N>>(static_cast<const uint16_t*>(weight), c, D);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = q[i];
+        for (int i = 0; i < N; ++i) w[i] = q[i];
     } else {
-        const Piece<float> q = load_piece(static_cast<const float*>(weight), c, D);
+        const auto q = load_some<Some<float, N>>(static_cast<const float*>(weight), c, D);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = q[i];
+        for (int i = 0; i < N; ++i) w[i] = q[i];
     }
 }
 
-// The codes of eight values of a group whose largest has these bits (without its sign).  A group that is not finite has scale NaN and
+// The codes of N values (4 or 8) of a group whose largest has these bits (without its sign).  A group that is not finite has scale NaN and
 // codes 0, one of next to nothing scale 0 and codes 0.
-struct Coded { uint32_t lo, hi; float scale; };
-__device__ __forceinline__ Coded code_piece(const float* v, uint32_t most_bits, int code) {
+template <int N> struct Coded { uint32_t w[N / 4]; float scale; };
+template <int N> __device__ __forceinline__ Coded<N> code_of(const float* v, uint32_t most_bits, int code) {
     const float most = __uint_as_float(most_bits);
     const bool finite = most_bits < 0x7f800000u, held = finite && most >= kTiny;
     const float top = code == DIVISION_CODE_INT8 ? 127.0f : 448.0f;
     const float inverse = top / most;
-    Coded r;
-    if (code == DIVISION_CODE_INT8) {
-        // rounded to nearest even by the addition of 1.5 * 2^23, whose last byte then holds the code
-        uint32_t q[8];
+    Coded<N> r;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = __float_as_uint(__builtin_fmaf(v[i], inverse, 12582912.0f)) & 0xffu;
-        r.lo = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
-        r.hi = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
-    } else {
-        int lo = 0, hi = 0;
-        lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inverse, v[1] * inverse, lo, false);
-        lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inverse, v[3] * inverse, lo, true);
-        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * inverse, v[5] * inverse, hi, false);
-        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * inverse, v[7] * inverse, hi, true);
-        r.lo = (uint32_t)lo;
-        r.hi = (uint32_t)hi;
+    for (int k = 0; k < N / 4; ++k) {
+        const float* e = v + 4 * k;
+        if (code == DIVISION_CODE_INT8) {
+            // rounded to nearest even by the addition of 1.5 * 2^23, whose last byte then holds the code
+            uint32_t q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = __float_as_uint(__builtin_fmaf(e[i], inverse, 12582912.0f)) & 0xffu;
+            r.w[k] = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+        } else {
+            int q = __builtin_amdgcn_cvt_pk_fp8_f32(e[0] * inverse, e[1] * inverse, 0, false);
+            r.w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(e[2] * inverse, e[3] * inverse, q, true);
+        }
+        if (!held) r.w[k] = 0;
     }
-    if (!held) r.lo = r.hi = 0;
     r.scale = !finite ? __uint_as_float(0x7fc00000u) : held ? most / top : 0.0f;
     return r;
 }
-template <typename C> __device__ __forceinline__ void store_codes(uint8_t* row, C c, C D, const Coded& k) {
-    if (c + kPiece <= D) {
-        const u32x2 q = {k.lo, k.hi};
-        __builtin_memcpy(row + c, &q, 8);
+template <int N, typename C> __device__ __forceinline__ void store_codes(uint8_t* row, C c, C D, const Coded<N>& k) {
+    if (c + N <= D) {
+        __builtin_memcpy(row + c, k.w, N);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (c + i < D) row[c + i] = (uint8_t)((i < 4 ? k.lo : k.hi) >> (i % 4 * 8));
+        for (int i = 0; i < N; ++i) if (c + i < D) row[c + i] = (uint8_t)(k.w[i / 4] >> (i % 4 * 8));
     }
 }
-__device__ __forceinline__ uint32_t most_of(const float* v) {
+template <int N> __device__ __forceinline__ uint32_t most_of(const float* v) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = MaxU::of(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    for (int i = 0; i < N; ++i) m = MaxU::of(m, __float_as_uint(v[i]) & 0x7fffffffu);
     return m;
 }
-// the largest of a group of columns: 4, 8 or 16 neighbouring lanes of a piece each
-__device__ __forceinline__ uint32_t most_of_group(uint32_t m, int group) {
-    m = over_lanes<MaxU, 4>(m);
-    if (group >= 64) m = MaxU::of(m, dpp<kHalfMirror>(m));
-    if (group >= 128) m = MaxU::of(m, dpp<kMirror>(m));
+// the largest of a group of 32, 64 or 128 columns: N of them in each of as many neighbouring lanes as it takes
+template <int N> __device__ __forceinline__ uint32_t most_of_group(uint32_t m, int group) {
+    m = over_lanes<MaxU, 32 / N>(m);
+    if constexpr (N == 8) {
+        if (group >= 64) m = MaxU::of(m, dpp<kHalfMirror>(m));
+        if (group >= 128) m = MaxU::of(m, dpp<kMirror>(m));
+    } else {
+        if (group >= 64) m = MaxU::of(m, dpp<kMirror>(m));
+        if (group >= 128) m = MaxU::of(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+    }
     return m;
 }
 
-// the scale of the group that starts with the piece at column c
+// the scale of the group that starts with column c
 template <typename C> __device__ __forceinline__ void store_scale(const NormArgs& a, int64_t row, C c, C D, float scale) {
     if (a.group == 0 ? c == 0 : c < D && (c & (a.group - 1)) == 0) a.scales[row * a.groups + (a.group ? c >> a.shift : 0)] = scale;
 }
 
-// s of the piece at column c
+// s of the unit at column c
 template <typename T, bool RES, bool PAST, typename C> __device__ __forceinline__ void load_sum(const NormArgs& a, int64_t row, C c, C D, float* v) {
-    const Piece<T> q = load_piece<PAST>(static_cast<const T*>(a.x) + row * a.x_stride, c, D);
+    const auto q = load_some<Unit<T>, PAST>(static_cast<const T*>(a.x) + row * a.x_stride, c, D);
     if constexpr (RES) {
-        const Piece<T> p = load_piece<PAST>(static_cast<const T*>(a.residual) + row * a.residual_stride, c, D);
+        const auto p = load_some<Unit<T>, PAST>(static_cast<const T*>(a.residual) + row * a.residual_stride, c, D);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = q[i] + p[i];
+        for (int i = 0; i < Unit<T>::kSize; ++i) v[i] = q[i] + p[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = q[i];
+        for (int i = 0; i < Unit<T>::kSize; ++i) v[i] = q[i];
     }
 }
 
-// A row per NT threads, R pieces each, NT * R * 8 >= D.
+// A row per NT threads, R units of sixteen bytes each: NT * R units hold a row.
 template <typename T, int NT, int R, bool RES, bool PAST>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_rows(NormArgs a) {
-    constexpr int ROWS = NT < 256 ? 256 / NT : 1;
+    constexpr int ROWS = NT < 256 ? 256 / NT : 1, N = Unit<T>::kSize;
     __shared__ uint32_t slots[NT > 64 ? 3 * (NT / 64) : 1];
     const int lane = threadIdx.x % NT, D = (int)a.D;
-    float w[R][8];
+    float w[R][N];
     int turn = 0;
 #pragma unroll
-    for (int r = 0; r < R; ++r) load_weight(a.weight, a.weight_bf16, (r * NT + lane) * kPiece, D, w[r]);
+    for (int r = 0; r < R; ++r) load_weight<N>(a.weight, a.weight_bf16, (r * NT + lane) * N, D, w[r]);
     for (int64_t row = (int64_t)blockIdx.x * ROWS + row_of_thread<NT>(); row < a.T; row += (int64_t)gridDim.x * ROWS) {
-        float v[R][8], sq = 0.0f;
+        float v[R][N], sq = 0.0f;
 #pragma unroll
-        for (int r = 0; r < R; ++r) load_sum<T, RES, PAST>(a, row, (r * NT + lane) * kPiece, D, v[r]);
+        for (int r = 0; r < R; ++r) load_sum<T, RES, PAST>(a, row, (r * NT + lane) * N, D, v[r]);
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sq = __builtin_fmaf(v[r][i], v[r][i], sq);
+            for (int i = 0; i < N; ++i) sq = __builtin_fmaf(v[r][i], v[r][i], sq);
         sq = row_sum<NT>(sq, slots + turn);
         if constexpr (NT > 64) turn ^= NT / 64;
         const float rstd = 1.0f / sqrtf(sq / (float)a.D + a.eps);
@@ -137,20 +140,19 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_rows(NormArgs a) {
         uint32_t most = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int c = (r * NT + lane) * kPiece;
-            if constexpr (RES) store_piece<PAST>(static_cast<T*>(a.sum) + row * a.D, c, D, v[r]);
+            const int c = (r * NT + lane) * N;
+            if constexpr (RES) store_some<Unit<T>, PAST>(static_cast<T*>(a.sum) + row * a.D, c, D, v[r]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[r][i] = v[r][i] * rstd * w[r][i];
-            if (a.y) store_piece<PAST>(static_cast<T*>(a.y) + row * a.D, c, D, v[r]);
-            most = MaxU::of(most, most_of(v[r]));
+            for (int i = 0; i < N; ++i) v[r][i] = v[r][i] * rstd * w[r][i];
+            if (a.y) store_some<Unit<T>, PAST>(static_cast<T*>(a.y) + row * a.D, c, D, v[r]);
+            most = MaxU::of(most, most_of<N>(v[r]));
         }
         if (a.code == DIVISION_CODE_NONE) continue;
         if (a.group == 0) most = over_row<MaxU, NT>(most, slots + (NT > 64 ? 2 * (NT / 64) : 0));
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int c = (r * NT + lane) * kPiece;
-            const uint32_t m = a.group == 0 ? most : most_of_group(most_of(v[r]), a.group);
-            const Coded k = code_piece(v[r], m, a.code);
+            const int c = (r * NT + lane) * N;
+            const Coded<N> k = code_of<N>(v[r], a.group == 0 ? most : most_of_group<N>(most_of<N>(v[r]), a.group), a.code);
             store_codes(a.codes + row * a.D, c, D, k);
             store_scale(a, row, c, D, k.scale);
         }
@@ -161,16 +163,17 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_rows(NormArgs a) {
 // that of |s * w| times rstd, which the first pass finds beside the sum.
 template <typename T, bool RES>
 __global__ __launch_bounds__(1024) void norm_wide(NormArgs a) {
+    constexpr int N = Unit<T>::kSize;
     __shared__ uint32_t slots[2 * 16];
     for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
         float sq = 0.0f;
         uint32_t most = 0;
-        for (int64_t c = (int64_t)threadIdx.x * kPiece; c < a.D; c += 1024 * kPiece) {
-            float v[8], w[8];
+        for (int64_t c = (int64_t)threadIdx.x * N; c < a.D; c += 1024 * N) {
+            float v[N], w[N];
             load_sum<T, RES, false>(a, row, c, a.D, v);
-            load_weight(a.weight, a.weight_bf16, c, a.D, w);
+            load_weight<N>(a.weight, a.weight_bf16, c, a.D, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < N; ++i) {
                 sq = __builtin_fmaf(v[i], v[i], sq);
                 most = MaxU::of(most, __float_as_uint(v[i] * w[i]) & 0x7fffffffu);
             }
@@ -180,17 +183,17 @@ __global__ __launch_bounds__(1024) void norm_wide(NormArgs a) {
         const float rstd = 1.0f / sqrtf(sq / (float)a.D + a.eps);
         most = __float_as_uint(__uint_as_float(most) * rstd);
         if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
-        for (int64_t c0 = 0; c0 < a.D; c0 += 1024 * kPiece) {          // every lane takes part in its group's maximum
-            const int64_t c = c0 + (int64_t)threadIdx.x * kPiece;
-            float v[8], w[8];
+        for (int64_t c0 = 0; c0 < a.D; c0 += 1024 * N) {    // every lane takes part in its group's maximum
+            const int64_t c = c0 + (int64_t)threadIdx.x * N;
+            float v[N], w[N];
             load_sum<T, RES, false>(a, row, c, a.D, v);
-            load_weight(a.weight, a.weight_bf16, c, a.D, w);
-            if constexpr (RES) store_piece(static_cast<T*>(a.sum) + row * a.D, c, a.D, v);
+            load_weight<N>(a.weight, a.weight_bf16, c, a.D, w);
+            if constexpr (RES) store_some<Unit<T>>(static_cast<T*>(a.sum) + row * a.D, c, a.D, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * w[i];
-            if (a.y) store_piece(static_cast<T*>(a.y) + row * a.D, c, a.D, v);
+            for (int i = 0; i < N; ++i) v[i] = v[i] * rstd * w[i];
+            if (a.y) store_some<Unit<T>>(static_cast<T*>(a.y) + row * a.D, c, a.D, v);
             if (a.code == DIVISION_CODE_NONE) continue;
-            const Coded k = code_piece(v, a.group == 0 ? most : most_of_group(most_of(v), a.group), a.code);
+            const Coded<N> k = code_of<N>(v, a.group == 0 ? most : most_of_group<N>(most_of<N>(v), a.group), a.code);
             store_codes(a.codes + row * a.D, c, a.D, k);
             store_scale(a, row, c, a.D, k.scale);
         }
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(256) void read_codes(ReadArgs a) {
                     v[4 * i + 3] = hi.y * scale;
                 }
             }
-            store_piece(static_cast<T*>(a.out) + row * a.D, c, a.D, v);
+            store_some<Piece<T>>(static_cast<T*>(a.out) + row * a.D, c, a.D, v);
         }
     }
 }
@@ -251,7 +254,8 @@ struct BackArgs {
 
 // What a thread reads of a row
 template <typename T, int R, bool PAST> struct BackRow {
-    Piece<T> grad[R], s[R], extra[R];
+    static constexpr int N = Unit<T>::kSize;
+    Unit<T> grad[R], s[R], extra[R];
     float rstd;
     template <int NT> __device__ __forceinline__ void load(const BackArgs& a, int64_t row, int lane, int D) {
         if (row >= a.T) {
@@ -262,13 +266,13 @@ template <typename T, int R, bool PAST> struct BackRow {
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int c = (r * NT + lane) * kPiece;
-            grad[r] = load_piece<PAST>(static_cast<const T*>(a.grad) + row * a.grad_stride, c, D);
-            s[r] = load_piece<PAST>(static_cast<const T*>(a.s) + row * a.s_stride, c, D);
+            const int c = (r * NT + lane) * N;
+            grad[r] = load_some<Unit<T>, PAST>(static_cast<const T*>(a.grad) + row * a.grad_stride, c, D);
+            s[r] = load_some<Unit<T>, PAST>(static_cast<const T*>(a.s) + row * a.s_stride, c, D);
         }
         if (a.grad_sum) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) extra[r] = load_piece<PAST>(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, (r * NT + lane) * kPiece, D);
+            for (int r = 0; r < R; ++r) extra[r] = load_some<Unit<T>, PAST>(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, (r * NT + lane) * N, D);
         }
         rstd = a.rstd[row];
     }
@@ -279,16 +283,16 @@ template <typename T, int R, bool PAST> struct BackRow {
 // row is loaded while the one before it is worked on.
 template <typename T, int NT, int R, int THREADS, bool AHEAD, bool PAST>
 __global__ __launch_bounds__(THREADS) void norm_back_rows(BackArgs a) {
-    constexpr int ROWS = THREADS / NT;
+    constexpr int ROWS = THREADS / NT, N = Unit<T>::kSize;
     __shared__ uint32_t slots[NT > 64 ? 2 * (THREADS / 64) : 1];
-    __shared__ float shares[ROWS > 1 ? THREADS * kPiece : 1];
+    __shared__ float shares[ROWS > 1 ? THREADS * N : 1];
     const int lane = threadIdx.x % NT, D = (int)a.D;
-    float w[R][8], dw[R][8];
+    float w[R][N], dw[R][N];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        load_weight(a.weight, a.weight_bf16, (r * NT + lane) * kPiece, D, w[r]);
+        load_weight<N>(a.weight, a.weight_bf16, (r * NT + lane) * N, D, w[r]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dw[r][i] = 0.0f;
+        for (int i = 0; i < N; ++i) dw[r][i] = 0.0f;
     }
     int turn = 0;
     const int64_t step = (int64_t)gridDim.x * ROWS;
@@ -302,7 +306,7 @@ __global__ __launch_bounds__(THREADS) void norm_back_rows(BackArgs a) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < N; ++i) {
                 const float n = q.s[r][i] * q.rstd, g = q.grad[r][i];
                 dot = __builtin_fmaf(g * w[r][i], n, dot);
                 dw[r][i] = __builtin_fmaf(g, n, dw[r][i]);
@@ -312,14 +316,14 @@ __global__ __launch_bounds__(THREADS) void norm_back_rows(BackArgs a) {
         if (row < a.T) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float d[8];
+                float d[N];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] = q.rstd * __builtin_fmaf(-(q.s[r][i] * q.rstd), along, q.grad[r][i] * w[r][i]);
+                for (int i = 0; i < N; ++i) d[i] = q.rstd * __builtin_fmaf(-(q.s[r][i] * q.rstd), along, q.grad[r][i] * w[r][i]);
                 if (a.grad_sum) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] += q.extra[r][i];
+                    for (int i = 0; i < N; ++i) d[i] += q.extra[r][i];
                 }
-                store_piece<PAST>(static_cast<T*>(a.dx) + row * a.D, (r * NT + lane) * kPiece, D, d);
+                store_some<Unit<T>, PAST>(static_cast<T*>(a.dx) + row * a.D, (r * NT + lane) * N, D, d);
             }
         }
         if constexpr (AHEAD) q = next;
@@ -331,17 +335,17 @@ __global__ __launch_bounds__(THREADS) void norm_back_rows(BackArgs a) {
         if constexpr (ROWS > 1) {                           // the workgroup's rows: added up in their order
             if (r) __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) shares[threadIdx.x / NT * (NT * 8) + i * NT + lane] = dw[r][i];
+            for (int i = 0; i < N; ++i) shares[threadIdx.x / NT * (NT * N) + i * NT + lane] = dw[r][i];
             __syncthreads();
-            for (int j = threadIdx.x; j < NT * 8; j += THREADS) {
-                const int c = (r * NT + j % NT) * kPiece + j / NT;
+            for (int j = threadIdx.x; j < NT * N; j += THREADS) {
+                const int c = (r * NT + j % NT) * N + j / NT;
                 float t = 0.0f;
 #pragma unroll
-                for (int k = 0; k < ROWS; ++k) t += shares[k * (NT * 8) + j];
+                for (int k = 0; k < ROWS; ++k) t += shares[k * (NT * N) + j];
                 if (c < D) part[c] = t;
             }
         } else {
-            store_piece(part, (r * NT + lane) * kPiece, D, dw[r]);
+            store_some<Some<float, N>>(part, (r * NT + lane) * N, D, dw[r]);
         }
     }
 }
@@ -349,6 +353,7 @@ __global__ __launch_bounds__(THREADS) void norm_back_rows(BackArgs a) {
 // Rows too long for the registers: read twice; a workgroup's share of dw lies in memory, each column a thread's own.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_back_wide(BackArgs a) {
+    constexpr int N = Unit<T>::kSize;
     __shared__ uint32_t slots[2 * 16];
     float* part = a.parts + (int64_t)blockIdx.x * a.D;
     int turn = 0;
@@ -358,36 +363,38 @@ __global__ __launch_bounds__(1024) void norm_back_wide(BackArgs a) {
         const T* grad = static_cast<const T*>(a.grad) + row * a.grad_stride;
         const T* s = static_cast<const T*>(a.s) + row * a.s_stride;
         float dot = 0.0f;
-        for (int64_t c = (int64_t)threadIdx.x * kPiece; c < a.D; c += 1024 * kPiece) {
-            const Piece<T> p = load_piece(grad, c, a.D), q = load_piece(s, c, a.D);
-            float w[8];
-            load_weight(a.weight, a.weight_bf16, c, a.D, w);
+        for (int64_t c = (int64_t)threadIdx.x * N; c < a.D; c += 1024 * N) {
+            const auto p = load_some<Unit<T>>(grad, c, a.D), q = load_some<Unit<T>>(s, c, a.D);
+            float w[N];
+            load_weight<N>(a.weight, a.weight_bf16, c, a.D, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dot = __builtin_fmaf(p[i] * w[i], q[i] * rstd, dot);
+            for (int i = 0; i < N; ++i) dot = __builtin_fmaf(p[i] * w[i], q[i] * rstd, dot);
         }
         const float along = row_sum<1024>(dot, slots + turn) / (float)a.D;
         turn ^= 16;
-        for (int64_t c = (int64_t)threadIdx.x * kPiece; c < a.D; c += 1024 * kPiece) {
-            const Piece<T> p = load_piece(grad, c, a.D), q = load_piece(s, c, a.D);
-            float w[8], u[8], n[8], dw[8];
-            load_weight(a.weight, a.weight_bf16, c, a.D, w);
-            const Piece<float> had = first ? Piece<float>{} : load_piece(static_cast<const float*>(part), c, a.D);
+        for (int64_t c = (int64_t)threadIdx.x * N; c < a.D; c += 1024 * N) {
+            const auto p = load_some<Unit<T>>(grad, c, a.D), q = load_some<Unit<T>>(s, c, a.D);
+            float w[N], u[N], n[N], dw[N];
+            load_weight<N>(a.weight, a.weight_bf16, c, a.D, w);
+            Some<float, N> had;
+            if (first) had.zero();
+            else had = load_some<Some<float, N>>(static_cast<const float*>(part), c, a.D);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < N; ++i) {
                 n[i] = q[i] * rstd;
                 u[i] = p[i] * w[i];
-                dw[i] = __builtin_fmaf(p[i], n[i], first ? 0.0f : had[i]);
+                dw[i] = __builtin_fmaf(p[i], n[i], had[i]);
             }
-            float d[8];
+            float d[N];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = rstd * __builtin_fmaf(-n[i], along, u[i]);
+            for (int i = 0; i < N; ++i) d[i] = rstd * __builtin_fmaf(-n[i], along, u[i]);
             if (a.grad_sum) {
-                const Piece<T> extra = load_piece(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, c, a.D);
+                const auto extra = load_some<Unit<T>>(static_cast<const T*>(a.grad_sum) + row * a.grad_sum_stride, c, a.D);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] += extra[i];
+                for (int i = 0; i < N; ++i) d[i] += extra[i];
             }
-            store_piece(static_cast<T*>(a.dx) + row * a.D, c, a.D, d);
-            store_piece(part, c, a.D, dw);
+            store_some<Unit<T>>(static_cast<T*>(a.dx) + row * a.D, c, a.D, d);
+            store_some<Some<float, N>>(part, c, a.D, dw);
         }
         first = false;
     }
@@ -437,49 +444,48 @@ int shift_of(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
 
 constexpr int64_t kMostWorkgroups = 2048;
 
-// The forward pass: threads a row and pieces a thread.  Up to 1024 columns a row is one wavefront's, which needs no barrier.
+// The forward pass: threads a row and units a thread (M: fp32 has half as many elements in one).  Up to 1024 columns a row is one wavefront's, which needs no barrier.
 template <typename T, bool RES, bool PAST> void launch_norm(const NormArgs& a, hipStream_t st) {
+    constexpr int M = (int)sizeof(T) / 2;
     const int64_t D = a.D;
-    void (*kern)(NormArgs) = D <= 128 ? norm_rows<T, 16, 1, RES, PAST> : D <= 512 ? norm_rows<T, 64, 1, RES, PAST> : D <= 1024 ? norm_rows<T, 64, 2, RES, PAST>
-                           : D <= 2048 ? norm_rows<T, 256, 1, RES, PAST> : D <= 4096 ? norm_rows<T, 256, 2, RES, PAST> : D <= 8192 ? norm_rows<T, 256, 4, RES, PAST>
-                           : D <= 16384 ? norm_rows<T, 1024, 2, RES, PAST> : norm_wide<T, RES>;
-    if constexpr (sizeof(T) == 2 || !RES) {                 // (fp32 with a residual would spill)
-        if (D > 16384 && D <= 32768) kern = norm_rows<T, 1024, 4, RES, PAST>;
+    void (*kern)(NormArgs) = D <= 128 ? norm_rows<T, 16 * M, 1, RES, PAST> : D <= 512 ? norm_rows<T, 64, M, RES, PAST> : D <= 1024 ? norm_rows<T, 64, 2 * M, RES, PAST>
+                           : D <= 2048 ? norm_rows<T, 256, M, RES, PAST> : D <= 4096 ? norm_rows<T, 256, 2 * M, RES, PAST> : D <= 8192 ? norm_rows<T, 256, 4 * M, RES, PAST>
+                           : D <= 16384 ? norm_rows<T, 1024, 2 * M, RES, PAST> : norm_wide<T, RES>;
+    if constexpr (sizeof(T) == 2 && (PAST || !RES)) {       // (the others would spill)
+        if (D > 16384 && D <= 32768) kern = norm_rows<T, 1024, 4 * M, RES, PAST>;
     }
-    const int64_t rows = D <= 128 ? 16 : D <= 1024 ? 4 : 1, grid = (a.T + rows - 1) / rows;
+    const int64_t rows = D <= 128 ? 16 / M : D <= 1024 ? 4 : 1, grid = (a.T + rows - 1) / rows;
     hipLaunchKernelGGL(kern, dim3((uint32_t)(grid < kMostWorkgroups ? grid : kMostWorkgroups)), dim3(D <= 8192 ? 256 : 1024), 0, st, a);
 }
-// bfloat16 alone: 16384 x 4096 with the residual and int8 codes 118 us through the caches, 102 past them (backward 99.6 and 92.5); of 16384 x 1024, which they
-// hold, 27.7 and 27.8 (backward 24.9 and 26.6).  fp32, whose stores are two to a piece: 8191 x 2561 with the residual 69 and 74.
+// Past the caches where they would not hold the call's tensors: 16384 x 4096 bfloat16 with the residual and int8 codes 118 us through them, 102 past them (backward 99.6 and
+// 92.5), 8192 x 4096 fp32 with the residual 99.7 and 92.7 (102.5 and 92.3); of 16384 x 1024 bfloat16, which they hold, 27.7 and 27.8 (24.9 and 26.6).
 template <typename T, bool RES> void launch_norm(const NormArgs& a, hipStream_t st) {
-    if constexpr (sizeof(T) == 2) {
-        if ((1 + 2 * RES + (a.y != nullptr)) * a.T * a.D * (int64_t)sizeof(T) > kCached) return launch_norm<T, RES, true>(a, st);
-    }
-    launch_norm<T, RES, false>(a, st);
+    const bool past = (1 + 2 * RES + (a.y != nullptr)) * a.T * a.D * (int64_t)sizeof(T) > kCached;
+    past ? launch_norm<T, RES, true>(a, st) : launch_norm<T, RES, false>(a, st);
 }
 
 // The backward pass: workgroups of 1024 threads, one a CU, so that few shares of dw are left to add up (16384 x 512 bfloat16: 14.6 us, 17.6 with four
 // times as many of 256 threads; 8191 x 2561 fp32 68 either way).  A piece a thread and the next row's loads ahead of the work, except from 513 to 1024 columns, where
 // two pieces on one wavefront need no barriers and leave fewer lanes idle (16384 x 768 bfloat16 26.4 -> 20.8 us), and beyond 8192.
 constexpr int kBackThreads = 1024;
-int64_t back_workgroups(int64_t T, int64_t D) {
-    const int rows = kBackThreads / (D <= 128 ? 16 : D <= 1024 ? 64 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024);
+// rows a workgroup holds side by side: M twice the threads a row of up to 128 columns for fp32
+int64_t back_workgroups(int64_t T, int64_t D, int M) {
+    const int rows = kBackThreads / (D <= 128 ? 16 * M : D <= 1024 ? 64 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024);
     const int64_t grid = (T + rows - 1) / rows, most = 256;
     return grid < most ? grid : most;
 }
 
 template <typename T, bool PAST> void launch_back(const BackArgs& a, hipStream_t st) {
-    void (*kern)(BackArgs) = a.D <= 128 ? norm_back_rows<T, 16, 1, kBackThreads, true, PAST> : a.D <= 512 ? norm_back_rows<T, 64, 1, kBackThreads, true, PAST>
-                           : a.D <= 1024 ? norm_back_rows<T, 64, 2, kBackThreads, false, PAST> : a.D <= 2048 ? norm_back_rows<T, 256, 1, kBackThreads, true, PAST>
-                           : a.D <= 4096 ? norm_back_rows<T, 512, 1, kBackThreads, true, PAST> : a.D <= 8192 ? norm_back_rows<T, 1024, 1, kBackThreads, true, PAST>
-                           : a.D <= 16384 ? norm_back_rows<T, 1024, 2, kBackThreads, false, PAST> : norm_back_wide<T>;
-    hipLaunchKernelGGL(kern, dim3((uint32_t)back_workgroups(a.T, a.D)), dim3(kBackThreads), 0, st, a);
+    constexpr int M = (int)sizeof(T) / 2, K = kBackThreads;
+    const int64_t D = a.D;
+    void (*kern)(BackArgs) = D <= 128 ? norm_back_rows<T, 16 * M, 1, K, true, PAST> : D <= 512 ? norm_back_rows<T, 64, M, K, true, PAST> : D <= 1024 ? norm_back_rows<T, 64, 2 * M, K, false, PAST>
+                           : D <= 2048 ? norm_back_rows<T, 256, M, K, true, PAST> : D <= 4096 ? norm_back_rows<T, 512, M, K, true, PAST> : D <= 8192 ? norm_back_rows<T, 1024, M, K, true, PAST>
+                           : D <= 16384 ? norm_back_rows<T, 1024, 2 * M, K, false, PAST> : norm_back_wide<T>;
+    hipLaunchKernelGGL(kern, dim3((uint32_t)back_workgroups(a.T, D, M)), dim3(kBackThreads), 0, st, a);
 }
 template <typename T> void launch_back(const BackArgs& a, hipStream_t st) {
-    if constexpr (sizeof(T) == 2) {
-        if ((3 + (a.grad_sum != nullptr)) * a.T * a.D * (int64_t)sizeof(T) > kCached) return launch_back<T, true>(a, st);
-    }
-    launch_back<T, false>(a, st);
+    const bool past = (3 + (a.grad_sum != nullptr)) * a.T * a.D * (int64_t)sizeof(T) > kCached;
+    past ? launch_back<T, true>(a, st) : launch_back<T, false>(a, st);
 }
 
 }  // namespace
@@ -531,7 +537,7 @@ int division_read_codes(const void* codes, const float* scales, int64_t T, int64
 }
 
 size_t division_rms_norm_backward_workspace(int64_t T, int64_t D) {
-    return rows_ok(T, D) != DIVISION_OK ? 0 : (size_t)back_workgroups(T, D) * (size_t)D * 4u;
+    return rows_ok(T, D) != DIVISION_OK ? 0 : (size_t)back_workgroups(T, D, 2) * (size_t)D * 4u;
 }
 
 int division_rms_norm_backward(const division_norm_back* n, void* hip_stream) {
@@ -558,7 +564,7 @@ int division_rms_norm_backward(const division_norm_back* n, void* hip_stream) {
         CHECKED(launched());
     }
     const int64_t grid = (n->D + 63) / 64;
-    hipLaunchKernelGGL(add_shares, dim3((uint32_t)(grid < 65536 ? grid : 65536)), dim3(1024), 0, st, a.parts, n->T > 0 ? back_workgroups(n->T, n->D) : 0, n->D,
+    hipLaunchKernelGGL(add_shares, dim3((uint32_t)(grid < 65536 ? grid : 65536)), dim3(1024), 0, st, a.parts, n->T > 0 ? back_workgroups(n->T, n->D, n->dt == DIVISION_F32 ? 2 : 1) : 0, n->D,
                        n->grad_weight, a.weight_bf16);
     return launched();
 }

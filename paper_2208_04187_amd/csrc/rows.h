@@ -26,75 +26,88 @@ template <typename T, typename V> __device__ __forceinline__ void store_past(T* 
     __builtin_nontemporal_store(q, reinterpret_cast<at_any_element*>(p));
 }
 
-// Element types: fp32 as float, bfloat16 as uint16_t.  A row may start at any element: rows of an odd width do, and then no
-// 16-byte access is aligned.  The machine takes such accesses of global memory (the ABI sets the unaligned mode); memcpy says so to the compiler, which
-// keeps them whole.
-template <typename T> struct Piece;
-template <> struct Piece<float> {
-    u32x4 w[2];
-    template <bool PAST = false> __device__ __forceinline__ void load(const float* p) {
-        if constexpr (PAST) { w[0] = load_past<u32x4>(p); w[1] = load_past<u32x4>(p + 4); }
-        else __builtin_memcpy(w, p, 32);
-    }
-    // its elements lo .. hi - 1 alone, zeros beside them
-    __device__ __forceinline__ void load(const float* p, int lo, int hi) {
-        uint32_t* e = reinterpret_cast<uint32_t*>(w);
+__device__ __forceinline__ uint16_t bf16_of(float v) { return (uint16_t)bf16_pack2(v, 0.0f); }
+
+// N elements of a row in a lane's registers: 4 or 8 of fp32 (float) or bfloat16 (uint16_t).  A row may start at any element: rows of an odd width do, and
+// then no 16-byte access is aligned.  The machine takes such accesses of global memory (the ABI sets the unaligned mode); memcpy says so to the compiler,
+// which keeps them whole.
+template <typename T, int N> struct Some {
+    static constexpr int kSize = N, kBytes = N * (int)sizeof(T);
+    uint32_t w[kBytes / 4];
+
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i >= lo && i < hi ? __float_as_uint(p[i]) : 0u;
+        for (uint32_t& v : w) v = 0;
     }
-    __device__ __forceinline__ void zero() { w[0] = u32x4{0, 0, 0, 0}; w[1] = w[0]; }
-    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i / 4][i % 4]); }
-    template <bool PAST = false> static __device__ __forceinline__ void store(float* p, const float* v) {
-        u32x4 q[2];
-        __builtin_memcpy(q, v, 32);
-        if constexpr (PAST) { store_past(p, q[0]); store_past(p + 4, q[1]); }
-        else __builtin_memcpy(p, q, 32);
-    }
-    static __device__ __forceinline__ void store(float* p, const float* v, int lo, int hi) {
+    template <bool PAST = false> __device__ __forceinline__ void load(const T* p) {
+        if constexpr (!PAST) {
+            __builtin_memcpy(w, p, kBytes);
+        } else if constexpr (kBytes == 8) {
+            const u32x2 q = load_past<u32x2>(p);
+            __builtin_memcpy(w, &q, 8);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i >= lo && i < hi) p[i] = v[i];
-    }
-};
-template <> struct Piece<uint16_t> {
-    u32x4 w;
-    template <bool PAST = false> __device__ __forceinline__ void load(const uint16_t* p) {
-        if constexpr (PAST) w = load_past<u32x4>(p);
-        else __builtin_memcpy(&w, p, 16);
-    }
-    __device__ __forceinline__ void load(const uint16_t* p, int lo, int hi) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t even = 2 * i >= lo && 2 * i < hi ? p[2 * i] : 0u, odd = 2 * i + 1 >= lo && 2 * i + 1 < hi ? p[2 * i + 1] : 0u;
-            w[i] = even | odd << 16;
+            for (int k = 0; k < kBytes / 16; ++k) {
+                const u32x4 q = load_past<u32x4>(p + k * (16 / (int)sizeof(T)));
+                __builtin_memcpy(w + 4 * k, &q, 16);
+            }
         }
     }
-    __device__ __forceinline__ void zero() { w = u32x4{0, 0, 0, 0}; }
-    __device__ __forceinline__ float operator[](int i) const { return i & 1 ? __uint_as_float(w[i / 2] & 0xffff0000u) : bf16_value(w[i / 2]); }
-    static __device__ __forceinline__ u32x4 packed(const float* v) {
-        return u32x4{bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]), bf16_pack2(v[4], v[5]), bf16_pack2(v[6], v[7])};
-    }
-    template <bool PAST = false> static __device__ __forceinline__ void store(uint16_t* p, const float* v) {
-        const u32x4 q = packed(v);
-        if constexpr (PAST) store_past(p, q);
-        else __builtin_memcpy(p, &q, 16);
-    }
-    static __device__ __forceinline__ void store(uint16_t* p, const float* v, int lo, int hi) {
-        const u32x4 q = packed(v);
+    // the elements lo .. hi - 1 alone, zeros beside them
+    __device__ __forceinline__ void load(const T* p, int lo, int hi) {
+        zero();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i >= lo && i < hi) p[i] = (uint16_t)(q[i / 2] >> (i & 1 ? 16 : 0));
+        for (int i = 0; i < N; ++i) {
+            if (i < lo || i >= hi) continue;
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
+            else w[i / 2] |= (uint32_t)p[i] << (i & 1 ? 16 : 0);
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return i & 1 ? __uint_as_float(w[i / 2] & 0xffff0000u) : bf16_value(w[i / 2]);
+    }
+    template <bool PAST = false> static __device__ __forceinline__ void store(T* p, const float* v) {
+        uint32_t w[kBytes / 4];
+        if constexpr (sizeof(T) == 4) {
+            __builtin_memcpy(w, v, kBytes);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) w[i] = bf16_pack2(v[2 * i], v[2 * i + 1]);
+        }
+        if constexpr (!PAST) {
+            __builtin_memcpy(p, w, kBytes);
+        } else if constexpr (kBytes == 8) {
+            store_past(p, u32x2{w[0], w[1]});
+        } else {
+#pragma unroll
+            for (int k = 0; k < kBytes / 16; ++k) store_past(p + k * (16 / (int)sizeof(T)), u32x4{w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]});
+        }
+    }
+    static __device__ __forceinline__ void store(T* p, const float* v, int lo, int hi) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i < lo || i >= hi) continue;
+            if constexpr (sizeof(T) == 4) p[i] = v[i];
+            else p[i] = bf16_of(v[i]);
+        }
     }
 };
-// The piece of a row that starts at column c of D: whole, the row's last, or behind its end (zeros, nothing stored).  C: int where c + 8 fits it, else int64_t
-template <bool PAST = false, typename T, typename C> __device__ __forceinline__ Piece<T> load_piece(const T* row, C c, C D) {
-    Piece<T> q;
-    if (c + kPiece <= D) q.template load<PAST>(row + c);
+template <typename T> using Piece = Some<T, kPiece>;
+// Sixteen bytes: what an access of a lane moves.  (Eight elements of fp32 are two accesses, each of which leaves gaps between the lanes.)
+template <typename T> using Unit = Some<T, 16 / (int)sizeof(T)>;
+
+// The N elements of a row from column c of D on: whole, the row's last, or behind its end (zeros, nothing stored).  C: int where c + N fits it, else int64_t
+template <typename S, bool PAST = false, typename T, typename C> __device__ __forceinline__ S load_some(const T* row, C c, C D) {
+    S q;
+    if (c + S::kSize <= D) q.template load<PAST>(row + c);
     else if (c < D) q.load(row + c, 0, (int)(D - c));
     else q.zero();
     return q;
 }
-template <bool PAST = false, typename T, typename C> __device__ __forceinline__ void store_piece(T* row, C c, C D, const float* v) {
-    if (c + kPiece <= D) Piece<T>::template store<PAST>(row + c, v);
-    else if (c < D) Piece<T>::store(row + c, v, 0, (int)(D - c));
+template <typename S, bool PAST = false, typename T, typename C> __device__ __forceinline__ void store_some(T* row, C c, C D, const float* v) {
+    if (c + S::kSize <= D) S::template store<PAST>(row + c, v);
+    else if (c < D) S::store(row + c, v, 0, (int)(D - c));
 }
 
 // Reductions over aligned groups of lanes by DPP (no LDS, no waits): every lane gets the result.  Within 16 lanes the four steps pair each lane with

@@ -252,11 +252,13 @@ def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(out, eager)), k
 
 
-@pytest.mark.parametrize("T,D", [(9001, 4104), (140003, 255), (3001, 16001), (2101, 20007), (35001, 1001)])
-def test_tensors_beyond_the_caches_give_what_their_slices_give(T, D):
+@pytest.mark.parametrize("dtype,T,D", [(torch.bfloat16, 9001, 4104), (torch.bfloat16, 140003, 255), (torch.bfloat16, 3001, 16001), (torch.bfloat16, 2101, 20007),
+                                       (torch.bfloat16, 35001, 1001), (torch.float32, 18001, 1001), (torch.float32, 2101, 8192), (torch.float32, 150003, 120),
+                                       (torch.float32, 1501, 12001), (torch.float32, 1001, 20007)])
+def test_tensors_beyond_the_caches_give_what_their_slices_give(dtype, T, D):
     """Calls of more than 256 MB go past the caches; rows do not depend on one another"""
     gen = torch.Generator(device="cuda").manual_seed(T)
-    x, r, g = ((torch.randn(T, D, device="cuda", generator=gen) * (k + 1)).bfloat16() for k in range(3))
+    x, r, g = ((torch.randn(T, D, device="cuda", generator=gen) * (k + 1)).to(dtype) for k in range(3))
     w = torch.rand(D, device="cuda", generator=gen) + 0.5
     big = pkg.division_rms_norm(x, w, residual=r, code="e4m3", group=64)
     dx, dw = pkg.division_rms_norm_backward(g, big.sum, w, big.rstd, grad_sum=r)
