@@ -191,7 +191,7 @@ int check(int64_t count, const division_gradient* g, bool clip) {
         if (!type_ok(g[i].dt) || g[i].n < 0 || (clip && !type_ok(g[i].out_dt))) return DIVISION_EINVAL;
         if (g[i].n > (int64_t(1) << 40)) return DIVISION_ERANGE;
         if (g[i].n == 0) continue;
-        if (!g[i].grad || (clip && !g[i].out)) return DIVISION_EINVAL;
+        if (!g[i].grad || (clip && (!g[i].out || (g[i].out == g[i].grad && g[i].out_dt != g[i].dt)))) return DIVISION_EINVAL;
         if (!aligned(g[i].grad, g[i].dt == DIVISION_BF16 ? 2 : 4) || (clip && !aligned(g[i].out, g[i].out_dt == DIVISION_BF16 ? 2 : 4))) return DIVISION_EALIGN;
     }
     return DIVISION_OK;

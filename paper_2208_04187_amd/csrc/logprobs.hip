@@ -75,36 +75,41 @@ template <typename T> __device__ __forceinline__ float element(const T* p);
 template <> __device__ __forceinline__ float element(const float* p) { return *p; }
 template <> __device__ __forceinline__ float element(const uint16_t* p) { return bf16_value(*p); }
 
-// The row's results from its joined share
-template <typename T> __device__ __forceinline__ float finish(const LogpArgs& a, int64_t row, const Share& s) {
+// The row's results from its joined share; id and z: the given token and its logit (any number where it is no token)
+__device__ __forceinline__ float finish(const LogpArgs& a, int64_t row, const Share& s, int64_t id, float z) {
     const bool empty = s.sum == 0.0f;                       // every logit -inf
     const float ln = logf(s.sum);
     const float left = huge(s.most) ? 0.0f : kLn2 * __builtin_fmaf(-s.most, kLog2e, point_of(s.most));     // r less its exact value
     const float lse = empty ? -__builtin_inff() : s.most + (ln + left);
     a.lse[row] = lse;
-    if (a.entropy) a.entropy[row] = empty ? 0.0f : ln - s.moment / s.sum * kLn2;
-    const int64_t id = a.ids[row];
+    if (a.entropy) {
+        const float h = ln - s.moment / s.sum * kLn2;
+        a.entropy[row] = empty || h < 0.0f ? 0.0f : h;      // (rounding may leave it just below)
+    }
     float logp = 0.0f;
     if (id != a.ignore) {
         if (id < 0 || id >= a.V) logp = __uint_as_float(0x7fc00000u);   // no such token
-        else logp = empty ? -__builtin_inff() : element(static_cast<const T*>(a.z) + row * a.stride + id) - lse;
+        else logp = empty ? -__builtin_inff() : z - lse;
     }
     a.logp[row] = logp;
     return lse;
 }
+template <typename T> __device__ __forceinline__ float logit_of(const LogpArgs& a, int64_t row, int64_t id) {
+    return id >= 0 && id < a.V ? element(static_cast<const T*>(a.z) + row * a.stride + id) : 0.0f;
+}
 __device__ __forceinline__ float logp_of_top(float z, float lse) { return lse == -__builtin_inff() ? lse : z - lse; }
 
 // The piece at column c of a row that ends at column `end`, -inf behind it
+template <typename T> __device__ __forceinline__ Piece<T> load_logits(const T* row, int c, int end) {
+    Piece<T> q;
+    if (c + kPiece <= end) q.load(row + c);
+    else q.load(row + c, 0, end - c, sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u);
+    return q;
+}
 template <typename T> __device__ __forceinline__ void load_logits(const T* row, int c, int end, float* v) {
-    if (c + kPiece <= end) {
-        Piece<T> q;
-        q.load(row + c);
+    const Piece<T> q = load_logits(row, c, end);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = q[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < end ? element(row + c + i) : -__builtin_inff();
-    }
+    for (int i = 0; i < 8; ++i) v[i] = q[i];
 }
 
 constexpr int kMostTop = 64;
@@ -310,25 +315,27 @@ __global__ __launch_bounds__(kThreads) void log_probs(LogpArgs a) {
     int where = c0 + (int)threadIdx.x * kPiece;             // the batch of the thread's largest logit
     for (int b = c0; b < end; b += kBatch) {
         const int c = b + (int)threadIdx.x * kPiece;
-        float v[kUnroll][8];
+        Piece<T> q[kUnroll];
         if (b + kBatch <= end) {
-            Piece<T> q[kUnroll];
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) q[u].load(row + c + u * (kThreads * kPiece));
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[u][i] = q[u][i];
         } else {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) load_logits(row, c + u * (kThreads * kPiece), end, v[u]);
+            for (int u = 0; u < kUnroll; ++u) q[u] = load_logits(row, c + u * (kThreads * kPiece), end);
         }
+        float v[kUnroll][8];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = q[u][i];
         add_batch<ENTROPY, TOP>(v, c, s, most, seen, where);
     }
-    move(s, most);                                      // to the thread's largest itself
+    const int64_t id = a.ids[at];
+    const float z = a.splits == 1 ? logit_of<T>(a, at, id) : 0.0f;
+    move(s, most);                                          // to the thread's largest itself
     const Share all = over_workgroup(s, slots);
     if (a.splits == 1) {
-        if (threadIdx.x == 0) result = finish<T>(a, at, all);
+        if (threadIdx.x == 0) result = finish(a, at, all, id, z);
     } else if (threadIdx.x == 0) {
         a.shares[item] = all;
     }
@@ -355,15 +362,25 @@ __global__ __launch_bounds__(kThreads) void join_shares(LogpArgs a) {
     __shared__ uint64_t keys[TOP ? kMostKeys : 1], found[TOP ? kMostKeys : 1], bound;
     __shared__ uint32_t count;
     __shared__ float result;
+    const int t = threadIdx.x, n = TOP ? a.splits * a.top : 0;
     for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
-        const int t = threadIdx.x;
-        const Share all = over_workgroup(t < a.splits ? a.shares[row * a.splits + t] : Share{kLowest, 0.0f, 0.0f}, slots);
-        if (t == 0) result = finish<T>(a, row, all);
+        // all that is read leaves before the first wait
+        const int64_t id = a.ids[row];
+        const Share share = t < a.splits ? a.shares[row * a.splits + t] : Share{kLowest, 0.0f, 0.0f};
+        uint64_t mine[TOP ? kMostKeys / kThreads : 1];
+        if constexpr (TOP) {
+#pragma unroll
+            for (int j = 0; j < kMostKeys / kThreads; ++j) mine[j] = t + j * kThreads < n ? a.keys[row * n + t + j * kThreads] : 0;
+        }
+        const float z = logit_of<T>(a, row, id);
+        const Share all = over_workgroup(share, slots);
+        if (t == 0) result = finish(a, row, all, id, z);
         if constexpr (TOP) {
             // each share's keys are in order: of the first few of every share, `top` or more in all, the top-th bounds the row's top-th from
             // below, and only what reaches the bound is put in order
-            const int n = a.splits * a.top, per = (a.top + a.splits - 1) / a.splits;
-            for (int i = t; i < n; i += kThreads) keys[i] = a.keys[row * n + i];
+            const int per = (a.top + a.splits - 1) / a.splits;
+#pragma unroll
+            for (int j = 0; j < kMostKeys / kThreads; ++j) if (t + j * kThreads < n) keys[t + j * kThreads] = mine[j];
             if (t == 0) { count = 0; bound = 1; }
             __syncthreads();
             const float lse = result;
@@ -376,8 +393,9 @@ __global__ __launch_bounds__(kThreads) void join_shares(LogpArgs a) {
             }
             __syncthreads();
             const uint64_t least = bound;
-            for (int i = t; i < n; i += kThreads)
-                if (keys[i] >= least) found[atomicAdd(&count, 1u)] = keys[i];  // any order, put in order below
+#pragma unroll
+            for (int j = 0; j < kMostKeys / kThreads; ++j)
+                if (mine[j] >= least) found[atomicAdd(&count, 1u)] = mine[j];  // any order, put in order below
             __syncthreads();
             const int m = (int)count;
             for (int i = t; i < m; i += kThreads) {

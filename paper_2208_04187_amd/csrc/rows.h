@@ -35,10 +35,11 @@ template <typename T, int N> struct Some {
     static constexpr int kSize = N, kBytes = N * (int)sizeof(T);
     uint32_t w[kBytes / 4];
 
-    __device__ __forceinline__ void zero() {
+    __device__ __forceinline__ void fill(uint32_t word) {
 #pragma unroll
-        for (uint32_t& v : w) v = 0;
+        for (uint32_t& v : w) v = word;
     }
+    __device__ __forceinline__ void zero() { fill(0); }
     template <bool PAST = false> __device__ __forceinline__ void load(const T* p) {
         if constexpr (!PAST) {
             __builtin_memcpy(w, p, kBytes);
@@ -53,14 +54,14 @@ template <typename T, int N> struct Some {
             }
         }
     }
-    // the elements lo .. hi - 1 alone, zeros beside them
-    __device__ __forceinline__ void load(const T* p, int lo, int hi) {
-        zero();
+    // the elements lo .. hi - 1 alone, `word` beside them
+    __device__ __forceinline__ void load(const T* p, int lo, int hi, uint32_t word = 0) {
+        fill(word);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (i < lo || i >= hi) continue;
             if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
-            else w[i / 2] |= (uint32_t)p[i] << (i & 1 ? 16 : 0);
+            else w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (uint32_t)p[i] << 16 : (w[i / 2] & 0xffff0000u) | p[i];
         }
     }
     __device__ __forceinline__ float operator[](int i) const {

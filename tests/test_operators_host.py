@@ -123,6 +123,10 @@ def test_clipping_refuses(change, code):
     assert _clip(**change) == code
 
 
+def test_clipping_into_its_own_memory_keeps_the_type():
+    assert _clip(grads=((4096, 4096, 10, 1, 0),)) == EINVAL and _clip(grads=((4096, 4096, 10, 0, 1),)) == EINVAL
+
+
 def test_gradient_workspace():
     L = pkg.lib()
     d = (ops._GradientDesc * 2)(ops._GradientDesc(64, None, 10, 0, 0), ops._GradientDesc(None, None, 0, 0, 0))
