@@ -14,23 +14,25 @@ __device__ __forceinline__ uint32_t bf16_pack2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2_t));
 }
 
-// Accesses that the caches do not keep.  Calls whose tensors are more than kCached together take them: what is read would not stay till the next
-// one, and the last-level cache (256 MB) loses nothing that it would give.
+// Whole vectors at any element's address: of a type that says so, not byte by byte with memcpy, which the compiler took apart (four fp32 into a store of three and one of one: 513 x
+// 32003 logits' gradient 30 us, 24 so).  PAST: the caches do not keep them.  Calls whose tensors are more than kCached together take that: what is read would not stay till the
+// next one, and the last-level cache (256 MB) loses nothing that it would give.
 constexpr int64_t kCached = int64_t(1) << 28;
-template <typename V, typename T> __device__ __forceinline__ V load_past(const T* p) {
+template <typename V, bool PAST, typename T> __device__ __forceinline__ V load_vector(const T* p) {
     typedef V at_any_element __attribute__((aligned(alignof(T))));
-    return __builtin_nontemporal_load(reinterpret_cast<const at_any_element*>(p));
+    if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const at_any_element*>(p));
+    else return *reinterpret_cast<const at_any_element*>(p);
 }
-template <typename T, typename V> __device__ __forceinline__ void store_past(T* p, V q) {
+template <bool PAST, typename T, typename V> __device__ __forceinline__ void store_vector(T* p, V q) {
     typedef V at_any_element __attribute__((aligned(alignof(T))));
-    __builtin_nontemporal_store(q, reinterpret_cast<at_any_element*>(p));
+    if constexpr (PAST) __builtin_nontemporal_store(q, reinterpret_cast<at_any_element*>(p));
+    else *reinterpret_cast<at_any_element*>(p) = q;
 }
 
 __device__ __forceinline__ uint16_t bf16_of(float v) { return (uint16_t)bf16_pack2(v, 0.0f); }
 
 // N elements of a row in a lane's registers: 4 or 8 of fp32 (float) or bfloat16 (uint16_t).  A row may start at any element: rows of an odd width do, and
-// then no 16-byte access is aligned.  The machine takes such accesses of global memory (the ABI sets the unaligned mode); memcpy says so to the compiler,
-// which keeps them whole.
+// then no 16-byte access is aligned.  The machine takes such accesses of global memory (the ABI sets the unaligned mode).
 template <typename T, int N> struct Some {
     static constexpr int kSize = N, kBytes = N * (int)sizeof(T);
     uint32_t w[kBytes / 4];
@@ -41,16 +43,14 @@ template <typename T, int N> struct Some {
     }
     __device__ __forceinline__ void zero() { fill(0); }
     template <bool PAST = false> __device__ __forceinline__ void load(const T* p) {
-        if constexpr (!PAST) {
-            __builtin_memcpy(w, p, kBytes);
-        } else if constexpr (kBytes == 8) {
-            const u32x2 q = load_past<u32x2>(p);
-            __builtin_memcpy(w, &q, 8);
+        if constexpr (kBytes == 8) {
+            const u32x2 q = load_vector<u32x2, PAST>(p);
+            w[0] = q.x; w[1] = q.y;
         } else {
 #pragma unroll
             for (int k = 0; k < kBytes / 16; ++k) {
-                const u32x4 q = load_past<u32x4>(p + k * (16 / (int)sizeof(T)));
-                __builtin_memcpy(w + 4 * k, &q, 16);
+                const u32x4 q = load_vector<u32x4, PAST>(p + k * (16 / (int)sizeof(T)));
+                w[4 * k] = q.x; w[4 * k + 1] = q.y; w[4 * k + 2] = q.z; w[4 * k + 3] = q.w;
             }
         }
     }
@@ -70,19 +70,16 @@ template <typename T, int N> struct Some {
     }
     template <bool PAST = false> static __device__ __forceinline__ void store(T* p, const float* v) {
         uint32_t w[kBytes / 4];
-        if constexpr (sizeof(T) == 4) {
-            __builtin_memcpy(w, v, kBytes);
-        } else {
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) w[i] = bf16_pack2(v[2 * i], v[2 * i + 1]);
+        for (int i = 0; i < kBytes / 4; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
+            else w[i] = bf16_pack2(v[2 * i], v[2 * i + 1]);
         }
-        if constexpr (!PAST) {
-            __builtin_memcpy(p, w, kBytes);
-        } else if constexpr (kBytes == 8) {
-            store_past(p, u32x2{w[0], w[1]});
+        if constexpr (kBytes == 8) {
+            store_vector<PAST>(p, u32x2{w[0], w[1]});
         } else {
 #pragma unroll
-            for (int k = 0; k < kBytes / 16; ++k) store_past(p + k * (16 / (int)sizeof(T)), u32x4{w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]});
+            for (int k = 0; k < kBytes / 16; ++k) store_vector<PAST>(p + k * (16 / (int)sizeof(T)), u32x4{w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]});
         }
     }
     static __device__ __forceinline__ void store(T* p, const float* v, int lo, int hi) {
