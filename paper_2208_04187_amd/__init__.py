@@ -1,7 +1,8 @@
 """DIVISION activation codec for AMD MI355X: HIP kernels behind a C ABI.
 
 compress / decompress of cached activation maps as in "DIVISION: Memory
-Efficient Training via Dual Activation Precision" (Sec. 4.1 and Sec. 4.2).
+Efficient Training via Dual Activation Precision" (Sec. 4.1 and Sec. 4.2), and the
+operators of a token model's training step beside its products.
 """
 from .binding import (DIVISION_BF16, DIVISION_F32, DivisionError, division_compress,  # noqa: F401
                       division_compress_batch, division_decompress, division_decompress_batch, division_kernel_name, division_packed_bytes, division_packed_layout, lib)
