@@ -113,12 +113,13 @@ template <typename T> __device__ __forceinline__ void load_logits(const T* row, 
 }
 
 constexpr int kMostTop = 64;
-constexpr int kCandidates = 1024;
-struct TopLds {
-    uint64_t keys[kThreads / 2];
+// NT: threads that share a row, 256 or 64
+template <int NT> struct TopLds {
+    static constexpr int kCandidates = 4 * NT;
+    uint64_t keys[NT == 64 ? NT : NT / 2];
     uint64_t found[kCandidates];
     uint64_t bound;
-    uint32_t winners[kThreads];
+    uint32_t winners[NT];
     uint32_t count, threads;
 };
 
@@ -128,15 +129,15 @@ template <int CTRL> __device__ __forceinline__ uint64_t max_with(uint64_t k) {
 }
 
 // Collects the keys from lds.bound up among the columns of the threads whose first key may reach it (upper).  In any order; lds.count may be more than fit.
-template <typename T> __device__ __forceinline__ void collect(const T* row, int c0, int end, uint64_t upper, TopLds& lds) {
+template <int NT, typename T> __device__ __forceinline__ void collect(const T* row, int c0, int end, uint64_t upper, TopLds<NT>& lds) {
     const uint64_t bound = lds.bound;
     const float least = bound == 1 ? -__builtin_inff() : value_of(bound);
     if (upper >= bound) lds.winners[atomicAdd(&lds.threads, 1u)] = threadIdx.x;
     __syncthreads();
-    const uint32_t steps = (uint32_t)(end - c0 + kThreads * kPiece - 1) / (kThreads * kPiece), all = lds.threads * steps;
-    for (uint32_t i = threadIdx.x; i < all; i += kThreads) {
+    const uint32_t steps = (uint32_t)(end - c0 + NT * kPiece - 1) / (NT * kPiece), all = lds.threads * steps;
+    for (uint32_t i = threadIdx.x; i < all; i += NT) {
         const uint32_t w = i / steps;
-        const int c = c0 + (int)((i - w * steps) * kThreads + lds.winners[w]) * kPiece;
+        const int c = c0 + (int)((i - w * steps) * NT + lds.winners[w]) * kPiece;
         if (c >= end) continue;
         float v[8];
         load_logits(row, c, end, v);
@@ -146,29 +147,30 @@ template <typename T> __device__ __forceinline__ void collect(const T* row, int 
             const uint64_t k = key_of(v[j], (uint32_t)(c + j));
             if (k < bound) continue;
             const uint32_t at = atomicAdd(&lds.count, 1u);
-            if (at < kCandidates) lds.found[at] = k;
+            if (at < lds.kCandidates) lds.found[at] = k;
         }
     }
     __syncthreads();
 }
 
 // The `top` first keys of a row's columns from c0 to end, in order, at out[0..top) (0 where there are fewer).  The calling thread's columns are the pieces
-// c0 + (s * kThreads + thread) * 8, s = 0, 1, ...; `seen` is the largest of them, in the batch at column `where` for the first time.  That bounds its first key from both
+// c0 + (s * NT + thread) * 8, s = 0, 1, ...; `seen` is the largest of them, in the batch at column `where` for the first time.  That bounds its first key from both
 // sides, without another look.  The top-th of the lower bounds of all groups of threads bounds the top-th key of all from below: only the
 // threads that may reach it are looked at again.  64 groups of four threads let through G ln(G / (G - top)) = 24 keys for twenty, but all for 64: from 24 on
 // 128 groups of two (89 for 64; putting them in order takes four times as long).  A key for each of the 256 threads instead: 2048 rows of 50048 with
 // twenty keys 77 us, 64 here.
-template <typename T>
-__device__ __forceinline__ void find_top(const T* row, int c0, int end, int top, float seen, int where, TopLds& lds, uint64_t* out) {
+template <int NT, typename T>
+__device__ __forceinline__ void find_top(const T* row, int c0, int end, int top, float seen, int where, TopLds<NT>& lds, uint64_t* out) {
     const int t = threadIdx.x;
     const bool has = c0 + t * kPiece < end;
-    const int last = where + (kUnroll - 1) * kThreads * kPiece + kPiece - 1;
+    const int last = where + (kUnroll - 1) * NT * kPiece + kPiece - 1;
     const int to = last < end ? last : end - 1;
-    uint64_t lower = max_with<kXor1>(has ? key_of(seen, (uint32_t)to) : 0);
-    const int size = top < 24 ? 4 : 2, groups = kThreads / size;
-    if (size == 4) lower = max_with<kXor2>(lower);
+    uint64_t lower = has ? key_of(seen, (uint32_t)to) : 0;
+    const int size = top < (NT == 64 ? 6 : 24) ? 4 : NT == 64 && top >= 12 ? 1 : 2, groups = NT / size;
+    if (size > 1) lower = max_with<kXor1>(lower);
+    if (size > 2) lower = max_with<kXor2>(lower);
     if (t % size == 0) lds.keys[t / size] = lower;
-    if (t == 0) lds.count = lds.threads = 0;
+    if (t == 0) { lds.count = lds.threads = 0; lds.bound = 1; }
     __syncthreads();
     if (t < groups) {
         const uint64_t mine = lds.keys[t];
@@ -182,7 +184,7 @@ __device__ __forceinline__ void find_top(const T* row, int c0, int end, int top,
     }
     __syncthreads();
     collect(row, c0, end, has ? key_of(seen, (uint32_t)where) : 0, lds);
-    if (lds.count > kCandidates) {
+    if (lds.count > lds.kCandidates) {
         // many equal logits at the bound: the threads' first keys themselves give a closer one
         __syncthreads();
         uint64_t best = 0;
@@ -190,7 +192,7 @@ __device__ __forceinline__ void find_top(const T* row, int c0, int end, int top,
             int first_at = where;                           // where every one is -inf or NaN: the first of all
 #pragma unroll 1
             for (int u = kUnroll - 1; u >= 0; --u) {
-                const int c = where + u * (kThreads * kPiece);
+                const int c = where + u * (NT * kPiece);
                 if (c >= end) continue;
                 float v[8];
                 load_logits(row, c, end, v);
@@ -204,15 +206,15 @@ __device__ __forceinline__ void find_top(const T* row, int c0, int end, int top,
         __syncthreads();
         int rank = 0;
 #pragma unroll 8
-        for (int j = 0; j < kThreads; ++j) rank += lds.found[j] > best;
+        for (int j = 0; j < NT; ++j) rank += lds.found[j] > best;
         if (best && rank == top - 1) lds.bound = best;
         __syncthreads();
         collect(row, c0, end, best, lds);
     }
     const int n = (int)lds.count;
-    if (n <= kCandidates) {
+    if (n <= lds.kCandidates) {
         if (t < top && t >= n) out[t] = 0;
-        for (int i = t; i < n; i += kThreads) {
+        for (int i = t; i < n; i += NT) {
             const uint64_t k = lds.found[i];
             int rank = 0;
 #pragma unroll 8
@@ -224,7 +226,7 @@ __device__ __forceinline__ void find_top(const T* row, int c0, int end, int top,
         uint64_t prior = ~0ull;
         for (int r = 0; r < top; ++r) {
             uint64_t mine = 0;
-            for (int c = c0 + t * kPiece; c < end; c += kThreads * kPiece) {
+            for (int c = c0 + t * kPiece; c < end; c += NT * kPiece) {
                 float v[8];
                 load_logits(row, c, end, v);
 #pragma unroll
@@ -238,20 +240,21 @@ __device__ __forceinline__ void find_top(const T* row, int c0, int end, int top,
             __syncthreads();
             uint64_t first = 0;
 #pragma unroll 8
-            for (int i = 0; i < kThreads; ++i) first = lds.found[i] > first ? lds.found[i] : first;
+            for (int i = 0; i < NT; ++i) first = lds.found[i] > first ? lds.found[i] : first;
             if (t == 0) out[r] = first;
             prior = first;
         }
     }
 }
 
-// The workgroup's shares joined; every thread gets the result.  slots: 3 * (kThreads / 64)
-__device__ __forceinline__ Share over_workgroup(const Share& s, float* slots) {
-    constexpr int W = kThreads / 64;
+// The workgroup's shares joined; every thread gets the result.  slots: 3 * (NT / 64)
+template <int NT> __device__ __forceinline__ Share over_workgroup(const Share& s, float* slots) {
+    constexpr int W = NT / 64;
     Share r = s;
     move(r, __uint_as_float(over_lanes<MaxF, 64>(__float_as_uint(s.most))));
     r.sum = sum_lanes<64>(r.sum);
     r.moment = sum_lanes<64>(r.moment);
+    if constexpr (W == 1) return r;
     if ((threadIdx.x & 63) == 0) {
         const int w = threadIdx.x >> 6;
         slots[w] = r.most; slots[W + w] = r.sum; slots[2 * W + w] = r.moment;
@@ -299,13 +302,13 @@ __device__ __forceinline__ void add_batch(const float (&v)[kUnroll][8], int c, S
     }
 }
 
-// A row, or a share of one, per workgroup: 32 logits a thread and batch, loaded before the first is used; ten and a half vector operations a logit (the machine's 2^x counts four), two
+// A row, or a share of one, per workgroup of NT threads: 32 logits a thread and batch, loaded before the first is used; ten and a half vector operations a logit (the machine's 2^x counts four), two
 // thirds of what a bfloat16 row's memory traffic leaves time for.  8192 x 50048 bfloat16: 820 MB in 142 us, 5.8 TB/s, with entropy 148 and twenty alternatives 184; 2048 x 50021
 // with entropy 50 us and with five alternatives 58, 3.6 TB/s: its rows, eight a CU, all reach their end at the same time, and start at odd elements (50048: 42 and 51).
-template <typename T, bool ENTROPY, bool TOP>
-__global__ __launch_bounds__(kThreads) void log_probs(LogpArgs a) {
-    __shared__ float slots[3 * (kThreads / 64)];
-    __shared__ TopLds lds;
+template <typename T, bool ENTROPY, bool TOP, int NT>
+__global__ __launch_bounds__(NT) void log_probs(LogpArgs a) {
+    __shared__ float slots[3 * (NT / 64)];
+    __shared__ TopLds<NT> lds;
     __shared__ float result;
     __shared__ uint64_t first[TOP ? kMostTop : 1];
     const int64_t item = a.first + blockIdx.x, at = a.splits == 1 ? item : item / a.splits;
@@ -315,15 +318,15 @@ __global__ __launch_bounds__(kThreads) void log_probs(LogpArgs a) {
     Share s{kLowest, 0.0f, 0.0f};
     float seen = -__builtin_inff(), most = kLowest;
     int where = c0 + (int)threadIdx.x * kPiece;             // the batch of the thread's largest logit
-    for (int b = c0; b < end; b += kBatch) {
+    for (int b = c0; b < end; b += (kUnroll * NT * kPiece)) {
         const int c = b + (int)threadIdx.x * kPiece;
         Piece<T> q[kUnroll];
-        if (b + kBatch <= end) {
+        if (b + (kUnroll * NT * kPiece) <= end) {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) q[u].load(row + c + u * (kThreads * kPiece));
+            for (int u = 0; u < kUnroll; ++u) q[u].load(row + c + u * (NT * kPiece));
         } else {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) q[u] = load_logits(row, c + u * (kThreads * kPiece), end);
+            for (int u = 0; u < kUnroll; ++u) q[u] = load_logits(row, c + u * (NT * kPiece), end);
         }
         float v[kUnroll][8];
 #pragma unroll
@@ -335,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void log_probs(LogpArgs a) {
     const int64_t id = a.ids[at];
     const float z = a.splits == 1 ? logit_of<T>(a, at, id) : 0.0f;
     move(s, most);                                          // to the thread's largest itself
-    const Share all = over_workgroup(s, slots);
+    const Share all = over_workgroup<NT>(s, slots);
     if (a.splits == 1) {
         if (threadIdx.x == 0) result = finish(a, at, all, id, z);
     } else if (threadIdx.x == 0) {
@@ -375,7 +378,7 @@ __global__ __launch_bounds__(kThreads) void join_shares(LogpArgs a) {
             for (int j = 0; j < kMostKeys / kThreads; ++j) mine[j] = t + j * kThreads < n ? a.keys[row * n + t + j * kThreads] : 0;
         }
         const float z = logit_of<T>(a, row, id);
-        const Share all = over_workgroup(share, slots);
+        const Share all = over_workgroup<kThreads>(share, slots);
         if (t == 0) result = finish(a, row, all, id, z);
         if constexpr (TOP) {
             // each share's keys are in order: of the first few of every share, `top` or more in all, the top-th bounds the row's top-th from
@@ -508,12 +511,21 @@ Split split_of(int64_t T, int64_t V, int top) {
     return {(int)((V + columns - 1) / columns), columns};
 }
 
+template <typename T, int NT> auto log_probs_kernel(const LogpArgs& a) {
+    return a.top ? (a.entropy ? log_probs<T, true, true, NT> : log_probs<T, false, true, NT>)
+                 : (a.entropy ? log_probs<T, true, false, NT> : log_probs<T, false, false, NT>);
+}
+// Short rows are one wavefront's each, whose joins need no barrier and whose end costs a quarter: 65536 x 1000 bfloat16 172 -> 42 us, with five alternatives 309 -> 76; 4096 x 8000 bfloat16 26 -> 19.
+// Longer ones keep four busier: 4096 x 8000 fp32 24 -> 26, 1024 x 30000 bfloat16 13.8 -> 16.5; twenty alternatives of 4096 x 8000 fp32 33 -> 42, of 4096 x 5000 bfloat16 27 -> 22.
+// More than 24 alternatives want more than 64 threads to bound them.
+bool short_row(int64_t V, size_t size, int top) { return top <= 24 && V * (int64_t)size <= (top > 5 ? 12288 : 16384); }
 template <typename T> int launch_log_probs(LogpArgs a, hipStream_t st) {
-    void (*kern)(LogpArgs) = a.top ? (a.entropy ? log_probs<T, true, true> : log_probs<T, false, true>)
-                                   : (a.entropy ? log_probs<T, true, false> : log_probs<T, false, false>);
+    const bool narrow = a.splits == 1 && short_row(a.V, sizeof(T), a.top);
+    void (*kern)(LogpArgs) = narrow ? log_probs_kernel<T, 64>(a) : log_probs_kernel<T, kThreads>(a);
+    const uint32_t threads = narrow ? 64 : kThreads;
     for (a.first = 0; a.first < a.T * a.splits; a.first += kMostItems) {
         const int64_t items = a.T * a.splits - a.first;
-        hipLaunchKernelGGL(kern, dim3((uint32_t)(items < kMostItems ? items : kMostItems)), dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL(kern, dim3((uint32_t)(items < kMostItems ? items : kMostItems)), dim3(threads), 0, st, a);
         CHECKED(launched());
     }
     if (a.splits == 1) return DIVISION_OK;

@@ -292,3 +292,26 @@ def test_gradients_beyond_the_caches_are_what_their_slices_are(dtype, T, V):
     assert torch.equal(part.top_ids, f.top_ids[5:9])
     _check(z[5:9], ids[5:9], part, 3)
     _check(z[5:9], ids[5:9], type(f)(*(v[5:9] for v in f)), 3)
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.bfloat16, 1000), (torch.bfloat16, 4096), (torch.bfloat16, 8190), (torch.float32, 2048), (torch.float32, 4001), (torch.float32, 30)])
+def test_many_short_rows(dtype, V):
+    """Rows that one wavefront works on each, and those just beyond its rule"""
+    z, ids = _logits(1300, V, dtype, 11)
+    low = torch.finfo(dtype).min
+    c = torch.arange(V)
+    z[0] = -INF
+    z[1] = low
+    z[2] = 0.0
+    z[3] = torch.where(c % 512 < 160, 50 + torch.rand(V, generator=torch.Generator().manual_seed(1)), torch.zeros(V)).to(dtype)       # a third of the threads hold all large ones
+    z[4] = torch.where(c % 512 < 160, 50.0, 0.0)
+    z[5, 5:] = -INF
+    z[6] = (z[6] * 2).round()
+    z[7, : V - 1] = -INF
+    z[8] = torch.linspace(-9, 9, V).to(dtype)
+    ids[9] = -100
+    for top in (0, 1, 5, 6, 11, 12, 20, 24, 25):
+        got = pkg.division_log_probs(z.cuda(), ids.cuda(), top=top, want_entropy=top != 6)
+        _check(z, ids, got, top)
+        again = pkg.division_log_probs(z.cuda(), ids.cuda(), top=top, want_entropy=top != 6)
+        assert all(a is None or torch.equal(a, b) for a, b in zip(got, again))
