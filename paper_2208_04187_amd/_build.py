@@ -107,7 +107,7 @@ def build_fastcall() -> Path:
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            "-I", str(root / "include"), "-I", str(root / "include" / "torch" / "csrc" / "api" / "include"),
            "-I", sysconfig.get_paths()["include"], "-I", "/opt/rocm/include", "-o", str(tmp), str(PKG / "csrc" / "fastcall.cpp"),
-           "-L", str(root / "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
+           "-L", str(root / "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         tmp.unlink(missing_ok=True)
