@@ -66,7 +66,7 @@ OPERATOR_DESCS += [_NormDesc, _NormBackDesc, _LogitsDesc, _LogitsBackDesc, _Grad
 
 
 def _fast():
-    """The native side of the binding: plain calls (contiguous tensors, nothing handed in) take the host 5 to 8 us there, 12 to 15 through what
+    """The native side of the binding: plain calls (contiguous tensors, nothing handed in) take the host 4 to 8 us there, 12 to 15 through what
     stands below, which serves every other one."""
     return binding._fast or binding._load_fast()
 
