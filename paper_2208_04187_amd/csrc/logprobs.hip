@@ -21,10 +21,11 @@ constexpr int kThreads = 256;
 constexpr int kUnroll = 4;                                 // pieces a thread has in flight
 constexpr int kBatch = kUnroll * kThreads * kPiece;    // columns of a workgroup's batch
 
-// e^z is taken as 2^(z * kLog2e - r) with r = most * kLog2e rounded: one fused multiplication and the machine's 2^x.  What the rounding of r leaves out is
-// put back where the row's sum is known (finish), and kLog2e's own error counts z - most times 1e-8.  Beyond kHuge the products would leave
-// binary32, but there two different numbers are more than 10^29 apart: a term is 1 at the maximum and 0 elsewhere.
-constexpr float kHuge = 1e37f;
+// e^z is taken as 2^(z * kLog2e - r) with r = most * kLog2e rounded: one fused multiplication and the machine's 2^x.  What the rounding of r leaves out, 2^-24 of it, is
+// the exponent at the maximum itself; it is put back where the row's sum is known (finish), and kLog2e's own error counts z - most times 1e-8.  Below kHuge r is below
+// 2^31 and that exponent within 64: 2^x and sums of it stay in range.  From there on two different binary32 numbers are 64 or more apart (2^30 from the number below it, 128 beyond): a term is 1 at the
+// maximum and 0 elsewhere, good to e^-64.
+constexpr float kHuge = 0x1p30f;
 __device__ __forceinline__ bool huge(float most) { return !(fabsf(most) < kHuge); }
 __device__ __forceinline__ float point_of(float most) { return huge(most) ? (most < 0.0f ? -2.0f * kHuge : 2.0f * kHuge) : most * kLog2e; }
 __device__ __forceinline__ float exp2_of(float t) { return __builtin_amdgcn_exp2f(t); }

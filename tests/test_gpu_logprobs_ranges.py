@@ -1,0 +1,113 @@
+"""Log probabilities where logits are large, share an offset, or are masked with finite numbers, against the definition in 64 bits.
+
+Bounds.  EPS is half a unit in the last place of binary32.  e^d of d = z - max <= 0 is off by (2 |d| + 3) EPS of itself; its exponent is taken against the maximum's own,
+whose rounding r EPS, r up to 2^30 log2 e, is put back later: `back` is that in e's powers, and costs EPS of itself in every term and in the logarithm.  A thread adds up to V / 64
+terms and joins in twenty steps more."""
+import math
+
+import pytest
+import torch
+
+import paper_2208_04187_amd as pkg
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+INF = math.inf
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def _definition(z, ids):
+    """lse, logp, entropy, ln S, mean |d|, the maximum"""
+    z = z.double().cpu()
+    most = z.amax(1)
+    d = z - most[:, None]
+    e = d.exp()
+    S, U = e.sum(1), -(e * d.clamp(min=-1e30)).sum(1)
+    logp = d.gather(1, ids.cpu()[:, None])[:, 0] - S.log()
+    return most + S.log(), logp, S.log() + U / S, S.log(), U / S, most
+
+
+def _bounds(V, mean, most):
+    back = most.abs().clamp(max=2.0 ** 30) * EPS
+    return (V / 64 + 30 + 2 * mean + 4 * back) * EPS, back
+
+
+def _near(got, want, bound, what):
+    got = got.double().cpu()
+    same = got == want.float().double()
+    bad = ~(same | ((got - want).abs() <= bound))
+    assert not bad.any(), (what, int(bad.sum()), got[bad][:4], want[bad][:4])
+
+
+def _order(z, top):
+    z = torch.where(z.isnan(), -INF, z.float().cpu())
+    return z.sort(dim=1, descending=True, stable=True).indices[:, :top]
+
+
+def _check(z, ids, got, top):
+    lse, logp, H, ln, mean, most = _definition(z, ids)
+    off, back = _bounds(z.shape[1], mean, most)
+    _near(got.lse, lse, off + 2 * EPS * lse.abs(), "lse")
+    _near(got.logp, logp, off + 2 * EPS * (lse.abs() + logp.abs()), "logp")
+    _near(got.entropy, H, (off + 10 * EPS) * (1 + H + 3 * mean) + 2 * EPS * H + 4 * EPS * back, "entropy")
+    if top:
+        want = _order(z, top)
+        assert torch.equal(got.top_ids.cpu(), want)
+        d = z.cpu().double().gather(1, want) - lse[:, None]
+        _near(got.top_logp, d, (off + 2 * EPS * lse.abs())[:, None] + 2 * EPS * d.abs(), "top")
+
+
+LARGE = [1e9, 2.0 ** 30 - 64, 2.0 ** 30, 3e9, 1e10, 1e12, 1e20, 1e30]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(1, 40), (3, 3000), (1, 70001), (1300, 300), (1030, 9001)])
+def test_rows_of_one_large_number_are_uniform(T, V, dtype):
+    values = torch.tensor([s * v for v in LARGE for s in (-1.0, 1.0)]).to(dtype)
+    for lo in range(0, len(values), T):
+        rows = values[lo:lo + T]
+        z = rows[:, None].expand(len(rows), V).repeat(-(-T // len(rows)), 1)[:T].contiguous()
+        ids = (torch.arange(T) * 7) % V
+        got = pkg.division_log_probs(z.cuda(), ids.cuda(), top=min(V, 20))
+        _check(z, ids, got, min(V, 20))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(2, 40), (1, 3000), (1, 131072), (5, 70001), (1300, 500), (1030, 9001)])
+def test_finite_masks_leave_the_rest_what_it_is(T, V, dtype):
+    """A mask of a large negative number is -inf to all that is not masked: whole threads', whole shares' columns of it"""
+    gen = torch.Generator().manual_seed(V)
+    z = (torch.randn(T, V, generator=gen) * 3).to(dtype)
+    ids = torch.randint(0, max(1, V // 20), (T,), generator=gen)
+    c = torch.arange(V)
+    for masked in (c >= max(1, V // 20), (c < V - max(1, V // 20)), c % 2 == 1):
+        at = torch.where(masked[ids], (~masked).nonzero()[0], ids)
+        hard = pkg.division_log_probs(z.masked_fill(masked, -INF).cuda(), at.cuda(), top=2)
+        for m in (-1e9, -1e10, -1e12, -1e20, -1e30, torch.finfo(dtype).min):
+            soft = z.masked_fill(masked, m)
+            got = pkg.division_log_probs(soft.cuda(), at.cuda(), top=2)
+            _check(soft, at, got, 2)
+            for a, b in ((got.lse, hard.lse), (got.logp, hard.logp), (got.entropy, hard.entropy)):
+                # a term that is zero either way: the same bits
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_logits_of_many_sizes(dtype):
+    gen = torch.Generator().manual_seed(4)
+    for V in (50, 5000, 40000):
+        z = torch.randn(24, V, generator=gen)
+        for t in range(24):
+            z[t] *= 10.0 ** (t * 1.5)
+        z[0, ::3] = 2.0 ** 30
+        z[1, ::3] = 2.0 ** 30
+        z[1, 1::3] = 2.0 ** 30 - 64
+        z[2] = 2.0 ** 30 - 64
+        z[2, ::5] = 2.0 ** 30 - 128
+        z[3] = -2.0 ** 30
+        z[3, ::5] = -2.0 ** 30 + 64
+        z = z.to(dtype)
+        ids = torch.randint(0, V, (24,), generator=gen)
+        for rows in (slice(None), slice(1, 2), slice(2, 3), slice(20, 21)):
+            _check(z[rows], ids[rows], pkg.division_log_probs(z[rows].cuda(), ids[rows].cuda(), top=9), 9)
