@@ -2,7 +2,8 @@
 compressed tensors cached for the backward pass.
 
 DivisionRMSNorm caches the residual stream's sum and one number a row.  Inside division_saved_tensors the sum is cached compressed as any other
-map of N x C x L (tokens x features) is; the norm's statistic stays exact.
+map of N x C x L (tokens x features) is.  All numbers that belong to rows (the norm's statistic, the codes' scales, lse and entropy) stay exact there: they are saved as
+vectors and matrices, which the hook keeps, whatever dimensions the rows have.
 
 DivisionNormLinear is a norm and the linear layer behind it.  The layer multiplies the norm's output in the model's own type; for its weight's gradient the
 output is cached in 8 bits (int8 or e4m3, a scale for each row or for 32, 64 or 128 columns), the output itself is not kept.
@@ -25,7 +26,7 @@ class _RMSNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, weight, eps):
         n = division_rms_norm(x, weight, eps, residual=residual)
-        ctx.save_for_backward(n.sum, weight, n.rstd)
+        ctx.save_for_backward(n.sum, weight, n.rstd.view(-1))
         ctx.added = residual is not None
         ctx.set_materialize_grads(False)
         return (n.y, n.sum) if ctx.added else n.y
@@ -35,7 +36,8 @@ class _RMSNorm(torch.autograd.Function):
         total, weight, rstd = ctx.saved_tensors
         if grad_y is None:                       # only the sum was used
             return grad_sum, grad_sum if ctx.added else None, None, None
-        dx, dw = division_rms_norm_backward(grad_y.contiguous(), total, weight, rstd, grad_sum=None if grad_sum is None else grad_sum.contiguous())
+        dx, dw = division_rms_norm_backward(grad_y.contiguous(), total, weight, rstd.view(total.shape[:-1]),
+                                            grad_sum=None if grad_sum is None else grad_sum.contiguous())
         return dx, dx if ctx.added else None, dw, None
 
 
@@ -43,7 +45,7 @@ class _NormLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, norm_weight, weight, bias, eps, code, group):
         n = division_rms_norm(x, norm_weight, eps, residual=residual, code=code, group=group)
-        ctx.save_for_backward(n.sum, norm_weight, n.rstd, n.codes, n.scales, weight)
+        ctx.save_for_backward(n.sum, norm_weight, n.rstd.view(-1), n.codes, n.scales.view(-1, n.scales.shape[-1]), weight)
         ctx.added, ctx.with_bias = residual is not None, bias is not None
         ctx.set_materialize_grads(False)
         out = F.linear(n.y, weight, bias)
@@ -55,11 +57,12 @@ class _NormLinear(torch.autograd.Function):
         if grad_out is None:
             return grad_sum, grad_sum if ctx.added else None, None, None, None, None, None, None
         g = grad_out.reshape(-1, grad_out.shape[-1])
-        values = division_read_codes(codes, scales, weight.dtype).view(-1, codes.shape[-1])
+        values = division_read_codes(codes.view(-1, codes.shape[-1]), scales, weight.dtype)
         grad_weight = g.t() @ values if ctx.needs_input_grad[3] else None
         grad_bias = g.sum(0) if ctx.with_bias and ctx.needs_input_grad[4] else None
         grad_y = (g @ weight).view(total.shape)
-        dx, dw = division_rms_norm_backward(grad_y, total, norm_weight, rstd, grad_sum=None if grad_sum is None else grad_sum.contiguous())
+        dx, dw = division_rms_norm_backward(grad_y, total, norm_weight, rstd.view(total.shape[:-1]),
+                                            grad_sum=None if grad_sum is None else grad_sum.contiguous())
         return dx, dx if ctx.added else None, dw, grad_weight, grad_bias, None, None, None
 
 
@@ -100,7 +103,7 @@ class _TokenLogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, ids, top, ignore_index, overwrite):
         f = division_log_probs(logits, ids, top=top, ignore_index=ignore_index)
-        ctx.save_for_backward(logits, ids, f.lse, f.entropy)
+        ctx.save_for_backward(logits, ids, f.lse.view(-1), f.entropy.view(-1))
         ctx.ignore_index, ctx.overwrite = ignore_index, overwrite
         ctx.set_materialize_grads(False)
         ctx.mark_non_differentiable(*(t for t in (f.lse, f.top_logp, f.top_ids) if t is not None))
@@ -108,7 +111,8 @@ class _TokenLogProbs(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_logp, grad_entropy, *rest):
-        logits, ids, lse, entropy = ctx.saved_tensors
+        logits, ids, *per_row = ctx.saved_tensors
+        lse, entropy = (t.view(ids.shape) for t in per_row)
         if grad_logp is None and grad_entropy is None:
             return None, None, None, None, None
         g = torch.zeros_like(lse) if grad_logp is None else grad_logp.contiguous()
