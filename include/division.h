@@ -421,6 +421,7 @@ int division_rms_norm_backward(const division_norm_back *norm, void *hip_stream)
 /*
  * Log probabilities of given tokens (logits: T rows of V, type dt), with the entropy of each row and its most probable tokens:
  *   lse = ln(sum of e^z over the row),  logp = z[id] - lse,  entropy = -(sum of p ln p),  p = e^(z - lse).
+ * logp and top_logp are (z - largest) - ln(sum of e^(z - largest)): an offset that all of a row's logits share takes no digits from them.
  *   ids        [T] token numbers.  ignore_index: logp 0, and no gradient from it.  Any other number outside [0, V): logp NaN.
  *   logp, lse  [T];  entropy  [T], may be null
  *   top        how many alternatives, 0 to 64 and at most V: top_logp, top_ids [T][top], by falling logit, equal ones (and +0, -0) by the lower number;

@@ -1,7 +1,7 @@
 // Log probabilities of given tokens for AMD MI355X (gfx950), with the entropy and the most probable alternatives of each row of
 // logits, and their gradient.  The softmax itself is never stored: a row keeps its logarithm of the sum and its entropy.
 //
-//   t_j = (z_j - m) log2 e;  S = sum 2^t;  U = sum t 2^t;   lse = m + ln S;  logp_i = z_i - lse;  H = ln S - U / S ln 2
+//   t_j = (z_j - m) log2 e;  S = sum 2^t;  U = sum t 2^t;   lse = m + ln S;  logp_i = (z_i - m) - ln S;  H = ln S - U / S ln 2
 //   p = e^(z - lse);    dz = g (delta_t - p) - gh p (ln p + H)
 //
 // One pass over the logits each.  A thread keeps a running (m, S, U) of its share of a row; shares are joined by
@@ -76,13 +76,18 @@ template <typename T> __device__ __forceinline__ float element(const T* p);
 template <> __device__ __forceinline__ float element(const float* p) { return *p; }
 template <> __device__ __forceinline__ float element(const uint16_t* p) { return bf16_value(*p); }
 
+// A row's lse = most + ln in two numbers: a log probability is (z - most) - ln, which a common offset of the logits takes no digits from (rounding lse to one number first does:
+// at an offset of 10^4 half of 10^-3).  ln is -inf where every logit is.
+struct Lse { float most, ln; };
+__device__ __forceinline__ float logp_of(float z, const Lse& l) { return l.ln == -__builtin_inff() ? l.ln : (z - l.most) - l.ln; }
+
 // The row's results from its joined share; id and z: the given token and its logit (any number where it is no token)
-__device__ __forceinline__ float finish(const LogpArgs& a, int64_t row, const Share& s, int64_t id, float z) {
+__device__ __forceinline__ Lse finish(const LogpArgs& a, int64_t row, const Share& s, int64_t id, float z) {
     const bool empty = s.sum == 0.0f;                       // every logit -inf
     const float ln = logf(s.sum);
     const float left = huge(s.most) ? 0.0f : kLn2 * __builtin_fmaf(-s.most, kLog2e, point_of(s.most));     // r less its exact value
-    const float lse = empty ? -__builtin_inff() : s.most + (ln + left);
-    a.lse[row] = lse;
+    const Lse lse{s.most, ln + left};
+    a.lse[row] = empty ? -__builtin_inff() : lse.most + lse.ln;
     if (a.entropy) {
         const float h = ln - s.moment / s.sum * kLn2;
         a.entropy[row] = empty || h < 0.0f ? 0.0f : h;      // (rounding may leave it just below)
@@ -90,7 +95,7 @@ __device__ __forceinline__ float finish(const LogpArgs& a, int64_t row, const Sh
     float logp = 0.0f;
     if (id != a.ignore) {
         if (id < 0 || id >= a.V) logp = __uint_as_float(0x7fc00000u);   // no such token
-        else logp = empty ? -__builtin_inff() : z - lse;
+        else logp = logp_of(z, lse);
     }
     a.logp[row] = logp;
     return lse;
@@ -98,7 +103,6 @@ __device__ __forceinline__ float finish(const LogpArgs& a, int64_t row, const Sh
 template <typename T> __device__ __forceinline__ float logit_of(const LogpArgs& a, int64_t row, int64_t id) {
     return id >= 0 && id < a.V ? element(static_cast<const T*>(a.z) + row * a.stride + id) : 0.0f;
 }
-__device__ __forceinline__ float logp_of_top(float z, float lse) { return lse == -__builtin_inff() ? lse : z - lse; }
 
 // The piece at column c of a row that ends at column `end`, -inf behind it
 template <typename T> __device__ __forceinline__ Piece<T> load_logits(const T* row, int c, int end) {
@@ -310,7 +314,7 @@ template <typename T, bool ENTROPY, bool TOP, int NT>
 __global__ __launch_bounds__(NT) void log_probs(LogpArgs a) {
     __shared__ float slots[3 * (NT / 64)];
     __shared__ TopLds<NT> lds;
-    __shared__ float result;
+    __shared__ Lse result;
     __shared__ uint64_t first[TOP ? kMostTop : 1];
     const int64_t item = a.first + blockIdx.x, at = a.splits == 1 ? item : item / a.splits;
     const int part = (int)(item - at * a.splits);
@@ -349,11 +353,11 @@ __global__ __launch_bounds__(NT) void log_probs(LogpArgs a) {
         find_top(row, c0, end, a.top, seen, where, lds, a.splits == 1 ? first : a.keys + item * a.top);
         if (a.splits == 1) {
             __syncthreads();
-            const float lse = result;
+            const Lse lse = result;
             if ((int)threadIdx.x < a.top) {
                 const uint64_t k = first[threadIdx.x];
                 a.top_ids[at * a.top + threadIdx.x] = column_of(k);
-                a.top_logp[at * a.top + threadIdx.x] = logp_of_top(value_of(k), lse);
+                a.top_logp[at * a.top + threadIdx.x] = logp_of(value_of(k), lse);
             }
         }
     }
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(kThreads) void join_shares(LogpArgs a) {
     __shared__ float slots[3 * (kThreads / 64)];
     __shared__ uint64_t keys[TOP ? kMostKeys : 1], found[TOP ? kMostKeys : 1], bound;
     __shared__ uint32_t count;
-    __shared__ float result;
+    __shared__ Lse result;
     const int t = threadIdx.x, n = TOP ? a.splits * a.top : 0;
     for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
         // all that is read leaves before the first wait
@@ -389,7 +393,7 @@ __global__ __launch_bounds__(kThreads) void join_shares(LogpArgs a) {
             for (int j = 0; j < kMostKeys / kThreads; ++j) if (t + j * kThreads < n) keys[t + j * kThreads] = mine[j];
             if (t == 0) { count = 0; bound = 1; }
             __syncthreads();
-            const float lse = result;
+            const Lse lse = result;
             if (t < a.splits * per) {
                 const uint64_t k = keys[t / per * a.top + t % per];
                 int rank = 0;
@@ -411,7 +415,7 @@ __global__ __launch_bounds__(kThreads) void join_shares(LogpArgs a) {
                 for (int j = 0; j < m; ++j) rank += found[j] > k;
                 if (rank < a.top) {
                     a.top_ids[row * a.top + rank] = column_of(k);
-                    a.top_logp[row * a.top + rank] = logp_of_top(value_of(k), lse);
+                    a.top_logp[row * a.top + rank] = logp_of(value_of(k), lse);
                 }
             }
         }

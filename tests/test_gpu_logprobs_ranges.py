@@ -111,3 +111,36 @@ def test_large_logits_of_many_sizes(dtype):
         ids = torch.randint(0, V, (24,), generator=gen)
         for rows in (slice(None), slice(1, 2), slice(2, 3), slice(20, 21)):
             _check(z[rows], ids[rows], pkg.division_log_probs(z[rows].cuda(), ids[rows].cuda(), top=9), 9)
+
+
+def _check_offsets(z, ids, got, top):
+    """As _check, by bounds that do not grow with lse"""
+    lse, logp, H, ln, mean, most = _definition(z, ids)
+    off, back = _bounds(z.shape[1], mean, most)
+    # the difference from the maximum, ln S, what is put back, and their difference: each rounded once
+    near = off + 2 * EPS * (ln + back)
+    d = z.double().cpu() - most[:, None]
+    _near(got.logp, logp, near + 2 * EPS * (d.gather(1, ids.cpu()[:, None])[:, 0].abs() + logp.abs()), "logp")
+    if top:
+        want = _order(z, top)
+        d = d.gather(1, want)
+        _near(got.top_logp, d - ln[:, None], near[:, None] + 2 * EPS * (d.abs() + (d - ln[:, None]).abs()), "top")
+
+
+def _confident(T, V, gen):
+    """Rows with one token of nearly all probability: log probabilities of -1e-4 to -1e-1"""
+    z = torch.randn(T, V, generator=gen)
+    ids = torch.randint(0, V, (T,), generator=gen)
+    z.scatter_(1, ids[:, None], math.log(V) + 3 + 6 * torch.rand(T, 1, generator=gen))
+    return z, ids
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(1, 1000), (3, 40), (2, 70001), (1300, 300), (1030, 9001)])
+def test_log_probabilities_do_not_lose_digits_to_a_common_offset(T, V, dtype):
+    gen = torch.Generator().manual_seed(T + V)
+    z, ids = _confident(T, V, gen)
+    for offset in (0.0, 300.0, -3e3, 1e4, 1e5):
+        moved = (z + offset).to(dtype)
+        top = min(V, 8)
+        _check_offsets(moved, ids, pkg.division_log_probs(moved.cuda(), ids.cuda(), top=top), top)
