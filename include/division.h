@@ -448,7 +448,13 @@ size_t division_log_probs_workspace(int64_t T, int64_t V, int top);
 int division_log_probs(const division_logits *logits, void *hip_stream);
 
 /*
- * Its gradient: grad_logits = grad_logp (1 at id - p) - grad_entropy p (ln p + entropy), of type dt.  lse and entropy as the forward call wrote them;
+ * The same, and lse_low [T] (null: not wanted) receives what the rounding of each lse to fp32 left out, 0 where lse is -inf: lse + lse_low is good to
+ * the sum's own digits however large the logits are.
+ */
+int division_log_probs_low(const division_logits *logits, float *lse_low, void *hip_stream);
+
+/*
+ * Its gradient: grad_logits = grad_logp (1 at id - p) - grad_entropy p (ln p + entropy), of type dt, with ln p = z - lse.  lse and entropy as the forward call wrote them;
  * grad_entropy (and then entropy) may be null.  grad_logits has rows grad_stride elements apart and may be logits itself (the same stride).
  */
 typedef struct division_logits_back {
@@ -461,6 +467,12 @@ typedef struct division_logits_back {
 } division_logits_back;
 
 int division_log_probs_backward(const division_logits_back *logits, void *hip_stream);
+
+/*
+ * The same with ln p = z - lse - lse_low, lse_low as division_log_probs_low wrote it (null: 0).  Without it p carries lse's rounding, 6e-8 |lse| of itself: a row of large equal
+ * logits has no p of its own left (at 10^10 the gradient is that of p = 1 everywhere).
+ */
+int division_log_probs_backward_low(const division_logits_back *logits, const float *lse_low, void *hip_stream);
 
 /*
  * The global norm of many gradients, and their clipping: norm = sqrt(sum of the squares of all elements), added up in binary64;

@@ -25,8 +25,9 @@ _LIB_PATH = Path(__file__).resolve().parent / "libdivision.so"
 _lib = None
 
 
-# Entries of the operators in operators.py: (name, argument types, result), and their descriptors
+# Entries of the operators in operators.py: (name, argument types, result), those that only callers of lib() use, and their descriptors
 OPERATOR_ENTRIES = []
+OPERATOR_OTHERS = []
 OPERATOR_DESCS = []
 
 
@@ -92,7 +93,7 @@ def lib() -> ctypes.CDLL:
         L.division_decompress_3d.argtypes = [vp, sz, i64, i64, i64, i64, i64, ci, ci, ci, vp, vp]
         L.division_kernel_name_3d.restype = ci
         L.division_kernel_name_3d.argtypes = [ci, vp, i64, i64, i64, i64, i64, ci, ci, ci, ctypes.c_char_p, sz]
-        for name, arguments, result in OPERATOR_ENTRIES:
+        for name, arguments, result in OPERATOR_ENTRIES + OPERATOR_OTHERS:
             entry = getattr(L, name)
             entry.argtypes, entry.restype = arguments, result
         _lib = L

@@ -35,8 +35,8 @@ decltype(&division_read_codes) read_codes;
 decltype(&division_rms_norm_backward_workspace) rms_norm_backward_workspace;
 decltype(&division_rms_norm_backward) rms_norm_backward;
 decltype(&division_log_probs_workspace) log_probs_workspace;
-decltype(&division_log_probs) log_probs;
-decltype(&division_log_probs_backward) log_probs_backward;
+decltype(&division_log_probs_low) log_probs;
+decltype(&division_log_probs_backward_low) log_probs_backward;
 decltype(&division_grad_norm_workspace) grad_norm_workspace;
 decltype(&division_clip_grads) clip_grads;
 
@@ -562,18 +562,21 @@ PyObject* py_rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) 
     END_HANDLE_TH_ERRORS
 }
 
-// log_probs(logits, ids, top, want_entropy, ignore_index)
+// log_probs(logits, ids, top, want_entropy, ignore_index, lse_low)
 PyObject* py_log_probs(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
-    PLAIN(5);
-    const at::Tensor *z = device_tensor(a[0]), *ids = device_tensor(a[1]);
+    PLAIN(6);
+    const at::Tensor *z = device_tensor(a[0]), *ids = device_tensor(a[1]), *low;
     RowsOf r;
     int top;
     int64_t ignore;
-    if (!log_probs || !rows_of(z, &r) || !per_row(ids, at::kLong, *z) || !whole32(a[2], &top) || top < 0 || top > 64 || top > r.D || !PyBool_Check(a[3]) || !whole(a[4], &ignore)) return none();
+    if (!log_probs || !rows_of(z, &r) || !per_row(ids, at::kLong, *z) || !whole32(a[2], &top) || top < 0 || top > 64 || top > r.D || !PyBool_Check(a[3]) || !whole(a[4], &ignore) ||
+        !maybe(a[5], &low) || (low && !per_row(low, at::kFloat, *z)))
+        return none();
     division_logits n{};
     n.logits = z->data_ptr(); n.ids = ids->data_ptr<int64_t>(); n.stride = n.V = r.D; n.T = r.T; n.ignore_index = ignore; n.dt = (division_dtype)r.dt; n.top = top;
     const bool want_entropy = a[3] == Py_True;
+    float* lp = low ? low->data_ptr<float>() : nullptr;
     void* st = current_stream();
     const at::Tensor in = *z;
     at::Tensor logp, entropy, lse, top_logp, top_ids, ws;
@@ -589,33 +592,35 @@ PyObject* py_log_probs(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
         if (n.workspace_bytes) ws = workspace(n.workspace_bytes, in);
         n.logp = logp.data_ptr<float>(); n.lse = lse.data_ptr<float>(); n.entropy = static_cast<float*>(at_or_null(entropy));
         n.top_logp = static_cast<float*>(at_or_null(top_logp)); n.top_ids = static_cast<int64_t*>(at_or_null(top_ids)); n.workspace = at_or_null(ws);
-        return log_probs(&n, st);
+        return log_probs(&n, lp, st);
     });
     return rc ? PyLong_FromLong(rc) : tuple_or_none({logp, entropy, lse, top_logp, top_ids});
     END_HANDLE_TH_ERRORS
 }
 
-// log_probs_backward(logits, ids, lse, grad_logp, entropy, grad_entropy, ignore_index)
+// log_probs_backward(logits, ids, lse, grad_logp, entropy, grad_entropy, ignore_index, lse_low)
 PyObject* py_log_probs_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
-    PLAIN(7);
-    const at::Tensor *z = device_tensor(a[0]), *ids = device_tensor(a[1]), *lse = device_tensor(a[2]), *g = device_tensor(a[3]), *h, *gh;
+    PLAIN(8);
+    const at::Tensor *z = device_tensor(a[0]), *ids = device_tensor(a[1]), *lse = device_tensor(a[2]), *g = device_tensor(a[3]), *h, *gh, *low;
     RowsOf r;
     int64_t ignore;
     if (!log_probs_backward || !rows_of(z, &r) || !per_row(ids, at::kLong, *z) || !per_row(lse, at::kFloat, *z) || !per_row(g, at::kFloat, *z) || !maybe(a[4], &h) ||
-        !maybe(a[5], &gh) || (h && !per_row(h, at::kFloat, *z)) || (gh && (!h || !per_row(gh, at::kFloat, *z))) || !whole(a[6], &ignore))
+        !maybe(a[5], &gh) || (h && !per_row(h, at::kFloat, *z)) || (gh && (!h || !per_row(gh, at::kFloat, *z))) || !whole(a[6], &ignore) ||
+        !maybe(a[7], &low) || (low && !per_row(low, at::kFloat, *z)))
         return none();
     division_logits_back n{};
     n.logits = z->data_ptr(); n.ids = ids->data_ptr<int64_t>(); n.lse = lse->data_ptr<float>(); n.grad_logp = g->data_ptr<float>();
     n.entropy = static_cast<const float*>(at_or_null(h)); n.grad_entropy = static_cast<const float*>(at_or_null(gh));
     n.stride = n.grad_stride = n.V = r.D; n.T = r.T; n.ignore_index = ignore; n.dt = (division_dtype)r.dt;
+    const float* lp = low ? low->data_ptr<float>() : nullptr;
     void* st = current_stream();
     const at::Tensor in = *z;
     at::Tensor out;
     const int rc = without_lock([&] {
         out = fresh_like(in);
         n.grad_logits = out.data_ptr();
-        return log_probs_backward(&n, st);
+        return log_probs_backward(&n, lp, st);
     });
     return rc ? PyLong_FromLong(rc) : wrap(std::move(out));
     END_HANDLE_TH_ERRORS

@@ -2,7 +2,7 @@
 // logits, and their gradient.  The softmax itself is never stored: a row keeps its logarithm of the sum and its entropy.
 //
 //   t_j = (z_j - m) log2 e;  S = sum 2^t;  U = sum t 2^t;   lse = m + ln S;  logp_i = (z_i - m) - ln S;  H = ln S - U / S ln 2
-//   p = e^(z - lse);    dz = g (delta_t - p) - gh p (ln p + H)
+//   ln p = z - lse;    dz = g (delta_t - p) - gh p (ln p + H)
 //
 // One pass over the logits each.  A thread keeps a running (m, S, U) of its share of a row; shares are joined by
 // moving both to the larger m.
@@ -62,7 +62,7 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 struct LogpArgs {
     const void* z;
     const int64_t* ids;
-    float *logp, *entropy, *lse, *top_logp;
+    float *logp, *entropy, *lse, *low, *top_logp;           // low: what lse's rounding left out
     int64_t* top_ids;
     Share* shares;                                          // [T][splits], where a row is split
     uint64_t* keys;                                         // [T][splits][top]
@@ -87,7 +87,12 @@ __device__ __forceinline__ Lse finish(const LogpArgs& a, int64_t row, const Shar
     const float ln = logf(s.sum);
     const float left = huge(s.most) ? 0.0f : kLn2 * __builtin_fmaf(-s.most, kLog2e, point_of(s.most));     // r less its exact value
     const Lse lse{s.most, ln + left};
-    a.lse[row] = empty ? -__builtin_inff() : lse.most + lse.ln;
+    const float one = empty ? -__builtin_inff() : lse.most + lse.ln;
+    a.lse[row] = one;
+    if (a.low) {
+        const float added = one - lse.most;
+        a.low[row] = empty ? 0.0f : (lse.most - (one - added)) + (lse.ln - added);      // exact
+    }
     if (a.entropy) {
         const float h = ln - s.moment / s.sum * kLn2;
         a.entropy[row] = empty || h < 0.0f ? 0.0f : h;      // (rounding may leave it just below)
@@ -428,7 +433,7 @@ __global__ __launch_bounds__(kThreads) void join_shares(LogpArgs a) {
 struct LogpBackArgs {
     const void* z;
     const int64_t* ids;
-    const float *lse, *entropy, *g, *gh;
+    const float *lse, *low, *entropy, *g, *gh;              // low: may be null
     void* out;
     int64_t stride, out_stride, T, V, ignore;
     int64_t parts, first;                                   // batches of a row; the batch that the launch's first workgroup works on
@@ -448,7 +453,9 @@ __global__ __launch_bounds__(kThreads) void log_probs_back(LogpBackArgs a) {
     row -= before;
     out -= before;
     const bool whole = b >= before && b + kBatch <= end;
-    const float lse = a.lse[at], h = ENTROPY ? a.entropy[at] : 0.0f, gh = ENTROPY ? a.gh[at] : 0.0f;
+    // ln p = (z - lse) - low: the second word keeps what p would lose to the rounding of lse (5e-4 of itself at 10^4), and is zero where none is given
+    const float lse = a.lse[at], low = a.low ? a.low[at] : 0.0f, h = ENTROPY ? a.entropy[at] - low : 0.0f, gh = ENTROPY ? a.gh[at] : 0.0f;
+    const float low2 = low * kLog2e;
     const int64_t id = a.ids[at];
     const bool empty = lse == -__builtin_inff(), token = id >= 0 && id < a.V && id != a.ignore;
     const int own = token ? (int)id + before : -N;
@@ -472,7 +479,7 @@ __global__ __launch_bounds__(kThreads) void log_probs_back(LogpBackArgs a) {
         float v[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float d = q[u][i] - lse, p = exp2_of(d * kLog2e);
+            const float d = q[u][i] - lse, p = exp2_of(__builtin_fmaf(d, kLog2e, -low2));
             v[i] = -p * (ENTROPY ? __builtin_fmaf(gh, fmaxf(d, kGone) + h, g) : g);
         }
         if (own >= c && own < c + N) {
@@ -549,7 +556,7 @@ size_t division_log_probs_workspace(int64_t T, int64_t V, int top) {
     return s.splits == 1 ? 0 : (size_t)T * (size_t)s.splits * ((size_t)top * 8u + sizeof(Share));
 }
 
-int division_log_probs(const division_logits* n, void* hip_stream) {
+int division_log_probs_low(const division_logits* n, float* lse_low, void* hip_stream) {
     if (!n || !type_ok(n->dt) || n->top < 0 || n->top > kMostTop || n->top > n->V) return DIVISION_EINVAL;
     CHECKED(sizes_ok(n->T, n->V, n->stride));
     if (n->T == 0) return DIVISION_OK;
@@ -557,12 +564,12 @@ int division_log_probs(const division_logits* n, void* hip_stream) {
     const size_t need = division_log_probs_workspace(n->T, n->V, n->top);
     if (need && !n->workspace) return DIVISION_EINVAL;
     if (!aligned(n->logits, n->dt == DIVISION_BF16 ? 2 : 4) || !aligned(n->ids, 8) || !aligned(n->logp, 4) || !aligned(n->lse, 4) || !aligned(n->entropy, 4) ||
-        !aligned(n->top_logp, 4) || !aligned(n->top_ids, 8) || !aligned(n->workspace, 8))
+        !aligned(n->top_logp, 4) || !aligned(n->top_ids, 8) || !aligned(n->workspace, 8) || !aligned(lse_low, 4))
         return DIVISION_EALIGN;
     if (n->workspace_bytes < need) return DIVISION_ESIZE;
     const Split s = split_of(n->T, n->V, n->top);
     LogpArgs a{};
-    a.z = n->logits; a.ids = n->ids; a.logp = n->logp; a.entropy = n->entropy; a.lse = n->lse; a.top_logp = n->top_logp; a.top_ids = n->top_ids;
+    a.z = n->logits; a.ids = n->ids; a.logp = n->logp; a.entropy = n->entropy; a.lse = n->lse; a.low = lse_low; a.top_logp = n->top_logp; a.top_ids = n->top_ids;
     a.keys = static_cast<uint64_t*>(n->workspace);
     a.shares = reinterpret_cast<Share*>(static_cast<char*>(n->workspace) + (size_t)n->T * s.splits * n->top * 8u);
     a.stride = n->stride; a.T = n->T; a.V = n->V; a.ignore = n->ignore_index; a.split = s.columns; a.splits = s.splits; a.top = n->top;
@@ -570,7 +577,9 @@ int division_log_probs(const division_logits* n, void* hip_stream) {
     return n->dt == DIVISION_F32 ? launch_log_probs<float>(a, st) : launch_log_probs<uint16_t>(a, st);
 }
 
-int division_log_probs_backward(const division_logits_back* n, void* hip_stream) {
+int division_log_probs(const division_logits* n, void* hip_stream) { return division_log_probs_low(n, nullptr, hip_stream); }
+
+int division_log_probs_backward_low(const division_logits_back* n, const float* lse_low, void* hip_stream) {
     if (!n || !type_ok(n->dt)) return DIVISION_EINVAL;
     CHECKED(sizes_ok(n->T, n->V, n->stride));
     CHECKED(sizes_ok(n->T, n->V, n->grad_stride));
@@ -578,11 +587,11 @@ int division_log_probs_backward(const division_logits_back* n, void* hip_stream)
     if (!n->logits || !n->ids || !n->lse || !n->grad_logp || !n->grad_logits || (n->grad_entropy && !n->entropy)) return DIVISION_EINVAL;
     const size_t e = n->dt == DIVISION_BF16 ? 2 : 4;
     if (!aligned(n->logits, e) || !aligned(n->grad_logits, e) || !aligned(n->ids, 8) || !aligned(n->lse, 4) || !aligned(n->entropy, 4) || !aligned(n->grad_logp, 4) ||
-        !aligned(n->grad_entropy, 4))
+        !aligned(n->grad_entropy, 4) || !aligned(lse_low, 4))
         return DIVISION_EALIGN;
     if (n->T > 1 && n->grad_stride < n->V) return DIVISION_EINVAL;          // rows of the gradient must not overlap
     LogpBackArgs a{};
-    a.z = n->logits; a.ids = n->ids; a.lse = n->lse; a.entropy = n->entropy; a.g = n->grad_logp; a.gh = n->grad_entropy; a.out = n->grad_logits;
+    a.z = n->logits; a.ids = n->ids; a.lse = n->lse; a.low = lse_low; a.entropy = n->entropy; a.g = n->grad_logp; a.gh = n->grad_entropy; a.out = n->grad_logits;
     a.stride = n->stride; a.out_stride = n->grad_stride; a.T = n->T; a.V = n->V; a.ignore = n->ignore_index;
     a.parts = (n->V + kPiece - 1 + kBatch - 1) / kBatch;                    // with the columns before a row's first
     // 4096 x 131072 bfloat16: 374 us through the caches, 347 past them; 2048 x 50048 fp32 174 and 156
@@ -598,5 +607,7 @@ int division_log_probs_backward(const division_logits_back* n, void* hip_stream)
     }
     return DIVISION_OK;
 }
+
+int division_log_probs_backward(const division_logits_back* n, void* hip_stream) { return division_log_probs_backward_low(n, nullptr, hip_stream); }
 
 }  // extern "C"

@@ -13,7 +13,7 @@ from typing import NamedTuple
 import torch
 
 from . import binding
-from .binding import OPERATOR_DESCS, OPERATOR_ENTRIES, DivisionError, _dt, _result, _stream, lib
+from .binding import OPERATOR_DESCS, OPERATOR_ENTRIES, OPERATOR_OTHERS, DivisionError, _dt, _result, _stream, lib
 
 _vp, _i64, _ci, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
 _CODES = {None: 0, "int8": 1, "e4m3": 2}
@@ -57,11 +57,13 @@ OPERATOR_ENTRIES += [
     ("division_rms_norm_backward_workspace", [_i64, _i64], _sz),
     ("division_rms_norm_backward", [_vp, _vp], _ci),
     ("division_log_probs_workspace", [_i64, _i64, _ci], _sz),
-    ("division_log_probs", [_vp, _vp], _ci),
-    ("division_log_probs_backward", [_vp, _vp], _ci),
+    ("division_log_probs_low", [_vp, _vp, _vp], _ci),
+    ("division_log_probs_backward_low", [_vp, _vp, _vp], _ci),
     ("division_grad_norm_workspace", [_i64, _vp], _sz),
     ("division_clip_grads", [_i64, _vp, ctypes.c_float, _ci, _vp, _vp, _sz, _vp], _ci),
 ]
+# the same without lse_low
+OPERATOR_OTHERS += [("division_log_probs", [_vp, _vp], _ci), ("division_log_probs_backward", [_vp, _vp], _ci)]
 OPERATOR_DESCS += [_NormDesc, _NormBackDesc, _LogitsDesc, _LogitsBackDesc, _GradientDesc]
 
 
@@ -251,19 +253,25 @@ class LogProbs(NamedTuple):
     top_ids: torch.Tensor | None
 
 
-def division_log_probs(logits: torch.Tensor, ids: torch.Tensor, top: int = 0, want_entropy: bool = True, ignore_index: int = -100, stream=None) -> LogProbs:
+def division_log_probs(logits: torch.Tensor, ids: torch.Tensor, top: int = 0, want_entropy: bool = True, ignore_index: int = -100,
+                       stream=None, lse_low: torch.Tensor | None = None) -> LogProbs:
     """Log probability of ids[...] among logits[..., V] (float32 or bfloat16), the entropy and, for top > 0, the `top` most probable tokens (at most 64).
 
     ids: int64.  Where it is ignore_index the log probability is 0; any other number outside the vocabulary gives NaN.  Logits of -inf are tokens
-    that cannot be; a row of nothing else has log probability -inf and entropy 0."""
+    that cannot be; a row of nothing else has log probability -inf and entropy 0.
+
+    lse_low (float32, a number for each row) receives what lse's rounding left out, for the backward pass: without it the gradient's probabilities are
+    off by lse's last bit, 3e-5 of themselves at an lse of 500."""
     if stream is None:
-        got = _fast().log_probs(logits, ids, top, want_entropy, ignore_index)
+        got = _fast().log_probs(logits, ids, top, want_entropy, ignore_index, lse_low)
         if got is not None:
             return LogProbs._make(_result(got, "division_log_probs"))
     T, stride, V = _rows(logits, "logits")
     lead = logits.shape[:-1]
     _dense(ids, "ids", dtype=torch.int64, shape=lead, device=logits.device)
     dt = _dt(logits.dtype)
+    if lse_low is not None:
+        _dense(lse_low, "lse_low", dtype=torch.float32, shape=lead, device=logits.device)
     if not 0 <= top <= min(64, V):
         raise ValueError("top is 0 to 64, and at most the vocabulary")
     f32 = dict(dtype=torch.float32, device=logits.device)
@@ -275,19 +283,19 @@ def division_log_probs(logits: torch.Tensor, ids: torch.Tensor, top: int = 0, wa
     ws = _workspace(nbytes, logits.device, stream) if nbytes else None
     d = _LogitsDesc(logits.data_ptr(), ids.data_ptr(), stride, T, V, ignore_index, dt, top, logp.data_ptr(), _at(entropy), lse.data_ptr(), _at(top_logp),
                     _at(top_ids), _at(ws), nbytes)
-    _checked(lib().division_log_probs(ctypes.byref(d), _stream(stream)), "division_log_probs")
+    _checked(lib().division_log_probs_low(ctypes.byref(d), _at(lse_low), _stream(stream)), "division_log_probs")
     return LogProbs(logp, entropy, lse, top_logp, top_ids)
 
 
 def division_log_probs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: torch.Tensor, grad_logp: torch.Tensor, entropy: torch.Tensor | None = None,
                                 grad_entropy: torch.Tensor | None = None, ignore_index: int = -100, out: torch.Tensor | None = None,
-                                stream=None) -> torch.Tensor:
+                                stream=None, lse_low: torch.Tensor | None = None) -> torch.Tensor:
     """The gradient of logits from those of logp and of the entropy (None: no gradient comes that way).
 
-    lse and entropy are what division_log_probs gave.  out: where the gradient goes; out=logits overwrites them, which saves a step its second-largest
+    lse, entropy and lse_low (None: zeros) are what division_log_probs gave.  out: where the gradient goes; out=logits overwrites them, which saves a step its second-largest
     tensor."""
     if out is None and stream is None:
-        got = _fast().log_probs_backward(logits, ids, lse, grad_logp, entropy, grad_entropy, ignore_index)
+        got = _fast().log_probs_backward(logits, ids, lse, grad_logp, entropy, grad_entropy, ignore_index, lse_low)
         if got is not None:
             return _result(got, "division_log_probs_backward")
     T, stride, V = _rows(logits, "logits")
@@ -296,7 +304,7 @@ def division_log_probs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: to
     dt = _dt(logits.dtype)
     if grad_entropy is not None and entropy is None:
         raise ValueError("the entropy's gradient needs the entropy")
-    for name, t in (("lse", lse), ("grad_logp", grad_logp), ("entropy", entropy), ("grad_entropy", grad_entropy)):
+    for name, t in (("lse", lse), ("grad_logp", grad_logp), ("entropy", entropy), ("grad_entropy", grad_entropy), ("lse_low", lse_low)):
         if t is not None:
             _dense(t, name, dtype=torch.float32, shape=lead, device=logits.device)
     if out is None:
@@ -307,7 +315,7 @@ def division_log_probs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: to
     _, out_stride, _ = _rows(out, "out")
     d = _LogitsBackDesc(logits.data_ptr(), ids.data_ptr(), lse.data_ptr(), _at(entropy), grad_logp.data_ptr(), _at(grad_entropy), stride, out_stride, T, V,
                         ignore_index, dt, out.data_ptr())
-    _checked(lib().division_log_probs_backward(ctypes.byref(d), _stream(stream)), "division_log_probs_backward")
+    _checked(lib().division_log_probs_backward_low(ctypes.byref(d), _at(lse_low), _stream(stream)), "division_log_probs_backward")
     return out
 
 

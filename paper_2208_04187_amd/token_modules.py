@@ -102,8 +102,9 @@ class DivisionNormLinear(torch.nn.Module):
 class _TokenLogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, ids, top, ignore_index, overwrite):
-        f = division_log_probs(logits, ids, top=top, ignore_index=ignore_index)
-        ctx.save_for_backward(logits, ids, f.lse.view(-1), f.entropy.view(-1))
+        low = torch.empty(ids.shape, dtype=torch.float32, device=ids.device)
+        f = division_log_probs(logits, ids, top=top, ignore_index=ignore_index, lse_low=low)
+        ctx.save_for_backward(logits, ids, f.lse.view(-1), f.entropy.view(-1), low.view(-1))
         ctx.ignore_index, ctx.overwrite = ignore_index, overwrite
         ctx.set_materialize_grads(False)
         ctx.mark_non_differentiable(*(t for t in (f.lse, f.top_logp, f.top_ids) if t is not None))
@@ -112,7 +113,7 @@ class _TokenLogProbs(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad_logp, grad_entropy, *rest):
         logits, ids, *per_row = ctx.saved_tensors
-        lse, entropy = (t.view(ids.shape) for t in per_row)
+        lse, entropy, low = (t.view(ids.shape) for t in per_row)
         if grad_logp is None and grad_entropy is None:
             return None, None, None, None, None
         g = torch.zeros_like(lse) if grad_logp is None else grad_logp.contiguous()
@@ -121,7 +122,7 @@ class _TokenLogProbs(torch.autograd.Function):
             out = logits.detach()
             torch.autograd.graph.increment_version(out)         # who saved the logits too is told that they are gone
         got = division_log_probs_backward(logits, ids, lse, g, entropy=entropy, grad_entropy=None if grad_entropy is None else grad_entropy.contiguous(),
-                                          ignore_index=ctx.ignore_index, out=out)
+                                          ignore_index=ctx.ignore_index, out=out, lse_low=low)
         return got, None, None, None, None
 
 

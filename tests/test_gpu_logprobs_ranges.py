@@ -144,3 +144,91 @@ def test_log_probabilities_do_not_lose_digits_to_a_common_offset(T, V, dtype):
         moved = (z + offset).to(dtype)
         top = min(V, 8)
         _check_offsets(moved, ids, pkg.division_log_probs(moved.cuda(), ids.cuda(), top=top), top)
+
+
+def _gradient(z, ids, g, gh=None):
+    """The gradient of the logits with respect to the definition itself, and its bound: p is off as e^d and as S are, the entropy as in _check"""
+    lse, _, H, ln, mean, most = _definition(z, ids)
+    off, back = _bounds(z.shape[1], mean, most)
+    d = z.double().cpu() - most[:, None] - ln[:, None]
+    p, g = d.exp(), g.double()[:, None]
+    one = torch.zeros_like(p).scatter_(1, ids[:, None], 1.0)
+    lost = (2 * d.abs() + 12) * EPS + (off + 2 * EPS * (ln + back))[:, None]
+    if gh is None:
+        return g * one - p * g, p * g.abs() * lost + 1e-37
+    gh = gh.double()[:, None]
+    per, size = g + gh * (d + H[:, None]), g.abs() + gh.abs() * (d.abs() + H[:, None].abs())
+    wrong = (off + 10 * EPS) * (1 + H + 3 * mean) + 2 * EPS * H + 4 * EPS * back
+    return g * one - p * per, p * (size * lost + gh.abs() * (wrong + off + 2 * EPS * (ln + back))[:, None]) + 1e-37
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(1, 1000), (3, 40), (2, 70001), (1300, 300), (1030, 9001)])
+def test_gradients_do_not_lose_digits_to_a_common_offset(T, V, dtype):
+    gen = torch.Generator().manual_seed(T + V + 1)
+    z, ids = _confident(T, V, gen)
+    g, gh = torch.randn(T, generator=gen), torch.randn(T, generator=gen)
+    for offset in (0.0, -3e3, 1e4, 1e5, 1e10, -1e30):
+        moved = (z + offset).to(dtype)
+        zc, ic = moved.cuda(), ids.cuda()
+        low = torch.empty(T, device="cuda")
+        f = pkg.division_log_probs(zc, ic, lse_low=low)
+        lse, _, _, ln, mean, most = _definition(moved, ids)
+        off, back = _bounds(V, mean, most)
+        _near(f.lse.double() + low.double(), lse, off + 4 * EPS * (ln + back) + lse.abs() * 2.0 ** -46, "both words")
+        for entropy in (False, True):
+            want, bound = _gradient(moved, ids, g, gh if entropy else None)
+            kw = dict(entropy=f.entropy, grad_entropy=gh.cuda()) if entropy else {}
+            got = pkg.division_log_probs_backward(zc, ic, f.lse, g.cuda(), lse_low=low, **kw)
+            lo, hi = want - bound - 2 * EPS * want.abs(), want + bound + 2 * EPS * want.abs()
+            if dtype == torch.bfloat16:
+                lo, hi = lo.float().bfloat16().double(), hi.float().bfloat16().double()
+            r = got.double().cpu()
+            bad = ~((lo <= r) & (r <= hi))
+            assert not bad.any(), (offset, entropy, int(bad.sum()), r[bad][:4], want[bad][:4])
+            # under autograd the second word comes along
+            leaf = zc.clone().requires_grad_()
+            t = pkg.division_token_log_probs(leaf, ic)
+            ((t.logp * g.cuda()).sum() + ((t.entropy * gh.cuda()).sum() if entropy else 0.0)).backward()
+            assert torch.equal(leaf.grad, got)
+
+
+def test_the_second_word_of_lse_is_zero_where_there_is_none():
+    z = torch.randn(6, 3000, generator=torch.Generator().manual_seed(1))
+    z[0] = -INF
+    z[1, 5] = INF
+    z[2, 5] = float("nan")
+    ids = torch.arange(6)
+    for rows in (z, z.repeat(300, 1)):
+        low = torch.full((len(rows),), 7.0, device="cuda")
+        f = pkg.division_log_probs(rows.cuda(), ids.repeat(len(rows) // 6).cuda(), lse_low=low)
+        assert f.lse[0] == -INF and low[0] == 0 and f.lse[1].isnan() and f.lse[2].isnan() and (low[3:6].abs() <= EPS * f.lse[3:6].abs()).all()
+        back = pkg.division_log_probs_backward(rows[:6].cuda(), ids.cuda(), f.lse[:6], torch.ones(6).cuda(), lse_low=low[:6])
+        assert not back[0].any() and back[1:3].isnan().all() and torch.isfinite(back[3:]).all()
+
+
+def test_second_words_of_other_types_and_shapes_are_refused():
+    z, ids = torch.randn(4, 100, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    f = pkg.division_log_probs(z, ids)
+    for low, err in ((torch.empty(4, dtype=torch.float64, device="cuda"), TypeError), (torch.empty(3, device="cuda"), ValueError), (torch.empty(4), ValueError),
+                     (torch.empty(8, device="cuda")[::2], ValueError)):
+        with pytest.raises(err):
+            pkg.division_log_probs(z, ids, lse_low=low)
+        with pytest.raises(err):
+            pkg.division_log_probs_backward(z, ids, f.lse, f.logp, lse_low=low)
+
+
+def test_the_second_word_through_both_sides_of_the_binding():
+    from paper_2208_04187_amd import binding
+    z, ids = torch.randn(3, 5, 3000, device="cuda") + 500, torch.randint(0, 3000, (3, 5), device="cuda")
+    binding._load_fast()
+    results = []
+    for fast in (binding._fast, binding._NothingFast()):
+        was, binding._fast = binding._fast, fast
+        try:
+            low = torch.empty(3, 5, device="cuda")
+            f = pkg.division_log_probs(z, ids, top=2, lse_low=low)
+            results.append([*f, low, pkg.division_log_probs_backward(z, ids, f.lse, f.logp, entropy=f.entropy, grad_entropy=f.logp, lse_low=low)])
+        finally:
+            binding._fast = was
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and results[0][-2].any()
