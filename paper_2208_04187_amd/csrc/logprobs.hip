@@ -199,17 +199,18 @@ __device__ __forceinline__ void find_top(const T* row, int c0, int end, int top,
         __syncthreads();
         uint64_t best = 0;
         if (has) {
-            int first_at = where;                           // where every one is -inf or NaN: the first of all
 #pragma unroll 1
-            for (int u = kUnroll - 1; u >= 0; --u) {
+            for (int u = 0; u < kUnroll; ++u) {             // the first key lies in the batch that `seen` is from; NaN is -inf there too
                 const int c = where + u * (NT * kPiece);
-                if (c >= end) continue;
+                if (c >= end) break;
                 float v[8];
                 load_logits(row, c, end, v);
 #pragma unroll
-                for (int i = 7; i >= 0; --i) if (v[i] == seen && c + i < end) first_at = c + i;
+                for (int i = 0; i < 8; ++i) {
+                    const uint64_t k = key_of(v[i], (uint32_t)(c + i));
+                    if (k > best && c + i < end) best = k;
+                }
             }
-            best = key_of(seen, (uint32_t)first_at);
         }
         lds.found[t] = best;
         if (t == 0) { lds.count = lds.threads = 0; lds.bound = 1; }

@@ -232,3 +232,22 @@ def test_the_second_word_through_both_sides_of_the_binding():
         finally:
             binding._fast = was
     assert all(torch.equal(a, b) for a, b in zip(*results)) and results[0][-2].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(1100, 20001), (1, 20001), (1, 131072), (1300, 8000), (1300, 4000), (1300, 30)])
+def test_nan_counts_as_minus_infinity_among_many_of_them(T, V, dtype):
+    """More tokens that cannot be than fit beside one another, NaN before them, and fewer finite logits than alternatives"""
+    z = torch.full((T, V), -INF)
+    z[:, :8] = float("nan")
+    z[:, V - 3] = 1.0
+    if T > 1:
+        z[1] = -INF
+        z[1, 9:17] = float("nan")
+        z[2, 100 % V:] = float("nan")
+        z[3] = float("nan")
+    z = z.to(dtype)
+    ids = torch.zeros(T, dtype=torch.int64)
+    for top in (5, 20, 30):
+        got = pkg.division_log_probs(z.cuda(), ids.cuda(), top=top)
+        assert torch.equal(got.top_ids[:5].cpu(), _order(z[:5], top)) and (got.top_ids[4:] == got.top_ids[-1]).all()
