@@ -163,30 +163,36 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_rows(NormArgs a) {
     }
 }
 
-// Rows too long for the registers: read twice (the second time from the caches where they hold it).  The largest |y| of the row is
-// that of |s * w| times rstd, which the first pass finds beside the sum.  4096 x 40000 bfloat16: 205 us, 1.6 times what a copy of the bytes takes; such rows are rare.
+// Rows too long for the registers: read twice (the second time from the caches where they hold it), and a third time where one scale is the row's: the largest |y| is that of y itself,
+// as in norm_rows (|s * w|, which the first pass could find, leaves binary32 where y does not).  4096 x 40000 bfloat16: 161 us a call, 1.25 times what a copy
+// of the bytes takes; with int8 codes and their reading back 309 us where groups of 64 columns have scales, 325 where rows have.
 template <typename T, bool RES>
 __global__ __launch_bounds__(1024) void norm_wide(NormArgs a) {
     constexpr int N = Unit<T>::kSize;
     __shared__ uint32_t slots[2 * 16];
     for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
         float sq = 0.0f;
-        uint32_t most = 0;
         for (int64_t c = (int64_t)threadIdx.x * N; c < a.D; c += 1024 * N) {
-            float v[N], w[N];
+            float v[N];
             load_sum<T, RES, false>(a, row, c, a.D, v);
-            load_weight<N>(a.weight, a.weight_bf16, c, a.D, w);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                sq = __builtin_fmaf(v[i], v[i], sq);
-                most = MaxU::of(most, __float_as_uint(v[i] * w[i]) & 0x7fffffffu);
-            }
+            for (int i = 0; i < N; ++i) sq = __builtin_fmaf(v[i], v[i], sq);
         }
         sq = row_sum<1024>(sq, slots);
-        most = over_row<MaxU, 1024>(most, slots + 16);
         const float rstd = 1.0f / sqrtf(sq / (float)a.D + a.eps);
-        most = __float_as_uint(__uint_as_float(most) * rstd);
         if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+        uint32_t most = 0;
+        if (a.code != DIVISION_CODE_NONE && a.group == 0) {
+            for (int64_t c = (int64_t)threadIdx.x * N; c < a.D; c += 1024 * N) {
+                float v[N], w[N];
+                load_sum<T, RES, false>(a, row, c, a.D, v);
+                load_weight<N>(a.weight, a.weight_bf16, c, a.D, w);
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] = v[i] * rstd * w[i];
+                most = MaxU::of(most, most_of<N>(v));
+            }
+            most = over_row<MaxU, 1024>(most, slots + 16);
+        }
         for (int64_t c0 = 0; c0 < a.D; c0 += 1024 * N) {    // every lane takes part in its group's maximum
             const int64_t c = c0 + (int64_t)threadIdx.x * N;
             float v[N], w[N];
