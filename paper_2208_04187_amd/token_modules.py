@@ -6,7 +6,8 @@ map of N x C x L (tokens x features) is.  All numbers that belong to rows (the n
 vectors and matrices, which the hook keeps, whatever dimensions the rows have.
 
 DivisionNormLinear is a norm and the linear layer behind it.  The layer multiplies the norm's output in the model's own type; for its weight's gradient the
-output is cached in 8 bits (int8 or e4m3, a scale for each row or for 32, 64 or 128 columns), the output itself is not kept.
+output is cached in 8 bits (int8 or e4m3, a scale for each row or for 32, 64 or 128 columns), the output itself is not kept.  Under autocast the layer's products are of its type, the norm of
+the stream's.
 
 division_token_log_probs is the loss: log probabilities and entropies with their gradients, alternatives beside them.  Of [tokens, vocabulary] only the logits are kept, and
 `overwrite` hands their memory to their gradient.
@@ -56,14 +57,23 @@ class _NormLinear(torch.autograd.Function):
         total, norm_weight, rstd, codes, scales, weight = ctx.saved_tensors
         if grad_out is None:
             return grad_sum, grad_sum if ctx.added else None, None, None, None, None, None, None
+        # the products in the type of the forward pass's, which autocast may have chosen; gradients in their tensors' types
         g = grad_out.reshape(-1, grad_out.shape[-1])
-        values = division_read_codes(codes.view(-1, codes.shape[-1]), scales, weight.dtype)
-        grad_weight = g.t() @ values if ctx.needs_input_grad[3] else None
-        grad_bias = g.sum(0) if ctx.with_bias and ctx.needs_input_grad[4] else None
-        grad_y = (g @ weight).view(total.shape)
+        values = division_read_codes(codes.view(-1, codes.shape[-1]), scales, torch.bfloat16 if g.dtype == torch.bfloat16 else torch.float32).to(g.dtype)
+        grad_weight = (g.t() @ values).to(weight.dtype) if ctx.needs_input_grad[3] else None
+        grad_bias = g.sum(0).to(weight.dtype) if ctx.with_bias and ctx.needs_input_grad[4] else None
+        grad_y = (g @ weight.to(g.dtype)).to(total.dtype).view(total.shape)
         dx, dw = division_rms_norm_backward(grad_y, total, norm_weight, rstd.view(total.shape[:-1]),
                                             grad_sum=None if grad_sum is None else grad_sum.contiguous())
         return dx, dx if ctx.added else None, dw, grad_weight, grad_bias, None, None, None
+
+
+def _beside_the_stream(x, residual):
+    """Under autocast a layer's output may be narrower than the stream it is added to: both in the wider type, as torch's own addition has it"""
+    if residual is None or x.dtype == residual.dtype or not torch.is_autocast_enabled(x.device.type):
+        return x, residual
+    wide = torch.promote_types(x.dtype, residual.dtype)
+    return x.to(wide), residual.to(wide)
 
 
 class DivisionRMSNorm(torch.nn.Module):
@@ -77,6 +87,7 @@ class DivisionRMSNorm(torch.nn.Module):
     def forward(self, x, residual=None):
         if residual is None:
             return _RMSNorm.apply(x, None, self.weight, self.eps), x
+        x, residual = _beside_the_stream(x, residual)
         return _RMSNorm.apply(x, residual, self.weight, self.eps)
 
 
@@ -96,6 +107,7 @@ class DivisionNormLinear(torch.nn.Module):
         args = (self.norm.weight, self.linear.weight, self.linear.bias, self.norm.eps, self.code, self.group)
         if residual is None:
             return _NormLinear.apply(x, None, *args), x
+        x, residual = _beside_the_stream(x, residual)
         return _NormLinear.apply(x, residual, *args)
 
 

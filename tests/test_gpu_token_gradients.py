@@ -1,4 +1,7 @@
-"""The modules of a token model's step beside the rest of torch: the saved-tensor hook."""
+"""The modules of a token model's step beside the rest of torch: the saved-tensor hook, autocast."""
+import os
+import sys
+
 import pytest
 import torch
 
@@ -73,3 +76,68 @@ def test_lse_and_entropy_stay_exact_under_the_saved_tensor_hook():
         (f.logp.sum() + f.entropy.sum()).backward()
         got.append(z.grad)
     assert torch.equal(got[0], got[1])
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("inside", [False, True])
+def test_norm_linear_trains_under_autocast(kind, inside):
+    gen = torch.Generator().manual_seed(4)
+    x, r, g = torch.randn(4, 6, 192, generator=gen).cuda(), torch.randn(4, 6, 192, generator=gen).cuda(), torch.randn(4, 6, 96, generator=gen).cuda()
+    m = pkg.DivisionNormLinear(192, 96, bias=True, code="int8", device="cuda")
+    got = []
+    for cast in (False, True):
+        m.zero_grad()
+        xc, rc = x.clone().requires_grad_(), r.clone().requires_grad_()
+        with torch.autocast("cuda", dtype=kind, enabled=cast):
+            out, s = m(xc, rc)
+            assert out.dtype == (kind if cast else torch.float32) and s.dtype == torch.float32
+            loss = (out * g).sum() + s.sum()
+            if inside:
+                loss.backward()
+        if not inside:
+            loss.backward()
+        got.append([t.clone() for t in (out.detach(), xc.grad, rc.grad, m.norm.weight.grad, m.linear.weight.grad, m.linear.bias.grad)])
+        assert all(t.dtype == torch.float32 for t in got[-1][1:])
+    # inputs and results of the products rounded to eight bits or more: 2^-8 each of three
+    for a, b in zip(got[1], got[0]):
+        _close(a, b, 3 * 2.0 ** -8)
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+def test_norms_take_a_layers_output_beside_a_wider_stream_under_autocast(kind):
+    """torch's own x + stream would be of the wider type"""
+    gen = torch.Generator().manual_seed(5)
+    x, r = torch.randn(4, 6, 192, generator=gen).cuda().to(kind), torch.randn(4, 6, 192, generator=gen).cuda()
+    norm, layer = pkg.DivisionRMSNorm(192, device="cuda"), pkg.DivisionNormLinear(192, 96, device="cuda")
+    for m in (norm, layer):
+        grads = []
+        for a in (x, x.float()):
+            a, b = a.clone().requires_grad_(), r.clone().requires_grad_()
+            with torch.autocast("cuda", dtype=kind):
+                y, s = m(a, b)
+            assert s.dtype == torch.float32
+            (y.float().sum() + s.sum()).backward()
+            assert a.grad.dtype == a.dtype
+            grads.append((y.detach(), s.detach(), a.grad.to(kind), b.grad))
+        assert all(torch.equal(p, q) for p, q in zip(*grads))
+    with pytest.raises((ValueError, TypeError)):
+        norm(x, r)                                  # without autocast types are the caller's to choose
+
+
+def test_the_examples_model_trains_under_autocast():
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import token_model
+    torch.manual_seed(0)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    net = token_model.TokenModel(97, dtype=torch.float32)
+    adam, losses = torch.optim.Adam(net.parameters(), lr=0.01), []
+    for step in range(120):
+        tokens = token_model.sample(97, 32, 64, gen)
+        with pkg.division_saved_tensors(B=8, b=4, seed=step * 1000), torch.autocast("cuda", dtype=torch.bfloat16):
+            loss = -pkg.division_token_log_probs(net(tokens[:, :-1]), tokens[:, 1:].contiguous(), overwrite=True).logp.mean()
+        loss.backward()
+        pkg.division_clip_grads([p.grad for p in net.parameters()], 0.5)
+        adam.step()
+        adam.zero_grad()
+        losses.append(loss.detach())
+    assert losses[0] > 4.0 and torch.stack(losses[-10:]).mean() < 0.9
