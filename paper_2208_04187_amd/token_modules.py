@@ -12,15 +12,43 @@ the stream's.
 division_token_log_probs is the loss: log probabilities and entropies with their gradients, alternatives beside them.  Of [tokens, vocabulary] only the logits are kept, and
 `overwrite` hands their memory to their gradient.
 
-Only calls the binding and torch's products.
+First derivatives only: a second one raises.  Only calls the binding and torch's products.
 """
 from __future__ import annotations
+
+import functools
 
 import torch
 import torch.nn.functional as F
 
 from .operators import (LogProbs, division_log_probs, division_log_probs_backward, division_read_codes, division_rms_norm,
                         division_rms_norm_backward)
+
+
+class _NoSecond(torch.autograd.Function):
+    """t, as the result of a graph that cannot be followed"""
+
+    @staticmethod
+    def forward(ctx, t, anchor):
+        return t.view_as(t)
+
+    @staticmethod
+    def backward(ctx, grad):
+        raise RuntimeError("trying to differentiate twice a function that has first derivatives only")
+
+
+def _first_derivatives(backward):
+    """Where a graph of the backward pass is asked for (create_graph), its results raise when they are differentiated.  (once_differentiable lets those through whose
+    incoming gradient is a constant, as of out.sum(): a gradient penalty beside a loss would be dropped in silence.)"""
+    @functools.wraps(backward)
+    def first(ctx, *grads):
+        with torch.no_grad():
+            got = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return got
+        anchor = torch.empty(0, requires_grad=True)
+        return tuple(g if g is None else _NoSecond.apply(g, anchor) for g in got)
+    return first
 
 
 class _RMSNorm(torch.autograd.Function):
@@ -33,6 +61,7 @@ class _RMSNorm(torch.autograd.Function):
         return (n.y, n.sum) if ctx.added else n.y
 
     @staticmethod
+    @_first_derivatives
     def backward(ctx, grad_y, grad_sum=None):
         total, weight, rstd = ctx.saved_tensors
         if grad_y is None:                       # only the sum was used
@@ -53,6 +82,7 @@ class _NormLinear(torch.autograd.Function):
         return (out, n.sum) if ctx.added else out
 
     @staticmethod
+    @_first_derivatives
     def backward(ctx, grad_out, grad_sum=None):
         total, norm_weight, rstd, codes, scales, weight = ctx.saved_tensors
         if grad_out is None:
@@ -123,6 +153,7 @@ class _TokenLogProbs(torch.autograd.Function):
         return tuple(f)
 
     @staticmethod
+    @_first_derivatives
     def backward(ctx, grad_logp, grad_entropy, *rest):
         logits, ids, *per_row = ctx.saved_tensors
         lse, entropy, low = (t.view(ids.shape) for t in per_row)

@@ -1,4 +1,4 @@
-"""The modules of a token model's step beside the rest of torch: the saved-tensor hook, autocast."""
+"""The modules of a token model's step beside the rest of torch: the saved-tensor hook, autocast, second derivatives."""
 import os
 import sys
 
@@ -141,3 +141,18 @@ def test_the_examples_model_trains_under_autocast():
         adam.zero_grad()
         losses.append(loss.detach())
     assert losses[0] > 4.0 and torch.stack(losses[-10:]).mean() < 0.9
+
+
+def test_second_derivatives_raise():
+    x, r = (torch.randn(3, 5, 64, device="cuda", requires_grad=True) for _ in range(2))
+    z, ids = torch.randn(3, 100, device="cuda", requires_grad=True), torch.zeros(3, dtype=torch.int64, device="cuda")
+    norm, layer = pkg.DivisionRMSNorm(64, device="cuda"), pkg.DivisionNormLinear(64, 32, device="cuda")
+    for leaf, call in ((x, lambda: norm(x, r)[0]), (x, lambda: layer(x, r)[0]), (layer.linear.weight, lambda: layer(x, r)[0]), (z, lambda: pkg.division_token_log_probs(z, ids).logp),
+                       (z, lambda: pkg.division_token_log_probs(z, ids).entropy)):
+        # also of a plain sum, whose incoming gradient is a constant, beside a loss that can be differentiated
+        for loss in (lambda y: y.square().sum(), lambda y: y.sum()):
+            plain, = torch.autograd.grad(loss(call()), leaf)
+            first, = torch.autograd.grad(loss(call()), leaf, create_graph=True)
+            assert torch.equal(first, plain)
+            with pytest.raises(RuntimeError, match="differentiate twice"):
+                (leaf.sum() + first.square().sum()).backward()
