@@ -147,7 +147,7 @@ class _TokenLogProbs(torch.autograd.Function):
         low = torch.empty(ids.shape, dtype=torch.float32, device=ids.device)
         f = division_log_probs(logits, ids, top=top, ignore_index=ignore_index, lse_low=low)
         ctx.save_for_backward(logits, ids, f.lse.view(-1), f.entropy.view(-1), low.view(-1))
-        ctx.ignore_index, ctx.overwrite = ignore_index, overwrite
+        ctx.ignore_index, ctx.overwrite, ctx.overwritten = ignore_index, overwrite, False
         ctx.set_materialize_grads(False)
         ctx.mark_non_differentiable(*(t for t in (f.lse, f.top_logp, f.top_ids) if t is not None))
         return tuple(f)
@@ -162,6 +162,9 @@ class _TokenLogProbs(torch.autograd.Function):
         g = torch.zeros_like(lse) if grad_logp is None else grad_logp.contiguous()
         out = None
         if ctx.overwrite:
+            if ctx.overwritten:                                 # torch itself does not look at the versions of what a saved-tensor hook has kept
+                raise RuntimeError("the logits have been overwritten by an earlier backward pass")
+            ctx.overwritten = True
             out = logits.detach()
             torch.autograd.graph.increment_version(out)         # who saved the logits too is told that they are gone
         got = division_log_probs_backward(logits, ids, lse, g, entropy=entropy, grad_entropy=None if grad_entropy is None else grad_entropy.contiguous(),
@@ -172,7 +175,8 @@ class _TokenLogProbs(torch.autograd.Function):
 def division_token_log_probs(logits: torch.Tensor, ids: torch.Tensor, top: int = 0, ignore_index: int = -100, overwrite: bool = False) -> LogProbs:
     """division_log_probs with gradients through logp and the entropy.
 
-    overwrite: the backward pass writes the gradient over the logits, which nothing else may need by then (a second backward pass raises)."""
+    overwrite: the backward pass writes the gradient over the logits, which nothing else may need by then.  A second backward pass raises; so does that of an
+    operation that saved the logits too, except under a saved-tensor hook, where torch does not see that they are gone."""
     lead = logits.shape[:-1]
     if logits.is_contiguous() and logits.dim() > 2 and logits.numel() > 0 and ids.shape == lead and ids.is_contiguous():
         # as rows: the saved-tensor hook keeps tensors of two dimensions as they are, and a softmax of rebuilt logits would be another one

@@ -156,3 +156,23 @@ def test_second_derivatives_raise():
             assert torch.equal(first, plain)
             with pytest.raises(RuntimeError, match="differentiate twice"):
                 (leaf.sum() + first.square().sum()).backward()
+
+
+@pytest.mark.parametrize("hook", [lambda: torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t), lambda: pkg.division_saved_tensors(B=8, b=2)])
+def test_a_second_backward_pass_over_overwritten_logits_raises_under_a_hook(hook):
+    """torch does not look at versions of what a hook has kept"""
+    leaf = torch.randn(3, 100, device="cuda", requires_grad=True)
+    ids = torch.zeros(3, dtype=torch.int64, device="cuda")
+    with hook():
+        f = pkg.division_token_log_probs(leaf * 1.0, ids, overwrite=True)
+    f.logp.sum().backward(retain_graph=True)
+    once = leaf.grad.clone()
+    with pytest.raises(RuntimeError, match="overwritten"):
+        f.logp.sum().backward()
+    assert torch.equal(leaf.grad, once)
+    with hook():
+        f = pkg.division_token_log_probs(leaf * 1.0, ids)
+    leaf.grad = None
+    f.logp.sum().backward(retain_graph=True)
+    f.logp.sum().backward()
+    assert torch.equal(leaf.grad, 2 * once)
