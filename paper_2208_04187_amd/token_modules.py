@@ -182,4 +182,4 @@ def division_token_log_probs(logits: torch.Tensor, ids: torch.Tensor, top: int =
         # as rows: the saved-tensor hook keeps tensors of two dimensions as they are, and a softmax of rebuilt logits would be another one
         logits, ids = logits.view(-1, logits.shape[-1]), ids.view(-1)
     got = _TokenLogProbs.apply(logits, ids, int(top), int(ignore_index), bool(overwrite))
-    return LogProbs._make(t if t is None else t.view(*lead, *t.shape[logits.dim() - 1:]) for t in got)
+    return LogProbs._make(t if t is None else t.view((*lead, *t.shape[logits.dim() - 1:])) for t in got)

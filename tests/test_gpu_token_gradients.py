@@ -176,3 +176,14 @@ def test_a_second_backward_pass_over_overwritten_logits_raises_under_a_hook(hook
     f.logp.sum().backward(retain_graph=True)
     f.logp.sum().backward()
     assert torch.equal(leaf.grad, 2 * once)
+
+
+def test_one_row_of_logits_alone():
+    z, i = torch.randn(301, device="cuda"), torch.tensor(17, device="cuda")
+    a, b = z.clone().requires_grad_(), z[None].clone().requires_grad_()
+    f, g = pkg.division_token_log_probs(a, i, top=3), pkg.division_token_log_probs(b, i[None], top=3)
+    for p, q in zip(f, g):
+        assert p.shape == q.shape[1:] and torch.equal(p, q[0])
+    f.logp.backward()
+    g.logp.sum().backward()
+    assert torch.equal(a.grad, b.grad[0])
