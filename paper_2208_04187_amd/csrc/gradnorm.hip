@@ -30,7 +30,7 @@ template <int N> struct Sources {
 };
 template <int N> struct Targets { void* out[N]; };
 struct NormArgs { Sources<288> t; double* parts; };
-struct ClipArgs { Sources<184> t; Targets<184> to; const double* parts; const float* factor; float* norm; float limit; int count; };
+struct ClipArgs { Sources<184> t; Targets<184> to; const double *parts, *factor; float* norm; float limit; int count; };
 static_assert(sizeof(NormArgs) <= 4096 && sizeof(ClipArgs) <= 4096, "kernel arguments");
 
 // The tensor of a run: the last one whose first run is not behind it.  The lanes hold the first runs of all tensors, so that a search is one read of the argument block
@@ -98,17 +98,14 @@ __global__ __launch_bounds__(kThreads) void add_squares(NormArgs a) {
     if (threadIdx.x == 0) a.parts[blockIdx.x] = s;
 }
 
-// The factor of the clipping, in two: the second is 1, or a power of two where the first alone would leave binary32's normal range
-struct Factor { float f, power; };
-__device__ __forceinline__ Factor factor_of(double norm, float limit) {
-    double c = limit / (norm + 1e-6);
-    c = c > 1.0 ? 1.0 : c;                                  // NaN stays
-    const bool small = c < 0x1p-100;
-    return {(float)(small ? c * 0x1p126 : c), small ? 0x1p-126f : 1.0f};
+// The factor of the clipping
+__device__ __forceinline__ double factor_of(double norm, float limit) {
+    const double c = limit / (norm + 1e-6);
+    return c > 1.0 ? 1.0 : c;                               // NaN stays
 }
 
 // The norm from the parts, and the factor (null: only the norm): 2048 parts 4.9 us
-__global__ __launch_bounds__(1024) void join_squares(const double* parts, int64_t count, float limit, float* norm, float* factor) {
+__global__ __launch_bounds__(1024) void join_squares(const double* parts, int64_t count, float limit, float* norm, double* factor) {
     __shared__ double slots[16];
     double s = 0.0;
     for (int64_t i = threadIdx.x; i < count; i += 1024) s += parts[i];
@@ -116,11 +113,7 @@ __global__ __launch_bounds__(1024) void join_squares(const double* parts, int64_
     if (threadIdx.x == 0) {
         const double n = sqrt(s);
         *norm = (float)n;
-        if (factor) {
-            const Factor c = factor_of(n, limit);
-            factor[0] = c.f;
-            factor[1] = c.power;
-        }
+        if (factor) *factor = factor_of(n, limit);
     }
 }
 
@@ -132,22 +125,32 @@ __device__ __forceinline__ void put(uint16_t* p, float v) { *p = bf16_of(v); }
 // A run of n elements.  Four a lane and access, so that the lanes' stores lie next to one another whatever the two types are (eight of fp32 are two stores
 // with gaps: 336 M gradients 641 us, 491 with four).  Stores go past the caches, which keep what the first pass has read of the gradients instead: 460 us, and of 25.6 M
 // gradients 38 us instead of 46.
-template <typename I, typename O> __device__ __forceinline__ void scale(const I* p, O* o, int n, float f, float power) {
+// A factor below kSmall may leave binary32's normal range, where its products with large elements do not: those are of binary64.
+constexpr double kSmall = 0x1p-100;
+template <typename I, typename O> __device__ __forceinline__ void scale(const I* p, O* o, int n, double c) {
     constexpr int U = (int)(kRun / (kThreads * 4));
+    const float f = (float)c;
     if (n == kRun) {
         Some<I, 4> q[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) q[u].load(p + (u * kThreads + threadIdx.x) * 4);
+        // (asked behind the loads, which need not wait for the factor: 336 M gradients 456 us, 464 with the question before them)
+        const bool small = c < kSmall;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[4];
+            if (small) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = q[u][i] * f * power;
+                for (int i = 0; i < 4; ++i) v[i] = (float)(q[u][i] * c);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = q[u][i] * f;
+            }
             Some<O, 4>::template store<true>(o + (u * kThreads + threadIdx.x) * 4, v);
         }
     } else {
 #pragma unroll 4
-        for (int i = threadIdx.x; i < n; i += kThreads) put(o + i, value(p + i) * f * power);
+        for (int i = threadIdx.x; i < n; i += kThreads) put(o + i, c < kSmall ? (float)(value(p + i) * c) : value(p + i) * f);
     }
 }
 
@@ -155,7 +158,7 @@ template <typename I, typename O> __device__ __forceinline__ void scale(const I*
 // parts itself, in the same order, instead of a launch between the two passes.  Bound by memory: 336 M bfloat16 gradients into fp32 2013 MB in 338 us, 6.0 TB/s.
 template <bool JOIN>
 __global__ __launch_bounds__(kThreads) void scale_all(ClipArgs a) {
-    Factor f;
+    double f;
     if constexpr (JOIN) {
         __shared__ double slots[kThreads / 64];
         double s = 0.0;
@@ -164,20 +167,20 @@ __global__ __launch_bounds__(kThreads) void scale_all(ClipArgs a) {
         if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
         f = factor_of(norm, a.limit);
     } else {
-        f = {a.factor[0], a.factor[1]};
+        f = *a.factor;
     }
     const uint32_t run = blockIdx.x;
     const int k = Tensors<decltype(a.t)>(a.t).of(run);
     const void* in = a.t.in[k];
     void* out = a.to.out[k];
-    if (f.f == 1.0f && f.power == 1.0f && in == out) return;
+    if ((float)f == 1.0f && in == out) return;
     const int64_t c = (int64_t)(run - a.t.first[k]) * kRun;
     const int n = elements_of(a.t, run, k);
     switch (a.t.last[k] & (kInBf16 | kOutBf16)) {
-        case 0: scale(static_cast<const float*>(in) + c, static_cast<float*>(out) + c, n, f.f, f.power); break;
-        case kInBf16: scale(static_cast<const uint16_t*>(in) + c, static_cast<float*>(out) + c, n, f.f, f.power); break;
-        case kOutBf16: scale(static_cast<const float*>(in) + c, static_cast<uint16_t*>(out) + c, n, f.f, f.power); break;
-        default: scale(static_cast<const uint16_t*>(in) + c, static_cast<uint16_t*>(out) + c, n, f.f, f.power);
+        case 0: scale(static_cast<const float*>(in) + c, static_cast<float*>(out) + c, n, f); break;
+        case kInBf16: scale(static_cast<const uint16_t*>(in) + c, static_cast<float*>(out) + c, n, f); break;
+        case kOutBf16: scale(static_cast<const float*>(in) + c, static_cast<uint16_t*>(out) + c, n, f); break;
+        default: scale(static_cast<const uint16_t*>(in) + c, static_cast<uint16_t*>(out) + c, n, f);
     }
 }
 
@@ -253,7 +256,7 @@ int division_clip_grads(int64_t count, const division_gradient* grads, float lim
     if (!aligned(norm, 4) || !aligned(workspace, 16)) return DIVISION_EALIGN;
     if (workspace_bytes < division_grad_norm_workspace(count, grads)) return DIVISION_ESIZE;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    float* factor = static_cast<float*>(workspace);
+    double* factor = static_cast<double*>(workspace);
     double* parts = reinterpret_cast<double*>(static_cast<char*>(workspace) + 16);
     int64_t done = 0, runs = 0, made = 0;
     NormArgs a;
