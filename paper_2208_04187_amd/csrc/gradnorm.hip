@@ -98,8 +98,9 @@ __global__ __launch_bounds__(kThreads) void add_squares(NormArgs a) {
     if (threadIdx.x == 0) a.parts[blockIdx.x] = s;
 }
 
-// The factor of the clipping
+// The factor of the clipping: 0 where the norm is infinite, whatever the limit is
 __device__ __forceinline__ double factor_of(double norm, float limit) {
+    if (norm == __builtin_inf()) return 0.0;
     const double c = limit / (norm + 1e-6);
     return c > 1.0 ? 1.0 : c;                               // NaN stays
 }

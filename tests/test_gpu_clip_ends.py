@@ -38,3 +38,16 @@ def test_a_small_factor_under_a_large_limit(n, dtype):
                     if a.dtype == torch.bfloat16:
                         lo, hi = lo.float().bfloat16().double(), hi.float().bfloat16().double()
                     assert ((lo <= r) & (r <= hi)).all(), (largest, limit, out_type)
+
+
+def test_no_limit():
+    """An infinite limit: finite gradients stay, an infinite norm makes the factor 0 as under any other limit"""
+    for many in (1, 300):
+        g = [torch.randn(70, device="cuda") for _ in range(many)] + [torch.randn(9, device="cuda").bfloat16()]
+        keep = [t.clone() for t in g]
+        assert math.isfinite(pkg.division_clip_grads(g, math.inf).item()) and all(torch.equal(a, b) for a, b in zip(g, keep))
+        g[0][3] = math.inf
+        assert pkg.division_clip_grads(g, math.inf).item() == math.inf
+        assert g[0][3].isnan() and not g[0][:3].any() and not g[0][4:].any() and not any(t.any() for t in g[1:])
+        keep[0][3] = float("nan")
+        assert pkg.division_clip_grads(keep, math.inf).isnan() and all(t.isnan().all() for t in keep)
