@@ -467,6 +467,11 @@ PyObject* tuple_or_none(std::initializer_list<at::Tensor> ts) {
 }
 at::Tensor workspace(size_t n, const at::Tensor& x) { return fresh({(int64_t)(n ? n : 1)}, at::kByte, x); }
 
+// as _written of operators.py: a tensor of the caller's that a call writes over
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // rms_norm(x, weight, eps, residual, code, group, want_y): code as a number
 PyObject* py_rms_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
@@ -594,6 +599,7 @@ PyObject* py_log_probs(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
         n.top_logp = static_cast<float*>(at_or_null(top_logp)); n.top_ids = static_cast<int64_t*>(at_or_null(top_ids)); n.workspace = at_or_null(ws);
         return log_probs(&n, lp, st);
     });
+    if (low && !rc) written(*low);
     return rc ? PyLong_FromLong(rc) : tuple_or_none({logp, entropy, lse, top_logp, top_ids});
     END_HANDLE_TH_ERRORS
 }
@@ -654,6 +660,8 @@ PyObject* py_clip_grads(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     const size_t need = grad_norm_workspace(count, grads.data());
     ws = workspace(need, one);
     const int rc = clip_grads(count, grads.data(), limit, clip, norm.data_ptr<float>(), ws.data_ptr(), need, st);
+    if (clip && !rc)
+        for (Py_ssize_t i = 0; i < count; ++i) written(THPVariable_Unpack(PySequence_Fast_GET_ITEM(a[1] == Py_None ? a[0] : a[1], i)));
     return rc ? PyLong_FromLong(rc) : wrap(std::move(norm));
     END_HANDLE_TH_ERRORS
 }

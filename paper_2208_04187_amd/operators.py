@@ -117,6 +117,11 @@ def _at(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
+def _written(*tensors):
+    """Tensors of the caller's that a call writes over: autograd compares versions before it uses what it saved."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
+
+
 def _workspace(nbytes: int, device, stream):
     """Memory for one call.  torch hands it out again when the call's tensors are gone: to the current stream's next call, behind this
     one, or, where the call runs on another stream, not before that stream has passed it."""
@@ -203,6 +208,7 @@ def division_read_codes(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.
         out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
     else:
         _dense(out, "out", shape=codes.shape, device=codes.device)
+        _written(out)
     if D == 0:
         raise DivisionError(1, "division_read_codes")
     _checked(lib().division_read_codes(codes.data_ptr(), scales.data_ptr(), codes.numel() // D, D, _CODES[code], group, _dt(out.dtype),
@@ -235,6 +241,7 @@ def division_rms_norm_backward(grad_y: torch.Tensor, sum: torch.Tensor, weight: 
         out = torch.empty(sum.shape, dtype=sum.dtype, device=sum.device)
     else:
         _dense(out, "out", dtype=sum.dtype, shape=sum.shape, device=sum.device)
+        _written(out)
     grad_weight = torch.empty_like(weight)
     nbytes = int(lib().division_rms_norm_backward_workspace(T, D))
     ws = _workspace(nbytes, sum.device, stream)
@@ -284,6 +291,7 @@ def division_log_probs(logits: torch.Tensor, ids: torch.Tensor, top: int = 0, wa
     d = _LogitsDesc(logits.data_ptr(), ids.data_ptr(), stride, T, V, ignore_index, dt, top, logp.data_ptr(), _at(entropy), lse.data_ptr(), _at(top_logp),
                     _at(top_ids), _at(ws), nbytes)
     _checked(lib().division_log_probs_low(ctypes.byref(d), _at(lse_low), _stream(stream)), "division_log_probs")
+    _written(lse_low)
     return LogProbs(logp, entropy, lse, top_logp, top_ids)
 
 
@@ -311,6 +319,8 @@ def division_log_probs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: to
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     elif out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must have the logits' shape and type")
+    else:
+        _written(out)
     _beside(out, logits.device, "out")
     _, out_stride, _ = _rows(out, "out")
     d = _LogitsBackDesc(logits.data_ptr(), ids.data_ptr(), lse.data_ptr(), _at(entropy), grad_logp.data_ptr(), _at(grad_entropy), stride, out_stride, T, V,
@@ -360,6 +370,8 @@ def _grads(grads, out, limit, stream, what):
     ws = _workspace(nbytes, device, stream)
     _checked(lib().division_clip_grads(len(grads), descs, limit if limit is not None else 0.0, limit is not None, norm.data_ptr(), ws.data_ptr(), nbytes,
                                        _stream(stream)), what)
+    if limit is not None:
+        _written(*outs)
     return norm
 
 

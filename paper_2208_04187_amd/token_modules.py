@@ -165,8 +165,7 @@ class _TokenLogProbs(torch.autograd.Function):
             if ctx.overwritten:                                 # torch itself does not look at the versions of what a saved-tensor hook has kept
                 raise RuntimeError("the logits have been overwritten by an earlier backward pass")
             ctx.overwritten = True
-            out = logits.detach()
-            torch.autograd.graph.increment_version(out)         # who saved the logits too is told that they are gone
+            out = logits.detach()                               # shares their version: who saved them too is told that they are gone
         got = division_log_probs_backward(logits, ids, lse, g, entropy=entropy, grad_entropy=None if grad_entropy is None else grad_entropy.contiguous(),
                                           ignore_index=ctx.ignore_index, out=out, lse_low=low)
         return got, None, None, None, None

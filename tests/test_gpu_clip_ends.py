@@ -51,3 +51,51 @@ def test_no_limit():
         assert g[0][3].isnan() and not g[0][:3].any() and not g[0][4:].any() and not any(t.any() for t in g[1:])
         keep[0][3] = float("nan")
         assert pkg.division_clip_grads(keep, math.inf).isnan() and all(t.isnan().all() for t in keep)
+
+
+def _general(call):
+    """The call without the binding's native side"""
+    from paper_2208_04187_amd import binding
+    binding._load_fast()
+    fast, binding._fast = binding._fast, binding._NothingFast()
+    try:
+        return call()
+    finally:
+        binding._fast = fast
+
+
+def test_autograd_is_told_of_what_is_written_over():
+    def moved(tensors, call):
+        was = [t._version for t in tensors]
+        call()
+        return [t._version > v for t, v in zip(tensors, was)]
+    for how in (lambda call: call(), _general):
+        g, out = [torch.randn(40, device="cuda"), torch.randn(3, 5, device="cuda")], [torch.empty(40, device="cuda"), torch.empty(3, 5, device="cuda")]
+        assert moved(g + out, lambda: how(lambda: pkg.division_clip_grads(g, 0.1))) == [True, True, False, False]
+        assert moved(g + out, lambda: how(lambda: pkg.division_clip_grads(g, 0.1, out=out))) == [False, False, True, True]
+        assert moved(g, lambda: how(lambda: pkg.division_grad_norm(g))) == [False, False]
+    x, w, ids = torch.randn(4, 64, device="cuda"), torch.ones(64, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    n, f = pkg.division_rms_norm(x, w, code="int8"), pkg.division_log_probs(x, ids)
+    out = torch.empty_like(x)
+    assert moved([x, out], lambda: pkg.division_read_codes(n.codes, n.scales, out=out)) == [False, True]
+    assert moved([x, out], lambda: pkg.division_rms_norm_backward(x, x, w, n.rstd, out=out)) == [False, True]
+    assert moved([x, out], lambda: pkg.division_log_probs_backward(x, ids, f.lse, f.logp, out=out)) == [False, True]
+    # who saved the logits is told that they are gone
+    leaf = torch.randn(4, 64, device="cuda", requires_grad=True)
+    z = leaf * 1.0
+    square = (z * z).sum()
+    pkg.division_log_probs_backward(z.detach(), ids, f.lse, f.logp, out=z.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        square.backward()
+
+
+def test_tensors_without_versions_are_clipped_too():
+    with torch.inference_mode():
+        g = [torch.randn(40, device="cuda"), torch.randn(7, device="cuda")]
+        out = [torch.empty_like(t) for t in g]
+    keep = [t.clone() for t in g]
+    for how in (lambda call: call(), _general):
+        how(lambda: pkg.division_clip_grads(g, 0.5, out=out))
+        assert all(not torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(g, out, keep))
+    pkg.division_clip_grads(g, 0.5)
+    assert all(torch.equal(a, b) for a, b in zip(g, out))
