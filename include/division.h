@@ -370,7 +370,8 @@ typedef enum { DIVISION_CODE_NONE = 0, DIVISION_CODE_INT8 = 1, DIVISION_CODE_E4M
 /*
  * Root-mean-square norm, with the residual stream's addition before it and an output in 8 bits behind it:
  *   s = x + residual (x where residual is null),  rstd = 1 / sqrt(mean of s^2 over the row + eps),  y = s * rstd * weight,
- * s and y in fp32; `sum` receives s rounded to dt, `y` y rounded to dt, the codes are y's own (not of the rounded y).
+ * s, its squares and y in fp32 (a row whose squares add up to more than 3.4e38 has rstd 0, and y 0); `sum` receives s rounded to dt, `y` y rounded to dt, the codes are y's own (not of the
+ * rounded y).
  *   sum     required with a residual (may be x or residual itself where that is dense), unused without one
  *   y       may be null (only codes are wanted)
  *   rstd    [T], may be null

@@ -168,7 +168,9 @@ template <int NT, typename T> __device__ __forceinline__ void collect(const T* r
 // sides, without another look.  The top-th of the lower bounds of all groups of threads bounds the top-th key of all from below: only the
 // threads that may reach it are looked at again.  64 groups of four threads let through G ln(G / (G - top)) = 24 keys for twenty, but all for 64: from 24 on
 // 128 groups of two (89 for 64; putting them in order takes four times as long).  A key for each of the 256 threads instead: 2048 rows of 50048 with
-// twenty keys 77 us, 64 here.
+// twenty keys 77 us, 64 here.  A wavefront's rows go by groups of four threads below six keys, of two below twelve, and by single threads from there on: 16384 x 3000 fp32 (and 65536 x 1000
+// bfloat16) with five keys 42.3, 42.4 and 43.5 us (72, 78 and 91), with eleven 52.4, 50.2 and 50.1 (79, 84 and 97), with twenty, for which sixteen groups of four are too few, 59.3 by two and 56.5
+// by one (90 and 101): longer rows gain by closer bounds, shorter ones by fewer keys to rank.
 template <int NT, typename T>
 __device__ __forceinline__ void find_top(const T* row, int c0, int end, int top, float seen, int where, TopLds<NT>& lds, uint64_t* out) {
     const int t = threadIdx.x;

@@ -381,7 +381,7 @@ def division_grad_norm(grads, stream=None) -> torch.Tensor:
 
 
 def division_clip_grads(grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
-    """Scales the gradients by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out` (of the same shapes; float32
+    """Scales the gradients by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out` (of the same shapes and strides; float32
     outputs for bfloat16 gradients, for instance), and returns their norm before that.  Nothing waits for the device: where the
     norm is not finite the gradients are not either, and the caller that wants to skip the step looks at it."""
     if not max_norm >= 0:
