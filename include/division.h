@@ -500,6 +500,140 @@ size_t division_grad_norm_workspace(int64_t count, const division_gradient *grad
 int division_clip_grads(int64_t count, const division_gradient *grads, float limit, int clip, float *norm,
                         void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/*
+ * Attention.  Query head h of H reads key head h / (H / G) of G.  q is [B][Sq][H][D], k and v are [B][Sk][G][D]: D elements next to one another, the three other
+ * strides (batch, token, head; in elements) any from 0 up that keep every row on 16 bytes, at most 8 MB a token and 64 MB for all heads (DIVISION_ERANGE).  D is a multiple of 8 up to 128;
+ * Sq and Sk up to 2^29, Sq * H / G up to 2^30, H up to 4096, B up to 2^24.
+ *
+ * Sequence b has min(Sk, max(0, lengths[b])) keys (all Sk where lengths is null); what lies behind them is not looked at and may hold anything.  Its query i stands at position
+ * starts[b] + i among the keys (Sk - Sq + i where starts is null).  It sees key j of them unless causal is 1 and j lies behind its position, or window > 0 and the two are window or
+ * more apart.  A key that some query sees and another does not reaches the other only where it or its value is not finite.
+ *
+ *   z = scale q k^T,   p = softmax(z) over the keys that are seen,   out = p v,   lse = ln(sum of exp(z))
+ *
+ * scale: positive and finite.  Products of bfloat16 tensors take their factors as they are, probabilities (and, backward, the scores' gradients) rounded to bfloat16; sums,
+ * maxima and exponentials are fp32.  fp32 tensors are multiplied in fp32.  A query that sees no key has out 0, lse -infinity and no gradient.
+ *   out  [B][Sq][H][D] of type dt, dense, on 16 bytes;   lse  [B][H][Sq]
+ *   workspace  division_attention_workspace(attention) bytes on 16, for few queries over many keys (may be null where that is 0)
+ */
+typedef struct division_attention {
+    const void *q, *k, *v;
+    int64_t q_strides[3], k_strides[3], v_strides[3];
+    int64_t B, Sq, Sk, H, G, D;
+    division_dtype dt;
+    float scale;
+    int causal;
+    int64_t window;
+    const int32_t *lengths, *starts;
+} division_attention;
+
+size_t division_attention_workspace(const division_attention *attention);
+
+int division_attend(const division_attention *attention, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Its backward pass: the gradients of q, k and v from that of out, and from out and lse as division_attend wrote them.
+ *   grad_out  as q, with strides of its own
+ *   grad_q [B][Sq][H][D], grad_k and grad_v [B][Sk][G][D], dense, on 16 bytes, written in full (zeros for keys that no query sees); sums over queries and heads are in an order
+ *             that sizes and positions alone decide
+ *   workspace division_attention_backward_workspace(attention) bytes on 16
+ */
+typedef struct division_attention_back {
+    const void *grad_out, *out;
+    const float *lse;
+    int64_t grad_out_strides[3];
+    void *grad_q, *grad_k, *grad_v;
+    void *workspace;
+    size_t workspace_bytes;
+} division_attention_back;
+
+size_t division_attention_backward_workspace(const division_attention *attention);
+
+int division_attention_backward(const division_attention *attention, const division_attention_back *back, void *hip_stream);
+
+/*
+ * The norms of queries and keys, head by head, and the rotation by their positions, in one pass.  x[0] are T tokens of heads[0] heads of D elements, x[1] the same tokens' heads[1] heads
+ * (0: there are none): elements next to one another, heads and tokens any stride from 0 up (in elements).
+ *   u = x / sqrt(mean of x^2 over the head + eps) * weight,   y = u with its first `rotated` elements turned: pair p (a, b) -> (a cos w - b sin w, a sin w + b cos w),
+ *   w = positions[t] * frequencies[p]
+ * rounded to dt once.  The pairs are elements (p, rotated / 2 + p), or (2 p, 2 p + 1) where next is 1; rotated / 2 frequencies, binary64.  Angles are taken in binary64.
+ * D is even and up to 512, rotated even and up to D, heads up to 4096 each.
+ *   y[k]     [T][heads[k]][D] of type dt, dense: may be x[k] itself where that is dense
+ *   rstd[k]  [T][heads[k]], may be null
+ */
+typedef struct division_rotate {
+    const void *x[2], *weight[2];
+    int64_t token_strides[2], head_strides[2], heads[2];
+    division_dtype weight_dt[2];
+    int64_t T, D, rotated;
+    division_dtype dt;
+    int next;
+    float eps;
+    const double *frequencies;
+    const int64_t *positions;
+    void *y[2];
+    float *rstd[2];
+} division_rotate;
+
+int division_head_norm_rotate(const division_rotate *rotate, void *hip_stream);
+
+/*
+ * Its backward pass: x, weight, frequencies and positions as in the forward call, whose y and rstd are not looked at.
+ *   grad_y[k]       the gradient of y[k], token_strides and head_strides its own;   rstd[k] as the forward call wrote it
+ *   grad_x[k]       [T][heads[k]][D] of type dt, dense: may be grad_y[k] or x[k] itself where that is dense
+ *   grad_weight[k]  [D] of type weight_dt[k]: the sum over tokens and heads in an order that sizes alone decide (zeros for T == 0)
+ *   workspace       division_head_norm_rotate_backward_workspace(T, D) bytes on 16
+ */
+typedef struct division_rotate_back {
+    const void *grad_y[2];
+    const float *rstd[2];
+    int64_t token_strides[2], head_strides[2];
+    void *grad_x[2], *grad_weight[2];
+    void *workspace;
+    size_t workspace_bytes;
+} division_rotate_back;
+
+size_t division_head_norm_rotate_backward_workspace(int64_t T, int64_t D);
+
+int division_head_norm_rotate_backward(const division_rotate *rotate, const division_rotate_back *back, void *hip_stream);
+
+/*
+ * Rows of a table, scaled: out[t] = scale * table[ids[t]] (a product in fp32, rounded to dt), zeros where ids[t] is ignore_index, NaN where it is any other number outside
+ * 0 .. V - 1.  table [V][D] and out [T][D] of type dt, dense; T, V and D below 2^31.
+ */
+int division_embedding(const int64_t *ids, int64_t T, const void *table, int64_t V, int64_t D, division_dtype dt, float scale, int64_t ignore_index, void *out, void *hip_stream);
+
+/*
+ * The table's gradient: grad_table[v] = scale * sum of grad[t] over the tokens with ids[t] = v, in fp32 and in the order of the tokens, rounded to table_dt; tokens of
+ * ignore_index or outside the table have none.
+ *   grad        T rows of D elements of type dt, grad_stride elements apart
+ *   grad_table  [V][D] of type table_dt, written in full; with add = 1 the sums are added to what it holds, and rows without a token are left as they are
+ *   workspace   division_embedding_backward_workspace(T, V, D) bytes on 16
+ */
+typedef struct division_embedding_back {
+    const void *grad;
+    const int64_t *ids;
+    int64_t grad_stride, T, V, D, ignore_index;
+    division_dtype dt, table_dt;
+    float scale;
+    int add;
+    void *grad_table;
+    void *workspace;
+    size_t workspace_bytes;
+} division_embedding_back;
+
+size_t division_embedding_backward_workspace(int64_t T, int64_t V, int64_t D);
+
+int division_embedding_backward(const division_embedding_back *back, void *hip_stream);
+
+/*
+ * Dropout whose mask is computed and not stored, with the addition to the residual stream: y = residual + V (.) x / (1 - p) (residual may be null), in fp32, rounded to dt.  V is
+ * that of division_dropout_forward with the same n, p and seed; the backward pass is the same call on the gradient without a residual.  Where V = 0 it is residual (or +0) whatever x.
+ * device_seed: null, or where on the device the seed is read from when the kernel runs (`seed` is not looked at then): a captured graph can be replayed with others.
+ * p from 0 to 1; y may be x or residual itself; n up to 2^35 (DIVISION_ERANGE).
+ */
+int division_dropout_add(const void *x, const void *residual, int64_t n, division_dtype dt, double p, uint64_t seed, const uint64_t *device_seed, void *y, void *hip_stream);
+
 /* Version of this ABI (host-only): DIVISION_ABI_VERSION of the header that the library was built with. */
 #define DIVISION_ABI_VERSION 1
 int division_abi_version(void);

@@ -2,7 +2,7 @@
 
 compress / decompress of cached activation maps as in "DIVISION: Memory
 Efficient Training via Dual Activation Precision" (Sec. 4.1 and Sec. 4.2), and the
-operators of a token model's training step beside its products.
+operators of a token model's training step beside its products, attention among them.
 """
 from .binding import (DIVISION_BF16, DIVISION_F32, DivisionError, division_compress,  # noqa: F401
                       division_compress_batch, division_decompress, division_decompress_batch, division_kernel_name, division_packed_bytes, division_packed_layout, lib)
@@ -17,4 +17,7 @@ from .binding import division_relu_compress, division_relu_compress_fused  # noq
 from .operators import Normed, division_read_codes, division_rms_norm, division_rms_norm_backward  # noqa: F401,E402
 from .operators import LogProbs, division_log_probs, division_log_probs_backward  # noqa: F401,E402
 from .operators import division_clip_grads, division_grad_norm  # noqa: F401,E402
+from .layer_operators import Attended, division_attention, division_attention_backward  # noqa: F401,E402
+from .layer_operators import Rotated, division_head_norm_rotate, division_head_norm_rotate_backward  # noqa: F401,E402
+from .layer_operators import division_dropout_add, division_embedding, division_embedding_backward  # noqa: F401,E402
 from .token_modules import DivisionNormLinear, DivisionRMSNorm, division_token_log_probs  # noqa: F401,E402

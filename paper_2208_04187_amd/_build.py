@@ -2,7 +2,7 @@
 
 division.hip (with the kernel families and the host side in the .h fragments it includes) instantiates
 its kernels once per element / cache type; it is compiled as three translation units (-DDIVISION_PART=0, 1, 2: float, bfloat16, bfloat16-cached float) beside masks.hip and the operators
-of a token model's step (norm.hip, logprobs.hip, gradnorm.hip), all in parallel, and the objects are linked into the one library.
+of a token model's step (norm.hip, logprobs.hip, gradnorm.hip) and of its layers (attention.hip, attention_back.hip, rotate.hip, embedding.hip, dropout_add.hip), all in parallel, and the objects are linked into the one library.
 """
 from __future__ import annotations
 
@@ -19,7 +19,12 @@ MASKS = PKG / "csrc" / "masks.hip"
 NORM = PKG / "csrc" / "norm.hip"
 LOGPROBS = PKG / "csrc" / "logprobs.hip"
 GRADNORM = PKG / "csrc" / "gradnorm.hip"
-SRCS = [DIVISION, MASKS, NORM, LOGPROBS, GRADNORM]
+ATTENTION = PKG / "csrc" / "attention.hip"
+ATTENTION_BACK = PKG / "csrc" / "attention_back.hip"
+ROTATE = PKG / "csrc" / "rotate.hip"
+EMBEDDING = PKG / "csrc" / "embedding.hip"
+DROPOUT_ADD = PKG / "csrc" / "dropout_add.hip"
+SRCS = [DIVISION, MASKS, NORM, LOGPROBS, GRADNORM, ATTENTION, ATTENTION_BACK, ROTATE, EMBEDDING, DROPOUT_ADD]
 LIB = PKG / "libdivision.so"
 CHECKS = PKG.parent / "tests" / "device_checks.hip"          # device helpers on their own, for the tests
 FASTCALL = PKG / "_fastcall.so"                              # imported by binding.py
@@ -37,6 +42,11 @@ UNITS = [
     ("norm.o", NORM, []),
     ("logprobs.o", LOGPROBS, []),
     ("gradnorm.o", GRADNORM, []),
+    ("attention.o", ATTENTION, []),
+    ("attention_back.o", ATTENTION_BACK, []),
+    ("rotate.o", ROTATE, []),
+    ("embedding.o", EMBEDDING, []),
+    ("dropout_add.o", DROPOUT_ADD, []),
 ]
 
 HIPCC_FLAGS = [

@@ -1,0 +1,349 @@
+// Attention of a token model for AMD MI355X (gfx950).
+//
+//   z = scale q k^T over the keys that a query sees;   out = softmax(z) v;   lse = ln(sum of exp(z))
+//
+// One pass over the keys with the running maximum and sum of each query's exponentials; scores and probabilities stay in registers.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <stddef.h>
+#include "../../include/division.h"
+
+namespace {
+#include "rows.h"
+#include "tiles.h"
+#include "attention_args.h"
+
+// What a wavefront holds of 32 columns: their running maximum (of the raw scores), sum and weighted values, [DP elements][columns] in blocks of 32 x 32
+template <typename T, int DP> struct Columns {
+    f32x16 o[DP / 32];
+    float most, total;                                      // both halves of a column have the maximum; each its own rows' part of the sum
+    Operand<T> q[DP / 16];
+
+    __device__ __forceinline__ void begin(const AttentionArgs& a, const char* q_head, uint32_t col, uint32_t cols, int half) {
+#pragma unroll
+        for (auto& b : o) b = (f32x16)(0.0f);
+        most = -INFINITY;
+        total = 0.0f;
+        const uint32_t i = col / (uint32_t)a.R, r = col % (uint32_t)a.R;
+        const char* row = q_head + row_offset(a.qs, i, (int)r);
+        const int row_bytes = a.D * (int)sizeof(T);
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+            const int at = (16 * s + 8 * half) * (int)sizeof(T);
+            q[s] = col < cols && at < row_bytes ? Operand<T>::at(row + at) : Operand<T>::zero();
+        }
+    }
+
+    // KT keys of the tiles, the first of them key `first`; from .. to - 1 are the keys that this lane's column sees, all of these where `whole`
+    template <int KT> __device__ __forceinline__ void add(const char* kt, const char* vt, int first, int from, int to, bool whole, float scale2, int lane) {
+        const int half = lane >> 5;
+        f32x16 z[KT / 32];
+#pragma unroll
+        for (int b = 0; b < KT / 32; ++b) {
+            z[b] = (f32x16)(0.0f);
+#pragma unroll
+            for (int s = 0; s < DP / 16; ++s) product(z[b], Tile<T, DP>::rows(kt, 32 * b, s, lane), q[s]);
+        }
+        if (!whole) {
+#pragma unroll
+            for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int j = first + 32 * b + block_row(i, half);
+                    z[b][i] = j >= from && j < to ? z[b][i] : -INFINITY;
+                }
+        }
+        float m = z[0][0];
+#pragma unroll
+        for (int b = 0; b < KT / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, z[b][i]);
+        m = halves_max(m);
+        // The maximum that exponents are taken against need not be the largest yet: sums and products stay exact to their last bits while they grow by at most 2^8, so that most tiles leave
+        // the weighted values alone
+        if (__any((m - most) * scale2 > 8.0f || most == -INFINITY)) {
+            m = fmaxf(m, most);
+            const float shrink = most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((most - m) * scale2);
+            total *= shrink;
+#pragma unroll
+            for (auto& b : o)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) b[i] *= shrink;
+            most = m;
+        }
+        const float by = most == -INFINITY ? 0.0f : most * scale2;
+#pragma unroll
+        for (int b = 0; b < KT / 32; ++b) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][i], scale2, -by));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) total += z[b][i];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = z[b][8 * c + j];
+                const Operand<T> p = Operand<T>::of(w);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) product(o[d], Tile<T, DP>::columns(vt, 32 * b + 16 * c, 32 * d, lane), p);
+            }
+        }
+    }
+};
+
+// A workgroup's tasks: which columns of which key head, which part of the keys
+struct Task { int group, block, split; };
+
+template <typename T> __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
+    else *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pack2(a, b), bf16_pack2(c, d)};
+}
+
+constexpr int kThreads = 256;
+
+// Four wavefronts of 32 columns each share the tiles of the keys.
+template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attend(AttentionArgs a) {
+    constexpr int kTile = KT * Tile<T, DP>::kRowBytes;
+    __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile];
+    const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
+    const int group = rest % a.groups, block = a.blocks - 1 - rest / a.groups;
+    const int b = group / a.G, g = group % a.G;
+    const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * 128u;
+    const uint32_t wave_col = first_col + 32 * wave, col = wave_col + (lane & 31);
+    const Seen seen = seen_of(a, b);
+    // the keys of the workgroup, of the wavefront and of the lane
+    const uint32_t last_col = min(first_col + 127u, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
+    int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
+    lo = max(lo, split * a.tiles);
+    hi = min(hi, (split + 1) * a.tiles);
+    const bool works = wave_col < cols;
+    const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
+    const int wave_from = seen.from(qa), whole_from = seen.from(qb), whole_to = seen.to(qa), wave_to = works ? seen.to(qb) : 0;
+    const int i = (int)(min(col, cols - 1) / (uint32_t)a.R);
+    const int from = seen.from(i), to = col < cols ? seen.to(i) : 0;
+    const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
+    const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
+    const int row_bytes = a.D * (int)sizeof(T);
+    const auto fetch = [&](int t) {
+        const int left = seen.keys - t * KT;
+        Tile<T, DP>::template fill<KT, kThreads>(tiles[t & 1][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
+        Tile<T, DP>::template fill<KT, kThreads>(tiles[t & 1][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
+    };
+    if (lo < hi) fetch(lo);
+    Columns<T, DP> c;
+    c.begin(a, a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head, col, cols, half);
+    const float scale2 = a.scale * kLog2e;
+    loads_done();
+    __syncthreads();
+    for (int t = lo; t < hi; ++t) {
+        if (t + 1 < hi) fetch(t + 1);
+        const int j = t * KT;
+        if (j < wave_to && j + KT > wave_from)
+            c.template add<KT>(tiles[t & 1][0], tiles[t & 1][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
+        loads_done();
+        __syncthreads();
+    }
+    if (col >= cols) return;
+    const float total = halves_sum(c.total);
+    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+    const float lse = total == 0.0f ? -INFINITY : __builtin_fmaf(c.most, a.scale, logf(total));
+    const int r = (int)(col % (uint32_t)a.R);
+    if (a.parts) {
+        // [split][group][column]: lse, and the values
+        const int64_t at = ((int64_t)split * a.groups + group) * cols + col;
+        if (half == 0) a.parts[at] = lse;
+        float* row = a.parts + (int64_t)a.splits * a.groups * cols + at * a.D;
+#pragma unroll
+        for (int d = 0; d < DP; d += 8) {
+            if (d >= a.D) continue;
+            const f32x16& o = c.o[d / 32];
+            const int n = d % 32 / 2;
+            *reinterpret_cast<f32x4*>(row + d + 4 * half) = f32x4{o[n] * inverse, o[n + 1] * inverse, o[n + 2] * inverse, o[n + 3] * inverse};
+        }
+        return;
+    }
+    if (half == 0) a.lse[((int64_t)b * a.H + g * a.R + r) * a.Sq + i] = lse;
+    T* row = reinterpret_cast<T*>(a.out) + (((int64_t)b * a.Sq + i) * a.H + g * a.R + r) * a.D;
+#pragma unroll
+    for (int d = 0; d < DP; d += 8) {
+        if (d >= a.D) continue;
+        const f32x16& o = c.o[d / 32];
+        const int n = d % 32 / 2;
+        put4(row + d + 4 * half, o[n] * inverse, o[n + 1] * inverse, o[n + 2] * inverse, o[n + 3] * inverse);
+    }
+}
+
+// Few columns: WK wavefronts have the same 32 columns and every WK-th tile of the keys each, in tiles of their own, and are joined at the end.
+template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * WK) void attend_few(AttentionArgs a) {
+    constexpr int kTile = KT * Tile<T, DP>::kRowBytes, kLoads = 2 * kTile / 1024, kRow = DP + 4;
+    static_assert(32 * kRow * 4 <= 4 * kTile, "a wavefront's values in place of its tiles");
+    __shared__ __attribute__((aligned(16))) char tiles[WK][2][2][kTile];
+    __shared__ float most[WK][32], totals[WK][32];
+    const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
+    const int group = rest % a.groups, block = a.blocks - 1 - rest / a.groups;
+    const int b = group / a.G, g = group % a.G;
+    const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * 32u, col = first_col + (lane & 31);
+    const Seen seen = seen_of(a, b);
+    const int qa = (int)(first_col / (uint32_t)a.R), qb = (int)(min(first_col + 31u, cols - 1) / (uint32_t)a.R);
+    const int whole_from = seen.from(qb), whole_to = seen.to(qa);
+    const int lo = max(seen.from(qa) / KT, split * a.tiles), hi = min((seen.to(qb) + KT - 1) / KT, (split + 1) * a.tiles);
+    const int i = (int)(min(col, cols - 1) / (uint32_t)a.R);
+    const int from = seen.from(i), to = col < cols ? seen.to(i) : 0;
+    const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
+    const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
+    const int row_bytes = a.D * (int)sizeof(T);
+    const auto fetch = [&](int t, int at) {
+        const int left = seen.keys - t * KT;
+        Tile<T, DP>::template fill<KT, 64>(tiles[wave][at][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
+        Tile<T, DP>::template fill<KT, 64>(tiles[wave][at][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
+    };
+    Columns<T, DP> c;
+    c.begin(a, a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head, col, cols, half);
+    const float scale2 = a.scale * kLog2e;
+    if (lo + wave < hi) fetch(lo + wave, 0);
+    for (int t = lo + wave, at = 0; t < hi; t += WK, at ^= 1) {
+        if (t + WK < hi) {
+            fetch(t + WK, at ^ 1);
+            loads_done<kLoads>();
+        } else {
+            loads_done();
+        }
+        const int j = t * KT;
+        c.template add<KT>(tiles[wave][at][0], tiles[wave][at][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
+    }
+    const float total = halves_sum(c.total);
+    if (half == 0) { most[wave][lane] = c.most; totals[wave][lane] = total; }
+    float* mine = reinterpret_cast<float*>(tiles[wave]) + (lane & 31) * kRow;
+#pragma unroll
+    for (int d = 0; d < DP; d += 8) {
+        const f32x16& o = c.o[d / 32];
+        const int n = d % 32 / 2;
+        *reinterpret_cast<f32x4*>(mine + d + 4 * half) = f32x4{o[n], o[n + 1], o[n + 2], o[n + 3]};
+    }
+    __syncthreads();
+    for (int e = thread; e < 32 * (DP / 4); e += 64 * WK) {
+        const int c1 = e / (DP / 4), d = e % (DP / 4) * 4;
+        const uint32_t at_col = first_col + c1;
+        if (at_col >= cols || d >= a.D) continue;
+        float m = most[0][c1], sum = 0.0f;
+#pragma unroll
+        for (int w = 1; w < WK; ++w) m = fmaxf(m, most[w][c1]);
+        f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < WK; ++w) {
+            const float by = most[w][c1] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((most[w][c1] - m) * scale2);
+            sum += by * totals[w][c1];
+            o += by * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(tiles[w]) + c1 * kRow + d);
+        }
+        o *= sum == 0.0f ? 0.0f : 1.0f / sum;
+        const float lse = sum == 0.0f ? -INFINITY : __builtin_fmaf(m, a.scale, logf(sum));
+        if (a.parts) {
+            const int64_t at = ((int64_t)split * a.groups + group) * cols + at_col;
+            if (d == 0) a.parts[at] = lse;
+            *reinterpret_cast<f32x4*>(a.parts + (int64_t)a.splits * a.groups * cols + at * a.D + d) = o;
+        } else {
+            const int i1 = (int)(at_col / (uint32_t)a.R), h = g * a.R + (int)(at_col % (uint32_t)a.R);
+            if (d == 0) a.lse[((int64_t)b * a.H + h) * a.Sq + i1] = lse;
+            put4(reinterpret_cast<T*>(a.out) + (((int64_t)b * a.Sq + i1) * a.H + h) * a.D + d, o[0], o[1], o[2], o[3]);
+        }
+    }
+}
+
+// The parts of the keys of each column: out = sum of exp(lse_part - lse) out_part.  32 lanes a column, four elements each.
+template <typename T> __global__ __launch_bounds__(kThreads) void join_parts(AttentionArgs a) {
+    const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R;
+    const int64_t n = (int64_t)a.groups * cols, at = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+    const int d = (threadIdx.x & 31) * 4;
+    if (at >= n) return;
+    float most = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) most = fmaxf(most, a.parts[s * n + at]);
+    const float* values = a.parts + a.splits * n;
+    f32x4 o = {0, 0, 0, 0};
+    float sum = 0.0f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float lse = a.parts[s * n + at];
+        if (lse == -INFINITY) continue;
+        const float by = __builtin_amdgcn_exp2f((lse - most) * kLog2e);
+        sum += by;
+        if (d < a.D) o += by * *reinterpret_cast<const f32x4*>(values + (s * n + at) * a.D + d);
+    }
+    o *= sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int group = (int)(at / cols), b = group / a.G;
+    const uint32_t col = (uint32_t)(at - (int64_t)group * cols);
+    const int i = (int)(col / (uint32_t)a.R), h = group % a.G * a.R + (int)(col % (uint32_t)a.R);
+    if (d == 0) a.lse[((int64_t)b * a.H + h) * a.Sq + i] = sum == 0.0f ? -INFINITY : most + logf(sum);
+    if (d < a.D) put4(reinterpret_cast<T*>(a.out) + (((int64_t)b * a.Sq + i) * a.H + h) * a.D + d, o[0], o[1], o[2], o[3]);
+}
+
+// ------------------------------------------------------------------ host side
+
+// How the work is cut: columns into blocks of 128 (of 32 where there are no more), and the keys into parts where that leaves less than two workgroups a CU.
+struct Cut { bool few; int64_t blocks; int splits, tiles, key_tile; };
+Cut cut_of(const division_attention& a) {
+    Cut c;
+    const int64_t R = a.H / a.G, cols = a.Sq * R;
+    c.few = cols <= 32;
+    c.blocks = (cols + (c.few ? 31 : 127)) / (c.few ? 32 : 128);
+    c.key_tile = c.few ? (a.dt == DIVISION_BF16 ? 32 : 32) : 64;
+    const int64_t tiles = (a.Sk + c.key_tile - 1) / c.key_tile, tasks = c.blocks * a.B * a.G;
+    // a part has at least two tiles for each wavefront that shares them
+    const int64_t least = c.few ? 8 : 8, room = tiles / least;
+    int64_t splits = tasks >= 256 ? 1 : (512 + tasks - 1) / tasks;
+    if (splits > room) splits = room;
+    if (splits > 64) splits = 64;
+    if (splits < 1) splits = 1;
+    c.tiles = (int)((tiles + splits - 1) / splits);
+    if (c.tiles < 1) c.tiles = 1;
+    c.splits = tiles ? (int)((tiles + c.tiles - 1) / c.tiles) : 1;
+    return c;
+}
+size_t parts_bytes(const division_attention& a, const Cut& c) { return c.splits > 1 ? (size_t)c.splits * a.B * a.Sq * a.H * (a.D + 1) * 4 : 0; }
+
+template <typename T, int DP> int run(const AttentionArgs& args, const Cut& c, int64_t grid, hipStream_t st) {
+    if (c.few) hipLaunchKernelGGL((attend_few<T, DP, 32, sizeof(T) == 2 ? 4 : 2>), dim3((uint32_t)grid), dim3(sizeof(T) == 2 ? 256 : 128), 0, st, args);
+    else hipLaunchKernelGGL((attend<T, DP, 64>), dim3((uint32_t)grid), dim3(kThreads), 0, st, args);
+    CHECKED(launched());
+    if (c.splits == 1) return DIVISION_OK;
+    const int64_t rows = (int64_t)args.groups * args.Sq * args.R;
+    hipLaunchKernelGGL(join_parts<T>, dim3((uint32_t)((rows + kThreads / 32 - 1) / (kThreads / 32))), dim3(kThreads), 0, st, args);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t division_attention_workspace(const division_attention* attention) {
+    if (!attention || check_attention(*attention) != DIVISION_OK || attention->B == 0 || attention->Sq == 0) return 0;
+    return parts_bytes(*attention, cut_of(*attention));
+}
+
+int division_attend(const division_attention* attention, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!attention) return DIVISION_EINVAL;
+    const division_attention& a = *attention;
+    CHECKED(check_attention(a));
+    if (a.B == 0 || a.Sq == 0) return DIVISION_OK;
+    if (!a.q || (a.Sk > 0 && (!a.k || !a.v)) || !out || !lse) return DIVISION_EINVAL;
+    if (!aligned(out, 16) || !aligned(lse, 4)) return DIVISION_EALIGN;
+    const Cut c = cut_of(a);
+    const size_t need = parts_bytes(a, c);
+    if (need && !workspace) return DIVISION_EINVAL;
+    if (need && !aligned(workspace, 16)) return DIVISION_EALIGN;
+    if (workspace_bytes < need) return DIVISION_ESIZE;
+    AttentionArgs args = args_of(a);
+    args.out = static_cast<char*>(out);
+    args.lse = lse;
+    args.parts = need ? static_cast<float*>(workspace) : nullptr;
+    args.blocks = (int)c.blocks;
+    args.splits = c.splits;
+    args.tiles = c.tiles;
+    const int64_t grid = c.blocks * args.groups * c.splits;
+    if (grid >= (int64_t(1) << 24)) return DIVISION_ERANGE;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, c, grid, st) : run<uint16_t, 128>(args, c, grid, st);
+    return a.D <= 64 ? run<float, 64>(args, c, grid, st) : run<float, 128>(args, c, grid, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,71 @@
+// Included inside the unnamed namespaces of attention.hip and attention_back.hip: their arguments, and what the host checks of both.
+
+// Strides are in bytes.  R query heads share a key head; the queries of one key head's are numbered i * R + r, head r of them of query i, and called columns.
+struct Heads { int64_t batch; int token, head; };
+struct AttentionArgs {
+    const char *q, *k, *v;
+    Heads qs, ks, vs;
+    const int *lengths, *starts;
+    char* out;
+    float *lse, *parts;
+    int64_t window;
+    int Sq, Sk, H, G, R, D, causal, groups;             // groups: B * G
+    int blocks, splits, tiles;                          // of columns; of keys, and how many tiles each has
+    float scale;
+};
+__device__ __forceinline__ int64_t row_offset(const Heads& s, int64_t token, int head) { return token * s.token + (int64_t)head * s.head; }
+template <typename A> __device__ __forceinline__ Seen seen_of(const A& a, int b) {
+    Seen s;
+    int n = a.Sk;
+    if (a.lengths) { n = a.lengths[b]; n = n < 0 ? 0 : n > a.Sk ? a.Sk : n; }
+    s.keys = n;
+    s.start = a.starts ? a.starts[b] : (int64_t)a.Sk - a.Sq;
+    s.window = a.window;
+    s.causal = a.causal;
+    s.Sq = a.Sq;
+    return s;
+}
+
+// ------------------------------------------------------------------ host side
+
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP; }
+#define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
+
+// a tensor of rows: not behind what an offset within a tile can say (kMostStride bytes a token, kMostStride for all heads), every row on 16 bytes
+constexpr int64_t kMostStride = 1 << 23, kMostTokens = 1 << 29;
+int check_heads(const void* p, const int64_t* strides, int64_t B, int64_t heads, int64_t es) {
+    const int64_t per = 16 / es;
+    if (strides[0] < 0 || strides[1] < 0 || strides[2] < 0) return DIVISION_EINVAL;
+    if (!aligned(p, 16) || strides[0] % per || strides[1] % per || strides[2] % per) return DIVISION_EALIGN;
+    if (strides[1] * es > kMostStride || strides[2] > (kMostStride * 8) / es / heads || strides[0] > (int64_t(1) << 40) / B) return DIVISION_ERANGE;
+    return DIVISION_OK;
+}
+int check_attention(const division_attention& a) {
+    if (a.dt != DIVISION_F32 && a.dt != DIVISION_BF16) return DIVISION_EINVAL;
+    if (a.B < 0 || a.Sq < 0 || a.Sk < 0 || a.H < 1 || a.G < 1 || a.H % a.G || a.D < 8 || a.D > 128 || a.D % 8 || a.window < 0 || (a.causal != 0 && a.causal != 1)) return DIVISION_EINVAL;
+    if (!(a.scale > 0.0f && a.scale <= 3.4e38f)) return DIVISION_EINVAL;
+    if (!aligned(a.lengths, 4) || !aligned(a.starts, 4)) return DIVISION_EALIGN;
+    if (a.B == 0 || a.Sq == 0) return DIVISION_OK;
+    const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4, R = a.H / a.G;
+    if (a.B > (1 << 24) || a.H > 4096 || a.Sq > kMostTokens || a.Sk > kMostTokens || a.Sq * R > (int64_t(1) << 30)) return DIVISION_ERANGE;
+    CHECKED(check_heads(a.q, a.q_strides, a.B, a.H, es));
+    if (a.Sk > 0) {
+        CHECKED(check_heads(a.k, a.k_strides, a.B, a.G, es));
+        CHECKED(check_heads(a.v, a.v_strides, a.B, a.G, es));
+    }
+    return DIVISION_OK;
+}
+Heads heads_of(const int64_t* strides, int64_t es) { return {strides[0] * es, (int)(strides[1] * es), (int)(strides[2] * es)}; }
+AttentionArgs args_of(const division_attention& a) {
+    const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4;
+    AttentionArgs r{};
+    r.q = static_cast<const char*>(a.q); r.k = static_cast<const char*>(a.k); r.v = static_cast<const char*>(a.v);
+    r.qs = heads_of(a.q_strides, es); r.ks = heads_of(a.k_strides, es); r.vs = heads_of(a.v_strides, es);
+    r.lengths = a.lengths; r.starts = a.starts;
+    // beyond all positions a window of any size is the same
+    r.window = a.window > (int64_t(1) << 40) ? (int64_t(1) << 40) : a.window;
+    r.Sq = (int)a.Sq; r.Sk = (int)a.Sk; r.H = (int)a.H; r.G = (int)a.G; r.R = (int)(a.H / a.G); r.D = (int)a.D;
+    r.causal = a.causal; r.groups = (int)(a.B * a.G); r.scale = a.scale;
+    return r;
+}

@@ -1,0 +1,308 @@
+// The backward pass of attention for AMD MI355X (gfx950).
+//
+//   p = exp(scale q k^T - lse),   ds = p (grad v^T - rowsum(grad out)),   dq = scale ds k,   dk = scale ds^T q,   dv = p^T grad
+//
+// The probabilities are computed again from lse, twice: once by workgroups that own queries (dq), once by ones that own keys (dk and dv, over all query heads that share them).  Seven
+// products instead of five, but every sum is in a workgroup's registers, in an order that sizes alone decide.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <stddef.h>
+#include "../../include/division.h"
+
+namespace {
+#include "rows.h"
+#include "fastdiv.h"
+#include "tiles.h"
+#include "attention_args.h"
+
+struct BackArgs : AttentionArgs {
+    const char *grad, *o;
+    Heads gs;
+    char *dq, *dk, *dv;
+    float *exponents, *deltas;                          // [group][column]: lse in powers of two (infinity where nothing is seen), rowsum(grad out)
+    FastDiv by_R;
+};
+
+template <typename T> __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
+    else *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pack2(a, b), bf16_pack2(c, d)};
+}
+// a lane's column of blocks [DP][32], times `by`, to a row
+template <typename T, int DP> __device__ __forceinline__ void put_column(T* row, const f32x16* o, float by, int D, int half) {
+#pragma unroll
+    for (int d = 0; d < DP; d += 8) {
+        if (d >= D) continue;
+        const f32x16& b = o[d / 32];
+        const int n = d % 32 / 2;
+        put4(row + d + 4 * half, b[n] * by, b[n + 1] * by, b[n + 2] * by, b[n + 3] * by);
+    }
+}
+// a lane's part of a row as the operands of its column; zeros where it is not `there`
+template <typename T, int DP> __device__ __forceinline__ void get_column(Operand<T>* v, const char* row, bool there, int row_bytes, int half) {
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+        const int at = (16 * s + 8 * half) * (int)sizeof(T);
+        v[s] = there && at < row_bytes ? Operand<T>::at(row + at) : Operand<T>::zero();
+    }
+}
+
+constexpr int kThreads = 256;
+
+// Four wavefronts of 32 columns (queries) each share the tiles of the keys and values.
+template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void back_queries(BackArgs a) {
+    constexpr int kTile = KT * Tile<T, DP>::kRowBytes;
+    __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile];
+    const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    const int group = blockIdx.x % a.groups, block = a.blocks - 1 - blockIdx.x / a.groups;
+    const int b = group / a.G, g = group % a.G;
+    const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * 128u;
+    const uint32_t wave_col = first_col + 32 * wave, col = wave_col + (lane & 31);
+    const Seen seen = seen_of(a, b);
+    const uint32_t last_col = min(first_col + 127u, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
+    const int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
+    const bool works = wave_col < cols, there = col < cols;
+    const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
+    const int wave_from = seen.from(qa), whole_from = seen.from(qb), whole_to = seen.to(qa), wave_to = works ? seen.to(qb) : 0;
+    const int i = (int)(min(col, cols - 1) / (uint32_t)a.R), r = (int)(min(col, cols - 1) % (uint32_t)a.R);
+    const int from = seen.from(i), to = there ? seen.to(i) : 0;
+    const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
+    const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
+    const int row_bytes = a.D * (int)sizeof(T);
+    const auto fetch = [&](int t) {
+        const int left = seen.keys - t * KT;
+        Tile<T, DP>::template fill<KT, kThreads>(tiles[t & 1][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
+        Tile<T, DP>::template fill<KT, kThreads>(tiles[t & 1][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
+    };
+    if (lo < hi) fetch(lo);
+    Operand<T> q[DP / 16], grad[DP / 16];
+    get_column<T, DP>(q, a.q + b * a.qs.batch + row_offset(a.qs, i, g * a.R + r), there, row_bytes, half);
+    get_column<T, DP>(grad, a.grad + b * a.gs.batch + row_offset(a.gs, i, g * a.R + r), there, row_bytes, half);
+    const int64_t row = ((int64_t)b * a.Sq + i) * a.H + g * a.R + r;
+    float delta = 0.0f;
+    {
+        Operand<T> o[DP / 16];
+        get_column<T, DP>(o, a.o + row * row_bytes, there, row_bytes, half);
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) delta = __builtin_fmaf(o[s][j], grad[s][j], delta);
+        delta = halves_sum(delta);
+    }
+    float exponent = there ? a.lse[((int64_t)b * a.H + g * a.R + r) * a.Sq + i] * kLog2e : INFINITY;
+    if (exponent == -INFINITY) exponent = INFINITY;
+    if (there && half == 0) {
+        a.exponents[(int64_t)group * cols + col] = exponent;
+        a.deltas[(int64_t)group * cols + col] = delta;
+    }
+    const float scale2 = a.scale * kLog2e;
+    f32x16 dq[DP / 32];
+#pragma unroll
+    for (auto& x : dq) x = (f32x16)(0.0f);
+    loads_done();
+    __syncthreads();
+    for (int t = lo; t < hi; ++t) {
+        if (t + 1 < hi) fetch(t + 1);
+        const int j0 = t * KT;
+        const char *kt = tiles[t & 1][0], *vt = tiles[t & 1][1];
+        if (j0 < wave_to && j0 + KT > wave_from) {
+            const bool whole = j0 >= whole_from && j0 + KT <= whole_to;
+#pragma unroll
+            for (int n = 0; n < KT / 32; ++n) {
+                f32x16 z = (f32x16)(0.0f), dp = (f32x16)(0.0f);
+#pragma unroll
+                for (int s = 0; s < DP / 16; ++s) product(z, Tile<T, DP>::rows(kt, 32 * n, s, lane), q[s]);
+#pragma unroll
+                for (int s = 0; s < DP / 16; ++s) product(dp, Tile<T, DP>::rows(vt, 32 * n, s, lane), grad[s]);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], scale2, -exponent));
+                    z[e] = p * (dp[e] - delta);
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int j = j0 + 32 * n + block_row(e, half);
+                        z[e] = j >= from && j < to ? z[e] : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = z[8 * c + j];
+                    const Operand<T> ds = Operand<T>::of(w);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) product(dq[d], Tile<T, DP>::columns(kt, 32 * n + 16 * c, 32 * d, lane), ds);
+                }
+            }
+        }
+        loads_done();
+        __syncthreads();
+    }
+    if (there) put_column<T, DP>(reinterpret_cast<T*>(a.dq) + row * a.D, dq, a.scale, a.D, half);
+}
+
+// Four wavefronts of 32 keys each share the tiles of the columns (queries of all heads that share the keys) and their gradients.
+template <typename T, int DP, int CT> __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void back_keys(BackArgs a) {
+    constexpr int kTile = CT * Tile<T, DP>::kRowBytes;
+    __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile];
+    __shared__ __attribute__((aligned(16))) float stats[2][2][CT];
+    const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    const int group = blockIdx.x % a.groups, block = blockIdx.x / a.groups;
+    const int b = group / a.G, g = group % a.G;
+    const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R;
+    const Seen seen = seen_of(a, b);
+    const int first = block * 128, wave_key = first + 32 * wave, key = wave_key + (lane & 31);
+    const int last = min(first + 127, seen.keys - 1), wave_last = min(wave_key + 31, seen.keys - 1);
+    // the columns of the workgroup, of the wavefront and of the lane: those of whole queries
+    const bool any = first < seen.keys, works = wave_key < seen.keys, there = key < seen.keys;
+    const int lo = any ? seen.query_from(first) * a.R / CT : 0, hi = any ? (seen.query_to(last) * a.R + CT - 1) / CT : 0;
+    const int wave_from = seen.query_from(min(wave_key, a.Sk - 1)) * a.R, wave_to = works ? seen.query_to(wave_last) * a.R : 0;
+    const int whole_from = seen.query_from(min(wave_key + 31, a.Sk - 1)) * a.R, whole_to = works && wave_key + 31 < seen.keys ? seen.query_to(wave_key) * a.R : 0;
+    const int from = there ? seen.query_from(key) * a.R : 0, to = there ? seen.query_to(key) * a.R : 0;
+    const char* q = a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head;
+    const char* gr = a.grad + b * a.gs.batch + (int64_t)g * a.R * a.gs.head;
+    const int row_bytes = a.D * (int)sizeof(T);
+    const auto fetch = [&](int t) {
+        const uint32_t c0 = (uint32_t)t * CT, i0 = c0 / (uint32_t)a.R, r0 = c0 - i0 * (uint32_t)a.R;
+        const int left = (int)(cols - c0);
+        const auto at = [&](const Heads& s) {
+            return [&, s](int row) { const uint32_t n = r0 + row, i = fdiv(n, a.by_R); return (int)i * s.token + (int)(n - i * (uint32_t)a.R) * s.head; };
+        };
+        Tile<T, DP>::template fill<CT, kThreads>(tiles[t & 1][0], q + (int64_t)i0 * a.qs.token, left, row_bytes, thread, at(a.qs));
+        Tile<T, DP>::template fill<CT, kThreads>(tiles[t & 1][1], gr + (int64_t)i0 * a.gs.token, left, row_bytes, thread, at(a.gs));
+    };
+    // a tile's numbers of its columns: two for each, on their way in a register
+    const auto stat = [&](int t) {
+        const uint32_t c = (uint32_t)t * CT + thread % CT;
+        if (thread >= 2 * CT) return 0.0f;
+        if (c >= cols) return thread < CT ? INFINITY : 0.0f;
+        return (thread < CT ? a.exponents : a.deltas)[(int64_t)group * cols + c];
+    };
+    float next = 0.0f;
+    if (lo < hi) { fetch(lo); next = stat(lo); }
+    Operand<T> k[DP / 16], v[DP / 16];
+    get_column<T, DP>(k, a.k + b * a.ks.batch + row_offset(a.ks, key, g), there, row_bytes, half);
+    get_column<T, DP>(v, a.v + b * a.vs.batch + row_offset(a.vs, key, g), there, row_bytes, half);
+    const float scale2 = a.scale * kLog2e;
+    f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (auto& x : dk) x = (f32x16)(0.0f);
+#pragma unroll
+    for (auto& x : dv) x = (f32x16)(0.0f);
+    if (lo < hi && thread < 2 * CT) stats[lo & 1][thread / CT][thread % CT] = next;
+    loads_done();
+    __syncthreads();
+    for (int t = lo; t < hi; ++t) {
+        if (t + 1 < hi) { fetch(t + 1); next = stat(t + 1); }
+        const int c0 = t * CT;
+        const char *qt = tiles[t & 1][0], *gt = tiles[t & 1][1];
+        if (c0 < wave_to && c0 + CT > wave_from) {
+            const bool whole = c0 >= whole_from && c0 + CT <= whole_to;
+#pragma unroll 1
+            for (int n = 0; n < CT / 32; ++n) {
+                f32x16 z = (f32x16)(0.0f), dp = (f32x16)(0.0f);
+#pragma unroll
+                for (int s = 0; s < DP / 16; ++s) product(z, Tile<T, DP>::rows(qt, 32 * n, s, lane), k[s]);
+#pragma unroll
+                for (int s = 0; s < DP / 16; ++s) product(dp, Tile<T, DP>::rows(gt, 32 * n, s, lane), v[s]);
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4 ex = *reinterpret_cast<const f32x4*>(&stats[t & 1][0][32 * n + block_row(e, half)]);
+                    const f32x4 de = *reinterpret_cast<const f32x4*>(&stats[t & 1][1][32 * n + block_row(e, half)]);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        z[e + f] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e + f], scale2, -ex[f]));
+                        dp[e + f] = z[e + f] * (dp[e + f] - de[f]);
+                    }
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int c = c0 + 32 * n + block_row(e, half);
+                        const bool sees = c >= from && c < to;
+                        z[e] = sees ? z[e] : 0.0f;
+                        dp[e] = sees ? dp[e] : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float w[8], x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) { w[j] = z[8 * c + j]; x[j] = dp[8 * c + j]; }
+                    const Operand<T> p = Operand<T>::of(w), ds = Operand<T>::of(x);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) product(dv[d], Tile<T, DP>::columns(gt, 32 * n + 16 * c, 32 * d, lane), p);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) product(dk[d], Tile<T, DP>::columns(qt, 32 * n + 16 * c, 32 * d, lane), ds);
+                }
+            }
+        }
+        if (t + 1 < hi && thread < 2 * CT) stats[(t + 1) & 1][thread / CT][thread % CT] = next;
+        loads_done();
+        __syncthreads();
+    }
+    if (key >= a.Sk) return;
+    const int64_t row = (((int64_t)b * a.Sk + key) * a.G + g) * a.D;
+    put_column<T, DP>(reinterpret_cast<T*>(a.dk) + row, dk, a.scale, a.D, half);
+    put_column<T, DP>(reinterpret_cast<T*>(a.dv) + row, dv, 1.0f, a.D, half);
+}
+
+// ------------------------------------------------------------------ host side
+
+size_t stats_bytes(const division_attention& a) { return (size_t)(a.B * a.Sq * a.H) * 8; }
+
+template <typename T, int DP> int run(BackArgs& args, hipStream_t st) {
+    if (args.Sq > 0) {
+        const int64_t blocks = ((int64_t)args.Sq * args.R + 127) / 128;
+        if (blocks * args.groups >= (int64_t(1) << 24)) return DIVISION_ERANGE;
+        args.blocks = (int)blocks;
+        hipLaunchKernelGGL((back_queries<T, DP, 64>), dim3((uint32_t)(blocks * args.groups)), dim3(kThreads), 0, st, args);
+        CHECKED(launched());
+    }
+    if (args.Sk > 0) {
+        const int64_t blocks = ((int64_t)args.Sk + 127) / 128;
+        if (blocks * args.groups >= (int64_t(1) << 24)) return DIVISION_ERANGE;
+        args.blocks = (int)blocks;
+        hipLaunchKernelGGL((back_keys<T, DP, 64>), dim3((uint32_t)(blocks * args.groups)), dim3(kThreads), 0, st, args);
+        CHECKED(launched());
+    }
+    return DIVISION_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t division_attention_backward_workspace(const division_attention* attention) {
+    if (!attention || check_attention(*attention) != DIVISION_OK) return 0;
+    return stats_bytes(*attention);
+}
+
+int division_attention_backward(const division_attention* attention, const division_attention_back* back, void* hip_stream) {
+    if (!attention || !back) return DIVISION_EINVAL;
+    const division_attention& a = *attention;
+    const division_attention_back& w = *back;
+    CHECKED(check_attention(a));
+    if (a.B == 0 || (a.Sq == 0 && a.Sk == 0)) return DIVISION_OK;
+    const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4;
+    if ((a.Sq > 0 && (!a.q || !w.grad_out || !w.out || !w.lse || !w.grad_q || !w.workspace)) || (a.Sk > 0 && (!w.grad_k || !w.grad_v || !a.k || !a.v))) return DIVISION_EINVAL;
+    if (!aligned(w.out, 16) || !aligned(w.lse, 4) || !aligned(w.grad_q, 16) || !aligned(w.grad_k, 16) || !aligned(w.grad_v, 16) || !aligned(w.workspace, 16)) return DIVISION_EALIGN;
+    if (a.Sq > 0) CHECKED(check_heads(w.grad_out, w.grad_out_strides, a.B, a.H, es));
+    if (w.workspace_bytes < stats_bytes(a)) return DIVISION_ESIZE;
+    BackArgs args{};
+    static_cast<AttentionArgs&>(args) = args_of(a);
+    args.grad = static_cast<const char*>(w.grad_out);
+    args.gs = heads_of(w.grad_out_strides, es);
+    args.o = static_cast<const char*>(w.out);
+    args.lse = const_cast<float*>(w.lse);
+    args.dq = static_cast<char*>(w.grad_q); args.dk = static_cast<char*>(w.grad_k); args.dv = static_cast<char*>(w.grad_v);
+    args.exponents = static_cast<float*>(w.workspace);
+    args.deltas = args.exponents + a.B * a.Sq * a.H;
+    args.by_R = make_fastdiv((uint32_t)args.R);
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, st) : run<uint16_t, 128>(args, st);
+    return a.D <= 64 ? run<float, 64>(args, st) : run<float, 128>(args, st);
+}
+
+}  // extern "C"

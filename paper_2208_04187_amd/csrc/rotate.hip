@@ -1,0 +1,383 @@
+// The norms of queries and keys, head by head, and the rotation by their positions, for AMD MI355X (gfx950).
+//
+//   u = x / sqrt(mean of x^2 over the head + eps) * weight;   pairs (a, b) of u -> (a cos - b sin, a sin + b cos), angle = position * frequency
+//
+// The angles are counted in turns in binary64 and taken to the nearest whole turn before a sine of 32 bits sees them: far positions turn as exactly as near ones.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <stddef.h>
+#include "../../include/division.h"
+
+namespace {
+#include "rows.h"
+
+constexpr int kThreads = 256;
+
+// Both tensors' heads are numbered through: those of the first, then those of the second.  Strides in elements.
+struct Side { const void *x, *weight, *grad; int64_t token, head, grad_token, grad_head; void* y; float* rstd; const float* rstd_in; int weight_bf16; };
+struct RotateArgs {
+    Side side[2];
+    const double* frequencies;
+    const int64_t* positions;
+    float* parts;
+    int64_t T;
+    int heads[2], D, pairs, rotated, block;             // pairs: D / 2, the first `rotated` of them turn; block: tokens a workgroup takes at a time
+    float eps;
+};
+
+// V pairs of a row from pair p on: v[0 .. V - 1] their first elements, v[V ..] the second ones.  NEXT: partners are neighbours, else half the rotated (or of the other) elements apart.
+template <typename T, int V, bool NEXT> struct Pairs {
+    static __device__ __forceinline__ int second(const RotateArgs& a, int p) { return p < a.rotated ? a.rotated : a.pairs - a.rotated; }
+    static __device__ __forceinline__ int first(const RotateArgs& a, int p) { return p < a.rotated ? p : a.rotated + p; }
+    static __device__ __forceinline__ void load(const T* row, const RotateArgs& a, int p, float* v) {
+        if constexpr (NEXT) {
+            if constexpr (V == 1) {
+                v[0] = Some1(row + 2 * p); v[1] = Some1(row + 2 * p + 1);
+            } else {
+                Some<T, V> q[2];
+                q[0].load(row + 2 * p); q[1].load(row + 2 * p + V);
+#pragma unroll
+                for (int i = 0; i < V; ++i) { v[i] = q[2 * i / V][2 * i % V]; v[V + i] = q[(2 * i + 1) / V][(2 * i + 1) % V]; }
+            }
+        } else {
+            const T* at = row + first(a, p);
+            if constexpr (V == 1) {
+                v[0] = Some1(at); v[1] = Some1(at + second(a, p));
+            } else {
+                Some<T, V> q[2];
+                q[0].load(at); q[1].load(at + second(a, p));
+#pragma unroll
+                for (int i = 0; i < V; ++i) { v[i] = q[0][i]; v[V + i] = q[1][i]; }
+            }
+        }
+    }
+    static __device__ __forceinline__ void store(T* row, const RotateArgs& a, int p, const float* v) {
+        if constexpr (V == 1) {
+            T* at = NEXT ? row + 2 * p : row + first(a, p);
+            put1(at, v[0]); put1(at + (NEXT ? 1 : second(a, p)), v[1]);
+        } else if constexpr (NEXT) {
+            float w[2 * V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) { w[2 * i] = v[i]; w[2 * i + 1] = v[V + i]; }
+            Some<T, V>::store(row + 2 * p, w); Some<T, V>::store(row + 2 * p + V, w + V);
+        } else {
+            T* at = row + first(a, p);
+            Some<T, V>::store(at, v); Some<T, V>::store(at + second(a, p), v + V);
+        }
+    }
+    static __device__ __forceinline__ float Some1(const T* p) {
+        if constexpr (sizeof(T) == 4) return *p;
+        else return bf16_value(*p);
+    }
+    static __device__ __forceinline__ void put1(T* p, float v) {
+        if constexpr (sizeof(T) == 4) *p = v;
+        else *p = bf16_of(v);
+    }
+};
+
+template <int V, bool NEXT> __device__ __forceinline__ void load_weight(const Side& s, const RotateArgs& a, int p, float* w) {
+    if (s.weight_bf16) Pairs<uint16_t, V, NEXT>::load(static_cast<const uint16_t*>(s.weight), a, p, w);
+    else Pairs<float, V, NEXT>::load(static_cast<const float*>(s.weight), a, p, w);
+}
+
+// cosine and sine of the angles of tokens t0 .. t0 + n - 1, [token][pair]
+__device__ __forceinline__ void angles(const RotateArgs& a, int64_t t0, int n, float2* to) {
+    for (int e = threadIdx.x; e < n * a.rotated; e += kThreads) {
+        const int t = e / a.rotated, p = e - t * a.rotated;
+        double turns = (double)a.positions[t0 + t] * a.frequencies[p] * 0.15915494309189533577;
+        turns -= rint(turns);
+        float s, c;
+        sincospif(2.0f * (float)turns, &s, &c);
+        to[e] = make_float2(c, s);
+    }
+}
+
+// LANES lanes have a head, U times V pairs each; a workgroup takes `block` tokens at a time, all heads of all of them one behind the other.
+template <typename T, int V, int U, int LANES, bool NEXT, bool BACK> __global__ __launch_bounds__(kThreads) void rotate(RotateArgs a) {
+    typedef Pairs<T, V, NEXT> P;
+    extern __shared__ __attribute__((aligned(16))) float2 turned[];
+    const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES, heads = a.heads[0] + a.heads[1];
+    float w[2][U][2 * V], dw[2][U][2 * V];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int p = (u * LANES + lane) * V;
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) w[k][u][i] = dw[k][u][i] = 0.0f;
+            if (p < a.pairs && a.heads[k]) load_weight<V, NEXT>(a.side[k], a, p, w[k][u]);
+        }
+    for (int64_t t0 = (int64_t)blockIdx.x * a.block; t0 < a.T; t0 += (int64_t)gridDim.x * a.block) {
+        const int n = (int)(a.T - t0 < a.block ? a.T - t0 : a.block);
+        __syncthreads();
+        angles(a, t0, n, turned);
+        __syncthreads();
+        // every lane goes round as often: the sums over lanes take all of them
+        const int rounds = (n * heads + kThreads / LANES - 1) / (kThreads / LANES);
+        for (int k = 0; k < rounds; ++k) {
+            const int e = k * (kThreads / LANES) + slot;
+            const bool there = e < n * heads;
+            const int t = there ? e / heads : 0, h = there ? e - t * heads : 0;
+            const bool second = h >= a.heads[0];
+            const Side& s = a.side[second ? 1 : 0];
+            const int head = second ? h - a.heads[0] : h;
+            const int64_t at = (t0 + t) * a.heads[second ? 1 : 0] + head;
+            const T* row = static_cast<const T*>(s.x) + (t0 + t) * s.token + (int64_t)head * s.head;
+            float x[U][2 * V], g[U][2 * V];
+            float sum = 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int p = (u * LANES + lane) * V;
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) x[u][i] = g[u][i] = 0.0f;
+                if (there && p < a.pairs) {
+                    P::load(row, a, p, x[u]);
+                    if constexpr (BACK) P::load(static_cast<const T*>(s.grad) + (t0 + t) * s.grad_token + (int64_t)head * s.grad_head, a, p, g[u]);
+                }
+            }
+            float rstd = 0.0f;
+            if constexpr (BACK) rstd = there ? s.rstd_in[at] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int p = (u * LANES + lane) * V;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    if constexpr (BACK) {
+                        // turned back
+                        float2 cs = make_float2(1.0f, 0.0f);
+                        if (p + i < a.rotated) cs = turned[t * a.rotated + p + i];
+                        const float ga = g[u][i], gb = g[u][V + i];
+                        g[u][i] = __builtin_fmaf(ga, cs.x, gb * cs.y);
+                        g[u][V + i] = __builtin_fmaf(gb, cs.x, -(ga * cs.y));
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) {
+                    if constexpr (BACK) {
+                        x[u][i] *= rstd;
+                        const float share = g[u][i] * x[u][i];
+                        if (second) dw[1][u][i] += share; else dw[0][u][i] += share;
+                        g[u][i] *= second ? w[1][u][i] : w[0][u][i];
+                        sum = __builtin_fmaf(g[u][i], x[u][i], sum);
+                    } else {
+                        sum = __builtin_fmaf(x[u][i], x[u][i], sum);
+                    }
+                }
+            }
+            sum = sum_lanes<LANES>(sum);
+            if constexpr (BACK) sum /= (float)a.D;
+            else rstd = 1.0f / sqrtf(sum / (float)a.D + a.eps);
+            if (!there) continue;
+            if (!BACK && lane == 0 && s.rstd) s.rstd[at] = rstd;
+            T* out = static_cast<T*>(s.y) + at * a.D;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int p = (u * LANES + lane) * V;
+                if (p >= a.pairs) continue;
+                float y[2 * V];
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) {
+                    if constexpr (BACK) y[i] = rstd * __builtin_fmaf(-x[u][i], sum, g[u][i]);
+                    else y[i] = x[u][i] * rstd * (second ? w[1][u][i] : w[0][u][i]);
+                }
+                if constexpr (!BACK) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float2 cs = make_float2(1.0f, 0.0f);
+                        if (p + i < a.rotated) cs = turned[t * a.rotated + p + i];
+                        const float ya = y[i], yb = y[V + i];
+                        y[i] = __builtin_fmaf(ya, cs.x, -(yb * cs.y));
+                        y[V + i] = __builtin_fmaf(ya, cs.y, yb * cs.x);
+                    }
+                }
+                P::store(out, a, p, y);
+            }
+        }
+    }
+    if constexpr (BACK) {
+        // the workgroup's share of the weights' gradients: slots one after the other
+        float* sums = reinterpret_cast<float*>(turned);         // [2][D]
+        __syncthreads();
+        for (int e = threadIdx.x; e < 2 * a.D; e += kThreads) sums[e] = 0.0f;
+        // within a wavefront by lanes, then wavefront by wavefront
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i)
+#pragma unroll
+                    for (int o = LANES; o < 64; o <<= 1) dw[k][u][i] += __shfl_xor(dw[k][u][i], o, 64);
+        for (int wave = 0; wave < kThreads / 64; ++wave) {
+            __syncthreads();
+            if ((int)(threadIdx.x >> 6) != wave || (threadIdx.x & 63) >= LANES) continue;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int p = (u * LANES + lane) * V;
+                    if (p >= a.pairs) continue;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int c = NEXT ? 2 * (p + i) : P::first(a, p) + i, d = NEXT ? c + 1 : c + P::second(a, p);
+                        sums[k * a.D + c] += dw[k][u][i];
+                        sums[k * a.D + d] += dw[k][u][V + i];
+                    }
+                }
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < 2 * a.D; e += kThreads) a.parts[(int64_t)blockIdx.x * 2 * a.D + e] = sums[e];
+    }
+}
+
+// The weights' gradients from the workgroups' shares, in a fixed order: 32 columns a workgroup, 32 threads a column
+struct AddArgs { const float* parts; void* out[2]; int bf16[2]; int count, D; };
+__global__ __launch_bounds__(1024) void add_weight_parts(AddArgs a) {
+    __shared__ float sums[32][33];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
+    float s = 0.0f;
+    if (c < 2 * a.D) {
+#pragma unroll 8
+        for (int r = row; r < a.count; r += 32) s += a.parts[(int64_t)r * 2 * a.D + c];
+    }
+    sums[row][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (row || c >= 2 * a.D) return;
+    s = 0.0f;
+    for (int r = 0; r < 32; ++r) s += sums[r][threadIdx.x];
+    const int k = c >= a.D, d = c - k * a.D;
+    if (!a.out[k]) return;
+    if (a.bf16[k]) static_cast<uint16_t*>(a.out[k])[d] = bf16_of(s);
+    else static_cast<float*>(a.out[k])[d] = s;
+}
+
+// ------------------------------------------------------------------ host side
+
+bool type_ok(division_dtype dt) { return dt == DIVISION_F32 || dt == DIVISION_BF16; }
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP; }
+#define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
+size_t size_of(division_dtype dt) { return dt == DIVISION_BF16 ? 2 : 4; }
+
+constexpr int kMostParts = 1024;                            // workgroups of a backward launch, which leave a share each
+int block_of(int64_t T) { return T >= 4096 ? 4 : 1; }
+int64_t grid_of(int64_t T, bool back) {
+    const int64_t n = (T + block_of(T) - 1) / block_of(T);
+    const int64_t most = back ? kMostParts : 1 << 20;
+    return n > most ? most : n;
+}
+
+// the tensors' own sizes; `back`: the gradients', which the forward pass has none of
+int check(const division_rotate& a, const division_rotate_back* back) {
+    if (!type_ok(a.dt) || a.T < 0 || a.D < 2 || a.D > 512 || a.D % 2 || a.rotated < 0 || a.rotated % 2 || a.rotated > a.D || (a.next != 0 && a.next != 1) || !(a.eps >= 0.0f)) return DIVISION_EINVAL;
+    if (a.T > 0x7fffffff) return DIVISION_ERANGE;
+    for (int k = 0; k < 2; ++k) {
+        if (a.heads[k] < 0 || (k == 0 && a.heads[k] == 0)) return DIVISION_EINVAL;
+        if (a.heads[k] == 0) continue;
+        if (a.heads[k] > 4096) return DIVISION_ERANGE;
+        if (!type_ok(a.weight_dt[k]) || !a.weight[k]) return DIVISION_EINVAL;
+        if (!aligned(a.weight[k], size_of(a.weight_dt[k]))) return DIVISION_EALIGN;
+        if (a.T == 0) continue;
+        const int64_t most = int64_t(1) << 40;
+        if (!a.x[k] || a.token_strides[k] < 0 || a.head_strides[k] < 0) return DIVISION_EINVAL;
+        if (!aligned(a.x[k], size_of(a.dt))) return DIVISION_EALIGN;
+        if (a.token_strides[k] > most / a.T || a.head_strides[k] > most / a.heads[k] || a.T * a.heads[k] > most / a.D) return DIVISION_ERANGE;
+        if (!back) {
+            if (!a.y[k]) return DIVISION_EINVAL;
+            if (!aligned(a.y[k], size_of(a.dt)) || !aligned(a.rstd[k], 4)) return DIVISION_EALIGN;
+        } else {
+            if (!back->grad_y[k] || !back->rstd[k] || !back->grad_x[k] || back->token_strides[k] < 0 || back->head_strides[k] < 0) return DIVISION_EINVAL;
+            if (!aligned(back->grad_y[k], size_of(a.dt)) || !aligned(back->rstd[k], 4) || !aligned(back->grad_x[k], size_of(a.dt))) return DIVISION_EALIGN;
+            if (back->token_strides[k] > most / a.T || back->head_strides[k] > most / a.heads[k]) return DIVISION_ERANGE;
+        }
+    }
+    if (a.T > 0 && ((a.rotated && !a.frequencies) || !a.positions)) return DIVISION_EINVAL;
+    return aligned(a.frequencies, 8) && aligned(a.positions, 8) ? DIVISION_OK : DIVISION_EALIGN;
+}
+
+RotateArgs args_of(const division_rotate& a) {
+    RotateArgs r{};
+    for (int k = 0; k < 2; ++k) {
+        r.side[k].x = a.x[k]; r.side[k].weight = a.weight[k];
+        r.side[k].token = a.token_strides[k]; r.side[k].head = a.head_strides[k];
+        r.side[k].y = a.y[k]; r.side[k].rstd = a.rstd[k];
+        r.side[k].weight_bf16 = a.weight_dt[k] == DIVISION_BF16;
+        r.heads[k] = (int)a.heads[k];
+    }
+    r.frequencies = a.frequencies; r.positions = a.positions;
+    r.T = a.T; r.D = (int)a.D; r.pairs = (int)a.D / 2; r.rotated = (int)a.rotated / 2; r.eps = a.eps;
+    r.block = block_of(a.T);
+    return r;
+}
+
+template <typename T, int V, int U, int LANES, bool BACK> int launch(const RotateArgs& a, bool next, uint32_t grid, hipStream_t st) {
+    size_t lds = (size_t)a.block * a.rotated * sizeof(float2);
+    if (BACK && lds < 2 * (size_t)a.D * 4) lds = 2 * (size_t)a.D * 4;
+    if (next) hipLaunchKernelGGL((rotate<T, V, U, LANES, true, BACK>), dim3(grid), dim3(kThreads), lds, st, a);
+    else hipLaunchKernelGGL((rotate<T, V, U, LANES, false, BACK>), dim3(grid), dim3(kThreads), lds, st, a);
+    return launched();
+}
+// Heads whose pairs are whole vectors of sixteen bytes; others element by element
+template <typename T, bool BACK> int run(const RotateArgs& a, bool next, hipStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const uint32_t grid = (uint32_t)grid_of(a.T, BACK);
+    if (a.pairs % V || (!next && a.rotated % V)) return a.pairs <= 64 ? launch<T, 1, 4, 16, BACK>(a, next, grid, st) : launch<T, 1, 4, 64, BACK>(a, next, grid, st);
+    const int units = a.pairs / V;
+    if (units <= 4) return launch<T, V, 1, 4, BACK>(a, next, grid, st);
+    if (units <= 8) return launch<T, V, 1, 8, BACK>(a, next, grid, st);
+    if (units <= 16) return launch<T, V, 1, 16, BACK>(a, next, grid, st);
+    if (units <= 32) return launch<T, V, 1, 32, BACK>(a, next, grid, st);
+    if constexpr (sizeof(T) == 4) return launch<T, V, 1, 64, BACK>(a, next, grid, st);
+    return DIVISION_EINVAL;
+}
+
+}  // namespace
+
+extern "C" {
+
+int division_head_norm_rotate(const division_rotate* rotate, void* hip_stream) {
+    if (!rotate) return DIVISION_EINVAL;
+    CHECKED(check(*rotate, nullptr));
+    if (rotate->T == 0) return DIVISION_OK;
+    const RotateArgs a = args_of(*rotate);
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    return rotate->dt == DIVISION_BF16 ? run<uint16_t, false>(a, rotate->next, st) : run<float, false>(a, rotate->next, st);
+}
+
+size_t division_head_norm_rotate_backward_workspace(int64_t T, int64_t D) {
+    return T <= 0 || T > 0x7fffffff || D < 2 || D > 512 ? 0 : (size_t)grid_of(T, true) * 2 * D * 4;
+}
+
+int division_head_norm_rotate_backward(const division_rotate* rotate, const division_rotate_back* back, void* hip_stream) {
+    if (!rotate || !back) return DIVISION_EINVAL;
+    CHECKED(check(*rotate, back));
+    const division_rotate& f = *rotate;
+    for (int k = 0; k < 2; ++k) {
+        if (f.heads[k] && !back->grad_weight[k]) return DIVISION_EINVAL;
+        if (f.heads[k] && !aligned(back->grad_weight[k], size_of(f.weight_dt[k]))) return DIVISION_EALIGN;
+    }
+    const size_t need = division_head_norm_rotate_backward_workspace(f.T, f.D);
+    if (need && !back->workspace) return DIVISION_EINVAL;
+    if (!aligned(back->workspace, 16)) return DIVISION_EALIGN;
+    if (back->workspace_bytes < need) return DIVISION_ESIZE;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    AddArgs add{};
+    if (f.T > 0) {
+        RotateArgs a = args_of(f);
+        for (int k = 0; k < 2; ++k) {
+            Side& s = a.side[k];
+            s.grad = back->grad_y[k]; s.grad_token = back->token_strides[k]; s.grad_head = back->head_strides[k];
+            s.rstd_in = back->rstd[k]; s.y = back->grad_x[k];
+        }
+        a.parts = static_cast<float*>(back->workspace);
+        CHECKED((f.dt == DIVISION_BF16 ? run<uint16_t, true>(a, f.next, st) : run<float, true>(a, f.next, st)));
+        add.parts = a.parts;
+        add.count = (int)grid_of(f.T, true);
+    }
+    add.D = (int)f.D;
+    for (int k = 0; k < 2; ++k) { add.out[k] = f.heads[k] ? back->grad_weight[k] : nullptr; add.bf16[k] = f.weight_dt[k] == DIVISION_BF16; }
+    hipLaunchKernelGGL(add_weight_parts, dim3((uint32_t)((2 * f.D + 31) / 32)), dim3(1024), 0, st, add);
+    return launched();
+}
+
+}  // extern "C"
