@@ -39,19 +39,18 @@ template <typename T, int DP> struct Columns {
         const int half = lane >> 5;
         f32x16 z[KT / 32];
 #pragma unroll
-        for (int b = 0; b < KT / 32; ++b) {
-            z[b] = (f32x16)(0.0f);
+        for (auto& b : z) b = (f32x16)(0.0f);
 #pragma unroll
-            for (int s = 0; s < DP / 16; ++s) product(z[b], Tile<T, DP>::rows(kt, 32 * b, s, lane), q[s]);
-        }
+        for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+            for (int b = 0; b < KT / 32; ++b) product(z[b], Tile<T, DP, KT>::rows(kt, 32 * b, s, lane), q[s]);
         if (!whole) {
+            uint32_t n = (uint32_t)(to - from);
+            stay_a_branch(n);
 #pragma unroll
             for (int b = 0; b < KT / 32; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int j = first + 32 * b + block_row(i, half);
-                    z[b][i] = j >= from && j < to ? z[b][i] : -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i) z[b][i] = (uint32_t)(first + 32 * b + block_row(i, half) - from) < n ? z[b][i] : -INFINITY;
         }
         float m = z[0][0];
 #pragma unroll
@@ -62,6 +61,7 @@ template <typename T, int DP> struct Columns {
         // The maximum that exponents are taken against need not be the largest yet: sums and products stay exact to their last bits while they grow by at most 2^8, so that most tiles leave
         // the weighted values alone
         if (__any((m - most) * scale2 > 8.0f || most == -INFINITY)) {
+            stay_a_branch(m);
             m = fmaxf(m, most);
             const float shrink = most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((most - m) * scale2);
             total *= shrink;
@@ -85,7 +85,7 @@ template <typename T, int DP> struct Columns {
                 for (int j = 0; j < 8; ++j) w[j] = z[b][8 * c + j];
                 const Operand<T> p = Operand<T>::of(w);
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) product(o[d], Tile<T, DP>::columns(vt, 32 * b + 16 * c, 32 * d, lane), p);
+                for (int d = 0; d < DP / 32; ++d) product(o[d], Tile<T, DP, KT>::columns(vt, 32 * b + 16 * c, 32 * d, lane), p);
             }
         }
     }
@@ -103,7 +103,7 @@ constexpr int kThreads = 256;
 
 // Four wavefronts of 32 columns each share the tiles of the keys.
 template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attend(AttentionArgs a) {
-    constexpr int kTile = KT * Tile<T, DP>::kRowBytes;
+    constexpr int kTile = Tile<T, DP, KT>::kBytes;
     __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile];
     const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
@@ -121,14 +121,14 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
     const int wave_from = seen.from(qa), whole_from = seen.from(qb), whole_to = seen.to(qa), wave_to = works ? seen.to(qb) : 0;
     const int i = (int)(min(col, cols - 1) / (uint32_t)a.R);
-    const int from = seen.from(i), to = col < cols ? seen.to(i) : 0;
+    const int from = seen.from(i), to = col < cols ? max(from, seen.to(i)) : from;
     const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
     const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     const int row_bytes = a.D * (int)sizeof(T);
     const auto fetch = [&](int t) {
         const int left = seen.keys - t * KT;
-        Tile<T, DP>::template fill<KT, kThreads>(tiles[t & 1][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
-        Tile<T, DP>::template fill<KT, kThreads>(tiles[t & 1][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
+        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
+        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
     };
     if (lo < hi) fetch(lo);
     Columns<T, DP> c;
@@ -139,8 +139,7 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     for (int t = lo; t < hi; ++t) {
         if (t + 1 < hi) fetch(t + 1);
         const int j = t * KT;
-        if (j < wave_to && j + KT > wave_from)
-            c.template add<KT>(tiles[t & 1][0], tiles[t & 1][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
+        c.template add<KT>(tiles[t & 1][0], tiles[t & 1][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
         loads_done();
         __syncthreads();
     }
@@ -176,7 +175,7 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
 
 // Few columns: WK wavefronts have the same 32 columns and every WK-th tile of the keys each, in tiles of their own, and are joined at the end.
 template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * WK) void attend_few(AttentionArgs a) {
-    constexpr int kTile = KT * Tile<T, DP>::kRowBytes, kLoads = 2 * kTile / 1024, kRow = DP + 4;
+    constexpr int kTile = Tile<T, DP, KT>::kBytes, kLoads = 2 * kTile / 1024, kRow = DP + 4;
     static_assert(32 * kRow * 4 <= 4 * kTile, "a wavefront's values in place of its tiles");
     __shared__ __attribute__((aligned(16))) char tiles[WK][2][2][kTile];
     __shared__ float most[WK][32], totals[WK][32];
@@ -190,14 +189,14 @@ template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * 
     const int whole_from = seen.from(qb), whole_to = seen.to(qa);
     const int lo = max(seen.from(qa) / KT, split * a.tiles), hi = min((seen.to(qb) + KT - 1) / KT, (split + 1) * a.tiles);
     const int i = (int)(min(col, cols - 1) / (uint32_t)a.R);
-    const int from = seen.from(i), to = col < cols ? seen.to(i) : 0;
+    const int from = seen.from(i), to = col < cols ? max(from, seen.to(i)) : from;
     const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
     const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     const int row_bytes = a.D * (int)sizeof(T);
     const auto fetch = [&](int t, int at) {
         const int left = seen.keys - t * KT;
-        Tile<T, DP>::template fill<KT, 64>(tiles[wave][at][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
-        Tile<T, DP>::template fill<KT, 64>(tiles[wave][at][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
+        Tile<T, DP, KT>::template fill<64>(tiles[wave][at][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
+        Tile<T, DP, KT>::template fill<64>(tiles[wave][at][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
     };
     Columns<T, DP> c;
     c.begin(a, a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head, col, cols, half);
@@ -256,18 +255,28 @@ template <typename T> __global__ __launch_bounds__(kThreads) void join_parts(Att
     const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R;
     const int64_t n = (int64_t)a.groups * cols, at = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
     const int d = (threadIdx.x & 31) * 4;
-    if (at >= n) return;
-    float most = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) most = fmaxf(most, a.parts[s * n + at]);
-    const float* values = a.parts + a.splits * n;
+    if (at >= n) return;                                    // whole groups of 32 lanes
+    // the parts' lse: two lanes' of each
+    const int lane = threadIdx.x & 31;
+    float lses[2], most = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        lses[k] = lane + 32 * k < a.splits ? a.parts[(lane + 32 * k) * n + at] : -INFINITY;
+        most = fmaxf(most, lses[k]);
+    }
+#pragma unroll
+    for (int k = 16; k; k >>= 1) most = fmaxf(most, __shfl_xor(most, k, 64));
+    const float* values = a.parts + a.splits * n + at * a.D + d;
     f32x4 o = {0, 0, 0, 0};
     float sum = 0.0f;
+#pragma unroll 8
     for (int s = 0; s < a.splits; ++s) {
-        const float lse = a.parts[s * n + at];
-        if (lse == -INFINITY) continue;
-        const float by = __builtin_amdgcn_exp2f((lse - most) * kLog2e);
+        const float lse = __shfl(s < 32 ? lses[0] : lses[1], (threadIdx.x & 32) + (s & 31), 64);
+        const bool some = lse != -INFINITY;                 // what no key was seen for was not written
+        const float by = some ? __builtin_amdgcn_exp2f((lse - most) * kLog2e) : 0.0f;
         sum += by;
-        if (d < a.D) o += by * *reinterpret_cast<const f32x4*>(values + (s * n + at) * a.D + d);
+        const f32x4 part = some && d < a.D ? *reinterpret_cast<const f32x4*>(values + s * n * a.D) : f32x4{0, 0, 0, 0};
+        o += by * part;
     }
     o *= sum == 0.0f ? 0.0f : 1.0f / sum;
     const int group = (int)(at / cols), b = group / a.G;
@@ -286,11 +295,10 @@ Cut cut_of(const division_attention& a) {
     const int64_t R = a.H / a.G, cols = a.Sq * R;
     c.few = cols <= 32;
     c.blocks = (cols + (c.few ? 31 : 127)) / (c.few ? 32 : 128);
-    c.key_tile = c.few ? (a.dt == DIVISION_BF16 ? 32 : 32) : 64;
+    c.key_tile = c.few ? 32 : 64;
     const int64_t tiles = (a.Sk + c.key_tile - 1) / c.key_tile, tasks = c.blocks * a.B * a.G;
-    // a part has at least two tiles for each wavefront that shares them
-    const int64_t least = c.few ? 8 : 8, room = tiles / least;
-    int64_t splits = tasks >= 256 ? 1 : (512 + tasks - 1) / tasks;
+    const int64_t least = c.few ? (a.dt == DIVISION_BF16 ? 4 : 2) : 4, room = tiles / least, wanted = c.few ? 1024 : 512;
+    int64_t splits = tasks >= (c.few ? 1024 : 256) ? 1 : (wanted + tasks - 1) / tasks;
     if (splits > room) splits = room;
     if (splits > 64) splits = 64;
     if (splits < 1) splits = 1;

@@ -19,7 +19,7 @@ struct BackArgs : AttentionArgs {
     const char *grad, *o;
     Heads gs;
     char *dq, *dk, *dv;
-    float *exponents, *deltas;                          // [group][column]: lse in powers of two (infinity where nothing is seen), rowsum(grad out)
+    float* stats;                                       // [group][column][2]: lse in powers of two (infinity where nothing is seen), rowsum(grad out)
     FastDiv by_R;
 };
 
@@ -50,7 +50,7 @@ constexpr int kThreads = 256;
 
 // Four wavefronts of 32 columns (queries) each share the tiles of the keys and values.
 template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void back_queries(BackArgs a) {
-    constexpr int kTile = KT * Tile<T, DP>::kRowBytes;
+    constexpr int kTile = Tile<T, DP, KT>::kBytes;
     __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile];
     const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int group = blockIdx.x % a.groups, block = a.blocks - 1 - blockIdx.x / a.groups;
@@ -64,36 +64,36 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
     const int wave_from = seen.from(qa), whole_from = seen.from(qb), whole_to = seen.to(qa), wave_to = works ? seen.to(qb) : 0;
     const int i = (int)(min(col, cols - 1) / (uint32_t)a.R), r = (int)(min(col, cols - 1) % (uint32_t)a.R);
-    const int from = seen.from(i), to = there ? seen.to(i) : 0;
+    const int from = seen.from(i), to = there ? max(from, seen.to(i)) : from;
     const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
     const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     const int row_bytes = a.D * (int)sizeof(T);
     const auto fetch = [&](int t) {
         const int left = seen.keys - t * KT;
-        Tile<T, DP>::template fill<KT, kThreads>(tiles[t & 1][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
-        Tile<T, DP>::template fill<KT, kThreads>(tiles[t & 1][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
+        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
+        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
     };
     if (lo < hi) fetch(lo);
     Operand<T> q[DP / 16], grad[DP / 16];
     get_column<T, DP>(q, a.q + b * a.qs.batch + row_offset(a.qs, i, g * a.R + r), there, row_bytes, half);
     get_column<T, DP>(grad, a.grad + b * a.gs.batch + row_offset(a.gs, i, g * a.R + r), there, row_bytes, half);
     const int64_t row = ((int64_t)b * a.Sq + i) * a.H + g * a.R + r;
+    // the diagonal of out grad^T, by the products that make grad v^T: where a query sees one key, whose value is its output, the two are equal to the last bit and the scores'
+    // gradient is 0
     float delta = 0.0f;
     {
         Operand<T> o[DP / 16];
         get_column<T, DP>(o, a.o + row * row_bytes, there, row_bytes, half);
+        f32x16 all = (f32x16)(0.0f);
 #pragma unroll
-        for (int s = 0; s < DP / 16; ++s)
+        for (int s = 0; s < DP / 16; ++s) product(all, o[s], grad[s]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) delta = __builtin_fmaf(o[s][j], grad[s][j], delta);
-        delta = halves_sum(delta);
+        for (int e = 0; e < 16; ++e) delta = block_row(e, half) == (lane & 31) ? all[e] : delta;
+        delta = halves_sum(delta);                      // the other half has 0
     }
     float exponent = there ? a.lse[((int64_t)b * a.H + g * a.R + r) * a.Sq + i] * kLog2e : INFINITY;
     if (exponent == -INFINITY) exponent = INFINITY;
-    if (there && half == 0) {
-        a.exponents[(int64_t)group * cols + col] = exponent;
-        a.deltas[(int64_t)group * cols + col] = delta;
-    }
+    if (there && half == 0) *reinterpret_cast<f32x2*>(a.stats + ((int64_t)group * cols + col) * 2) = f32x2{exponent, delta};
     const float scale2 = a.scale * kLog2e;
     f32x16 dq[DP / 32];
 #pragma unroll
@@ -104,26 +104,26 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
         if (t + 1 < hi) fetch(t + 1);
         const int j0 = t * KT;
         const char *kt = tiles[t & 1][0], *vt = tiles[t & 1][1];
-        if (j0 < wave_to && j0 + KT > wave_from) {
+        {
             const bool whole = j0 >= whole_from && j0 + KT <= whole_to;
 #pragma unroll
             for (int n = 0; n < KT / 32; ++n) {
                 f32x16 z = (f32x16)(0.0f), dp = (f32x16)(0.0f);
 #pragma unroll
-                for (int s = 0; s < DP / 16; ++s) product(z, Tile<T, DP>::rows(kt, 32 * n, s, lane), q[s]);
-#pragma unroll
-                for (int s = 0; s < DP / 16; ++s) product(dp, Tile<T, DP>::rows(vt, 32 * n, s, lane), grad[s]);
+                for (int s = 0; s < DP / 16; ++s) {
+                    product(z, Tile<T, DP, KT>::rows(kt, 32 * n, s, lane), q[s]);
+                    product(dp, Tile<T, DP, KT>::rows(vt, 32 * n, s, lane), grad[s]);
+                }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], scale2, -exponent));
                     z[e] = p * (dp[e] - delta);
                 }
                 if (!whole) {
+                    uint32_t keys = (uint32_t)(to - from);
+                    stay_a_branch(keys);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int j = j0 + 32 * n + block_row(e, half);
-                        z[e] = j >= from && j < to ? z[e] : 0.0f;
-                    }
+                    for (int e = 0; e < 16; ++e) z[e] = (uint32_t)(j0 + 32 * n + block_row(e, half) - from) < keys ? z[e] : 0.0f;
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -132,7 +132,7 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
                     for (int j = 0; j < 8; ++j) w[j] = z[8 * c + j];
                     const Operand<T> ds = Operand<T>::of(w);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) product(dq[d], Tile<T, DP>::columns(kt, 32 * n + 16 * c, 32 * d, lane), ds);
+                    for (int d = 0; d < DP / 32; ++d) product(dq[d], Tile<T, DP, KT>::columns(kt, 32 * n + 16 * c, 32 * d, lane), ds);
                 }
             }
         }
@@ -142,12 +142,19 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     if (there) put_column<T, DP>(reinterpret_cast<T*>(a.dq) + row * a.D, dq, a.scale, a.D, half);
 }
 
-// Four wavefronts of 32 keys each share the tiles of the columns (queries of all heads that share the keys) and their gradients.
-template <typename T, int DP, int CT> __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void back_keys(BackArgs a) {
-    constexpr int kTile = CT * Tile<T, DP>::kRowBytes;
-    __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile];
-    __shared__ __attribute__((aligned(16))) float stats[2][2][CT];
-    const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+// Wavefronts of 32 keys each, four of them for 128 keys, share the tiles of the columns (queries of all heads that share the keys) and their gradients.  SETS such fours take every SETS-th
+// tile each and are added up at the end: with two there are always two wavefronts a SIMD, one with the matrix unit while the other takes exponentials.  VALUES: the values wait in the
+// local memory, not in registers.
+template <typename T, int DP, int CT, int SETS, int STAGES, bool VALUES> __global__ __launch_bounds__(kThreads * SETS) void back_keys(BackArgs a) {
+    typedef Tile<T, DP, CT> Columns;
+    typedef Tile<T, DP, 128> Values;
+    constexpr int kTiles = SETS * STAGES * 2 * Columns::kBytes, kLoads = 2 * Columns::kBytes / 16 / kThreads, kSum = 4 * 64 * (DP / 32) * 16 * 4;
+    static_assert(SETS == 1 || kSum <= kTiles + (VALUES ? Values::kBytes : 0), "one set's blocks in place of the tiles");
+    __shared__ __attribute__((aligned(16))) char memory[kTiles + (VALUES ? Values::kBytes : 0)];
+    __shared__ __attribute__((aligned(16))) float stats[SETS][STAGES][CT][2];
+    static_assert(CT == 32, "a tile's numbers are one load of a wavefront");
+    const int set = SETS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads), thread = threadIdx.x % kThreads, lane = thread & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int group = blockIdx.x % a.groups, block = blockIdx.x / a.groups;
     const int b = group / a.G, g = group % a.G;
     const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R;
@@ -159,68 +166,75 @@ template <typename T, int DP, int CT> __global__ __launch_bounds__(kThreads, siz
     const int lo = any ? seen.query_from(first) * a.R / CT : 0, hi = any ? (seen.query_to(last) * a.R + CT - 1) / CT : 0;
     const int wave_from = seen.query_from(min(wave_key, a.Sk - 1)) * a.R, wave_to = works ? seen.query_to(wave_last) * a.R : 0;
     const int whole_from = seen.query_from(min(wave_key + 31, a.Sk - 1)) * a.R, whole_to = works && wave_key + 31 < seen.keys ? seen.query_to(wave_key) * a.R : 0;
-    const int from = there ? seen.query_from(key) * a.R : 0, to = there ? seen.query_to(key) * a.R : 0;
+    const int from = there ? seen.query_from(key) * a.R : 0, to = there ? max(from, seen.query_to(key) * a.R) : 0;
     const char* q = a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head;
     const char* gr = a.grad + b * a.gs.batch + (int64_t)g * a.R * a.gs.head;
     const int row_bytes = a.D * (int)sizeof(T);
-    const auto fetch = [&](int t) {
+    char* mine = memory + set * STAGES * 2 * Columns::kBytes;
+    const auto fetch = [&](int t, int at) {
         const uint32_t c0 = (uint32_t)t * CT, i0 = c0 / (uint32_t)a.R, r0 = c0 - i0 * (uint32_t)a.R;
         const int left = (int)(cols - c0);
-        const auto at = [&](const Heads& s) {
+        const auto offset = [&](const Heads& s) {
             return [&, s](int row) { const uint32_t n = r0 + row, i = fdiv(n, a.by_R); return (int)i * s.token + (int)(n - i * (uint32_t)a.R) * s.head; };
         };
-        Tile<T, DP>::template fill<CT, kThreads>(tiles[t & 1][0], q + (int64_t)i0 * a.qs.token, left, row_bytes, thread, at(a.qs));
-        Tile<T, DP>::template fill<CT, kThreads>(tiles[t & 1][1], gr + (int64_t)i0 * a.gs.token, left, row_bytes, thread, at(a.gs));
+        char* to = mine + at * 2 * Columns::kBytes;
+        if (wave == 0) {                                    // columns behind the last have zeros: their rows are zeros too
+            load_lds4(buffer(a.stats + ((int64_t)group * cols + c0) * 2, 4u * 2 * (uint32_t)min(left, CT)), stats[set][at], (uint32_t)lane * 4);
+        }
+        Columns::template fill<kThreads>(to, q + (int64_t)i0 * a.qs.token, left, row_bytes, thread, offset(a.qs));
+        Columns::template fill<kThreads>(to + Columns::kBytes, gr + (int64_t)i0 * a.gs.token, left, row_bytes, thread, offset(a.gs));
     };
-    // a tile's numbers of its columns: two for each, on their way in a register
-    const auto stat = [&](int t) {
-        const uint32_t c = (uint32_t)t * CT + thread % CT;
-        if (thread >= 2 * CT) return 0.0f;
-        if (c >= cols) return thread < CT ? INFINITY : 0.0f;
-        return (thread < CT ? a.exponents : a.deltas)[(int64_t)group * cols + c];
-    };
-    float next = 0.0f;
-    if (lo < hi) { fetch(lo); next = stat(lo); }
-    Operand<T> k[DP / 16], v[DP / 16];
+#pragma unroll
+    for (int n = 0; n < STAGES - 1; ++n)
+        if (lo + n * SETS + set < hi) fetch(lo + n * SETS + set, n);
+    char* values = memory + kTiles;
+    const char* v_head = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
+    if constexpr (VALUES)
+        Values::template fill<kThreads * SETS>(values, v_head + (int64_t)first * a.vs.token, seen.keys - first, row_bytes, threadIdx.x, [&](int row) { return row * a.vs.token; });
+    Operand<T> k[DP / 16], v[VALUES ? 1 : DP / 16];
     get_column<T, DP>(k, a.k + b * a.ks.batch + row_offset(a.ks, key, g), there, row_bytes, half);
-    get_column<T, DP>(v, a.v + b * a.vs.batch + row_offset(a.vs, key, g), there, row_bytes, half);
+    if constexpr (!VALUES) get_column<T, DP>(v, v_head + (int64_t)key * a.vs.token, there, row_bytes, half);
     const float scale2 = a.scale * kLog2e;
     f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (auto& x : dk) x = (f32x16)(0.0f);
 #pragma unroll
     for (auto& x : dv) x = (f32x16)(0.0f);
-    if (lo < hi && thread < 2 * CT) stats[lo & 1][thread / CT][thread % CT] = next;
     loads_done();
     __syncthreads();
-    for (int t = lo; t < hi; ++t) {
-        if (t + 1 < hi) { fetch(t + 1); next = stat(t + 1); }
+    int at = 0;
+    for (int t0 = lo; t0 < hi; t0 += SETS, at = at + 1 == STAGES ? 0 : at + 1) {
+        const int t = t0 + set;
+        const bool more = t + (STAGES - 1) * SETS < hi;
+        if (more) fetch(t + (STAGES - 1) * SETS, at == 0 ? STAGES - 1 : at - 1);
         const int c0 = t * CT;
-        const char *qt = tiles[t & 1][0], *gt = tiles[t & 1][1];
-        if (c0 < wave_to && c0 + CT > wave_from) {
+        const char *qt = mine + at * 2 * Columns::kBytes, *gt = qt + Columns::kBytes;
+        if (t < hi) {
             const bool whole = c0 >= whole_from && c0 + CT <= whole_to;
 #pragma unroll 1
             for (int n = 0; n < CT / 32; ++n) {
                 f32x16 z = (f32x16)(0.0f), dp = (f32x16)(0.0f);
 #pragma unroll
-                for (int s = 0; s < DP / 16; ++s) product(z, Tile<T, DP>::rows(qt, 32 * n, s, lane), k[s]);
+                for (int s = 0; s < DP / 16; ++s) {
+                    product(z, Columns::rows(qt, 32 * n, s, lane), k[s]);
+                    if constexpr (VALUES) product(dp, Columns::rows(gt, 32 * n, s, lane), Values::rows(values, 32 * wave, s, lane));
+                    else product(dp, Columns::rows(gt, 32 * n, s, lane), v[s]);
+                }
 #pragma unroll
-                for (int s = 0; s < DP / 16; ++s) product(dp, Tile<T, DP>::rows(gt, 32 * n, s, lane), v[s]);
+                for (int e = 0; e < 16; e += 2) {
+                    const f32x4 two = *reinterpret_cast<const f32x4*>(stats[set][at][32 * n + block_row(e, half)]);
 #pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    const f32x4 ex = *reinterpret_cast<const f32x4*>(&stats[t & 1][0][32 * n + block_row(e, half)]);
-                    const f32x4 de = *reinterpret_cast<const f32x4*>(&stats[t & 1][1][32 * n + block_row(e, half)]);
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) {
-                        z[e + f] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e + f], scale2, -ex[f]));
-                        dp[e + f] = z[e + f] * (dp[e + f] - de[f]);
+                    for (int f = 0; f < 2; ++f) {
+                        z[e + f] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e + f], scale2, -two[2 * f]));
+                        dp[e + f] = z[e + f] * (dp[e + f] - two[2 * f + 1]);
                     }
                 }
                 if (!whole) {
+                    uint32_t seeing = (uint32_t)(to - from);
+                    stay_a_branch(seeing);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int c = c0 + 32 * n + block_row(e, half);
-                        const bool sees = c >= from && c < to;
+                        const bool sees = (uint32_t)(c0 + 32 * n + block_row(e, half) - from) < seeing;
                         z[e] = sees ? z[e] : 0.0f;
                         dp[e] = sees ? dp[e] : 0.0f;
                     }
@@ -232,15 +246,42 @@ template <typename T, int DP, int CT> __global__ __launch_bounds__(kThreads, siz
                     for (int j = 0; j < 8; ++j) { w[j] = z[8 * c + j]; x[j] = dp[8 * c + j]; }
                     const Operand<T> p = Operand<T>::of(w), ds = Operand<T>::of(x);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) product(dv[d], Tile<T, DP>::columns(gt, 32 * n + 16 * c, 32 * d, lane), p);
+                    for (int d = 0; d < DP / 32; ++d) product(dv[d], Columns::columns(gt, 32 * n + 16 * c, 32 * d, lane), p);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) product(dk[d], Tile<T, DP>::columns(qt, 32 * n + 16 * c, 32 * d, lane), ds);
+                    for (int d = 0; d < DP / 32; ++d) product(dk[d], Columns::columns(qt, 32 * n + 16 * c, 32 * d, lane), ds);
                 }
             }
         }
-        if (t + 1 < hi && thread < 2 * CT) stats[(t + 1) & 1][thread / CT][thread % CT] = next;
-        loads_done();
+        // the next tile is there when all but the newest's loads are
+        if (more && STAGES > 2) loads_done<(STAGES - 2) * kLoads>();
+        else loads_done();
         __syncthreads();
+    }
+    if constexpr (SETS == 2) {
+        f32x4* sums = reinterpret_cast<f32x4*>(memory) + thread;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            f32x16* o = part ? dv : dk;
+            if (part) __syncthreads();
+            if (set) {
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sums[(4 * d + e) * kThreads] = f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+            }
+            __syncthreads();
+            if (!set) {
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const f32x4 more = sums[(4 * d + e) * kThreads];
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) o[d][4 * e + f] += more[f];
+                    }
+            }
+        }
+        if (set) return;
     }
     if (key >= a.Sk) return;
     const int64_t row = (((int64_t)b * a.Sk + key) * a.G + g) * a.D;
@@ -264,7 +305,8 @@ template <typename T, int DP> int run(BackArgs& args, hipStream_t st) {
         const int64_t blocks = ((int64_t)args.Sk + 127) / 128;
         if (blocks * args.groups >= (int64_t(1) << 24)) return DIVISION_ERANGE;
         args.blocks = (int)blocks;
-        hipLaunchKernelGGL((back_keys<T, DP, 64>), dim3((uint32_t)(blocks * args.groups)), dim3(kThreads), 0, st, args);
+        constexpr bool kPair = sizeof(T) == 2 || DP == 64;
+        hipLaunchKernelGGL((back_keys<T, DP, 32, kPair ? 2 : 1, 2, sizeof(T) == 2 && DP == 128>), dim3((uint32_t)(blocks * args.groups)), dim3(kPair ? 2 * kThreads : kThreads), 0, st, args);
         CHECKED(launched());
     }
     return DIVISION_OK;
@@ -297,8 +339,7 @@ int division_attention_backward(const division_attention* attention, const divis
     args.o = static_cast<const char*>(w.out);
     args.lse = const_cast<float*>(w.lse);
     args.dq = static_cast<char*>(w.grad_q); args.dk = static_cast<char*>(w.grad_k); args.dv = static_cast<char*>(w.grad_v);
-    args.exponents = static_cast<float*>(w.workspace);
-    args.deltas = args.exponents + a.B * a.Sq * a.H;
+    args.stats = static_cast<float*>(w.workspace);
     args.by_R = make_fastdiv((uint32_t)args.R);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, st) : run<uint16_t, 128>(args, st);

@@ -45,6 +45,7 @@ template <typename T, bool PAST> __global__ __launch_bounds__(kThreads) void loo
 // ------------------------------------------------------------------ the tokens in the order of their ids
 
 constexpr int kOrderThreads = 1024, kOrderWaves = kOrderThreads / 64, kMostRows = 512;       // rows of the table whose tokens a workgroup puts in order
+constexpr int kKept = 16;                                   // ids of a thread that stay in registers between the two times they are looked at: 16384 tokens
 
 struct OrderArgs {
     const int64_t* ids;
@@ -56,7 +57,7 @@ struct OrderArgs {
 
 // Every workgroup reads all ids and keeps those of its rows; how many lie before its rows tells it where its tokens begin, so that workgroups need not wait for one another.  Each wavefront
 // has an equal run of the tokens.  First they count: [row][wavefront].  The running sum over these numbers is where a wavefront's tokens of a row begin, and then each puts its own there,
-// in their order.  T ids are read twice by each workgroup, from the caches.
+// in their order.
 __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     extern __shared__ uint32_t counts[];                    // [rows][kOrderWaves]
     __shared__ uint32_t sums[kOrderWaves], before;
@@ -67,14 +68,31 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     for (int e = threadIdx.x; e < n; e += kOrderThreads) counts[e] = 0;
     if (threadIdx.x == 0) before = 0;
     __syncthreads();
-    uint32_t less = 0;
-    for (uint32_t t = first + lane; t < end; t += 64) {
-        const int64_t id = a.ids[t];
-        if (id < 0 || id >= a.V || id == a.ignore) continue;
-        if (id < lo) ++less;
-        else if (id - lo < rows) atomicAdd(&counts[(uint32_t)(id - lo) * kOrderWaves + wave], 1u);
+    // the row among the workgroup's; before them: kBefore, none of them: kNone
+    constexpr uint32_t kNone = 0xffffffffu, kBefore = 0xfffffffeu;
+    const auto row_of = [&](uint32_t t) {
+        const int64_t id = t < end ? a.ids[t] : -1;
+        if (id < 0 || id >= a.V || id == a.ignore) return kNone;
+        return id < lo ? kBefore : id - lo < rows ? (uint32_t)(id - lo) : kNone;
+    };
+    uint32_t less = 0, kept[kKept];
+    const auto count = [&](uint32_t row) {
+        if (row == kBefore) ++less;
+        else if (row != kNone) atomicAdd(&counts[row * kOrderWaves + wave], 1u);
+    };
+#pragma unroll
+    for (int k = 0; k < kKept; ++k) kept[k] = row_of(first + k * 64 + lane);
+#pragma unroll
+    for (int k = 0; k < kKept; ++k) count(kept[k]);
+    for (uint32_t t = first + kKept * 64; t < end; t += 256) {
+        uint32_t more[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) more[k] = row_of(t + k * 64 + lane);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) count(more[k]);
     }
-    atomicAdd(&before, less);
+    for (int o = 32; o; o >>= 1) less += (uint32_t)__shfl_xor((int)less, o, 64);
+    if (lane == 0) atomicAdd(&before, less);
     __syncthreads();
     // running sum over all numbers: a run of them a thread
     const int each = (n + kOrderThreads - 1) / kOrderThreads, from = min((int)threadIdx.x * each, n), to = min(from + each, n);
@@ -98,12 +116,8 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     }
     if (lo + rows == a.V && threadIdx.x == kOrderThreads - 1) a.starts[a.V] = at;
     __syncthreads();
-    for (uint32_t t0 = first; t0 < end; t0 += 64) {
-        const uint32_t t = t0 + lane;
-        const int64_t id = t < end ? a.ids[t] : -1;
-        const bool mine = id >= lo && id - lo < rows && id != a.ignore;
-        const uint32_t row = mine ? (uint32_t)(id - lo) : 0xffffffffu;
-        uint64_t left = __ballot(mine);
+    const auto place = [&](uint32_t row, uint32_t t) {
+        uint64_t left = __ballot(row < kBefore);
         while (left) {                                      // the tokens of one row at a time
             const int leader = __builtin_ctzll(left);
             const uint32_t theirs = (uint32_t)__builtin_amdgcn_readlane((int)row, leader);
@@ -114,102 +128,145 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
             left &= ~same;
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // the next token of this row may be another lane's
         }
+    };
+#pragma unroll
+    for (int k = 0; k < kKept; ++k) place(kept[k], first + k * 64 + lane);
+    for (uint32_t t = first + kKept * 64; t < end; t += 256) {
+        uint32_t more[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) more[k] = row_of(t + k * 64 + lane);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) place(more[k], t + k * 64 + lane);
     }
 }
 
 // ------------------------------------------------------------------ the rows' sums
 
-constexpr int kMany = 128;                                  // a row of more tokens is added up by several wavefronts, a part of so many tokens each
-
 struct SumArgs {
     const void* grad;
     const int64_t* ids;
     const uint32_t *order, *starts;
-    float* parts;                                           // [parts of the sorted tokens][2][D]: of the row that begins before the part, of the one that ends behind it
+    float* parts;                                           // [parts of the sorted tokens][2][D]: of the row that began before the part, of the one that begins in it
     void* out;
     int64_t stride, V, D;
-    uint32_t T;
+    uint32_t T, part;                                       // part: tokens that a wavefront adds up at most; a row of more is added up in parts
     float scale;
-    int add, columns;                                       // columns: pieces of 512 elements (bfloat16) or 256 of a row
+    int add, columns;                                       // columns: pieces of 64 * kSize * P elements of a row
 };
 
-// C elements a lane of the sum over tokens order[from .. to - 1], four at a time on their way
-template <typename T> __device__ __forceinline__ void sum_rows(const SumArgs& a, uint32_t from, uint32_t to, int64_t c, float* v) {
+// P vectors a lane of a row's columns, 64 lanes' vectors one behind the other
+template <typename T, int P> struct Row {
     typedef Unit<T> U;
-    const T* grad = static_cast<const T*>(a.grad);
+    float v[P][U::kSize];
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int i = 0; i < U::kSize; ++i) v[i] = 0.0f;
-    uint32_t k = from;
-    for (; k + 4 <= to; k += 4) {
-        U q[4];
+        for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) q[u] = load_some<U>(grad + (int64_t)a.order[k + u] * a.stride, c, a.D);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int i = 0; i < U::kSize; ++i) v[i] += q[u][i];
+            for (int i = 0; i < U::kSize; ++i) v[p][i] = 0.0f;
     }
-    for (; k < to; ++k) {
-        const U q = load_some<U>(grad + (int64_t)a.order[k] * a.stride, c, a.D);
+    // adds tokens order[from .. to - 1], several rows at a time on their way; first: a column
+    __device__ __forceinline__ void add(const SumArgs& a, uint32_t from, uint32_t to, int64_t c) {
+        constexpr int kAtOnce = P == 1 ? 8 : 4;
+        const T* grad = static_cast<const T*>(a.grad);
+        uint32_t k = from;
+        for (; k + kAtOnce <= to; k += kAtOnce) {
+            U q[kAtOnce][P];
 #pragma unroll
-        for (int i = 0; i < U::kSize; ++i) v[i] += q[i];
+            for (int u = 0; u < kAtOnce; ++u) {
+                const T* row = grad + (int64_t)a.order[k + u] * a.stride;
+#pragma unroll
+                for (int p = 0; p < P; ++p) q[u][p] = load_some<U>(row, c + p * 64 * U::kSize, a.D);
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int i = 0; i < U::kSize; ++i) v[p][i] += q[u][p][i];
+        }
+        for (; k < to; ++k) {
+            const T* row = grad + (int64_t)a.order[k] * a.stride;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const U q = load_some<U>(row, c + p * 64 * U::kSize, a.D);
+#pragma unroll
+                for (int i = 0; i < U::kSize; ++i) v[p][i] += q[i];
+            }
+        }
     }
-}
+};
 
-// Parts of rows of many tokens: a wavefront has kMany sorted tokens and a piece of the columns.  At most two such rows have tokens among them.
-template <typename T> __global__ __launch_bounds__(kThreads) void sum_parts(SumArgs a) {
-    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-    const uint32_t part = (uint32_t)(item / a.columns), begin = part * kMany, total = a.starts[a.V];
+// Parts of rows of many tokens: a wavefront has `part` sorted tokens and a piece of the columns.  Of such rows at most two have tokens among them.
+template <typename T, int P> __global__ __launch_bounds__(kThreads) void sum_parts(SumArgs a) {
+    typedef Unit<T> U;
+    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const uint32_t part = (uint32_t)(item / a.columns), begin = part * a.part, total = a.starts[a.V];
     if (begin >= total) return;
-    const uint32_t end = min(begin + kMany, total);
-    const int64_t c = ((item % a.columns) * 64 + (threadIdx.x & 63)) * Unit<T>::kSize;
+    const uint32_t end = min(begin + a.part, total);
+    const int64_t c = ((item % a.columns) * 64 * P + (threadIdx.x & 63)) * U::kSize;
     const int64_t rows[2] = {a.ids[a.order[begin]], a.ids[a.order[end - 1]]};
     for (int k = 0; k < 2; ++k) {
         if (k && rows[1] == rows[0]) break;
         const uint32_t from = a.starts[rows[k]], to = a.starts[rows[k] + 1];
-        if (to - from <= kMany) continue;
-        float v[Unit<T>::kSize];
-        sum_rows<T>(a, max(from, begin), min(to, end), c, v);
-        // the second place: rows that begin in this part
-        store_some<Unit<float>>(a.parts + ((int64_t)part * 2 + (from > begin)) * a.D, c, a.D, v);
-        if constexpr (sizeof(T) == 2) store_some<Unit<float>>(a.parts + ((int64_t)part * 2 + (from > begin)) * a.D, c + 4, a.D, v + 4);
+        if (to - from <= a.part) continue;
+        Row<T, P> sum;
+        sum.zero();
+        sum.add(a, max(from, begin), min(to, end), c);
+        float* out = a.parts + ((int64_t)part * 2 + (from >= begin)) * a.D;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < U::kSize; i += 4) store_some<Unit<float>>(out, c + p * 64 * U::kSize + i, a.D, sum.v[p] + i);
     }
 }
 
-// The table's gradient: a wavefront has a row and a piece of the columns.
-template <typename T, typename O> __global__ __launch_bounds__(kThreads) void sum_tokens(SumArgs a) {
+// The table's gradient: a wavefront has kRows rows, whose tokens lie one behind the other in the order, and a piece of the columns.
+constexpr int kRows = 4;
+template <typename T, typename O, int P> __global__ __launch_bounds__(kThreads) void sum_tokens(SumArgs a) {
     typedef Unit<T> U;
-    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64, row = item / a.columns;
-    if (row >= a.V) return;
-    const int64_t c = ((item % a.columns) * 64 + (threadIdx.x & 63)) * U::kSize;
-    const uint32_t from = (uint32_t)__builtin_amdgcn_readfirstlane((int)a.starts[row]), to = (uint32_t)__builtin_amdgcn_readfirstlane((int)a.starts[row + 1]);
-    if (a.add && from == to) return;
-    float v[U::kSize];
-    if (to - from <= kMany) {
-        sum_rows<T>(a, from, to, c, v);
-    } else {
+    typedef Some<O, U::kSize> Out;
+    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), row0 = item / a.columns * kRows;
+    if (row0 >= a.V) return;
+    const int64_t c = ((item % a.columns) * 64 * P + (threadIdx.x & 63)) * U::kSize;
+    uint32_t starts[kRows + 1];
 #pragma unroll
-        for (int i = 0; i < U::kSize; ++i) v[i] = 0.0f;
-        for (uint32_t part = from / kMany; part <= (to - 1) / kMany; ++part) {
-            const float* p = a.parts + ((int64_t)part * 2 + (from > part * kMany)) * a.D;
+    for (int r = 0; r <= kRows; ++r) starts[r] = a.starts[row0 + r < a.V ? row0 + r : a.V];
+    for (int r = 0; r < kRows; ++r) {
+        if (row0 + r >= a.V) return;
+        const uint32_t from = starts[r], to = starts[r + 1];
+        if (a.add && from == to) continue;
+        Row<T, P> sum;
+        sum.zero();
+        if (to - from <= a.part) {
+            sum.add(a, from, to, c);
+        } else {
+            const uint32_t first = from / a.part, last = (to - 1) / a.part;
+#pragma unroll 4
+            for (uint32_t part = first; part <= last; ++part) {
+                const float* q = a.parts + ((int64_t)part * 2 + (from >= part * a.part)) * a.D;
 #pragma unroll
-            for (int i = 0; i < U::kSize; i += 4) {
-                const Unit<float> q = load_some<Unit<float>>(p, c + i, a.D);
+                for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[i + k] += q[k];
+                    for (int i = 0; i < U::kSize; i += 4) {
+                        const Unit<float> u = load_some<Unit<float>>(q, c + p * 64 * U::kSize + i, a.D);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sum.v[p][i + k] += u[k];
+                    }
             }
         }
-    }
-    O* out = static_cast<O*>(a.out) + row * a.D;
-    typedef Some<O, U::kSize> Out;
+        O* out = static_cast<O*>(a.out) + (row0 + r) * a.D;
 #pragma unroll
-    for (int i = 0; i < U::kSize; ++i) v[i] *= a.scale;
-    if (a.add) {
-        const Out q = load_some<Out>(out, c, a.D);
+        for (int p = 0; p < P; ++p) {
 #pragma unroll
-        for (int i = 0; i < U::kSize; ++i) v[i] += q[i];
+            for (int i = 0; i < U::kSize; ++i) sum.v[p][i] *= a.scale;
+            if (a.add) {
+                const Out q = load_some<Out>(out, c + p * 64 * U::kSize, a.D);
+#pragma unroll
+                for (int i = 0; i < U::kSize; ++i) sum.v[p][i] += q[i];
+            }
+            store_some<Out>(out, c + p * 64 * U::kSize, a.D, sum.v[p]);
+        }
     }
-    store_some<Out>(out, c, a.D, v);
 }
 
 // ------------------------------------------------------------------ host side
@@ -221,6 +278,12 @@ int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION
 size_t size_of(division_dtype dt) { return dt == DIVISION_BF16 ? 2 : 4; }
 constexpr int64_t kMostWorkgroups = int64_t(1) << 24, kMostTokens = int64_t(1) << 31, kMostElements = int64_t(1) << 40;
 
+// tokens of a part: few enough that one row's keep many wavefronts busy, and no more than 2048 parts, which the row's own adds up one after the other
+uint32_t part_of(int64_t T) {
+    uint32_t n = 32;
+    while (T / n > 2048) n *= 2;
+    return n;
+}
 // the workspace: order, starts, parts
 struct Places { size_t order, starts, parts, bytes; };
 Places places_of(int64_t T, int64_t V, int64_t D) {
@@ -228,7 +291,7 @@ Places places_of(int64_t T, int64_t V, int64_t D) {
     p.order = 0;
     p.starts = (size_t)(T * 4 + 15) / 16 * 16;
     p.parts = p.starts + (size_t)((V + 1) * 4 + 15) / 16 * 16;
-    p.bytes = p.parts + (T > kMany ? (size_t)((T + kMany - 1) / kMany) * 2 * D * 4 : 0);
+    p.bytes = p.parts + (T > part_of(T) ? (size_t)((T + part_of(T) - 1) / part_of(T)) * 2 * D * 4 : 0);
     return p;
 }
 int check_sizes(int64_t T, int64_t V, int64_t D) {
@@ -271,25 +334,29 @@ int division_embedding_backward(const division_embedding_back* back, void* hip_s
     char* ws = static_cast<char*>(b.workspace);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     OrderArgs o{b.ids, reinterpret_cast<uint32_t*>(ws + at.order), reinterpret_cast<uint32_t*>(ws + at.starts), b.V, b.ignore_index, (uint32_t)b.T, 0};
-    // two workgroups a CU at most, a row each at least
-    int64_t rows = (b.V + 511) / 512;
+    int64_t rows = (b.V + 255) / 256;                       // one workgroup a CU: each reads all ids
     if (rows > kMostRows) rows = kMostRows;
     o.rows = (int)rows;
     const int64_t workgroups = (b.V + rows - 1) / rows;
     if (workgroups * kOrderThreads >= (int64_t(1) << 32)) return DIVISION_ERANGE;
-    const int64_t size = 16 / size_of(b.dt), columns = (b.D + 64 * size - 1) / (64 * size);
-    const int64_t parts = ((b.T + kMany - 1) / kMany * columns + 3) / 4, grid = (b.V * columns + 3) / 4;
+    const uint32_t part = part_of(b.T);
+    SumArgs s{b.grad, b.ids, o.order, o.starts, reinterpret_cast<float*>(ws + at.parts), b.grad_table, b.grad_stride, b.V, b.D, (uint32_t)b.T, part, b.scale, b.add, 0};
+    const bool wide = b.D > 64 * (int64_t)(16 / size_of(b.dt));
+    const int64_t each = 64 * (int64_t)(16 / size_of(b.dt)) * (wide ? 2 : 1), columns = (b.D + each - 1) / each;
+    s.columns = (int)columns;
+    const int64_t parts = ((b.T + part - 1) / part * columns + 3) / 4, grid = ((b.V + kRows - 1) / kRows * columns + 3) / 4;
     if (parts >= kMostWorkgroups || grid >= kMostWorkgroups) return DIVISION_ERANGE;
     hipLaunchKernelGGL(order_tokens, dim3((uint32_t)workgroups), dim3(kOrderThreads), (size_t)rows * kOrderWaves * 4, st, o);
     CHECKED(launched());
-    const SumArgs s{b.grad, b.ids, o.order, o.starts, reinterpret_cast<float*>(ws + at.parts), b.grad_table, b.grad_stride, b.V, b.D, (uint32_t)b.T, b.scale, b.add, (int)columns};
-    if (b.T > kMany) {
-        void (*kernel)(SumArgs) = b.dt == DIVISION_BF16 ? sum_parts<uint16_t> : sum_parts<float>;
+    const bool half = b.dt == DIVISION_BF16;
+    void (*kernel)(SumArgs);
+    if (b.T > part) {
+        kernel = half ? (wide ? sum_parts<uint16_t, 2> : sum_parts<uint16_t, 1>) : wide ? sum_parts<float, 2> : sum_parts<float, 1>;
         hipLaunchKernelGGL(kernel, dim3((uint32_t)parts), dim3(kThreads), 0, st, s);
         CHECKED(launched());
     }
-    void (*kernel)(SumArgs) = b.dt == DIVISION_BF16 ? (b.table_dt == DIVISION_BF16 ? sum_tokens<uint16_t, uint16_t> : sum_tokens<uint16_t, float>)
-                              : b.table_dt == DIVISION_BF16 ? sum_tokens<float, uint16_t> : sum_tokens<float, float>;
+    if (b.table_dt == DIVISION_BF16) kernel = half ? (wide ? sum_tokens<uint16_t, uint16_t, 2> : sum_tokens<uint16_t, uint16_t, 1>) : wide ? sum_tokens<float, uint16_t, 2> : sum_tokens<float, uint16_t, 1>;
+    else kernel = half ? (wide ? sum_tokens<uint16_t, float, 2> : sum_tokens<uint16_t, float, 1>) : wide ? sum_tokens<float, float, 2> : sum_tokens<float, float, 1>;
     hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kThreads), 0, st, s);
     return launched();
 }

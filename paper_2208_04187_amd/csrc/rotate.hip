@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Both tensors' heads are numbered through: those of the first, then those of the second.  Strides in elements.
+// Strides in elements.  The first `first` workgroups have the first tensor's heads, the others the second's.
 struct Side { const void *x, *weight, *grad; int64_t token, head, grad_token, grad_head; void* y; float* rstd; const float* rstd_in; int weight_bf16; };
 struct RotateArgs {
     Side side[2];
@@ -21,7 +21,7 @@ struct RotateArgs {
     const int64_t* positions;
     float* parts;
     int64_t T;
-    int heads[2], D, pairs, rotated, block;             // pairs: D / 2, the first `rotated` of them turn; block: tokens a workgroup takes at a time
+    int heads[2], first, D, pairs, rotated, block;      // pairs: D / 2, the first `rotated` of them turn; block: tokens a workgroup takes at a time
     float eps;
 };
 
@@ -96,68 +96,70 @@ __device__ __forceinline__ void angles(const RotateArgs& a, int64_t t0, int n, f
 template <typename T, int V, int U, int LANES, bool NEXT, bool BACK> __global__ __launch_bounds__(kThreads) void rotate(RotateArgs a) {
     typedef Pairs<T, V, NEXT> P;
     extern __shared__ __attribute__((aligned(16))) float2 turned[];
-    const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES, heads = a.heads[0] + a.heads[1];
-    float w[2][U][2 * V], dw[2][U][2 * V];
+    constexpr int kSlots = kThreads / LANES;
+    const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    const bool second = (int)blockIdx.x >= a.first;
+    const Side s = a.side[second ? 1 : 0];
+    const int heads = a.heads[second ? 1 : 0], workgroup = blockIdx.x - (second ? a.first : 0), workgroups = second ? (int)gridDim.x - a.first : a.first;
+    float w[U][2 * V], dw[U][2 * V];
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int u = 0; u < U; ++u) {
+        const int p = (u * LANES + lane) * V;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int p = (u * LANES + lane) * V;
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) w[k][u][i] = dw[k][u][i] = 0.0f;
-            if (p < a.pairs && a.heads[k]) load_weight<V, NEXT>(a.side[k], a, p, w[k][u]);
-        }
-    for (int64_t t0 = (int64_t)blockIdx.x * a.block; t0 < a.T; t0 += (int64_t)gridDim.x * a.block) {
-        const int n = (int)(a.T - t0 < a.block ? a.T - t0 : a.block);
-        __syncthreads();
-        angles(a, t0, n, turned);
-        __syncthreads();
+        for (int i = 0; i < 2 * V; ++i) w[u][i] = dw[u][i] = 0.0f;
+        if (p < a.pairs) load_weight<V, NEXT>(s, a, p, w[u]);
+    }
+    const float over = 1.0f / (float)a.D;
+    for (int64_t t0 = (int64_t)workgroup * a.block; t0 < a.T; t0 += (int64_t)workgroups * a.block) {
+        const int n = (int)(a.T - t0 < a.block ? a.T - t0 : a.block), items = n * heads;
         // every lane goes round as often: the sums over lanes take all of them
-        const int rounds = (n * heads + kThreads / LANES - 1) / (kThreads / LANES);
-        for (int k = 0; k < rounds; ++k) {
-            const int e = k * (kThreads / LANES) + slot;
-            const bool there = e < n * heads;
-            const int t = there ? e / heads : 0, h = there ? e - t * heads : 0;
-            const bool second = h >= a.heads[0];
-            const Side& s = a.side[second ? 1 : 0];
-            const int head = second ? h - a.heads[0] : h;
-            const int64_t at = (t0 + t) * a.heads[second ? 1 : 0] + head;
-            const T* row = static_cast<const T*>(s.x) + (t0 + t) * s.token + (int64_t)head * s.head;
-            float x[U][2 * V], g[U][2 * V];
-            float sum = 0.0f;
+        const int rounds = (items + kSlots - 1) / kSlots;
+        float x[U][2 * V], g[U][2 * V], rstd = 0.0f;
+        const auto load = [&](int e) {
+            const int t = e / heads, h = e - t * heads;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int p = (u * LANES + lane) * V;
 #pragma unroll
                 for (int i = 0; i < 2 * V; ++i) x[u][i] = g[u][i] = 0.0f;
-                if (there && p < a.pairs) {
-                    P::load(row, a, p, x[u]);
-                    if constexpr (BACK) P::load(static_cast<const T*>(s.grad) + (t0 + t) * s.grad_token + (int64_t)head * s.grad_head, a, p, g[u]);
+                if (e < items && p < a.pairs) {
+                    P::load(static_cast<const T*>(s.x) + (t0 + t) * s.token + (int64_t)h * s.head, a, p, x[u]);
+                    if constexpr (BACK) P::load(static_cast<const T*>(s.grad) + (t0 + t) * s.grad_token + (int64_t)h * s.grad_head, a, p, g[u]);
                 }
             }
-            float rstd = 0.0f;
-            if constexpr (BACK) rstd = there ? s.rstd_in[at] : 0.0f;
+            if constexpr (BACK) rstd = e < items ? s.rstd_in[t0 * heads + e] : 0.0f;
+        };
+        load(slot);                                         // on its way while the angles are taken
+        __syncthreads();
+        angles(a, t0, n, turned);
+        __syncthreads();
+        for (int k = 0; k < rounds; ++k) {
+            const int e = k * kSlots + slot, t = e / heads;
+            if (k) load(e);
+            float sum = 0.0f;
+            float2 cs[U][V];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int p = (u * LANES + lane) * V;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    if constexpr (BACK) {
-                        // turned back
-                        float2 cs = make_float2(1.0f, 0.0f);
-                        if (p + i < a.rotated) cs = turned[t * a.rotated + p + i];
+                    cs[u][i] = make_float2(1.0f, 0.0f);
+                    if (e < items && p + i < a.rotated) cs[u][i] = turned[t * a.rotated + p + i];
+                }
+                if constexpr (BACK) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {           // turned back
                         const float ga = g[u][i], gb = g[u][V + i];
-                        g[u][i] = __builtin_fmaf(ga, cs.x, gb * cs.y);
-                        g[u][V + i] = __builtin_fmaf(gb, cs.x, -(ga * cs.y));
+                        g[u][i] = __builtin_fmaf(ga, cs[u][i].x, gb * cs[u][i].y);
+                        g[u][V + i] = __builtin_fmaf(gb, cs[u][i].x, -(ga * cs[u][i].y));
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < 2 * V; ++i) {
                     if constexpr (BACK) {
                         x[u][i] *= rstd;
-                        const float share = g[u][i] * x[u][i];
-                        if (second) dw[1][u][i] += share; else dw[0][u][i] += share;
-                        g[u][i] *= second ? w[1][u][i] : w[0][u][i];
+                        dw[u][i] = __builtin_fmaf(g[u][i], x[u][i], dw[u][i]);
+                        g[u][i] *= w[u][i];
                         sum = __builtin_fmaf(g[u][i], x[u][i], sum);
                     } else {
                         sum = __builtin_fmaf(x[u][i], x[u][i], sum);
@@ -165,11 +167,11 @@ template <typename T, int V, int U, int LANES, bool NEXT, bool BACK> __global__ 
                 }
             }
             sum = sum_lanes<LANES>(sum);
-            if constexpr (BACK) sum /= (float)a.D;
+            if constexpr (BACK) sum *= over;
             else rstd = 1.0f / sqrtf(sum / (float)a.D + a.eps);
-            if (!there) continue;
-            if (!BACK && lane == 0 && s.rstd) s.rstd[at] = rstd;
-            T* out = static_cast<T*>(s.y) + at * a.D;
+            if (e >= items) continue;
+            if (!BACK && lane == 0 && s.rstd) s.rstd[t0 * heads + e] = rstd;
+            T* out = static_cast<T*>(s.y) + (t0 * heads + e) * a.D;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int p = (u * LANES + lane) * V;
@@ -178,16 +180,14 @@ template <typename T, int V, int U, int LANES, bool NEXT, bool BACK> __global__ 
 #pragma unroll
                 for (int i = 0; i < 2 * V; ++i) {
                     if constexpr (BACK) y[i] = rstd * __builtin_fmaf(-x[u][i], sum, g[u][i]);
-                    else y[i] = x[u][i] * rstd * (second ? w[1][u][i] : w[0][u][i]);
+                    else y[i] = x[u][i] * rstd * w[u][i];
                 }
                 if constexpr (!BACK) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        float2 cs = make_float2(1.0f, 0.0f);
-                        if (p + i < a.rotated) cs = turned[t * a.rotated + p + i];
                         const float ya = y[i], yb = y[V + i];
-                        y[i] = __builtin_fmaf(ya, cs.x, -(yb * cs.y));
-                        y[V + i] = __builtin_fmaf(ya, cs.y, yb * cs.x);
+                        y[i] = __builtin_fmaf(ya, cs[u][i].x, -(yb * cs[u][i].y));
+                        y[V + i] = __builtin_fmaf(ya, cs[u][i].y, yb * cs[u][i].x);
                     }
                 }
                 P::store(out, a, p, y);
@@ -195,60 +195,53 @@ template <typename T, int V, int U, int LANES, bool NEXT, bool BACK> __global__ 
         }
     }
     if constexpr (BACK) {
-        // the workgroup's share of the weights' gradients: slots one after the other
-        float* sums = reinterpret_cast<float*>(turned);         // [2][D]
+        // the workgroup's share of the weight's gradient: lanes of a wavefront that have the same columns, then wavefront by wavefront
+        float* sums = reinterpret_cast<float*>(turned);     // [D]
         __syncthreads();
-        for (int e = threadIdx.x; e < 2 * a.D; e += kThreads) sums[e] = 0.0f;
-        // within a wavefront by lanes, then wavefront by wavefront
+        for (int e = threadIdx.x; e < a.D; e += kThreads) sums[e] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int i = 0; i < 2 * V; ++i)
 #pragma unroll
-                for (int i = 0; i < 2 * V; ++i)
-#pragma unroll
-                    for (int o = LANES; o < 64; o <<= 1) dw[k][u][i] += __shfl_xor(dw[k][u][i], o, 64);
+                for (int o = LANES; o < 64; o <<= 1) dw[u][i] += __shfl_xor(dw[u][i], o, 64);
         for (int wave = 0; wave < kThreads / 64; ++wave) {
             __syncthreads();
             if ((int)(threadIdx.x >> 6) != wave || (threadIdx.x & 63) >= LANES) continue;
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int u = 0; u < U; ++u) {
+                const int p = (u * LANES + lane) * V;
+                if (p >= a.pairs) continue;
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int p = (u * LANES + lane) * V;
-                    if (p >= a.pairs) continue;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const int c = NEXT ? 2 * (p + i) : P::first(a, p) + i, d = NEXT ? c + 1 : c + P::second(a, p);
-                        sums[k * a.D + c] += dw[k][u][i];
-                        sums[k * a.D + d] += dw[k][u][V + i];
-                    }
+                for (int i = 0; i < V; ++i) {
+                    const int c = NEXT ? 2 * (p + i) : P::first(a, p) + i, d = NEXT ? c + 1 : c + P::second(a, p);
+                    sums[c] += dw[u][i];
+                    sums[d] += dw[u][V + i];
                 }
+            }
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < 2 * a.D; e += kThreads) a.parts[(int64_t)blockIdx.x * 2 * a.D + e] = sums[e];
+        for (int e = threadIdx.x; e < a.D; e += kThreads) a.parts[(int64_t)blockIdx.x * a.D + e] = sums[e];
     }
 }
 
 // The weights' gradients from the workgroups' shares, in a fixed order: 32 columns a workgroup, 32 threads a column
-struct AddArgs { const float* parts; void* out[2]; int bf16[2]; int count, D; };
+struct AddArgs { const float* parts; void* out[2]; int bf16[2]; int first[2], count[2], D, blocks; };
 __global__ __launch_bounds__(1024) void add_weight_parts(AddArgs a) {
     __shared__ float sums[32][33];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
+    const int k = (int)blockIdx.x >= a.blocks, c = ((int)blockIdx.x - k * a.blocks) * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
     float s = 0.0f;
-    if (c < 2 * a.D) {
+    if (c < a.D) {
 #pragma unroll 8
-        for (int r = row; r < a.count; r += 32) s += a.parts[(int64_t)r * 2 * a.D + c];
+        for (int r = row; r < a.count[k]; r += 32) s += a.parts[(int64_t)(a.first[k] + r) * a.D + c];
     }
     sums[row][threadIdx.x & 31] = s;
     __syncthreads();
-    if (row || c >= 2 * a.D) return;
+    if (row || c >= a.D) return;
     s = 0.0f;
     for (int r = 0; r < 32; ++r) s += sums[r][threadIdx.x];
-    const int k = c >= a.D, d = c - k * a.D;
-    if (!a.out[k]) return;
-    if (a.bf16[k]) static_cast<uint16_t*>(a.out[k])[d] = bf16_of(s);
-    else static_cast<float*>(a.out[k])[d] = s;
+    if (a.bf16[k]) static_cast<uint16_t*>(a.out[k])[c] = bf16_of(s);
+    else static_cast<float*>(a.out[k])[c] = s;
 }
 
 // ------------------------------------------------------------------ host side
@@ -259,12 +252,18 @@ int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION
 #define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
 size_t size_of(division_dtype dt) { return dt == DIVISION_BF16 ? 2 : 4; }
 
-constexpr int kMostParts = 1024;                            // workgroups of a backward launch, which leave a share each
+constexpr int kMostParts = 1024;                            // workgroups of a backward launch for each tensor, which leave a share each
 int block_of(int64_t T) { return T >= 4096 ? 4 : 1; }
-int64_t grid_of(int64_t T, bool back) {
+// workgroups of a tensor of so many heads, of the other's `most`: forward as many as there are blocks of tokens, backward as the shares of the weight's gradient allow
+int grid_of(int64_t T, int64_t heads, int64_t most_heads, bool back) {
+    if (T == 0 || heads == 0) return 0;
     const int64_t n = (T + block_of(T) - 1) / block_of(T);
-    const int64_t most = back ? kMostParts : 1 << 20;
-    return n > most ? most : n;
+    int64_t most = back ? kMostParts : 1 << 20;
+    if (back) {                                             // as many for each head
+        most = most * heads / most_heads;
+        if (most < 64) most = 64;
+    }
+    return (int)(n > most ? most : n);
 }
 
 // the tensors' own sizes; `back`: the gradients', which the forward pass has none of
@@ -312,15 +311,17 @@ RotateArgs args_of(const division_rotate& a) {
 
 template <typename T, int V, int U, int LANES, bool BACK> int launch(const RotateArgs& a, bool next, uint32_t grid, hipStream_t st) {
     size_t lds = (size_t)a.block * a.rotated * sizeof(float2);
-    if (BACK && lds < 2 * (size_t)a.D * 4) lds = 2 * (size_t)a.D * 4;
+    if (BACK && lds < (size_t)a.D * 4) lds = (size_t)a.D * 4;
     if (next) hipLaunchKernelGGL((rotate<T, V, U, LANES, true, BACK>), dim3(grid), dim3(kThreads), lds, st, a);
     else hipLaunchKernelGGL((rotate<T, V, U, LANES, false, BACK>), dim3(grid), dim3(kThreads), lds, st, a);
     return launched();
 }
 // Heads whose pairs are whole vectors of sixteen bytes; others element by element
-template <typename T, bool BACK> int run(const RotateArgs& a, bool next, hipStream_t st) {
+template <typename T, bool BACK> int run(RotateArgs& a, bool next, hipStream_t st) {
     constexpr int V = 16 / (int)sizeof(T);
-    const uint32_t grid = (uint32_t)grid_of(a.T, BACK);
+    const int most = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
+    a.first = grid_of(a.T, a.heads[0], most, BACK);
+    const uint32_t grid = (uint32_t)(a.first + grid_of(a.T, a.heads[1], most, BACK));
     if (a.pairs % V || (!next && a.rotated % V)) return a.pairs <= 64 ? launch<T, 1, 4, 16, BACK>(a, next, grid, st) : launch<T, 1, 4, 64, BACK>(a, next, grid, st);
     const int units = a.pairs / V;
     if (units <= 4) return launch<T, V, 1, 4, BACK>(a, next, grid, st);
@@ -339,13 +340,13 @@ int division_head_norm_rotate(const division_rotate* rotate, void* hip_stream) {
     if (!rotate) return DIVISION_EINVAL;
     CHECKED(check(*rotate, nullptr));
     if (rotate->T == 0) return DIVISION_OK;
-    const RotateArgs a = args_of(*rotate);
+    RotateArgs a = args_of(*rotate);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return rotate->dt == DIVISION_BF16 ? run<uint16_t, false>(a, rotate->next, st) : run<float, false>(a, rotate->next, st);
 }
 
 size_t division_head_norm_rotate_backward_workspace(int64_t T, int64_t D) {
-    return T <= 0 || T > 0x7fffffff || D < 2 || D > 512 ? 0 : (size_t)grid_of(T, true) * 2 * D * 4;
+    return T <= 0 || T > 0x7fffffff || D < 2 || D > 512 ? 0 : (size_t)grid_of(T, 1, 1, true) * 2 * D * 4;
 }
 
 int division_head_norm_rotate_backward(const division_rotate* rotate, const division_rotate_back* back, void* hip_stream) {
@@ -372,11 +373,14 @@ int division_head_norm_rotate_backward(const division_rotate* rotate, const divi
         a.parts = static_cast<float*>(back->workspace);
         CHECKED((f.dt == DIVISION_BF16 ? run<uint16_t, true>(a, f.next, st) : run<float, true>(a, f.next, st)));
         add.parts = a.parts;
-        add.count = (int)grid_of(f.T, true);
+        const int most = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
+        add.count[0] = add.first[1] = a.first;
+        add.count[1] = grid_of(f.T, a.heads[1], most, true);
     }
     add.D = (int)f.D;
-    for (int k = 0; k < 2; ++k) { add.out[k] = f.heads[k] ? back->grad_weight[k] : nullptr; add.bf16[k] = f.weight_dt[k] == DIVISION_BF16; }
-    hipLaunchKernelGGL(add_weight_parts, dim3((uint32_t)((2 * f.D + 31) / 32)), dim3(1024), 0, st, add);
+    add.blocks = (int)((f.D + 31) / 32);
+    for (int k = 0; k < 2; ++k) { add.out[k] = back->grad_weight[k]; add.bf16[k] = f.weight_dt[k] == DIVISION_BF16; }
+    hipLaunchKernelGGL(add_weight_parts, dim3((uint32_t)(add.blocks * (f.heads[1] ? 2 : 1))), dim3(1024), 0, st, add);
     return launched();
 }
 

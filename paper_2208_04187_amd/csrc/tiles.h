@@ -44,42 +44,53 @@ __device__ __forceinline__ void product(f32x16& c, const Operand<float>& a, cons
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
 }
 
-// Rows of DP elements in the local memory, in pieces of 16 bytes.  A piece's place in its row is exchanged with the row's number, so that neither
-// sixteen rows at one column nor four rows at four neighbouring columns (eight in fp32) share banks.
-template <typename T, int DP> struct Tile {
-    static constexpr int kRowBytes = DP * (int)sizeof(T), kPieces = kRowBytes / 16;
-    static __device__ __forceinline__ int turn(int row) {
-        if constexpr (sizeof(T) == 4) return (row >> 2 & 1) << 3 | (row & 3) << 1 | (row >> 3 & 1);
-        else if constexpr (kPieces == 16) return (row & 3) << 2 | (row >> 2 & 3);
-        else return (row >> 1 & 1) << 2 | (row >> 2 & 3);
-    }
-    static __device__ __forceinline__ int place(int row, int piece) { return row * kRowBytes + ((piece ^ turn(row)) << 4); }
+// Loads into the local memory: 64 lanes' sixteen (four) bytes of a buffer, each from an offset of its own, one behind the other from `to` on; beyond the buffer's bytes zeros.  In assembly, since
+// the compiler has every later read of the local memory wait for its builtin's, which leaves nothing of fetching ahead (backward pass of 2 x 4096 tokens, 32 heads: 937 us, BACK_US so).  No register
+// is written: the loads count for loads_done() alone.
+__device__ __forceinline__ u32x4 buffer(const void* base, uint32_t bytes) {
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    return {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xffffu)), bytes, 0x00020000u};
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)LDS_AT(const void, p)); }
+__device__ __forceinline__ void load_lds16(u32x4 from, const void* to, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_address(to)), "v"(offset), "s"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void load_lds4(u32x4 from, const void* to, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds_address(to)), "v"(offset), "s"(from) : "memory", "m0");
+}
 
-    // rows 0 .. ROWS - 1 from global memory by THREADS threads, without a register between: those from `rows` on and pieces behind the row's bytes are zeros.  at(row): a row's
-    // offset from base, below 2^31 - 16.  The data are there when the wavefront has waited for its loads.
-    template <int ROWS, int THREADS, typename At> static __device__ __forceinline__ void fill(char* tile, const char* base, int rows, int row_bytes, int thread, At&& at) {
-        constexpr int kEach = ROWS * kPieces / THREADS;
-        static_assert(kEach * THREADS == ROWS * kPieces, "whole pieces a thread");
-        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, 0x7fffffff, 0x00020000);
+// ROWS rows of DP elements in the local memory: strips of 64 bytes of all rows, one strip behind the other, a row's four pieces of 16 bytes exchanged with bits 2 and 3 of its number.  Sixteen
+// rows at one column then touch all banks, as four rows at 64 bytes do; and a lane's places are two numbers, whatever the strip and the sixteen rows, to which the instructions
+// themselves add the rest (with whole rows behind one another, exchanged over sixteen pieces, the places took 40 registers).
+template <typename T, int DP, int ROWS> struct Tile {
+    static constexpr int kRowBytes = DP * (int)sizeof(T), kStrip = ROWS * 64, kBytes = ROWS * kRowBytes;
+    static __device__ __forceinline__ int turn(int row) { return row >> 2 & 3; }
+
+    // the rows from global memory by THREADS threads, without a register between: those from `rows` on and pieces behind the row's bytes are zeros.  at(row): a row's
+    // offset from base, below 2^31 - 512.  The data are there when the wavefront has waited for its loads.
+    template <int THREADS, typename At> static __device__ __forceinline__ void fill(char* tile, const char* base, int rows, int row_bytes, int thread, At&& at) {
+        constexpr int kEach = kBytes / 16 / THREADS;
+        static_assert(kEach * THREADS * 16 == kBytes && (THREADS * 16) % 64 == 0, "whole pieces a thread");
+        const u32x4 from = buffer(base, 0x7fffffffu);
         const int first = __builtin_amdgcn_readfirstlane(thread & ~63);
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
-            const int slot = u * THREADS + thread, row = slot / kPieces, piece = (slot % kPieces) ^ turn(row);
+            const int slot = u * THREADS + thread, row = slot / 4 % ROWS, piece = slot / (4 * ROWS) * 4 + ((slot & 3) ^ turn(row));
             // an offset beyond the buffer reads zeros
             const uint32_t off = row < rows && piece * 16 < row_bytes ? (uint32_t)(at(row) + piece * 16) : 0x80000000u;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, LDS_AT(void, tile + (u * THREADS + first) * 16), 16, (int)off, 0, 0, 0);
+            load_lds16(from, tile + (u * THREADS + first) * 16, off);
         }
     }
 
-    // operand of rows row0 + l % 32: inner indices 16 step .. of the rows' elements
+    // operand of rows row0 + l % 32 (row0 a multiple of 16): inner indices 16 step .. of the rows' elements
     static __device__ __forceinline__ Operand<T> rows(const char* tile, int row0, int step, int lane) {
-        const int row = row0 + (lane & 31), half = lane >> 5;
+        const int half = lane >> 5, at = (lane & 31) * 64, t = turn(lane & 31);
         if constexpr (sizeof(T) == 2) {
-            return Operand<T>::at(tile + place(row, 2 * step + half));
+            return Operand<T>::at(tile + row0 * 64 + step / 2 * kStrip + at + (((2 * (step & 1) + half) ^ t) << 4));
         } else {
             Operand<T> o;
-            o.lo = *reinterpret_cast<const f32x4*>(tile + place(row, 4 * step + 2 * half));
-            o.hi = *reinterpret_cast<const f32x4*>(tile + place(row, 4 * step + 2 * half + 1));
+            o.lo = *reinterpret_cast<const f32x4*>(tile + row0 * 64 + step * kStrip + at + (((2 * half) ^ t) << 4));
+            o.hi = *reinterpret_cast<const f32x4*>(tile + row0 * 64 + step * kStrip + at + (((2 * half + 1) ^ t) << 4));
             return o;
         }
     }
@@ -88,23 +99,36 @@ template <typename T, int DP> struct Tile {
         const int half = lane >> 5;
         if constexpr (sizeof(T) == 2) {
             // four rows of sixteen lanes' four columns each come back as a lane's column of four rows
-            const int i = lane & 15, row = row0 + 4 * half + (i >> 2), col = col0 + (lane & 16) + (i & 3) * 4;
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_AT(s16x4, tile + place(row, col >> 3) + (col & 4) * 2));
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_AT(s16x4, tile + place(row + 8, col >> 3) + (col & 4) * 2));
+            const int i = lane & 15, piece = (lane & 16) / 8 + (i & 3) / 2;
+            const char* row = tile + row0 * 64 + col0 / 32 * kStrip + (4 * half + (i >> 2)) * 64 + (i & 1) * 8;
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_AT(s16x4, row + ((piece ^ half) << 4)));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_AT(s16x4, row + 512 + ((piece ^ half ^ 2) << 4)));
             const u32x2 p = __builtin_bit_cast(u32x2, a), q = __builtin_bit_cast(u32x2, b);
             return {__builtin_bit_cast(bf16x8, (u32x4{p.x, p.y, q.x, q.y}))};
         } else {
             float v[8];
-            const int col = col0 + (lane & 31);
+            const int i = lane & 15;
+            const char* row = tile + row0 * 64 + (col0 / 16 + (lane >> 4 & 1)) * kStrip + 4 * half * 64 + (i & 3) * 4;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float*>(tile + place(row0 + 8 * (j / 4) + 4 * half + j % 4, col >> 2) + (col & 3) * 4);
+            for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float*>(row + (8 * (j / 4) + j % 4) * 64 + (((i >> 2) ^ half ^ (2 * (j / 4))) << 4));
             return Operand<T>::of(v);
         }
     }
 };
 
-// all but the last LEFT loads that the wavefront has begun are there
-template <int LEFT = 0> __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
+// all but the last LEFT loads that the wavefront has begun are there.  (The builtin: the compiler sees that its own loads before a loop need no wait within it.)
+template <int LEFT = 0> __device__ __forceinline__ void loads_done() {
+    if constexpr (LEFT == 0) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        asm volatile("" ::: "memory");
+    } else {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+    }
+}
+
+// of a number that everything in a branch depends on: what few tiles need stays there.  Without it the compiler does that for all tiles and selects (a border costs a hundred vector
+// instructions a tile).
+template <typename V> __device__ __forceinline__ void stay_a_branch(V& v) { asm volatile("" : "+v"(v)); }
 
 // over the two halves that share a column, for both
 __device__ __forceinline__ float halves_sum(float v) {
