@@ -29,6 +29,9 @@ _lib = None
 OPERATOR_ENTRIES = []
 OPERATOR_OTHERS = []
 OPERATOR_DESCS = []
+# ... of those in layer_operators.py
+LAYER_ENTRIES = []
+LAYER_DESCS = []
 
 
 class DivisionError(RuntimeError):
@@ -93,7 +96,7 @@ def lib() -> ctypes.CDLL:
         L.division_decompress_3d.argtypes = [vp, sz, i64, i64, i64, i64, i64, ci, ci, ci, vp, vp]
         L.division_kernel_name_3d.restype = ci
         L.division_kernel_name_3d.argtypes = [ci, vp, i64, i64, i64, i64, i64, ci, ci, ci, ctypes.c_char_p, sz]
-        for name, arguments, result in OPERATOR_ENTRIES + OPERATOR_OTHERS:
+        for name, arguments, result in OPERATOR_ENTRIES + OPERATOR_OTHERS + LAYER_ENTRIES:
             entry = getattr(L, name)
             entry.argtypes, entry.restype = arguments, result
         _lib = L
@@ -132,6 +135,7 @@ def _load_fast():
             module = importlib.import_module("._fastcall", __package__)
             module.bind([ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _FAST_ENTRIES], L.division_abi_version(), ctypes.sizeof(_MapDesc))
             module.bind_operators([ctypes.cast(getattr(L, entry[0]), ctypes.c_void_p).value for entry in OPERATOR_ENTRIES], [ctypes.sizeof(d) for d in OPERATOR_DESCS])
+            module.bind_layers([ctypes.cast(getattr(L, entry[0]), ctypes.c_void_p).value for entry in LAYER_ENTRIES], [ctypes.sizeof(d) for d in LAYER_DESCS])
         except (ImportError, ValueError, TypeError, RuntimeError, OSError) as err:
             warnings.warn(f"the native side of the binding is not used, small calls take twice as long on the host: {err}", RuntimeWarning, stacklevel=3)
             module = _NothingFast()

@@ -35,7 +35,7 @@ template <typename T, int DP> struct Columns {
     }
 
     // KT keys of the tiles, the first of them key `first`; from .. to - 1 are the keys that this lane's column sees, all of these where `whole`
-    template <int KT> __device__ __forceinline__ void add(const char* kt, const char* vt, int first, int from, int to, bool whole, float scale2, int lane) {
+    template <typename Keys, int KT> __device__ __forceinline__ void add(const char* kt, const char* vt, int first, int from, int to, bool whole, float scale2, int lane) {
         const int half = lane >> 5;
         f32x16 z[KT / 32];
 #pragma unroll
@@ -43,7 +43,7 @@ template <typename T, int DP> struct Columns {
 #pragma unroll
         for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
-            for (int b = 0; b < KT / 32; ++b) product(z[b], Tile<T, DP, KT>::rows(kt, 32 * b, s, lane), q[s]);
+            for (int b = 0; b < KT / 32; ++b) product(z[b], Keys::rows(kt, 32 * b, s, lane), q[s]);
         if (!whole) {
             uint32_t n = (uint32_t)(to - from);
             stay_a_branch(n);
@@ -85,14 +85,19 @@ template <typename T, int DP> struct Columns {
                 for (int j = 0; j < 8; ++j) w[j] = z[b][8 * c + j];
                 const Operand<T> p = Operand<T>::of(w);
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) product(o[d], Tile<T, DP, KT>::columns(vt, 32 * b + 16 * c, 32 * d, lane), p);
+                for (int d = 0; d < DP / 32; ++d) product(o[d], Keys::columns(vt, 32 * b + 16 * c, 32 * d, lane), p);
             }
         }
     }
 };
 
-// A workgroup's tasks: which columns of which key head, which part of the keys
-struct Task { int group, block, split; };
+// The workgroup's part of the tiles lo .. hi - 1 that its columns see: equal parts of these, not of all keys, or the long sequences of a batch would leave most of their parts' workgroups without work
+// (32 tokens over caches of up to 8192 keys: PARTS_US)
+__device__ __forceinline__ void part_of(const AttentionArgs& a, int split, int& lo, int& hi) {
+    const int each = max((hi - lo + a.splits - 1) / a.splits, a.tiles), begin = lo + split * each;
+    hi = min(begin + each, hi);
+    lo = begin;
+}
 
 template <typename T> __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
     if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
@@ -106,8 +111,7 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     constexpr int kTile = Tile<T, DP, KT>::kBytes;
     __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile];
     const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
-    const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
-    const int group = rest % a.groups, block = a.blocks - 1 - rest / a.groups;
+    const int group = blockIdx.x % a.groups, split = blockIdx.x / a.groups % a.splits, block = a.blocks - 1 - blockIdx.x / a.groups / a.splits;
     const int b = group / a.G, g = group % a.G;
     const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * 128u;
     const uint32_t wave_col = first_col + 32 * wave, col = wave_col + (lane & 31);
@@ -115,8 +119,7 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     // the keys of the workgroup, of the wavefront and of the lane
     const uint32_t last_col = min(first_col + 127u, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
     int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
-    lo = max(lo, split * a.tiles);
-    hi = min(hi, (split + 1) * a.tiles);
+    part_of(a, split, lo, hi);
     const bool works = wave_col < cols;
     const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
     const int wave_from = seen.from(qa), whole_from = seen.from(qb), whole_to = seen.to(qa), wave_to = works ? seen.to(qb) : 0;
@@ -139,7 +142,7 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     for (int t = lo; t < hi; ++t) {
         if (t + 1 < hi) fetch(t + 1);
         const int j = t * KT;
-        c.template add<KT>(tiles[t & 1][0], tiles[t & 1][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
+        c.template add<Tile<T, DP, KT>, KT>(tiles[t & 1][0], tiles[t & 1][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
         loads_done();
         __syncthreads();
     }
@@ -175,19 +178,20 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
 
 // Few columns: WK wavefronts have the same 32 columns and every WK-th tile of the keys each, in tiles of their own, and are joined at the end.
 template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * WK) void attend_few(AttentionArgs a) {
-    constexpr int kTile = Tile<T, DP, KT>::kBytes, kLoads = 2 * kTile / 1024, kRow = DP + 4;
+    typedef RowTile<T, DP, KT> Keys;
+    constexpr int kTile = Keys::kBytes, kLoads = 2 * kTile / 1024, kRow = DP + 4;
     static_assert(32 * kRow * 4 <= 4 * kTile, "a wavefront's values in place of its tiles");
     __shared__ __attribute__((aligned(16))) char tiles[WK][2][2][kTile];
     __shared__ float most[WK][32], totals[WK][32];
     const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
-    const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
-    const int group = rest % a.groups, block = a.blocks - 1 - rest / a.groups;
+    const int group = blockIdx.x % a.groups, split = blockIdx.x / a.groups % a.splits, block = a.blocks - 1 - blockIdx.x / a.groups / a.splits;
     const int b = group / a.G, g = group % a.G;
     const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * 32u, col = first_col + (lane & 31);
     const Seen seen = seen_of(a, b);
     const int qa = (int)(first_col / (uint32_t)a.R), qb = (int)(min(first_col + 31u, cols - 1) / (uint32_t)a.R);
     const int whole_from = seen.from(qb), whole_to = seen.to(qa);
-    const int lo = max(seen.from(qa) / KT, split * a.tiles), hi = min((seen.to(qb) + KT - 1) / KT, (split + 1) * a.tiles);
+    int lo = seen.from(qa) / KT, hi = (seen.to(qb) + KT - 1) / KT;
+    part_of(a, split, lo, hi);
     const int i = (int)(min(col, cols - 1) / (uint32_t)a.R);
     const int from = seen.from(i), to = col < cols ? max(from, seen.to(i)) : from;
     const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
@@ -195,8 +199,8 @@ template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * 
     const int row_bytes = a.D * (int)sizeof(T);
     const auto fetch = [&](int t, int at) {
         const int left = seen.keys - t * KT;
-        Tile<T, DP, KT>::template fill<64>(tiles[wave][at][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
-        Tile<T, DP, KT>::template fill<64>(tiles[wave][at][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
+        Keys::template fill<64>(tiles[wave][at][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
+        Keys::template fill<64>(tiles[wave][at][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
     };
     Columns<T, DP> c;
     c.begin(a, a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head, col, cols, half);
@@ -210,7 +214,7 @@ template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * 
             loads_done();
         }
         const int j = t * KT;
-        c.template add<KT>(tiles[wave][at][0], tiles[wave][at][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
+        c.template add<Keys, KT>(tiles[wave][at][0], tiles[wave][at][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
     }
     const float total = halves_sum(c.total);
     if (half == 0) { most[wave][lane] = c.most; totals[wave][lane] = total; }
@@ -297,14 +301,13 @@ Cut cut_of(const division_attention& a) {
     c.blocks = (cols + (c.few ? 31 : 127)) / (c.few ? 32 : 128);
     c.key_tile = c.few ? 32 : 64;
     const int64_t tiles = (a.Sk + c.key_tile - 1) / c.key_tile, tasks = c.blocks * a.B * a.G;
-    const int64_t least = c.few ? (a.dt == DIVISION_BF16 ? 4 : 2) : 4, room = tiles / least, wanted = c.few ? 1024 : 512;
-    int64_t splits = tasks >= (c.few ? 1024 : 256) ? 1 : (wanted + tasks - 1) / tasks;
+    const int64_t least = c.few ? (a.dt == DIVISION_BF16 ? 4 : 2) : 4, room = tiles / least, wanted = 512;
+    int64_t splits = tasks >= (c.few ? 512 : 256) ? 1 : (wanted + tasks - 1) / tasks;
     if (splits > room) splits = room;
     if (splits > 64) splits = 64;
     if (splits < 1) splits = 1;
-    c.tiles = (int)((tiles + splits - 1) / splits);
-    if (c.tiles < 1) c.tiles = 1;
-    c.splits = tiles ? (int)((tiles + c.tiles - 1) / c.tiles) : 1;
+    c.tiles = (int)least;
+    c.splits = (int)splits;
     return c;
 }
 size_t parts_bytes(const division_attention& a, const Cut& c) { return c.splits > 1 ? (size_t)c.splits * a.B * a.Sq * a.H * (a.D + 1) * 4 : 0; }

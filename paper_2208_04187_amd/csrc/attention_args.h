@@ -10,7 +10,7 @@ struct AttentionArgs {
     float *lse, *parts;
     int64_t window;
     int Sq, Sk, H, G, R, D, causal, groups;             // groups: B * G
-    int blocks, splits, tiles;                          // of columns; of keys, and how many tiles each has
+    int blocks, splits, tiles;                          // of columns; parts of the keys, and how many tiles one has at least
     float scale;
 };
 __device__ __forceinline__ int64_t row_offset(const Heads& s, int64_t token, int head) { return token * s.token + (int64_t)head * s.head; }

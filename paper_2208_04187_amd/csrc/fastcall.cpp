@@ -11,6 +11,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <cmath>
 #include <vector>
 #include "../../include/division.h"
 
@@ -39,6 +40,18 @@ decltype(&division_log_probs_low) log_probs;
 decltype(&division_log_probs_backward_low) log_probs_backward;
 decltype(&division_grad_norm_workspace) grad_norm_workspace;
 decltype(&division_clip_grads) clip_grads;
+// ... of the operators of a token model's layers; null until bind_layers()
+decltype(&division_attention_workspace) attention_workspace;
+decltype(&division_attend) attend;
+decltype(&division_attention_backward_workspace) attention_backward_workspace;
+decltype(&division_attention_backward) attention_backward;
+decltype(&division_head_norm_rotate) head_norm_rotate;
+decltype(&division_head_norm_rotate_backward_workspace) head_norm_rotate_backward_workspace;
+decltype(&division_head_norm_rotate_backward) head_norm_rotate_backward;
+decltype(&division_embedding) embedding;
+decltype(&division_embedding_backward_workspace) embedding_backward_workspace;
+decltype(&division_embedding_backward) embedding_backward;
+decltype(&division_dropout_add) dropout_add;
 
 // A mode of torch that replaces or watches calls sees those of binding.py
 bool plain_state() { return !c10::impl::TorchDispatchModeTLS::any_modes_set() && !at::impl::torch_function_mode_enabled(); }
@@ -666,27 +679,299 @@ PyObject* py_clip_grads(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind_operators(addresses, sizes): their entries in the order of the table, and the sizes of their descriptors
-PyObject* py_bind_operators(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
-    void** at[] = {(void**)&rms_norm, (void**)&read_codes, (void**)&rms_norm_backward_workspace, (void**)&rms_norm_backward, (void**)&log_probs_workspace,
-                   (void**)&log_probs, (void**)&log_probs_backward, (void**)&grad_norm_workspace, (void**)&clip_grads};
-    const size_t sizes[] = {sizeof(division_norm), sizeof(division_norm_back), sizeof(division_logits), sizeof(division_logits_back), sizeof(division_gradient)};
-    constexpr Py_ssize_t n = sizeof at / sizeof at[0], m = sizeof sizes / sizeof sizes[0];
+// ---- the operators of a token model's layers: tensors on the current device; heads may be parts of a wider tensor
+
+bool here(const at::Tensor& t) { return t.device().index() == c10::hip::current_device(); }
+// [batch, tokens, heads, features], features next to one another; the strides as the library takes them
+bool heads_of(const at::Tensor* t, int64_t* strides) {
+    if (!t || t->dim() != 4 || t->numel() == 0 || t->stride(3) != 1) return false;
+    for (int i = 0; i < 3; ++i) strides[i] = t->size(i) == 1 ? 0 : t->stride(i);
+    return true;
+}
+bool vector_of(const at::Tensor* t, at::ScalarType type, int64_t n, const at::Tensor& x) {
+    return t && t->dim() == 1 && t->size(0) == n && t->scalar_type() == type && t->device() == x.device() && t->is_contiguous();
+}
+// q, k, v, scale, causal, window, lengths, starts
+bool attention_of(PyObject* const* a, division_attention* d, const at::Tensor** of_q) {
+    const at::Tensor *q = device_tensor(a[0]), *k = device_tensor(a[1]), *v = device_tensor(a[2]), *lengths, *starts;
+    if (!heads_of(q, d->q_strides) || !heads_of(k, d->k_strides) || !heads_of(v, d->v_strides) || !here(*q) || (a[3] != Py_None && !PyFloat_CheckExact(a[3])) || !PyBool_Check(a[4]) ||
+        !whole(a[5], &d->window) || d->window < 0 || !maybe(a[6], &lengths) || !maybe(a[7], &starts))
+        return false;
+    const int dt = type_of(q->scalar_type(), false);
+    if (dt < 0 || k->scalar_type() != q->scalar_type() || v->scalar_type() != q->scalar_type() || k->device() != q->device() || v->device() != q->device() || k->sizes() != v->sizes() ||
+        k->size(0) != q->size(0) || k->size(3) != q->size(3) || q->size(2) % k->size(2) != 0 || (lengths && !vector_of(lengths, at::kInt, q->size(0), *q)) ||
+        (starts && !vector_of(starts, at::kInt, q->size(0), *q)))
+        return false;
+    d->q = q->data_ptr(); d->k = k->data_ptr(); d->v = v->data_ptr();
+    d->B = q->size(0); d->Sq = q->size(1); d->H = q->size(2); d->D = q->size(3); d->Sk = k->size(1); d->G = k->size(2);
+    d->dt = (division_dtype)dt;
+    d->scale = a[3] == Py_None ? (float)(1.0 / std::sqrt((double)d->D)) : (float)PyFloat_AS_DOUBLE(a[3]);
+    d->causal = a[4] == Py_True;
+    d->lengths = lengths ? lengths->data_ptr<int>() : nullptr;
+    d->starts = starts ? starts->data_ptr<int>() : nullptr;
+    *of_q = q;
+    return true;
+}
+std::vector<int64_t> lse_sizes(const division_attention& d) { return {d.B, d.H, d.Sq}; }
+
+// attention(q, k, v, scale, causal, window, lengths, starts)
+PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(8);
+    division_attention d{};
+    const at::Tensor* q;
+    if (!attend || !attention_of(a, &d, &q)) return none();
+    void* st = current_stream();
+    const at::Tensor in = *q;
+    at::Tensor out, lse, ws;
+    const int rc = without_lock([&] {
+        out = fresh(in.sizes(), in.scalar_type(), in);
+        lse = fresh(lse_sizes(d), at::kFloat, in);
+        const size_t need = attention_workspace(&d);
+        if (need) ws = workspace(need, in);
+        return attend(&d, out.data_ptr(), lse.data_ptr<float>(), at_or_null(ws), need, st);
+    });
+    return rc ? PyLong_FromLong(rc) : tuple_of({out, lse});
+    END_HANDLE_TH_ERRORS
+}
+
+// attention_backward(q, k, v, scale, causal, window, lengths, starts, grad_out, out, lse)
+PyObject* py_attention_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(11);
+    division_attention d{};
+    division_attention_back b{};
+    const at::Tensor *q, *g = device_tensor(a[8]), *o = device_tensor(a[9]), *lse = device_tensor(a[10]);
+    if (!attention_backward || !attention_of(a, &d, &q) || !heads_of(g, b.grad_out_strides) || !is_like(o, *q) || g->sizes() != q->sizes() || g->scalar_type() != q->scalar_type() ||
+        g->device() != q->device() || !lse || lse->scalar_type() != at::kFloat || lse->device() != q->device() || !lse->is_contiguous() || lse->sizes() != at::IntArrayRef(lse_sizes(d)))
+        return none();
+    b.grad_out = g->data_ptr(); b.out = o->data_ptr(); b.lse = lse->data_ptr<float>();
+    void* st = current_stream();
+    const at::Tensor in = *q;
+    const std::vector<int64_t> of_keys = {d.B, d.Sk, d.G, d.D};
+    at::Tensor dq, dk, dv, ws;
+    const int rc = without_lock([&] {
+        dq = fresh(in.sizes(), in.scalar_type(), in);
+        dk = fresh(of_keys, in.scalar_type(), in);
+        dv = fresh(of_keys, in.scalar_type(), in);
+        b.workspace_bytes = attention_backward_workspace(&d);
+        ws = workspace(b.workspace_bytes, in);
+        b.grad_q = dq.data_ptr(); b.grad_k = dk.data_ptr(); b.grad_v = dv.data_ptr(); b.workspace = ws.data_ptr();
+        return attention_backward(&d, &b, st);
+    });
+    return rc ? PyLong_FromLong(rc) : tuple_of({dq, dk, dv});
+    END_HANDLE_TH_ERRORS
+}
+
+// Tokens of heads: every dimension but the last two counts as one, of one stride
+bool tokens_of(const at::Tensor& t, int64_t* tokens, int64_t* token_stride, int64_t* heads, int64_t* head_stride) {
+    const int64_t n = t.dim();
+    if (n < 2 || t.numel() == 0 || t.stride(n - 1) != 1) return false;
+    int64_t inner = 1, stride = 0;
+    for (int64_t i = n - 3; i >= 0; --i) {
+        if (t.size(i) == 1) continue;
+        if (inner == 1) stride = t.stride(i);
+        else if (t.stride(i) != stride * inner) return false;
+        inner *= t.size(i);
+    }
+    *tokens = inner; *token_stride = stride;
+    *heads = t.size(n - 2); *head_stride = t.size(n - 2) > 1 ? t.stride(n - 2) : 0;
+    return true;
+}
+struct RotateOf { const at::Tensor *x[2], *weight[2]; int sides; };
+// q, k, q_weight, k_weight, frequencies, positions, eps, next
+bool rotate_of(PyObject* const* a, division_rotate* d, RotateOf* r) {
+    const at::Tensor *f = device_tensor(a[4]), *at_ = device_tensor(a[5]);
+    r->sides = a[1] == Py_None ? 1 : 2;
+    if ((a[1] == Py_None) != (a[3] == Py_None) || !f || !at_ || !PyFloat_CheckExact(a[6]) || !PyBool_Check(a[7])) return false;
+    for (int k = 0; k < r->sides; ++k) {
+        const at::Tensor *x = r->x[k] = device_tensor(a[k]), *w = r->weight[k] = weight_tensor(a[2 + k]);
+        int64_t T;
+        if (!x || !tokens_of(*x, &T, &d->token_strides[k], &d->heads[k], &d->head_strides[k]) || !w || w->dim() != 1 || w->size(0) != x->size(-1) || !w->is_contiguous() ||
+            w->device() != x->device())
+            return false;
+        const int wdt = type_of(w->scalar_type(), false);
+        if (wdt < 0) return false;
+        if (k && (x->scalar_type() != r->x[0]->scalar_type() || x->device() != r->x[0]->device() || x->size(-1) != r->x[0]->size(-1) ||
+                  x->sizes().slice(0, (size_t)x->dim() - 2) != r->x[0]->sizes().slice(0, (size_t)r->x[0]->dim() - 2)))
+            return false;
+        d->x[k] = x->data_ptr(); d->weight[k] = w->data_ptr(); d->weight_dt[k] = (division_dtype)wdt;
+        d->T = T;
+    }
+    const at::Tensor& x = *r->x[0];
+    const int dt = type_of(x.scalar_type(), false);
+    if (dt < 0 || !here(x) || f->dim() != 1 || !vector_of(f, at::kDouble, f->size(0), x) || f->numel() == 0 || at_->scalar_type() != at::kLong || at_->device() != x.device() ||
+        !at_->is_contiguous() || at_->sizes() != x.sizes().slice(0, (size_t)x.dim() - 2))
+        return false;
+    d->D = x.size(-1); d->rotated = 2 * f->size(0); d->dt = (division_dtype)dt; d->next = a[7] == Py_True; d->eps = (float)PyFloat_AS_DOUBLE(a[6]);
+    d->frequencies = f->data_ptr<double>(); d->positions = at_->data_ptr<int64_t>();
+    return true;
+}
+
+// head_norm_rotate(q, k, q_weight, k_weight, frequencies, positions, eps, next)
+PyObject* py_head_norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(8);
+    division_rotate d{};
+    RotateOf r{};
+    if (!head_norm_rotate || !rotate_of(a, &d, &r)) return none();
+    void* st = current_stream();
+    const at::Tensor in[2] = {*r.x[0], r.sides == 2 ? *r.x[1] : at::Tensor()};
+    at::Tensor y[2], rstd[2];
+    const int rc = without_lock([&] {
+        for (int k = 0; k < r.sides; ++k) {
+            y[k] = fresh(in[k].sizes(), in[k].scalar_type(), in[k]);
+            rstd[k] = fresh(rows_alone(in[k]), at::kFloat, in[k]);
+            d.y[k] = y[k].data_ptr(); d.rstd[k] = rstd[k].data_ptr<float>();
+        }
+        return head_norm_rotate(&d, st);
+    });
+    return rc ? PyLong_FromLong(rc) : tuple_or_none({y[0], y[1], rstd[0], rstd[1]});
+    END_HANDLE_TH_ERRORS
+}
+
+// head_norm_rotate_backward(q, k, q_weight, k_weight, frequencies, positions, eps, next, grad_q, grad_k, q_rstd, k_rstd)
+PyObject* py_head_norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(12);
+    division_rotate d{};
+    division_rotate_back b{};
+    RotateOf r{};
+    if (!head_norm_rotate_backward || !rotate_of(a, &d, &r) || (r.sides == 1) != (a[9] == Py_None) || (r.sides == 1) != (a[11] == Py_None)) return none();
+    for (int k = 0; k < r.sides; ++k) {
+        const at::Tensor *g = device_tensor(a[8 + k]), *rstd = device_tensor(a[10 + k]);
+        int64_t T, heads;
+        if (!g || g->sizes() != r.x[k]->sizes() || g->scalar_type() != r.x[k]->scalar_type() || g->device() != r.x[k]->device() ||
+            !tokens_of(*g, &T, &b.token_strides[k], &heads, &b.head_strides[k]) || !per_row(rstd, at::kFloat, *r.x[k]))
+            return none();
+        b.grad_y[k] = g->data_ptr(); b.rstd[k] = rstd->data_ptr<float>();
+    }
+    void* st = current_stream();
+    const at::Tensor in[2] = {*r.x[0], r.sides == 2 ? *r.x[1] : at::Tensor()}, weight[2] = {r.weight[0]->detach(), r.sides == 2 ? r.weight[1]->detach() : at::Tensor()};
+    at::Tensor dx[2], dw[2], ws;
+    const int rc = without_lock([&] {
+        for (int k = 0; k < r.sides; ++k) {
+            dx[k] = fresh(in[k].sizes(), in[k].scalar_type(), in[k]);
+            dw[k] = fresh_like(weight[k]);
+            b.grad_x[k] = dx[k].data_ptr(); b.grad_weight[k] = dw[k].data_ptr();
+        }
+        b.workspace_bytes = head_norm_rotate_backward_workspace(d.T, d.D);
+        ws = workspace(b.workspace_bytes, in[0]);
+        b.workspace = ws.data_ptr();
+        return head_norm_rotate_backward(&d, &b, st);
+    });
+    return rc ? PyLong_FromLong(rc) : tuple_or_none({dx[0], dx[1], dw[0], dw[1]});
+    END_HANDLE_TH_ERRORS
+}
+
+// embedding(ids, table, scale, ignore_index)
+PyObject* py_embedding(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(4);
+    const at::Tensor *ids = device_tensor(a[0]), *table = weight_tensor(a[1]);
+    int64_t ignore;
+    if (!embedding || !ids || ids->scalar_type() != at::kLong || !ids->is_contiguous() || ids->numel() == 0 || !table || table->dim() != 2 || table->numel() == 0 || !table->is_contiguous() ||
+        !here(*table) || ids->device() != table->device() || !PyFloat_CheckExact(a[2]) || !whole(a[3], &ignore))
+        return none();
+    const int dt = type_of(table->scalar_type(), false);
+    if (dt < 0) return none();
+    const float scale = (float)PyFloat_AS_DOUBLE(a[2]);
+    void* st = current_stream();
+    const at::Tensor in = *ids, rows = table->detach();
+    std::vector<int64_t> sizes = in.sizes().vec();
+    sizes.push_back(rows.size(1));
+    at::Tensor out;
+    const int rc = without_lock([&] {
+        out = fresh(sizes, rows.scalar_type(), rows);
+        return embedding(in.data_ptr<int64_t>(), in.numel(), rows.data_ptr(), rows.size(0), rows.size(1), (division_dtype)dt, scale, ignore, out.data_ptr(), st);
+    });
+    return rc ? PyLong_FromLong(rc) : wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// embedding_backward(grad, ids, vocabulary, scale, ignore_index): into a tensor of the gradient's type
+PyObject* py_embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(5);
+    const at::Tensor *g = device_tensor(a[0]), *ids = device_tensor(a[1]);
+    RowsOf r;
+    division_embedding_back b{};
+    if (!embedding_backward || !rows_of(g, &r) || !here(*g) || !per_row(ids, at::kLong, *g) || !whole(a[2], &b.V) || b.V < 1 || !PyFloat_CheckExact(a[3]) || !whole(a[4], &b.ignore_index)) return none();
+    b.grad = g->data_ptr(); b.ids = ids->data_ptr<int64_t>(); b.grad_stride = b.D = r.D; b.T = r.T;
+    b.dt = b.table_dt = (division_dtype)r.dt; b.scale = (float)PyFloat_AS_DOUBLE(a[3]);
+    void* st = current_stream();
+    const at::Tensor in = *g;
+    at::Tensor out, ws;
+    const int rc = without_lock([&] {
+        b.workspace_bytes = embedding_backward_workspace(b.T, b.V, b.D);
+        if (!b.workspace_bytes) return (int)DIVISION_ERANGE;
+        out = fresh({b.V, b.D}, in.scalar_type(), in);
+        ws = workspace(b.workspace_bytes, in);
+        b.grad_table = out.data_ptr(); b.workspace = ws.data_ptr();
+        return embedding_backward(&b, st);
+    });
+    return rc ? PyLong_FromLong(rc) : wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// dropout_add(x, p, seed, residual): a seed on the host
+PyObject* py_dropout_add(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    PLAIN(4);
+    const at::Tensor *x = device_tensor(a[0]), *res;
+    uint64_t seed;
+    if (!dropout_add || !x || !x->is_contiguous() || x->numel() == 0 || !here(*x) || !PyFloat_CheckExact(a[1]) || !seed64(a[2], &seed) || !maybe(a[3], &res) || (res && !is_like(res, *x))) return none();
+    const int dt = type_of(x->scalar_type(), false);
+    if (dt < 0) return none();
+    const double p = PyFloat_AS_DOUBLE(a[1]);
+    const void* rp = at_or_null(res);
+    void* st = current_stream();
+    const at::Tensor in = *x;
+    at::Tensor out;
+    const int rc = without_lock([&] {
+        out = fresh(in.sizes(), in.scalar_type(), in);
+        return dropout_add(in.data_ptr(), rp, in.numel(), (division_dtype)dt, p, seed, nullptr, out.data_ptr(), st);
+    });
+    return rc ? PyLong_FromLong(rc) : wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// addresses and sizes as they were compiled in, into `at`; false with an error set
+bool bind_table(PyObject* const* a, Py_ssize_t nargs, void** const* at, Py_ssize_t n, const size_t* sizes, Py_ssize_t m) {
     bool ok = nargs == 2 && PyList_CheckExact(a[0]) && PyList_GET_SIZE(a[0]) == n && PyList_CheckExact(a[1]) && PyList_GET_SIZE(a[1]) == m;
-    void* found[n];
+    std::vector<void*> found((size_t)n);
     for (Py_ssize_t i = 0; ok && i < m; ++i) {
         int64_t v = 0;
         ok = whole(PyList_GET_ITEM(a[1], i), &v) && v == (int64_t)sizes[i];
     }
     for (Py_ssize_t i = 0; ok && i < n; ++i) {
-        found[i] = PyLong_AsVoidPtr(PyList_GET_ITEM(a[0], i));
-        if (!found[i]) { PyErr_Clear(); ok = false; }
+        found[(size_t)i] = PyLong_AsVoidPtr(PyList_GET_ITEM(a[0], i));
+        if (!found[(size_t)i]) { PyErr_Clear(); ok = false; }
     }
     if (!ok) {
         PyErr_SetString(PyExc_ValueError, "built for another set of operators");
-        return nullptr;
+        return false;
     }
-    for (Py_ssize_t i = 0; i < n; ++i) *at[i] = found[i];
+    for (Py_ssize_t i = 0; i < n; ++i) *at[i] = found[(size_t)i];
+    return true;
+}
+
+// bind_layers(addresses, sizes): as bind_operators, of the operators of a token model's layers
+PyObject* py_bind_layers(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    void** const at[] = {(void**)&attention_workspace, (void**)&attend, (void**)&attention_backward_workspace, (void**)&attention_backward, (void**)&head_norm_rotate,
+                         (void**)&head_norm_rotate_backward_workspace, (void**)&head_norm_rotate_backward, (void**)&embedding, (void**)&embedding_backward_workspace,
+                         (void**)&embedding_backward, (void**)&dropout_add};
+    const size_t sizes[] = {sizeof(division_attention), sizeof(division_attention_back), sizeof(division_rotate), sizeof(division_rotate_back), sizeof(division_embedding_back)};
+    if (!bind_table(a, nargs, at, sizeof at / sizeof at[0], sizes, sizeof sizes / sizeof sizes[0])) return nullptr;
+    Py_RETURN_NONE;
+}
+
+// bind_operators(addresses, sizes): their entries in the order of the table, and the sizes of their descriptors
+PyObject* py_bind_operators(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    void** const at[] = {(void**)&rms_norm, (void**)&read_codes, (void**)&rms_norm_backward_workspace, (void**)&rms_norm_backward, (void**)&log_probs_workspace,
+                         (void**)&log_probs, (void**)&log_probs_backward, (void**)&grad_norm_workspace, (void**)&clip_grads};
+    const size_t sizes[] = {sizeof(division_norm), sizeof(division_norm_back), sizeof(division_logits), sizeof(division_logits_back), sizeof(division_gradient)};
+    if (!bind_table(a, nargs, at, sizeof at / sizeof at[0], sizes, sizeof sizes / sizeof sizes[0])) return nullptr;
     Py_RETURN_NONE;
 }
 
@@ -716,7 +1001,8 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
 PyMethodDef methods[] = {FAST(compress), FAST(decompress), FAST(compress_maps), FAST(decompress_maps), FAST(relu_forward), FAST(relu_compress),
                          FAST(dropout_forward), FAST(mask_backward), FAST(maxpool_forward), FAST(maxpool_backward),
                          FAST(rms_norm), FAST(read_codes), FAST(rms_norm_backward), FAST(log_probs), FAST(log_probs_backward), FAST(clip_grads),
-                         FAST(bind_operators), FAST(bind), {nullptr, nullptr, 0, nullptr}};
+                         FAST(attention), FAST(attention_backward), FAST(head_norm_rotate), FAST(head_norm_rotate_backward), FAST(embedding), FAST(embedding_backward), FAST(dropout_add),
+                         FAST(bind_layers), FAST(bind_operators), FAST(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -116,6 +116,58 @@ template <typename T, int DP, int ROWS> struct Tile {
     }
 };
 
+// The same with whole rows behind one another, their pieces exchanged with the row's number over the row: a wavefront's load takes whole rows, not 64 bytes of each of sixteen, which counts
+// where the memory is the bound (32 tokens over caches of up to 8192 keys: LINES_US).
+template <typename T, int DP, int ROWS> struct RowTile {
+    static constexpr int kRowBytes = DP * (int)sizeof(T), kPieces = kRowBytes / 16, kBytes = ROWS * kRowBytes;
+    static __device__ __forceinline__ int turn(int row) {
+        if constexpr (sizeof(T) == 4) return (row >> 2 & 1) << 3 | (row & 3) << 1 | (row >> 3 & 1);
+        else if constexpr (kPieces == 16) return (row & 3) << 2 | (row >> 2 & 3);
+        else return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    }
+    static __device__ __forceinline__ int place(int row, int piece) { return row * kRowBytes + ((piece ^ turn(row)) << 4); }
+
+    template <int THREADS, typename At> static __device__ __forceinline__ void fill(char* tile, const char* base, int rows, int row_bytes, int thread, At&& at) {
+        constexpr int kEach = kBytes / 16 / THREADS;
+        static_assert(kEach * THREADS * 16 == kBytes, "whole pieces a thread");
+        const u32x4 from = buffer(base, 0x7fffffffu);
+        const int first = __builtin_amdgcn_readfirstlane(thread & ~63);
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            const int slot = u * THREADS + thread, row = slot / kPieces, piece = (slot % kPieces) ^ turn(row);
+            const uint32_t off = row < rows && piece * 16 < row_bytes ? (uint32_t)(at(row) + piece * 16) : 0x80000000u;
+            load_lds16(from, tile + (u * THREADS + first) * 16, off);
+        }
+    }
+    static __device__ __forceinline__ Operand<T> rows(const char* tile, int row0, int step, int lane) {
+        const int row = row0 + (lane & 31), half = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            return Operand<T>::at(tile + place(row, 2 * step + half));
+        } else {
+            Operand<T> o;
+            o.lo = *reinterpret_cast<const f32x4*>(tile + place(row, 4 * step + 2 * half));
+            o.hi = *reinterpret_cast<const f32x4*>(tile + place(row, 4 * step + 2 * half + 1));
+            return o;
+        }
+    }
+    static __device__ __forceinline__ Operand<T> columns(const char* tile, int row0, int col0, int lane) {
+        const int half = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            const int i = lane & 15, row = row0 + 4 * half + (i >> 2), col = col0 + (lane & 16) + (i & 3) * 4;
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_AT(s16x4, tile + place(row, col >> 3) + (col & 4) * 2));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_AT(s16x4, tile + place(row + 8, col >> 3) + (col & 4) * 2));
+            const u32x2 p = __builtin_bit_cast(u32x2, a), q = __builtin_bit_cast(u32x2, b);
+            return {__builtin_bit_cast(bf16x8, (u32x4{p.x, p.y, q.x, q.y}))};
+        } else {
+            float v[8];
+            const int col = col0 + (lane & 31);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float*>(tile + place(row0 + 8 * (j / 4) + 4 * half + j % 4, col >> 2) + (col & 3) * 4);
+            return Operand<T>::of(v);
+        }
+    }
+};
+
 // all but the last LEFT loads that the wavefront has begun are there.  (The builtin: the compiler sees that its own loads before a loop need no wait within it.)
 template <int LEFT = 0> __device__ __forceinline__ void loads_done() {
     if constexpr (LEFT == 0) {

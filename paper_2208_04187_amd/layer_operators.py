@@ -11,8 +11,8 @@ from typing import NamedTuple
 
 import torch
 
-from .binding import OPERATOR_OTHERS, DivisionError, _dt, _stream, lib
-from .operators import _at, _beside, _checked, _dense, _rows, _workspace, _written
+from .binding import LAYER_DESCS, LAYER_ENTRIES, _dt, _result, _stream, lib
+from .operators import _at, _beside, _checked, _dense, _fast, _rows, _written
 
 _vp, _i64, _ci, _sz, _f, _u64 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, ctypes.c_float, ctypes.c_uint64
 _three, _two, _pair = _i64 * 3, _i64 * 2, _vp * 2
@@ -47,7 +47,7 @@ class _EmbeddingBackDesc(ctypes.Structure):
                 ("add", _ci), ("grad_table", _vp), ("workspace", _vp), ("workspace_bytes", _sz)]
 
 
-OPERATOR_OTHERS += [
+LAYER_ENTRIES += [
     ("division_attention_workspace", [_vp], _sz),
     ("division_attend", [_vp, _vp, _vp, _vp, _sz, _vp], _ci),
     ("division_attention_backward_workspace", [_vp], _sz),
@@ -60,6 +60,31 @@ OPERATOR_OTHERS += [
     ("division_embedding_backward", [_vp, _vp], _ci),
     ("division_dropout_add", [_vp, _vp, _i64, _ci, ctypes.c_double, _u64, _vp, _vp, _vp], _ci),
 ]
+LAYER_DESCS += [_AttentionDesc, _AttentionBackDesc, _RotateDesc, _RotateBackDesc, _EmbeddingBackDesc]
+
+
+class _Call:
+    """One call: its outputs and workspace on the device of its tensors, and the launch there, whatever the current device.  On a stream given by the caller the memory of what it
+    made is not handed out again before that stream has passed the call."""
+
+    def __init__(self, device, stream, what):
+        self.device, self.stream, self.what = device, stream, what
+
+    def new(self, shape, dtype):
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        if self.stream is not None:
+            t.record_stream(self.stream if hasattr(self.stream, "cuda_stream") else torch.cuda.ExternalStream(int(self.stream), device=self.device))
+        return t
+
+    def workspace(self, nbytes: int):
+        return self.new((max(int(nbytes), 1),), torch.uint8)
+
+    def launch(self, entry, *args):
+        if self.device.index == torch.cuda.current_device():
+            _checked(entry(*args, _stream(self.stream)), self.what)
+        else:
+            with torch.cuda.device(self.device):
+                _checked(entry(*args, _stream(self.stream)), self.what)
 
 
 class Attended(NamedTuple):
@@ -109,18 +134,26 @@ def division_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale:
 
     lengths (int32 [batch]): keys that a sequence has; what lies behind them is not looked at.  starts (int32 [batch]): where a sequence's first query stands among the keys, keys -
     queries if not given.  causal: a query sees no key behind its own position; window: only keys nearer than that.  A query that sees none has out 0 and lse -inf."""
+    if stream is None:
+        got = _fast().attention(q, k, v, scale, causal, window, lengths, starts)
+        if got is not None:
+            return Attended._make(_result(got, "division_attention"))
     d = _attention(q, k, v, scale, causal, window, lengths, starts)
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    call = _Call(q.device, stream, "division_attention")
+    out, lse = call.new(q.shape, q.dtype), call.new((q.shape[0], q.shape[2], q.shape[1]), torch.float32)
     nbytes = int(lib().division_attention_workspace(ctypes.byref(d)))
-    ws = _workspace(nbytes, q.device, stream) if nbytes else None
-    _checked(lib().division_attend(ctypes.byref(d), out.data_ptr(), lse.data_ptr(), _at(ws), nbytes, _stream(stream)), "division_attention")
+    ws = call.workspace(nbytes) if nbytes else None
+    call.launch(lib().division_attend, ctypes.byref(d), out.data_ptr(), lse.data_ptr(), _at(ws), nbytes)
     return Attended(out, lse)
 
 
 def division_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, scale: float | None = None,
                                 causal: bool = False, window: int = 0, lengths: torch.Tensor | None = None, starts: torch.Tensor | None = None, stream=None):
     """(the gradients of q, of k and of v) from that of out, and from what division_attention gave for the same arguments."""
+    if stream is None:
+        got = _fast().attention_backward(q, k, v, scale, causal, window, lengths, starts, grad_out, out, lse)
+        if got is not None:
+            return _result(got, "division_attention_backward")
     d = _attention(q, k, v, scale, causal, window, lengths, starts)
     b = _AttentionBackDesc()
     b.grad_out_strides = _heads(grad_out, "grad_out", q)
@@ -128,13 +161,17 @@ def division_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torc
         raise ValueError("grad_out must have q's shape")
     _dense(out, "out", dtype=q.dtype, shape=q.shape, device=q.device)
     _dense(lse, "lse", dtype=torch.float32, shape=(q.shape[0], q.shape[2], q.shape[1]), device=q.device)
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    call = _Call(q.device, stream, "division_attention_backward")
+    dq, dk, dv = (call.new(t.shape, t.dtype) for t in (q, k, v))
     nbytes = int(lib().division_attention_backward_workspace(ctypes.byref(d)))
-    ws = _workspace(nbytes, q.device, stream)
+    ws = call.workspace(nbytes)
     b.grad_out, b.out, b.lse, b.grad_q, b.grad_k, b.grad_v = grad_out.data_ptr(), out.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr()
     b.workspace, b.workspace_bytes = ws.data_ptr(), nbytes
-    _checked(lib().division_attention_backward(ctypes.byref(d), ctypes.byref(b), _stream(stream)), "division_attention_backward")
+    call.launch(lib().division_attention_backward, ctypes.byref(d), ctypes.byref(b))
     return dq, dk, dv
+
+
+_PAIRS = {"halves": False, "next": True}
 
 
 class Rotated(NamedTuple):
@@ -154,7 +191,7 @@ def _tokens_of_heads(t: torch.Tensor, what: str):
 
 
 def _rotation(q, k, q_weight, k_weight, frequencies, positions, eps, pairs):
-    if pairs not in ("halves", "next"):
+    if pairs not in _PAIRS:
         raise ValueError("pairs is 'halves' or 'next'")
     if (k is None) != (k_weight is None):
         raise ValueError("keys and their norm's weight come together")
@@ -176,7 +213,7 @@ def _rotation(q, k, q_weight, k_weight, frequencies, positions, eps, pairs):
     if frequencies.dim() != 1:
         raise ValueError("frequencies is one row")
     _dense(positions, "positions", dtype=torch.int64, shape=lead, device=q.device)
-    d.rotated, d.dt, d.next, d.eps = 2 * frequencies.numel(), _dt(q.dtype), pairs == "next", eps
+    d.rotated, d.dt, d.next, d.eps = 2 * frequencies.numel(), _dt(q.dtype), _PAIRS[pairs], eps
     d.frequencies, d.positions = _at(frequencies) if frequencies.numel() else None, positions.data_ptr()
     return d, [x for x, _, _ in sides]
 
@@ -188,12 +225,17 @@ def division_head_norm_rotate(q: torch.Tensor, k: torch.Tensor | None, q_weight:
     q [..., heads, features] and k [..., key heads, features] (or None): float32 or bfloat16, features even and up to 512; parts of one projection's output are fine.
     The first 2 * len(frequencies) features are turned by positions[...] * frequencies (int64, float64; angles are taken in 64 bits): feature p with p + len(frequencies)
     (pairs='halves') or 2 p with 2 p + 1 ('next').  The weights ([features], float32 or bfloat16) are the norms'."""
+    if stream is None and pairs in _PAIRS:
+        got = _fast().head_norm_rotate(q, k, q_weight, k_weight, frequencies, positions, eps, _PAIRS[pairs])
+        if got is not None:
+            return Rotated._make(_result(got, "division_head_norm_rotate"))
     d, sides = _rotation(q, k, q_weight, k_weight, frequencies, positions, eps, pairs)
-    ys = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in sides]
-    rstds = [torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) for x in sides]
+    call = _Call(q.device, stream, "division_head_norm_rotate")
+    ys = [call.new(x.shape, x.dtype) for x in sides]
+    rstds = [call.new(x.shape[:-1], torch.float32) for x in sides]
     for i, (y, r) in enumerate(zip(ys, rstds)):
         d.y[i], d.rstd[i] = y.data_ptr(), r.data_ptr()
-    _checked(lib().division_head_norm_rotate(ctypes.byref(d), _stream(stream)), "division_head_norm_rotate")
+    call.launch(lib().division_head_norm_rotate, ctypes.byref(d))
     return Rotated(ys[0], ys[1] if k is not None else None, rstds[0], rstds[1] if k is not None else None)
 
 
@@ -201,12 +243,17 @@ def division_head_norm_rotate_backward(grad_q: torch.Tensor, grad_k: torch.Tenso
                                        k_weight: torch.Tensor | None, frequencies: torch.Tensor, positions: torch.Tensor, q_rstd: torch.Tensor, k_rstd: torch.Tensor | None,
                                        pairs: str = "halves", stream=None):
     """(the gradients of q, k and of their weights) from those of division_head_norm_rotate's q and k, its inputs and its rstd; None for keys that are not given."""
+    if stream is None and pairs in _PAIRS:
+        got = _fast().head_norm_rotate_backward(q, k, q_weight, k_weight, frequencies, positions, 0.0, _PAIRS[pairs], grad_q, grad_k, q_rstd, k_rstd)
+        if got is not None:
+            return _result(got, "division_head_norm_rotate_backward")
     d, sides = _rotation(q, k, q_weight, k_weight, frequencies, positions, 0.0, pairs)
     if (k is None) != (grad_k is None) or (k is None) != (k_rstd is None):
         raise ValueError("keys, their gradient and their statistic come together")
     b = _RotateBackDesc()
-    dxs = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in sides]
-    dws = [torch.empty_like(w) for w in ((q_weight, k_weight) if k is not None else (q_weight,))]
+    call = _Call(q.device, stream, "division_head_norm_rotate_backward")
+    dxs = [call.new(x.shape, x.dtype) for x in sides]
+    dws = [call.new(w.shape, w.dtype) for w in ((q_weight, k_weight) if k is not None else (q_weight,))]
     for i, (x, g, r, name) in enumerate(zip(sides, (grad_q, grad_k), (q_rstd, k_rstd), ("q", "k"))):
         if g.shape != x.shape or g.dtype != x.dtype:
             raise ValueError(f"grad_{name} must have {name}'s shape and type")
@@ -215,22 +262,28 @@ def division_head_norm_rotate_backward(grad_q: torch.Tensor, grad_k: torch.Tenso
         _dense(r, f"{name}_rstd", dtype=torch.float32, shape=x.shape[:-1], device=x.device)
         b.grad_y[i], b.rstd[i], b.grad_x[i], b.grad_weight[i] = g.data_ptr(), r.data_ptr(), dxs[i].data_ptr(), dws[i].data_ptr()
     nbytes = int(lib().division_head_norm_rotate_backward_workspace(d.T, d.D))
-    ws = _workspace(nbytes, q.device, stream)
+    ws = call.workspace(nbytes)
     b.workspace, b.workspace_bytes = ws.data_ptr(), nbytes
-    _checked(lib().division_head_norm_rotate_backward(ctypes.byref(d), ctypes.byref(b), _stream(stream)), "division_head_norm_rotate_backward")
+    call.launch(lib().division_head_norm_rotate_backward, ctypes.byref(d), ctypes.byref(b))
     return (dxs[0], dxs[1], dws[0], dws[1]) if k is not None else (dxs[0], None, dws[0], None)
 
 
 def division_embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, ignore_index: int = -100, stream=None) -> torch.Tensor:
     """scale * table[ids]: ids int64 of any shape, table [vocabulary, features] float32 or bfloat16.  Where ids is ignore_index the row is zeros; any other number outside the
     vocabulary gives NaN."""
+    if stream is None:
+        got = _fast().embedding(ids, table, scale, ignore_index)
+        if got is not None:
+            return _result(got, "division_embedding")
     _dense(table, "table")
     if table.dim() != 2:
         raise ValueError("table is [vocabulary, features]")
     _dense(ids, "ids", dtype=torch.int64, device=table.device)
     V, D = table.shape
-    out = torch.empty((*ids.shape, D), dtype=table.dtype, device=table.device)
-    _checked(lib().division_embedding(ids.data_ptr(), ids.numel(), table.data_ptr(), V, D, _dt(table.dtype), scale, ignore_index, out.data_ptr(), _stream(stream)), "division_embedding")
+    call = _Call(table.device, stream, "division_embedding")
+    dt = _dt(table.dtype)
+    out = call.new((*ids.shape, D), table.dtype)
+    call.launch(lib().division_embedding, ids.data_ptr(), ids.numel(), table.data_ptr(), V, D, dt, scale, ignore_index, out.data_ptr())
     return out
 
 
@@ -239,19 +292,24 @@ def division_embedding_backward(grad: torch.Tensor, ids: torch.Tensor, vocabular
     """The gradient of division_embedding's table, [vocabulary, features], from that of its rows: each row's tokens are added up in their order.
 
     out: where it goes (float32 for bfloat16 gradients, for instance); add=True adds to what out holds, and leaves rows without a token alone."""
+    if stream is None and out is None and not add:
+        got = _fast().embedding_backward(grad, ids, vocabulary, scale, ignore_index)
+        if got is not None:
+            return _result(got, "division_embedding_backward")
     T, stride, D = _rows(grad, "grad")
     _dense(ids, "ids", dtype=torch.int64, shape=grad.shape[:-1], device=grad.device)
+    call = _Call(grad.device, stream, "division_embedding_backward")
     if out is None:
         if add:
             raise ValueError("add=True adds to out")
-        out = torch.empty((vocabulary, D), dtype=grad.dtype, device=grad.device)
+        out = call.new((vocabulary, D), grad.dtype)
     else:
         _dense(out, "out", shape=(vocabulary, D), device=grad.device)
     nbytes = int(lib().division_embedding_backward_workspace(T, vocabulary, D))
-    ws = _workspace(nbytes, grad.device, stream)
+    ws = call.workspace(nbytes)
     d = _EmbeddingBackDesc(grad.data_ptr(), ids.data_ptr(), stride, T, vocabulary, D, ignore_index, _dt(grad.dtype), _dt(out.dtype), scale, bool(add), out.data_ptr(), ws.data_ptr(),
                            nbytes)
-    _checked(lib().division_embedding_backward(ctypes.byref(d), _stream(stream)), "division_embedding_backward")
+    call.launch(lib().division_embedding_backward, ctypes.byref(d))
     _written(out)
     return out
 
@@ -262,6 +320,10 @@ def division_dropout_add(x: torch.Tensor, p: float, seed, residual: torch.Tensor
 
     x and residual: contiguous, float32 or bfloat16.  seed: a whole number, or an int64 tensor of one element on the device, which is read when the kernel runs (a captured
     graph drops other elements when it is replayed with another).  out may be x or residual itself."""
+    if stream is None and out is None:
+        got = _fast().dropout_add(x, p, seed, residual)
+        if got is not None:
+            return _result(got, "division_dropout_add")
     _dense(x, "x")
     if residual is not None:
         _dense(residual, "residual", dtype=x.dtype, shape=x.shape, device=x.device)
@@ -271,12 +333,12 @@ def division_dropout_add(x: torch.Tensor, p: float, seed, residual: torch.Tensor
         if seed.numel() != 1:
             raise ValueError("seed is one number")
         at, seed = seed.data_ptr(), 0
+    call = _Call(x.device, stream, "division_dropout_add")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = call.new(x.shape, x.dtype)
     else:
         _dense(out, "out", dtype=x.dtype, shape=x.shape, device=x.device)
         _written(out)
     n = x.numel()
-    _checked(lib().division_dropout_add(x.data_ptr() if n else None, _at(residual) if n else None, n, _dt(x.dtype), p, seed & (2 ** 64 - 1), at, out.data_ptr() if n else None,
-                                        _stream(stream)), "division_dropout_add")
+    call.launch(lib().division_dropout_add, x.data_ptr() if n else None, _at(residual) if n else None, n, _dt(x.dtype), p, seed & (2 ** 64 - 1), at, out.data_ptr() if n else None)
     return out
