@@ -254,38 +254,56 @@ template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * 
     }
 }
 
-// The parts of the keys of each column: out = sum of exp(lse_part - lse) out_part.  32 lanes a column, four elements each.
-template <typename T> __global__ __launch_bounds__(kThreads) void join_parts(AttentionArgs a) {
-    const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R;
-    const int64_t n = (int64_t)a.groups * cols, at = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-    const int d = (threadIdx.x & 31) * 4;
-    if (at >= n) return;                                    // whole groups of 32 lanes
-    // the parts' lse: two lanes' of each
-    const int lane = threadIdx.x & 31;
-    float lses[2], most = -INFINITY;
+// The parts of the keys of a column: out = sum of exp(lse_part - lse) out_part.  32 lanes have a column's elements and eight of its parts, whose loads all leave before the first wait (one after the
+// other, 32 parts of 32 columns took 12 us); GROUPS such groups, joined through the local memory, where there are more.
+constexpr int kMostSplits = 64, kParts = 8;
+template <typename T, int GROUPS> __global__ __launch_bounds__(kThreads) void join_parts(AttentionArgs a) {
+    const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, lane = threadIdx.x & 31, own = threadIdx.x / 32 % GROUPS;
+    const uint32_t n = (uint32_t)a.groups * cols, at = blockIdx.x * (kThreads / 32 / GROUPS) + threadIdx.x / 32 / GROUPS;
+    if (GROUPS == 1 && at >= n) return;
+    const int d = (int)lane * 4;
+    const float* from = a.parts + (int64_t)a.splits * n + (int64_t)at * a.D + (d < a.D ? d : 0);
+    float lses[kParts], most = -INFINITY;
+    f32x4 parts[kParts];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        lses[k] = lane + 32 * k < a.splits ? a.parts[(lane + 32 * k) * n + at] : -INFINITY;
-        most = fmaxf(most, lses[k]);
+    for (int k = 0; k < kParts; ++k) {                      // behind the last part that again, which counts for nothing: no load waits for a branch
+        const int s = (int)own + k * GROUPS;
+        const int64_t row = (int64_t)(s < a.splits ? s : a.splits - 1) * n;
+        const float lse = a.parts[row + at];
+        lses[k] = s < a.splits ? lse : -INFINITY;
+        parts[k] = *reinterpret_cast<const f32x4*>(from + row * a.D);
     }
 #pragma unroll
-    for (int k = 16; k; k >>= 1) most = fmaxf(most, __shfl_xor(most, k, 64));
-    const float* values = a.parts + a.splits * n + at * a.D + d;
+    for (int k = 0; k < kParts; ++k) most = fmaxf(most, lses[k]);
     f32x4 o = {0, 0, 0, 0};
     float sum = 0.0f;
-#pragma unroll 8
-    for (int s = 0; s < a.splits; ++s) {
-        const float lse = __shfl(s < 32 ? lses[0] : lses[1], (threadIdx.x & 32) + (s & 31), 64);
-        const bool some = lse != -INFINITY;                 // what no key was seen for was not written
-        const float by = some ? __builtin_amdgcn_exp2f((lse - most) * kLog2e) : 0.0f;
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {                      // a part that saw no key has zeros
+        const float by = lses[k] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((lses[k] - most) * kLog2e);
         sum += by;
-        const f32x4 part = some && d < a.D ? *reinterpret_cast<const f32x4*>(values + s * n * a.D) : f32x4{0, 0, 0, 0};
-        o += by * part;
+        o += by * parts[k];
+    }
+    if constexpr (GROUPS > 1) {
+        __shared__ float mosts[GROUPS], sums[GROUPS];
+        __shared__ f32x4 values[GROUPS][32];
+        values[own][lane] = o;
+        if (lane == 0) { mosts[own] = most; sums[own] = sum; }
+        __syncthreads();
+        if (own) return;
+#pragma unroll
+        for (int k = 1; k < GROUPS; ++k) most = fmaxf(most, mosts[k]);
+        o = f32x4{0, 0, 0, 0};
+        sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) {
+            const float by = mosts[k] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mosts[k] - most) * kLog2e);
+            sum += by * sums[k];
+            o += by * values[k][lane];
+        }
     }
     o *= sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int group = (int)(at / cols), b = group / a.G;
-    const uint32_t col = (uint32_t)(at - (int64_t)group * cols);
-    const int i = (int)(col / (uint32_t)a.R), h = group % a.G * a.R + (int)(col % (uint32_t)a.R);
+    const uint32_t group = at / cols, col = at - group * cols, i = col / (uint32_t)a.R;
+    const int b = (int)group / a.G, h = (int)group % a.G * a.R + (int)(col - i * (uint32_t)a.R);
     if (d == 0) a.lse[((int64_t)b * a.H + h) * a.Sq + i] = sum == 0.0f ? -INFINITY : most + logf(sum);
     if (d < a.D) put4(reinterpret_cast<T*>(a.out) + (((int64_t)b * a.Sq + i) * a.H + h) * a.D + d, o[0], o[1], o[2], o[3]);
 }
@@ -304,7 +322,7 @@ Cut cut_of(const division_attention& a) {
     const int64_t least = c.few ? (a.dt == DIVISION_BF16 ? 4 : 2) : 4, room = tiles / least, wanted = 512;
     int64_t splits = tasks >= (c.few ? 512 : 256) ? 1 : (wanted + tasks - 1) / tasks;
     if (splits > room) splits = room;
-    if (splits > 64) splits = 64;
+    if (splits > kMostSplits) splits = kMostSplits;
     if (splits < 1) splits = 1;
     c.tiles = (int)least;
     c.splits = (int)splits;
@@ -318,7 +336,8 @@ template <typename T, int DP> int run(const AttentionArgs& args, const Cut& c, i
     CHECKED(launched());
     if (c.splits == 1) return DIVISION_OK;
     const int64_t rows = (int64_t)args.groups * args.Sq * args.R;
-    hipLaunchKernelGGL(join_parts<T>, dim3((uint32_t)((rows + kThreads / 32 - 1) / (kThreads / 32))), dim3(kThreads), 0, st, args);
+    if (c.splits <= kParts) hipLaunchKernelGGL((join_parts<T, 1>), dim3((uint32_t)((rows + 7) / 8)), dim3(kThreads), 0, st, args);
+    else hipLaunchKernelGGL((join_parts<T, kMostSplits / kParts>), dim3((uint32_t)rows), dim3(kThreads), 0, st, args);
     return launched();
 }
 

@@ -21,7 +21,7 @@ struct RotateArgs {
     const int64_t* positions;
     float* parts;
     int64_t T;
-    int heads[2], first, D, pairs, rotated, block;      // pairs: D / 2, the first `rotated` of them turn; block: tokens a workgroup takes at a time
+    int heads[2], block[2], first, D, pairs, rotated;   // pairs: D / 2, the first `rotated` of them turn; block: tokens a workgroup takes at a time
     float eps;
 };
 
@@ -100,7 +100,7 @@ template <typename T, int V, int U, int LANES, bool NEXT, bool BACK> __global__ 
     const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     const bool second = (int)blockIdx.x >= a.first;
     const Side s = a.side[second ? 1 : 0];
-    const int heads = a.heads[second ? 1 : 0], workgroup = blockIdx.x - (second ? a.first : 0), workgroups = second ? (int)gridDim.x - a.first : a.first;
+    const int heads = a.heads[second ? 1 : 0], block = a.block[second ? 1 : 0], workgroup = blockIdx.x - (second ? a.first : 0), workgroups = second ? (int)gridDim.x - a.first : a.first;
     float w[U][2 * V], dw[U][2 * V];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -110,8 +110,8 @@ template <typename T, int V, int U, int LANES, bool NEXT, bool BACK> __global__ 
         if (p < a.pairs) load_weight<V, NEXT>(s, a, p, w[u]);
     }
     const float over = 1.0f / (float)a.D;
-    for (int64_t t0 = (int64_t)workgroup * a.block; t0 < a.T; t0 += (int64_t)workgroups * a.block) {
-        const int n = (int)(a.T - t0 < a.block ? a.T - t0 : a.block), items = n * heads;
+    for (int64_t t0 = (int64_t)workgroup * block; t0 < a.T; t0 += (int64_t)workgroups * block) {
+        const int n = (int)(a.T - t0 < block ? a.T - t0 : block), items = n * heads;
         // every lane goes round as often: the sums over lanes take all of them
         const int rounds = (items + kSlots - 1) / kSlots;
         float x[U][2 * V], g[U][2 * V], rstd = 0.0f;
@@ -252,17 +252,21 @@ int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION
 #define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
 size_t size_of(division_dtype dt) { return dt == DIVISION_BF16 ? 2 : 4; }
 
-constexpr int kMostParts = 1024;                            // workgroups of a backward launch for each tensor, which leave a share each
-int block_of(int64_t T) { return T >= 4096 ? 4 : 1; }
-// workgroups of a tensor of so many heads, of the other's `most`: forward as many as there are blocks of tokens, backward as the shares of the weight's gradient allow
-int grid_of(int64_t T, int64_t heads, int64_t most_heads, bool back) {
+constexpr int kMostParts = 1024;                            // workgroups of a backward launch, which leave a share of a weight's gradient each: what the CUs hold at once
+
+// Tokens that a workgroup takes at a time: about four rounds of its lanes over their heads for each time the angles are taken, one where tokens are few.
+int block_of(int64_t T, int64_t heads, int slots) {
+    int block = (int)(4 * slots / heads);
+    if (block > 16) block = 16;
+    while (block > 1 && T < 1024 * (int64_t)block) block /= 2;
+    return block < 1 ? 1 : block;
+}
+// workgroups of one tensor: forward one for each block of tokens, backward its share of kMostParts
+int grid_of(int64_t T, int64_t heads, int64_t all_heads, int block, bool back) {
     if (T == 0 || heads == 0) return 0;
-    const int64_t n = (T + block_of(T) - 1) / block_of(T);
-    int64_t most = back ? kMostParts : 1 << 20;
-    if (back) {                                             // as many for each head
-        most = most * heads / most_heads;
-        if (most < 64) most = 64;
-    }
+    const int64_t n = (T + block - 1) / block;
+    int64_t most = back ? kMostParts * heads / all_heads : 1 << 20;
+    if (most < 1) most = 1;
     return (int)(n > most ? most : n);
 }
 
@@ -305,12 +309,15 @@ RotateArgs args_of(const division_rotate& a) {
     }
     r.frequencies = a.frequencies; r.positions = a.positions;
     r.T = a.T; r.D = (int)a.D; r.pairs = (int)a.D / 2; r.rotated = (int)a.rotated / 2; r.eps = a.eps;
-    r.block = block_of(a.T);
     return r;
 }
 
-template <typename T, int V, int U, int LANES, bool BACK> int launch(const RotateArgs& a, bool next, uint32_t grid, hipStream_t st) {
-    size_t lds = (size_t)a.block * a.rotated * sizeof(float2);
+template <typename T, int V, int U, int LANES, bool BACK> int launch(RotateArgs& a, bool next, hipStream_t st) {
+    for (int k = 0; k < 2; ++k) a.block[k] = a.heads[k] ? block_of(a.T, a.heads[k], kThreads / LANES) : 0;
+    a.first = grid_of(a.T, a.heads[0], a.heads[0] + a.heads[1], a.block[0], BACK);
+    const uint32_t grid = (uint32_t)(a.first + grid_of(a.T, a.heads[1], a.heads[0] + a.heads[1], a.block[1], BACK));
+    const int block = a.block[0] > a.block[1] ? a.block[0] : a.block[1];
+    size_t lds = (size_t)block * a.rotated * sizeof(float2);
     if (BACK && lds < (size_t)a.D * 4) lds = (size_t)a.D * 4;
     if (next) hipLaunchKernelGGL((rotate<T, V, U, LANES, true, BACK>), dim3(grid), dim3(kThreads), lds, st, a);
     else hipLaunchKernelGGL((rotate<T, V, U, LANES, false, BACK>), dim3(grid), dim3(kThreads), lds, st, a);
@@ -319,16 +326,13 @@ template <typename T, int V, int U, int LANES, bool BACK> int launch(const Rotat
 // Heads whose pairs are whole vectors of sixteen bytes; others element by element
 template <typename T, bool BACK> int run(RotateArgs& a, bool next, hipStream_t st) {
     constexpr int V = 16 / (int)sizeof(T);
-    const int most = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
-    a.first = grid_of(a.T, a.heads[0], most, BACK);
-    const uint32_t grid = (uint32_t)(a.first + grid_of(a.T, a.heads[1], most, BACK));
-    if (a.pairs % V || (!next && a.rotated % V)) return a.pairs <= 64 ? launch<T, 1, 4, 16, BACK>(a, next, grid, st) : launch<T, 1, 4, 64, BACK>(a, next, grid, st);
+    if (a.pairs % V || (!next && a.rotated % V)) return a.pairs <= 64 ? launch<T, 1, 4, 16, BACK>(a, next, st) : launch<T, 1, 4, 64, BACK>(a, next, st);
     const int units = a.pairs / V;
-    if (units <= 4) return launch<T, V, 1, 4, BACK>(a, next, grid, st);
-    if (units <= 8) return launch<T, V, 1, 8, BACK>(a, next, grid, st);
-    if (units <= 16) return launch<T, V, 1, 16, BACK>(a, next, grid, st);
-    if (units <= 32) return launch<T, V, 1, 32, BACK>(a, next, grid, st);
-    if constexpr (sizeof(T) == 4) return launch<T, V, 1, 64, BACK>(a, next, grid, st);
+    if (units <= 4) return launch<T, V, 1, 4, BACK>(a, next, st);
+    if (units <= 8) return launch<T, V, 1, 8, BACK>(a, next, st);
+    if (units <= 16) return launch<T, V, 1, 16, BACK>(a, next, st);
+    if (units <= 32) return launch<T, V, 1, 32, BACK>(a, next, st);
+    if constexpr (sizeof(T) == 4) return launch<T, V, 1, 64, BACK>(a, next, st);
     return DIVISION_EINVAL;
 }
 
@@ -346,7 +350,7 @@ int division_head_norm_rotate(const division_rotate* rotate, void* hip_stream) {
 }
 
 size_t division_head_norm_rotate_backward_workspace(int64_t T, int64_t D) {
-    return T <= 0 || T > 0x7fffffff || D < 2 || D > 512 ? 0 : (size_t)grid_of(T, 1, 1, true) * 2 * D * 4;
+    return T <= 0 || T > 0x7fffffff || D < 2 || D > 512 ? 0 : (size_t)(T < kMostParts ? T + 1 : kMostParts + 1) * D * 4 * 2;
 }
 
 int division_head_norm_rotate_backward(const division_rotate* rotate, const division_rotate_back* back, void* hip_stream) {
@@ -373,9 +377,8 @@ int division_head_norm_rotate_backward(const division_rotate* rotate, const divi
         a.parts = static_cast<float*>(back->workspace);
         CHECKED((f.dt == DIVISION_BF16 ? run<uint16_t, true>(a, f.next, st) : run<float, true>(a, f.next, st)));
         add.parts = a.parts;
-        const int most = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
         add.count[0] = add.first[1] = a.first;
-        add.count[1] = grid_of(f.T, a.heads[1], most, true);
+        add.count[1] = grid_of(f.T, a.heads[1], a.heads[0] + a.heads[1], a.block[1], true);
     }
     add.D = (int)f.D;
     add.blocks = (int)((f.D + 31) / 32);
