@@ -21,3 +21,4 @@ from .layer_operators import Attended, division_attention, division_attention_ba
 from .layer_operators import Rotated, division_head_norm_rotate, division_head_norm_rotate_backward  # noqa: F401,E402
 from .layer_operators import division_dropout_add, division_embedding, division_embedding_backward  # noqa: F401,E402
 from .token_modules import DivisionNormLinear, DivisionRMSNorm, division_token_log_probs  # noqa: F401,E402
+from .layer_modules import DivisionEmbedding, DivisionHeadNormRotation, DivisionResidualDropout, division_token_attention  # noqa: F401,E402
