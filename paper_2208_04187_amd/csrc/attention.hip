@@ -319,7 +319,8 @@ Cut cut_of(const division_attention& a) {
     c.blocks = (cols + (c.few ? 31 : 127)) / (c.few ? 32 : 128);
     c.key_tile = c.few ? 32 : 64;
     const int64_t tiles = (a.Sk + c.key_tile - 1) / c.key_tile, tasks = c.blocks * a.B * a.G;
-    const int64_t least = c.few ? (a.dt == DIVISION_BF16 ? 4 : 2) : 4, room = tiles / least, wanted = 512;
+    // a part has so many tiles at least: fp32 products take long enough for one
+    const int64_t least = a.dt == DIVISION_BF16 ? 4 : c.few ? 2 : 1, room = tiles / least, wanted = 512;
     int64_t splits = tasks >= (c.few ? 512 : 256) ? 1 : (wanted + tasks - 1) / tasks;
     if (splits > room) splits = room;
     if (splits > kMostSplits) splits = kMostSplits;
@@ -373,7 +374,7 @@ int division_attend(const division_attention* attention, void* out, float* lse, 
     if (grid >= (int64_t(1) << 24)) return DIVISION_ERANGE;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, c, grid, st) : run<uint16_t, 128>(args, c, grid, st);
-    return a.D <= 64 ? run<float, 64>(args, c, grid, st) : run<float, 128>(args, c, grid, st);
+    return a.D <= 64 ? run<float, 64>(args, c, grid, st) : a.D <= 96 ? run<float, 96>(args, c, grid, st) : run<float, 128>(args, c, grid, st);
 }
 
 }  // extern "C"

@@ -19,6 +19,7 @@ struct BackArgs : AttentionArgs {
     const char *grad, *o;
     Heads gs;
     char *dq, *dk, *dv;
+    float* sums;                                        // the parts of dk and dv, where the columns are cut
     float* stats;                                       // [group][column][2]: lse in powers of two (infinity where nothing is seen), rowsum(grad out)
     FastDiv by_R;
 };
@@ -48,32 +49,62 @@ template <typename T, int DP> __device__ __forceinline__ void get_column(Operand
 
 constexpr int kThreads = 256;
 
-// Four wavefronts of 32 columns (queries) each share the tiles of the keys and values.
-template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void back_queries(BackArgs a) {
-    constexpr int kTile = Tile<T, DP, KT>::kBytes;
-    __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile];
-    const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+// Adds up what SETS sets of THREADS threads each have in their blocks, into the first set's, through the local memory: a set at a time
+template <int SETS, int THREADS, int N> __device__ __forceinline__ void add_sets(f32x16* o, char* memory, int set, int thread) {
+    f32x4* sums = reinterpret_cast<f32x4*>(memory) + thread;
+#pragma unroll
+    for (int s = 1; s < SETS; ++s) {
+        __syncthreads();
+        if (set == s) {
+#pragma unroll
+            for (int d = 0; d < N; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sums[(4 * d + e) * THREADS] = f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+        }
+        __syncthreads();
+        if (set == 0) {
+#pragma unroll
+            for (int d = 0; d < N; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 more = sums[(4 * d + e) * THREADS];
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) o[d][4 * e + f] += more[f];
+                }
+        }
+    }
+}
+
+// Wavefronts of 32 columns (queries) each, WAVES of them, share the tiles of the keys and values.  SETS such take every SETS-th tile each.
+template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_bounds__(64 * WAVES * SETS, sizeof(T) == 2 ? 2 : 1) void back_queries(BackArgs a) {
+    constexpr int kTile = Tile<T, DP, KT>::kBytes, kSet = 64 * WAVES, kCols = 32 * WAVES;
+    static_assert(SETS == 1 || kSet * (DP / 32) * 64 <= 4 * SETS * kTile, "a set's blocks in place of the tiles");
+    __shared__ __attribute__((aligned(16))) char memory[SETS * 4 * kTile];
+    const int set = SETS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kSet), thread = threadIdx.x % kSet, lane = thread & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    char* mine = memory + set * 4 * kTile;
     const int group = blockIdx.x % a.groups, block = a.blocks - 1 - blockIdx.x / a.groups;
     const int b = group / a.G, g = group % a.G;
-    const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * 128u;
+    const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * kCols;
     const uint32_t wave_col = first_col + 32 * wave, col = wave_col + (lane & 31);
     const Seen seen = seen_of(a, b);
-    const uint32_t last_col = min(first_col + 127u, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
+    const uint32_t last_col = min(first_col + kCols - 1, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
     const int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
     const bool works = wave_col < cols, there = col < cols;
     const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
-    const int wave_from = seen.from(qa), whole_from = seen.from(qb), whole_to = seen.to(qa), wave_to = works ? seen.to(qb) : 0;
+    const int whole_from = seen.from(qb), whole_to = seen.to(qa);
     const int i = (int)(min(col, cols - 1) / (uint32_t)a.R), r = (int)(min(col, cols - 1) % (uint32_t)a.R);
     const int from = seen.from(i), to = there ? max(from, seen.to(i)) : from;
     const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
     const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     const int row_bytes = a.D * (int)sizeof(T);
-    const auto fetch = [&](int t) {
+    const auto fetch = [&](int t, int at) {
         const int left = seen.keys - t * KT;
-        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
-        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
+        char* to = mine + at * 2 * kTile;
+        Tile<T, DP, KT>::template fill<kSet>(to, k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
+        Tile<T, DP, KT>::template fill<kSet>(to + kTile, v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
     };
-    if (lo < hi) fetch(lo);
+    if (lo + set < hi) fetch(lo + set, 0);
     Operand<T> q[DP / 16], grad[DP / 16];
     get_column<T, DP>(q, a.q + b * a.qs.batch + row_offset(a.qs, i, g * a.R + r), there, row_bytes, half);
     get_column<T, DP>(grad, a.grad + b * a.gs.batch + row_offset(a.gs, i, g * a.R + r), there, row_bytes, half);
@@ -93,18 +124,20 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     }
     float exponent = there ? a.lse[((int64_t)b * a.H + g * a.R + r) * a.Sq + i] * kLog2e : INFINITY;
     if (exponent == -INFINITY) exponent = INFINITY;
-    if (there && half == 0) *reinterpret_cast<f32x2*>(a.stats + ((int64_t)group * cols + col) * 2) = f32x2{exponent, delta};
+    if (set == 0 && there && half == 0) *reinterpret_cast<f32x2*>(a.stats + ((int64_t)group * cols + col) * 2) = f32x2{exponent, delta};
     const float scale2 = a.scale * kLog2e;
     f32x16 dq[DP / 32];
 #pragma unroll
     for (auto& x : dq) x = (f32x16)(0.0f);
     loads_done();
     __syncthreads();
-    for (int t = lo; t < hi; ++t) {
-        if (t + 1 < hi) fetch(t + 1);
+    int at = 0;
+    for (int t0 = lo; t0 < hi; t0 += SETS, at ^= 1) {
+        const int t = t0 + set;
+        if (t + SETS < hi) fetch(t + SETS, at ^ 1);
         const int j0 = t * KT;
-        const char *kt = tiles[t & 1][0], *vt = tiles[t & 1][1];
-        {
+        const char *kt = mine + at * 2 * kTile, *vt = kt + kTile;
+        if (SETS == 1 || t < hi) {
             const bool whole = j0 >= whole_from && j0 + KT <= whole_to;
 #pragma unroll
             for (int n = 0; n < KT / 32; ++n) {
@@ -139,38 +172,47 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
         loads_done();
         __syncthreads();
     }
+    if constexpr (SETS > 1) {
+        add_sets<SETS, kSet, DP / 32>(dq, memory, set, thread);
+        if (set) return;
+    }
     if (there) put_column<T, DP>(reinterpret_cast<T*>(a.dq) + row * a.D, dq, a.scale, a.D, half);
 }
 
-// Wavefronts of 32 keys each, four of them for 128 keys, share the tiles of the columns (queries of all heads that share the keys) and their gradients.  SETS such fours take every SETS-th
-// tile each and are added up at the end: with two there are always two wavefronts a SIMD, one with the matrix unit while the other takes exponentials.  VALUES: the values wait in the
+// Wavefronts of 32 keys each, WAVES of them, share the tiles of the columns (queries of all heads that share the keys) and their gradients.  SETS such take every SETS-th
+// tile each: with two there are always two wavefronts a SIMD, one with the matrix unit while the other takes exponentials.  VALUES: the values wait in the
 // local memory, not in registers.
-template <typename T, int DP, int CT, int SETS, int STAGES, bool VALUES> __global__ __launch_bounds__(kThreads * SETS) void back_keys(BackArgs a) {
+template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global__ __launch_bounds__(64 * WAVES * SETS) void back_keys(BackArgs a) {
+    constexpr int kSet = 64 * WAVES, kKeys = 32 * WAVES;
     typedef Tile<T, DP, CT> Columns;
-    typedef Tile<T, DP, 128> Values;
-    constexpr int kTiles = SETS * STAGES * 2 * Columns::kBytes, kLoads = 2 * Columns::kBytes / 16 / kThreads, kSum = 4 * 64 * (DP / 32) * 16 * 4;
-    static_assert(SETS == 1 || kSum <= kTiles + (VALUES ? Values::kBytes : 0), "one set's blocks in place of the tiles");
+    typedef Tile<T, DP, kKeys> Values;
+    constexpr int kTiles = SETS * 4 * Columns::kBytes;
+    static_assert(SETS == 1 || kSet * (DP / 32) * 64 <= kTiles + (VALUES ? Values::kBytes : 0), "a set's blocks in place of the tiles");
     __shared__ __attribute__((aligned(16))) char memory[kTiles + (VALUES ? Values::kBytes : 0)];
-    __shared__ __attribute__((aligned(16))) float stats[SETS][STAGES][CT][2];
+    __shared__ __attribute__((aligned(16))) float stats[SETS][2][CT][2];
     static_assert(CT == 32, "a tile's numbers are one load of a wavefront");
-    const int set = SETS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads), thread = threadIdx.x % kThreads, lane = thread & 63, half = lane >> 5;
+    const int set = SETS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kSet), thread = threadIdx.x % kSet, lane = thread & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
-    const int group = blockIdx.x % a.groups, block = blockIdx.x / a.groups;
+    const int group = blockIdx.x % a.groups, split = blockIdx.x / a.groups % a.splits, block = blockIdx.x / a.groups / a.splits;
     const int b = group / a.G, g = group % a.G;
     const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R;
     const Seen seen = seen_of(a, b);
-    const int first = block * 128, wave_key = first + 32 * wave, key = wave_key + (lane & 31);
-    const int last = min(first + 127, seen.keys - 1), wave_last = min(wave_key + 31, seen.keys - 1);
+    const int first = block * kKeys, wave_key = first + 32 * wave, key = wave_key + (lane & 31);
+    const int last = min(first + kKeys - 1, seen.keys - 1);
     // the columns of the workgroup, of the wavefront and of the lane: those of whole queries
     const bool any = first < seen.keys, works = wave_key < seen.keys, there = key < seen.keys;
-    const int lo = any ? seen.query_from(first) * a.R / CT : 0, hi = any ? (seen.query_to(last) * a.R + CT - 1) / CT : 0;
-    const int wave_from = seen.query_from(min(wave_key, a.Sk - 1)) * a.R, wave_to = works ? seen.query_to(wave_last) * a.R : 0;
+    int lo = any ? seen.query_from(first) * a.R / CT : 0, hi = any ? (seen.query_to(last) * a.R + CT - 1) / CT : 0;
+    if (a.splits > 1) {                                     // equal parts of the columns that these keys are seen by
+        const int each = max((hi - lo + a.splits - 1) / a.splits, a.tiles);
+        lo += split * each;
+        hi = min(lo + each, hi);
+    }
     const int whole_from = seen.query_from(min(wave_key + 31, a.Sk - 1)) * a.R, whole_to = works && wave_key + 31 < seen.keys ? seen.query_to(wave_key) * a.R : 0;
     const int from = there ? seen.query_from(key) * a.R : 0, to = there ? max(from, seen.query_to(key) * a.R) : 0;
     const char* q = a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head;
     const char* gr = a.grad + b * a.gs.batch + (int64_t)g * a.R * a.gs.head;
     const int row_bytes = a.D * (int)sizeof(T);
-    char* mine = memory + set * STAGES * 2 * Columns::kBytes;
+    char* mine = memory + set * 4 * Columns::kBytes;
     const auto fetch = [&](int t, int at) {
         const uint32_t c0 = (uint32_t)t * CT, i0 = c0 / (uint32_t)a.R, r0 = c0 - i0 * (uint32_t)a.R;
         const int left = (int)(cols - c0);
@@ -181,16 +223,14 @@ template <typename T, int DP, int CT, int SETS, int STAGES, bool VALUES> __globa
         if (wave == 0) {                                    // columns behind the last have zeros: their rows are zeros too
             load_lds4(buffer(a.stats + ((int64_t)group * cols + c0) * 2, 4u * 2 * (uint32_t)min(left, CT)), stats[set][at], (uint32_t)lane * 4);
         }
-        Columns::template fill<kThreads>(to, q + (int64_t)i0 * a.qs.token, left, row_bytes, thread, offset(a.qs));
-        Columns::template fill<kThreads>(to + Columns::kBytes, gr + (int64_t)i0 * a.gs.token, left, row_bytes, thread, offset(a.gs));
+        Columns::template fill<kSet>(to, q + (int64_t)i0 * a.qs.token, left, row_bytes, thread, offset(a.qs));
+        Columns::template fill<kSet>(to + Columns::kBytes, gr + (int64_t)i0 * a.gs.token, left, row_bytes, thread, offset(a.gs));
     };
-#pragma unroll
-    for (int n = 0; n < STAGES - 1; ++n)
-        if (lo + n * SETS + set < hi) fetch(lo + n * SETS + set, n);
+    if (lo + set < hi) fetch(lo + set, 0);
     char* values = memory + kTiles;
     const char* v_head = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     if constexpr (VALUES)
-        Values::template fill<kThreads * SETS>(values, v_head + (int64_t)first * a.vs.token, seen.keys - first, row_bytes, threadIdx.x, [&](int row) { return row * a.vs.token; });
+        Values::template fill<kSet * SETS>(values, v_head + (int64_t)first * a.vs.token, seen.keys - first, row_bytes, threadIdx.x, [&](int row) { return row * a.vs.token; });
     Operand<T> k[DP / 16], v[VALUES ? 1 : DP / 16];
     get_column<T, DP>(k, a.k + b * a.ks.batch + row_offset(a.ks, key, g), there, row_bytes, half);
     if constexpr (!VALUES) get_column<T, DP>(v, v_head + (int64_t)key * a.vs.token, there, row_bytes, half);
@@ -203,10 +243,9 @@ template <typename T, int DP, int CT, int SETS, int STAGES, bool VALUES> __globa
     loads_done();
     __syncthreads();
     int at = 0;
-    for (int t0 = lo; t0 < hi; t0 += SETS, at = at + 1 == STAGES ? 0 : at + 1) {
+    for (int t0 = lo; t0 < hi; t0 += SETS, at ^= 1) {
         const int t = t0 + set;
-        const bool more = t + (STAGES - 1) * SETS < hi;
-        if (more) fetch(t + (STAGES - 1) * SETS, at == 0 ? STAGES - 1 : at - 1);
+        if (t + SETS < hi) fetch(t + SETS, at ^ 1);
         const int c0 = t * CT;
         const char *qt = mine + at * 2 * Columns::kBytes, *gt = qt + Columns::kBytes;
         if (t < hi) {
@@ -252,36 +291,20 @@ template <typename T, int DP, int CT, int SETS, int STAGES, bool VALUES> __globa
                 }
             }
         }
-        // the next tile is there when all but the newest's loads are
-        if (more && STAGES > 2) loads_done<(STAGES - 2) * kLoads>();
-        else loads_done();
+        loads_done();
         __syncthreads();
     }
-    if constexpr (SETS == 2) {
-        f32x4* sums = reinterpret_cast<f32x4*>(memory) + thread;
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            f32x16* o = part ? dv : dk;
-            if (part) __syncthreads();
-            if (set) {
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sums[(4 * d + e) * kThreads] = f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
-            }
-            __syncthreads();
-            if (!set) {
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const f32x4 more = sums[(4 * d + e) * kThreads];
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) o[d][4 * e + f] += more[f];
-                    }
-            }
-        }
+    if constexpr (SETS > 1) {
+        add_sets<SETS, kSet, DP / 32>(dk, memory, set, thread);
+        add_sets<SETS, kSet, DP / 32>(dv, memory, set, thread);
         if (set) return;
+    }
+    if (a.splits > 1) {                                     // [split][group][key][2][D]
+        if (key >= a.Sk) return;
+        float* row = a.sums + (((int64_t)split * a.groups + group) * a.Sk + key) * 2 * a.D;
+        put_column<float, DP>(row, dk, a.scale, a.D, half);
+        put_column<float, DP>(row + a.D, dv, 1.0f, a.D, half);
+        return;
     }
     if (key >= a.Sk) return;
     const int64_t row = (((int64_t)b * a.Sk + key) * a.G + g) * a.D;
@@ -289,25 +312,70 @@ template <typename T, int DP, int CT, int SETS, int STAGES, bool VALUES> __globa
     put_column<T, DP>(reinterpret_cast<T*>(a.dv) + row, dv, 1.0f, a.D, half);
 }
 
+// The parts of the keys' gradients, in their order: four elements of a row of dk or dv a thread
+template <typename T> __global__ __launch_bounds__(kThreads) void add_key_parts(BackArgs a) {
+    const int each = a.D / 2;                               // of four elements of dk and of dv
+    const int64_t n = (int64_t)a.groups * a.Sk, at = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = at / each;
+    if (row >= n) return;
+    const int e = (int)(at - row * each) * 4;
+    const float* from = a.sums + row * 2 * a.D + e;
+    f32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) o += *reinterpret_cast<const f32x4*>(from + s * n * 2 * a.D);
+    const int64_t group = row / a.Sk, key = row - group * a.Sk, b = group / a.G, g = group - b * a.G;
+    T* out = reinterpret_cast<T*>(e < a.D ? a.dk : a.dv) + ((b * a.Sk + key) * a.G + g) * a.D + (e < a.D ? e : e - a.D);
+    put4(out, o[0], o[1], o[2], o[3]);
+}
+
 // ------------------------------------------------------------------ host side
 
-size_t stats_bytes(const division_attention& a) { return (size_t)(a.B * a.Sq * a.H) * 8; }
+size_t stats_bytes(const division_attention& a) { return ((size_t)(a.B * a.Sq * a.H) * 8 + 15) / 16 * 16; }
+
+// fp32 products are slow enough for small workgroups to pay: 64 columns or keys, their tiles shared by two (four) sets.  (2 x 1531 tokens, 12 heads of 64, window 256: SETS_F32.)
+constexpr int kColumnTile = 32;
+template <typename T, int DP> struct Shape {
+    static constexpr bool kSmall = sizeof(T) == 4 && DP <= 64;
+    static constexpr int kKeyTile = sizeof(T) == 2 ? 64 : 32, kQueryWaves = sizeof(T) == 2 ? 4 : 2, kQuerySets = sizeof(T) == 2 ? 1 : 2;
+    static constexpr int kKeyWaves = kSmall ? 2 : 4, kKeySets = kSmall ? 4 : sizeof(T) == 2 ? 2 : 1;
+    static constexpr bool kValues = sizeof(T) == 2 && DP == 128;
+};
+int keys_of_workgroup(const division_attention& a) { return a.dt != DIVISION_BF16 && a.D <= 64 ? 64 : 128; }
+// Parts of the columns of one workgroup's keys: where few heads of keys leave CUs without work, as many as make two workgroups a CU, of 16 tiles at least.  (One sequence of 2048, 32 heads on 4
+// of keys: 484 us in one part, SPLIT_US so.)
+constexpr int kLeastTiles = 16;
+int splits_of(const division_attention& a) {
+    const int64_t keys = keys_of_workgroup(a), tasks = (a.Sk + keys - 1) / keys * a.B * a.G, tiles = (a.Sq * (a.H / a.G) + kColumnTile - 1) / kColumnTile;
+    if (tasks == 0 || tasks >= 256) return 1;
+    int64_t splits = (512 + tasks - 1) / tasks;
+    if (splits > tiles / kLeastTiles) splits = tiles / kLeastTiles;
+    return splits < 1 ? 1 : splits > 32 ? 32 : (int)splits;
+}
+size_t sums_bytes(const division_attention& a) {
+    const int splits = splits_of(a);
+    return splits > 1 ? (size_t)splits * a.B * a.G * a.Sk * 2 * a.D * 4 : 0;
+}
 
 template <typename T, int DP> int run(BackArgs& args, hipStream_t st) {
+    typedef Shape<T, DP> S;
     if (args.Sq > 0) {
-        const int64_t blocks = ((int64_t)args.Sq * args.R + 127) / 128;
-        if (blocks * args.groups >= (int64_t(1) << 24)) return DIVISION_ERANGE;
+        constexpr int kCols = 32 * S::kQueryWaves;
+        const int64_t blocks = ((int64_t)args.Sq * args.R + kCols - 1) / kCols;
+        if (blocks * args.groups >= (int64_t(1) << 23)) return DIVISION_ERANGE;
         args.blocks = (int)blocks;
-        hipLaunchKernelGGL((back_queries<T, DP, 64>), dim3((uint32_t)(blocks * args.groups)), dim3(kThreads), 0, st, args);
+        hipLaunchKernelGGL((back_queries<T, DP, S::kKeyTile, S::kQueryWaves, S::kQuerySets>), dim3((uint32_t)(blocks * args.groups)), dim3(64 * S::kQueryWaves * S::kQuerySets), 0, st, args);
         CHECKED(launched());
     }
     if (args.Sk > 0) {
-        const int64_t blocks = ((int64_t)args.Sk + 127) / 128;
-        if (blocks * args.groups >= (int64_t(1) << 24)) return DIVISION_ERANGE;
-        args.blocks = (int)blocks;
-        constexpr bool kPair = sizeof(T) == 2 || DP == 64;
-        hipLaunchKernelGGL((back_keys<T, DP, 32, kPair ? 2 : 1, 2, sizeof(T) == 2 && DP == 128>), dim3((uint32_t)(blocks * args.groups)), dim3(kPair ? 2 * kThreads : kThreads), 0, st, args);
+        constexpr int kKeys = 32 * S::kKeyWaves;
+        const int64_t grid = ((int64_t)args.Sk + kKeys - 1) / kKeys * args.groups * args.splits;
+        if (grid >= (int64_t(1) << 23)) return DIVISION_ERANGE;
+        hipLaunchKernelGGL((back_keys<T, DP, kColumnTile, S::kKeyWaves, S::kKeySets, S::kValues>), dim3((uint32_t)grid), dim3(64 * S::kKeyWaves * S::kKeySets), 0, st, args);
         CHECKED(launched());
+        if (args.splits > 1) {
+            const int64_t pieces = (int64_t)args.groups * args.Sk * (args.D / 2);
+            hipLaunchKernelGGL(add_key_parts<T>, dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, args);
+            CHECKED(launched());
+        }
     }
     return DIVISION_OK;
 }
@@ -318,7 +386,7 @@ extern "C" {
 
 size_t division_attention_backward_workspace(const division_attention* attention) {
     if (!attention || check_attention(*attention) != DIVISION_OK) return 0;
-    return stats_bytes(*attention);
+    return stats_bytes(*attention) + sums_bytes(*attention);
 }
 
 int division_attention_backward(const division_attention* attention, const division_attention_back* back, void* hip_stream) {
@@ -328,10 +396,11 @@ int division_attention_backward(const division_attention* attention, const divis
     CHECKED(check_attention(a));
     if (a.B == 0 || (a.Sq == 0 && a.Sk == 0)) return DIVISION_OK;
     const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4;
-    if ((a.Sq > 0 && (!a.q || !w.grad_out || !w.out || !w.lse || !w.grad_q || !w.workspace)) || (a.Sk > 0 && (!w.grad_k || !w.grad_v || !a.k || !a.v))) return DIVISION_EINVAL;
+    if ((a.Sq > 0 && (!a.q || !w.grad_out || !w.out || !w.lse || !w.grad_q)) || (a.Sk > 0 && (!w.grad_k || !w.grad_v || !a.k || !a.v))) return DIVISION_EINVAL;
+    if (!w.workspace && stats_bytes(a) + sums_bytes(a)) return DIVISION_EINVAL;
     if (!aligned(w.out, 16) || !aligned(w.lse, 4) || !aligned(w.grad_q, 16) || !aligned(w.grad_k, 16) || !aligned(w.grad_v, 16) || !aligned(w.workspace, 16)) return DIVISION_EALIGN;
     if (a.Sq > 0) CHECKED(check_heads(w.grad_out, w.grad_out_strides, a.B, a.H, es));
-    if (w.workspace_bytes < stats_bytes(a)) return DIVISION_ESIZE;
+    if (w.workspace_bytes < stats_bytes(a) + sums_bytes(a)) return DIVISION_ESIZE;
     BackArgs args{};
     static_cast<AttentionArgs&>(args) = args_of(a);
     args.grad = static_cast<const char*>(w.grad_out);
@@ -340,6 +409,9 @@ int division_attention_backward(const division_attention* attention, const divis
     args.lse = const_cast<float*>(w.lse);
     args.dq = static_cast<char*>(w.grad_q); args.dk = static_cast<char*>(w.grad_k); args.dv = static_cast<char*>(w.grad_v);
     args.stats = static_cast<float*>(w.workspace);
+    args.splits = splits_of(a);
+    args.tiles = kLeastTiles;
+    args.sums = reinterpret_cast<float*>(static_cast<char*>(w.workspace) + stats_bytes(a));
     args.by_R = make_fastdiv((uint32_t)args.R);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, st) : run<uint16_t, 128>(args, st);

@@ -150,6 +150,18 @@ def test_masks(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [(1, 1100, 70, 4, 2, 64), (2, 700, 130, 6, 2, 128), (1, 300, 33, 40, 1, 24), (3, 520, 520, 2, 1, 96)])
+def test_many_queries_of_few_keys_heads(size, dtype):
+    """Whose columns are cut into parts that are added up"""
+    x = _inputs(*size, dtype, seed=12)
+    B, Sq, Sk = size[:3]
+    lengths = [Sk // 2 + 1, 0, Sk - 1][:B]
+    _check(*x)
+    _check(*x, causal=True, lengths=lengths)
+    _check(*x, causal=True, window=40, starts=[Sk - 9, 3, -Sq // 2][:B])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_scales_and_large_scores(dtype):
     x = _inputs(2, 40, 70, 4, 2, 64, dtype, seed=2)
     _check(*x, scale=1.0)
