@@ -120,8 +120,11 @@ template <typename T, int DP, int ROWS> struct Tile {
 // where the memory is the bound (32 tokens over caches of up to 8192 keys: LINES_US).
 template <typename T, int DP, int ROWS> struct RowTile {
     static constexpr int kRowBytes = DP * (int)sizeof(T), kPieces = kRowBytes / 16, kBytes = ROWS * kRowBytes;
+    // below kTurns, of which a row has a whole number: an exchanged piece stays in its row
+    static constexpr int kTurns = sizeof(T) == 2 && kPieces == 16 ? 16 : 8;
+    static_assert(kPieces % kTurns == 0, "pieces stay in their row");
     static __device__ __forceinline__ int turn(int row) {
-        if constexpr (sizeof(T) == 4) return (row >> 2 & 1) << 3 | (row & 3) << 1 | (row >> 3 & 1);
+        if constexpr (sizeof(T) == 4) return (row & 3) << 1 | (row >> 2 & 1);
         else if constexpr (kPieces == 16) return (row & 3) << 2 | (row >> 2 & 3);
         else return (row >> 1 & 1) << 2 | (row >> 2 & 3);
     }

@@ -119,7 +119,7 @@ def _check(q, k, v, g, causal=False, window=0, lengths=None, starts=None, scale=
 # batch, queries, keys, heads, key heads, features
 SIZES = [(1, 1, 1, 1, 1, 8), (2, 1, 1, 4, 2, 64), (1, 2, 2, 1, 1, 128), (2, 31, 31, 2, 1, 64), (1, 32, 32, 3, 3, 40), (2, 33, 33, 4, 2, 128), (1, 63, 65, 2, 2, 64), (2, 65, 64, 6, 2, 72),
          (1, 129, 129, 2, 1, 128), (1, 200, 77, 5, 1, 16), (1, 77, 200, 5, 1, 96), (1, 1, 300, 8, 2, 128), (2, 1, 1000, 32, 1, 64), (1, 1, 33, 33, 1, 24), (1, 6, 515, 5, 1, 128),
-         (2, 7, 515, 10, 2, 64), (1, 8, 700, 8, 2, 104), (1, 300, 1, 2, 1, 64), (1, 1, 4097, 4, 2, 128), (1, 257, 600, 2, 2, 120)]
+         (2, 7, 515, 10, 2, 64), (1, 1, 500, 4, 1, 96), (2, 2, 70, 6, 3, 88), (1, 8, 700, 8, 2, 104), (1, 300, 1, 2, 1, 64), (1, 1, 4097, 4, 2, 128), (1, 257, 600, 2, 2, 120)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
