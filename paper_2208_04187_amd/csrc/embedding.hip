@@ -122,11 +122,12 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
             const int leader = __builtin_ctzll(left);
             const uint32_t theirs = (uint32_t)__builtin_amdgcn_readlane((int)row, leader);
             const uint64_t same = __ballot(row == theirs);
-            const uint32_t begin = counts[theirs * kOrderWaves + wave];
+            // the wavefront's own counter: one lane moves it on (a fence in the place of the atomic waits for the stores too, a microsecond a time)
+            uint32_t begin = 0;
+            if (lane == leader) begin = atomicAdd(&counts[theirs * kOrderWaves + wave], (uint32_t)__builtin_popcountll(same));
+            begin = (uint32_t)__builtin_amdgcn_readlane((int)begin, leader);
             if (row == theirs) a.order[begin + __builtin_popcountll(same & ((1ull << lane) - 1))] = t;
-            if (lane == leader) counts[theirs * kOrderWaves + wave] = begin + __builtin_popcountll(same);
             left &= ~same;
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // the next token of this row may be another lane's
         }
     };
 #pragma unroll
@@ -152,6 +153,7 @@ struct SumArgs {
     uint32_t T, part;                                       // part: tokens that a wavefront adds up at most; a row of more is added up in parts
     float scale;
     int add, columns;                                       // columns: pieces of 64 * kSize * P elements of a row
+    int64_t count;                                          // parts of the tokens, where there are more than one's
 };
 
 // P vectors a lane of a row's columns, 64 lanes' vectors one behind the other
@@ -196,14 +198,30 @@ template <typename T, int P> struct Row {
     }
 };
 
-// Parts of rows of many tokens: a wavefront has `part` sorted tokens and a piece of the columns.  Of such rows at most two have tokens among them.
-template <typename T, int P> __global__ __launch_bounds__(kThreads) void sum_parts(SumArgs a) {
+// A row's sum goes out: scaled, rounded, added to what is there
+template <typename T, typename O, int P> __device__ __forceinline__ void put_row(const SumArgs& a, int64_t row, int64_t c, Row<T, P>& sum) {
     typedef Unit<T> U;
-    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-    const uint32_t part = (uint32_t)(item / a.columns), begin = part * a.part, total = a.starts[a.V];
+    typedef Some<O, U::kSize> Out;
+    O* out = static_cast<O*>(a.out) + row * a.D;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+#pragma unroll
+        for (int i = 0; i < U::kSize; ++i) sum.v[p][i] *= a.scale;
+        if (a.add) {
+            const Out q = load_some<Out>(out, c + p * 64 * U::kSize, a.D);
+#pragma unroll
+            for (int i = 0; i < U::kSize; ++i) sum.v[p][i] += q[i];
+        }
+        store_some<Out>(out, c + p * 64 * U::kSize, a.D, sum.v[p]);
+    }
+}
+
+// Parts of rows of many tokens: a wavefront has `part` sorted tokens and a piece of the columns.  Of such rows at most two have tokens among them.
+template <typename T, int P> __device__ __forceinline__ void sum_part(const SumArgs& a, uint32_t part, int64_t c) {
+    typedef Unit<T> U;
+    const uint32_t begin = part * a.part, total = a.starts[a.V];
     if (begin >= total) return;
     const uint32_t end = min(begin + a.part, total);
-    const int64_t c = ((item % a.columns) * 64 * P + (threadIdx.x & 63)) * U::kSize;
     const int64_t rows[2] = {a.ids[a.order[begin]], a.ids[a.order[end - 1]]};
     for (int k = 0; k < 2; ++k) {
         if (k && rows[1] == rows[0]) break;
@@ -220,53 +238,74 @@ template <typename T, int P> __global__ __launch_bounds__(kThreads) void sum_par
     }
 }
 
-// The table's gradient: a wavefront has kRows rows, whose tokens lie one behind the other in the order, and a piece of the columns.
+// The table's gradient: the first wavefronts have parts of rows of many tokens, each of the others kRows rows, whose tokens lie one behind the other in the order; all a piece of the columns.
 constexpr int kRows = 4;
 template <typename T, typename O, int P> __global__ __launch_bounds__(kThreads) void sum_tokens(SumArgs a) {
     typedef Unit<T> U;
-    typedef Some<O, U::kSize> Out;
-    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), row0 = item / a.columns * kRows;
+    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), which = item / a.columns;
+    const int64_t c = ((item - which * a.columns) * 64 * P + (threadIdx.x & 63)) * U::kSize;
+    if (which < a.count) {
+        sum_part<T, P>(a, (uint32_t)which, c);
+        return;
+    }
+    const int64_t row0 = (which - a.count) * kRows;
     if (row0 >= a.V) return;
-    const int64_t c = ((item % a.columns) * 64 * P + (threadIdx.x & 63)) * U::kSize;
     uint32_t starts[kRows + 1];
 #pragma unroll
     for (int r = 0; r <= kRows; ++r) starts[r] = a.starts[row0 + r < a.V ? row0 + r : a.V];
     for (int r = 0; r < kRows; ++r) {
         if (row0 + r >= a.V) return;
-        const uint32_t from = starts[r], to = starts[r + 1];
-        if (a.add && from == to) continue;
+        const uint32_t n = starts[r + 1] - starts[r];
+        if (n > a.part || (a.add && n == 0)) continue;
         Row<T, P> sum;
         sum.zero();
-        if (to - from <= a.part) {
-            sum.add(a, from, to, c);
-        } else {
-            const uint32_t first = from / a.part, last = (to - 1) / a.part;
-#pragma unroll 4
-            for (uint32_t part = first; part <= last; ++part) {
-                const float* q = a.parts + ((int64_t)part * 2 + (from >= part * a.part)) * a.D;
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int i = 0; i < U::kSize; i += 4) {
-                        const Unit<float> u = load_some<Unit<float>>(q, c + p * 64 * U::kSize + i, a.D);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) sum.v[p][i + k] += u[k];
-                    }
-            }
-        }
-        O* out = static_cast<O*>(a.out) + (row0 + r) * a.D;
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-#pragma unroll
-            for (int i = 0; i < U::kSize; ++i) sum.v[p][i] *= a.scale;
-            if (a.add) {
-                const Out q = load_some<Out>(out, c + p * 64 * U::kSize, a.D);
-#pragma unroll
-                for (int i = 0; i < U::kSize; ++i) sum.v[p][i] += q[i];
-            }
-            store_some<Out>(out, c + p * 64 * U::kSize, a.D, sum.v[p]);
-        }
+        sum.add(a, starts[r], starts[r + 1], c);
+        put_row<T, O, P>(a, row0 + r, c, sum);
     }
+}
+
+// The rows of many tokens, from their parts: the workgroup of the part that such a row begins in has it, a wavefront every fourth part
+template <typename T, typename O, int P> __global__ __launch_bounds__(kThreads) void join_rows(SumArgs a) {
+    typedef Unit<T> U;
+    constexpr int kWaves = kThreads / 64;
+    __shared__ float sums[kWaves - 1][P * U::kSize][64];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), lane = threadIdx.x & 63;
+    const uint32_t part = blockIdx.x / a.columns, begin = part * a.part, total = a.starts[a.V];
+    if (begin >= total) return;
+    const int64_t row = a.ids[a.order[min(begin + a.part, total) - 1]];             // it goes on behind the part
+    const uint32_t from = a.starts[row], to = a.starts[row + 1];
+    if (to - from <= a.part || from < begin) return;
+    const int64_t c = ((int64_t)(blockIdx.x - part * a.columns) * 64 * P + lane) * U::kSize;
+    Row<T, P> sum;
+    sum.zero();
+    const uint32_t last = (to - 1) / a.part;
+#pragma unroll 4
+    for (uint32_t k = part + wave; k <= last; k += kWaves) {
+        const float* q = a.parts + ((int64_t)k * 2 + (k == part)) * a.D;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < U::kSize; i += 4) {
+                const Unit<float> u = load_some<Unit<float>>(q, c + p * 64 * U::kSize + i, a.D);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) sum.v[p][i + n] += u[n];
+            }
+    }
+    if (wave) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < U::kSize; ++i) sums[wave - 1][p * U::kSize + i][lane] = sum.v[p][i];
+    }
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int w = 0; w < kWaves - 1; ++w)
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < U::kSize; ++i) sum.v[p][i] += sums[w][p * U::kSize + i][lane];
+    put_row<T, O, P>(a, row, c, sum);
 }
 
 // ------------------------------------------------------------------ host side
@@ -340,24 +379,29 @@ int division_embedding_backward(const division_embedding_back* back, void* hip_s
     const int64_t workgroups = (b.V + rows - 1) / rows;
     if (workgroups * kOrderThreads >= (int64_t(1) << 32)) return DIVISION_ERANGE;
     const uint32_t part = part_of(b.T);
-    SumArgs s{b.grad, b.ids, o.order, o.starts, reinterpret_cast<float*>(ws + at.parts), b.grad_table, b.grad_stride, b.V, b.D, (uint32_t)b.T, part, b.scale, b.add, 0};
+    SumArgs s{b.grad, b.ids, o.order, o.starts, reinterpret_cast<float*>(ws + at.parts), b.grad_table, b.grad_stride, b.V, b.D, (uint32_t)b.T, part, b.scale, b.add, 0, 0};
     const bool wide = b.D > 64 * (int64_t)(16 / size_of(b.dt));
     const int64_t each = 64 * (int64_t)(16 / size_of(b.dt)) * (wide ? 2 : 1), columns = (b.D + each - 1) / each;
     s.columns = (int)columns;
-    const int64_t parts = ((b.T + part - 1) / part * columns + 3) / 4, grid = ((b.V + kRows - 1) / kRows * columns + 3) / 4;
-    if (parts >= kMostWorkgroups || grid >= kMostWorkgroups) return DIVISION_ERANGE;
+    s.count = b.T > part ? (b.T + part - 1) / part : 0;
+    const int64_t joins = s.count * columns, grid = ((s.count + (b.V + kRows - 1) / kRows) * columns + 3) / 4;
+    if (grid >= kMostWorkgroups || joins >= kMostWorkgroups) return DIVISION_ERANGE;
     hipLaunchKernelGGL(order_tokens, dim3((uint32_t)workgroups), dim3(kOrderThreads), (size_t)rows * kOrderWaves * 4, st, o);
     CHECKED(launched());
     const bool half = b.dt == DIVISION_BF16;
-    void (*kernel)(SumArgs);
-    if (b.T > part) {
-        kernel = half ? (wide ? sum_parts<uint16_t, 2> : sum_parts<uint16_t, 1>) : wide ? sum_parts<float, 2> : sum_parts<float, 1>;
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)parts), dim3(kThreads), 0, st, s);
-        CHECKED(launched());
+    void (*sum)(SumArgs);
+    void (*join)(SumArgs);
+#define OF_TYPES(T, O) sum = wide ? sum_tokens<T, O, 2> : sum_tokens<T, O, 1>; join = wide ? join_rows<T, O, 2> : join_rows<T, O, 1>
+    if (b.table_dt == DIVISION_BF16) {
+        if (half) { OF_TYPES(uint16_t, uint16_t); } else { OF_TYPES(float, uint16_t); }
+    } else {
+        if (half) { OF_TYPES(uint16_t, float); } else { OF_TYPES(float, float); }
     }
-    if (b.table_dt == DIVISION_BF16) kernel = half ? (wide ? sum_tokens<uint16_t, uint16_t, 2> : sum_tokens<uint16_t, uint16_t, 1>) : wide ? sum_tokens<float, uint16_t, 2> : sum_tokens<float, uint16_t, 1>;
-    else kernel = half ? (wide ? sum_tokens<uint16_t, float, 2> : sum_tokens<uint16_t, float, 1>) : wide ? sum_tokens<float, float, 2> : sum_tokens<float, float, 1>;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kThreads), 0, st, s);
+#undef OF_TYPES
+    hipLaunchKernelGGL(sum, dim3((uint32_t)grid), dim3(kThreads), 0, st, s);
+    CHECKED(launched());
+    if (!s.count) return DIVISION_OK;
+    hipLaunchKernelGGL(join, dim3((uint32_t)joins), dim3(kThreads), 0, st, s);
     return launched();
 }
 
