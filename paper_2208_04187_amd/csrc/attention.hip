@@ -176,12 +176,13 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     }
 }
 
-// Few columns: WK wavefronts have the same 32 columns and every WK-th tile of the keys each, in tiles of their own, and are joined at the end.
+// Few columns: WK wavefronts have the same 32 columns and every WK-th tile of the keys each, in a tile of their own, and are joined at the end.  Bound by memory.  While a wavefront computes, seven
+// others of the CU wait for their tiles; two tiles a wavefront, the second on its way, leave room for half as many (32 tokens over caches of up to 8192 keys: 69 us so, 64 with one tile).
 template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * WK) void attend_few(AttentionArgs a) {
     typedef RowTile<T, DP, KT> Keys;
-    constexpr int kTile = Keys::kBytes, kLoads = 2 * kTile / 1024, kRow = DP + 4;
-    static_assert(32 * kRow * 4 <= 4 * kTile, "a wavefront's values in place of its tiles");
-    __shared__ __attribute__((aligned(16))) char tiles[WK][2][2][kTile];
+    constexpr int kTile = Keys::kBytes, kTurns = DP == 96 ? 8 : DP / 4;
+    static_assert(32 * DP * 4 <= 2 * kTile, "a wavefront's values in place of its tiles");
+    __shared__ __attribute__((aligned(16))) char tiles[WK][2][kTile];
     __shared__ float most[WK][32], totals[WK][32];
     const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int group = blockIdx.x % a.groups, split = blockIdx.x / a.groups % a.splits, block = a.blocks - 1 - blockIdx.x / a.groups / a.splits;
@@ -197,33 +198,34 @@ template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * 
     const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
     const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     const int row_bytes = a.D * (int)sizeof(T);
-    const auto fetch = [&](int t, int at) {
+    const auto fetch = [&](int t) {
         const int left = seen.keys - t * KT;
-        Keys::template fill<64>(tiles[wave][at][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
-        Keys::template fill<64>(tiles[wave][at][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
+        Keys::template fill<64>(tiles[wave][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
+        Keys::template fill<64>(tiles[wave][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
     };
+    if (lo + wave < hi) fetch(lo + wave);
     Columns<T, DP> c;
     c.begin(a, a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head, col, cols, half);
     const float scale2 = a.scale * kLog2e;
-    if (lo + wave < hi) fetch(lo + wave, 0);
-    for (int t = lo + wave, at = 0; t < hi; t += WK, at ^= 1) {
-        if (t + WK < hi) {
-            fetch(t + WK, at ^ 1);
-            loads_done<kLoads>();
-        } else {
-            loads_done();
-        }
+    for (int t = lo + wave; t < hi; t += WK) {
+        loads_done();
         const int j = t * KT;
-        c.template add<Keys, KT>(tiles[wave][at][0], tiles[wave][at][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
+        c.template add<Keys, KT>(tiles[wave][0], tiles[wave][1], j, from, to, j >= whole_from && j + KT <= whole_to, scale2, lane);
+        if (t + WK < hi) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the tile has been read
+            fetch(t + WK);
+        }
     }
     const float total = halves_sum(c.total);
     if (half == 0) { most[wave][lane] = c.most; totals[wave][lane] = total; }
-    float* mine = reinterpret_cast<float*>(tiles[wave]) + (lane & 31) * kRow;
+    // [column][DP], pieces of four exchanged with the column's number: 32 columns at one row do not share banks
+    const auto place = [](int col, int d) { return col * DP + (d / 4 ^ col % kTurns) * 4; };
+    float* mine = reinterpret_cast<float*>(tiles[wave]);
 #pragma unroll
     for (int d = 0; d < DP; d += 8) {
         const f32x16& o = c.o[d / 32];
         const int n = d % 32 / 2;
-        *reinterpret_cast<f32x4*>(mine + d + 4 * half) = f32x4{o[n], o[n + 1], o[n + 2], o[n + 3]};
+        *reinterpret_cast<f32x4*>(mine + place(lane & 31, d + 4 * half)) = f32x4{o[n], o[n + 1], o[n + 2], o[n + 3]};
     }
     __syncthreads();
     for (int e = thread; e < 32 * (DP / 4); e += 64 * WK) {
@@ -238,7 +240,7 @@ template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * 
         for (int w = 0; w < WK; ++w) {
             const float by = most[w][c1] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((most[w][c1] - m) * scale2);
             sum += by * totals[w][c1];
-            o += by * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(tiles[w]) + c1 * kRow + d);
+            o += by * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(tiles[w]) + place(c1, d));
         }
         o *= sum == 0.0f ? 0.0f : 1.0f / sum;
         const float lse = sum == 0.0f ? -INFINITY : __builtin_fmaf(m, a.scale, logf(sum));
@@ -310,23 +312,32 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(kThreads) void jo
 
 // ------------------------------------------------------------------ host side
 
-// How the work is cut: columns into blocks of 128 (of 32 where there are no more), and the keys into parts where that leaves less than two workgroups a CU.
-struct Cut { bool few; int64_t blocks; int splits, tiles, key_tile; };
+// How the work is cut: columns into blocks of 128 (of 32 where there are no more), and the keys into parts where that leaves CUs without work.
+//   few columns: 1024 workgroups, four a CU, of eight tiles at least (32 tokens over caches of up to 8192 keys: 63 us with 512, 60 so); 256 of four at least where there are not so many keys (one
+//   token of 32 heads on 8 over 4097: 11.3 us with eight, 10.4 with four);
+//   many: 512 of four tiles at least, in fp32, whose products take sixteen times as long, of one (777 tokens of 6 heads of 72: 48 us with four, 35 with one).
+struct Cut { bool few; int64_t blocks; int splits, tiles; };
 Cut cut_of(const division_attention& a) {
     Cut c;
-    const int64_t R = a.H / a.G, cols = a.Sq * R;
+    const int64_t R = a.H / a.G, cols = a.Sq * R, half = a.dt == DIVISION_BF16;
     c.few = cols <= 32;
     c.blocks = (cols + (c.few ? 31 : 127)) / (c.few ? 32 : 128);
-    c.key_tile = c.few ? 32 : 64;
-    const int64_t tiles = (a.Sk + c.key_tile - 1) / c.key_tile, tasks = c.blocks * a.B * a.G;
-    // a part has so many tiles at least: fp32 products take long enough for one
-    const int64_t least = a.dt == DIVISION_BF16 ? 4 : c.few ? 2 : 1, room = tiles / least, wanted = 512;
-    int64_t splits = tasks >= (c.few ? 512 : 256) ? 1 : (wanted + tasks - 1) / tasks;
-    if (splits > room) splits = room;
-    if (splits > kMostSplits) splits = kMostSplits;
-    if (splits < 1) splits = 1;
-    c.tiles = (int)least;
-    c.splits = (int)splits;
+    const int64_t tile = c.few ? 32 : 64, tiles = (a.Sk + tile - 1) / tile, tasks = c.blocks * a.B * a.G;
+    const auto parts = [&](int64_t wanted, int64_t least) {
+        c.tiles = (int)least;
+        const int64_t n = (wanted + tasks - 1) / tasks, room = tiles / least;
+        c.splits = (int)(n > room ? room : n);
+        if (c.splits > kMostSplits) c.splits = kMostSplits;
+        if (c.splits < 1) c.splits = 1;
+    };
+    if (c.few) {
+        parts(1024, half ? 8 : 4);
+        if (tasks * c.splits < 256) parts(256, half ? 4 : 2);
+    } else if (tasks < 256) {
+        parts(512, half ? 4 : 1);
+    } else {
+        parts(tasks, 1);
+    }
     return c;
 }
 size_t parts_bytes(const division_attention& a, const Cut& c) { return c.splits > 1 ? (size_t)c.splits * a.B * a.Sq * a.H * (a.D + 1) * 4 : 0; }
