@@ -502,7 +502,7 @@ int division_clip_grads(int64_t count, const division_gradient *grads, float lim
 
 /*
  * Attention.  Query head h of H reads key head h / (H / G) of G.  q is [B][Sq][H][D], k and v are [B][Sk][G][D]: D elements next to one another, the three other
- * strides (batch, token, head; in elements) any from 0 up that keep every row on 16 bytes, at most 8 MB a token and 64 MB for all heads (DIVISION_ERANGE).  D is a multiple of 8 up to 128;
+ * strides (batch, token, head; in elements) any from 0 up that keep every row on 16 bytes, at most 8 MB a token and 1 GB for the heads that share a key head (DIVISION_ERANGE).  D is a multiple of 8 up to 128;
  * Sq and Sk up to 2^29, Sq * H / G up to 2^30, H up to 4096, B up to 2^24.
  *
  * Sequence b has min(Sk, max(0, lengths[b])) keys (all Sk where lengths is null); what lies behind them is not looked at and may hold anything.  Its query i stands at position
@@ -511,7 +511,7 @@ int division_clip_grads(int64_t count, const division_gradient *grads, float lim
  *
  *   z = scale q k^T,   p = softmax(z) over the keys that are seen,   out = p v,   lse = ln(sum of exp(z))
  *
- * scale: positive and finite.  Products of bfloat16 tensors take their factors as they are, probabilities (and, backward, the scores' gradients) rounded to bfloat16; sums,
+ * scale: positive, up to 2e38.  Products of bfloat16 tensors take their factors as they are, probabilities (and, backward, the scores' gradients) rounded to bfloat16; sums,
  * maxima and exponentials are fp32.  fp32 tensors are multiplied in fp32.  A query that sees no key has out 0, lse -infinity and no gradient.
  *   out  [B][Sq][H][D] of type dt, dense, on 16 bytes;   lse  [B][H][Sq]
  *   workspace  division_attention_workspace(attention) bytes on 16, for few queries over many keys (may be null where that is 0)

@@ -32,27 +32,27 @@ bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % 
 int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP; }
 #define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
 
-// a tensor of rows: not behind what an offset within a tile can say (kMostStride bytes a token, kMostStride for all heads), every row on 16 bytes
-constexpr int64_t kMostStride = 1 << 23, kMostTokens = 1 << 29;
-int check_heads(const void* p, const int64_t* strides, int64_t B, int64_t heads, int64_t es) {
+// A tensor of rows: nothing behind what 31 bits say of a tile's rows, which are up to 129 tokens' of the `share` heads that have one key head; every row on 16 bytes
+constexpr int64_t kMostStride = 1 << 23, kMostHeads = 1 << 30, kMostTokens = 1 << 29;
+int check_heads(const void* p, const int64_t* strides, int64_t B, int64_t share, int64_t es) {
     const int64_t per = 16 / es;
     if (strides[0] < 0 || strides[1] < 0 || strides[2] < 0) return DIVISION_EINVAL;
     if (!aligned(p, 16) || strides[0] % per || strides[1] % per || strides[2] % per) return DIVISION_EALIGN;
-    if (strides[1] * es > kMostStride || strides[2] > (kMostStride * 8) / es / heads || strides[0] > (int64_t(1) << 40) / B) return DIVISION_ERANGE;
+    if (strides[1] > kMostStride / es || strides[2] > kMostHeads / es / share || strides[0] > (int64_t(1) << 40) / B) return DIVISION_ERANGE;
     return DIVISION_OK;
 }
 int check_attention(const division_attention& a) {
     if (a.dt != DIVISION_F32 && a.dt != DIVISION_BF16) return DIVISION_EINVAL;
     if (a.B < 0 || a.Sq < 0 || a.Sk < 0 || a.H < 1 || a.G < 1 || a.H % a.G || a.D < 8 || a.D > 128 || a.D % 8 || a.window < 0 || (a.causal != 0 && a.causal != 1)) return DIVISION_EINVAL;
-    if (!(a.scale > 0.0f && a.scale <= 3.4e38f)) return DIVISION_EINVAL;
+    if (!(a.scale > 0.0f && a.scale <= 2e38f)) return DIVISION_EINVAL;
     if (!aligned(a.lengths, 4) || !aligned(a.starts, 4)) return DIVISION_EALIGN;
     if (a.B == 0 || a.Sq == 0) return DIVISION_OK;
     const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4, R = a.H / a.G;
     if (a.B > (1 << 24) || a.H > 4096 || a.Sq > kMostTokens || a.Sk > kMostTokens || a.Sq * R > (int64_t(1) << 30)) return DIVISION_ERANGE;
-    CHECKED(check_heads(a.q, a.q_strides, a.B, a.H, es));
+    CHECKED(check_heads(a.q, a.q_strides, a.B, R, es));
     if (a.Sk > 0) {
-        CHECKED(check_heads(a.k, a.k_strides, a.B, a.G, es));
-        CHECKED(check_heads(a.v, a.v_strides, a.B, a.G, es));
+        CHECKED(check_heads(a.k, a.k_strides, a.B, 1, es));
+        CHECKED(check_heads(a.v, a.v_strides, a.B, 1, es));
     }
     return DIVISION_OK;
 }

@@ -331,7 +331,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void add_key_parts(
 
 size_t stats_bytes(const division_attention& a) { return ((size_t)(a.B * a.Sq * a.H) * 8 + 15) / 16 * 16; }
 
-// fp32 products are slow enough for small workgroups to pay: 64 columns or keys, their tiles shared by two (four) sets.  (2 x 1531 tokens, 12 heads of 64, window 256: SETS_F32.)
+// fp32 products are slow enough for small workgroups to pay: 64 columns or keys, their tiles shared by two (four) sets.  (2 x 1531 tokens, 12 heads of 64, window 256: 228 us with workgroups of 128, 191 so.)
 constexpr int kColumnTile = 32;
 template <typename T, int DP> struct Shape {
     static constexpr bool kSmall = sizeof(T) == 4 && DP <= 64;
@@ -341,7 +341,7 @@ template <typename T, int DP> struct Shape {
 };
 int keys_of_workgroup(const division_attention& a) { return a.dt != DIVISION_BF16 && a.D <= 64 ? 64 : 128; }
 // Parts of the columns of one workgroup's keys: where few heads of keys leave CUs without work, as many as make two workgroups a CU, of 16 tiles at least.  (One sequence of 2048, 32 heads on 4
-// of keys: 484 us in one part, SPLIT_US so.)
+// of keys: 484 us in one part, 181 so.)
 constexpr int kLeastTiles = 16;
 int splits_of(const division_attention& a) {
     const int64_t keys = keys_of_workgroup(a), tasks = (a.Sk + keys - 1) / keys * a.B * a.G, tiles = (a.Sq * (a.H / a.G) + kColumnTile - 1) / kColumnTile;
@@ -399,7 +399,7 @@ int division_attention_backward(const division_attention* attention, const divis
     if ((a.Sq > 0 && (!a.q || !w.grad_out || !w.out || !w.lse || !w.grad_q)) || (a.Sk > 0 && (!w.grad_k || !w.grad_v || !a.k || !a.v))) return DIVISION_EINVAL;
     if (!w.workspace && stats_bytes(a) + sums_bytes(a)) return DIVISION_EINVAL;
     if (!aligned(w.out, 16) || !aligned(w.lse, 4) || !aligned(w.grad_q, 16) || !aligned(w.grad_k, 16) || !aligned(w.grad_v, 16) || !aligned(w.workspace, 16)) return DIVISION_EALIGN;
-    if (a.Sq > 0) CHECKED(check_heads(w.grad_out, w.grad_out_strides, a.B, a.H, es));
+    if (a.Sq > 0) CHECKED(check_heads(w.grad_out, w.grad_out_strides, a.B, a.H / a.G, es));
     if (w.workspace_bytes < stats_bytes(a) + sums_bytes(a)) return DIVISION_ESIZE;
     BackArgs args{};
     static_cast<AttentionArgs&>(args) = args_of(a);

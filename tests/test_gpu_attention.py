@@ -215,7 +215,9 @@ def test_strides(dtype):
     q, k, v = x[..., per: per + H * D].unflatten(2, (H, D)), x[..., per + H * D: per + (H + G) * D].unflatten(2, (G, D)), x[..., -G * D:].unflatten(2, (G, D))
     g = torch.randn(B, H, S, D, generator=gen).to(dtype).cuda().transpose(1, 2)
     other = torch.randn(S, G, B, D, generator=gen).to(dtype).cuda().permute(2, 0, 1, 3)
-    for qq, kk, vv, gg in ((q, k, v, g), (q, other, v, g), (q[:1].expand(B, S, H, D), k[:, :, :1].expand(B, S, G, D), v, g[:, :1].expand(B, S, H, D)), (q[:, 5:], k[:, 3:60], v[:, 10:67], g[:, 5:])):
+    far = torch.empty(H * (1 << 24), dtype=dtype, device="cuda").as_strided((B, S, H, D), (S * D, D, 1 << 24, 1))      # heads 32 or 64 MB apart, tokens next to one another
+    far.copy_(q)
+    for qq, kk, vv, gg in ((q, k, v, g), (q, other, v, g), (far, far[:, :, :G], v, far), (q[:1].expand(B, S, H, D), k[:, :, :1].expand(B, S, G, D), v, g[:, :1].expand(B, S, H, D)), (q[:, 5:], k[:, 3:60], v[:, 10:67], g[:, 5:])):
         dense = [t.contiguous() for t in (qq, kk, vv, gg)]
         a, b = pkg.division_attention(qq, kk, vv, causal=True), pkg.division_attention(*dense[:3], causal=True)
         assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse) and a.out.is_contiguous()

@@ -27,7 +27,7 @@ BAD = [(dict(dt=2), EINVAL), (dict(dt=7), EINVAL), (dict(B=-1), EINVAL), (dict(S
        (dict(D=136), EINVAL), (dict(D=60), EINVAL), (dict(D=4), EINVAL), (dict(window=-1), EINVAL), (dict(causal=2), EINVAL), (dict(scale=0.0), EINVAL), (dict(scale=-1.0), EINVAL),
        (dict(scale=math.inf), EINVAL), (dict(scale=math.nan), EINVAL), (dict(q=None), EINVAL), (dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(q=4104), EALIGN), (dict(k=4104), EALIGN),
        (dict(v=4104), EALIGN), (dict(q_strides=(4, 64, 64)), EALIGN), (dict(k_strides=(64, 4, 64)), EALIGN), (dict(v_strides=(64, 64, 4)), EALIGN), (dict(q_strides=(-8, 64, 64)), EINVAL),
-       (dict(k_strides=(64, -8, 64)), EINVAL), (dict(q_strides=(64, 1 << 23, 64)), ERANGE), (dict(k_strides=(64, 64, 1 << 25)), ERANGE), (dict(v_strides=(1 << 40, 64, 64)), ERANGE), (dict(lengths=2), EALIGN),
+       (dict(k_strides=(64, -8, 64)), EINVAL), (dict(q_strides=(64, 1 << 23, 64)), ERANGE), (dict(k_strides=(64, 64, (1 << 29) + 8)), ERANGE), (dict(q_strides=(64, 64, (1 << 28) + 8)), ERANGE), (dict(scale=3e38), EINVAL), (dict(v_strides=(1 << 40, 64, 64)), ERANGE), (dict(lengths=2), EALIGN),
        (dict(starts=6), EALIGN), (dict(Sk=(1 << 29) + 1), ERANGE), (dict(Sq=(1 << 29) + 1), ERANGE), (dict(H=8194, G=2), ERANGE), (dict(Sq=1 << 29, H=8), ERANGE), (dict(B=(1 << 24) + 1), ERANGE)]
 
 
