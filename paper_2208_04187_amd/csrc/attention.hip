@@ -343,7 +343,8 @@ Cut cut_of(const division_attention& a) {
 size_t parts_bytes(const division_attention& a, const Cut& c) { return c.splits > 1 ? (size_t)c.splits * a.B * a.Sq * a.H * (a.D + 1) * 4 : 0; }
 
 template <typename T, int DP> int run(const AttentionArgs& args, const Cut& c, int64_t grid, hipStream_t st) {
-    if (c.few) hipLaunchKernelGGL((attend_few<T, DP, 32, sizeof(T) == 2 ? 4 : 2>), dim3((uint32_t)grid), dim3(sizeof(T) == 2 ? 256 : 128), 0, st, args);
+    constexpr int kFew = sizeof(T) == 2 && DP == 96 ? 128 : DP;                      // 96 bfloat16 are no rows of eight pieces
+    if (c.few) hipLaunchKernelGGL((attend_few<T, kFew, 32, sizeof(T) == 2 ? 4 : 2>), dim3((uint32_t)grid), dim3(sizeof(T) == 2 ? 256 : 128), 0, st, args);
     else hipLaunchKernelGGL((attend<T, DP, 64>), dim3((uint32_t)grid), dim3(kThreads), 0, st, args);
     CHECKED(launched());
     if (c.splits == 1) return DIVISION_OK;
@@ -384,8 +385,8 @@ int division_attend(const division_attention* attention, void* out, float* lse, 
     const int64_t grid = c.blocks * args.groups * c.splits;
     if (grid >= (int64_t(1) << 24)) return DIVISION_ERANGE;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, c, grid, st) : run<uint16_t, 128>(args, c, grid, st);
-    return a.D <= 64 ? run<float, 64>(args, c, grid, st) : a.D <= 96 ? run<float, 96>(args, c, grid, st) : run<float, 128>(args, c, grid, st);
+    if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, c, grid, st) : a.D <= 96 && !c.few ? run<uint16_t, 96>(args, c, grid, st) : run<uint16_t, 128>(args, c, grid, st);
+    return a.D <= 32 ? run<float, 32>(args, c, grid, st) : a.D <= 64 ? run<float, 64>(args, c, grid, st) : a.D <= 96 ? run<float, 96>(args, c, grid, st) : run<float, 128>(args, c, grid, st);
 }
 
 }  // extern "C"

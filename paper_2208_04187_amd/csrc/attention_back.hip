@@ -19,7 +19,8 @@ struct BackArgs : AttentionArgs {
     const char *grad, *o;
     Heads gs;
     char *dq, *dk, *dv;
-    float* sums;                                        // the parts of dk and dv, where the columns are cut
+    float *key_sums, *query_sums;                       // the parts of dk and dv, where the columns are cut, and of dq, where the keys are
+    int query_splits;
     float* stats;                                       // [group][column][2]: lse in powers of two (infinity where nothing is seen), rowsum(grad out)
     FastDiv by_R;
 };
@@ -48,6 +49,15 @@ template <typename T, int DP> __device__ __forceinline__ void get_column(Operand
 }
 
 constexpr int kThreads = 256;
+
+// A workgroup's part of the tiles lo .. hi - 1 that it would have to look at: equal parts, of kLeastTiles at least
+template <typename T> constexpr int kLeastTiles = sizeof(T) == 2 ? 8 : 4;
+__device__ __forceinline__ void part_of(int split, int splits, int least, int& lo, int& hi) {
+    if (splits == 1) return;
+    const int each = max((hi - lo + splits - 1) / splits, least);
+    lo += split * each;
+    hi = min(lo + each, hi);
+}
 
 // Adds up what SETS sets of THREADS threads each have in their blocks, into the first set's, through the local memory: a set at a time
 template <int SETS, int THREADS, int N> __device__ __forceinline__ void add_sets(f32x16* o, char* memory, int set, int thread) {
@@ -83,13 +93,14 @@ template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_b
     const int set = SETS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kSet), thread = threadIdx.x % kSet, lane = thread & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     char* mine = memory + set * 4 * kTile;
-    const int group = blockIdx.x % a.groups, block = a.blocks - 1 - blockIdx.x / a.groups;
+    const int group = blockIdx.x % a.groups, split = blockIdx.x / a.groups % a.query_splits, block = a.blocks - 1 - blockIdx.x / a.groups / a.query_splits;
     const int b = group / a.G, g = group % a.G;
     const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * kCols;
     const uint32_t wave_col = first_col + 32 * wave, col = wave_col + (lane & 31);
     const Seen seen = seen_of(a, b);
     const uint32_t last_col = min(first_col + kCols - 1, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
-    const int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
+    int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
+    part_of(split, a.query_splits, kLeastTiles<T>, lo, hi);
     const bool works = wave_col < cols, there = col < cols;
     const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
     const int whole_from = seen.from(qb), whole_to = seen.to(qa);
@@ -124,7 +135,7 @@ template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_b
     }
     float exponent = there ? a.lse[((int64_t)b * a.H + g * a.R + r) * a.Sq + i] * kLog2e : INFINITY;
     if (exponent == -INFINITY) exponent = INFINITY;
-    if (set == 0 && there && half == 0) *reinterpret_cast<f32x2*>(a.stats + ((int64_t)group * cols + col) * 2) = f32x2{exponent, delta};
+    if (split == 0 && set == 0 && there && half == 0) *reinterpret_cast<f32x2*>(a.stats + ((int64_t)group * cols + col) * 2) = f32x2{exponent, delta};
     const float scale2 = a.scale * kLog2e;
     f32x16 dq[DP / 32];
 #pragma unroll
@@ -176,7 +187,9 @@ template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_b
         add_sets<SETS, kSet, DP / 32>(dq, memory, set, thread);
         if (set) return;
     }
-    if (there) put_column<T, DP>(reinterpret_cast<T*>(a.dq) + row * a.D, dq, a.scale, a.D, half);
+    if (!there) return;
+    if (a.query_splits > 1) put_column<float, DP>(a.query_sums + (((int64_t)split * a.groups + group) * cols + col) * a.D, dq, a.scale, a.D, half);     // [split][group][column][D]
+    else put_column<T, DP>(reinterpret_cast<T*>(a.dq) + row * a.D, dq, a.scale, a.D, half);
 }
 
 // Wavefronts of 32 keys each, WAVES of them, share the tiles of the columns (queries of all heads that share the keys) and their gradients.  SETS such take every SETS-th
@@ -202,11 +215,7 @@ template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global
     // the columns of the workgroup, of the wavefront and of the lane: those of whole queries
     const bool any = first < seen.keys, works = wave_key < seen.keys, there = key < seen.keys;
     int lo = any ? seen.query_from(first) * a.R / CT : 0, hi = any ? (seen.query_to(last) * a.R + CT - 1) / CT : 0;
-    if (a.splits > 1) {                                     // equal parts of the columns that these keys are seen by
-        const int each = max((hi - lo + a.splits - 1) / a.splits, a.tiles);
-        lo += split * each;
-        hi = min(lo + each, hi);
-    }
+    part_of(split, a.splits, kLeastTiles<T>, lo, hi);
     const int whole_from = seen.query_from(min(wave_key + 31, a.Sk - 1)) * a.R, whole_to = works && wave_key + 31 < seen.keys ? seen.query_to(wave_key) * a.R : 0;
     const int from = there ? seen.query_from(key) * a.R : 0, to = there ? max(from, seen.query_to(key) * a.R) : 0;
     const char* q = a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head;
@@ -301,7 +310,7 @@ template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global
     }
     if (a.splits > 1) {                                     // [split][group][key][2][D]
         if (key >= a.Sk) return;
-        float* row = a.sums + (((int64_t)split * a.groups + group) * a.Sk + key) * 2 * a.D;
+        float* row = a.key_sums + (((int64_t)split * a.groups + group) * a.Sk + key) * 2 * a.D;
         put_column<float, DP>(row, dk, a.scale, a.D, half);
         put_column<float, DP>(row + a.D, dv, 1.0f, a.D, half);
         return;
@@ -312,18 +321,24 @@ template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global
     put_column<T, DP>(reinterpret_cast<T*>(a.dv) + row, dv, 1.0f, a.D, half);
 }
 
-// The parts of the keys' gradients, in their order: four elements of a row of dk or dv a thread
-template <typename T> __global__ __launch_bounds__(kThreads) void add_key_parts(BackArgs a) {
-    const int each = a.D / 2;                               // of four elements of dk and of dv
-    const int64_t n = (int64_t)a.groups * a.Sk, at = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = at / each;
+// The parts of gradients, in their order: four elements a thread.  QUERIES: of dq, [group][column][D]; else of dk and dv, [group][key][2][D]
+template <typename T, bool QUERIES> __global__ __launch_bounds__(kThreads) void add_parts(BackArgs a) {
+    const int pieces = (QUERIES ? a.D : 2 * a.D) / 4, splits = QUERIES ? a.query_splits : a.splits;
+    const int64_t rows = QUERIES ? (int64_t)a.Sq * a.R : a.Sk, n = (int64_t)a.groups * rows, at = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = at / pieces;
     if (row >= n) return;
-    const int e = (int)(at - row * each) * 4;
-    const float* from = a.sums + row * 2 * a.D + e;
+    const int e = (int)(at - row * pieces) * 4;
+    const float* from = (QUERIES ? a.query_sums : a.key_sums) + at * 4;
     f32x4 o = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) o += *reinterpret_cast<const f32x4*>(from + s * n * 2 * a.D);
-    const int64_t group = row / a.Sk, key = row - group * a.Sk, b = group / a.G, g = group - b * a.G;
-    T* out = reinterpret_cast<T*>(e < a.D ? a.dk : a.dv) + ((b * a.Sk + key) * a.G + g) * a.D + (e < a.D ? e : e - a.D);
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) o += *reinterpret_cast<const f32x4*>(from + s * n * pieces * 4);
+    const int64_t group = row / rows, r = row - group * rows, b = group / a.G, g = group - b * a.G;
+    T* out;
+    if constexpr (QUERIES) {
+        const int64_t i = r / a.R;
+        out = reinterpret_cast<T*>(a.dq) + ((b * a.Sq + i) * a.H + g * a.R + (r - i * a.R)) * a.D + e;
+    } else {
+        out = reinterpret_cast<T*>(e < a.D ? a.dk : a.dv) + ((b * a.Sk + r) * a.G + g) * a.D + (e < a.D ? e : e - a.D);
+    }
     put4(out, o[0], o[1], o[2], o[3]);
 }
 
@@ -339,31 +354,41 @@ template <typename T, int DP> struct Shape {
     static constexpr int kKeyWaves = kSmall ? 2 : 4, kKeySets = kSmall ? 4 : sizeof(T) == 2 ? 2 : 1;
     static constexpr bool kValues = sizeof(T) == 2 && DP == 128;
 };
-int keys_of_workgroup(const division_attention& a) { return a.dt != DIVISION_BF16 && a.D <= 64 ? 64 : 128; }
-// Parts of the columns of one workgroup's keys: where few heads of keys leave CUs without work, as many as make two workgroups a CU, of 16 tiles at least.  (One sequence of 2048, 32 heads on 4
-// of keys: 484 us in one part, 181 so.)
-constexpr int kLeastTiles = 16;
-int splits_of(const division_attention& a) {
-    const int64_t keys = keys_of_workgroup(a), tasks = (a.Sk + keys - 1) / keys * a.B * a.G, tiles = (a.Sq * (a.H / a.G) + kColumnTile - 1) / kColumnTile;
+// Parts of what a workgroup would have to look at, where there are few workgroups: as many as make two a CU.  (One sequence of 2048, 32 heads on 4 of keys: 484 us with the columns of 128 keys in one
+// part, 181 so.  Two heads of 4090 tokens, whose queries' keys are cut too: 163 us in one part, QUERY_US so.)
+constexpr int kMostSplits = 32;
+int parts_of(int64_t tasks, int64_t tiles, int64_t least) {
     if (tasks == 0 || tasks >= 256) return 1;
-    int64_t splits = (512 + tasks - 1) / tasks;
-    if (splits > tiles / kLeastTiles) splits = tiles / kLeastTiles;
-    return splits < 1 ? 1 : splits > 32 ? 32 : (int)splits;
+    int64_t n = (512 + tasks - 1) / tasks;
+    if (n > tiles / least) n = tiles / least;
+    return n < 1 ? 1 : n > kMostSplits ? kMostSplits : (int)n;
 }
-size_t sums_bytes(const division_attention& a) {
-    const int splits = splits_of(a);
-    return splits > 1 ? (size_t)splits * a.B * a.G * a.Sk * 2 * a.D * 4 : 0;
+struct Splits { int queries, keys; };
+Splits splits_of(const division_attention& a) {
+    const bool half = a.dt == DIVISION_BF16;
+    const int64_t cols = a.Sq * (a.H / a.G), groups = a.B * a.G, key_tile = half ? 64 : 32, of_queries = half ? 128 : 64, of_keys = half || a.D > 64 ? 128 : 64, least = half ? 8 : 4;
+    return {parts_of((cols + of_queries - 1) / of_queries * groups, (a.Sk + key_tile - 1) / key_tile, least),
+            parts_of((a.Sk + of_keys - 1) / of_keys * groups, (cols + kColumnTile - 1) / kColumnTile, least)};
 }
+size_t key_bytes(const division_attention& a) { const int n = splits_of(a).keys; return n > 1 ? (size_t)n * a.B * a.G * a.Sk * 2 * a.D * 4 : 0; }
+size_t query_bytes(const division_attention& a) { const int n = splits_of(a).queries; return n > 1 ? (size_t)n * a.B * a.H * a.Sq * a.D * 4 : 0; }
+size_t back_bytes(const division_attention& a) { return stats_bytes(a) + key_bytes(a) + query_bytes(a); }
 
 template <typename T, int DP> int run(BackArgs& args, hipStream_t st) {
     typedef Shape<T, DP> S;
     if (args.Sq > 0) {
         constexpr int kCols = 32 * S::kQueryWaves;
         const int64_t blocks = ((int64_t)args.Sq * args.R + kCols - 1) / kCols;
-        if (blocks * args.groups >= (int64_t(1) << 23)) return DIVISION_ERANGE;
+        const int64_t grid = blocks * args.groups * args.query_splits;
+        if (grid >= (int64_t(1) << 23)) return DIVISION_ERANGE;
         args.blocks = (int)blocks;
-        hipLaunchKernelGGL((back_queries<T, DP, S::kKeyTile, S::kQueryWaves, S::kQuerySets>), dim3((uint32_t)(blocks * args.groups)), dim3(64 * S::kQueryWaves * S::kQuerySets), 0, st, args);
+        hipLaunchKernelGGL((back_queries<T, DP, S::kKeyTile, S::kQueryWaves, S::kQuerySets>), dim3((uint32_t)grid), dim3(64 * S::kQueryWaves * S::kQuerySets), 0, st, args);
         CHECKED(launched());
+        if (args.query_splits > 1) {
+            const int64_t pieces = (int64_t)args.groups * args.Sq * args.R * (args.D / 4);
+            hipLaunchKernelGGL((add_parts<T, true>), dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, args);
+            CHECKED(launched());
+        }
     }
     if (args.Sk > 0) {
         constexpr int kKeys = 32 * S::kKeyWaves;
@@ -373,7 +398,7 @@ template <typename T, int DP> int run(BackArgs& args, hipStream_t st) {
         CHECKED(launched());
         if (args.splits > 1) {
             const int64_t pieces = (int64_t)args.groups * args.Sk * (args.D / 2);
-            hipLaunchKernelGGL(add_key_parts<T>, dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, args);
+            hipLaunchKernelGGL((add_parts<T, false>), dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, args);
             CHECKED(launched());
         }
     }
@@ -386,7 +411,7 @@ extern "C" {
 
 size_t division_attention_backward_workspace(const division_attention* attention) {
     if (!attention || check_attention(*attention) != DIVISION_OK) return 0;
-    return stats_bytes(*attention) + sums_bytes(*attention);
+    return back_bytes(*attention);
 }
 
 int division_attention_backward(const division_attention* attention, const division_attention_back* back, void* hip_stream) {
@@ -397,10 +422,11 @@ int division_attention_backward(const division_attention* attention, const divis
     if (a.B == 0 || (a.Sq == 0 && a.Sk == 0)) return DIVISION_OK;
     const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4;
     if ((a.Sq > 0 && (!a.q || !w.grad_out || !w.out || !w.lse || !w.grad_q)) || (a.Sk > 0 && (!w.grad_k || !w.grad_v || !a.k || !a.v))) return DIVISION_EINVAL;
-    if (!w.workspace && stats_bytes(a) + sums_bytes(a)) return DIVISION_EINVAL;
+    const size_t need = back_bytes(a);
+    if (!w.workspace && need) return DIVISION_EINVAL;
     if (!aligned(w.out, 16) || !aligned(w.lse, 4) || !aligned(w.grad_q, 16) || !aligned(w.grad_k, 16) || !aligned(w.grad_v, 16) || !aligned(w.workspace, 16)) return DIVISION_EALIGN;
     if (a.Sq > 0) CHECKED(check_heads(w.grad_out, w.grad_out_strides, a.B, a.H / a.G, es));
-    if (w.workspace_bytes < stats_bytes(a) + sums_bytes(a)) return DIVISION_ESIZE;
+    if (w.workspace_bytes < need) return DIVISION_ESIZE;
     BackArgs args{};
     static_cast<AttentionArgs&>(args) = args_of(a);
     args.grad = static_cast<const char*>(w.grad_out);
@@ -409,13 +435,15 @@ int division_attention_backward(const division_attention* attention, const divis
     args.lse = const_cast<float*>(w.lse);
     args.dq = static_cast<char*>(w.grad_q); args.dk = static_cast<char*>(w.grad_k); args.dv = static_cast<char*>(w.grad_v);
     args.stats = static_cast<float*>(w.workspace);
-    args.splits = splits_of(a);
-    args.tiles = kLeastTiles;
-    args.sums = reinterpret_cast<float*>(static_cast<char*>(w.workspace) + stats_bytes(a));
+    const Splits splits = splits_of(a);
+    args.splits = splits.keys;
+    args.query_splits = splits.queries;
+    args.key_sums = reinterpret_cast<float*>(static_cast<char*>(w.workspace) + stats_bytes(a));
+    args.query_sums = reinterpret_cast<float*>(static_cast<char*>(w.workspace) + stats_bytes(a) + key_bytes(a));
     args.by_R = make_fastdiv((uint32_t)args.R);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, st) : run<uint16_t, 128>(args, st);
-    return a.D <= 64 ? run<float, 64>(args, st) : run<float, 128>(args, st);
+    if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, st) : a.D <= 96 ? run<uint16_t, 96>(args, st) : run<uint16_t, 128>(args, st);
+    return a.D <= 32 ? run<float, 32>(args, st) : a.D <= 64 ? run<float, 64>(args, st) : a.D <= 96 ? run<float, 96>(args, st) : run<float, 128>(args, st);
 }
 
 }  // extern "C"
