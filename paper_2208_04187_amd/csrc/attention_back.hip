@@ -50,8 +50,9 @@ template <typename T, int DP> __device__ __forceinline__ void get_column(Operand
 
 constexpr int kThreads = 256;
 
-// A workgroup's part of the tiles lo .. hi - 1 that it would have to look at: equal parts, of kLeastTiles at least
-template <typename T> constexpr int kLeastTiles = sizeof(T) == 2 ? 8 : 4;
+// A workgroup's part of the tiles lo .. hi - 1 that it would have to look at: equal parts, of so many tiles at least.  (An fp32 tile keeps a wavefront busy for 5 to 7 us.)
+template <typename T> constexpr int kLeastKeys = sizeof(T) == 2 ? 4 : 2;
+template <typename T> constexpr int kLeastColumns = sizeof(T) == 2 ? 8 : 2;
 __device__ __forceinline__ void part_of(int split, int splits, int least, int& lo, int& hi) {
     if (splits == 1) return;
     const int each = max((hi - lo + splits - 1) / splits, least);
@@ -100,7 +101,7 @@ template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_b
     const Seen seen = seen_of(a, b);
     const uint32_t last_col = min(first_col + kCols - 1, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
     int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
-    part_of(split, a.query_splits, kLeastTiles<T>, lo, hi);
+    part_of(split, a.query_splits, kLeastKeys<T>, lo, hi);
     const bool works = wave_col < cols, there = col < cols;
     const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
     const int whole_from = seen.from(qb), whole_to = seen.to(qa);
@@ -215,7 +216,7 @@ template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global
     // the columns of the workgroup, of the wavefront and of the lane: those of whole queries
     const bool any = first < seen.keys, works = wave_key < seen.keys, there = key < seen.keys;
     int lo = any ? seen.query_from(first) * a.R / CT : 0, hi = any ? (seen.query_to(last) * a.R + CT - 1) / CT : 0;
-    part_of(split, a.splits, kLeastTiles<T>, lo, hi);
+    part_of(split, a.splits, kLeastColumns<T>, lo, hi);
     const int whole_from = seen.query_from(min(wave_key + 31, a.Sk - 1)) * a.R, whole_to = works && wave_key + 31 < seen.keys ? seen.query_to(wave_key) * a.R : 0;
     const int from = there ? seen.query_from(key) * a.R : 0, to = there ? max(from, seen.query_to(key) * a.R) : 0;
     const char* q = a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head;
@@ -366,9 +367,9 @@ int parts_of(int64_t tasks, int64_t tiles, int64_t least) {
 struct Splits { int queries, keys; };
 Splits splits_of(const division_attention& a) {
     const bool half = a.dt == DIVISION_BF16;
-    const int64_t cols = a.Sq * (a.H / a.G), groups = a.B * a.G, key_tile = half ? 64 : 32, of_queries = half ? 128 : 64, of_keys = half || a.D > 64 ? 128 : 64, least = half ? 8 : 4;
-    return {parts_of((cols + of_queries - 1) / of_queries * groups, (a.Sk + key_tile - 1) / key_tile, least),
-            parts_of((a.Sk + of_keys - 1) / of_keys * groups, (cols + kColumnTile - 1) / kColumnTile, least)};
+    const int64_t cols = a.Sq * (a.H / a.G), groups = a.B * a.G, key_tile = half ? 64 : 32, of_queries = half ? 128 : 64, of_keys = half || a.D > 64 ? 128 : 64;
+    return {parts_of((cols + of_queries - 1) / of_queries * groups, (a.Sk + key_tile - 1) / key_tile, half ? kLeastKeys<uint16_t> : kLeastKeys<float>),
+            parts_of((a.Sk + of_keys - 1) / of_keys * groups, (cols + kColumnTile - 1) / kColumnTile, half ? kLeastColumns<uint16_t> : kLeastColumns<float>)};
 }
 size_t key_bytes(const division_attention& a) { const int n = splits_of(a).keys; return n > 1 ? (size_t)n * a.B * a.G * a.Sk * 2 * a.D * 4 : 0; }
 size_t query_bytes(const division_attention& a) { const int n = splits_of(a).queries; return n > 1 ? (size_t)n * a.B * a.H * a.Sq * a.D * 4 : 0; }

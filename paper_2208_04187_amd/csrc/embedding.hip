@@ -116,12 +116,27 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     }
     if (lo + rows == a.V && threadIdx.x == kOrderThreads - 1) a.starts[a.V] = at;
     __syncthreads();
-    // The lanes with the same row find one another by its bits; the first of them moves the wavefront's own counter on.  (A row at a time, frequent tokens of a small vocabulary took a third of a
-    // microsecond each: 14669 tokens of 1645 57 us, PLACE_US so.)
+    // A row's tokens among the wavefront's 64: where there is one row or two, which is most often, one after the other; the lanes of more rows find their likes by the rows' bits.  (All by their bits:
+    // 16384 tokens of 32768 21 us instead of 15; all one after the other: a third of a microsecond for each row.)  The wavefront's own counter is moved on by one lane with an atomic, since the next
+    // that reads it is another's.
     const auto place = [&](uint32_t row, uint32_t t) {
-        const bool mine = row < kBefore;
-        uint64_t same = __ballot(mine);
-        if (!same) return;
+        const uint64_t below = (1ull << lane) - 1;
+        uint64_t left = __ballot(row < kBefore);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            if (!left) return;
+            const int leader = __builtin_ctzll(left);
+            const uint32_t theirs = (uint32_t)__builtin_amdgcn_readlane((int)row, leader);
+            const uint64_t same = __ballot(row == theirs);
+            uint32_t begin = 0;
+            if (lane == leader) begin = atomicAdd(&counts[theirs * kOrderWaves + wave], (uint32_t)__builtin_popcountll(same));
+            begin = (uint32_t)__builtin_amdgcn_readlane((int)begin, leader);
+            if (row == theirs) a.order[begin + __builtin_popcountll(same & below)] = t;
+            left &= ~same;
+        }
+        if (!left) return;
+        const bool mine = left >> lane & 1;
+        uint64_t same = left;
         for (int bit = 0; bit < a.bits; ++bit) {
             const uint64_t set = __ballot(row >> bit & 1);
             same &= row >> bit & 1 ? set : ~set;
@@ -130,7 +145,7 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
         uint32_t begin = 0;
         if (mine && lane == leader) begin = atomicAdd(&counts[row * kOrderWaves + wave], (uint32_t)__builtin_popcountll(same));
         begin = (uint32_t)__shfl((int)begin, leader, 64);
-        if (mine) a.order[begin + __builtin_popcountll(same & ((1ull << lane) - 1))] = t;
+        if (mine) a.order[begin + __builtin_popcountll(same & below)] = t;
     };
 #pragma unroll
     for (int k = 0; k < kKept; ++k) place(kept[k], first + k * 64 + lane);
@@ -154,7 +169,7 @@ struct SumArgs {
     int64_t stride, V, D;
     uint32_t T, part;                                       // part: tokens that a wavefront adds up at most; a row of more is added up in parts
     float scale;
-    int add, columns;                                       // columns: pieces of 64 * kSize * P elements of a row
+    int add, columns, rows;                                 // columns: pieces of 64 * kSize * P elements of a row
     int64_t count;                                          // parts of the tokens, where there are more than one's
 };
 
@@ -168,33 +183,47 @@ template <typename T, int P> struct Row {
 #pragma unroll
             for (int i = 0; i < U::kSize; ++i) v[p][i] = 0.0f;
     }
-    // adds tokens order[from .. to - 1], several rows at a time on their way; first: a column
+    // adds tokens order[from .. to - 1]; c: a column.  64 tokens' numbers come at once, a lane each, their rows several at a time.
     __device__ __forceinline__ void add(const SumArgs& a, uint32_t from, uint32_t to, int64_t c) {
         constexpr int kAtOnce = P == 1 ? 8 : 4;
         const T* grad = static_cast<const T*>(a.grad);
-        uint32_t k = from;
-        for (; k + kAtOnce <= to; k += kAtOnce) {
-            U q[kAtOnce][P];
+        const uint32_t lane = threadIdx.x & 63;
+        for (uint32_t k = from; k < to; k += 64) {
+            const int n = (int)min(to - k, 64u);
+            const int tokens = (int)a.order[min(k + lane, to - 1)];
+            int j = 0;
+            for (; j + kAtOnce <= n; j += kAtOnce) {
+                U q[kAtOnce][P];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                const T* row = grad + (int64_t)a.order[k + u] * a.stride;
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const T* row = grad + (int64_t)(uint32_t)__builtin_amdgcn_readlane(tokens, j + u) * a.stride;
 #pragma unroll
-                for (int p = 0; p < P; ++p) q[u][p] = load_some<U>(row, c + p * 64 * U::kSize, a.D);
+                    for (int p = 0; p < P; ++p) q[u][p] = load_some<U>(row, c + p * 64 * U::kSize, a.D);
+                }
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int i = 0; i < U::kSize; ++i) v[p][i] += q[u][p][i];
             }
+            // the last ones all at once too: rows that are none count for nothing
+            if (j < n) {
+                U q[kAtOnce - 1][P];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u)
+                for (int u = 0; u < kAtOnce - 1; ++u) {
+                    const T* row = grad + (int64_t)(uint32_t)__builtin_amdgcn_readlane(tokens, min(j + u, n - 1)) * a.stride;
 #pragma unroll
-                for (int p = 0; p < P; ++p)
+                    for (int p = 0; p < P; ++p) q[u][p] = load_some<U>(row, c + p * 64 * U::kSize, a.D);
+                }
 #pragma unroll
-                    for (int i = 0; i < U::kSize; ++i) v[p][i] += q[u][p][i];
-        }
-        for (; k < to; ++k) {
-            const T* row = grad + (int64_t)a.order[k] * a.stride;
+                for (int u = 0; u < kAtOnce - 1; ++u) {
+                    if (j + u >= n) break;
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const U q = load_some<U>(row, c + p * 64 * U::kSize, a.D);
+                    for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int i = 0; i < U::kSize; ++i) v[p][i] += q[i];
+                        for (int i = 0; i < U::kSize; ++i) v[p][i] += q[u][p][i];
+                }
             }
         }
     }
@@ -240,7 +269,8 @@ template <typename T, int P> __device__ __forceinline__ void sum_part(const SumA
     }
 }
 
-// The table's gradient: the first wavefronts have parts of rows of many tokens, each of the others kRows rows, whose tokens lie one behind the other in the order; all a piece of the columns.
+// The table's gradient: the first wavefronts have parts of rows of many tokens, each of the others kRows rows (one where there are not wavefronts enough for all SIMDs otherwise), whose tokens lie
+// one behind the other in the order; all a piece of the columns.
 constexpr int kRows = 4;
 template <typename T, typename O, int P> __global__ __launch_bounds__(kThreads) void sum_tokens(SumArgs a) {
     typedef Unit<T> U;
@@ -250,12 +280,12 @@ template <typename T, typename O, int P> __global__ __launch_bounds__(kThreads) 
         sum_part<T, P>(a, (uint32_t)which, c);
         return;
     }
-    const int64_t row0 = (which - a.count) * kRows;
+    const int64_t row0 = (which - a.count) * a.rows;
     if (row0 >= a.V) return;
     uint32_t starts[kRows + 1];
 #pragma unroll
     for (int r = 0; r <= kRows; ++r) starts[r] = a.starts[row0 + r < a.V ? row0 + r : a.V];
-    for (int r = 0; r < kRows; ++r) {
+    for (int r = 0; r < a.rows; ++r) {
         if (row0 + r >= a.V) return;
         const uint32_t n = starts[r + 1] - starts[r];
         if (n > a.part || (a.add && n == 0)) continue;
@@ -382,12 +412,13 @@ int division_embedding_backward(const division_embedding_back* back, void* hip_s
     const int64_t workgroups = (b.V + rows - 1) / rows;
     if (workgroups * kOrderThreads >= (int64_t(1) << 32)) return DIVISION_ERANGE;
     const uint32_t part = part_of(b.T);
-    SumArgs s{b.grad, b.ids, o.order, o.starts, reinterpret_cast<float*>(ws + at.parts), b.grad_table, b.grad_stride, b.V, b.D, (uint32_t)b.T, part, b.scale, b.add, 0, 0};
+    SumArgs s{b.grad, b.ids, o.order, o.starts, reinterpret_cast<float*>(ws + at.parts), b.grad_table, b.grad_stride, b.V, b.D, (uint32_t)b.T, part, b.scale, b.add, 0, 0, 0};
     const bool wide = b.D > 64 * (int64_t)(16 / size_of(b.dt));
     const int64_t each = 64 * (int64_t)(16 / size_of(b.dt)) * (wide ? 2 : 1), columns = (b.D + each - 1) / each;
     s.columns = (int)columns;
     s.count = b.T > part ? (b.T + part - 1) / part : 0;
-    const int64_t joins = s.count * columns, grid = ((s.count + (b.V + kRows - 1) / kRows) * columns + 3) / 4;
+    s.rows = b.V * columns < 8192 * kRows ? 1 : kRows;
+    const int64_t joins = s.count * columns, grid = ((s.count + (b.V + s.rows - 1) / s.rows) * columns + 3) / 4;
     if (grid >= kMostWorkgroups || joins >= kMostWorkgroups) return DIVISION_ERANGE;
     hipLaunchKernelGGL(order_tokens, dim3((uint32_t)workgroups), dim3(kOrderThreads), (size_t)rows * kOrderWaves * 4, st, o);
     CHECKED(launched());
