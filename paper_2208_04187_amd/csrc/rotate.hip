@@ -26,7 +26,7 @@ struct RotateArgs {
 };
 
 // V pairs of a row from pair p on: v[0 .. V - 1] their first elements, v[V ..] the second ones.  NEXT: partners are neighbours, else half the rotated (or of the other) elements apart.
-template <typename T, int V, bool NEXT> struct Pairs {
+template <typename T, int V, bool NEXT, bool PAST = false> struct Pairs {
     static __device__ __forceinline__ int second(const RotateArgs& a, int p) { return p < a.rotated ? a.rotated : a.pairs - a.rotated; }
     static __device__ __forceinline__ int first(const RotateArgs& a, int p) { return p < a.rotated ? p : a.rotated + p; }
     static __device__ __forceinline__ void load(const T* row, const RotateArgs& a, int p, float* v) {
@@ -35,7 +35,7 @@ template <typename T, int V, bool NEXT> struct Pairs {
                 v[0] = Some1(row + 2 * p); v[1] = Some1(row + 2 * p + 1);
             } else {
                 Some<T, V> q[2];
-                q[0].load(row + 2 * p); q[1].load(row + 2 * p + V);
+                q[0].template load<PAST>(row + 2 * p); q[1].template load<PAST>(row + 2 * p + V);
 #pragma unroll
                 for (int i = 0; i < V; ++i) { v[i] = q[2 * i / V][2 * i % V]; v[V + i] = q[(2 * i + 1) / V][(2 * i + 1) % V]; }
             }
@@ -45,7 +45,7 @@ template <typename T, int V, bool NEXT> struct Pairs {
                 v[0] = Some1(at); v[1] = Some1(at + second(a, p));
             } else {
                 Some<T, V> q[2];
-                q[0].load(at); q[1].load(at + second(a, p));
+                q[0].template load<PAST>(at); q[1].template load<PAST>(at + second(a, p));
 #pragma unroll
                 for (int i = 0; i < V; ++i) { v[i] = q[0][i]; v[V + i] = q[1][i]; }
             }
@@ -59,10 +59,10 @@ template <typename T, int V, bool NEXT> struct Pairs {
             float w[2 * V];
 #pragma unroll
             for (int i = 0; i < V; ++i) { w[2 * i] = v[i]; w[2 * i + 1] = v[V + i]; }
-            Some<T, V>::store(row + 2 * p, w); Some<T, V>::store(row + 2 * p + V, w + V);
+            Some<T, V>::template store<PAST>(row + 2 * p, w); Some<T, V>::template store<PAST>(row + 2 * p + V, w + V);
         } else {
             T* at = row + first(a, p);
-            Some<T, V>::store(at, v); Some<T, V>::store(at + second(a, p), v + V);
+            Some<T, V>::template store<PAST>(at, v); Some<T, V>::template store<PAST>(at + second(a, p), v + V);
         }
     }
     static __device__ __forceinline__ float Some1(const T* p) {
@@ -93,8 +93,8 @@ __device__ __forceinline__ void angles(const RotateArgs& a, int64_t t0, int n, f
 }
 
 // LANES lanes have a head, U times V pairs each; a workgroup takes `block` tokens at a time, all heads of all of them one behind the other.
-template <typename T, int V, int U, int LANES, bool NEXT, bool BACK> __global__ __launch_bounds__(kThreads) void rotate(RotateArgs a) {
-    typedef Pairs<T, V, NEXT> P;
+template <typename T, int V, int U, int LANES, bool NEXT, bool BACK, bool PAST> __global__ __launch_bounds__(kThreads) void rotate(RotateArgs a) {
+    typedef Pairs<T, V, NEXT, PAST> P;
     extern __shared__ __attribute__((aligned(16))) float2 turned[];
     constexpr int kSlots = kThreads / LANES;
     const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES;
@@ -319,8 +319,13 @@ template <typename T, int V, int U, int LANES, bool BACK> int launch(RotateArgs&
     const int block = a.block[0] > a.block[1] ? a.block[0] : a.block[1];
     size_t lds = (size_t)block * a.rotated * sizeof(float2);
     if (BACK && lds < (size_t)a.D * 4) lds = (size_t)a.D * 4;
-    if (next) hipLaunchKernelGGL((rotate<T, V, U, LANES, true, BACK>), dim3(grid), dim3(kThreads), lds, st, a);
-    else hipLaunchKernelGGL((rotate<T, V, U, LANES, false, BACK>), dim3(grid), dim3(kThreads), lds, st, a);
+    // Calls whose tensors together are beyond the caches go past them (67200 tokens, 32 heads on 4 of 64 in bfloat16: 70.8 us kept, 66.0 so; backward 116 and 107).  Only whole vectors: single
+    // elements count on the caches to join them.
+    constexpr bool kPast = V > 1;
+    const bool past = kPast && a.T * (a.heads[0] + a.heads[1]) * (BACK ? 3 : 2) * a.D * (int64_t)sizeof(T) > kCached;
+    void (*kernel)(RotateArgs) = next ? (past ? rotate<T, V, U, LANES, true, BACK, kPast> : rotate<T, V, U, LANES, true, BACK, false>)
+                                      : past ? rotate<T, V, U, LANES, false, BACK, kPast> : rotate<T, V, U, LANES, false, BACK, false>;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), lds, st, a);
     return launched();
 }
 // Heads whose pairs are whole vectors of sixteen bytes; others element by element

@@ -55,6 +55,10 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_
 __device__ __forceinline__ void load_lds16(u32x4 from, const void* to, uint32_t offset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_address(to)), "v"(offset), "s"(from) : "memory", "m0");
 }
+// the same past the caches
+__device__ __forceinline__ void load_lds16_past(u32x4 from, const void* to, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds_address(to)), "v"(offset), "s"(from) : "memory", "m0");
+}
 __device__ __forceinline__ void load_lds4(u32x4 from, const void* to, uint32_t offset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds_address(to)), "v"(offset), "s"(from) : "memory", "m0");
 }
@@ -118,7 +122,8 @@ template <typename T, int DP, int ROWS> struct Tile {
 };
 
 // The same with whole rows behind one another, their pieces exchanged with the row's number over the row: a wavefront's load takes whole rows, not 64 bytes of each of sixteen, which counts
-// where the memory is the bound (32 tokens over caches of up to 8192 keys: 94 us in strips, 85 in rows).
+// where the memory is the bound (32 tokens over caches of up to 8192 keys: 94 us in strips, 85 in rows).  What is loaded is looked at once and goes past the caches (from memory, not from the
+// last-level cache, 69 us and 60).
 template <typename T, int DP, int ROWS> struct RowTile {
     static constexpr int kRowBytes = DP * (int)sizeof(T), kPieces = kRowBytes / 16, kBytes = ROWS * kRowBytes;
     // below kTurns, of which a row has a whole number: an exchanged piece stays in its row
@@ -140,7 +145,7 @@ template <typename T, int DP, int ROWS> struct RowTile {
         for (int u = 0; u < kEach; ++u) {
             const int slot = u * THREADS + thread, row = slot / kPieces, piece = (slot % kPieces) ^ turn(row);
             const uint32_t off = row < rows && piece * 16 < row_bytes ? (uint32_t)(at(row) + piece * 16) : 0x80000000u;
-            load_lds16(from, tile + (u * THREADS + first) * 16, off);
+            load_lds16_past(from, tile + (u * THREADS + first) * 16, off);
         }
     }
     static __device__ __forceinline__ Operand<T> rows(const char* tile, int row0, int step, int lane) {
