@@ -116,6 +116,7 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * 128u;
     const uint32_t wave_col = first_col + 32 * wave, col = wave_col + (lane & 31);
     const Seen seen = seen_of(a, b);
+    const int first_key = seen.from(0);                     // what stands before every query's keys is not looked at either
     // the keys of the workgroup, of the wavefront and of the lane
     const uint32_t last_col = min(first_col + 127u, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
     int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
@@ -129,9 +130,9 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     const int row_bytes = a.D * (int)sizeof(T);
     const auto fetch = [&](int t) {
-        const int left = seen.keys - t * KT;
-        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
-        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
+        const int low = first_key - t * KT, left = seen.keys - t * KT;
+        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][0], k + (int64_t)t * KT * a.ks.token, low, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
+        Tile<T, DP, KT>::template fill<kThreads>(tiles[t & 1][1], v + (int64_t)t * KT * a.vs.token, low, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
     };
     if (lo < hi) fetch(lo);
     Columns<T, DP> c;
@@ -189,6 +190,7 @@ template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * 
     const int b = group / a.G, g = group % a.G;
     const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * 32u, col = first_col + (lane & 31);
     const Seen seen = seen_of(a, b);
+    const int first_key = seen.from(0);                     // what stands before every query's keys is not looked at either
     const int qa = (int)(first_col / (uint32_t)a.R), qb = (int)(min(first_col + 31u, cols - 1) / (uint32_t)a.R);
     const int whole_from = seen.from(qb), whole_to = seen.to(qa);
     int lo = seen.from(qa) / KT, hi = (seen.to(qb) + KT - 1) / KT;
@@ -199,9 +201,9 @@ template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * 
     const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     const int row_bytes = a.D * (int)sizeof(T);
     const auto fetch = [&](int t) {
-        const int left = seen.keys - t * KT;
-        Keys::template fill<64>(tiles[wave][0], k + (int64_t)t * KT * a.ks.token, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
-        Keys::template fill<64>(tiles[wave][1], v + (int64_t)t * KT * a.vs.token, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
+        const int low = first_key - t * KT, left = seen.keys - t * KT;
+        Keys::template fill<64>(tiles[wave][0], k + (int64_t)t * KT * a.ks.token, low, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
+        Keys::template fill<64>(tiles[wave][1], v + (int64_t)t * KT * a.vs.token, low, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
     };
     if (lo + wave < hi) fetch(lo + wave);
     Columns<T, DP> c;

@@ -23,6 +23,10 @@ template <typename A> __device__ __forceinline__ Seen seen_of(const A& a, int b)
     s.window = a.window;
     s.causal = a.causal;
     s.Sq = a.Sq;
+    // keys that stand behind every query's are as ones behind the sequence: a cache may hold anything there
+    const int64_t behind = s.start + a.Sq;
+    if (a.causal) s.keys = Seen::within(behind, s.keys);
+    else if (a.window) s.keys = Seen::within(behind + a.window - 1, s.keys);
     return s;
 }
 
@@ -46,10 +50,10 @@ int check_attention(const division_attention& a) {
     if (a.B < 0 || a.Sq < 0 || a.Sk < 0 || a.H < 1 || a.G < 1 || a.H % a.G || a.D < 8 || a.D > 128 || a.D % 8 || a.window < 0 || (a.causal != 0 && a.causal != 1)) return DIVISION_EINVAL;
     if (!(a.scale > 0.0f && a.scale <= 2e38f)) return DIVISION_EINVAL;
     if (!aligned(a.lengths, 4) || !aligned(a.starts, 4)) return DIVISION_EALIGN;
-    if (a.B == 0 || a.Sq == 0) return DIVISION_OK;
+    if (a.B == 0) return DIVISION_OK;
     const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4, R = a.H / a.G;
     if (a.B > (1 << 24) || a.H > 4096 || a.Sq > kMostTokens || a.Sk > kMostTokens || a.Sq * R > (int64_t(1) << 30)) return DIVISION_ERANGE;
-    CHECKED(check_heads(a.q, a.q_strides, a.B, R, es));
+    if (a.Sq > 0) CHECKED(check_heads(a.q, a.q_strides, a.B, R, es));
     if (a.Sk > 0) {
         CHECKED(check_heads(a.k, a.k_strides, a.B, 1, es));
         CHECKED(check_heads(a.v, a.v_strides, a.B, 1, es));

@@ -99,6 +99,7 @@ template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_b
     const uint32_t cols = (uint32_t)a.Sq * (uint32_t)a.R, first_col = (uint32_t)block * kCols;
     const uint32_t wave_col = first_col + 32 * wave, col = wave_col + (lane & 31);
     const Seen seen = seen_of(a, b);
+    const int first_key = seen.from(0);                     // what stands before every query's keys is not looked at either
     const uint32_t last_col = min(first_col + kCols - 1, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
     int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
     part_of(split, a.query_splits, kLeastKeys<T>, lo, hi);
@@ -111,10 +112,10 @@ template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_b
     const char* v = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     const int row_bytes = a.D * (int)sizeof(T);
     const auto fetch = [&](int t, int at) {
-        const int left = seen.keys - t * KT;
+        const int low = first_key - t * KT, left = seen.keys - t * KT;
         char* to = mine + at * 2 * kTile;
-        Tile<T, DP, KT>::template fill<kSet>(to, k + (int64_t)t * KT * a.ks.token, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
-        Tile<T, DP, KT>::template fill<kSet>(to + kTile, v + (int64_t)t * KT * a.vs.token, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
+        Tile<T, DP, KT>::template fill<kSet>(to, k + (int64_t)t * KT * a.ks.token, low, left, row_bytes, thread, [&](int row) { return row * a.ks.token; });
+        Tile<T, DP, KT>::template fill<kSet>(to + kTile, v + (int64_t)t * KT * a.vs.token, low, left, row_bytes, thread, [&](int row) { return row * a.vs.token; });
     };
     if (lo + set < hi) fetch(lo + set, 0);
     Operand<T> q[DP / 16], grad[DP / 16];
@@ -233,14 +234,14 @@ template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global
         if (wave == 0) {                                    // columns behind the last have zeros: their rows are zeros too
             load_lds4(buffer(a.stats + ((int64_t)group * cols + c0) * 2, 4u * 2 * (uint32_t)min(left, CT)), stats[set][at], (uint32_t)lane * 4);
         }
-        Columns::template fill<kSet>(to, q + (int64_t)i0 * a.qs.token, left, row_bytes, thread, offset(a.qs));
-        Columns::template fill<kSet>(to + Columns::kBytes, gr + (int64_t)i0 * a.gs.token, left, row_bytes, thread, offset(a.gs));
+        Columns::template fill<kSet>(to, q + (int64_t)i0 * a.qs.token, 0, left, row_bytes, thread, offset(a.qs));
+        Columns::template fill<kSet>(to + Columns::kBytes, gr + (int64_t)i0 * a.gs.token, 0, left, row_bytes, thread, offset(a.gs));
     };
     if (lo + set < hi) fetch(lo + set, 0);
     char* values = memory + kTiles;
     const char* v_head = a.v + b * a.vs.batch + (int64_t)g * a.vs.head;
     if constexpr (VALUES)
-        Values::template fill<kSet * SETS>(values, v_head + (int64_t)first * a.vs.token, seen.keys - first, row_bytes, threadIdx.x, [&](int row) { return row * a.vs.token; });
+        Values::template fill<kSet * SETS>(values, v_head + (int64_t)first * a.vs.token, 0, seen.keys - first, row_bytes, threadIdx.x, [&](int row) { return row * a.vs.token; });
     Operand<T> k[DP / 16], v[VALUES ? 1 : DP / 16];
     get_column<T, DP>(k, a.k + b * a.ks.batch + row_offset(a.ks, key, g), there, row_bytes, half);
     if constexpr (!VALUES) get_column<T, DP>(v, v_head + (int64_t)key * a.vs.token, there, row_bytes, half);
@@ -356,7 +357,7 @@ template <typename T, int DP> struct Shape {
     static constexpr bool kValues = sizeof(T) == 2 && DP == 128;
 };
 // Parts of what a workgroup would have to look at, where there are few workgroups: as many as make two a CU.  (One sequence of 2048, 32 heads on 4 of keys: 484 us with the columns of 128 keys in one
-// part, 181 so.  Two heads of 4090 tokens, whose queries' keys are cut too: 163 us in one part, QUERY_US so.)
+// part, 181 so.  Two heads of 4090 tokens, whose queries' keys are cut too: 163 us in one part, 100 so.)
 constexpr int kMostSplits = 32;
 int parts_of(int64_t tasks, int64_t tiles, int64_t least) {
     if (tasks == 0 || tasks >= 256) return 1;
@@ -377,11 +378,11 @@ size_t back_bytes(const division_attention& a) { return stats_bytes(a) + key_byt
 
 template <typename T, int DP> int run(BackArgs& args, hipStream_t st) {
     typedef Shape<T, DP> S;
+    constexpr int kCols = 32 * S::kQueryWaves, kKeys = 32 * S::kKeyWaves;
+    const int64_t blocks = ((int64_t)args.Sq * args.R + kCols - 1) / kCols;
+    const int64_t grid = blocks * args.groups * args.query_splits, key_grid = ((int64_t)args.Sk + kKeys - 1) / kKeys * args.groups * args.splits;
+    if (grid >= (int64_t(1) << 23) || key_grid >= (int64_t(1) << 23)) return DIVISION_ERANGE;
     if (args.Sq > 0) {
-        constexpr int kCols = 32 * S::kQueryWaves;
-        const int64_t blocks = ((int64_t)args.Sq * args.R + kCols - 1) / kCols;
-        const int64_t grid = blocks * args.groups * args.query_splits;
-        if (grid >= (int64_t(1) << 23)) return DIVISION_ERANGE;
         args.blocks = (int)blocks;
         hipLaunchKernelGGL((back_queries<T, DP, S::kKeyTile, S::kQueryWaves, S::kQuerySets>), dim3((uint32_t)grid), dim3(64 * S::kQueryWaves * S::kQuerySets), 0, st, args);
         CHECKED(launched());
@@ -392,10 +393,7 @@ template <typename T, int DP> int run(BackArgs& args, hipStream_t st) {
         }
     }
     if (args.Sk > 0) {
-        constexpr int kKeys = 32 * S::kKeyWaves;
-        const int64_t grid = ((int64_t)args.Sk + kKeys - 1) / kKeys * args.groups * args.splits;
-        if (grid >= (int64_t(1) << 23)) return DIVISION_ERANGE;
-        hipLaunchKernelGGL((back_keys<T, DP, kColumnTile, S::kKeyWaves, S::kKeySets, S::kValues>), dim3((uint32_t)grid), dim3(64 * S::kKeyWaves * S::kKeySets), 0, st, args);
+        hipLaunchKernelGGL((back_keys<T, DP, kColumnTile, S::kKeyWaves, S::kKeySets, S::kValues>), dim3((uint32_t)key_grid), dim3(64 * S::kKeyWaves * S::kKeySets), 0, st, args);
         CHECKED(launched());
         if (args.splits > 1) {
             const int64_t pieces = (int64_t)args.groups * args.Sk * (args.D / 2);

@@ -70,19 +70,20 @@ template <typename T, int DP, int ROWS> struct Tile {
     static constexpr int kRowBytes = DP * (int)sizeof(T), kStrip = ROWS * 64, kBytes = ROWS * kRowBytes;
     static __device__ __forceinline__ int turn(int row) { return row >> 2 & 3; }
 
-    // the rows from global memory by THREADS threads, without a register between: those from `rows` on and pieces behind the row's bytes are zeros.  at(row): a row's
+    // the rows from global memory by THREADS threads, without a register between: those before `low`, from `rows` on and pieces behind the row's bytes are zeros.  at(row): a row's
     // offset from base, below 2^31 - 512.  The data are there when the wavefront has waited for its loads.
-    template <int THREADS, typename At> static __device__ __forceinline__ void fill(char* tile, const char* base, int rows, int row_bytes, int thread, At&& at) {
+    template <int THREADS, typename At> static __device__ __forceinline__ void fill(char* tile, const char* base, int low, int rows, int row_bytes, int thread, At&& at) {
         constexpr int kSlots = kBytes / 16, kEach = (kSlots + THREADS - 1) / THREADS;
         static_assert(kSlots % 64 == 0 && THREADS % 64 == 0, "whole wavefronts");
         const u32x4 from = buffer(base, 0x7fffffffu);
+        const uint32_t count = rows > low ? (uint32_t)(rows - low) : 0u;     // a tile may lie behind the last row
         const int first = __builtin_amdgcn_readfirstlane(thread & ~63);
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
             if (kSlots % THREADS != 0 && u * THREADS + first >= kSlots) break;     // the last pieces are fewer wavefronts'
             const int slot = u * THREADS + thread, row = slot / 4 % ROWS, piece = slot / (4 * ROWS) * 4 + ((slot & 3) ^ turn(row));
             // an offset beyond the buffer reads zeros
-            const uint32_t off = row < rows && piece * 16 < row_bytes ? (uint32_t)(at(row) + piece * 16) : 0x80000000u;
+            const uint32_t off = (uint32_t)(row - low) < count && piece * 16 < row_bytes ? (uint32_t)(at(row) + piece * 16) : 0x80000000u;
             load_lds16(from, tile + (u * THREADS + first) * 16, off);
         }
     }
@@ -136,15 +137,16 @@ template <typename T, int DP, int ROWS> struct RowTile {
     }
     static __device__ __forceinline__ int place(int row, int piece) { return row * kRowBytes + ((piece ^ turn(row)) << 4); }
 
-    template <int THREADS, typename At> static __device__ __forceinline__ void fill(char* tile, const char* base, int rows, int row_bytes, int thread, At&& at) {
+    template <int THREADS, typename At> static __device__ __forceinline__ void fill(char* tile, const char* base, int low, int rows, int row_bytes, int thread, At&& at) {
         constexpr int kEach = kBytes / 16 / THREADS;
         static_assert(kEach * THREADS * 16 == kBytes, "whole pieces a thread");
         const u32x4 from = buffer(base, 0x7fffffffu);
+        const uint32_t count = rows > low ? (uint32_t)(rows - low) : 0u;     // a tile may lie behind the last row
         const int first = __builtin_amdgcn_readfirstlane(thread & ~63);
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
             const int slot = u * THREADS + thread, row = slot / kPieces, piece = (slot % kPieces) ^ turn(row);
-            const uint32_t off = row < rows && piece * 16 < row_bytes ? (uint32_t)(at(row) + piece * 16) : 0x80000000u;
+            const uint32_t off = (uint32_t)(row - low) < count && piece * 16 < row_bytes ? (uint32_t)(at(row) + piece * 16) : 0x80000000u;
             load_lds16_past(from, tile + (u * THREADS + first) * 16, off);
         }
     }

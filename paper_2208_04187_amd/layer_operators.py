@@ -116,7 +116,7 @@ def _attention(q, k, v, scale, causal, window, lengths, starts):
     for name, t in (("lengths", lengths), ("starts", starts)):
         if t is not None:
             _dense(t, name, dtype=torch.int32, shape=(B,), device=q.device)
-    if not window >= 0:
+    if not 0 <= window < 2 ** 63:
         raise ValueError("window is a whole number from 0 up")
     d.q, d.k, d.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
     d.B, d.Sq, d.Sk, d.H, d.G, d.D, d.dt = B, Sq, Sk, H, G, D, _dt(q.dtype)
@@ -133,7 +133,8 @@ def division_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale:
     projection's output and of a cache are).  Query head h reads key head h // (heads / key heads).  scale: 1 / sqrt(features).
 
     lengths (int32 [batch]): keys that a sequence has; what lies behind them is not looked at.  starts (int32 [batch]): where a sequence's first query stands among the keys, keys -
-    queries if not given.  causal: a query sees no key behind its own position; window: only keys nearer than that.  A query that sees none has out 0 and lse -inf."""
+    queries if not given.  causal: a query sees no key behind its own position; window: only keys nearer than that.  What no query of a sequence can see behind its last key
+    or before its first one is not looked at either.  A query that sees none has out 0 and lse -inf."""
     if stream is None:
         got = _fast().attention(q, k, v, scale, causal, window, lengths, starts)
         if got is not None:

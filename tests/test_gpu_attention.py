@@ -193,6 +193,30 @@ def test_what_lies_behind_a_sequence_is_not_looked_at(size, dtype):
         assert all(t.isfinite().all() for row in got for t in (row[0], *row[2:]))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [(2, 50, 300, 4, 2, 64), (2, 1, 300, 8, 2, 128), (2, 5, 300, 4, 4, 40), (2, 140, 300, 2, 2, 96)])
+def test_what_no_query_sees_is_not_looked_at(size, dtype):
+    """A cache behind the position that a sequence has come to, or before its window, holds anything"""
+    q, k, v, g = (t.cuda() for t in _inputs(*size, dtype, seed=14))
+    B, Sq, Sk = size[:3]
+    starts = [37, 101]
+    for kw in (dict(causal=True), dict(causal=True, window=21), dict(window=21), dict(window=70, lengths=[90, 300])):
+        seen = _seen(B, Sq, Sk, kw.get("causal", False), kw.get("window", 0), kw.get("lengths"), starts)
+        none = ~seen.any(1).cuda()[..., None, None]
+        assert none.any(1).all()
+        kw = {**kw, "starts": torch.tensor(starts, dtype=torch.int32, device="cuda")}
+        if "lengths" in kw:
+            kw["lengths"] = torch.tensor(kw["lengths"], dtype=torch.int32, device="cuda")
+        got = []
+        for word in (0.0, math.nan, math.inf, torch.finfo(dtype).min):
+            kk, vv = k.masked_fill(none, word), v.masked_fill(none, word)
+            a = pkg.division_attention(q, kk, vv, **kw)
+            got.append((*a, *pkg.division_attention_backward(g, q, kk, vv, a.out, a.lse, **kw)))
+        for row in got[1:]:
+            assert all(torch.equal(p, r) for p, r in zip(row, got[0]))
+        assert all(t.isfinite().all() for t in (got[0][0], *got[0][2:]))
+
+
 def test_nan_and_infinity_reach_those_who_see_them():
     q, k, v, g = (t.cuda() for t in _inputs(1, 70, 70, 2, 2, 64, F32, seed=5))
     for t, place in ((q, 0), (k, 1), (v, 2)):

@@ -59,7 +59,10 @@ def _attention_back(change):
 
 @pytest.mark.parametrize("change,code", BAD + [*[({k: None}, EINVAL) for k in ("grad_out", "out", "lse", "grad_q", "grad_k", "grad_v", "workspace")], *[({k: 8}, EALIGN) for k in ("grad_out", "out", "grad_q", "grad_k", "grad_v", "workspace")],
                                                (dict(lse=2), EALIGN), (dict(grad_out_strides=(64, 4, 64)), EALIGN), (dict(grad_out_strides=(64, 64, -8)), EINVAL),
-                                               (dict(workspace_bytes=2 * 5 * 4 * 8 - 1), ESIZE), (dict(B=0, grad_out=None), 0)])
+                                               (dict(workspace_bytes=2 * 5 * 4 * 8 - 1), ESIZE), (dict(B=0, grad_out=None), 0),
+                                               # without queries the keys' gradients are zeros, and the keys as they have to be; more workgroups of keys than a launch has
+                                               (dict(Sq=0, Sk=(1 << 29) + 1), ERANGE), (dict(Sq=0, k_strides=(64, 1 << 23, 64)), ERANGE), (dict(Sq=0, v_strides=(64, 4, 64)), EALIGN),
+                                               (dict(B=1 << 20, Sq=1, Sk=1 << 15, G=1, workspace_bytes=1 << 50), ERANGE)])
 def test_attention_backward_refuses(change, code):
     assert _attention_back(change) == code
 
