@@ -177,9 +177,10 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     }
 }
 
-// Few columns: WK wavefronts have the same 32 columns and every WK-th tile of the keys each, in a tile of their own, and are joined at the end.  Bound by memory.  While a wavefront computes, seven
+// Few columns: WK wavefronts have the same 32 columns and every WK-th tile of the keys each, in a tile of their own, and are joined at the end.  PAST: the keys are looked at by this workgroup
+// alone.  Bound by memory then.  While a wavefront computes, seven
 // others of the CU wait for their tiles; two tiles a wavefront, the second on its way, leave room for half as many (32 tokens over caches of up to 8192 keys: 69 us so, 64 with one tile).
-template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * WK) void attend_few(AttentionArgs a) {
+template <typename T, int DP, int KT, int WK, bool PAST> __global__ __launch_bounds__(64 * WK) void attend_few(AttentionArgs a) {
     typedef RowTile<T, DP, KT> Keys;
     constexpr int kTile = Keys::kBytes, kTurns = DP == 96 ? 8 : DP / 4;
     static_assert(32 * DP * 4 <= 2 * kTile, "a wavefront's values in place of its tiles");
@@ -202,8 +203,8 @@ template <typename T, int DP, int KT, int WK> __global__ __launch_bounds__(64 * 
     const int row_bytes = a.D * (int)sizeof(T);
     const auto fetch = [&](int t) {
         const int low = first_key - t * KT, left = seen.keys - t * KT;
-        Keys::template fill<64>(tiles[wave][0], k + (int64_t)t * KT * a.ks.token, low, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
-        Keys::template fill<64>(tiles[wave][1], v + (int64_t)t * KT * a.vs.token, low, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
+        Keys::template fill<64, PAST>(tiles[wave][0], k + (int64_t)t * KT * a.ks.token, low, left, row_bytes, lane, [&](int row) { return row * a.ks.token; });
+        Keys::template fill<64, PAST>(tiles[wave][1], v + (int64_t)t * KT * a.vs.token, low, left, row_bytes, lane, [&](int row) { return row * a.vs.token; });
     };
     if (lo + wave < hi) fetch(lo + wave);
     Columns<T, DP> c;
@@ -314,15 +315,20 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(kThreads) void jo
 
 // ------------------------------------------------------------------ host side
 
-// How the work is cut: columns into blocks of 128 (of 32 where there are no more), and the keys into parts where that leaves CUs without work.
-//   few columns: 1024 workgroups, four a CU, of eight tiles at least (32 tokens over caches of up to 8192 keys: 63 us with 512, 60 so); 256 of four at least where there are not so many keys (one
-//   token of 32 heads on 8 over 4097: 11.3 us with eight, 10.4 with four);
-//   many: 512 of four tiles at least, in fp32, whose products take sixteen times as long, of one (777 tokens of 6 heads of 72: 48 us with four, 35 with one).
+// How the work is cut: columns into blocks, of 128 for attend or of 32 for attend_few, and the keys into parts where that leaves CUs without work.
+//   one block of 32 (few queries): attend_few, 1024 workgroups, four a CU, of eight tiles at least (32 tokens over caches of up to 8192 keys: 63 us with 512, 60 so); 256 of four at least where there
+//   are not so many keys (one token of 32 heads on 8 over 4097: 11.3 us with eight, 10.4 with four);
+//   blocks of 128 that leave CUs or matrix units without work: attend_few too, whose wavefronts share the keys of 32 columns without a second kernel.  bfloat16, 16 heads of 64, 1024 tokens: 23.4 us
+//   from attend, 11.3 so, 16 heads of 128 26.8 and 17.3, 32 heads of 64, 512 tokens 17.3 and 8.3; but, since a tile is read for fewer columns, 64 tokens of 32 heads on 8 over 16000 keys 24 and 34, 32
+//   heads of 128, 1000 tokens 24.8 and 27.5, hence the limits.  fp32, 8 heads of 64, 4 x 1024 tokens: 77 and 57, 777 tokens of 6 heads of 72 35 and 28, but 16 x 256 tokens of 16 heads of 64 36 and 47.
+//   256 workgroups at least, 512 where fp32 sequences are long (4 heads of 128, 2048 tokens: 84 and 65 us; 8 heads, 1024 tokens 47 and 59);
+//   else attend, in bfloat16 over long sequences with 512 workgroups of four tiles at least.
 struct Cut { bool few; int64_t blocks; int splits, tiles; };
 Cut cut_of(const division_attention& a) {
     Cut c;
     const int64_t R = a.H / a.G, cols = a.Sq * R, half = a.dt == DIVISION_BF16;
-    c.few = cols <= 32;
+    const int64_t wide = (cols + 127) / 128 * a.B * a.G;
+    c.few = cols <= 32 || (half ? a.Sk <= 2048 && (wide <= 128 || (wide < 256 && a.Sk >= 512 && (a.D <= 64 || a.D > 96))) : wide < (a.Sk < 1024 ? 256 : a.D <= 64 ? 512 : 320));
     c.blocks = (cols + (c.few ? 31 : 127)) / (c.few ? 32 : 128);
     const int64_t tile = c.few ? 32 : 64, tiles = (a.Sk + tile - 1) / tile, tasks = c.blocks * a.B * a.G;
     const auto parts = [&](int64_t wanted, int64_t least) {
@@ -333,10 +339,10 @@ Cut cut_of(const division_attention& a) {
         if (c.splits < 1) c.splits = 1;
     };
     if (c.few) {
-        parts(1024, half ? 8 : 4);
-        if (tasks * c.splits < 256) parts(256, half ? 4 : 2);
+        parts(cols <= 32 ? 1024 : half || a.Sk < 2048 ? 256 : 512, half ? 8 : 4);
+        if (cols <= 32 && tasks * c.splits < 256) parts(256, half ? 4 : 2);
     } else if (tasks < 256) {
-        parts(512, half ? 4 : 1);
+        parts(512, 4);
     } else {
         parts(tasks, 1);
     }
@@ -346,7 +352,15 @@ size_t parts_bytes(const division_attention& a, const Cut& c) { return c.splits 
 
 template <typename T, int DP> int run(const AttentionArgs& args, const Cut& c, int64_t grid, hipStream_t st) {
     constexpr int kFew = sizeof(T) == 2 && DP == 96 ? 128 : DP;                      // 96 bfloat16 are no rows of eight pieces
-    if (c.few) hipLaunchKernelGGL((attend_few<T, kFew, 32, sizeof(T) == 2 ? 4 : 2>), dim3((uint32_t)grid), dim3(sizeof(T) == 2 ? 256 : 128), 0, st, args);
+    // keys that one block of columns looks at are looked at once
+    // keys that one block of columns looks at are looked at once.  In fp32 two wavefronts, so that two workgroups fit a CU's local memory, unless there are no two (16 tokens over 2000 keys, 8 heads of
+    // 128: 80 us with four, 69 so; one token of 32 heads on 8 over 4000: 19 us with two, 14 so)
+    void (*few)(AttentionArgs) = c.blocks > 1 ? attend_few<T, kFew, 32, 4, false> : attend_few<T, kFew, 32, 4, true>;
+    int waves = 4;
+    if constexpr (sizeof(T) == 4) {
+        if (c.blocks == 1 && grid > 256) { few = attend_few<T, kFew, 32, 2, true>; waves = 2; }
+    }
+    if (c.few) hipLaunchKernelGGL(few, dim3((uint32_t)grid), dim3(64 * waves), 0, st, args);
     else hipLaunchKernelGGL((attend<T, DP, 64>), dim3((uint32_t)grid), dim3(kThreads), 0, st, args);
     CHECKED(launched());
     if (c.splits == 1) return DIVISION_OK;

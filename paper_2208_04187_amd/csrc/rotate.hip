@@ -319,7 +319,7 @@ template <typename T, int V, int U, int LANES, bool BACK> int launch(RotateArgs&
     const int block = a.block[0] > a.block[1] ? a.block[0] : a.block[1];
     size_t lds = (size_t)block * a.rotated * sizeof(float2);
     if (BACK && lds < (size_t)a.D * 4) lds = (size_t)a.D * 4;
-    // Calls whose tensors together are beyond the caches go past them (67200 tokens, 32 heads on 4 of 64 in bfloat16: 70.8 us kept, 66.0 so; backward 116 and 107).  Only whole vectors: single
+    // Calls whose tensors together are beyond the caches go past them (16384 tokens, 32 and 8 heads of 128 in bfloat16: 70.8 us kept, 66.0 so; backward 116 and 107).  Only whole vectors: single
     // elements count on the caches to join them.
     constexpr bool kPast = V > 1;
     const bool past = kPast && a.T * (a.heads[0] + a.heads[1]) * (BACK ? 3 : 2) * a.D * (int64_t)sizeof(T) > kCached;

@@ -137,7 +137,7 @@ template <typename T, int DP, int ROWS> struct RowTile {
     }
     static __device__ __forceinline__ int place(int row, int piece) { return row * kRowBytes + ((piece ^ turn(row)) << 4); }
 
-    template <int THREADS, typename At> static __device__ __forceinline__ void fill(char* tile, const char* base, int low, int rows, int row_bytes, int thread, At&& at) {
+    template <int THREADS, bool PAST, typename At> static __device__ __forceinline__ void fill(char* tile, const char* base, int low, int rows, int row_bytes, int thread, At&& at) {
         constexpr int kEach = kBytes / 16 / THREADS;
         static_assert(kEach * THREADS * 16 == kBytes, "whole pieces a thread");
         const u32x4 from = buffer(base, 0x7fffffffu);
@@ -147,7 +147,8 @@ template <typename T, int DP, int ROWS> struct RowTile {
         for (int u = 0; u < kEach; ++u) {
             const int slot = u * THREADS + thread, row = slot / kPieces, piece = (slot % kPieces) ^ turn(row);
             const uint32_t off = (uint32_t)(row - low) < count && piece * 16 < row_bytes ? (uint32_t)(at(row) + piece * 16) : 0x80000000u;
-            load_lds16_past(from, tile + (u * THREADS + first) * 16, off);
+            if constexpr (PAST) load_lds16_past(from, tile + (u * THREADS + first) * 16, off);
+            else load_lds16(from, tile + (u * THREADS + first) * 16, off);
         }
     }
     static __device__ __forceinline__ Operand<T> rows(const char* tile, int row0, int step, int lane) {

@@ -162,6 +162,21 @@ def test_many_queries_of_few_keys_heads(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [24, 64, 72, 128])
+def test_many_workgroups(D, dtype):
+    """Whole blocks of 128 queries for all CUs, without parts of the keys, and as few as that a block of 32 pays"""
+    _check(*_inputs(16, 130, 140, 16, 16, D, dtype), causal=True)
+    _check(*_inputs(16, 130, 140, 16, 8, D, dtype), window=50, lengths=[140 - 9 * b for b in range(16)])
+    _check(*_inputs(3, 200, 600, 16, 8, D, dtype), causal=True, lengths=[600, 77, 0])
+
+
+@pytest.mark.parametrize("size", [(1, 200, 2500, 2, 1, 64), (2, 70, 2100, 4, 2, 128), (1, 300, 2300, 3, 3, 96)])
+def test_parts_of_long_sequences(size):
+    _check(*_inputs(*size, BF16), causal=True)
+    _check(*_inputs(*size, BF16), window=700, lengths=[2000, 100][:size[0]])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_scales_and_large_scores(dtype):
     x = _inputs(2, 40, 70, 4, 2, 64, dtype, seed=2)
     _check(*x, scale=1.0)
