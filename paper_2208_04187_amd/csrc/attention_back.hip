@@ -20,7 +20,7 @@ struct BackArgs : AttentionArgs {
     Heads gs;
     char *dq, *dk, *dv;
     float *key_sums, *query_sums;                       // the parts of dk and dv, where the columns are cut, and of dq, where the keys are
-    int query_splits;
+    int query_splits, least_keys, least_columns;        // parts, and how many tiles one has at least
     float* stats;                                       // [group][column][2]: lse in powers of two (infinity where nothing is seen), rowsum(grad out)
     FastDiv by_R;
 };
@@ -50,9 +50,7 @@ template <typename T, int DP> __device__ __forceinline__ void get_column(Operand
 
 constexpr int kThreads = 256;
 
-// A workgroup's part of the tiles lo .. hi - 1 that it would have to look at: equal parts, of so many tiles at least.  (An fp32 tile keeps a wavefront busy for 5 to 7 us.)
-template <typename T> constexpr int kLeastKeys = sizeof(T) == 2 ? 4 : 2;
-template <typename T> constexpr int kLeastColumns = sizeof(T) == 2 ? 8 : 2;
+// A workgroup's part of the tiles lo .. hi - 1 that it would have to look at: equal parts, of so many tiles at least
 __device__ __forceinline__ void part_of(int split, int splits, int least, int& lo, int& hi) {
     if (splits == 1) return;
     const int each = max((hi - lo + splits - 1) / splits, least);
@@ -102,7 +100,7 @@ template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_b
     const int first_key = seen.from(0);                     // what stands before every query's keys is not looked at either
     const uint32_t last_col = min(first_col + kCols - 1, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
     int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
-    part_of(split, a.query_splits, kLeastKeys<T>, lo, hi);
+    part_of(split, a.query_splits, a.least_keys, lo, hi);
     const bool works = wave_col < cols, there = col < cols;
     const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
     const int whole_from = seen.from(qb), whole_to = seen.to(qa);
@@ -217,7 +215,7 @@ template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global
     // the columns of the workgroup, of the wavefront and of the lane: those of whole queries
     const bool any = first < seen.keys, works = wave_key < seen.keys, there = key < seen.keys;
     int lo = any ? seen.query_from(first) * a.R / CT : 0, hi = any ? (seen.query_to(last) * a.R + CT - 1) / CT : 0;
-    part_of(split, a.splits, kLeastColumns<T>, lo, hi);
+    part_of(split, a.splits, a.least_columns, lo, hi);
     const int whole_from = seen.query_from(min(wave_key + 31, a.Sk - 1)) * a.R, whole_to = works && wave_key + 31 < seen.keys ? seen.query_to(wave_key) * a.R : 0;
     const int from = there ? seen.query_from(key) * a.R : 0, to = there ? max(from, seen.query_to(key) * a.R) : 0;
     const char* q = a.q + b * a.qs.batch + (int64_t)g * a.R * a.qs.head;
@@ -348,16 +346,19 @@ template <typename T, bool QUERIES> __global__ __launch_bounds__(kThreads) void 
 
 size_t stats_bytes(const division_attention& a) { return ((size_t)(a.B * a.Sq * a.H) * 8 + 15) / 16 * 16; }
 
-// fp32 products are slow enough for small workgroups to pay: 64 columns or keys, their tiles shared by two (four) sets.  (2 x 1531 tokens, 12 heads of 64, window 256: 228 us with workgroups of 128, 191 so.)
+// The workgroups' shapes.  fp32 products are slow enough for small ones to pay: 64 columns or keys, their tiles shared by two (four) sets.  (2 x 1531 tokens, 12 heads of 64, window 256: 228 us with
+// workgroups of 128, 191 so.)  FEW, in bfloat16: 64 too, and four sets, where blocks of 128 leave CUs without work (16 heads of 64, 1024 tokens: 52 us, 32 so; of 128, 81 and 47; but 2 x 12 heads of
+// 64, 1531 tokens, which make 288 blocks, 48 and 55).
 constexpr int kColumnTile = 32;
-template <typename T, int DP> struct Shape {
-    static constexpr bool kSmall = sizeof(T) == 4 && DP <= 64;
-    static constexpr int kKeyTile = sizeof(T) == 2 ? 64 : 32, kQueryWaves = sizeof(T) == 2 ? 4 : 2, kQuerySets = sizeof(T) == 2 ? 1 : 2;
-    static constexpr int kKeyWaves = kSmall ? 2 : 4, kKeySets = kSmall ? 4 : sizeof(T) == 2 ? 2 : 1;
-    static constexpr bool kValues = sizeof(T) == 2 && DP == 128;
+template <typename T, int DP, bool FEW> struct Shape {
+    static constexpr bool kHalf = sizeof(T) == 2, kSmall = !kHalf && DP <= 64;
+    static constexpr int kKeyTile = kHalf && !FEW ? 64 : 32, kQueryWaves = kHalf && !FEW ? 4 : 2, kQuerySets = kHalf ? (FEW ? 4 : 1) : 2;
+    static constexpr int kKeyWaves = kSmall || FEW ? 2 : 4, kKeySets = kSmall || FEW ? 4 : kHalf ? 2 : 1;
+    static constexpr bool kValues = kHalf && DP == 128;
 };
-// Parts of what a workgroup would have to look at, where there are few workgroups: as many as make two a CU.  (One sequence of 2048, 32 heads on 4 of keys: 484 us with the columns of 128 keys in one
-// part, 181 so.  Two heads of 4090 tokens, whose queries' keys are cut too: 163 us in one part, 100 so.)
+// Parts of what a workgroup would have to look at, where there are few workgroups: as many as make two a CU, of so many tiles at least that they pay for adding them up.  (One sequence of 2048, 32 heads
+// on 4 of keys: 484 us with the columns of 128 keys in one part, 166 so.  Two heads of 4090 tokens, whose queries' keys are cut too: 163 us in one part, 90 so.  Parts of 8 tiles for four sets: 8 heads
+// of 64, 1024 tokens 47 us, 31 with 24.)
 constexpr int kMostSplits = 32;
 int parts_of(int64_t tasks, int64_t tiles, int64_t least) {
     if (tasks == 0 || tasks >= 256) return 1;
@@ -365,43 +366,66 @@ int parts_of(int64_t tasks, int64_t tiles, int64_t least) {
     if (n > tiles / least) n = tiles / least;
     return n < 1 ? 1 : n > kMostSplits ? kMostSplits : (int)n;
 }
-struct Splits { int queries, keys; };
+struct Splits { int queries, keys, least_keys, least_columns; bool few_queries, few_keys; };
 Splits splits_of(const division_attention& a) {
     const bool half = a.dt == DIVISION_BF16;
-    const int64_t cols = a.Sq * (a.H / a.G), groups = a.B * a.G, key_tile = half ? 64 : 32, of_queries = half ? 128 : 64, of_keys = half || a.D > 64 ? 128 : 64;
-    return {parts_of((cols + of_queries - 1) / of_queries * groups, (a.Sk + key_tile - 1) / key_tile, half ? kLeastKeys<uint16_t> : kLeastKeys<float>),
-            parts_of((a.Sk + of_keys - 1) / of_keys * groups, (cols + kColumnTile - 1) / kColumnTile, half ? kLeastColumns<uint16_t> : kLeastColumns<float>)};
+    const int64_t cols = a.Sq * (a.H / a.G), groups = a.B * a.G;
+    Splits s;
+    // not over long sequences, whose parts keep larger workgroups busy too (two heads of 128, 4090 tokens: 89 us, 97 with small ones)
+    s.few_queries = half && (cols + 127) / 128 * groups < 256 && a.Sk <= 2048;
+    s.few_keys = half && (a.Sk + 127) / 128 * groups < 256 && cols <= 4096;
+    s.least_keys = s.few_queries ? 24 : half ? 4 : 2;
+    s.least_columns = s.few_keys ? 24 : half ? 8 : 2;
+    const int64_t key_tile = half && !s.few_queries ? 64 : 32, of_queries = half && !s.few_queries ? 128 : 64, of_keys = s.few_keys || (!half && a.D <= 64) ? 64 : 128;
+    s.queries = parts_of((cols + of_queries - 1) / of_queries * groups, (a.Sk + key_tile - 1) / key_tile, s.least_keys);
+    s.keys = parts_of((a.Sk + of_keys - 1) / of_keys * groups, (cols + kColumnTile - 1) / kColumnTile, s.least_columns);
+    return s;
 }
 size_t key_bytes(const division_attention& a) { const int n = splits_of(a).keys; return n > 1 ? (size_t)n * a.B * a.G * a.Sk * 2 * a.D * 4 : 0; }
 size_t query_bytes(const division_attention& a) { const int n = splits_of(a).queries; return n > 1 ? (size_t)n * a.B * a.H * a.Sq * a.D * 4 : 0; }
 size_t back_bytes(const division_attention& a) { return stats_bytes(a) + key_bytes(a) + query_bytes(a); }
 
-template <typename T, int DP> int run(BackArgs& args, hipStream_t st) {
-    typedef Shape<T, DP> S;
-    constexpr int kCols = 32 * S::kQueryWaves, kKeys = 32 * S::kKeyWaves;
-    const int64_t blocks = ((int64_t)args.Sq * args.R + kCols - 1) / kCols;
-    const int64_t grid = blocks * args.groups * args.query_splits, key_grid = ((int64_t)args.Sk + kKeys - 1) / kKeys * args.groups * args.splits;
-    if (grid >= (int64_t(1) << 23) || key_grid >= (int64_t(1) << 23)) return DIVISION_ERANGE;
-    if (args.Sq > 0) {
-        args.blocks = (int)blocks;
-        hipLaunchKernelGGL((back_queries<T, DP, S::kKeyTile, S::kQueryWaves, S::kQuerySets>), dim3((uint32_t)grid), dim3(64 * S::kQueryWaves * S::kQuerySets), 0, st, args);
-        CHECKED(launched());
-        if (args.query_splits > 1) {
-            const int64_t pieces = (int64_t)args.groups * args.Sq * args.R * (args.D / 4);
-            hipLaunchKernelGGL((add_parts<T, true>), dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, args);
-            CHECKED(launched());
-        }
-    }
-    if (args.Sk > 0) {
-        hipLaunchKernelGGL((back_keys<T, DP, kColumnTile, S::kKeyWaves, S::kKeySets, S::kValues>), dim3((uint32_t)key_grid), dim3(64 * S::kKeyWaves * S::kKeySets), 0, st, args);
-        CHECKED(launched());
-        if (args.splits > 1) {
-            const int64_t pieces = (int64_t)args.groups * args.Sk * (args.D / 2);
-            hipLaunchKernelGGL((add_parts<T, false>), dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, args);
-            CHECKED(launched());
-        }
-    }
-    return DIVISION_OK;
+// The two launches; `check`: whether they can be, without them
+template <typename T, int DP, bool FEW> int run_queries(BackArgs& args, bool check, hipStream_t st) {
+    typedef Shape<T, DP, FEW> S;
+    constexpr int kCols = 32 * S::kQueryWaves, kWorkgroup = 64 * S::kQueryWaves * S::kQuerySets;
+    const int64_t blocks = ((int64_t)args.Sq * args.R + kCols - 1) / kCols, grid = blocks * args.groups * args.query_splits;
+    if (grid >= (int64_t(1) << 23)) return DIVISION_ERANGE;
+    if (check || grid == 0) return DIVISION_OK;
+    args.blocks = (int)blocks;
+    hipLaunchKernelGGL((back_queries<T, DP, S::kKeyTile, S::kQueryWaves, S::kQuerySets>), dim3((uint32_t)grid), dim3(kWorkgroup), 0, st, args);
+    CHECKED(launched());
+    if (args.query_splits == 1) return DIVISION_OK;
+    const int64_t pieces = (int64_t)args.groups * args.Sq * args.R * (args.D / 4);
+    hipLaunchKernelGGL((add_parts<T, true>), dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, args);
+    return launched();
+}
+template <typename T, int DP, bool FEW> int run_keys(const BackArgs& args, bool check, hipStream_t st) {
+    typedef Shape<T, DP, FEW> S;
+    constexpr int kKeys = 32 * S::kKeyWaves, kWorkgroup = 64 * S::kKeyWaves * S::kKeySets;
+    const int64_t grid = ((int64_t)args.Sk + kKeys - 1) / kKeys * args.groups * args.splits;
+    if (grid >= (int64_t(1) << 23)) return DIVISION_ERANGE;
+    if (check || grid == 0) return DIVISION_OK;
+    hipLaunchKernelGGL((back_keys<T, DP, kColumnTile, S::kKeyWaves, S::kKeySets, S::kValues>), dim3((uint32_t)grid), dim3(kWorkgroup), 0, st, args);
+    CHECKED(launched());
+    if (args.splits == 1) return DIVISION_OK;
+    const int64_t pieces = (int64_t)args.groups * args.Sk * (args.D / 2);
+    hipLaunchKernelGGL((add_parts<T, false>), dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, args);
+    return launched();
+}
+template <typename T, int DP> int run(BackArgs& args, const Splits& splits, hipStream_t st) {
+    const auto queries = [&](bool check) {
+        if constexpr (sizeof(T) == 2) if (splits.few_queries) return run_queries<T, DP, true>(args, check, st);
+        return run_queries<T, DP, false>(args, check, st);
+    };
+    const auto keys = [&](bool check) {
+        if constexpr (sizeof(T) == 2) if (splits.few_keys) return run_keys<T, DP, true>(args, check, st);
+        return run_keys<T, DP, false>(args, check, st);
+    };
+    CHECKED(queries(true));
+    CHECKED(keys(true));
+    CHECKED(queries(false));
+    return keys(false);
 }
 
 }  // namespace
@@ -437,12 +461,14 @@ int division_attention_backward(const division_attention* attention, const divis
     const Splits splits = splits_of(a);
     args.splits = splits.keys;
     args.query_splits = splits.queries;
+    args.least_keys = splits.least_keys;
+    args.least_columns = splits.least_columns;
     args.key_sums = reinterpret_cast<float*>(static_cast<char*>(w.workspace) + stats_bytes(a));
     args.query_sums = reinterpret_cast<float*>(static_cast<char*>(w.workspace) + stats_bytes(a) + key_bytes(a));
     args.by_R = make_fastdiv((uint32_t)args.R);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, st) : a.D <= 96 ? run<uint16_t, 96>(args, st) : run<uint16_t, 128>(args, st);
-    return a.D <= 32 ? run<float, 32>(args, st) : a.D <= 64 ? run<float, 64>(args, st) : a.D <= 96 ? run<float, 96>(args, st) : run<float, 128>(args, st);
+    if (a.dt == DIVISION_BF16) return a.D <= 64 ? run<uint16_t, 64>(args, splits, st) : a.D <= 96 ? run<uint16_t, 96>(args, splits, st) : run<uint16_t, 128>(args, splits, st);
+    return a.D <= 32 ? run<float, 32>(args, splits, st) : a.D <= 64 ? run<float, 64>(args, splits, st) : a.D <= 96 ? run<float, 96>(args, splits, st) : run<float, 128>(args, splits, st);
 }
 
 }  // extern "C"

@@ -170,6 +170,15 @@ def test_many_workgroups(D, dtype):
     _check(*_inputs(3, 200, 600, 16, 8, D, dtype), causal=True, lengths=[600, 77, 0])
 
 
+@pytest.mark.parametrize("D", [40, 64, 96, 128])
+def test_gradients_of_few_workgroups(D):
+    """Blocks of 64 whose tiles four groups of wavefronts share, in parts and not; many keys of few queries, many queries of few keys"""
+    _check(*_inputs(2, 700, 700, 2, 2, D, BF16), causal=True, lengths=[700, 333])
+    _check(*_inputs(1, 70, 1900, 4, 2, D, BF16), causal=True, window=900)
+    _check(*_inputs(1, 1030, 130, 8, 2, D, BF16))
+    _check(*_inputs(1, 1300, 130, 8, 2, D, BF16), window=100)
+
+
 @pytest.mark.parametrize("size", [(1, 200, 2500, 2, 1, 64), (2, 70, 2100, 4, 2, 128), (1, 300, 2300, 3, 3, 96)])
 def test_parts_of_long_sequences(size):
     _check(*_inputs(*size, BF16), causal=True)
