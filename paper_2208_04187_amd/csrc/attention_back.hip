@@ -84,7 +84,10 @@ template <int SETS, int THREADS, int N> __device__ __forceinline__ void add_sets
     }
 }
 
-// Wavefronts of 32 columns (queries) each, WAVES of them, share the tiles of the keys and values.  SETS such take every SETS-th tile each.
+// Wavefronts of 32 columns (queries) each, WAVES of them, share the tiles of the keys and values.  SETS such take every SETS-th tile each.  Z = K Q^T and dP = V grad^T have a query a lane, to whom
+// its lse and rowsum belong; dS's registers are the operand of dQ = K^T dS as they are.  The rowsum is left in `stats` for the other kernel.
+// Three products.  Bound by the matrix unit and its power: 2 x 4096 tokens, 32 heads on 8 of 128 in bfloat16, causal, 392 to 416 us = 990 to 1050 TFLOP/s; 2 x 1531 tokens of 12 heads of 64 in fp32,
+// window 256, 87 us, of which the products of whole tiles alone are 56.
 template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_bounds__(64 * WAVES * SETS, sizeof(T) == 2 ? 2 : 1) void back_queries(BackArgs a) {
     constexpr int kTile = Tile<T, DP, KT>::kBytes, kSet = 64 * WAVES, kCols = 32 * WAVES;
     static_assert(SETS == 1 || kSet * (DP / 32) * 64 <= 4 * SETS * kTile, "a set's blocks in place of the tiles");
@@ -194,7 +197,9 @@ template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_b
 
 // Wavefronts of 32 keys each, WAVES of them, share the tiles of the columns (queries of all heads that share the keys) and their gradients.  SETS such take every SETS-th
 // tile each: with two there are always two wavefronts a SIMD, one with the matrix unit while the other takes exponentials.  VALUES: the values wait in the
-// local memory, not in registers.
+// local memory, not in registers, of which dK, dV and K take 192 at 128 features.  Z = Q K^T and dP = grad V^T have a key a lane: P and dS are operands of dV = grad^T P and dK = Q^T dS as they are.
+// Four products.  Bound as the queries' kernel: the same cases 574 to 630 us = 870 to 960 TFLOP/s, and 123 us in fp32 (75 for the products alone; 576 workgroups on 256 CUs leave a third of the last
+// round empty).
 template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global__ __launch_bounds__(64 * WAVES * SETS) void back_keys(BackArgs a) {
     constexpr int kSet = 64 * WAVES, kKeys = 32 * WAVES;
     typedef Tile<T, DP, CT> Columns;
@@ -321,7 +326,7 @@ template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global
     put_column<T, DP>(reinterpret_cast<T*>(a.dv) + row, dv, 1.0f, a.D, half);
 }
 
-// The parts of gradients, in their order: four elements a thread.  QUERIES: of dq, [group][column][D]; else of dk and dv, [group][key][2][D]
+// The parts of gradients, in their order: four elements a thread, eight loads on their way.  Bound by memory.  QUERIES: of dq, [group][column][D]; else of dk and dv, [group][key][2][D]
 template <typename T, bool QUERIES> __global__ __launch_bounds__(kThreads) void add_parts(BackArgs a) {
     const int pieces = (QUERIES ? a.D : 2 * a.D) / 4, splits = QUERIES ? a.query_splits : a.splits;
     const int64_t rows = QUERIES ? (int64_t)a.Sq * a.R : a.Sk, n = (int64_t)a.groups * rows, at = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = at / pieces;

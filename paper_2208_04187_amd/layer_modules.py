@@ -9,6 +9,9 @@ DivisionHeadNormRotation caches the tensors before the norm, as DivisionRMSNorm 
 DivisionEmbedding caches the tokens, DivisionResidualDropout nothing but its seed.
 
 First derivatives only: a second one raises.  Only calls the binding.
+
+A backward pass that is captured into a graph needs parameters that no eager graph still holds (drop its outputs first): torch adds a parameter's gradient up on the stream on which the first
+graph met it, which a capture cannot leave.  The first call of a DivisionHeadNormRotation on a device copies its frequencies there: make it before the capture.
 """
 from __future__ import annotations
 
@@ -164,7 +167,8 @@ class _ResidualDropout(torch.autograd.Function):
 
 class DivisionResidualDropout(torch.nn.Module):
     """forward(x, residual=None) -> residual + dropout(x), kept elements divided by 1 - p, without a stored mask.  Call number n of this module while training drops what seed + n says
-    (DivisionDropout's elements of the same call); in eval mode nothing is dropped."""
+    (DivisionDropout's elements of the same call); in eval mode nothing is dropped.  A captured graph drops the captured call's elements whenever it is replayed: for others each time call
+    division_dropout_add with a seed on the device."""
 
     def __init__(self, p: float = 0.5, seed: int = 0):
         super().__init__()
