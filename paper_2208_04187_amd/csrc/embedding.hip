@@ -46,51 +46,64 @@ template <typename T, bool PAST> __global__ __launch_bounds__(kThreads) void loo
 // ------------------------------------------------------------------ the tokens in the order of their ids
 
 constexpr int kOrderThreads = 1024, kOrderWaves = kOrderThreads / 64, kMostRows = 512;       // rows of the table whose tokens a workgroup puts in order
-constexpr int kKept = 16;                                   // ids of a thread that stay in registers between the two times they are looked at: 16384 tokens
+constexpr int kKept = 16;                                   // ids of a thread that come at once
 
+// Rows are dealt out to the workgroups like cards, since a tokenizer's frequent tokens have the lowest numbers: row k 2^bits + w of the table is row k of workgroup w, place w * rows + k of all.
+// (16384 tokens whose frequencies fall as 1 / (number + 3): 25.5 us with neighbours in a workgroup, 12.6 so, and the rows' sums 32 and 24.)
+struct Dealt {
+    int bits;                                               // of the workgroups' number
+    uint32_t rows;                                          // of a workgroup
+    __host__ __device__ __forceinline__ uint32_t workgroups() const { return 1u << bits; }
+    __host__ __device__ __forceinline__ uint32_t places() const { return rows << bits; }
+    __device__ __forceinline__ uint32_t place(uint32_t row) const { return (row & (workgroups() - 1)) * rows + (row >> bits); }
+    __device__ __forceinline__ uint32_t row(uint32_t place) const { return (place % rows << bits) + place / rows; }
+};
 struct OrderArgs {
     const int64_t* ids;
-    uint32_t *order, *starts;                               // [T] tokens by (id, number); [V + 1] where a row's begin
+    uint32_t *order, *starts;                               // [T] tokens by (place of the id, number); [places + 1] where a place's begin
     int64_t V, ignore;
     uint32_t T;
-    int rows, bits;                                         // of a workgroup, and of a row's number among them
+    int bits;                                               // of a row's number among a workgroup's
+    Dealt dealt;
 };
 
 // One launch instead of the passes of a sort.  Every workgroup reads all ids and keeps those of its rows; how many lie before its rows tells it where its tokens begin, so that workgroups need not wait for one another.  Each wavefront
 // has an equal run of the tokens.  First they count: [row][wavefront].  The running sum over these numbers is where a wavefront's tokens of a row begin, and then each puts its own there,
-// in their order.  Bound by its chain of trips and barriers: 16384 tokens of 32768 rows, 256 workgroups, 15.6 us.
+// in their order.  Bound by its chain: 16384 tokens of 32768 rows, 256 workgroups,
+// 12 to 14 us, of which the ids take 5.3 until they are there (one by one, 4 more), the running sum 1.3, putting tokens in their places 1.2 and more.
 __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     extern __shared__ uint32_t counts[];                    // [rows][kOrderWaves]
     __shared__ uint32_t sums[kOrderWaves], before;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.rows * kOrderWaves;
-    const int64_t lo = (int64_t)blockIdx.x * a.rows;
-    const uint32_t rows = (uint32_t)(a.V - lo < a.rows ? a.V - lo : a.rows);
+    __shared__ uint16_t kept[kKept][kOrderThreads];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)a.dealt.rows * kOrderWaves;
     const uint32_t run = (((a.T + kOrderWaves - 1) / kOrderWaves) + 63) & ~63u, first = wave * run, end = min(first + run, a.T);
     for (int e = threadIdx.x; e < n; e += kOrderThreads) counts[e] = 0;
     if (threadIdx.x == 0) before = 0;
     __syncthreads();
-    // the row among the workgroup's; before them: kBefore, none of them: kNone
-    constexpr uint32_t kNone = 0xffffffffu, kBefore = 0xfffffffeu;
-    const auto row_of = [&](uint32_t t) {
-        const int64_t id = t < end ? a.ids[t] : -1;
-        if (id < 0 || id >= a.V || id == a.ignore) return kNone;
-        return id < lo ? kBefore : id - lo < rows ? (uint32_t)(id - lo) : kNone;
+    // the row among the workgroup's; another before them: kBefore, none of them: kNone
+    constexpr uint32_t kNone = 0xffffu, kBefore = 0xfffeu;
+    // of kKept times 64 tokens, whose ids come at once: behind the last token its id again, which is none then
+    const auto rows_of = [&](uint32_t* to, uint32_t t) {
+        int64_t ids[kKept];
+#pragma unroll
+        for (int k = 0; k < kKept; ++k) ids[k] = a.ids[min(t + k * 64 + lane, end - 1)];
+#pragma unroll
+        for (int k = 0; k < kKept; ++k) {
+            const bool none = t + k * 64 + lane >= end || ids[k] < 0 || ids[k] >= a.V || ids[k] == a.ignore;
+            const uint32_t w = (uint32_t)ids[k] & (a.dealt.workgroups() - 1);
+            to[k] = none || w > blockIdx.x ? kNone : w < blockIdx.x ? kBefore : (uint32_t)ids[k] >> a.dealt.bits;
+        }
     };
-    uint32_t less = 0, kept[kKept];
-    const auto count = [&](uint32_t row) {
-        if (row == kBefore) ++less;
-        else if (row != kNone) atomicAdd(&counts[row * kOrderWaves + wave], 1u);
-    };
+    uint32_t less = 0;
+    for (uint32_t t = first; t < end; t += kKept * 64) {
+        uint32_t rows[kKept];
+        rows_of(rows, t);
 #pragma unroll
-    for (int k = 0; k < kKept; ++k) kept[k] = row_of(first + k * 64 + lane);
-#pragma unroll
-    for (int k = 0; k < kKept; ++k) count(kept[k]);
-    for (uint32_t t = first + kKept * 64; t < end; t += 256) {
-        uint32_t more[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) more[k] = row_of(t + k * 64 + lane);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) count(more[k]);
+        for (int k = 0; k < kKept; ++k) {
+            if (rows[k] == kBefore) ++less;
+            else if (rows[k] != kNone) atomicAdd(&counts[rows[k] * kOrderWaves + wave], 1u);
+            if (t == first) kept[k][threadIdx.x] = (uint16_t)rows[k];
+        }
     }
     for (int o = 32; o; o >>= 1) less += (uint32_t)__shfl_xor((int)less, o, 64);
     if (lane == 0) atomicAdd(&before, less);
@@ -112,13 +125,13 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     for (int e = from; e < to; ++e) {
         const uint32_t c = counts[e];
         counts[e] = at;
-        if (e % kOrderWaves == 0 && (uint32_t)(e / kOrderWaves) < rows) a.starts[lo + e / kOrderWaves] = at;
+        if (e % kOrderWaves == 0) a.starts[blockIdx.x * a.dealt.rows + e / kOrderWaves] = at;
         at += c;
     }
-    if (lo + rows == a.V && threadIdx.x == kOrderThreads - 1) a.starts[a.V] = at;
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == kOrderThreads - 1) a.starts[a.dealt.places()] = at;
     __syncthreads();
     // A row's tokens among the wavefront's 64: where there is one row or two, which is most often, one after the other; the lanes of more rows find their likes by the rows' bits.  (All by their bits:
-    // 16384 tokens of 32768 21 us instead of 15; all one after the other: a third of a microsecond for each row.)  The wavefront's own counter is moved on by one lane with an atomic, since the next
+    // 6 us more for 16384 tokens of 32768; all one after the other: a third of a microsecond for each row.)  The wavefront's own counter is moved on by one lane with an atomic, since the next
     // that reads it is another's.
     const auto place = [&](uint32_t row, uint32_t t) {
         const uint64_t below = (1ull << lane) - 1;
@@ -148,14 +161,16 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
         begin = (uint32_t)__shfl((int)begin, leader, 64);
         if (mine) a.order[begin + __builtin_popcountll(same & below)] = t;
     };
+    // (One round after another, not unrolled: sixteen copies of it take longer to come from memory than to run.)
+    for (uint32_t t = first; t < end; t += kKept * 64) {
+        if (t != first) {
+            uint32_t rows[kKept];
+            rows_of(rows, t);
 #pragma unroll
-    for (int k = 0; k < kKept; ++k) place(kept[k], first + k * 64 + lane);
-    for (uint32_t t = first + kKept * 64; t < end; t += 256) {
-        uint32_t more[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) more[k] = row_of(t + k * 64 + lane);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) place(more[k], t + k * 64 + lane);
+            for (int k = 0; k < kKept; ++k) kept[k][threadIdx.x] = (uint16_t)rows[k];
+        }
+#pragma unroll 1
+        for (int k = 0; k < kKept; ++k) place(kept[k][threadIdx.x], t + k * 64 + lane);
     }
 }
 
@@ -165,12 +180,13 @@ struct SumArgs {
     const void* grad;
     const int64_t* ids;
     const uint32_t *order, *starts;
+    Dealt dealt;
     float* parts;                                           // [parts of the sorted tokens][2][D]: of the row that began before the part, of the one that begins in it
     void* out;
     int64_t stride, V, D;
     uint32_t T, part;                                       // part: tokens that a wavefront adds up at most; a row of more is added up in parts
     float scale;
-    int add, columns, rows;                                 // columns: pieces of 64 * kSize * P elements of a row
+    int add, columns, rows, whole;                          // columns: pieces of 64 * kSize * P elements of a row; whole: no row ends within a vector
     int64_t count;                                          // parts of the tokens, where there are more than one's
 };
 
@@ -186,6 +202,18 @@ template <typename T, int P> struct Row {
     }
     // adds tokens order[from .. to - 1]; c: a column.  64 tokens' numbers come at once, a lane each, their rows several at a time.
     __device__ __forceinline__ void add(const SumArgs& a, uint32_t from, uint32_t to, int64_t c) {
+        if (a.whole) add_of<true>(a, from, to, c);
+        else add_of<false>(a, from, to, c);
+    }
+    // WHOLE: rows are whole vectors.  Lanes behind the last column take the first one's, so that no load waits for a branch
+    template <bool WHOLE> __device__ __forceinline__ void add_of(const SumArgs& a, uint32_t from, uint32_t to, int64_t c) {
+        int64_t cs[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) cs[p] = WHOLE && c + p * 64 * U::kSize >= a.D ? 0 : c + p * 64 * U::kSize;
+        const auto load = [&](U& q, const T* row, int p) {
+            if constexpr (WHOLE) q.load(row + cs[p]);
+            else q = load_some<U>(row, cs[p], a.D);
+        };
         constexpr int kAtOnce = P == 1 ? 8 : 4;
         const T* grad = static_cast<const T*>(a.grad);
         const uint32_t lane = threadIdx.x & 63;
@@ -199,7 +227,7 @@ template <typename T, int P> struct Row {
                 for (int u = 0; u < kAtOnce; ++u) {
                     const T* row = grad + (int64_t)(uint32_t)__builtin_amdgcn_readlane(tokens, j + u) * a.stride;
 #pragma unroll
-                    for (int p = 0; p < P; ++p) q[u][p] = load_some<U>(row, c + p * 64 * U::kSize, a.D);
+                    for (int p = 0; p < P; ++p) load(q[u][p], row, p);
                 }
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u)
@@ -215,7 +243,7 @@ template <typename T, int P> struct Row {
                 for (int u = 0; u < kAtOnce - 1; ++u) {
                     const T* row = grad + (int64_t)(uint32_t)__builtin_amdgcn_readlane(tokens, min(j + u, n - 1)) * a.stride;
 #pragma unroll
-                    for (int p = 0; p < P; ++p) q[u][p] = load_some<U>(row, c + p * 64 * U::kSize, a.D);
+                    for (int p = 0; p < P; ++p) load(q[u][p], row, p);
                 }
 #pragma unroll
                 for (int u = 0; u < kAtOnce - 1; ++u) {
@@ -251,13 +279,13 @@ template <typename T, typename O, int P> __device__ __forceinline__ void put_row
 // Parts of rows of many tokens: a wavefront has `part` sorted tokens and a piece of the columns.  Of such rows at most two have tokens among them.
 template <typename T, int P> __device__ __forceinline__ void sum_part(const SumArgs& a, uint32_t part, int64_t c) {
     typedef Unit<T> U;
-    const uint32_t begin = part * a.part, total = a.starts[a.V];
+    const uint32_t begin = part * a.part, total = a.starts[a.dealt.places()];
     if (begin >= total) return;
     const uint32_t end = min(begin + a.part, total);
-    const int64_t rows[2] = {a.ids[a.order[begin]], a.ids[a.order[end - 1]]};
+    const uint32_t places[2] = {a.dealt.place((uint32_t)a.ids[a.order[begin]]), a.dealt.place((uint32_t)a.ids[a.order[end - 1]])};
     for (int k = 0; k < 2; ++k) {
-        if (k && rows[1] == rows[0]) break;
-        const uint32_t from = a.starts[rows[k]], to = a.starts[rows[k] + 1];
+        if (k && places[1] == places[0]) break;
+        const uint32_t from = a.starts[places[k]], to = a.starts[places[k] + 1];
         if (to - from <= a.part) continue;
         Row<T, P> sum;
         sum.zero();
@@ -272,7 +300,7 @@ template <typename T, int P> __device__ __forceinline__ void sum_part(const SumA
 
 // The table's gradient: the first wavefronts have parts of rows of many tokens, each of the others kRows rows (one where there are not wavefronts enough for all SIMDs otherwise), whose tokens lie
 // one behind the other in the order; all a piece of the columns.  No row is written twice, rows without a token get their zeros here.  Bound by memory and the longest chain, three dependent loads
-// before the first row: 16384 tokens of 32768 rows of 1024 in bfloat16 19 us (100 MB).
+// before the first row: 16384 tokens of 32768 rows of 1024 in bfloat16 18 us (100 MB), 24 where tokens are as uneven as 1 / (number + 3).
 constexpr int kRows = 4;
 template <typename T, typename O, int P> __global__ __launch_bounds__(kThreads) void sum_tokens(SumArgs a) {
     typedef Unit<T> U;
@@ -282,19 +310,20 @@ template <typename T, typename O, int P> __global__ __launch_bounds__(kThreads) 
         sum_part<T, P>(a, (uint32_t)which, c);
         return;
     }
-    const int64_t row0 = (which - a.count) * a.rows;
-    if (row0 >= a.V) return;
+    const int64_t place0 = (which - a.count) * a.rows, places = a.dealt.places();
+    if (place0 >= places) return;
     uint32_t starts[kRows + 1];
 #pragma unroll
-    for (int r = 0; r <= kRows; ++r) starts[r] = a.starts[row0 + r < a.V ? row0 + r : a.V];
+    for (int r = 0; r <= kRows; ++r) starts[r] = a.starts[place0 + r < places ? place0 + r : places];
     for (int r = 0; r < a.rows; ++r) {
-        if (row0 + r >= a.V) return;
+        if (place0 + r >= places) return;
+        const int64_t row = a.dealt.row((uint32_t)(place0 + r));
         const uint32_t n = starts[r + 1] - starts[r];
-        if (n > a.part || (a.add && n == 0)) continue;
+        if (row >= a.V || n > a.part || (a.add && n == 0)) continue;
         Row<T, P> sum;
         sum.zero();
         sum.add(a, starts[r], starts[r + 1], c);
-        put_row<T, O, P>(a, row0 + r, c, sum);
+        put_row<T, O, P>(a, row, c, sum);
     }
 }
 
@@ -304,10 +333,10 @@ template <typename T, typename O, int P> __global__ __launch_bounds__(kThreads) 
     constexpr int kWaves = kThreads / 64;
     __shared__ float sums[kWaves - 1][P * U::kSize][64];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), lane = threadIdx.x & 63;
-    const uint32_t part = blockIdx.x / a.columns, begin = part * a.part, total = a.starts[a.V];
+    const uint32_t part = blockIdx.x / a.columns, begin = part * a.part, total = a.starts[a.dealt.places()];
     if (begin >= total) return;
     const int64_t row = a.ids[a.order[min(begin + a.part, total) - 1]];             // it goes on behind the part
-    const uint32_t from = a.starts[row], to = a.starts[row + 1];
+    const uint32_t place = a.dealt.place((uint32_t)row), from = a.starts[place], to = a.starts[place + 1];
     if (to - from <= a.part || from < begin) return;
     const int64_t c = ((int64_t)(blockIdx.x - part * a.columns) * 64 * P + lane) * U::kSize;
     Row<T, P> sum;
@@ -358,12 +387,15 @@ uint32_t part_of(int64_t T) {
     return n;
 }
 // the workspace: order, starts, parts
-struct Places { size_t order, starts, parts, bytes; };
+struct Places { size_t order, starts, parts, bytes; Dealt dealt; };
 Places places_of(int64_t T, int64_t V, int64_t D) {
     Places p;
+    p.dealt.bits = 0;                                       // 256 workgroups, one a CU, since each reads all ids; fewer for fewer rows, more where they would have more than kMostRows
+    while (((int64_t)1 << p.dealt.bits) < V && (p.dealt.bits < 8 || (V >> p.dealt.bits) >= kMostRows)) ++p.dealt.bits;
+    p.dealt.rows = (uint32_t)((V + p.dealt.workgroups() - 1) >> p.dealt.bits);
     p.order = 0;
     p.starts = (size_t)(T * 4 + 15) / 16 * 16;
-    p.parts = p.starts + (size_t)((V + 1) * 4 + 15) / 16 * 16;
+    p.parts = p.starts + ((size_t)p.dealt.places() * 4 + 4 + 15) / 16 * 16;
     p.bytes = p.parts + (T > part_of(T) ? (size_t)((T + part_of(T) - 1) / part_of(T)) * 2 * D * 4 : 0);
     return p;
 }
@@ -406,23 +438,20 @@ int division_embedding_backward(const division_embedding_back* back, void* hip_s
     if (b.workspace_bytes < at.bytes) return DIVISION_ESIZE;
     char* ws = static_cast<char*>(b.workspace);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    OrderArgs o{b.ids, reinterpret_cast<uint32_t*>(ws + at.order), reinterpret_cast<uint32_t*>(ws + at.starts), b.V, b.ignore_index, (uint32_t)b.T, 0, 0};
-    int64_t rows = (b.V + 255) / 256;                       // one workgroup a CU: each reads all ids
-    if (rows > kMostRows) rows = kMostRows;
-    o.rows = (int)rows;
-    while ((1 << o.bits) < rows) ++o.bits;
-    const int64_t workgroups = (b.V + rows - 1) / rows;
-    if (workgroups * kOrderThreads >= (int64_t(1) << 32)) return DIVISION_ERANGE;
+    const Dealt& dealt = at.dealt;
+    if ((int64_t)dealt.workgroups() * kOrderThreads >= (int64_t(1) << 32)) return DIVISION_ERANGE;
+    OrderArgs o{b.ids, reinterpret_cast<uint32_t*>(ws + at.order), reinterpret_cast<uint32_t*>(ws + at.starts), b.V, b.ignore_index, (uint32_t)b.T, 0, dealt};
+    while ((1u << o.bits) < dealt.rows) ++o.bits;
     const uint32_t part = part_of(b.T);
-    SumArgs s{b.grad, b.ids, o.order, o.starts, reinterpret_cast<float*>(ws + at.parts), b.grad_table, b.grad_stride, b.V, b.D, (uint32_t)b.T, part, b.scale, b.add, 0, 0, 0};
+    SumArgs s{b.grad, b.ids, o.order, o.starts, dealt, reinterpret_cast<float*>(ws + at.parts), b.grad_table, b.grad_stride, b.V, b.D, (uint32_t)b.T, part, b.scale, b.add, 0, 0, b.D % (16 / (int64_t)size_of(b.dt)) == 0, 0};
     const bool wide = b.D > 64 * (int64_t)(16 / size_of(b.dt));
     const int64_t each = 64 * (int64_t)(16 / size_of(b.dt)) * (wide ? 2 : 1), columns = (b.D + each - 1) / each;
     s.columns = (int)columns;
     s.count = b.T > part ? (b.T + part - 1) / part : 0;
     s.rows = b.V * columns < 8192 * kRows ? 1 : kRows;
-    const int64_t joins = s.count * columns, grid = ((s.count + (b.V + s.rows - 1) / s.rows) * columns + 3) / 4;
+    const int64_t joins = s.count * columns, grid = ((s.count + ((int64_t)dealt.places() + s.rows - 1) / s.rows) * columns + 3) / 4;
     if (grid >= kMostWorkgroups || joins >= kMostWorkgroups) return DIVISION_ERANGE;
-    hipLaunchKernelGGL(order_tokens, dim3((uint32_t)workgroups), dim3(kOrderThreads), (size_t)rows * kOrderWaves * 4, st, o);
+    hipLaunchKernelGGL(order_tokens, dim3(dealt.workgroups()), dim3(kOrderThreads), (size_t)dealt.rows * kOrderWaves * 4, st, o);
     CHECKED(launched());
     const bool half = b.dt == DIVISION_BF16;
     void (*sum)(SumArgs);

@@ -81,6 +81,19 @@ def test_gradient(T, V, D, power, dtype):
         assert torch.equal(got[row].cpu(), (s * torch.tensor(1.7)).to(dtype))
 
 
+@pytest.mark.parametrize("V", [2, 3, 127, 128, 255, 256, 257, 511, 1025, 65537, 131071, 131072, 131073, 300000])
+@pytest.mark.parametrize("T", [70, 16385, 50000])
+def test_tables_of_all_sizes(T, V):
+    """Every row once at least, where there are tokens enough, the last ones among them"""
+    gen = torch.Generator().manual_seed(T + V)
+    ids = torch.cat([torch.arange(V - 1, max(V - 1 - T // 2, -1), -1), torch.randint(0, V, (T,), generator=gen)])[:T]
+    ids = ids[torch.randperm(T, generator=gen)]
+    whole = torch.randint(-4, 5, (T, 8), generator=gen)
+    want = torch.zeros(V, 8, dtype=torch.float64).index_add_(0, ids, whole.double())
+    got = pkg.division_embedding_backward(whole.float().cuda(), ids.cuda(), V)
+    assert torch.equal(got.cpu().double(), want)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_adding_to_a_gradient_leaves_other_rows_alone(dtype):
     gen = torch.Generator().manual_seed(1)
