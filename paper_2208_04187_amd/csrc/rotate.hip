@@ -29,27 +29,38 @@ struct RotateArgs {
 template <typename T, int V, bool NEXT, bool PAST = false> struct Pairs {
     static __device__ __forceinline__ int second(const RotateArgs& a, int p) { return p < a.rotated ? a.rotated : a.pairs - a.rotated; }
     static __device__ __forceinline__ int first(const RotateArgs& a, int p) { return p < a.rotated ? p : a.rotated + p; }
-    static __device__ __forceinline__ void load(const T* row, const RotateArgs& a, int p, float* v) {
-        if constexpr (NEXT) {
-            if constexpr (V == 1) {
-                v[0] = Some1(row + 2 * p); v[1] = Some1(row + 2 * p + 1);
-            } else {
-                Some<T, V> q[2];
-                q[0].template load<PAST>(row + 2 * p); q[1].template load<PAST>(row + 2 * p + V);
+    // as they come from memory, and their values
+    struct Raw { Some<T, V == 1 ? 16 / (int)sizeof(T) : V> q[V == 1 ? 1 : 2]; };
+    static __device__ __forceinline__ Raw none() {
+        Raw r;
 #pragma unroll
-                for (int i = 0; i < V; ++i) { v[i] = q[2 * i / V][2 * i % V]; v[V + i] = q[(2 * i + 1) / V][(2 * i + 1) % V]; }
-            }
+        for (auto& q : r.q) q.zero();
+        return r;
+    }
+    static __device__ __forceinline__ void fetch(const T* row, const RotateArgs& a, int p, Raw& r) {
+        const T* at = NEXT ? row + 2 * p : row + first(a, p);
+        const int apart = NEXT ? V : second(a, p);
+        if constexpr (V == 1) {
+            r.q[0].w[0] = word(at); r.q[0].w[1] = word(at + apart);
         } else {
-            const T* at = row + first(a, p);
-            if constexpr (V == 1) {
-                v[0] = Some1(at); v[1] = Some1(at + second(a, p));
-            } else {
-                Some<T, V> q[2];
-                q[0].template load<PAST>(at); q[1].template load<PAST>(at + second(a, p));
+            r.q[0].template load<PAST>(at); r.q[1].template load<PAST>(at + apart);
+        }
+    }
+    static __device__ __forceinline__ void values(const Raw& r, float* v) {
+        if constexpr (V == 1) {
+            v[0] = __uint_as_float(r.q[0].w[0]); v[1] = __uint_as_float(r.q[0].w[1]);
+        } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) { v[i] = q[0][i]; v[V + i] = q[1][i]; }
+            for (int i = 0; i < V; ++i) {
+                if constexpr (NEXT) { v[i] = r.q[2 * i / V][2 * i % V]; v[V + i] = r.q[(2 * i + 1) / V][(2 * i + 1) % V]; }
+                else { v[i] = r.q[0][i]; v[V + i] = r.q[1][i]; }
             }
         }
+    }
+    static __device__ __forceinline__ void load(const T* row, const RotateArgs& a, int p, float* v) {
+        Raw r;
+        fetch(row, a, p, r);
+        values(r, v);
     }
     static __device__ __forceinline__ void store(T* row, const RotateArgs& a, int p, const float* v) {
         if constexpr (V == 1) {
@@ -65,9 +76,9 @@ template <typename T, int V, bool NEXT, bool PAST = false> struct Pairs {
             Some<T, V>::template store<PAST>(at, v); Some<T, V>::template store<PAST>(at + second(a, p), v + V);
         }
     }
-    static __device__ __forceinline__ float Some1(const T* p) {
-        if constexpr (sizeof(T) == 4) return *p;
-        else return bf16_value(*p);
+    static __device__ __forceinline__ uint32_t word(const T* p) {
+        if constexpr (sizeof(T) == 4) return __float_as_uint(*p);
+        else return (uint32_t)*p << 16;
     }
     static __device__ __forceinline__ void put1(T* p, float v) {
         if constexpr (sizeof(T) == 4) *p = v;
@@ -95,7 +106,7 @@ __device__ __forceinline__ void angles(const RotateArgs& a, int64_t t0, int n, f
 // LANES lanes have a head, U times V pairs each; a workgroup takes `block` tokens at a time, all heads of all of them one behind the other: the angles, whose sines in binary64 turns cost most of the
 // arithmetic, are taken once for a token's heads and wait in the local memory.  A lane has both elements of its pairs, so that the norm's sum is the only exchange.  Backward each workgroup keeps its
 // share of the weights' gradients in registers over all its tokens.
-// Bound by memory: 16384 tokens, 32 and 8 heads of 128 in bfloat16, 65 us = 5.2 TB/s; backward 102 us = 5.0 TB/s and 4.6 us for the shares.
+// Bound by memory: 16384 tokens, 32 and 8 heads of 128 in bfloat16, 61 us = 5.5 TB/s; backward 96 us = 5.3 TB/s and 4.6 us for the shares.
 template <typename T, int V, int U, int LANES, bool NEXT, bool BACK, bool PAST> __global__ __launch_bounds__(kThreads) void rotate(RotateArgs a) {
     typedef Pairs<T, V, NEXT, PAST> P;
     extern __shared__ __attribute__((aligned(16))) float2 turned[];
@@ -117,20 +128,21 @@ template <typename T, int V, int U, int LANES, bool NEXT, bool BACK, bool PAST> 
         const int n = (int)(a.T - t0 < block ? a.T - t0 : block), items = n * heads;
         // every lane goes round as often: the sums over lanes take all of them
         const int rounds = (items + kSlots - 1) / kSlots;
-        float x[U][2 * V], g[U][2 * V], rstd = 0.0f;
+        typename P::Raw next_x[U], next_g[U];
+        float next_rstd = 0.0f;
         const auto load = [&](int e) {
             const int t = e / heads, h = e - t * heads;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int p = (u * LANES + lane) * V;
-#pragma unroll
-                for (int i = 0; i < 2 * V; ++i) x[u][i] = g[u][i] = 0.0f;
+                next_x[u] = P::none();
+                if constexpr (BACK) next_g[u] = P::none();
                 if (e < items && p < a.pairs) {
-                    P::load(static_cast<const T*>(s.x) + (t0 + t) * s.token + (int64_t)h * s.head, a, p, x[u]);
-                    if constexpr (BACK) P::load(static_cast<const T*>(s.grad) + (t0 + t) * s.grad_token + (int64_t)h * s.grad_head, a, p, g[u]);
+                    P::fetch(static_cast<const T*>(s.x) + (t0 + t) * s.token + (int64_t)h * s.head, a, p, next_x[u]);
+                    if constexpr (BACK) P::fetch(static_cast<const T*>(s.grad) + (t0 + t) * s.grad_token + (int64_t)h * s.grad_head, a, p, next_g[u]);
                 }
             }
-            if constexpr (BACK) rstd = e < items ? s.rstd_in[t0 * heads + e] : 0.0f;
+            if constexpr (BACK) next_rstd = e < items ? s.rstd_in[t0 * heads + e] : 0.0f;
         };
         load(slot);                                         // on its way while the angles are taken
         __syncthreads();
@@ -138,7 +150,15 @@ template <typename T, int V, int U, int LANES, bool NEXT, bool BACK, bool PAST> 
         __syncthreads();
         for (int k = 0; k < rounds; ++k) {
             const int e = k * kSlots + slot, t = e / heads;
-            if (k) load(e);
+            if (BACK && k) load(e);
+            float x[U][2 * V], g[U][2 * V], rstd = next_rstd;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                P::values(next_x[u], x[u]);
+                if constexpr (BACK) P::values(next_g[u], g[u]);
+            }
+            // on its way while these are turned (66.3 us without, 61.9 so); backward the registers count for more (101.5 and 111)
+            if (!BACK && k + 1 < rounds) load(e + kSlots);
             float sum = 0.0f;
             float2 cs[U][V];
 #pragma unroll
