@@ -106,7 +106,7 @@ __device__ __forceinline__ void angles(const RotateArgs& a, int64_t t0, int n, f
 // LANES lanes have a head, U times V pairs each; a workgroup takes `block` tokens at a time, all heads of all of them one behind the other: the angles, whose sines in binary64 turns cost most of the
 // arithmetic, are taken once for a token's heads and wait in the local memory.  A lane has both elements of its pairs, so that the norm's sum is the only exchange.  Backward each workgroup keeps its
 // share of the weights' gradients in registers over all its tokens.
-// Bound by memory: 16384 tokens, 32 and 8 heads of 128 in bfloat16, 61 us = 5.5 TB/s; backward 96 us = 5.3 TB/s and 4.6 us for the shares.
+// Bound by memory: 16384 tokens, 32 and 8 heads of 128 in bfloat16, 60 us = 5.6 TB/s; backward 88 us = 5.7 TB/s and 4.6 us for the shares.
 template <typename T, int V, int U, int LANES, bool NEXT, bool BACK, bool PAST> __global__ __launch_bounds__(kThreads) void rotate(RotateArgs a) {
     typedef Pairs<T, V, NEXT, PAST> P;
     extern __shared__ __attribute__((aligned(16))) float2 turned[];
@@ -277,9 +277,10 @@ size_t size_of(division_dtype dt) { return dt == DIVISION_BF16 ? 2 : 4; }
 
 constexpr int kMostParts = 1024;                            // workgroups of a backward launch, which leave a share of a weight's gradient each: what the CUs hold at once
 
-// Tokens that a workgroup takes at a time: about four rounds of its lanes over their heads for each time the angles are taken, one where tokens are few.
-int block_of(int64_t T, int64_t heads, int slots) {
-    int block = (int)(4 * slots / heads);
+// Tokens that a workgroup takes at a time: two rounds of its lanes over their heads for each time the angles are taken, one backward (forward one, two, three, four and eight rounds 64, 60.5, 61.5, 61.8
+// and 66 us, backward 93, 98.5, 100, 101.5 and 107), one token where tokens are few.
+int block_of(int64_t T, int64_t heads, int slots, bool back) {
+    int block = (int)((back ? 1 : 2) * slots / heads);
     if (block > 16) block = 16;
     while (block > 1 && T < 1024 * (int64_t)block) block /= 2;
     return block < 1 ? 1 : block;
@@ -336,7 +337,7 @@ RotateArgs args_of(const division_rotate& a) {
 }
 
 template <typename T, int V, int U, int LANES, bool BACK> int launch(RotateArgs& a, bool next, hipStream_t st) {
-    for (int k = 0; k < 2; ++k) a.block[k] = a.heads[k] ? block_of(a.T, a.heads[k], kThreads / LANES) : 0;
+    for (int k = 0; k < 2; ++k) a.block[k] = a.heads[k] ? block_of(a.T, a.heads[k], kThreads / LANES, BACK) : 0;
     a.first = grid_of(a.T, a.heads[0], a.heads[0] + a.heads[1], a.block[0], BACK);
     const uint32_t grid = (uint32_t)(a.first + grid_of(a.T, a.heads[1], a.heads[0] + a.heads[1], a.block[1], BACK));
     const int block = a.block[0] > a.block[1] ? a.block[0] : a.block[1];
