@@ -28,9 +28,9 @@ struct LookupArgs {
 // start at any element).
 template <typename T, bool PAST> __global__ __launch_bounds__(kThreads) void lookup(LookupArgs a) {
     typedef Unit<T> U;
-    const int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x, t = e / a.each;
-    if (t >= a.T) return;
-    const int64_t c = (e - t * a.each) * U::kSize, id = a.ids[t];
+    const uint32_t e = blockIdx.x * kThreads + threadIdx.x, token = e / (uint32_t)a.each;       // below 2^32: a launch has no more threads
+    if (token >= a.T) return;
+    const int64_t t = token, c = (int64_t)(e - token * (uint32_t)a.each) * U::kSize, id = a.ids[t];
     float v[U::kSize];
     if (id >= 0 && id < a.V && id != a.ignore) {
         const U q = load_some<U>(static_cast<const T*>(a.table) + id * a.D, c, a.D);
