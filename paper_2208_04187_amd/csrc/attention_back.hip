@@ -352,21 +352,23 @@ template <typename T, bool QUERIES> __global__ __launch_bounds__(kThreads) void 
 size_t stats_bytes(const division_attention& a) { return ((size_t)(a.B * a.Sq * a.H) * 8 + 15) / 16 * 16; }
 
 // The workgroups' shapes.  fp32 products are slow enough for small ones to pay: 64 columns or keys, their tiles shared by two (four) sets.  (2 x 1531 tokens, 12 heads of 64, window 256: 228 us with
-// workgroups of 128, 191 so.)  FEW, in bfloat16: 64 too, and four sets, where blocks of 128 leave CUs without work (16 heads of 64, 1024 tokens: 52 us, 32 so; of 128, 81 and 47; but 2 x 12 heads of
+// workgroups of 128, 191 so; 4 x 1024 tokens, 8 heads of 128, causal, 405 and 301.)  FEW, in bfloat16: 64 too, and four sets, where blocks of 128 leave CUs without work (16 heads of 64, 1024 tokens: 52 us, 32 so; of 128, 81 and 47; but 2 x 12 heads of
 // 64, 1531 tokens, which make 288 blocks, 48 and 55).
 constexpr int kColumnTile = 32;
 template <typename T, int DP, bool FEW> struct Shape {
     static constexpr bool kHalf = sizeof(T) == 2, kSmall = !kHalf && DP <= 64;
     static constexpr int kKeyTile = kHalf && !FEW ? 64 : 32, kQueryWaves = kHalf && !FEW ? 4 : 2, kQuerySets = kHalf ? (FEW ? 4 : 1) : 2;
-    static constexpr int kKeyWaves = kSmall || FEW ? 2 : 4, kKeySets = kSmall || FEW ? 4 : kHalf ? 2 : 1;
+    static constexpr int kKeyWaves = !kHalf || FEW ? 2 : 4, kKeySets = kSmall || FEW ? 4 : 2;
     static constexpr bool kValues = kHalf && DP == 128;
 };
 // Parts of what a workgroup would have to look at, where there are few workgroups: as many as make two a CU, of so many tiles at least that they pay for adding them up.  (One sequence of 2048, 32 heads
 // on 4 of keys: 484 us with the columns of 128 keys in one part, 166 so.  Two heads of 4090 tokens, whose queries' keys are cut too: 163 us in one part, 90 so.  Parts of 8 tiles for four sets: 8 heads
 // of 64, 1024 tokens 47 us, 31 with 24.)
+// enough: workgroups that need no parts, one for every CU, two where a CU has room for one and the other half's end would be waited for (fp32 keys of more than 64 features: 8 heads of 128, 2048 tokens:
+// 490 us with 256, 386 so).
 constexpr int kMostSplits = 32;
-int parts_of(int64_t tasks, int64_t tiles, int64_t least) {
-    if (tasks == 0 || tasks >= 256) return 1;
+int parts_of(int64_t tasks, int64_t tiles, int64_t least, int64_t enough) {
+    if (tasks == 0 || tasks >= enough) return 1;
     int64_t n = (512 + tasks - 1) / tasks;
     if (n > tiles / least) n = tiles / least;
     return n < 1 ? 1 : n > kMostSplits ? kMostSplits : (int)n;
@@ -381,9 +383,9 @@ Splits splits_of(const division_attention& a) {
     s.few_keys = half && (a.Sk + 127) / 128 * groups < 256 && cols <= 4096;
     s.least_keys = s.few_queries ? 24 : half ? 4 : 2;
     s.least_columns = s.few_keys ? 24 : half ? 8 : 2;
-    const int64_t key_tile = half && !s.few_queries ? 64 : 32, of_queries = half && !s.few_queries ? 128 : 64, of_keys = s.few_keys || (!half && a.D <= 64) ? 64 : 128;
-    s.queries = parts_of((cols + of_queries - 1) / of_queries * groups, (a.Sk + key_tile - 1) / key_tile, s.least_keys);
-    s.keys = parts_of((a.Sk + of_keys - 1) / of_keys * groups, (cols + kColumnTile - 1) / kColumnTile, s.least_columns);
+    const int64_t key_tile = half && !s.few_queries ? 64 : 32, of_queries = half && !s.few_queries ? 128 : 64, of_keys = s.few_keys || !half ? 64 : 128;
+    s.queries = parts_of((cols + of_queries - 1) / of_queries * groups, (a.Sk + key_tile - 1) / key_tile, s.least_keys, 256);
+    s.keys = parts_of((a.Sk + of_keys - 1) / of_keys * groups, (cols + kColumnTile - 1) / kColumnTile, s.least_columns, half || a.D <= 64 ? 256 : 512);
     return s;
 }
 size_t key_bytes(const division_attention& a) { const int n = splits_of(a).keys; return n > 1 ? (size_t)n * a.B * a.G * a.Sk * 2 * a.D * 4 : 0; }
