@@ -24,7 +24,7 @@ struct LookupArgs {
     float scale;
     int each;                                               // pieces of a row
 };
-// A piece of sixteen bytes a lane; ids[t] behind the table is no token: its row is NaN.  Bound by memory and, in small calls, two trips to it: 2999 rows of 1155 in fp32 5.9 us = 4.7 TB/s (rows
+// A piece of sixteen bytes a lane; ids[t] behind the table is no token: its row is NaN.  Bound by memory and, in small calls, two trips to it: 2999 rows of 1155 in fp32 5.5 us = 5.0 TB/s (rows
 // start at any element).
 template <typename T, bool PAST> __global__ __launch_bounds__(kThreads) void lookup(LookupArgs a) {
     typedef Unit<T> U;

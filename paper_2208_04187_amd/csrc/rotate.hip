@@ -106,7 +106,7 @@ __device__ __forceinline__ void angles(const RotateArgs& a, int64_t t0, int n, f
 // LANES lanes have a head, U times V pairs each; a workgroup takes `block` tokens at a time, all heads of all of them one behind the other: the angles, whose sines in binary64 turns cost most of the
 // arithmetic, are taken once for a token's heads and wait in the local memory.  A lane has both elements of its pairs, so that the norm's sum is the only exchange.  Backward each workgroup keeps its
 // share of the weights' gradients in registers over all its tokens.
-// Bound by memory: 16384 tokens, 32 and 8 heads of 128 in bfloat16, 60 us = 5.6 TB/s; backward 88 us = 5.7 TB/s and 4.6 us for the shares.
+// Bound by memory: 16384 tokens, 32 and 8 heads of 128 in bfloat16, 59 us = 5.7 TB/s; backward 87 us = 5.8 TB/s and 4.5 us for the shares.
 template <typename T, int V, int U, int LANES, bool NEXT, bool BACK, bool PAST> __global__ __launch_bounds__(kThreads) void rotate(RotateArgs a) {
     typedef Pairs<T, V, NEXT, PAST> P;
     extern __shared__ __attribute__((aligned(16))) float2 turned[];
