@@ -23,9 +23,11 @@ from .token_modules import _beside_the_stream, _first_derivatives
 
 
 def _fits(t: torch.Tensor) -> bool:
-    """Whether attention takes the rows as they lie: on 16 bytes, features next to one another"""
-    per = 16 // t.element_size()
-    return t.data_ptr() % 16 == 0 and t.stride(3) == 1 and all(n == 1 or s % per == 0 for n, s in zip(t.shape[:3], t.stride()[:3]))
+    """Whether attention takes the rows as they lie: on 16 bytes, features next to one another, tokens at most 8 MB apart and heads all within 1 GB"""
+    size = t.element_size()
+    if t.data_ptr() % 16 or t.stride(3) != 1 or any(n > 1 and s * size % 16 for n, s in zip(t.shape[:3], t.stride()[:3])):
+        return False
+    return (t.shape[1] <= 1 or t.stride(1) * size <= 1 << 23) and (t.shape[2] <= 1 or t.stride(2) * size * t.shape[2] <= 1 << 30)
 
 
 def _matrix(t: torch.Tensor) -> torch.Tensor:

@@ -182,6 +182,19 @@ def test_rows_that_attention_does_not_take_as_they_lie_are_copied():
     assert torch.equal(got[..., 1:], torch.autograd.grad((out * out).sum(), y)[0]) and not got[..., 0].any()
 
 
+def test_rows_farther_apart_than_attention_takes_are_copied():
+    """Tokens 9 MB apart, as in a batch of thousands whose first dimension is the tokens; heads 300 MB apart"""
+    gen = torch.Generator().manual_seed(6)
+    x = torch.randn(2, 5, 4, 16, generator=gen).bfloat16().cuda()
+    dense = [x.clone().requires_grad_() for _ in range(2)]
+    want = torch.autograd.grad(pkg.division_token_attention(dense[0], dense[1], dense[1], causal=True).float().square().sum(), dense)
+    for tokens, heads in ((9 << 19, 16), (16, 150 << 20)):
+        far = [torch.empty(2 * 80 + 5 * tokens + 4 * heads, dtype=torch.bfloat16, device="cuda").as_strided(x.shape, (80, tokens, heads, 1)).copy_(x).requires_grad_() for _ in range(2)]
+        out = pkg.division_token_attention(far[0], far[1], far[1], causal=True)
+        assert all(torch.equal(g, w) for g, w in zip(torch.autograd.grad(out.float().square().sum(), far), want))
+        del far, out
+
+
 def test_second_derivatives_raise():
     x = torch.randn(1, 4, 2, 16, device="cuda", requires_grad=True)
     e = pkg.DivisionEmbedding(7, 4, device="cuda")
