@@ -45,6 +45,7 @@ template <typename T, bool PAST> __global__ __launch_bounds__(kThreads) void loo
 
 // ------------------------------------------------------------------ the tokens in the order of their ids
 
+struct AddU { static __device__ __forceinline__ uint32_t of(uint32_t a, uint32_t b) { return a + b; } };
 constexpr int kOrderThreads = 1024, kOrderWaves = kOrderThreads / 64, kMostRows = 512;       // rows of the table whose tokens a workgroup puts in order
 constexpr int kKept = 16;                                   // ids of a thread that come at once
 
@@ -69,43 +70,47 @@ struct OrderArgs {
 
 // One launch instead of the passes of a sort.  Every workgroup reads all ids and keeps those of its rows; how many lie before its rows tells it where its tokens begin, so that workgroups need not wait for one another.  Each wavefront
 // has an equal run of the tokens.  First they count: [row][wavefront].  The running sum over these numbers is where a wavefront's tokens of a row begin, and then each puts its own there,
-// in their order.  Bound by its chain: 16384 tokens of 32768 rows, 256 workgroups,
-// 12 to 14 us, of which the ids take 5.3 until they are there (one by one, 4 more), the running sum 1.3, putting tokens in their places 1.2 and more.
+// in their order.  Bound by its chain: 16384 tokens of 32768 rows, 256 workgroups, 10.5 us for even tokens, 13 for uneven ones: 2 until all workgroups have begun, 3 to 4 until all ids are sorted out
+// (loaded one by one, 4 more), 1.3 for the running sum, 1 and more for putting tokens in their places.
 __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     extern __shared__ uint32_t counts[];                    // [rows][kOrderWaves]
     __shared__ uint32_t sums[kOrderWaves], before;
     __shared__ uint16_t kept[kKept][kOrderThreads];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)a.dealt.rows * kOrderWaves;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = (int)a.dealt.rows * kOrderWaves;
     const uint32_t run = (((a.T + kOrderWaves - 1) / kOrderWaves) + 63) & ~63u, first = wave * run, end = min(first + run, a.T);
     for (int e = threadIdx.x; e < n; e += kOrderThreads) counts[e] = 0;
     if (threadIdx.x == 0) before = 0;
     __syncthreads();
-    // the row among the workgroup's; another before them: kBefore, none of them: kNone
-    constexpr uint32_t kNone = 0xffffu, kBefore = 0xfffeu;
-    // of kKept times 64 tokens, whose ids come at once: behind the last token its id again, which is none then
-    const auto rows_of = [&](uint32_t* to, uint32_t t) {
-        int64_t ids[kKept];
+    constexpr uint32_t kNone = 0xffffu;                     // not of the workgroup's rows
+    // of kKept times 64 tokens, whose ids come at once, behind the run's end zeros; `lower` counts those of workgroups before.  (By way of a bounded buffer and 32-bit comparisons: four wavefronts a SIMD do each of these instructions, and with
+    // 64-bit addresses and comparisons they took half as long again as the trip to memory.)
+    const uint32_t ignore = a.ignore >= 0 && a.ignore < a.V ? (uint32_t)a.ignore : 0xffffffffu;
+    const auto rows_of = [&](uint32_t* to, uint32_t t, uint32_t& lower) {
+        const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<int64_t*>(a.ids + t), 0, (int)((end - t < kKept * 64 ? end - t : kKept * 64) * 8), 0x00020000);
+        const uint32_t there = end - t > (uint32_t)lane ? (end - t - lane + 63) / 64 : 0;
+        u32x2 ids[kKept];
 #pragma unroll
-        for (int k = 0; k < kKept; ++k) ids[k] = a.ids[min(t + k * 64 + lane, end - 1)];
+        for (int k = 0; k < kKept; ++k) ids[k] = __builtin_amdgcn_raw_buffer_load_b64(from, (k * 64 + lane) * 8, 0, 0);
 #pragma unroll
         for (int k = 0; k < kKept; ++k) {
-            const bool none = t + k * 64 + lane >= end || ids[k] < 0 || ids[k] >= a.V || ids[k] == a.ignore;
-            const uint32_t w = (uint32_t)ids[k] & (a.dealt.workgroups() - 1);
-            to[k] = none || w > blockIdx.x ? kNone : w < blockIdx.x ? kBefore : (uint32_t)ids[k] >> a.dealt.bits;
+            const uint32_t id = ids[k].x;
+            const bool one = ((uint32_t)k < there) & (ids[k].y == 0) & (id < (uint32_t)a.V) & (id != ignore);
+            const uint32_t w = one ? id & (a.dealt.workgroups() - 1) : 0xffffffffu, row = id >> a.dealt.bits;
+            to[k] = w == blockIdx.x ? row : kNone;
+            lower += w < blockIdx.x ? 1u : 0u;
         }
     };
     uint32_t less = 0;
     for (uint32_t t = first; t < end; t += kKept * 64) {
         uint32_t rows[kKept];
-        rows_of(rows, t);
+        rows_of(rows, t, less);
 #pragma unroll
         for (int k = 0; k < kKept; ++k) {
-            if (rows[k] == kBefore) ++less;
-            else if (rows[k] != kNone) atomicAdd(&counts[rows[k] * kOrderWaves + wave], 1u);
+            if (rows[k] != kNone) atomicAdd(&counts[rows[k] * kOrderWaves + wave], 1u);
             if (t == first) kept[k][threadIdx.x] = (uint16_t)rows[k];
         }
     }
-    for (int o = 32; o; o >>= 1) less += (uint32_t)__shfl_xor((int)less, o, 64);
+    less = over_lanes<AddU, 64>(less);
     if (lane == 0) atomicAdd(&before, less);
     __syncthreads();
     // running sum over all numbers: a run of them a thread
@@ -120,8 +125,7 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     }
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
-    uint32_t at = before + upto - own;
-    for (int w = 0; w < wave; ++w) at += sums[w];
+    uint32_t at = before + upto - own + over_lanes<AddU, kOrderWaves>((lane & (kOrderWaves - 1)) < wave ? sums[lane & (kOrderWaves - 1)] : 0u);
     for (int e = from; e < to; ++e) {
         const uint32_t c = counts[e];
         counts[e] = at;
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     // that reads it is another's.
     const auto place = [&](uint32_t row, uint32_t t) {
         const uint64_t below = (1ull << lane) - 1;
-        uint64_t left = __ballot(row < kBefore);
+        uint64_t left = __ballot(row != kNone);
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             if (!left) return;
@@ -165,7 +169,7 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens(OrderArgs a) {
     for (uint32_t t = first; t < end; t += kKept * 64) {
         if (t != first) {
             uint32_t rows[kKept];
-            rows_of(rows, t);
+            rows_of(rows, t, less);
 #pragma unroll
             for (int k = 0; k < kKept; ++k) kept[k][threadIdx.x] = (uint16_t)rows[k];
         }
