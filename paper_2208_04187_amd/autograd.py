@@ -214,6 +214,20 @@ class DivisionMaxPool2d(torch.nn.Module):
         return _MaxPool2d.apply(x, self.k)
 
 
+def _call_seed(module) -> int:
+    """The seed of this call of a dropout module: seed + the call's number or, where seed is None, a draw from torch's generator of the host.
+
+    Activation checkpointing runs a forward again inside the backward pass.  It puts torch's generators back before, so that a draw is the same again; a
+    number would be the next one, and what is rebuilt not what made the loss."""
+    if module.seed is None:
+        return int(torch.randint(2 ** 63 - 1, (), dtype=torch.int64, device="cpu"))
+    if torch._C._current_graph_task_id() != -1:
+        raise RuntimeError(f"{type(module).__name__} is called inside a backward pass, as by activation checkpointing, where its next number would drop other elements than "
+                           "the forward pass did; with seed=None it draws from torch's generator, which checkpointing puts back")
+    module.calls += 1
+    return module.seed + module.calls
+
+
 class DivisionDropout(torch.nn.Module):
     """Keeps an element with probability 1 - p while training; the mask of call number n of this module
     comes from seed + n.  Identity in eval mode."""

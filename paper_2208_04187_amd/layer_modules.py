@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import torch
 
+from .autograd import _call_seed
 from .layer_operators import (_tokens_of_heads, division_attention, division_attention_backward, division_dropout_add, division_embedding, division_embedding_backward,
                               division_head_norm_rotate, division_head_norm_rotate_backward)
 from .token_modules import _beside_the_stream, _first_derivatives
@@ -169,18 +170,18 @@ class _ResidualDropout(torch.autograd.Function):
 
 class DivisionResidualDropout(torch.nn.Module):
     """forward(x, residual=None) -> residual + dropout(x), kept elements divided by 1 - p, without a stored mask.  Call number n of this module while training drops what seed + n says
-    (DivisionDropout's elements of the same call); in eval mode nothing is dropped.  A captured graph drops the captured call's elements whenever it is replayed: for others each time call
+    (DivisionDropout's elements of the same call); in eval mode nothing is dropped.  Under activation checkpointing seed is None: a call draws its own from torch's generator, which is put back before
+    the forward runs again; a numbered call inside a backward pass raises.  A captured graph drops the captured call's elements whenever it is replayed: for others each time call
     division_dropout_add with a seed on the device."""
 
-    def __init__(self, p: float = 0.5, seed: int = 0):
+    def __init__(self, p: float = 0.5, seed: int | None = 0):
         super().__init__()
         if not 0.0 <= p <= 1.0:
             raise ValueError("p is a probability")
-        self.p, self.seed, self.calls = float(p), int(seed), 0
+        self.p, self.seed, self.calls = float(p), None if seed is None else int(seed), 0
 
     def forward(self, x, residual=None):
         x, residual = _beside_the_stream(x, residual)
         if not self.training or self.p == 0.0:
             return x if residual is None else x + residual
-        self.calls += 1
-        return _ResidualDropout.apply(x, residual, self.p, self.seed + self.calls)
+        return _ResidualDropout.apply(x, residual, self.p, _call_seed(self))

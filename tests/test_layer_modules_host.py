@@ -1,0 +1,75 @@
+"""The layer operators' modules with stand-ins for the kernels: what they do around them (no GPU needed)."""
+import pytest
+import torch
+from torch.utils.checkpoint import checkpoint
+
+import paper_2208_04187_amd as pkg
+from paper_2208_04187_amd import layer_modules
+
+
+def _drop(x, p, seed, residual=None):
+    kept = torch.rand(x.shape, generator=torch.Generator().manual_seed(seed % 2 ** 63)) >= p
+    y = torch.where(kept, x / (1 - p), 0.0)
+    return y if residual is None else y + residual
+
+
+@pytest.fixture
+def stand_in(monkeypatch):
+    monkeypatch.setattr(layer_modules, "division_dropout_add", _drop)
+
+
+def _model(seed):
+    torch.manual_seed(1)
+    return torch.nn.Linear(16, 16), pkg.DivisionResidualDropout(0.5, seed=seed), torch.nn.Linear(16, 16)
+
+
+def _step(parts, x, wrap):
+    """One step behind one seed of torch's: the loss, and all gradients"""
+    first, drop, last = parts
+    x = x.clone().requires_grad_()
+    torch.manual_seed(2)
+    y = wrap(lambda t: last(drop(first(t), t)).tanh(), x)
+    loss = (y * y).sum()
+    return loss, torch.autograd.grad(loss, [x, *first.parameters(), *last.parameters()])
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_a_checkpointed_forward_drops_the_same_again(stand_in, reentrant):
+    x = torch.randn(8, 16, generator=torch.Generator().manual_seed(3))
+    want = _step(_model(None), x, lambda f, t: f(t))
+
+    def step():
+        parts = _model(None)
+        leaf = x.clone().requires_grad_()
+        torch.manual_seed(2)
+        y = checkpoint(lambda t: parts[2](parts[1](parts[0](t), t)).tanh(), leaf, use_reentrant=reentrant)
+        loss = (y * y).sum()
+        loss.backward()
+        return loss, (leaf.grad, *(p.grad for m in (parts[0], parts[2]) for p in m.parameters()))
+    got = step()
+    assert torch.equal(got[0], want[0]) and all(torch.equal(a, b) for a, b in zip(got[1], want[1]))
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_a_numbered_call_is_not_made_again_in_the_backward_pass(stand_in, reentrant):
+    """Its number would be another, and its mask not the one that made the loss"""
+    first, drop, last = _model(5)
+    x = torch.randn(8, 16, generator=torch.Generator().manual_seed(3)).requires_grad_()
+    y = checkpoint(lambda t: last(drop(first(t), t)).tanh(), x, use_reentrant=reentrant)
+    with pytest.raises(RuntimeError, match="seed=None"):
+        y.sum().backward()
+    assert drop.calls == 1
+
+
+def test_calls_have_their_numbers_and_drawn_seeds_are_torchs(stand_in):
+    x, r = torch.ones(64), torch.zeros(64)
+    drop = pkg.DivisionResidualDropout(0.5, seed=7)
+    assert torch.equal(drop(x, r), _drop(x, 0.5, 8, r)) and torch.equal(drop(x), _drop(x, 0.5, 9)) and drop.calls == 2
+    drop = pkg.DivisionResidualDropout(0.5, seed=None)
+    torch.manual_seed(4)
+    a, b = drop(x), drop(x)
+    torch.manual_seed(4)
+    assert torch.equal(drop(x), a) and torch.equal(drop(x), b) and not torch.equal(a, b)
+    state = torch.get_rng_state()
+    drop.eval()
+    assert drop(x) is x and torch.equal(torch.get_rng_state(), state)
