@@ -230,14 +230,14 @@ def _call_seed(module) -> int:
 
 class DivisionDropout(torch.nn.Module):
     """Keeps an element with probability 1 - p while training; the mask of call number n of this module
-    comes from seed + n.  Identity in eval mode."""
+    comes from seed + n, with seed=None (as activation checkpointing needs it) from torch's generator.
+    Identity in eval mode."""
 
-    def __init__(self, p: float = 0.5, seed: int = 0):
+    def __init__(self, p: float = 0.5, seed: int | None = 0):
         super().__init__()
-        self.p, self.seed, self.calls = float(p), int(seed), 0
+        self.p, self.seed, self.calls = float(p), None if seed is None else int(seed), 0
 
     def forward(self, x):
         if not self.training or self.p == 0.0:
             return x
-        self.calls += 1
-        return _Dropout.apply(x, self.p, self.seed + self.calls)
+        return _Dropout.apply(x, self.p, _call_seed(self))

@@ -4,7 +4,7 @@ import torch
 from torch.utils.checkpoint import checkpoint
 
 import paper_2208_04187_amd as pkg
-from paper_2208_04187_amd import layer_modules
+from paper_2208_04187_amd import autograd, layer_modules
 
 
 def _drop(x, p, seed, residual=None):
@@ -73,3 +73,32 @@ def test_calls_have_their_numbers_and_drawn_seeds_are_torchs(stand_in):
     state = torch.get_rng_state()
     drop.eval()
     assert drop(x) is x and torch.equal(torch.get_rng_state(), state)
+
+
+@pytest.fixture
+def mask_stand_in(monkeypatch):
+    monkeypatch.setattr(autograd, "division_dropout_forward", lambda x, p, seed: (_drop(x, p, seed) * (1 - p), _drop(torch.ones_like(x), p, seed) != 0))
+    monkeypatch.setattr(autograd, "division_mask_backward", lambda mask, grad: torch.where(mask, grad, 0.0))
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_dropout_with_a_stored_mask_under_checkpointing(mask_stand_in, reentrant):
+    x = torch.randn(8, 16, generator=torch.Generator().manual_seed(3))
+    grads = []
+    for run in (lambda f, t: f(t), lambda f, t: checkpoint(f, t, use_reentrant=reentrant)):
+        torch.manual_seed(1)
+        net = torch.nn.Sequential(torch.nn.Linear(16, 16), pkg.DivisionDropout(0.5, seed=None), torch.nn.Linear(16, 16), torch.nn.Tanh())
+        leaf = x.clone().requires_grad_()
+        torch.manual_seed(2)
+        (run(net, leaf) ** 2).sum().backward()
+        grads.append([leaf.grad, *(p.grad for p in net.parameters())])
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
+    drop = pkg.DivisionDropout(0.5, seed=5)
+    leaf = x.clone().requires_grad_()
+    y = checkpoint(lambda t: drop(t.sin()).exp(), leaf, use_reentrant=reentrant)
+    with pytest.raises(RuntimeError, match="seed=None"):
+        y.sum().backward()
+    assert drop.calls == 1
+    drop = pkg.DivisionDropout(0.5, seed=5)
+    for n in (6, 7):
+        assert torch.equal(drop(x), autograd.division_dropout_forward(x, 0.5, n)[0])
