@@ -503,7 +503,8 @@ int division_clip_grads(int64_t count, const division_gradient *grads, float lim
 /*
  * Attention.  Query head h of H reads key head h / (H / G) of G.  q is [B][Sq][H][D], k and v are [B][Sk][G][D]: D elements next to one another, the three other
  * strides (batch, token, head; in elements) any from 0 up that keep every row on 16 bytes, at most 8 MB a token and 1 GB for the heads that share a key head (DIVISION_ERANGE).  D is a multiple of 8 up to 128;
- * Sq and Sk up to 2^29, Sq * H / G up to 2^30, H up to 4096, B up to 2^24, and B * G times the blocks of 64 that Sq * H / G queries or Sk keys make below 2^23 (DIVISION_ERANGE).
+ * Sq and Sk up to 2^29, Sq * H / G up to 2^30, H up to 4096, B up to 2^24, B * G below 2^24, and B * G times the blocks of 64 that Sq * H / G queries or Sk keys make below 2^23
+ * (DIVISION_ERANGE).
  *
  * Sequence b has min(Sk, max(0, lengths[b])) keys (all Sk where lengths is null); what lies behind them is not looked at and may hold anything.  Its query i stands at position
  * starts[b] + i among the keys (Sk - Sq + i where starts is null).  It sees key j of them unless causal is 1 and j lies behind its position, or window > 0 and the two are window or

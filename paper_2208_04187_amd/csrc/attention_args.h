@@ -37,7 +37,7 @@ int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION
 #define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
 
 // A tensor of rows: nothing behind what 31 bits say of a tile's rows, which are up to 129 tokens' of the `share` heads that have one key head; every row on 16 bytes
-constexpr int64_t kMostStride = 1 << 23, kMostHeads = 1 << 30, kMostTokens = 1 << 29;
+constexpr int64_t kMostStride = 1 << 23, kMostHeads = 1 << 30, kMostTokens = 1 << 29, kMostGroups = 1 << 24;
 int check_heads(const void* p, const int64_t* strides, int64_t B, int64_t share, int64_t es) {
     const int64_t per = 16 / es;
     if (strides[0] < 0 || strides[1] < 0 || strides[2] < 0) return DIVISION_EINVAL;
@@ -53,6 +53,8 @@ int check_attention(const division_attention& a) {
     if (a.B == 0) return DIVISION_OK;
     const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4, R = a.H / a.G;
     if (a.B > (1 << 24) || a.H > 4096 || a.Sq > kMostTokens || a.Sk > kMostTokens || a.Sq * R > (int64_t(1) << 30)) return DIVISION_ERANGE;
+    // more than any launch has room for, before it is narrowed
+    if ((a.Sq > 0 || a.Sk > 0) && a.B * a.G >= kMostGroups) return DIVISION_ERANGE;
     if (a.Sq > 0) CHECKED(check_heads(a.q, a.q_strides, a.B, R, es));
     if (a.Sk > 0) {
         CHECKED(check_heads(a.k, a.k_strides, a.B, 1, es));
