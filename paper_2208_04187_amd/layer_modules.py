@@ -123,7 +123,8 @@ class DivisionHeadNormRotation(torch.nn.Module):
     def frequencies(self, device):
         # no buffer: a module's .to(dtype) would round it
         if self._frequencies is None or self._frequencies.device != device:
-            self._frequencies = torch.tensor([self.base ** (-p / self.rotated) for p in range(0, self.rotated, 2)], dtype=torch.float64).to(device)
+            with torch.inference_mode(False):               # kept for later calls, whose backward pass cannot take what was made in inference mode
+                self._frequencies = torch.tensor([self.base ** (-p / self.rotated) for p in range(0, self.rotated, 2)], dtype=torch.float64).to(device)
         return self._frequencies
 
     def forward(self, q, k, positions):

@@ -102,3 +102,26 @@ def test_dropout_with_a_stored_mask_under_checkpointing(mask_stand_in, reentrant
     drop = pkg.DivisionDropout(0.5, seed=5)
     for n in (6, 7):
         assert torch.equal(drop(x), autograd.division_dropout_forward(x, 0.5, n)[0])
+
+
+class _Save(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, f):
+        ctx.save_for_backward(f)
+        return x * 1.0
+
+    @staticmethod
+    def backward(ctx, g):
+        return g * ctx.saved_tensors[0].sum(), None
+
+
+def test_a_rotation_that_began_in_inference_mode_trains():
+    m = pkg.DivisionHeadNormRotation(16, rotated=8)
+    cpu = torch.device("cpu")
+    with torch.inference_mode():
+        first = m.frequencies(cpu)
+    assert not first.is_inference() and m.frequencies(cpu) is first
+    assert torch.equal(first, torch.tensor([10000.0 ** (-p / 8) for p in (0, 2, 4, 6)], dtype=torch.float64))
+    x = torch.ones(3, dtype=torch.float64, requires_grad=True)
+    _Save.apply(x, first).sum().backward()
+    assert torch.equal(x.grad, first.sum().expand(3))
