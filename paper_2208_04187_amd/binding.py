@@ -170,6 +170,26 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+class _Memory:
+    """What a call on a stream of its own makes: memory of that stream, so that the call waits for whatever used it before.  (A block that the current stream has given back may still be in
+    use by what is queued there, behind which another stream does not wait.)  What is returned goes back to that stream when the current one, which the caller reads it on, has passed its last use."""
+
+    def __init__(self, stream, device):
+        self.side = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+        self.current = torch.cuda.current_stream(device)
+
+    def __call__(self, make, *args, **kw):
+        with torch.cuda.stream(self.side):
+            t = make(*args, **kw)
+        t.record_stream(self.current)
+        return t
+
+
+def _memory(stream, device):
+    """make(torch.empty, ...) for the outputs and workspaces of a call: on the given stream, or on the current one"""
+    return (lambda make, *args, **kw: make(*args, **kw)) if stream is None else _Memory(stream, device)
+
+
 # Size of a packed buffer: a function of whole numbers alone, asked for on every call of a training step with the same
 # few shapes (1.3 us through the C entry, 0.15 us from the table).
 @functools.lru_cache(maxsize=4096)

@@ -11,7 +11,7 @@ from typing import NamedTuple
 
 import torch
 
-from .binding import LAYER_DESCS, LAYER_ENTRIES, _dt, _result, _stream, lib
+from .binding import LAYER_DESCS, LAYER_ENTRIES, _dt, _memory, _result, _stream, lib
 from .operators import _at, _beside, _checked, _dense, _fast, _rows, _written
 
 _vp, _i64, _ci, _sz, _f, _u64 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, ctypes.c_float, ctypes.c_uint64
@@ -64,17 +64,14 @@ LAYER_DESCS += [_AttentionDesc, _AttentionBackDesc, _RotateDesc, _RotateBackDesc
 
 
 class _Call:
-    """One call: its outputs and workspace on the device of its tensors, and the launch there, whatever the current device.  On a stream given by the caller the memory of what it
-    made is not handed out again before that stream has passed the call."""
+    """One call: its outputs and workspace on the device of its tensors, in the memory of its stream, and the launch there, whatever the current device."""
 
     def __init__(self, device, stream, what):
         self.device, self.stream, self.what = device, stream, what
+        self.make = _memory(stream, device)
 
     def new(self, shape, dtype):
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if self.stream is not None:
-            t.record_stream(self.stream if hasattr(self.stream, "cuda_stream") else torch.cuda.ExternalStream(int(self.stream), device=self.device))
-        return t
+        return self.make(torch.empty, shape, dtype=dtype, device=self.device)
 
     def workspace(self, nbytes: int):
         return self.new((max(int(nbytes), 1),), torch.uint8)

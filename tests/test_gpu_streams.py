@@ -1,0 +1,74 @@
+"""Calls on a stream of their own: what they write is memory of that stream, not what the current stream has given back and may still be using.
+
+Shown by the addresses alone, between waits for the device: a block that the current stream has just given back, of the very size that the call asks for, is what the allocator would hand
+out to the current stream."""
+import pytest
+import torch
+
+import paper_2208_04187_amd as pkg
+
+pytestmark = pytest.mark.gpu
+
+
+def _tensors(got):
+    return [t for t in (got if isinstance(got, (list, tuple)) else [got]) if t is not None]
+
+
+def _place(t):
+    s = t.untyped_storage()
+    return s.data_ptr(), s.data_ptr() + max(s.nbytes(), 1)
+
+
+def _apart(call, inputs=()):
+    """call(stream): the same results on a stream of its own and on the current one, in memory that the current stream has not had"""
+    want = [t.clone() for t in _tensors(call(None))]
+    spare = _tensors(call(None))
+    torch.cuda.synchronize()
+    own = [_place(t) for t in spare if not any(t is i for i in inputs)]
+    del spare
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        got = _tensors(call(stream))
+        torch.cuda.synchronize()
+        for t in got:
+            a, b = _place(t)
+            assert any(t is i for i in inputs) or all(b <= p or q <= a for p, q in own)
+        assert len(got) == len(want) and all(torch.equal(a.reshape(-1).view(torch.uint8), b.reshape(-1).view(torch.uint8)) for a, b in zip(got, want))
+        # given back while the current stream has them in use: not the side stream's next memory
+        made = [t for t in got if not any(t is i for i in inputs) and t.numel()]
+        places = [_place(t) for t in made]
+        torch.cuda._sleep(2 ** 26)
+        kept = [t.clone() for t in made]
+        sizes = [t.untyped_storage().nbytes() for t in made]
+        del got, made, t
+        with torch.cuda.stream(side):
+            again = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+        assert not set(_place(t)[0] for t in again) & set(p for p, _ in places)
+        torch.cuda.synchronize()
+        del again, kept
+
+
+def _layer_calls():
+    gen = torch.Generator().manual_seed(1)
+    q, k = torch.randn(2, 300, 8, 64, generator=gen).cuda(), torch.randn(2, 300, 2, 64, generator=gen).cuda()
+    a = pkg.division_attention(q, k, k, causal=True)
+    w, f, at = torch.rand(64, generator=gen).cuda(), torch.rand(32, generator=gen).double().cuda(), torch.arange(600, device="cuda").view(2, 300)
+    r = pkg.division_head_norm_rotate(q, k, w, w, f, at)
+    ids, table = torch.randint(0, 500, (600,), generator=gen).cuda(), torch.randn(500, 1000, generator=gen).cuda()
+    rows = torch.randn(600, 1000, generator=gen).cuda()
+    held, summed = torch.empty_like(rows), torch.zeros(500, 1000, device="cuda")
+    return {"attention": lambda s: pkg.division_attention(q, k, k, causal=True, stream=s), "attention_token": lambda s: pkg.division_attention(q[:, :1], k, k, stream=s),
+            "attention_backward": lambda s: pkg.division_attention_backward(q, q, k, k, a.out, a.lse, causal=True, stream=s),
+            "rotate": lambda s: pkg.division_head_norm_rotate(q, k, w, w, f, at, stream=s),
+            "rotate_backward": lambda s: pkg.division_head_norm_rotate_backward(q, k, q, k, w, w, f, at, r.q_rstd, r.k_rstd, stream=s),
+            "embedding": lambda s: pkg.division_embedding(ids, table, stream=s), "embedding_backward": lambda s: pkg.division_embedding_backward(rows, ids, 500, stream=s),
+            "embedding_backward_out": lambda s: pkg.division_embedding_backward(rows, ids, 500, out=summed, stream=s), "dropout_add": lambda s: pkg.division_dropout_add(rows, 0.5, 3, stream=s),
+            "dropout_add_out": lambda s: pkg.division_dropout_add(rows, 0.5, 3, out=held, stream=s)}, (held, summed)
+
+
+@pytest.mark.parametrize("name", ["attention", "attention_token", "attention_backward", "rotate", "rotate_backward", "embedding", "embedding_backward", "embedding_backward_out", "dropout_add",
+                                  "dropout_add_out"])
+def test_layer_operators(name):
+    calls, inputs = _layer_calls()
+    torch.cuda.synchronize()
+    _apart(calls[name], inputs)
