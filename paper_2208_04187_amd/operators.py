@@ -13,7 +13,7 @@ from typing import NamedTuple
 import torch
 
 from . import binding
-from .binding import OPERATOR_DESCS, OPERATOR_ENTRIES, OPERATOR_OTHERS, DivisionError, _dt, _result, _stream, lib
+from .binding import OPERATOR_DESCS, OPERATOR_ENTRIES, OPERATOR_OTHERS, DivisionError, _dt, _memory, _result, _stream, lib
 
 _vp, _i64, _ci, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
 _CODES = {None: 0, "int8": 1, "e4m3": 2}
@@ -122,13 +122,9 @@ def _written(*tensors):
     torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
 
 
-def _workspace(nbytes: int, device, stream):
-    """Memory for one call.  torch hands it out again when the call's tensors are gone: to the current stream's next call, behind this
-    one, or, where the call runs on another stream, not before that stream has passed it."""
-    ws = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
-    if stream is not None:
-        ws.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device))
-    return ws
+def _workspace(nbytes: int, device, make):
+    """Memory for one call, of the stream that it runs on: torch hands it out again, behind this call, when the call's tensors are gone."""
+    return make(torch.empty, max(int(nbytes), 1), dtype=torch.uint8, device=device)
 
 
 def _group_count(D: int, group: int) -> int:
@@ -173,14 +169,14 @@ def division_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, 
         _, rs, _ = _rows(residual, "residual")
     if not want_y and code is None:
         raise ValueError("want_y=False leaves nothing to compute without a code")
-    lead = x.shape[:-1]
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_y else None
-    total = torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual is not None else x
-    rstd = torch.empty(lead, dtype=torch.float32, device=x.device)
+    lead, make = x.shape[:-1], _memory(stream, x.device)
+    y = make(torch.empty, x.shape, dtype=x.dtype, device=x.device) if want_y else None
+    total = make(torch.empty, x.shape, dtype=x.dtype, device=x.device) if residual is not None else x
+    rstd = make(torch.empty, lead, dtype=torch.float32, device=x.device)
     codes = scales = None
     if code is not None:
-        codes = torch.empty(x.shape, dtype=_CODE_TYPES[code], device=x.device)
-        scales = torch.empty((*lead, _group_count(D, group)), dtype=torch.float32, device=x.device)
+        codes = make(torch.empty, x.shape, dtype=_CODE_TYPES[code], device=x.device)
+        scales = make(torch.empty, (*lead, _group_count(D, group)), dtype=torch.float32, device=x.device)
     d = _NormDesc(x.data_ptr(), _at(residual), weight.data_ptr(), xs, rs, T, D, dt, wdt, eps, total.data_ptr() if residual is not None else None,
                   _at(y), rstd.data_ptr(), _CODES[code], group, _at(codes), _at(scales))
     _checked(lib().division_rms_norm(ctypes.byref(d), _stream(stream)), "division_rms_norm")
@@ -205,7 +201,7 @@ def division_read_codes(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.
         raise ValueError("scales do not fit the codes")
     group = fits[0]                     # more than one scale a row: of one group size alone
     if out is None:
-        out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+        out = _memory(stream, codes.device)(torch.empty, codes.shape, dtype=dtype, device=codes.device)
     else:
         _dense(out, "out", shape=codes.shape, device=codes.device)
         _written(out)
@@ -237,14 +233,15 @@ def division_rms_norm_backward(grad_y: torch.Tensor, sum: torch.Tensor, weight: 
         if g is not None:
             _beside(g, sum.device, name)
         strides.append(_rows(g, name)[1] if g is not None else 0)
+    make = _memory(stream, sum.device)
     if out is None:
-        out = torch.empty(sum.shape, dtype=sum.dtype, device=sum.device)
+        out = make(torch.empty, sum.shape, dtype=sum.dtype, device=sum.device)
     else:
         _dense(out, "out", dtype=sum.dtype, shape=sum.shape, device=sum.device)
         _written(out)
-    grad_weight = torch.empty_like(weight)
+    grad_weight = make(torch.empty_like, weight)
     nbytes = int(lib().division_rms_norm_backward_workspace(T, D))
-    ws = _workspace(nbytes, sum.device, stream)
+    ws = _workspace(nbytes, sum.device, make)
     d = _NormBackDesc(grad_y.data_ptr(), sum.data_ptr(), _at(grad_sum), weight.data_ptr(), rstd.data_ptr(), strides[0], ss, strides[1], T, D, dt, wdt,
                       out.data_ptr(), grad_weight.data_ptr(), ws.data_ptr(), nbytes)
     _checked(lib().division_rms_norm_backward(ctypes.byref(d), _stream(stream)), "division_rms_norm_backward")
@@ -281,13 +278,13 @@ def division_log_probs(logits: torch.Tensor, ids: torch.Tensor, top: int = 0, wa
         _dense(lse_low, "lse_low", dtype=torch.float32, shape=lead, device=logits.device)
     if not 0 <= top <= min(64, V):
         raise ValueError("top is 0 to 64, and at most the vocabulary")
-    f32 = dict(dtype=torch.float32, device=logits.device)
-    logp, lse = torch.empty(lead, **f32), torch.empty(lead, **f32)
-    entropy = torch.empty(lead, **f32) if want_entropy else None
-    top_logp = torch.empty((*lead, top), **f32) if top else None
-    top_ids = torch.empty((*lead, top), dtype=torch.int64, device=logits.device) if top else None
+    f32, make = dict(dtype=torch.float32, device=logits.device), _memory(stream, logits.device)
+    logp, lse = make(torch.empty, lead, **f32), make(torch.empty, lead, **f32)
+    entropy = make(torch.empty, lead, **f32) if want_entropy else None
+    top_logp = make(torch.empty, (*lead, top), **f32) if top else None
+    top_ids = make(torch.empty, (*lead, top), dtype=torch.int64, device=logits.device) if top else None
     nbytes = int(lib().division_log_probs_workspace(T, V, top))
-    ws = _workspace(nbytes, logits.device, stream) if nbytes else None
+    ws = _workspace(nbytes, logits.device, make) if nbytes else None
     d = _LogitsDesc(logits.data_ptr(), ids.data_ptr(), stride, T, V, ignore_index, dt, top, logp.data_ptr(), _at(entropy), lse.data_ptr(), _at(top_logp),
                     _at(top_ids), _at(ws), nbytes)
     _checked(lib().division_log_probs_low(ctypes.byref(d), _at(lse_low), _stream(stream)), "division_log_probs")
@@ -316,7 +313,7 @@ def division_log_probs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: to
         if t is not None:
             _dense(t, name, dtype=torch.float32, shape=lead, device=logits.device)
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        out = _memory(stream, logits.device)(torch.empty, logits.shape, dtype=logits.dtype, device=logits.device)
     elif out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must have the logits' shape and type")
     else:
@@ -365,9 +362,10 @@ def _grads(grads, out, limit, stream, what):
             _beside(o, device, "an output")
         n = g.numel()
         descs[i] = _GradientDesc(g.data_ptr() if n else None, o.data_ptr() if n else None, n, _dt(g.dtype), _dt(o.dtype))
-    norm = torch.empty((), dtype=torch.float32, device=device)
+    make = _memory(stream, device)
+    norm = make(torch.empty, (), dtype=torch.float32, device=device)
     nbytes = int(lib().division_grad_norm_workspace(len(grads), descs))
-    ws = _workspace(nbytes, device, stream)
+    ws = _workspace(nbytes, device, make)
     _checked(lib().division_clip_grads(len(grads), descs, limit if limit is not None else 0.0, limit is not None, norm.data_ptr(), ws.data_ptr(), nbytes,
                                        _stream(stream)), what)
     if limit is not None:

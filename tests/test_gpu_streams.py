@@ -72,3 +72,24 @@ def test_layer_operators(name):
     calls, inputs = _layer_calls()
     torch.cuda.synchronize()
     _apart(calls[name], inputs)
+
+
+def _step_calls():
+    gen = torch.Generator().manual_seed(2)
+    x, r, w = torch.randn(700, 500, generator=gen).cuda(), torch.randn(700, 500, generator=gen).cuda(), torch.rand(500, generator=gen).cuda()
+    n = pkg.division_rms_norm(x, w, residual=r, code="int8")
+    logits, ids = torch.randn(64, 20000, generator=gen).cuda(), torch.randint(0, 20000, (64,), generator=gen).cuda()
+    f = pkg.division_log_probs(logits, ids)
+    grads = [torch.randn(1000, 300, generator=gen).cuda(), torch.randn(77, generator=gen).cuda()]
+    held = torch.empty_like(x)
+    return {"rms_norm": lambda s: pkg.division_rms_norm(x, w, residual=r, code="e4m3", group=128, stream=s)[:4], "read_codes": lambda s: pkg.division_read_codes(n.codes, n.scales, torch.float32, stream=s),
+            "rms_norm_backward": lambda s: pkg.division_rms_norm_backward(r, x, w, n.rstd, stream=s), "rms_norm_backward_out": lambda s: pkg.division_rms_norm_backward(r, x, w, n.rstd, out=held, stream=s),
+            "log_probs": lambda s: pkg.division_log_probs(logits, ids, top=5, stream=s), "log_probs_backward": lambda s: pkg.division_log_probs_backward(logits, ids, f.lse, f.lse, stream=s),
+            "grad_norm": lambda s: pkg.division_grad_norm(grads, stream=s)}, (held,)
+
+
+@pytest.mark.parametrize("name", ["rms_norm", "read_codes", "rms_norm_backward", "rms_norm_backward_out", "log_probs", "log_probs_backward", "grad_norm"])
+def test_step_operators(name):
+    calls, inputs = _step_calls()
+    torch.cuda.synchronize()
+    _apart(calls[name], inputs)
