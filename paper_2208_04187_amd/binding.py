@@ -231,7 +231,7 @@ def division_compress(x: torch.Tensor, B: int, b: int, seed: int, packed: torch.
     if need == 0:
         raise DivisionError(1, "division_packed_bytes")
     if packed is None:
-        packed = torch.empty(need, dtype=torch.uint8, device=x.device)
+        packed = _memory(stream, x.device)(torch.empty, need, dtype=torch.uint8, device=x.device)
     rc = lib().division_compress(x.data_ptr(), N, C, H, W, _dt(x.dtype, c16), B, b, seed & (2 ** 64 - 1),
                                  packed.data_ptr(), packed.numel() * packed.element_size(), _stream(stream))
     if rc:
@@ -247,7 +247,7 @@ def division_decompress(packed: torch.Tensor, shape, B: int, b: int, dtype=torch
             return _result(got, "division_decompress")
     N, C, H, W = shape
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=packed.device)
+        out = _memory(stream, packed.device)(torch.empty, shape, dtype=dtype, device=packed.device)
     rc = lib().division_decompress(packed.data_ptr(), packed.numel() * packed.element_size(),
                                    N, C, H, W, _dt(dtype, c16), B, b, out.data_ptr(), _stream(stream))
     if rc:
@@ -284,7 +284,7 @@ def division_compress_3d(x: torch.Tensor, B: int, b: int, seed: int, packed: tor
     if need == 0:
         raise DivisionError(1, "division_packed_bytes_3d")
     if packed is None:
-        packed = torch.empty(need, dtype=torch.uint8, device=x.device)
+        packed = _memory(stream, x.device)(torch.empty, need, dtype=torch.uint8, device=x.device)
     rc = lib().division_compress_3d(x.data_ptr(), N, C, D, H, W, _dt(x.dtype, c16), B, b, seed & (2 ** 64 - 1),
                                     packed.data_ptr(), packed.numel() * packed.element_size(), _stream(stream))
     if rc:
@@ -300,7 +300,7 @@ def division_decompress_3d(packed: torch.Tensor, shape, B: int, b: int, dtype=to
             return _result(got, "division_decompress_3d")
     N, C, D, H, W = shape
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=packed.device)
+        out = _memory(stream, packed.device)(torch.empty, shape, dtype=dtype, device=packed.device)
     rc = lib().division_decompress_3d(packed.data_ptr(), packed.numel() * packed.element_size(),
                                       N, C, D, H, W, _dt(dtype, c16), B, b, out.data_ptr(), _stream(stream))
     if rc:
@@ -360,7 +360,7 @@ def division_compress_maps(xs, B, b, seeds, packed=None, stream=None, c16: bool 
         need = _packed_bytes(N, C, D, H, W, Bs[i], bs[i], _dt(x.dtype, use16))
         if need == 0:
             raise DivisionError(1, "division_packed_bytes_3d")
-        pk = packed[i] if packed is not None else torch.empty(need, dtype=torch.uint8, device=x.device)
+        pk = packed[i] if packed is not None else _memory(stream, x.device)(torch.empty, need, dtype=torch.uint8, device=x.device)
         made.append(pk)
         descs[i] = _MapDesc(x.data_ptr(), pk.data_ptr(), None, pk.numel() * pk.element_size(), N, C, D, H, W,
                             _dt(x.dtype, use16), Bs[i], bs[i], seeds[i] & (2 ** 64 - 1))
@@ -385,7 +385,7 @@ def division_decompress_maps(packed, shapes, B, b, dtypes=torch.float32, out=Non
     for i, pk in enumerate(packed):
         N, C, D, H, W = _dims5(shapes[i])
         use16 = c16 and dts[i] == torch.float32
-        y = out[i] if out is not None else torch.empty(tuple(shapes[i]), dtype=dts[i], device=pk.device)
+        y = out[i] if out is not None else _memory(stream, pk.device)(torch.empty, tuple(shapes[i]), dtype=dts[i], device=pk.device)
         made.append(y)
         descs[i] = _MapDesc(None, pk.data_ptr(), y.data_ptr(), pk.numel() * pk.element_size(), N, C, D, H, W,
                             _dt(dts[i], use16), Bs[i], bs[i], 0)
@@ -417,7 +417,8 @@ def division_compress_batch(xs, B: int, b: int, seeds, packed=None, stream=None,
     if need == 0:
         raise DivisionError(1, "division_packed_bytes")
     if packed is None:
-        packed = [torch.empty(need, dtype=torch.uint8, device=x0.device) for _ in xs]
+        make = _memory(stream, x0.device)
+        packed = [make(torch.empty, need, dtype=torch.uint8, device=x0.device) for _ in xs]
     packed = list(packed)
     if len(packed) != len(xs):
         raise ValueError("one packed buffer per tensor")
@@ -438,7 +439,8 @@ def division_decompress_batch(packed, shape, B: int, b: int, dtype=torch.float32
         return []
     N, C, H, W = shape
     if out is None:
-        out = [torch.empty(shape, dtype=dtype, device=packed[0].device) for _ in packed]
+        make = _memory(stream, packed[0].device)
+        out = [make(torch.empty, shape, dtype=dtype, device=packed[0].device) for _ in packed]
     out = list(out)
     if len(out) != len(packed):
         raise ValueError("one output per packed buffer")
@@ -479,11 +481,11 @@ def division_relu_forward(x: torch.Tensor, out: torch.Tensor | None = None, mask
         if got is not None:
             return _result(got, "division_relu_forward")
     _flat_ok(x, "x")
-    n = x.numel()
+    n, make = x.numel(), _memory(stream, x.device)
     if out is None:
-        out = torch.empty_like(x)
+        out = make(torch.empty_like, x)
     if mask is None:
-        mask = torch.empty(division_mask_bytes(n) // 4, dtype=torch.int32, device=x.device)
+        mask = make(torch.empty, division_mask_bytes(n) // 4, dtype=torch.int32, device=x.device)
     rc = lib().division_relu_forward(x.data_ptr(), n, _dt(x.dtype), out.data_ptr(), mask.data_ptr(),
                                      mask.numel() * mask.element_size(), _stream(stream))
     if rc:
@@ -503,16 +505,16 @@ def division_relu_compress(x: torch.Tensor, B: int, b: int, seed: int, out: torc
     if x.dim() != 4 or not x.is_cuda or not x.is_contiguous():
         raise ValueError("x must be a contiguous 4-d device tensor")
     N, C, H, W = x.shape
-    n = x.numel()
+    n, make = x.numel(), _memory(stream, x.device)
     if out is None:
-        out = torch.empty_like(x)
+        out = make(torch.empty_like, x)
     if mask is None:
-        mask = torch.empty(division_mask_bytes(n) // 4, dtype=torch.int32, device=x.device)
+        mask = make(torch.empty, division_mask_bytes(n) // 4, dtype=torch.int32, device=x.device)
     if packed is None:
         need = _packed_bytes(N, C, 1, H, W, B, b, _dt(x.dtype, c16))
         if need == 0:
             raise DivisionError(1, "division_packed_bytes")
-        packed = torch.empty(need, dtype=torch.uint8, device=x.device)
+        packed = make(torch.empty, need, dtype=torch.uint8, device=x.device)
     rc = lib().division_relu_compress(x.data_ptr(), N, C, H, W, _dt(x.dtype, c16), B, b, seed & (2 ** 64 - 1),
                                       out.data_ptr(), mask.data_ptr(), mask.numel() * mask.element_size(),
                                       packed.data_ptr(), packed.numel() * packed.element_size(), _stream(stream))
@@ -534,11 +536,11 @@ def division_dropout_forward(x: torch.Tensor, p: float, seed: int, out: torch.Te
         if got is not None:
             return _result(got, "division_dropout_forward")
     _flat_ok(x, "x")
-    n = x.numel()
+    n, make = x.numel(), _memory(stream, x.device)
     if out is None:
-        out = torch.empty_like(x)
+        out = make(torch.empty_like, x)
     if mask is None:
-        mask = torch.empty(division_mask_bytes(n) // 4, dtype=torch.int32, device=x.device)
+        mask = make(torch.empty, division_mask_bytes(n) // 4, dtype=torch.int32, device=x.device)
     rc = lib().division_dropout_forward(x.data_ptr(), n, _dt(x.dtype), p, seed & (2 ** 64 - 1), out.data_ptr(),
                                         mask.data_ptr(), mask.numel() * mask.element_size(), _stream(stream))
     if rc:
@@ -554,7 +556,7 @@ def division_mask_backward(mask: torch.Tensor, grad_out: torch.Tensor, out: torc
             return _result(got, "division_mask_backward")
     _flat_ok(grad_out, "grad_out")
     if out is None:
-        out = torch.empty_like(grad_out)
+        out = _memory(stream, grad_out.device)(torch.empty_like, grad_out)
     rc = lib().division_mask_backward(mask.data_ptr(), mask.numel() * mask.element_size(), grad_out.data_ptr(),
                                       grad_out.numel(), _dt(grad_out.dtype), out.data_ptr(), _stream(stream))
     if rc:
@@ -572,8 +574,9 @@ def division_maxpool_forward(x: torch.Tensor, k: int, stream=None):
         raise ValueError("x must be 4-d")
     _flat_ok(x, "x")
     N, C, H, W = x.shape
-    y = torch.empty((N, C, H // k, W // k), dtype=x.dtype, device=x.device)
-    mask = torch.empty(division_mask_bytes(x.numel()) // 4, dtype=torch.int32, device=x.device)
+    make = _memory(stream, x.device)
+    y = make(torch.empty, (N, C, H // k, W // k), dtype=x.dtype, device=x.device)
+    mask = make(torch.empty, division_mask_bytes(x.numel()) // 4, dtype=torch.int32, device=x.device)
     rc = lib().division_maxpool_forward(x.data_ptr(), N, C, H, W, _dt(x.dtype), k, y.data_ptr(), mask.data_ptr(),
                                         mask.numel() * 4, _stream(stream))
     if rc:
@@ -591,7 +594,7 @@ def division_maxpool_backward(mask: torch.Tensor, grad_out: torch.Tensor, shape,
     N, C, H, W = shape
     if tuple(grad_out.shape) != (N, C, H // k, W // k):
         raise ValueError("grad_out has the wrong shape")
-    out = torch.empty(tuple(shape), dtype=grad_out.dtype, device=grad_out.device)
+    out = _memory(stream, grad_out.device)(torch.empty, tuple(shape), dtype=grad_out.dtype, device=grad_out.device)
     rc = lib().division_maxpool_backward(mask.data_ptr(), mask.numel() * mask.element_size(), grad_out.data_ptr(),
                                          N, C, H, W, _dt(grad_out.dtype), k, out.data_ptr(), _stream(stream))
     if rc:

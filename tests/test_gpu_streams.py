@@ -93,3 +93,27 @@ def test_step_operators(name):
     calls, inputs = _step_calls()
     torch.cuda.synchronize()
     _apart(calls[name], inputs)
+
+
+def _codec_calls():
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(4, 16, 32, 32, generator=gen).cuda()
+    deep = torch.randn(2, 8, 4, 16, 16, generator=gen).cuda()
+    packed, packed3 = pkg.division_compress(x, 8, 2, 1), pkg.division_compress_3d(deep, 8, 2, 1)
+    (_, kept), (_, at) = pkg.division_dropout_forward(x, 0.5, 1), pkg.division_maxpool_forward(x, 2)
+    small = torch.randn(4, 16, 16, 16, generator=gen).cuda()
+    return {"compress": lambda s: pkg.division_compress(x, 8, 2, 1, stream=s), "decompress": lambda s: pkg.division_decompress(packed, x.shape, 8, 2, stream=s),
+            "compress_3d": lambda s: pkg.division_compress_3d(deep, 8, 2, 1, stream=s), "decompress_3d": lambda s: pkg.division_decompress_3d(packed3, deep.shape, 8, 2, stream=s),
+            "compress_maps": lambda s: pkg.division_compress_maps([x, small], 8, 2, [1, 2], stream=s), "decompress_maps": lambda s: pkg.division_decompress_maps([packed, packed], [x.shape] * 2, 8, 2, stream=s),
+            "compress_batch": lambda s: pkg.division_compress_batch([x, x], 8, 2, [1, 2], stream=s), "decompress_batch": lambda s: pkg.division_decompress_batch([packed, packed], x.shape, 8, 2, stream=s),
+            "relu_forward": lambda s: pkg.division_relu_forward(x, stream=s), "relu_compress": lambda s: pkg.division_relu_compress(x, 8, 2, 1, stream=s),
+            "dropout_forward": lambda s: pkg.division_dropout_forward(x, 0.5, 1, stream=s), "mask_backward": lambda s: pkg.division_mask_backward(kept, x, stream=s),
+            "maxpool_forward": lambda s: pkg.division_maxpool_forward(x, 2, stream=s), "maxpool_backward": lambda s: pkg.division_maxpool_backward(at, small, x.shape, 2, stream=s)}
+
+
+@pytest.mark.parametrize("name", ["compress", "decompress", "compress_3d", "decompress_3d", "compress_maps", "decompress_maps", "compress_batch", "decompress_batch", "relu_forward", "relu_compress",
+                                  "dropout_forward", "mask_backward", "maxpool_forward", "maxpool_backward"])
+def test_codec_and_masks(name):
+    calls = _codec_calls()
+    torch.cuda.synchronize()
+    _apart(calls[name])
