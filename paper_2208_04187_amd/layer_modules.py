@@ -31,6 +31,11 @@ def _fits(t: torch.Tensor) -> bool:
     return (t.shape[1] <= 1 or t.stride(1) * size <= 1 << 23) and (t.shape[2] <= 1 or t.stride(2) * size * t.shape[2] <= 1 << 30)
 
 
+def _as_rows(t: torch.Tensor) -> torch.Tensor:
+    """t, or a dense copy where attention does not take its rows as they lie (a dense tensor may begin off 16 bytes itself)"""
+    return t if _fits(t) else t.clone(memory_format=torch.contiguous_format)
+
+
 def _matrix(t: torch.Tensor) -> torch.Tensor:
     """[batch, tokens, heads, features] as [batch * tokens, heads * features], without a copy where the strides allow it"""
     return t.detach().reshape(t.shape[0] * t.shape[1], t.shape[2] * t.shape[3])
@@ -39,7 +44,7 @@ def _matrix(t: torch.Tensor) -> torch.Tensor:
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, scale, causal, window, lengths, starts):
-        q, k, v = (t if _fits(t) else t.contiguous() for t in (q, k, v))
+        q, k, v = _as_rows(q), _as_rows(k), _as_rows(v)
         a = division_attention(q, k, v, scale, causal, window, lengths, starts)
         ctx.save_for_backward(*(_matrix(t) for t in (q, k, v, a.out)), a.lse.view(-1), lengths, starts)
         ctx.shapes, ctx.settings = (q.shape, k.shape), (scale, causal, window)
@@ -55,9 +60,7 @@ class _Attention(torch.autograd.Function):
         q, k, v, out, lse, lengths, starts = ctx.saved_tensors
         of_q, of_k = ctx.shapes
         q, k, v, out = q.view(of_q), k.view(of_k), v.view(of_k), out.view(of_q)
-        if not _fits(grad_out):
-            grad_out = grad_out.contiguous()
-        grads = division_attention_backward(grad_out, q, k, v, out, lse.view(of_q[0], of_q[2], of_q[1]), *ctx.settings, lengths, starts)
+        grads = division_attention_backward(_as_rows(grad_out), q, k, v, out, lse.view(of_q[0], of_q[2], of_q[1]), *ctx.settings, lengths, starts)
         return (*grads, None, None, None, None, None)
 
 

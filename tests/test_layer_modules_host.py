@@ -125,3 +125,32 @@ def test_a_rotation_that_began_in_inference_mode_trains():
     x = torch.ones(3, dtype=torch.float64, requires_grad=True)
     _Save.apply(x, first).sum().backward()
     assert torch.equal(x.grad, first.sum().expand(3))
+
+
+class _Attended:
+    def __init__(self, q):
+        self.out, self.lse = torch.zeros(q.shape, dtype=q.dtype), torch.zeros(q.shape[0], q.shape[2], q.shape[1])
+
+
+def test_attention_under_autograd_copies_dense_rows_that_start_off_16_bytes(monkeypatch):
+    """A dense tensor is its own contiguous()"""
+    seen = []
+
+    def attend(q, k, v, *rest):
+        seen.extend((q, k, v))
+        return _Attended(q)
+
+    def backward(grad_out, q, k, v, *rest):
+        seen.extend((grad_out, q, k, v))
+        return torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    monkeypatch.setattr(layer_modules, "division_attention", attend)
+    monkeypatch.setattr(layer_modules, "division_attention_backward", backward)
+    for dtype in (torch.float32, torch.bfloat16):
+        room = torch.randn(8 + 2 * 5 * 4 * 16).to(dtype)
+        for off in range(1, 16 // room.element_size()):
+            x = room[off: off + 2 * 5 * 4 * 16].view(2, 5, 4, 16).requires_grad_()
+            assert x.is_contiguous() and x.data_ptr() % 16
+            seen.clear()
+            out = pkg.division_token_attention(x, x, x)
+            out.backward(x.detach())
+            assert len(seen) == 7 and all(t.data_ptr() % 16 == 0 and torch.equal(t, x) for t in seen)
