@@ -25,6 +25,8 @@ from .token_modules import _beside_the_stream, _first_derivatives
 
 def _fits(t: torch.Tensor) -> bool:
     """Whether attention takes the rows as they lie: on 16 bytes, features next to one another, tokens at most 8 MB apart and heads all within 1 GB"""
+    if t.dim() != 4:
+        return True                                         # for the call itself to refuse
     size = t.element_size()
     if t.data_ptr() % 16 or t.stride(3) != 1 or any(n > 1 and s * size % 16 for n, s in zip(t.shape[:3], t.stride()[:3])):
         return False

@@ -154,3 +154,10 @@ def test_attention_under_autograd_copies_dense_rows_that_start_off_16_bytes(monk
             out = pkg.division_token_attention(x, x, x)
             out.backward(x.detach())
             assert len(seen) == 7 and all(t.data_ptr() % 16 == 0 and torch.equal(t, x) for t in seen)
+
+
+def test_attention_under_autograd_refuses_other_than_four_dimensions():
+    for shape in ((4,), (3, 16), (2, 3, 16), (1, 2, 3, 4, 16)):
+        x = torch.zeros(shape, requires_grad=True)
+        with pytest.raises(ValueError, match="batch, tokens, heads, features"):
+            pkg.division_token_attention(x, x, x)
