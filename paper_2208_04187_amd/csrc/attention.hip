@@ -157,10 +157,9 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     const float lse = total == 0.0f ? -INFINITY : __builtin_fmaf(c.most, a.scale, logf(total));
     const int r = (int)(col % (uint32_t)a.R);
     if (a.parts) {
-        // [split][group][column]: lse, and the values
         const int64_t at = ((int64_t)split * a.groups + group) * cols + col;
         if (half == 0) a.parts[at] = lse;
-        float* row = a.parts + (int64_t)a.splits * a.groups * cols + at * a.D;
+        float* row = a.values + at * a.D;
 #pragma unroll
         for (int d = 0; d < DP; d += 8) {
             if (d >= a.D) continue;
@@ -254,7 +253,7 @@ template <typename T, int DP, int KT, int WK, bool PAST> __global__ __launch_bou
         if (a.parts) {
             const int64_t at = ((int64_t)split * a.groups + group) * cols + at_col;
             if (d == 0) a.parts[at] = lse;
-            *reinterpret_cast<f32x4*>(a.parts + (int64_t)a.splits * a.groups * cols + at * a.D + d) = o;
+            *reinterpret_cast<f32x4*>(a.values + at * a.D + d) = o;
         } else {
             const int i1 = (int)(at_col / (uint32_t)a.R), h = g * a.R + (int)(at_col % (uint32_t)a.R);
             if (d == 0) a.lse[((int64_t)b * a.H + h) * a.Sq + i1] = lse;
@@ -271,7 +270,7 @@ template <typename T, int GROUPS> __global__ __launch_bounds__(kThreads) void jo
     const uint32_t n = (uint32_t)a.groups * cols, at = blockIdx.x * (kThreads / 32 / GROUPS) + threadIdx.x / 32 / GROUPS;
     if (GROUPS == 1 && at >= n) return;
     const int d = (int)lane * 4;
-    const float* from = a.parts + (int64_t)a.splits * n + (int64_t)at * a.D + (d < a.D ? d : 0);
+    const float* from = a.values + (int64_t)at * a.D + (d < a.D ? d : 0);
     float lses[kParts], most = -INFINITY;
     f32x4 parts[kParts];
 #pragma unroll
@@ -352,7 +351,8 @@ Cut cut_of(const division_attention& a) {
     }
     return c;
 }
-size_t parts_bytes(const division_attention& a, const Cut& c) { return c.splits > 1 ? (size_t)c.splits * a.B * a.Sq * a.H * (a.D + 1) * 4 : 0; }
+size_t lse_bytes(const division_attention& a, const Cut& c) { return ((size_t)c.splits * a.B * a.Sq * a.H * 4 + 15) / 16 * 16; }
+size_t parts_bytes(const division_attention& a, const Cut& c) { return c.splits > 1 ? lse_bytes(a, c) + (size_t)c.splits * a.B * a.Sq * a.H * a.D * 4 : 0; }
 
 template <typename T, int DP> int run(const AttentionArgs& args, const Cut& c, int64_t grid, hipStream_t st) {
     constexpr int kFew = sizeof(T) == 2 && DP == 96 ? 128 : DP;                      // 96 bfloat16 are no rows of eight pieces
@@ -399,6 +399,7 @@ int division_attend(const division_attention* attention, void* out, float* lse, 
     args.out = static_cast<char*>(out);
     args.lse = lse;
     args.parts = need ? static_cast<float*>(workspace) : nullptr;
+    args.values = need ? reinterpret_cast<float*>(static_cast<char*>(workspace) + lse_bytes(a, c)) : nullptr;
     args.blocks = (int)c.blocks;
     args.splits = c.splits;
     args.tiles = c.tiles;

@@ -7,7 +7,7 @@ struct AttentionArgs {
     Heads qs, ks, vs;
     const int *lengths, *starts;
     char* out;
-    float *lse, *parts;
+    float *lse, *parts, *values;                        // parts of the keys: [split][group][column] their lse, and behind them on 16 bytes their values of D elements each
     int64_t window;
     int Sq, Sk, H, G, R, D, causal, groups;             // groups: B * G
     int blocks, splits, tiles;                          // of columns; parts of the keys, and how many tiles one has at least
