@@ -35,7 +35,7 @@ struct DropoutArgs {
     const void *x, *residual;
     void* y;
     const uint64_t* seed_at;                                // or null
-    int64_t n;
+    int64_t n, begin;                                       // elements, and the launch's first one
     uint64_t seed;
     uint32_t thr;
     float by;
@@ -47,7 +47,7 @@ template <typename T, bool ADD, bool PAST> __global__ __launch_bounds__(kThreads
     typedef Unit<T> U;
     const uint64_t seed = (a.seed_at ? *a.seed_at : a.seed) ^ kDropoutStream;
     const uint32_t seed_a = mix32((uint32_t)seed ^ 0x243F6A88u), seed_c = mix32((uint32_t)(seed >> 32) ^ 0x85A308D3u);
-    const int64_t first = ((int64_t)blockIdx.x * kUnroll * kThreads + threadIdx.x) * U::kSize;
+    const int64_t first = a.begin + ((int64_t)blockIdx.x * kUnroll * kThreads + threadIdx.x) * U::kSize;
     const T *x = static_cast<const T*>(a.x), *r = static_cast<const T*>(a.residual);
     U q[kUnroll], s[kUnroll];
 #pragma unroll
@@ -77,13 +77,19 @@ template <typename T, bool ADD, bool PAST> __global__ __launch_bounds__(kThreads
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
-template <typename T> int run(const DropoutArgs& a, hipStream_t st) {
-    const int64_t per = (int64_t)kThreads * kUnroll * Unit<T>::kSize, grid = (a.n + per - 1) / per;
-    if (a.n > (int64_t(1) << 35) || grid >= (int64_t(1) << 24)) return DIVISION_ERANGE;
+constexpr int64_t kMostWorkgroups = int64_t(1) << 23;        // of a launch, which has fewer than 2^32 threads
+
+template <typename T> int run(DropoutArgs& a, hipStream_t st) {
+    constexpr int64_t per = (int64_t)kThreads * kUnroll * Unit<T>::kSize;
+    if (a.n > (int64_t(1) << 35)) return DIVISION_ERANGE;
     const bool past = a.n * (int64_t)sizeof(T) * (a.residual ? 3 : 2) > kCached;
     void (*kernel)(DropoutArgs) = a.residual ? (past ? dropout_add<T, true, true> : dropout_add<T, true, false>) : past ? dropout_add<T, false, true> : dropout_add<T, false, false>;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kThreads), 0, st, a);
-    return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP;
+    for (a.begin = 0; a.begin < a.n; a.begin += kMostWorkgroups * per) {
+        const int64_t left = (a.n - a.begin + per - 1) / per;
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)(left < kMostWorkgroups ? left : kMostWorkgroups)), dim3(kThreads), 0, st, a);
+        if (hipGetLastError() != hipSuccess) return DIVISION_EHIP;
+    }
+    return DIVISION_OK;
 }
 
 }  // namespace
