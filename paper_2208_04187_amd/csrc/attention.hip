@@ -99,11 +99,6 @@ __device__ __forceinline__ void part_of(const AttentionArgs& a, int split, int& 
     lo = begin;
 }
 
-template <typename T> __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
-    else *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pack2(a, b), bf16_pack2(c, d)};
-}
-
 constexpr int kThreads = 256;
 
 // Four wavefronts of 32 columns each share the tiles of the keys, two tiles of 64 keys in the local memory, the second on its way while the first is looked at.  S = K Q^T, so that a lane has one
@@ -125,9 +120,8 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
     const uint32_t last_col = min(first_col + 127u, cols - 1), wave_last = min(wave_col + 31u, cols - 1);
     int lo = seen.from((int)(first_col / (uint32_t)a.R)) / KT, hi = (seen.to((int)(last_col / (uint32_t)a.R)) + KT - 1) / KT;
     part_of(a, split, lo, hi);
-    const bool works = wave_col < cols;
-    const int qa = works ? (int)(wave_col / (uint32_t)a.R) : 0, qb = works ? (int)(wave_last / (uint32_t)a.R) : 0;
-    const int wave_from = seen.from(qa), whole_from = seen.from(qb), whole_to = seen.to(qa), wave_to = works ? seen.to(qb) : 0;
+    const int qa = wave_col < cols ? (int)(wave_col / (uint32_t)a.R) : 0, qb = wave_col < cols ? (int)(wave_last / (uint32_t)a.R) : 0;
+    const int whole_from = seen.from(qb), whole_to = seen.to(qa);
     const int i = (int)(min(col, cols - 1) / (uint32_t)a.R);
     const int from = seen.from(i), to = col < cols ? max(from, seen.to(i)) : from;
     const char* k = a.k + b * a.ks.batch + (int64_t)g * a.ks.head;
@@ -355,17 +349,18 @@ size_t lse_bytes(const division_attention& a, const Cut& c) { return ((size_t)c.
 size_t parts_bytes(const division_attention& a, const Cut& c) { return c.splits > 1 ? lse_bytes(a, c) + (size_t)c.splits * a.B * a.Sq * a.H * a.D * 4 : 0; }
 
 template <typename T, int DP> int run(const AttentionArgs& args, const Cut& c, int64_t grid, hipStream_t st) {
-    constexpr int kFew = sizeof(T) == 2 && DP == 96 ? 128 : DP;                      // 96 bfloat16 are no rows of eight pieces
-    // keys that one block of columns looks at are looked at once
-    // keys that one block of columns looks at are looked at once.  In fp32 two wavefronts, so that two workgroups fit a CU's local memory, unless there are no two (16 tokens over 2000 keys, 8 heads of
-    // 128: 80 us with four, 69 so; one token of 32 heads on 8 over 4000: 19 us with two, 14 so)
-    void (*few)(AttentionArgs) = c.blocks > 1 ? attend_few<T, kFew, 32, 4, false> : attend_few<T, kFew, 32, 4, true>;
-    int waves = 4;
-    if constexpr (sizeof(T) == 4) {
-        if (c.blocks == 1 && grid > 256) { few = attend_few<T, kFew, 32, 2, true>; waves = 2; }
+    constexpr bool kFew = sizeof(T) == 4 || DP != 96;                                // 96 bfloat16 are no rows of eight pieces: few columns of such heads take 128
+    if constexpr (kFew) {
+        // keys that one block of columns looks at are looked at once.  In fp32 two wavefronts, so that two workgroups fit a CU's local memory, unless there are no two (16 tokens over 2000 keys, 8 heads of
+        // 128: 80 us with four, 69 so; one token of 32 heads on 8 over 4000: 19 us with two, 14 so)
+        void (*few)(AttentionArgs) = c.blocks > 1 ? attend_few<T, DP, 32, 4, false> : attend_few<T, DP, 32, 4, true>;
+        int waves = 4;
+        if constexpr (sizeof(T) == 4) {
+            if (c.blocks == 1 && grid > 256) { few = attend_few<T, DP, 32, 2, true>; waves = 2; }
+        }
+        if (c.few) hipLaunchKernelGGL(few, dim3((uint32_t)grid), dim3(64 * waves), 0, st, args);
     }
-    if (c.few) hipLaunchKernelGGL(few, dim3((uint32_t)grid), dim3(64 * waves), 0, st, args);
-    else hipLaunchKernelGGL((attend<T, DP, 64>), dim3((uint32_t)grid), dim3(kThreads), 0, st, args);
+    if (!c.few) hipLaunchKernelGGL((attend<T, DP, 64>), dim3((uint32_t)grid), dim3(kThreads), 0, st, args);
     CHECKED(launched());
     if (c.splits == 1) return DIVISION_OK;
     const int64_t rows = (int64_t)args.groups * args.Sq * args.R;

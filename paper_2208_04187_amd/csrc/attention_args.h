@@ -32,9 +32,7 @@ template <typename A> __device__ __forceinline__ Seen seen_of(const A& a, int b)
 
 // ------------------------------------------------------------------ host side
 
-bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP; }
-#define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
+#include "launch.h"
 
 // A tensor of rows: nothing behind what 31 bits say of a tile's rows, which are up to 129 tokens' of the `share` heads that have one key head; every row on 16 bytes
 constexpr int64_t kMostStride = 1 << 23, kMostHeads = 1 << 30, kMostTokens = 1 << 29, kMostGroups = 1 << 24;
@@ -46,12 +44,12 @@ int check_heads(const void* p, const int64_t* strides, int64_t B, int64_t share,
     return DIVISION_OK;
 }
 int check_attention(const division_attention& a) {
-    if (a.dt != DIVISION_F32 && a.dt != DIVISION_BF16) return DIVISION_EINVAL;
+    if (!type_ok(a.dt)) return DIVISION_EINVAL;
     if (a.B < 0 || a.Sq < 0 || a.Sk < 0 || a.H < 1 || a.G < 1 || a.H % a.G || a.D < 8 || a.D > 128 || a.D % 8 || a.window < 0 || (a.causal != 0 && a.causal != 1)) return DIVISION_EINVAL;
     if (!(a.scale > 0.0f && a.scale <= 2e38f)) return DIVISION_EINVAL;
     if (!aligned(a.lengths, 4) || !aligned(a.starts, 4)) return DIVISION_EALIGN;
     if (a.B == 0) return DIVISION_OK;
-    const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4, R = a.H / a.G;
+    const int64_t es = (int64_t)size_of(a.dt), R = a.H / a.G;
     if (a.B > (1 << 24) || a.H > 4096 || a.Sq > kMostTokens || a.Sk > kMostTokens || a.Sq * R > (int64_t(1) << 30)) return DIVISION_ERANGE;
     // more than any launch has room for, before it is narrowed
     if ((a.Sq > 0 || a.Sk > 0) && a.B * a.G >= kMostGroups) return DIVISION_ERANGE;
@@ -64,7 +62,7 @@ int check_attention(const division_attention& a) {
 }
 Heads heads_of(const int64_t* strides, int64_t es) { return {strides[0] * es, (int)(strides[1] * es), (int)(strides[2] * es)}; }
 AttentionArgs args_of(const division_attention& a) {
-    const int64_t es = a.dt == DIVISION_BF16 ? 2 : 4;
+    const int64_t es = (int64_t)size_of(a.dt);
     AttentionArgs r{};
     r.q = static_cast<const char*>(a.q); r.k = static_cast<const char*>(a.k); r.v = static_cast<const char*>(a.v);
     r.qs = heads_of(a.q_strides, es); r.ks = heads_of(a.k_strides, es); r.vs = heads_of(a.v_strides, es);

@@ -25,10 +25,6 @@ struct BackArgs : AttentionArgs {
     FastDiv by_R;
 };
 
-template <typename T> __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
-    else *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pack2(a, b), bf16_pack2(c, d)};
-}
 // a lane's column of blocks [DP][32], times `by`, to a row
 template <typename T, int DP> __device__ __forceinline__ void put_column(T* row, const f32x16* o, float by, int D, int half) {
 #pragma unroll

@@ -75,7 +75,7 @@ template <typename T, bool ADD, bool PAST> __global__ __launch_bounds__(kThreads
     }
 }
 
-bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+#include "launch.h"
 
 constexpr int64_t kMostWorkgroups = int64_t(1) << 23;        // of a launch, which has fewer than 2^32 threads
 
@@ -87,7 +87,7 @@ template <typename T> int run(DropoutArgs& a, hipStream_t st) {
     for (a.begin = 0; a.begin < a.n; a.begin += kMostWorkgroups * per) {
         const int64_t left = (a.n - a.begin + per - 1) / per;
         hipLaunchKernelGGL(kernel, dim3((uint32_t)(left < kMostWorkgroups ? left : kMostWorkgroups)), dim3(kThreads), 0, st, a);
-        if (hipGetLastError() != hipSuccess) return DIVISION_EHIP;
+        CHECKED(launched());
     }
     return DIVISION_OK;
 }
@@ -97,10 +97,10 @@ template <typename T> int run(DropoutArgs& a, hipStream_t st) {
 extern "C" {
 
 int division_dropout_add(const void* x, const void* residual, int64_t n, division_dtype dt, double p, uint64_t seed, const uint64_t* device_seed, void* y, void* hip_stream) {
-    if (n < 0 || (dt != DIVISION_F32 && dt != DIVISION_BF16) || !(p >= 0.0 && p <= 1.0)) return DIVISION_EINVAL;
+    if (n < 0 || !type_ok(dt) || !(p >= 0.0 && p <= 1.0)) return DIVISION_EINVAL;
     if (n == 0) return DIVISION_OK;
     if (!x || !y) return DIVISION_EINVAL;
-    const size_t es = dt == DIVISION_BF16 ? 2 : 4;
+    const size_t es = size_of(dt);
     if (!aligned(x, es) || !aligned(residual, es) || !aligned(y, es) || !aligned(device_seed, 8)) return DIVISION_EALIGN;
     DropoutArgs a{};
     a.x = x; a.residual = residual; a.y = y; a.n = n; a.seed = seed; a.seed_at = device_seed;

@@ -377,11 +377,7 @@ template <typename T, typename O, int P> __global__ __launch_bounds__(kThreads) 
 
 // ------------------------------------------------------------------ host side
 
-bool type_ok(division_dtype dt) { return dt == DIVISION_F32 || dt == DIVISION_BF16; }
-bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP; }
-#define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
-size_t size_of(division_dtype dt) { return dt == DIVISION_BF16 ? 2 : 4; }
+#include "launch.h"
 constexpr int64_t kMostWorkgroups = int64_t(1) << 24, kMostTokens = int64_t(1) << 31, kMostElements = int64_t(1) << 40;
 
 // tokens of a part: few enough that one row's keep many wavefronts busy, and no more than 2048 parts, which the row's own adds up one after the other

@@ -269,11 +269,7 @@ __global__ __launch_bounds__(1024) void add_weight_parts(AddArgs a) {
 
 // ------------------------------------------------------------------ host side
 
-bool type_ok(division_dtype dt) { return dt == DIVISION_F32 || dt == DIVISION_BF16; }
-bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-int launched() { return hipGetLastError() == hipSuccess ? DIVISION_OK : DIVISION_EHIP; }
-#define CHECKED(call) do { const int rc_ = (call); if (rc_ != DIVISION_OK) return rc_; } while (0)
-size_t size_of(division_dtype dt) { return dt == DIVISION_BF16 ? 2 : 4; }
+#include "launch.h"
 
 constexpr int kMostParts = 1024;                            // workgroups of a backward launch, which leave a share of a weight's gradient each: what the CUs hold at once
 

@@ -11,7 +11,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 #define LDS_AT(T, p) ((__attribute__((address_space(3))) T*)(p))
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // The row of a 32 x 32 block that register i of this lane holds
 __device__ __forceinline__ int block_row(int i, int half) { return 8 * (i / 4) + 4 * half + i % 4; }
@@ -42,6 +42,11 @@ __device__ __forceinline__ void product(f32x16& c, const Operand<uint16_t>& a, c
 __device__ __forceinline__ void product(f32x16& c, const Operand<float>& a, const Operand<float>& b) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+}
+
+template <typename T> __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
+    else *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pack2(a, b), bf16_pack2(c, d)};
 }
 
 // Loads into the local memory: 64 lanes' sixteen (four) bytes of a buffer, each from an offset of its own, one behind the other from `to` on; beyond the buffer's bytes zeros.  In assembly, since
