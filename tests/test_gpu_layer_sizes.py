@@ -30,9 +30,10 @@ def _rotation_inputs(dtype, T, heads, D, seed):
 
 @pytest.mark.parametrize("pairs", ["halves", "next"])
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_rotation_beyond_the_caches(dtype, pairs):
+@pytest.mark.parametrize("D", [32, 64, 128, 256, 512])
+def test_rotation_beyond_the_caches(D, dtype, pairs):
     """A token's results are its own: the same bits as in two calls that stay within the caches"""
-    D, heads = 128, (32, 8)
+    heads = (32, 8)
     T = CACHED // (2 * sum(heads) * D * dtype.itemsize) + 77
     q, k, w, f, at = _rotation_inputs(dtype, T, heads, D, 1)
     halves = [slice(0, T // 3), slice(T // 3, 2 * T // 3), slice(2 * T // 3, T)]
