@@ -601,13 +601,14 @@ int division_head_norm_rotate_backward(const division_rotate *rotate, const divi
 
 /*
  * Rows of a table, scaled: out[t] = scale * table[ids[t]] (a product in fp32, rounded to dt), zeros where ids[t] is ignore_index, NaN where it is any other number outside
- * 0 .. V - 1.  table [V][D] and out [T][D] of type dt, dense; T, V and D below 2^31.
+ * 0 .. V - 1.  table [V][D] and out [T][D] of type dt, dense; T, V and D below 2^31, and T rows' pieces of 16 bytes below 2^32 - 255 (DIVISION_ERANGE).
  */
 int division_embedding(const int64_t *ids, int64_t T, const void *table, int64_t V, int64_t D, division_dtype dt, float scale, int64_t ignore_index, void *out, void *hip_stream);
 
 /*
  * The table's gradient: grad_table[v] = scale * sum of grad[t] over the tokens with ids[t] = v, in fp32 and in the order of the tokens, rounded to table_dt; tokens of
- * ignore_index or outside the table have none.
+ * ignore_index or outside the table have none.  T and D below 2^31, V below 2^30, and V rows' pieces of 2 KB of gradient up to 2^27 (DIVISION_ERANGE beyond what a launch has room for).  A row of many
+ * tokens is added up in parts, and these in an order of their own: both are decided by T and by where the row's tokens stand among all.
  *   grad        T rows of D elements of type dt, grad_stride elements apart
  *   grad_table  [V][D] of type table_dt, written in full; with add = 1 the sums are added to what it holds, and rows without a token are left as they are
  *   workspace   division_embedding_backward_workspace(T, V, D) bytes on 16

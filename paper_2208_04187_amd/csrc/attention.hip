@@ -83,6 +83,8 @@ template <typename T, int DP> struct Columns {
                 float w[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) w[j] = z[b][8 * c + j];
+                // bfloat16: rounded, as the matrix instruction takes both factors of one type, by half a step of 2^-8 each; `total` has them unrounded.  (Error of the output, as a norm, against 64 bits: 0.0016 for
+                // the output's own rounding, 0.0021 with this one; a second product of what the rounding left out would keep it, for half as many products again.)
                 const Operand<T> p = Operand<T>::of(w);
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d) product(o[d], Keys::columns(vt, 32 * b + 16 * c, 32 * d, lane), p);
@@ -175,8 +177,11 @@ template <typename T, int DP, int KT> __global__ __launch_bounds__(kThreads, siz
 }
 
 // Few columns: WK wavefronts have the same 32 columns and every WK-th tile of the keys each, in a tile of their own, and are joined at the end.  PAST: the keys are looked at by this workgroup
-// alone.  Bound by memory then: 32 tokens of 32 heads on 4 of 128 over caches of up to 8192 keys, 56 us = 4.7 TB/s.  While a wavefront computes, seven
-// others of the CU wait for their tiles; two tiles a wavefront, the second on its way, leave room for half as many (32 tokens over caches of up to 8192 keys: 69 us so, 64 with one tile).
+// alone.  Bound by memory then: 32 tokens of 32 heads on 4 of 128 over caches of up to 8192 keys in bfloat16, 56 us = 4.7 TB/s.  While a wavefront computes, seven
+// others of the CU wait for their tiles; two tiles a wavefront, the second on its way, leave room for half as many (the same call: 69 us so, 64 with one tile).  In fp32 of more than 64 features a CU has room
+// for one workgroup of four wavefronts or two of two, a SIMD for one wavefront, and each tile is waited for in full: the same caches in fp32 188 us = 2.9 TB/s; 3 x 777 tokens of 6 heads on 2 of 72, which see up
+// to 480 and 184 keys and none, 26.6 us, where the longest wavefront has four tiles of 2.6 us of products: 9.1 if no query sees a key (438 workgroups' starts and ends, one a CU), 17.9 if 128 keys of the first
+// sequence are seen (a tile a wavefront), 21.9 if its 480 are.
 template <typename T, int DP, int KT, int WK, bool PAST> __global__ __launch_bounds__(64 * WK) void attend_few(AttentionArgs a) {
     typedef RowTile<T, DP, KT> Keys;
     constexpr int kTile = Keys::kBytes, kTurns = DP == 96 ? 8 : DP / 4;

@@ -173,7 +173,7 @@ template <typename T, int DP, int KT, int WAVES, int SETS> __global__ __launch_b
                     float w[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) w[j] = z[8 * c + j];
-                    const Operand<T> ds = Operand<T>::of(w);
+                    const Operand<T> ds = Operand<T>::of(w);            // bfloat16: rounded, as the matrix instruction takes both factors of one type; z and dp are not (the gradients' error 0.0017 -> 0.0024)
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d) product(dq[d], Tile<T, DP, KT>::columns(kt, 32 * n + 16 * c, 32 * d, lane), ds);
                 }
@@ -293,7 +293,7 @@ template <typename T, int DP, int CT, int WAVES, int SETS, bool VALUES> __global
                     float w[8], x[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) { w[j] = z[8 * c + j]; x[j] = dp[8 * c + j]; }
-                    const Operand<T> p = Operand<T>::of(w), ds = Operand<T>::of(x);
+                    const Operand<T> p = Operand<T>::of(w), ds = Operand<T>::of(x);     // rounded in bfloat16, as in the queries' kernel
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d) product(dv[d], Columns::columns(gt, 32 * n + 16 * c, 32 * d, lane), p);
 #pragma unroll
@@ -374,7 +374,8 @@ Splits splits_of(const division_attention& a) {
     const bool half = a.dt == DIVISION_BF16;
     const int64_t cols = a.Sq * (a.H / a.G), groups = a.B * a.G;
     Splits s;
-    // not over long sequences, whose parts keep larger workgroups busy too (two heads of 128, 4090 tokens: 89 us, 97 with small ones)
+    // not over long sequences, whose parts keep larger workgroups busy too (two heads of 128, 4090 tokens: 89 us, 97 with small ones).  A window is not looked at here, though it leaves a block few tiles and
+    // no parts: 2 x 3000 tokens, 8 heads on 4 of 128, window 79 take 69 us (187 without one)
     s.few_queries = half && (cols + 127) / 128 * groups < 256 && a.Sk <= 2048;
     s.few_keys = half && (a.Sk + 127) / 128 * groups < 256 && cols <= 4096;
     s.least_keys = s.few_queries ? 24 : half ? 4 : 2;

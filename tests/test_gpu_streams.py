@@ -117,3 +117,15 @@ def test_codec_and_masks(name):
     calls = _codec_calls()
     torch.cuda.synchronize()
     _apart(calls[name])
+
+
+def test_the_default_stream_by_its_handle_and_the_current_one_by_name():
+    calls = {**_layer_calls()[0], **_step_calls()[0], **_codec_calls()}
+    torch.cuda.synchronize()
+    for name, call in calls.items():
+        want = [t.clone() for t in _tensors(call(None))]
+        assert torch.cuda.default_stream().cuda_stream == 0
+        for stream in (0, torch.cuda.default_stream(), torch.cuda.current_stream()):
+            got = _tensors(call(stream))
+            torch.cuda.synchronize()
+            assert all(torch.equal(a.reshape(-1).view(torch.uint8), b.reshape(-1).view(torch.uint8)) for a, b in zip(got, want)), name
