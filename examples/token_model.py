@@ -34,7 +34,7 @@ class Block(torch.nn.Module):
 class Attention(torch.nn.Module):
     """Two query heads for each head of keys and values"""
 
-    def __init__(self, width, heads, code, group, dtype, dropout):
+    def __init__(self, width, heads, code, group, dtype, dropout, seed):
         super().__init__()
         self.heads, self.key_heads, self.features = heads, max(1, heads // 2), width // heads
         parts = (self.heads, self.key_heads, self.key_heads)
@@ -42,7 +42,7 @@ class Attention(torch.nn.Module):
         self.project = dv.DivisionNormLinear(width, sum(self.parts), code=code, group=group, device="cuda", dtype=dtype)
         self.rotate = dv.DivisionHeadNormRotation(self.features, device="cuda", dtype=dtype)
         self.out = torch.nn.Linear(width, width, bias=False, device="cuda", dtype=dtype)
-        self.drop = dv.DivisionResidualDropout(dropout)
+        self.drop = dv.DivisionResidualDropout(dropout, seed)
 
     def forward(self, x, residual, positions, cache=None):
         h, stream = self.project(x, residual)
@@ -63,7 +63,7 @@ class TokenModel(torch.nn.Module):
         super().__init__()
         if heads:
             self.embed = dv.DivisionEmbedding(vocabulary, width, device="cuda", dtype=dtype)
-            self.attention = torch.nn.ModuleList([Attention(width, heads, code, group, dtype, dropout) for _ in range(layers)])
+            self.attention = torch.nn.ModuleList([Attention(width, heads, code, group, dtype, dropout, k << 32) for k in range(layers)])         # seeds far apart: modules of one seed drop the same elements
         else:
             self.embed = torch.nn.Embedding(vocabulary, width, device="cuda", dtype=dtype)
             self.attention = None

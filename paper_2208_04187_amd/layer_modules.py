@@ -176,7 +176,7 @@ class _ResidualDropout(torch.autograd.Function):
 
 class DivisionResidualDropout(torch.nn.Module):
     """forward(x, residual=None) -> residual + dropout(x), kept elements divided by 1 - p, without a stored mask.  Call number n of this module while training drops what seed + n says
-    (DivisionDropout's elements of the same call); in eval mode nothing is dropped.  Under activation checkpointing seed is None: a call draws its own from torch's generator, which is put back before
+    (DivisionDropout's elements of the same call): modules of a model need seeds farther apart than they have calls.  In eval mode nothing is dropped.  Under activation checkpointing seed is None: a call draws its own from torch's generator, which is put back before
     the forward runs again; a numbered call inside a backward pass raises.  A captured graph drops the captured call's elements whenever it is replayed: for others each time call
     division_dropout_add with a seed on the device."""
 
