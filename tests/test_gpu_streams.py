@@ -129,3 +129,39 @@ def test_the_default_stream_by_its_handle_and_the_current_one_by_name():
             got = _tensors(call(stream))
             torch.cuda.synchronize()
             assert all(torch.equal(a.reshape(-1).view(torch.uint8), b.reshape(-1).view(torch.uint8)) for a, b in zip(got, want)), name
+
+
+def test_a_fork_within_a_graph():
+    """Calls on another stream that a captured one waits for, replayed between eager work"""
+    gen = torch.Generator().manual_seed(4)
+    q, k = torch.randn(2, 60, 4, 64, generator=gen).cuda(), torch.randn(2, 900, 2, 64, generator=gen).cuda()
+    w, x = torch.rand(64, generator=gen).cuda(), torch.randn(300, 64, generator=gen).cuda()
+
+    def step(side=None):
+        current = torch.cuda.current_stream()
+        if side is not None:
+            side.wait_stream(current)
+        a = pkg.division_attention(q, k, k, causal=True, stream=side)
+        back = pkg.division_attention_backward(q, q, k, k, a.out, a.lse, causal=True, stream=side)
+        n = pkg.division_rms_norm(x, w, stream=side)
+        b = pkg.division_rms_norm_backward(x, x, w, n.rstd, stream=side)
+        d = pkg.division_dropout_add(n.y, 0.5, 3, residual=x, stream=side)
+        y = x * 2
+        if side is not None:
+            current.wait_stream(side)
+        return (*a, *back, n.y, *b, d, y)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    main.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(main):
+        step(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=main):
+            outs = step(side)
+    for _ in range(3):
+        for t in (q, k, x):
+            t.mul_(0.9).add_(0.01)
+        want = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
