@@ -172,22 +172,32 @@ def _stream(stream) -> int:
 
 class _Memory:
     """What a call on a stream of its own makes: memory of that stream, so that the call waits for whatever used it before.  (A block that the current stream has given back may still be in
-    use by what is queued there, behind which another stream does not wait.)  What is returned goes back to that stream when the current one, which the caller reads it on, has passed its last use."""
+    use by what is queued there, behind which another stream does not wait.)  What the caller is given goes back to that stream when the current one, which it is read on, has passed its last use."""
 
     def __init__(self, stream, device):
         self.side = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
         self.current = torch.cuda.current_stream(device)
 
-    def __call__(self, make, *args, **kw):
-        with torch.cuda.stream(self.side):
-            t = make(*args, **kw)
-        t.record_stream(self.current)
-        return t
+    def __call__(self, make, *args, given=True, **kw):
+        if self.side.device_index == self.current.device_index == torch.cuda.current_device():
+            # 1 us where the context manager, which looks after other devices too, takes 6
+            torch.cuda.set_stream(self.side)
+            try:
+                got = make(*args, **kw)
+            finally:
+                torch.cuda.set_stream(self.current)
+        else:
+            with torch.cuda.stream(self.side):
+                got = make(*args, **kw)
+        if given:                               # 2 us on the host, and as much when it goes back
+            for t in got if isinstance(got, list) else (got,):
+                t.record_stream(self.current)
+        return got
 
 
 def _memory(stream, device):
-    """make(torch.empty, ...) for the outputs and workspaces of a call: on the given stream, or on the current one"""
-    return (lambda make, *args, **kw: make(*args, **kw)) if stream is None else _Memory(stream, device)
+    """make(torch.empty, ...) for the outputs (one or a list) and workspaces (given=False) of a call: on the given stream, or on the current one"""
+    return (lambda make, *args, given=True, **kw: make(*args, **kw)) if stream is None else _Memory(stream, device)
 
 
 # Size of a packed buffer: a function of whole numbers alone, asked for on every call of a training step with the same
@@ -351,19 +361,21 @@ def division_compress_maps(xs, B, b, seeds, packed=None, stream=None, c16: bool 
     if len(seeds) != n or len(Bs) != n or len(bs) != n:
         raise ValueError("one seed (and block size, code width) per map")
     descs = (_MapDesc * max(n, 1))()
-    made = []
+    need, shapes = [], []
     for i, x in enumerate(xs):
         if not x.is_cuda or not x.is_contiguous():
             raise ValueError("every map must be a contiguous device tensor")
-        N, C, D, H, W = _dims5(x.shape)
-        use16 = c16 and x.dtype == torch.float32
-        need = _packed_bytes(N, C, D, H, W, Bs[i], bs[i], _dt(x.dtype, use16))
-        if need == 0:
+        shapes.append(_dims5(x.shape))
+        need.append(_packed_bytes(*shapes[i], Bs[i], bs[i], _dt(x.dtype, c16 and x.dtype == torch.float32)))
+        if need[i] == 0:
             raise DivisionError(1, "division_packed_bytes_3d")
-        pk = packed[i] if packed is not None else _memory(stream, x.device)(torch.empty, need, dtype=torch.uint8, device=x.device)
-        made.append(pk)
-        descs[i] = _MapDesc(x.data_ptr(), pk.data_ptr(), None, pk.numel() * pk.element_size(), N, C, D, H, W,
-                            _dt(x.dtype, use16), Bs[i], bs[i], seeds[i] & (2 ** 64 - 1))
+    if packed is not None:
+        made = [packed[i] for i in range(n)]
+    else:
+        made = _memory(stream, xs[0].device)(lambda: [torch.empty(m, dtype=torch.uint8, device=x.device) for m, x in zip(need, xs)]) if n else []
+    for i, (x, pk) in enumerate(zip(xs, made)):
+        descs[i] = _MapDesc(x.data_ptr(), pk.data_ptr(), None, pk.numel() * pk.element_size(), *shapes[i],
+                            _dt(x.dtype, c16 and x.dtype == torch.float32), Bs[i], bs[i], seeds[i] & (2 ** 64 - 1))
     rc = lib().division_compress_maps(n, descs, _stream(stream))
     if rc:
         raise DivisionError(rc, "division_compress_maps")
@@ -381,14 +393,14 @@ def division_decompress_maps(packed, shapes, B, b, dtypes=torch.float32, out=Non
     if len(shapes) != n or len(Bs) != n or len(bs) != n or len(dts) != n:
         raise ValueError("one shape (and block size, code width, dtype) per map")
     descs = (_MapDesc * max(n, 1))()
-    made = []
-    for i, pk in enumerate(packed):
-        N, C, D, H, W = _dims5(shapes[i])
-        use16 = c16 and dts[i] == torch.float32
-        y = out[i] if out is not None else _memory(stream, pk.device)(torch.empty, tuple(shapes[i]), dtype=dts[i], device=pk.device)
-        made.append(y)
-        descs[i] = _MapDesc(None, pk.data_ptr(), y.data_ptr(), pk.numel() * pk.element_size(), N, C, D, H, W,
-                            _dt(dts[i], use16), Bs[i], bs[i], 0)
+    dims = [_dims5(s) for s in shapes]
+    if out is not None:
+        made = [out[i] for i in range(n)]
+    else:
+        made = _memory(stream, packed[0].device)(lambda: [torch.empty(tuple(s), dtype=t, device=pk.device) for s, t, pk in zip(shapes, dts, packed)]) if n else []
+    for i, (pk, y) in enumerate(zip(packed, made)):
+        descs[i] = _MapDesc(None, pk.data_ptr(), y.data_ptr(), pk.numel() * pk.element_size(), *dims[i],
+                            _dt(dts[i], c16 and dts[i] == torch.float32), Bs[i], bs[i], 0)
     rc = lib().division_decompress_maps(n, descs, _stream(stream))
     if rc:
         raise DivisionError(rc, "division_decompress_maps")
@@ -417,8 +429,7 @@ def division_compress_batch(xs, B: int, b: int, seeds, packed=None, stream=None,
     if need == 0:
         raise DivisionError(1, "division_packed_bytes")
     if packed is None:
-        make = _memory(stream, x0.device)
-        packed = [make(torch.empty, need, dtype=torch.uint8, device=x0.device) for _ in xs]
+        packed = _memory(stream, x0.device)(lambda: [torch.empty(need, dtype=torch.uint8, device=x0.device) for _ in xs])
     packed = list(packed)
     if len(packed) != len(xs):
         raise ValueError("one packed buffer per tensor")
@@ -439,8 +450,7 @@ def division_decompress_batch(packed, shape, B: int, b: int, dtype=torch.float32
         return []
     N, C, H, W = shape
     if out is None:
-        make = _memory(stream, packed[0].device)
-        out = [make(torch.empty, shape, dtype=dtype, device=packed[0].device) for _ in packed]
+        out = _memory(stream, packed[0].device)(lambda: [torch.empty(shape, dtype=dtype, device=packed[0].device) for _ in packed])
     out = list(out)
     if len(out) != len(packed):
         raise ValueError("one output per packed buffer")

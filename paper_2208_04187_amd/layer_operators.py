@@ -74,7 +74,7 @@ class _Call:
         return self.make(torch.empty, shape, dtype=dtype, device=self.device)
 
     def workspace(self, nbytes: int):
-        return self.new((max(int(nbytes), 1),), torch.uint8)
+        return self.make(torch.empty, max(int(nbytes), 1), dtype=torch.uint8, device=self.device, given=False)
 
     def launch(self, entry, *args):
         if self.device.index == torch.cuda.current_device():

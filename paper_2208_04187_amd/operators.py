@@ -124,7 +124,7 @@ def _written(*tensors):
 
 def _workspace(nbytes: int, device, make):
     """Memory for one call, of the stream that it runs on: torch hands it out again, behind this call, when the call's tensors are gone."""
-    return make(torch.empty, max(int(nbytes), 1), dtype=torch.uint8, device=device)
+    return make(torch.empty, max(int(nbytes), 1), dtype=torch.uint8, device=device, given=False)
 
 
 def _group_count(D: int, group: int) -> int:
