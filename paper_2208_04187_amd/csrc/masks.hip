@@ -16,29 +16,11 @@
 
 namespace {
 #include "fastdiv.h"
+#include "dropout_words.h"
 
 constexpr int kThreads = 256;
 constexpr int kVecPerThread = 4;                  // 16-byte vectors a thread handles, kThreads apart
-constexpr uint32_t kWeyl = 0x9E3779B9u;
-constexpr uint64_t kDropoutStream = 0xD509A5B3C2E1F047ull;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-// 32-bit xorshift-multiply finaliser (shifts 16/15/16): the codec's random source
-__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
-    x ^= x >> 16; x *= 0x7feb352du;
-    x ^= x >> 15; x *= 0x846ca68bu;
-    x ^= x >> 16;
-    return x;
-}
-
-// random word of element pair j of a stream segment with keys (k1, k2)
-__device__ __forceinline__ uint32_t pair_word(uint32_t k1, uint32_t k2, uint32_t j) {
-    uint32_t x = k1 + j * kWeyl;
-    x ^= x >> 16; x *= 0x7feb352du;
-    x = x ^ (x >> 15) ^ k2; x *= 0x846ca68bu;
-    x ^= x >> 16;
-    return x;
-}
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_u32(uint32_t v) {
